@@ -347,6 +347,177 @@ int normpre_profile_read(normpre_handle* h, int n_classes, double* ms, int64_t* 
 int normpre_normalize_cols_noalloc(int64_t rows, int64_t cols, float mu, const void* G, int g_dtype,
                                    float* M, const void* W, int w_dtype, float* Psi, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Training operators around the step: the attention between a decoder layer's
+ * projections, and 8-bit checkpoints of the activations that the layer's
+ * backward pass reads.  Their backward passes produce the gradients G that
+ * normpre_step takes.  (No counterpart in the paper, which trains decoder-only
+ * models and says nothing of how their gradients are computed.)
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * Causal softmax attention over a pack of sequences, with grouped key / value
+ * heads.  Sequence s occupies n_s consecutive rows (tokens) of every tensor,
+ * after the rows of the sequences before it.  For a row i of a sequence and
+ * query head h, with key / value head h / (n_heads / n_kv_heads), c = scale
+ * and j over the sequence's rows up to and including i:
+ *   s_ij = c <q_i, k_j>        lse_i = ln sum_j exp(s_ij)
+ *   p_ij = exp(s_ij - lse_i)   o_i   = sum_j p_ij v_j
+ * and backward, with delta_i = <do_i, o_i>:
+ *   ds_ij = p_ij (<do_i, v_j> - delta_i)
+ *   dq_i = c sum_j ds_ij k_j
+ *   dk_j = c sum_i ds_ij q_i   dv_j = sum_i p_ij do_i   (i also over the query
+ *                                                        heads of the group)
+ * Rows that belong to no sequence (from sum n_s to `tokens`) get o = 0,
+ * lse = -inf and zero gradients, whatever their inputs hold; what a row of
+ * another sequence holds never reaches a sequence.  Within a sequence a
+ * non-finite value of token j reaches, besides the rows i >= j that see it,
+ * the rows of j's aligned block of 128 rows (0 * NaN in the tile products).
+ */
+typedef struct normpre_attn normpre_attn;
+
+typedef struct normpre_attn_config {
+  int n_heads;         /* query heads, >= 1 */
+  int n_kv_heads;      /* key / value heads, a divisor of n_heads */
+  int head_dim;        /* a multiple of 8, in [8, 128] */
+  int max_seqs;        /* most sequences of one pack, in [1, 65536] */
+  int64_t max_tokens;  /* most rows of one call, in [1, 2^24] */
+  int dtype;           /* normpre_dtype of Q, K, V, O and the gradients.  BF16: products on the tensor
+                          cores, bf16 operands (the probabilities and ds rounded to bf16 once each) with
+                          fp32 accumulation; softmax statistics in fp32.  F32: everything in fp32 */
+  float scale;         /* c, finite and > 0; 0 selects 1 / sqrt(head_dim) */
+} normpre_attn_config;
+
+/* One [tokens][heads][head_dim] tensor on the device; the last dimension is
+ * contiguous.  Strides in elements, each a multiple of 16 bytes and at least
+ * head_dim; an output's rows must not overlap.  Slices of a fused projection
+ * fit as they are. */
+typedef struct normpre_heads {
+  void* data;            /* 16-byte aligned */
+  int64_t token_stride;  /* from row to row */
+  int64_t head_stride;   /* from head to head */
+} normpre_heads;
+
+/*
+ * Creates a plan for the heads and the largest pack in `cfg`; it holds the
+ * work lists of the current lengths and the backward pass's workspace
+ * (n_heads * max_tokens floats).  No sequences until normpre_attn_set_lengths.
+ * Errors (message from normpre_last_error(NULL), as for every normpre_attn_*
+ * call): ARG, SHAPE, DTYPE, CUDA.
+ */
+int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out);
+
+/*
+ * The lengths of the next pack: lengths[s] >= 0 rows for sequence s (host
+ * array; zero-length sequences are allowed, n_seqs = 0 is an empty pack).
+ * Work lists are rebuilt on the host and copied on `stream`, so calls queued
+ * on that stream before it still use the old lengths; once per batch, not per
+ * layer.  Not for use during stream capture.
+ * Errors: ARG, SHAPE (more than the plan's max_seqs / max_tokens), CUDA.
+ */
+int normpre_attn_set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, void* stream);
+
+/*
+ * Forward pass over `tokens` rows (sum of lengths <= tokens <= max_tokens).
+ *   out  written in full.
+ *   lse  device fp32 [n_heads][tokens], written in full; natural logarithm.
+ * Asynchronous on `stream`; allocates nothing.
+ * Errors: ARG, SHAPE, ALIGN, CUDA.
+ */
+int normpre_attn_forward(normpre_attn* a, int64_t tokens, const normpre_heads* q, const normpre_heads* k,
+                         const normpre_heads* v, const normpre_heads* out, float* lse, void* stream);
+
+/*
+ * Backward pass: dq, dk, dv are written in full from the forward pass's
+ * tensors and dout.  Sums run in a fixed order: the same inputs give the same
+ * bits.  The plan's workspace is used, so two backward passes of one plan must
+ * not run concurrently.  Asynchronous on `stream`; allocates nothing.
+ * Errors: ARG, SHAPE, ALIGN, CUDA.
+ */
+int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* q, const normpre_heads* k,
+                          const normpre_heads* v, const normpre_heads* out, const float* lse,
+                          const normpre_heads* dout, const normpre_heads* dq, const normpre_heads* dk,
+                          const normpre_heads* dv, void* stream);
+
+/* Synchronizes `stream`, then reports and clears the plan's device flag:
+ * TIMEOUT if a bounded wait gave up since the last call, else OK. */
+int normpre_attn_sync_status(normpre_attn* a, void* stream);
+
+/* Synchronizes the plan's device and releases the plan.  NULL is ignored. */
+void normpre_attn_free(normpre_attn* a);
+
+/*
+ * Checkpoints: a row-major matrix of activations x (tokens x features) kept as
+ * 8-bit integers with one power-of-two step per block of 32 consecutive
+ * elements of a row (the last block of a row may be shorter).  With
+ * e = the least integer >= -126 such that max |x| <= 127 * 2^e over the block,
+ *   code = x * 2^-e rounded to the nearest integer, ties to even
+ *   xhat = code * 2^e,   |xhat - x| <= 2^(e-1)
+ * A code has at most seven bits and a sign, so xhat is exactly a bf16 and an
+ * fp32 number: reading a checkpoint rounds nothing.  A block that holds a NaN
+ * or an infinity is marked and restores to NaN as a whole.
+ *
+ * Storage (device, caller-owned, 16-byte aligned):
+ *   codes  int8 [tokens][ld], ld = features rounded up to 32 (padding zero)
+ *   steps  uint8 [ceil(features / 128)][tokens][4]: byte b of panel p and row t
+ *          is e + 127 of the block of elements 128 p + 32 b ..; 255 marks a
+ *          non-finite block.  Blocks past the row's end hold 1.
+ * normpre_ckpt_bytes gives both sizes.  Values are fp32 or bf16 (normpre_dtype)
+ * with a row stride `ld` in elements, at least `features`.
+ * Calls are asynchronous on `stream`, on the current device, and allocate
+ * nothing.  Errors (message from normpre_last_error(NULL)): ARG, SHAPE
+ * (tokens in [0, 2^31), features in [1, 2^20]), DTYPE, ALIGN, CUDA.
+ */
+int normpre_ckpt_bytes(int64_t tokens, int64_t features, int64_t* codes_bytes, int64_t* steps_bytes);
+
+int normpre_ckpt_pack(int64_t tokens, int64_t features, const void* x, int x_dtype, int64_t x_ld, void* codes,
+                      void* steps, void* stream);
+
+/* xhat, in y's dtype. */
+int normpre_ckpt_restore(int64_t tokens, int64_t features, const void* codes, const void* steps, void* y,
+                         int y_dtype, int64_t y_ld, void* stream);
+
+/*
+ * Weight gradient of a linear layer y = x W^T from its input's checkpoint:
+ *   dW (out_features x features) = dY^T xhat, or dW + dY^T xhat with
+ *   accumulate = 1 (gradients of several micro-batches),
+ * fp32 sums over the tokens, rounded once to dW's dtype.  dy: device, tokens x
+ * out_features, row stride dy_ld; dw: device, row stride dw_ld.  bf16 dY with
+ * rows on 16-byte boundaries runs on the tensor cores; fp32 dY, and rows off
+ * those boundaries, on an fp32 kernel.  The sums' order is fixed.
+ * Out_features in [1, 2^20].  A device-side timeout is reported by
+ * normpre_ckpt_sync_status.
+ */
+int normpre_ckpt_wgrad(int64_t tokens, int64_t out_features, int64_t features, const void* dy, int dy_dtype,
+                       int64_t dy_ld, const void* codes, const void* steps, void* dw, int dw_dtype, int64_t dw_ld,
+                       int accumulate, void* stream);
+
+/*
+ * Gated activation h = silu(gate) * up, silu(g) = g / (1 + exp(-g)), from the
+ * values themselves, with checkpoints of gate and up written in the same pass.
+ * gate, up and h share one dtype (fp32 arithmetic, h rounded once).
+ */
+int normpre_ckpt_swiglu(int64_t tokens, int64_t features, int dtype, const void* gate, int64_t gate_ld,
+                        const void* up, int64_t up_ld, void* h, int64_t h_ld, void* gate_codes, void* gate_steps,
+                        void* up_codes, void* up_steps, void* stream);
+
+/*
+ * Its backward pass from the checkpoints, with g, u the restored values and
+ * s = 1 / (1 + exp(-g)):
+ *   dgate = dh u s (1 + g (1 - s)),   dup = dh g s
+ */
+int normpre_ckpt_swiglu_backward(int64_t tokens, int64_t features, int dtype, const void* gate_codes,
+                                 const void* gate_steps, const void* up_codes, const void* up_steps, const void* dh,
+                                 int64_t dh_ld, void* dgate, int64_t dgate_ld, void* dup, int64_t dup_ld,
+                                 void* stream);
+
+/* Synchronizes `stream`, then reports and clears the current device's flag of
+ * the checkpoint kernels: TIMEOUT if a bounded wait gave up since the last
+ * call, else OK. */
+int normpre_ckpt_sync_status(void* stream);
+
 /* Releases the handle made by normpre_init and every device buffer it owns
  * (the caller's W, G and M, which carry the optimizer's state across the steps
  * of Algorithm 1, are untouched).  NULL is ignored. */

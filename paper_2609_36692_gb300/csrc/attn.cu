@@ -1,0 +1,241 @@
+// Packed causal attention: plan, argument checks and launches of the
+// normpre_attn_* entry points.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <memory>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "../../include/normpre.h"
+#include "attn.h"
+#include "internal.h"
+
+using namespace normpre;
+
+struct normpre_attn {
+  normpre_attn_config cfg;
+  int device = 0;
+  int64_t max_blocks = 0;
+  int n_blocks = 0;
+  int64_t total = 0;
+  void* lists = nullptr;       // two AttnBlock[max_blocks]
+  float* delta = nullptr;      // [n_heads][max_tokens]
+  int* flags = nullptr;
+  std::vector<AttnBlock> host; // staging of `lists`
+};
+
+namespace {
+
+int fail(int code, const std::string& msg) {
+  set_thread_error(msg);
+  return code;
+}
+int cuda_fail(cudaError_t e, const char* what) {
+  return fail(NORMPRE_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+}
+
+void release(normpre_attn* a) {
+  cudaFree(a->lists);
+  cudaFree(a->delta);
+  cudaFree(a->flags);
+  delete a;
+}
+struct Release {
+  void operator()(normpre_attn* a) const { release(a); }
+};
+
+// Checks one tensor argument and copies it; a stride that no address uses (a
+// single row or head) is replaced by a valid one.
+int take(const normpre_attn* a, const normpre_heads* t, int64_t tokens, int heads, const char* name, bool output,
+         AttnTensor* out) {
+  if (!t || !t->data) return fail(NORMPRE_ERR_ARG, std::string(name) + ": null");
+  const int64_t d = a->cfg.head_dim, per16 = a->cfg.dtype == NORMPRE_BF16 ? 8 : 4;
+  int64_t ts = tokens > 1 ? t->token_stride : 0, hs = heads > 1 ? t->head_stride : 0;
+  if (tokens > 1 && (ts < d || ts > (int64_t(1) << 30)))
+    return fail(NORMPRE_ERR_SHAPE, std::string(name) + ": token stride must be in [head_dim, 2^30]");
+  if (heads > 1 && (hs < d || hs > (int64_t(1) << 36)))
+    return fail(NORMPRE_ERR_SHAPE, std::string(name) + ": head stride must be in [head_dim, 2^36]");
+  if ((reinterpret_cast<uintptr_t>(t->data) & 15u) || ts % per16 || hs % per16)
+    return fail(NORMPRE_ERR_ALIGN, std::string(name) + ": data and strides must be multiples of 16 bytes");
+  if (output && tokens > 1 && heads > 1) {
+    const bool by_token = ts >= hs;   // rows outermost, or heads
+    const int64_t inner = by_token ? (heads - 1) * hs + d : (tokens - 1) * ts + d;
+    if ((by_token ? ts : hs) < inner) return fail(NORMPRE_ERR_SHAPE, std::string(name) + ": overlapping strides");
+  }
+  if (!ts) ts = round_up(d, 8);
+  if (!hs) hs = round_up(d, 8);
+  *out = AttnTensor{t->data, ts, hs};
+  return NORMPRE_OK;
+}
+
+AttnArgs base_args(const normpre_attn* a, int64_t tokens) {
+  AttnArgs g = {};
+  const AttnBlock* lists = static_cast<const AttnBlock*>(a->lists);
+  g.by_query = lists;
+  g.by_key = lists + a->max_blocks;
+  g.n_blocks = a->n_blocks;
+  g.total = static_cast<int>(a->total);
+  g.tokens = static_cast<int>(tokens);
+  g.heads = a->cfg.n_heads;
+  g.kv_heads = a->cfg.n_kv_heads;
+  g.group = a->cfg.n_heads / a->cfg.n_kv_heads;
+  g.dim = a->cfg.head_dim;
+  g.scale = a->cfg.scale;
+  g.scale_log2 = a->cfg.scale * 1.4426950408889634f;
+  g.delta = a->delta;
+  g.flags = a->flags;
+  return g;
+}
+
+int check_tokens(const normpre_attn* a, int64_t tokens) {
+  if (tokens < a->total || tokens > a->cfg.max_tokens)
+    return fail(NORMPRE_ERR_SHAPE, "tokens must be between the sum of the lengths and max_tokens");
+  return NORMPRE_OK;
+}
+
+int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_t s) {
+  int64_t total = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    if (lengths[i] < 0) return fail(NORMPRE_ERR_ARG, "lengths[" + std::to_string(i) + "] is negative");
+    if (lengths[i] > a->cfg.max_tokens - total) return fail(NORMPRE_ERR_SHAPE, "the lengths exceed max_tokens");
+    total += lengths[i];
+  }
+  std::vector<AttnBlock> blocks;
+  int64_t start = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    for (int64_t b = 0; b * 128 < lengths[i]; ++b)
+      blocks.push_back(AttnBlock{static_cast<int>(start), static_cast<int>(lengths[i]), static_cast<int>(b), 0});
+    start += lengths[i];
+  }
+  const size_t n = blocks.size();
+  // longest work first: the last CTAs to start then have little to do
+  auto keys = [](const AttnBlock& b) { return b.blk; };
+  auto queries = [](const AttnBlock& b) { return (b.len - 1) / 128 - b.blk; };
+  std::stable_sort(blocks.begin(), blocks.end(),
+                   [&](const AttnBlock& x, const AttnBlock& y) { return keys(x) > keys(y); });
+  std::copy(blocks.begin(), blocks.end(), a->host.begin());
+  std::stable_sort(blocks.begin(), blocks.end(),
+                   [&](const AttnBlock& x, const AttnBlock& y) { return queries(x) > queries(y); });
+  std::copy(blocks.begin(), blocks.end(), a->host.begin() + a->max_blocks);
+  // pageable source: the runtime has taken its copy when the calls return
+  AttnBlock* dev = static_cast<AttnBlock*>(a->lists);
+  if (n) {
+    cudaError_t e = cudaMemcpyAsync(dev, a->host.data(), n * sizeof(AttnBlock), cudaMemcpyHostToDevice, s);
+    if (!e) e = cudaMemcpyAsync(dev + a->max_blocks, a->host.data() + a->max_blocks, n * sizeof(AttnBlock),
+                                cudaMemcpyHostToDevice, s);
+    if (e) return cuda_fail(e, "cudaMemcpyAsync");
+  }
+  a->n_blocks = static_cast<int>(n);
+  a->total = total;
+  return NORMPRE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out) {
+  if (!cfg || !out) return fail(NORMPRE_ERR_ARG, "null argument");
+  *out = nullptr;
+  if (cfg->dtype != NORMPRE_F32 && cfg->dtype != NORMPRE_BF16)
+    return fail(NORMPRE_ERR_DTYPE, "dtype must be NORMPRE_F32 or NORMPRE_BF16");
+  if (cfg->n_heads < 1 || cfg->n_kv_heads < 1 || cfg->n_heads > 65535 || cfg->n_heads % cfg->n_kv_heads)
+    return fail(NORMPRE_ERR_SHAPE, "n_heads must be in [1, 65535] and a multiple of n_kv_heads");
+  if (cfg->head_dim < 8 || cfg->head_dim > 128 || cfg->head_dim % 8)
+    return fail(NORMPRE_ERR_SHAPE, "head_dim must be a multiple of 8 in [8, 128]");
+  if (cfg->max_tokens < 1 || cfg->max_tokens > (int64_t(1) << 24) || cfg->max_seqs < 1 || cfg->max_seqs > 65536)
+    return fail(NORMPRE_ERR_SHAPE, "max_tokens must be in [1, 2^24] and max_seqs in [1, 65536]");
+  if (!std::isfinite(cfg->scale) || cfg->scale < 0.f) return fail(NORMPRE_ERR_ARG, "scale must be finite and >= 0");
+  try {
+    std::unique_ptr<normpre_attn, Release> a(new normpre_attn());
+    a->cfg = *cfg;
+    if (a->cfg.scale == 0.f) a->cfg.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(cfg->head_dim)));
+    a->max_blocks = cfg->max_tokens / 128 + std::min<int64_t>(cfg->max_seqs, cfg->max_tokens);
+    a->host.resize(2 * a->max_blocks);
+    cudaError_t e = cudaGetDevice(&a->device);
+    if (!e) e = cudaMalloc(&a->lists, 2 * a->max_blocks * sizeof(AttnBlock));
+    if (!e) e = cudaMalloc(&a->delta, static_cast<size_t>(cfg->n_heads) * cfg->max_tokens * sizeof(float));
+    if (!e) e = cudaMalloc(&a->flags, sizeof(int));
+    if (!e) e = cudaMemset(a->flags, 0, sizeof(int));
+    if (e) return cuda_fail(e, "normpre_attn_init");
+    *out = a.release();
+  } catch (const std::bad_alloc&) {
+    return fail(NORMPRE_ERR_CUDA, "out of host memory");
+  }
+  return NORMPRE_OK;
+}
+
+int normpre_attn_set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, void* stream) {
+  if (!a || (n_seqs > 0 && !lengths)) return fail(NORMPRE_ERR_ARG, "null argument");
+  if (n_seqs < 0) return fail(NORMPRE_ERR_ARG, "n_seqs is negative");
+  if (n_seqs > a->cfg.max_seqs) return fail(NORMPRE_ERR_SHAPE, "more sequences than max_seqs");
+  DeviceGuard device_guard(a->device);
+  try {
+    return set_lengths(a, n_seqs, lengths, static_cast<cudaStream_t>(stream));
+  } catch (const std::bad_alloc&) {
+    return fail(NORMPRE_ERR_CUDA, "out of host memory");
+  }
+}
+
+int normpre_attn_forward(normpre_attn* a, int64_t tokens, const normpre_heads* q, const normpre_heads* k,
+                         const normpre_heads* v, const normpre_heads* out, float* lse, void* stream) {
+  if (!a) return fail(NORMPRE_ERR_ARG, "null plan");
+  int rc = check_tokens(a, tokens);
+  if (rc || !tokens) return rc;
+  AttnArgs g = base_args(a, tokens);
+  const int h = a->cfg.n_heads, hk = a->cfg.n_kv_heads;
+  if ((rc = take(a, q, tokens, h, "q", false, &g.q)) || (rc = take(a, k, tokens, hk, "k", false, &g.k)) ||
+      (rc = take(a, v, tokens, hk, "v", false, &g.v)) || (rc = take(a, out, tokens, h, "out", true, &g.o)))
+    return rc;
+  if (!lse) return fail(NORMPRE_ERR_ARG, "lse: null");
+  g.lse = lse;
+  DeviceGuard device_guard(a->device);
+  const cudaError_t e = launch_attn_forward_simt(g, a->cfg.dtype, static_cast<cudaStream_t>(stream));
+  return e ? cuda_fail(e, "attention forward") : NORMPRE_OK;
+}
+
+int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* q, const normpre_heads* k,
+                          const normpre_heads* v, const normpre_heads* out, const float* lse,
+                          const normpre_heads* dout, const normpre_heads* dq, const normpre_heads* dk,
+                          const normpre_heads* dv, void* stream) {
+  if (!a) return fail(NORMPRE_ERR_ARG, "null plan");
+  int rc = check_tokens(a, tokens);
+  if (rc || !tokens) return rc;
+  AttnArgs g = base_args(a, tokens);
+  const int h = a->cfg.n_heads, hk = a->cfg.n_kv_heads;
+  if ((rc = take(a, q, tokens, h, "q", false, &g.q)) || (rc = take(a, k, tokens, hk, "k", false, &g.k)) ||
+      (rc = take(a, v, tokens, hk, "v", false, &g.v)) || (rc = take(a, out, tokens, h, "out", false, &g.o)) ||
+      (rc = take(a, dout, tokens, h, "dout", false, &g.dout)) || (rc = take(a, dq, tokens, h, "dq", true, &g.dq)) ||
+      (rc = take(a, dk, tokens, hk, "dk", true, &g.dk)) || (rc = take(a, dv, tokens, hk, "dv", true, &g.dv)))
+    return rc;
+  if (!lse) return fail(NORMPRE_ERR_ARG, "lse: null");
+  g.lse = const_cast<float*>(lse);
+  DeviceGuard device_guard(a->device);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = launch_attn_delta(g, a->cfg.dtype, s);
+  if (!e) e = launch_attn_backward_simt(g, a->cfg.dtype, s);
+  return e ? cuda_fail(e, "attention backward") : NORMPRE_OK;
+}
+
+int normpre_attn_sync_status(normpre_attn* a, void* stream) {
+  if (!a) return fail(NORMPRE_ERR_ARG, "null plan");
+  DeviceGuard device_guard(a->device);
+  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+  int flags = 0;
+  if (!e) e = cudaMemcpy(&flags, a->flags, sizeof(int), cudaMemcpyDeviceToHost);
+  if (!e && flags) e = cudaMemset(a->flags, 0, sizeof(int));
+  if (e) return cuda_fail(e, "normpre_attn_sync_status");
+  return flags & kFlagTimeout ? fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait gave up") : NORMPRE_OK;
+}
+
+void normpre_attn_free(normpre_attn* a) {
+  if (!a) return;
+  DeviceGuard device_guard(a->device);
+  cudaDeviceSynchronize();
+  release(a);
+}
+
+}  // extern "C"

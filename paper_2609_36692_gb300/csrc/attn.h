@@ -1,0 +1,45 @@
+// Packed causal attention: what the host side (attn.cu) and the kernels share.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace normpre {
+
+// 128 rows of one sequence: rows start + 128 blk .. of the pack, of which the
+// sequence holds min(128, len - 128 blk).
+struct AttnBlock {
+  int start;   // the sequence's first row
+  int len;     // the sequence's rows
+  int blk;     // index of the block in the sequence
+  int pad;
+};
+
+// A [tokens][heads][head_dim] tensor, strides in elements.
+struct AttnTensor {
+  void* p;
+  int64_t ts, hs;
+};
+
+struct AttnArgs {
+  AttnTensor q, k, v, o, dout, dq, dk, dv;
+  float* lse;                // [heads][tokens]
+  float* delta;              // [heads][tokens] <do_i, o_i>
+  const AttnBlock* by_query; // blocks, the ones that see the most keys first
+  const AttnBlock* by_key;   // blocks, the ones seen by the most queries first
+  int n_blocks;
+  int total;                 // rows that belong to sequences
+  int tokens;
+  int heads, kv_heads, group, dim;
+  float scale;               // c
+  float scale_log2;          // c log2(e): exp(c x) = exp2(scale_log2 x)
+  int* flags;
+};
+
+// Plain kernels, one CTA per 64 rows and head (attn_simt.cu).
+cudaError_t launch_attn_forward_simt(const AttnArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_attn_backward_simt(const AttnArgs& a, int dtype, cudaStream_t s);
+// delta_i = <do_i, o_i>; zero for rows outside the sequences.
+cudaError_t launch_attn_delta(const AttnArgs& a, int dtype, cudaStream_t s);
+
+}  // namespace normpre

@@ -1,0 +1,422 @@
+// 8-bit activation checkpoints: pack, restore and the gated activation that
+// writes and reads them, with the normpre_ckpt_* entry points.
+//
+// All of these stream: each value is read once and each result written once.
+// A CTA takes 128 features (a panel) of 64 rows; 8 lanes share a row, 16
+// features each, so that a warp reads and writes whole 32-byte sectors of 4
+// rows, the maximum of a 32-element block needs one shuffle, and the steps of
+// consecutive rows (one 32-bit word per row and panel) leave in whole sectors.
+// Bound by HBM.
+#include <atomic>
+#include <string>
+
+#include "../../include/normpre.h"
+#include "ckpt.h"
+#include "common.cuh"
+#include "internal.h"
+
+namespace normpre {
+namespace {
+
+constexpr int kRows = 64;        // rows of a CTA
+constexpr int kThreads = 256;
+
+// 16 consecutive elements; `n` of them exist.
+template <bool VEC, typename T>
+__device__ __forceinline__ void load16(const T* p, int n, float (&v)[16]) {
+  if (VEC && n >= 16) {
+    load8(p, v);
+    load8(p + 8, v + 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
+  }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store16(T* p, int n, const float (&v)[16]) {
+  if (VEC && n >= 16) {
+    store8(p, v);
+    store8(p + 8, v + 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i < n) p[i] = from_f32<T>(v[i]);
+  }
+}
+
+// Rounds a lane's 16 elements of a row to codes and returns the row's step
+// word of the panel in the first of its 8 lanes.  The step exponent e is the
+// least with max |x| <= 127 * 2^e: with 2^f <= max < 2^(f+1), f - 6 if the
+// significand is at most 127/64, else f - 5.
+__device__ __forceinline__ uint32_t encode16(const float (&v)[16], uint4& codes) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  const bool finite = top < 0x7F800000u;
+  const int byte = finite ? max(1, static_cast<int>(top >> 23) - 6 + ((top & 0x7FFFFFu) > 0x7E0000u ? 1 : 0)) : 255;
+  const float inv = __uint_as_float(static_cast<uint32_t>(254 - byte) << 23);   // 2^-e
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = static_cast<uint32_t>(__float2int_rn(v[4 * i + j] * inv)) & 0xFFu;
+    w[i] = finite ? b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24) : 0u;
+  }
+  codes = make_uint4(w[0], w[1], w[2], w[3]);
+  // lanes 0, 2, 4, 6 of the row hold its four blocks
+  uint32_t word = static_cast<uint32_t>(byte);
+  word |= __shfl_down_sync(0xffffffffu, word, 2) << 8;
+  word |= __shfl_down_sync(0xffffffffu, word, 4) << 16;
+  return word;
+}
+
+__device__ __forceinline__ void decode16(const uint4& codes, float step, float (&v)[16]) {
+  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = static_cast<float>(static_cast<int8_t>(w[i >> 2] >> (8 * (i & 3)))) * step;
+}
+
+// A lane's place: row of the CTA's pass, feature, and what exists there.
+struct Place {
+  int64_t row;
+  int64_t feature;
+  int64_t word;   // index of the row's step word of the panel
+  int n;          // elements of the lane's 16 that exist
+  bool codes;     // the lane's codes (padding included) exist
+};
+__device__ __forceinline__ Place place(int64_t tokens, int64_t features, int64_t ld, int pass) {
+  Place p;
+  const unsigned panels = static_cast<unsigned>((features + kCkptPanel - 1) / kCkptPanel);
+  const unsigned range = blockIdx.x / panels, panel = blockIdx.x - range * panels;
+  p.row = static_cast<int64_t>(range) * kRows + pass * 32 + (threadIdx.x >> 3);
+  p.feature = static_cast<int64_t>(panel) * kCkptPanel + (threadIdx.x & 7) * 16;
+  p.word = panel * tokens + p.row;
+  const bool in = p.row < tokens;
+  p.codes = in && p.feature < ld;
+  p.n = in ? static_cast<int>(max(int64_t(0), min(int64_t(16), features - p.feature))) : 0;
+  return p;
+}
+
+struct PackArgs {
+  int64_t tokens, features, ld;
+  const void* x;
+  int64_t x_ld;
+  int8_t* codes;
+  uint32_t* steps;
+};
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_ckpt_pack(const __grid_constant__ PackArgs a) {
+#pragma unroll
+  for (int pass = 0; pass < kRows / 32; ++pass) {
+    const Place p = place(a.tokens, a.features, a.ld, pass);
+    float v[16];
+    load16<VEC>(static_cast<const T*>(a.x) + p.row * a.x_ld + p.feature, p.n, v);
+    uint4 codes;
+    const uint32_t word = encode16(v, codes);
+    if (p.codes) *reinterpret_cast<uint4*>(a.codes + p.row * a.ld + p.feature) = codes;
+    if ((threadIdx.x & 7) == 0 && p.row < a.tokens) a.steps[p.word] = word;
+  }
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_ckpt_restore(const __grid_constant__ PackArgs a, T* y) {
+#pragma unroll
+  for (int pass = 0; pass < kRows / 32; ++pass) {
+    const Place p = place(a.tokens, a.features, a.ld, pass);
+    if (!p.n) continue;
+    const uint4 codes = __ldg(reinterpret_cast<const uint4*>(a.codes + p.row * a.ld + p.feature));
+    const uint32_t word = __ldg(a.steps + p.word);
+    float v[16];
+    decode16(codes, ckpt_step(word, (threadIdx.x & 7) >> 1), v);
+    store16<VEC>(y + p.row * a.x_ld + p.feature, p.n, v);
+  }
+}
+
+struct SwigluArgs {
+  int64_t tokens, features, ld;
+  const void *gate, *up, *dh;
+  void *h, *dgate, *dup;
+  int64_t gate_ld, up_ld, h_ld, dgate_ld, dup_ld, dh_ld;
+  int8_t *gate_codes, *up_codes;
+  uint32_t *gate_steps, *up_steps;
+};
+
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_ckpt_swiglu(const __grid_constant__ SwigluArgs a) {
+#pragma unroll
+  for (int pass = 0; pass < kRows / 32; ++pass) {
+    const Place p = place(a.tokens, a.features, a.ld, pass);
+    float g[16], u[16];
+    load16<VEC>(static_cast<const T*>(a.gate) + p.row * a.gate_ld + p.feature, p.n, g);
+    load16<VEC>(static_cast<const T*>(a.up) + p.row * a.up_ld + p.feature, p.n, u);
+    uint4 gc, uc;
+    const uint32_t gw = encode16(g, gc), uw = encode16(u, uc);
+    if (p.codes) {
+      *reinterpret_cast<uint4*>(a.gate_codes + p.row * a.ld + p.feature) = gc;
+      *reinterpret_cast<uint4*>(a.up_codes + p.row * a.ld + p.feature) = uc;
+    }
+    if ((threadIdx.x & 7) == 0 && p.row < a.tokens) {
+      a.gate_steps[p.word] = gw;
+      a.up_steps[p.word] = uw;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u[i] *= g[i] * sigmoid(g[i]);
+    store16<VEC>(static_cast<T*>(a.h) + p.row * a.h_ld + p.feature, p.n, u);
+  }
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_ckpt_swiglu_bwd(const __grid_constant__ SwigluArgs a) {
+#pragma unroll
+  for (int pass = 0; pass < kRows / 32; ++pass) {
+    const Place p = place(a.tokens, a.features, a.ld, pass);
+    if (!p.n) continue;
+    const int block = (threadIdx.x & 7) >> 1;
+    const int64_t at = p.row * a.ld + p.feature;
+    float g[16], u[16], d[16];
+    load16<VEC>(static_cast<const T*>(a.dh) + p.row * a.dh_ld + p.feature, p.n, d);
+    decode16(__ldg(reinterpret_cast<const uint4*>(a.gate_codes + at)), ckpt_step(__ldg(a.gate_steps + p.word), block), g);
+    decode16(__ldg(reinterpret_cast<const uint4*>(a.up_codes + at)), ckpt_step(__ldg(a.up_steps + p.word), block), u);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float s = sigmoid(g[i]);
+      u[i] *= d[i] * s * fmaf(g[i], 1.f - s, 1.f);
+      g[i] *= d[i] * s;
+    }
+    store16<VEC>(static_cast<T*>(a.dgate) + p.row * a.dgate_ld + p.feature, p.n, u);
+    store16<VEC>(static_cast<T*>(a.dup) + p.row * a.dup_ld + p.feature, p.n, g);
+  }
+}
+
+__device__ int d_ckpt_flags;
+
+// The current device's flag word; its address is looked up once per device.
+cudaError_t ckpt_flags(int** out) {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<int*> known[kMaxDevices];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e) return e;
+  int* p = dev < kMaxDevices ? known[dev].load(std::memory_order_acquire) : nullptr;
+  if (!p) {
+    void* v = nullptr;
+    if ((e = cudaGetSymbolAddress(&v, d_ckpt_flags))) return e;
+    p = static_cast<int*>(v);
+    if (dev < kMaxDevices) known[dev].store(p, std::memory_order_release);
+  }
+  *out = p;
+  return cudaSuccess;
+}
+
+int fail(int code, const std::string& msg) {
+  set_thread_error(msg);
+  return code;
+}
+int done(cudaError_t e, const char* what) {
+  return e ? fail(NORMPRE_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e)) : NORMPRE_OK;
+}
+
+// One CTA per panel and kRows rows, the panels of a row range next to each other.
+int64_t panel_ctas(int64_t tokens, int64_t features) { return ckpt_panels(features) * cdiv(tokens, kRows); }
+
+int check_shape(int64_t tokens, int64_t features) {
+  if (tokens < 0 || tokens >= (int64_t(1) << 31) || features < 1 || features > (int64_t(1) << 20))
+    return fail(NORMPRE_ERR_SHAPE, "tokens must be in [0, 2^31) and features in [1, 2^20]");
+  if (panel_ctas(tokens, features) >= (int64_t(1) << 31)) return fail(NORMPRE_ERR_SHAPE, "the matrix is too large");
+  return NORMPRE_OK;
+}
+int check_dtype(int dtype, const char* name) {
+  if (dtype != NORMPRE_F32 && dtype != NORMPRE_BF16)
+    return fail(NORMPRE_ERR_DTYPE, std::string(name) + ": dtype must be NORMPRE_F32 or NORMPRE_BF16");
+  return NORMPRE_OK;
+}
+int check_ptr(const void* p, const char* name) {
+  if (!p) return fail(NORMPRE_ERR_ARG, std::string(name) + ": null");
+  if (reinterpret_cast<uintptr_t>(p) & 15u) return fail(NORMPRE_ERR_ALIGN, std::string(name) + " must be 16-byte aligned");
+  return NORMPRE_OK;
+}
+int check_matrix(const void* p, int64_t ld, int64_t cols, const char* name) {
+  if (ld < cols || ld > (int64_t(1) << 31))
+    return fail(NORMPRE_ERR_SHAPE, std::string(name) + ": the row stride must be in [columns, 2^31]");
+  return check_ptr(p, name);
+}
+// Rows on 16-byte boundaries: whole-vector accesses.
+bool vec_rows(int64_t ld, int dtype) { return ld % (dtype == NORMPRE_BF16 ? 8 : 4) == 0; }
+
+}  // namespace
+}  // namespace normpre
+
+using namespace normpre;
+
+#define CKPT_TRY(x)      \
+  do {                   \
+    const int rc_ = (x); \
+    if (rc_) return rc_; \
+  } while (0)
+
+// kernel<T, VEC> for a dtype and whether every row starts on 16 bytes
+#define CKPT_DISPATCH(kernel, dtype, vec, ...)                                   \
+  do {                                                                           \
+    if ((dtype) == NORMPRE_F32) {                                                \
+      if (vec) kernel<float, true> __VA_ARGS__; else kernel<float, false> __VA_ARGS__; \
+    } else {                                                                     \
+      if (vec) kernel<bf16, true> __VA_ARGS__; else kernel<bf16, false> __VA_ARGS__;   \
+    }                                                                            \
+  } while (0)
+
+extern "C" {
+
+int normpre_ckpt_bytes(int64_t tokens, int64_t features, int64_t* codes_bytes, int64_t* steps_bytes) {
+  CKPT_TRY(check_shape(tokens, features));
+  if (!codes_bytes || !steps_bytes) return fail(NORMPRE_ERR_ARG, "null argument");
+  *codes_bytes = tokens * ckpt_ld(features);
+  *steps_bytes = 4 * tokens * ckpt_panels(features);
+  return NORMPRE_OK;
+}
+
+int normpre_ckpt_pack(int64_t tokens, int64_t features, const void* x, int x_dtype, int64_t x_ld, void* codes,
+                      void* steps, void* stream) {
+  CKPT_TRY(check_shape(tokens, features));
+  CKPT_TRY(check_dtype(x_dtype, "x"));
+  if (!tokens) return NORMPRE_OK;
+  CKPT_TRY(check_matrix(x, x_ld, features, "x"));
+  CKPT_TRY(check_ptr(codes, "codes"));
+  CKPT_TRY(check_ptr(steps, "steps"));
+  PackArgs a = {tokens, features, ckpt_ld(features), x, x_ld, static_cast<int8_t*>(codes), static_cast<uint32_t*>(steps)};
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const unsigned grid = static_cast<unsigned>(panel_ctas(tokens, features));
+  CKPT_DISPATCH(k_ckpt_pack, x_dtype, vec_rows(x_ld, x_dtype), <<<grid, kThreads, 0, s>>>(a));
+  return done(cudaGetLastError(), "checkpoint pack");
+}
+
+int normpre_ckpt_restore(int64_t tokens, int64_t features, const void* codes, const void* steps, void* y,
+                         int y_dtype, int64_t y_ld, void* stream) {
+  CKPT_TRY(check_shape(tokens, features));
+  CKPT_TRY(check_dtype(y_dtype, "y"));
+  if (!tokens) return NORMPRE_OK;
+  CKPT_TRY(check_ptr(codes, "codes"));
+  CKPT_TRY(check_ptr(steps, "steps"));
+  CKPT_TRY(check_matrix(y, y_ld, features, "y"));
+  PackArgs a = {tokens, features, ckpt_ld(features), nullptr, y_ld,
+                const_cast<int8_t*>(static_cast<const int8_t*>(codes)),
+                const_cast<uint32_t*>(static_cast<const uint32_t*>(steps))};
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const unsigned grid = static_cast<unsigned>(panel_ctas(tokens, features));
+  const bool vec = vec_rows(y_ld, y_dtype);
+  if (y_dtype == NORMPRE_F32) {
+    if (vec) k_ckpt_restore<float, true><<<grid, kThreads, 0, s>>>(a, static_cast<float*>(y));
+    else k_ckpt_restore<float, false><<<grid, kThreads, 0, s>>>(a, static_cast<float*>(y));
+  } else {
+    if (vec) k_ckpt_restore<bf16, true><<<grid, kThreads, 0, s>>>(a, static_cast<bf16*>(y));
+    else k_ckpt_restore<bf16, false><<<grid, kThreads, 0, s>>>(a, static_cast<bf16*>(y));
+  }
+  return done(cudaGetLastError(), "checkpoint restore");
+}
+
+int normpre_ckpt_wgrad(int64_t tokens, int64_t out_features, int64_t features, const void* dy, int dy_dtype,
+                       int64_t dy_ld, const void* codes, const void* steps, void* dw, int dw_dtype, int64_t dw_ld,
+                       int accumulate, void* stream) {
+  CKPT_TRY(check_shape(tokens, features));
+  if (out_features < 1 || out_features > (int64_t(1) << 20))
+    return fail(NORMPRE_ERR_SHAPE, "out_features must be in [1, 2^20]");
+  CKPT_TRY(check_dtype(dy_dtype, "dy"));
+  CKPT_TRY(check_dtype(dw_dtype, "dw"));
+  if (accumulate != 0 && accumulate != 1) return fail(NORMPRE_ERR_ARG, "accumulate must be 0 or 1");
+  CKPT_TRY(check_matrix(dw, dw_ld, features, "dw"));
+  if (tokens) {
+    CKPT_TRY(check_matrix(dy, dy_ld, out_features, "dy"));
+    CKPT_TRY(check_ptr(codes, "codes"));
+    CKPT_TRY(check_ptr(steps, "steps"));
+  } else if (accumulate) {
+    return NORMPRE_OK;
+  }
+  WgradArgs a = {};
+  a.dy = dy;
+  a.dy_ld = dy_ld;
+  a.x = CkptView{static_cast<const int8_t*>(codes), static_cast<const uint32_t*>(steps)};
+  a.x_ld = ckpt_ld(features);
+  a.dw = dw;
+  a.dw_ld = dw_ld;
+  a.tokens = tokens;
+  a.n = static_cast<int>(out_features);
+  a.k = static_cast<int>(features);
+  a.accumulate = accumulate;
+  cudaError_t e = ckpt_flags(&a.flags);
+  if (!e) e = launch_ckpt_wgrad_simt(a, dy_dtype, dw_dtype, static_cast<cudaStream_t>(stream));
+  return done(e, "checkpoint weight gradient");
+}
+
+int normpre_ckpt_swiglu(int64_t tokens, int64_t features, int dtype, const void* gate, int64_t gate_ld,
+                        const void* up, int64_t up_ld, void* h, int64_t h_ld, void* gate_codes, void* gate_steps,
+                        void* up_codes, void* up_steps, void* stream) {
+  CKPT_TRY(check_shape(tokens, features));
+  CKPT_TRY(check_dtype(dtype, "gate, up and h"));
+  if (!tokens) return NORMPRE_OK;
+  CKPT_TRY(check_matrix(gate, gate_ld, features, "gate"));
+  CKPT_TRY(check_matrix(up, up_ld, features, "up"));
+  CKPT_TRY(check_matrix(h, h_ld, features, "h"));
+  CKPT_TRY(check_ptr(gate_codes, "gate_codes"));
+  CKPT_TRY(check_ptr(gate_steps, "gate_steps"));
+  CKPT_TRY(check_ptr(up_codes, "up_codes"));
+  CKPT_TRY(check_ptr(up_steps, "up_steps"));
+  SwigluArgs a = {};
+  a.tokens = tokens; a.features = features; a.ld = ckpt_ld(features);
+  a.gate = gate; a.gate_ld = gate_ld;
+  a.up = up; a.up_ld = up_ld;
+  a.h = h; a.h_ld = h_ld;
+  a.gate_codes = static_cast<int8_t*>(gate_codes); a.gate_steps = static_cast<uint32_t*>(gate_steps);
+  a.up_codes = static_cast<int8_t*>(up_codes); a.up_steps = static_cast<uint32_t*>(up_steps);
+  const bool vec = vec_rows(gate_ld, dtype) && vec_rows(up_ld, dtype) && vec_rows(h_ld, dtype);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const unsigned grid = static_cast<unsigned>(panel_ctas(tokens, features));
+  CKPT_DISPATCH(k_ckpt_swiglu, dtype, vec, <<<grid, kThreads, 0, s>>>(a));
+  return done(cudaGetLastError(), "checkpoint swiglu");
+}
+
+int normpre_ckpt_swiglu_backward(int64_t tokens, int64_t features, int dtype, const void* gate_codes,
+                                 const void* gate_steps, const void* up_codes, const void* up_steps, const void* dh,
+                                 int64_t dh_ld, void* dgate, int64_t dgate_ld, void* dup, int64_t dup_ld,
+                                 void* stream) {
+  CKPT_TRY(check_shape(tokens, features));
+  CKPT_TRY(check_dtype(dtype, "dh, dgate and dup"));
+  if (!tokens) return NORMPRE_OK;
+  CKPT_TRY(check_matrix(dh, dh_ld, features, "dh"));
+  CKPT_TRY(check_matrix(dgate, dgate_ld, features, "dgate"));
+  CKPT_TRY(check_matrix(dup, dup_ld, features, "dup"));
+  CKPT_TRY(check_ptr(gate_codes, "gate_codes"));
+  CKPT_TRY(check_ptr(gate_steps, "gate_steps"));
+  CKPT_TRY(check_ptr(up_codes, "up_codes"));
+  CKPT_TRY(check_ptr(up_steps, "up_steps"));
+  SwigluArgs a = {};
+  a.tokens = tokens; a.features = features; a.ld = ckpt_ld(features);
+  a.dh = dh; a.dh_ld = dh_ld;
+  a.dgate = dgate; a.dgate_ld = dgate_ld;
+  a.dup = dup; a.dup_ld = dup_ld;
+  a.gate_codes = const_cast<int8_t*>(static_cast<const int8_t*>(gate_codes));
+  a.gate_steps = const_cast<uint32_t*>(static_cast<const uint32_t*>(gate_steps));
+  a.up_codes = const_cast<int8_t*>(static_cast<const int8_t*>(up_codes));
+  a.up_steps = const_cast<uint32_t*>(static_cast<const uint32_t*>(up_steps));
+  const bool vec = vec_rows(dh_ld, dtype) && vec_rows(dgate_ld, dtype) && vec_rows(dup_ld, dtype);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const unsigned grid = static_cast<unsigned>(panel_ctas(tokens, features));
+  CKPT_DISPATCH(k_ckpt_swiglu_bwd, dtype, vec, <<<grid, kThreads, 0, s>>>(a));
+  return done(cudaGetLastError(), "checkpoint swiglu backward");
+}
+
+int normpre_ckpt_sync_status(void* stream) {
+  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+  int* flags = nullptr;
+  int v = 0;
+  if (!e) e = ckpt_flags(&flags);
+  if (!e) e = cudaMemcpy(&v, flags, sizeof(int), cudaMemcpyDeviceToHost);
+  if (!e && v) e = cudaMemset(flags, 0, sizeof(int));
+  if (e) return done(e, "normpre_ckpt_sync_status");
+  return v & kFlagTimeout ? fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait gave up") : NORMPRE_OK;
+}
+
+}  // extern "C"

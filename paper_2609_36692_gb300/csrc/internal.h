@@ -330,6 +330,24 @@ cudaError_t launch_contract_bf16(const ContractBf16Launch& c, cudaStream_t s);
 // Records the message returned by normpre_last_error(NULL) on this thread.
 void set_thread_error(const std::string& msg);
 
+// Makes the handle's device current for one entry point and gives the caller
+// its own current device back on the way out.
+class DeviceGuard {
+ public:
+  explicit DeviceGuard(int dev) {
+    if (cudaGetDevice(&prev_) == cudaSuccess && prev_ != dev) changed_ = cudaSetDevice(dev) == cudaSuccess;
+  }
+  ~DeviceGuard() {
+    if (changed_) cudaSetDevice(prev_);
+  }
+  DeviceGuard(const DeviceGuard&) = delete;
+  DeviceGuard& operator=(const DeviceGuard&) = delete;
+
+ private:
+  int prev_ = 0;
+  bool changed_ = false;
+};
+
 // Device properties cached per process.
 int device_sm_count();
 bool driver_encode_tiled(CUtensorMap* map, CUtensorMapDataType dt, uint32_t rank, void* addr,

@@ -189,24 +189,6 @@ const char* normpre_last_error(const normpre_handle* h) {
 
 namespace {
 
-// Makes the handle's device current for one entry point and gives the caller
-// its own current device back on the way out.
-class DeviceGuard {
- public:
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev_) == cudaSuccess && prev_ != dev) changed_ = cudaSetDevice(dev) == cudaSuccess;
-  }
-  ~DeviceGuard() {
-    if (changed_) cudaSetDevice(prev_);
-  }
-  DeviceGuard(const DeviceGuard&) = delete;
-  DeviceGuard& operator=(const DeviceGuard&) = delete;
-
- private:
-  int prev_ = 0;
-  bool changed_ = false;
-};
-
 // Everything a handle holds, on the current device: what normpre_free
 // releases, and what a normpre_init that fails part way has created so far.
 void release_handle(normpre_handle* h) {

@@ -51,6 +51,26 @@ class normpre_config(ctypes.Structure):
     ]
 
 
+class normpre_attn_config(ctypes.Structure):
+    _fields_ = [
+        ("n_heads", ctypes.c_int),
+        ("n_kv_heads", ctypes.c_int),
+        ("head_dim", ctypes.c_int),
+        ("max_seqs", ctypes.c_int),
+        ("max_tokens", ctypes.c_int64),
+        ("dtype", ctypes.c_int),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class normpre_heads(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+    ]
+
+
 class NormPreError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__("%s: %s" % (STATUS_NAMES.get(status, status), message))
@@ -100,6 +120,26 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.normpre_normalize_cols_noalloc.restype = ctypes.c_int
     lib.normpre_sketch_omega.argtypes = [ctypes.c_uint64, ctypes.c_int, i64, i64, ctypes.c_int, P, P, P, P]
     lib.normpre_sketch_omega.restype = ctypes.c_int
+    HP = ctypes.POINTER(normpre_heads)
+    i32 = ctypes.c_int
+    lib.normpre_attn_init.argtypes = [ctypes.POINTER(normpre_attn_config), ctypes.POINTER(P)]
+    lib.normpre_attn_set_lengths.argtypes = [P, i32, ctypes.POINTER(i64), P]
+    lib.normpre_attn_forward.argtypes = [P, i64, HP, HP, HP, HP, P, P]
+    lib.normpre_attn_backward.argtypes = [P, i64, HP, HP, HP, HP, P, HP, HP, HP, HP, P]
+    lib.normpre_attn_sync_status.argtypes = [P, P]
+    lib.normpre_attn_free.argtypes = [P]
+    lib.normpre_ckpt_bytes.argtypes = [i64, i64, ctypes.POINTER(i64), ctypes.POINTER(i64)]
+    lib.normpre_ckpt_pack.argtypes = [i64, i64, P, i32, i64, P, P, P]
+    lib.normpre_ckpt_restore.argtypes = [i64, i64, P, P, P, i32, i64, P]
+    lib.normpre_ckpt_wgrad.argtypes = [i64, i64, i64, P, i32, i64, P, P, P, i32, i64, i32, P]
+    lib.normpre_ckpt_swiglu.argtypes = [i64, i64, i32, P, i64, P, i64, P, i64, P, P, P, P, P]
+    lib.normpre_ckpt_swiglu_backward.argtypes = [i64, i64, i32, P, P, P, P, P, i64, P, i64, P, i64, P]
+    lib.normpre_ckpt_sync_status.argtypes = [P]
+    for name in ("attn_init", "attn_set_lengths", "attn_forward", "attn_backward", "attn_sync_status",
+                 "ckpt_bytes", "ckpt_pack", "ckpt_restore", "ckpt_wgrad", "ckpt_swiglu", "ckpt_swiglu_backward",
+                 "ckpt_sync_status"):
+        getattr(lib, "normpre_" + name).restype = ctypes.c_int
+    lib.normpre_attn_free.restype = None
     lib.normpre_free.argtypes = [P]
     lib.normpre_free.restype = None
     lib.normpre_last_error.argtypes = [P]
@@ -212,6 +252,85 @@ def normpre_sketch_omega(seed: int, matrix_id: int, t: int, n_a: int, l: int, om
     return _check(load_library().normpre_sketch_omega(int(seed), int(matrix_id), int(t), int(n_a), int(l),
                                                       omega_ptr, words_ptr or None, uniforms_ptr or None,
                                                       stream))
+
+
+def normpre_attn_init(cfg: normpre_attn_config) -> int:
+    h = ctypes.c_void_p()
+    _check(load_library().normpre_attn_init(ctypes.byref(cfg), ctypes.byref(h)))
+    return h.value
+
+
+def normpre_attn_set_lengths(plan: int, lengths: Sequence[int], stream: int = 0) -> int:
+    arr = (ctypes.c_int64 * max(1, len(lengths)))(*[int(n) for n in lengths])
+    return _check(load_library().normpre_attn_set_lengths(plan, len(lengths), arr, stream))
+
+
+def normpre_attn_forward(plan: int, tokens: int, q: normpre_heads, k: normpre_heads, v: normpre_heads,
+                         out: normpre_heads, lse_ptr: int, stream: int = 0) -> int:
+    r = ctypes.byref
+    return _check(load_library().normpre_attn_forward(plan, int(tokens), r(q), r(k), r(v), r(out), lse_ptr, stream))
+
+
+def normpre_attn_backward(plan: int, tokens: int, q: normpre_heads, k: normpre_heads, v: normpre_heads,
+                          out: normpre_heads, lse_ptr: int, dout: normpre_heads, dq: normpre_heads,
+                          dk: normpre_heads, dv: normpre_heads, stream: int = 0) -> int:
+    r = ctypes.byref
+    return _check(load_library().normpre_attn_backward(plan, int(tokens), r(q), r(k), r(v), r(out), lse_ptr, r(dout),
+                                                       r(dq), r(dk), r(dv), stream))
+
+
+def normpre_attn_sync_status(plan: int, stream: int = 0, raise_on_error: bool = True) -> int:
+    rc = load_library().normpre_attn_sync_status(plan, stream)
+    return _check(rc) if raise_on_error else rc
+
+
+def normpre_attn_free(plan: int) -> None:
+    if plan:
+        load_library().normpre_attn_free(plan)
+
+
+def normpre_ckpt_bytes(tokens: int, features: int):
+    c, s = ctypes.c_int64(), ctypes.c_int64()
+    _check(load_library().normpre_ckpt_bytes(int(tokens), int(features), ctypes.byref(c), ctypes.byref(s)))
+    return c.value, s.value
+
+
+def normpre_ckpt_pack(tokens: int, features: int, x_ptr: int, x_dtype: int, x_ld: int, codes_ptr: int,
+                      steps_ptr: int, stream: int = 0) -> int:
+    return _check(load_library().normpre_ckpt_pack(tokens, features, x_ptr, x_dtype, x_ld, codes_ptr, steps_ptr, stream))
+
+
+def normpre_ckpt_restore(tokens: int, features: int, codes_ptr: int, steps_ptr: int, y_ptr: int, y_dtype: int,
+                         y_ld: int, stream: int = 0) -> int:
+    return _check(load_library().normpre_ckpt_restore(tokens, features, codes_ptr, steps_ptr, y_ptr, y_dtype, y_ld,
+                                                      stream))
+
+
+def normpre_ckpt_wgrad(tokens: int, out_features: int, features: int, dy_ptr: int, dy_dtype: int, dy_ld: int,
+                       codes_ptr: int, steps_ptr: int, dw_ptr: int, dw_dtype: int, dw_ld: int, accumulate: int = 0,
+                       stream: int = 0) -> int:
+    return _check(load_library().normpre_ckpt_wgrad(tokens, out_features, features, dy_ptr, dy_dtype, dy_ld, codes_ptr,
+                                                    steps_ptr, dw_ptr, dw_dtype, dw_ld, int(accumulate), stream))
+
+
+def normpre_ckpt_swiglu(tokens: int, features: int, dtype: int, gate_ptr: int, gate_ld: int, up_ptr: int, up_ld: int,
+                        h_ptr: int, h_ld: int, gate_codes: int, gate_steps: int, up_codes: int, up_steps: int,
+                        stream: int = 0) -> int:
+    return _check(load_library().normpre_ckpt_swiglu(tokens, features, dtype, gate_ptr, gate_ld, up_ptr, up_ld, h_ptr,
+                                                     h_ld, gate_codes, gate_steps, up_codes, up_steps, stream))
+
+
+def normpre_ckpt_swiglu_backward(tokens: int, features: int, dtype: int, gate_codes: int, gate_steps: int,
+                                 up_codes: int, up_steps: int, dh_ptr: int, dh_ld: int, dgate_ptr: int,
+                                 dgate_ld: int, dup_ptr: int, dup_ld: int, stream: int = 0) -> int:
+    return _check(load_library().normpre_ckpt_swiglu_backward(tokens, features, dtype, gate_codes, gate_steps,
+                                                              up_codes, up_steps, dh_ptr, dh_ld, dgate_ptr, dgate_ld,
+                                                              dup_ptr, dup_ld, stream))
+
+
+def normpre_ckpt_sync_status(stream: int = 0, raise_on_error: bool = True) -> int:
+    rc = load_library().normpre_ckpt_sync_status(stream)
+    return _check(rc) if raise_on_error else rc
 
 
 def normpre_free(handle: int) -> None:
