@@ -19,9 +19,9 @@ struct normpre_attn {
   normpre_attn_config cfg;
   int device = 0;
   int64_t max_blocks = 0;
-  int n_blocks = 0;
+  int n_blocks = 0, n_pairs = 0;
   int64_t total = 0;
-  void* lists = nullptr;       // two AttnBlock[max_blocks]
+  void* lists = nullptr;       // three AttnBlock[max_blocks]
   float* delta = nullptr;      // [n_heads][max_tokens]
   int* flags = nullptr;
   std::vector<AttnBlock> host; // staging of `lists`
@@ -76,7 +76,9 @@ AttnArgs base_args(const normpre_attn* a, int64_t tokens) {
   const AttnBlock* lists = static_cast<const AttnBlock*>(a->lists);
   g.by_query = lists;
   g.by_key = lists + a->max_blocks;
+  g.by_pair = lists + 2 * a->max_blocks;
   g.n_blocks = a->n_blocks;
+  g.n_pairs = a->n_pairs;
   g.total = static_cast<int>(a->total);
   g.tokens = static_cast<int>(tokens);
   g.heads = a->cfg.n_heads;
@@ -117,6 +119,9 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
   std::stable_sort(blocks.begin(), blocks.end(),
                    [&](const AttnBlock& x, const AttnBlock& y) { return keys(x) > keys(y); });
   std::copy(blocks.begin(), blocks.end(), a->host.begin());
+  const auto pairs_end = std::copy_if(blocks.begin(), blocks.end(), a->host.begin() + 2 * a->max_blocks,
+                                      [](const AttnBlock& b) { return b.blk % 2 == 0; });
+  const size_t n_pairs = static_cast<size_t>(pairs_end - (a->host.begin() + 2 * a->max_blocks));
   std::stable_sort(blocks.begin(), blocks.end(),
                    [&](const AttnBlock& x, const AttnBlock& y) { return queries(x) > queries(y); });
   std::copy(blocks.begin(), blocks.end(), a->host.begin() + a->max_blocks);
@@ -126,9 +131,12 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
     cudaError_t e = cudaMemcpyAsync(dev, a->host.data(), n * sizeof(AttnBlock), cudaMemcpyHostToDevice, s);
     if (!e) e = cudaMemcpyAsync(dev + a->max_blocks, a->host.data() + a->max_blocks, n * sizeof(AttnBlock),
                                 cudaMemcpyHostToDevice, s);
+    if (!e) e = cudaMemcpyAsync(dev + 2 * a->max_blocks, a->host.data() + 2 * a->max_blocks,
+                                n_pairs * sizeof(AttnBlock), cudaMemcpyHostToDevice, s);
     if (e) return cuda_fail(e, "cudaMemcpyAsync");
   }
   a->n_blocks = static_cast<int>(n);
+  a->n_pairs = static_cast<int>(n_pairs);
   a->total = total;
   return NORMPRE_OK;
 }
@@ -154,9 +162,9 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out) {
     a->cfg = *cfg;
     if (a->cfg.scale == 0.f) a->cfg.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(cfg->head_dim)));
     a->max_blocks = cfg->max_tokens / 128 + std::min<int64_t>(cfg->max_seqs, cfg->max_tokens);
-    a->host.resize(2 * a->max_blocks);
+    a->host.resize(3 * a->max_blocks);
     cudaError_t e = cudaGetDevice(&a->device);
-    if (!e) e = cudaMalloc(&a->lists, 2 * a->max_blocks * sizeof(AttnBlock));
+    if (!e) e = cudaMalloc(&a->lists, 3 * a->max_blocks * sizeof(AttnBlock));
     if (!e) e = cudaMalloc(&a->delta, static_cast<size_t>(cfg->n_heads) * cfg->max_tokens * sizeof(float));
     if (!e) e = cudaMalloc(&a->flags, sizeof(int));
     if (!e) e = cudaMemset(a->flags, 0, sizeof(int));
@@ -193,8 +201,11 @@ int normpre_attn_forward(normpre_attn* a, int64_t tokens, const normpre_heads* q
   if (!lse) return fail(NORMPRE_ERR_ARG, "lse: null");
   g.lse = lse;
   DeviceGuard device_guard(a->device);
-  const cudaError_t e = launch_attn_forward_simt(g, a->cfg.dtype, static_cast<cudaStream_t>(stream));
-  return e ? cuda_fail(e, "attention forward") : NORMPRE_OK;
+  std::string err;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = a->cfg.dtype == NORMPRE_BF16 ? launch_attn_forward_tc(g, s, &err)
+                                                     : launch_attn_forward_simt(g, s);
+  return e ? cuda_fail(e, err.empty() ? "attention forward" : err.c_str()) : NORMPRE_OK;
 }
 
 int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* q, const normpre_heads* k,

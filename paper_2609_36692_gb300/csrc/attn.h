@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <string>
+
 namespace normpre {
 
 // 128 rows of one sequence: rows start + 128 blk .. of the pack, of which the
@@ -27,7 +29,8 @@ struct AttnArgs {
   float* delta;              // [heads][tokens] <do_i, o_i>
   const AttnBlock* by_query; // blocks, the ones that see the most keys first
   const AttnBlock* by_key;   // blocks, the ones seen by the most queries first
-  int n_blocks;
+  const AttnBlock* by_pair;  // the blocks of even index, in by_query's order
+  int n_blocks, n_pairs;
   int total;                 // rows that belong to sequences
   int tokens;
   int heads, kv_heads, group, dim;
@@ -37,8 +40,10 @@ struct AttnArgs {
 };
 
 // Plain kernels, one CTA per 64 rows and head (attn_simt.cu).
-cudaError_t launch_attn_forward_simt(const AttnArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t s);
 cudaError_t launch_attn_backward_simt(const AttnArgs& a, int dtype, cudaStream_t s);
+// Tensor-core kernels, bf16 (attn_fwd.cu).
+cudaError_t launch_attn_forward_tc(const AttnArgs& a, cudaStream_t s, std::string* err);
 // delta_i = <do_i, o_i>; zero for rows outside the sequences.
 cudaError_t launch_attn_delta(const AttnArgs& a, int dtype, cudaStream_t s);
 

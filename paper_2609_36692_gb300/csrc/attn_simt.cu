@@ -407,12 +407,9 @@ cudaError_t backward(const AttnArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_attn_forward_simt(const AttnArgs& a, int dtype, cudaStream_t s) {
-  if (dtype == 0)
-    return a.dim <= 64 ? run(k_attn_fwd<float, 64>, a, a.heads, fwd_smem<64>(), s)
-                       : run(k_attn_fwd<float, 128>, a, a.heads, fwd_smem<128>(), s);
-  return a.dim <= 64 ? run(k_attn_fwd<bf16, 64>, a, a.heads, fwd_smem<64>(), s)
-                     : run(k_attn_fwd<bf16, 128>, a, a.heads, fwd_smem<128>(), s);
+cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t s) {
+  return a.dim <= 64 ? run(k_attn_fwd<float, 64>, a, a.heads, fwd_smem<64>(), s)
+                     : run(k_attn_fwd<float, 128>, a, a.heads, fwd_smem<128>(), s);
 }
 
 cudaError_t launch_attn_backward_simt(const AttnArgs& a, int dtype, cudaStream_t s) {
