@@ -227,8 +227,9 @@ int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* 
   DeviceGuard device_guard(a->device);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = launch_attn_delta(g, a->cfg.dtype, s);
-  if (!e) e = launch_attn_backward_simt(g, a->cfg.dtype, s);
-  return e ? cuda_fail(e, "attention backward") : NORMPRE_OK;
+  std::string err;
+  if (!e) e = a->cfg.dtype == NORMPRE_BF16 ? launch_attn_backward_tc(g, s, &err) : launch_attn_backward_simt(g, s);
+  return e ? cuda_fail(e, err.empty() ? "attention backward" : err.c_str()) : NORMPRE_OK;
 }
 
 int normpre_attn_sync_status(normpre_attn* a, void* stream) {

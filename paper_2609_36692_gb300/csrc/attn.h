@@ -39,11 +39,12 @@ struct AttnArgs {
   int* flags;
 };
 
-// Plain kernels, one CTA per 64 rows and head (attn_simt.cu).
+// fp32 kernels, one CTA per 64 rows and head (attn_simt.cu).
 cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t s);
-cudaError_t launch_attn_backward_simt(const AttnArgs& a, int dtype, cudaStream_t s);
-// Tensor-core kernels, bf16 (attn_fwd.cu).
+cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s);
+// Tensor-core kernels, bf16 (attn_fwd.cu, attn_bwd.cu).
 cudaError_t launch_attn_forward_tc(const AttnArgs& a, cudaStream_t s, std::string* err);
+cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t s, std::string* err);
 // delta_i = <do_i, o_i>; zero for rows outside the sequences.
 cudaError_t launch_attn_delta(const AttnArgs& a, int dtype, cudaStream_t s);
 

@@ -412,9 +412,8 @@ cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t s) {
                      : run(k_attn_fwd<float, 128>, a, a.heads, fwd_smem<128>(), s);
 }
 
-cudaError_t launch_attn_backward_simt(const AttnArgs& a, int dtype, cudaStream_t s) {
-  if (dtype == 0) return a.dim <= 64 ? backward<float, 64>(a, s) : backward<float, 128>(a, s);
-  return a.dim <= 64 ? backward<bf16, 64>(a, s) : backward<bf16, 128>(a, s);
+cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s) {
+  return a.dim <= 64 ? backward<float, 64>(a, s) : backward<float, 128>(a, s);
 }
 
 cudaError_t launch_attn_delta(const AttnArgs& a, int dtype, cudaStream_t s) {
