@@ -347,8 +347,12 @@ int normpre_ckpt_wgrad(int64_t tokens, int64_t out_features, int64_t features, c
   a.k = static_cast<int>(features);
   a.accumulate = accumulate;
   cudaError_t e = ckpt_flags(&a.flags);
-  if (!e) e = launch_ckpt_wgrad_simt(a, dy_dtype, dw_dtype, static_cast<cudaStream_t>(stream));
-  return done(e, "checkpoint weight gradient");
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  std::string err;
+  if (!e) e = tokens && dy_dtype == NORMPRE_BF16 && vec_rows(dy_ld, dy_dtype)
+                  ? launch_ckpt_wgrad_tc(a, dw_dtype, s, &err)
+                  : launch_ckpt_wgrad_simt(a, dy_dtype, dw_dtype, s);
+  return done(e, err.empty() ? "checkpoint weight gradient" : err.c_str());
 }
 
 int normpre_ckpt_swiglu(int64_t tokens, int64_t features, int dtype, const void* gate, int64_t gate_ld,

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <string>
+
 namespace normpre {
 
 constexpr int kCkptBlock = 32;    // elements that share a step
@@ -37,6 +39,8 @@ struct WgradArgs {
   int accumulate;
   int* flags;
 };
+// bf16 dY whose base and rows are on 16-byte boundaries; at least one token.
+cudaError_t launch_ckpt_wgrad_tc(const WgradArgs& a, int dw_dtype, cudaStream_t s, std::string* err);
 cudaError_t launch_ckpt_wgrad_simt(const WgradArgs& a, int dy_dtype, int dw_dtype, cudaStream_t s);
 
 }  // namespace normpre

@@ -1,12 +1,36 @@
 // Weight gradient of a linear layer from its input's 8-bit checkpoint:
 // dW = dY^T xhat, summed over the tokens.
 //
+// k_wgrad_tc: bf16 dY on tcgen05.  xhat is exact in bf16 and so is dY, so that
+// one kind::f16 product with fp32 accumulation computes the sums.  A tile of
+// 128 features x 256 outputs (the transposed piece of dW: a TMEM lane is a
+// feature, so that a warp stores 32 consecutive elements of a row of dW) is
+// summed 64 tokens at a time: TMA brings the codes and the dY boxes into a
+// ring, eight warps turn codes into swizzled bf16 tiles (a byte becomes an
+// fp32 by permutation into 2^23 + byte, one packed FMA takes off the offset
+// and scales, one conversion packs two), one thread issues the MMAs, and four
+// warps drain a finished accumulator (two in TMEM) while the next tile runs.
+// Both operands are read along their rows (MN-major), as they lie in memory:
+// nothing is transposed.  The 128 side is the converted one: it costs about
+// 160 issue cycles per SM sub-partition against 512 of the MMAs.
+//   Two CTAs of a cluster take two neighbouring feature tiles of the same
+// outputs and each multicasts half of their dY boxes to both (24 KB instead of
+// 40 KB of L2 reads a step).
+//   With too few tiles for the SMs, clusters of 2, 4 or 8 CTAs split a tile's
+// tokens instead and join through distributed shared memory: each CTA lays its
+// accumulator out in its (then idle) ring and sums one slice of the outputs
+// over the ranks in rank order.
+//
 // k_wgrad_simt: fp32 arithmetic, one CTA of 256 threads per 64 x 64 piece of
 // dW, 16 tokens at a time through shared memory, a 4 x 4 piece per thread; any
 // dtype, stride and size.  Bound by the fp32 FMA pipe.
+#include <algorithm>
+#include <atomic>
+
 #include "ckpt.h"
 #include "common.cuh"
 #include "internal.h"
+#include "tc.cuh"
 
 namespace normpre {
 namespace {
@@ -55,7 +79,373 @@ __global__ void __launch_bounds__(256) k_wgrad_simt(const __grid_constant__ Wgra
     }
 }
 
+constexpr int kTileK = 128, kTileN = 256, kStep = 64;   // features, outputs, tokens of a step
+constexpr int kRing = 4, kXbuf = 3;
+constexpr int kBox = 64 * 128;                           // bytes of 64 rows of 64 bf16
+constexpr int kDyBytes = 4 * kBox, kCodeBytes = kStep * kTileK, kXBytes = 2 * kBox;
+constexpr int kStageBytes = kDyBytes + kCodeBytes;
+constexpr int kConvert = 8;                              // converting warps
+constexpr int kTcThreads = 32 * (4 + kConvert + 2);      // drain, convert, TMA, MMA
+constexpr size_t kTcSmem = kRing * kStageBytes + kXbuf * kXBytes + kRing * kStep * 4 + 512;
+
+struct WgradTcArgs {
+  WgradArgs a;
+  CUtensorMap dy, codes;
+  int tiles_k, tiles_n, units;   // units: tiles, or pairs of feature tiles
+};
+
+struct WgradBars {
+  uint64_t full[kRing], empty[kRing], xfull[kXbuf], xempty[kXbuf], tfull[2], tempty[2], drain;
+  uint32_t tmem;
+  int abort;
+  uint32_t issued[kRing];   // last parity + 1 of full
+};
+
+// 4 bytes from global to shared memory (zero if !in), and the arrival of the
+// thread's copies so far on a barrier.
+__device__ __forceinline__ void copy4_async(uint32_t* dst, const uint32_t* src, bool in) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(tc::su32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::su32(bar)) : "memory");
+}
+// A float of another CTA's shared memory in the cluster.
+__device__ __forceinline__ float4 remote_float4(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(r) : "memory");
+  return v;
+}
+
+// Four codes -> two bf16 pairs, code * step.
+__device__ __forceinline__ void convert4(uint32_t w, uint64_t step2, uint64_t off2, uint32_t& p0, uint32_t& p1) {
+  w ^= 0x80808080u;   // code + 128
+  float f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 + i));   // 2^23 + code + 128
+  float lo, hi;
+  tc::unpack2(tc::fma2(tc::pack2(f[0], f[1]), step2, off2), lo, hi);
+  p0 = pack_bf16x2(lo, hi);
+  tc::unpack2(tc::fma2(tc::pack2(f[2], f[3]), step2, off2), lo, hi);
+  p1 = pack_bf16x2(lo, hi);
+}
+
+// SPLIT: the cluster's CTAs share a tile and split its tokens; otherwise a
+// cluster of two takes two feature tiles and shares dY.
+template <typename TW, bool SPLIT>
+__global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constant__ WgradTcArgs f) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t* ring = smem;                                   // [kRing] dY boxes, codes
+  uint8_t* xbuf = ring + kRing * kStageBytes;             // [kXbuf]
+  uint32_t* steps = reinterpret_cast<uint32_t*>(xbuf + kXbuf * kXBytes);   // [kRing][kStep]
+  WgradBars* b = reinterpret_cast<WgradBars*>(steps + kRing * kStep);
+  static_assert(sizeof(WgradBars) <= 512, "barriers");
+  const WgradArgs& a = f.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_rank();
+  uint32_t csize;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(csize));
+  const int unit0 = blockIdx.x / csize, nunits = gridDim.x / csize;
+  const int total = static_cast<int>((a.tokens + kStep - 1) / kStep);
+  const int s0 = SPLIT ? static_cast<int>(static_cast<int64_t>(total) * rank / csize) : 0;
+  const int s1 = SPLIT ? static_cast<int>(static_cast<int64_t>(total) * (rank + 1) / csize) : total;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kRing; ++i) {
+      tc::mbar_init(&b->full[i], 1 + 32);
+      tc::mbar_init(&b->empty[i], SPLIT ? 1 : 2);
+      b->issued[i] = 0;
+    }
+    for (int i = 0; i < kXbuf; ++i) {
+      tc::mbar_init(&b->xfull[i], kConvert);
+      tc::mbar_init(&b->xempty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&b->tfull[i], 1);
+      tc::mbar_init(&b->tempty[i], 4);
+    }
+    tc::mbar_init(&b->drain, 1);
+    b->abort = 0;
+    tc::fence_barrier_init();
+    tc::prefetch_map(&f.dy);
+    tc::prefetch_map(&f.codes);
+  }
+  __syncthreads();
+  tc::cluster_sync();   // the peer's barriers exist before a multicast reaches them
+  if (warp == 13) {
+    tc::tmem_alloc(&b->tmem, 512);
+    tc::tmem_relinquish();
+    tc::fence_before();
+  }
+  __syncthreads();
+  tc::fence_after();
+  const uint32_t tmem = b->tmem;
+  bool ok = true;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, &b->abort));
+    return ok;
+  };
+  // feature tile and output tile of a unit
+  auto tile_k = [&](int u) { return SPLIT ? u % f.tiles_k : 2 * (u % ((f.tiles_k + 1) / 2)) + static_cast<int>(rank); };
+  auto tile_n = [&](int u) { return SPLIT ? u / f.tiles_k : u / ((f.tiles_k + 1) / 2); };
+
+  if (warp == 12) {
+    // ---------------- TMA, and the step words by plain asynchronous copies ----------------
+    int st = 0;
+    uint32_t phase = 0;
+    for (int u = unit0; u < f.units && ok; u += nunits) {
+      const int tk = tile_k(u), n0 = tile_n(u) * kTileN;
+      const uint32_t* words = a.x.steps + static_cast<int64_t>(tk) * a.tokens;
+      for (int s = s0; s < s1; ++s) {
+        if (!wait(&b->empty[st], phase ^ 1u)) break;
+        uint8_t* dst = ring + st * kStageBytes;
+        const int t0 = s * kStep;
+        if (lane == 0) {
+          tc::mbar_expect_tx(&b->full[st], kStageBytes);
+          b->issued[st] = phase + 1;
+          if (SPLIT) {
+            for (int i = 0; i < 4; ++i) tc::tma_load_3d(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, t0, 0);
+          } else {
+            for (int i = 2 * rank; i < 2 * static_cast<int>(rank) + 2; ++i)
+              tc::tma_load_3d_mc(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, t0, 0, 3);
+          }
+          tc::tma_load_3d(dst + kDyBytes, &f.codes, &b->full[st], tk * kTileK, t0, 0);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = lane; i < kStep; i += 32) {
+          const bool in = tk < f.tiles_k && t0 + i < a.tokens;
+          copy4_async(steps + st * kStep + i, in ? words + t0 + i : a.x.steps, in);
+        }
+        copies_arrive(&b->full[st]);
+        if (++st == kRing) { st = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 13) {
+    // ---------------- MMA ----------------
+    constexpr uint32_t idesc = tc::idesc_bf16(kTileK, kTileN, 1, 1);
+    int st = 0, xb = 0, acc = 0;
+    uint32_t phase = 0, xphase = 0, tphase = 0;
+    for (int u = unit0; u < f.units && ok; u += nunits) {
+      if (!wait(&b->tempty[acc], tphase ^ 1u)) break;
+      tc::fence_after();
+      for (int s = s0; s < s1; ++s) {
+        if (!wait(&b->full[st], phase) || !wait(&b->xfull[xb], xphase)) break;
+        tc::fence_after();
+        if (lane == 0) {
+          const uint32_t dy = tc::su32(ring + st * kStageBytes), x = tc::su32(xbuf + xb * kXBytes);
+#pragma unroll
+          for (int kk = 0; kk < kStep / 16; ++kk)
+            tc::mma_bf16(tmem + 256 * acc, tc::sdesc(x + kk * 2048, kBox, 1024), tc::sdesc(dy + kk * 2048, kBox, 1024),
+                         idesc, s != s0 || kk != 0);
+          if (SPLIT) tc::mma_commit(&b->empty[st]);
+          else tc::mma_commit_mc(&b->empty[st], 3);
+          tc::mma_commit(&b->xempty[xb]);
+        }
+        __syncwarp();
+        if (++st == kRing) { st = 0; phase ^= 1u; }
+        if (++xb == kXbuf) { xb = 0; xphase ^= 1u; }
+      }
+      if (!ok) break;
+      if (lane == 0) tc::mma_commit(&b->tfull[acc]);
+      __syncwarp();
+      acc ^= 1;
+      if (acc == 0) tphase ^= 1u;
+    }
+    // every MMA issued by lane 0 has completed once `drain` fires
+    if (lane == 0) {
+      tc::mma_commit(&b->drain);
+      volatile int never = 0;
+      tc::mbar_wait(&b->drain, 0, &never);
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    // ---------------- codes -> bf16 ----------------
+    // 8 rows x 4 blocks per warp: lanes of 8 rows, whose 16-byte pieces the
+    // swizzle spreads over all banks
+    const int row = 8 * (warp - 4) + (lane & 7), blk = lane >> 3, sw = row & 7;
+    int st = 0, xb = 0;
+    uint32_t phase = 0, xphase = 0;
+    for (int u = unit0; u < f.units && ok; u += nunits)
+      for (int s = s0; s < s1; ++s) {
+        if (!wait(&b->full[st], phase)) break;
+        const uint8_t* src = ring + st * kStageBytes + kDyBytes + row * kTileK;
+        uint4 c[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) c[i] = *reinterpret_cast<const uint4*>(src + (((2 * blk + i) ^ sw) << 4));
+        const float step = ckpt_step(steps[st * kStep + row], blk);
+        const float off = -8388736.f * step;             // -(2^23 + 128) step
+        const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
+        if (!wait(&b->xempty[xb], xphase ^ 1u)) break;
+        uint8_t* dst = xbuf + xb * kXBytes + (blk >> 1) * kBox + row * 128;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint4 v;
+            convert4(w[2 * h], step2, off2, v.x, v.y);
+            convert4(w[2 * h + 1], step2, off2, v.z, v.w);
+            *reinterpret_cast<uint4*>(dst + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
+          }
+        }
+        tc::fence_smem_async();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&b->xfull[xb]);
+        if (++st == kRing) { st = 0; phase ^= 1u; }
+        if (++xb == kXbuf) { xb = 0; xphase ^= 1u; }
+      }
+  } else if (!SPLIT) {
+    // ---------------- drain: warp's 32 features x 256 outputs ----------------
+    int acc = 0;
+    uint32_t tphase = 0;
+    for (int u = unit0; u < f.units && ok; u += nunits) {
+      if (!wait(&b->tfull[acc], tphase)) break;
+      tc::fence_after();
+      const int k = tile_k(u) * kTileK + 32 * warp + lane, n0 = tile_n(u) * kTileN;
+      TW* dw = static_cast<TW*>(a.dw) + static_cast<int64_t>(n0) * a.dw_ld + k;
+#pragma unroll 1
+      for (int c = 0; c < kTileN && n0 + c < a.n; c += 32) {
+        uint32_t r[32];
+        tc::tmem_ld32(tmem + 256 * acc + c + (static_cast<uint32_t>(32 * warp) << 16), r);
+        tc::tmem_ld_wait();
+        if (k < a.k) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (n0 + c + e < a.n) {
+              TW* p = dw + (c + e) * a.dw_ld;
+              const float v = __uint_as_float(r[e]);
+              *p = from_f32<TW>(a.accumulate ? to_f32(*p) + v : v);
+            }
+        }
+      }
+      tc::fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&b->tempty[acc]);
+      acc ^= 1;
+      if (acc == 0) tphase ^= 1u;
+    }
+  }
+  if (SPLIT) {
+    // one unit per cluster; each CTA's partial tile goes to its ring as
+    // [outputs][features], free once the accumulator is complete
+    float* part = reinterpret_cast<float*>(ring);
+    if (warp < 4) {
+      if (s1 > s0 && wait(&b->tfull[0], 0)) {
+        tc::fence_after();
+#pragma unroll 1
+        for (int c = 0; c < kTileN; c += 32) {
+          uint32_t r[32];
+          tc::tmem_ld32(tmem + c + (static_cast<uint32_t>(32 * warp) << 16), r);
+          tc::tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) part[(c + e) * kTileK + 32 * warp + lane] = __uint_as_float(r[e]);
+        }
+      }
+    }
+    __syncthreads();
+    tc::cluster_sync();
+    const int k0 = tile_k(unit0) * kTileK, n0 = tile_n(unit0) * kTileN, rows = kTileN / csize;
+    for (int i = threadIdx.x; i < rows * (kTileK / 4); i += kTcThreads) {
+      const int n = rank * rows + i / (kTileK / 4), k = 4 * (i % (kTileK / 4));
+      if (n0 + n >= a.n || k0 + k >= a.k) continue;
+      float v[4] = {};
+      for (uint32_t q = 0; q < csize; ++q) {
+        if (static_cast<int64_t>(total) * q / csize == static_cast<int64_t>(total) * (q + 1) / csize) continue;   // no tokens
+        const float4 w = remote_float4(tc::su32(part + n * kTileK + k), q);
+        v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+      }
+      TW* p = static_cast<TW*>(a.dw) + static_cast<int64_t>(n0 + n) * a.dw_ld + k0 + k;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (k0 + k + e < a.k) p[e] = from_f32<TW>(a.accumulate ? to_f32(p[e]) + v[e] : v[e]);
+    }
+  }
+  if (!ok && lane == 0) {
+    *static_cast<volatile int*>(&b->abort) = 1;
+    raise_flag(a.flags, kFlagTimeout);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && *static_cast<volatile int*>(&b->abort)) {
+    // let every TMA copy still in flight land before the CTA exits
+    volatile int never = 0;
+    for (int i = 0; i < kRing; ++i)
+      if (b->issued[i]) tc::mbar_wait(&b->full[i], b->issued[i] - 1, &never);
+  }
+  __syncthreads();
+  // no CTA exits while the other may still multicast into it, arrive on its
+  // barriers or read its partial tile
+  tc::cluster_sync();
+  if (warp == 13) {
+    tc::fence_after();
+    tc::tmem_dealloc(tmem, 512);
+  }
+}
+
+template <typename TW, bool SPLIT>
+cudaError_t launch_tc(WgradTcArgs f, int cluster, cudaStream_t s) {
+  auto kernel = k_wgrad_tc<TW, SPLIT>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kTcSmem));
+  if (e) return e;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  cfg.blockDim = dim3(kTcThreads);
+  cfg.dynamicSmemBytes = kTcSmem;
+  cfg.stream = s;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int clusters = f.units;
+  if (!SPLIT) {
+    // how many pairs run at once: a GPC with an odd number of SMs leaves one out
+    static std::atomic<int> known{0};
+    int fit = known.load(std::memory_order_relaxed);
+    if (!fit) {
+      cfg.gridDim = dim3(2 * std::max(1, device_sm_count() / 2));
+      if ((e = cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg))) return e;
+      known.store(fit = std::max(1, fit), std::memory_order_relaxed);
+    }
+    clusters = std::min(clusters, fit);
+  }
+  cfg.gridDim = dim3(clusters * cluster);
+  return cudaLaunchKernelEx(&cfg, kernel, f);
+}
+
 }  // namespace
+
+cudaError_t launch_ckpt_wgrad_tc(const WgradArgs& a, int dw_dtype, cudaStream_t s, std::string* err) {
+  WgradTcArgs f;
+  f.a = a;
+  const uint64_t t = static_cast<uint64_t>(a.tokens);
+  const uint64_t dy_dims[3] = {static_cast<uint64_t>(a.n), t, 1};
+  const uint64_t dy_strides[2] = {static_cast<uint64_t>(a.dy_ld) * 2, static_cast<uint64_t>(a.dy_ld) * 2};
+  const uint32_t dy_box[3] = {64, kStep, 1};
+  const uint64_t c_dims[3] = {static_cast<uint64_t>(a.x_ld), t, 1};
+  const uint64_t c_strides[2] = {static_cast<uint64_t>(a.x_ld), static_cast<uint64_t>(a.x_ld)};
+  const uint32_t c_box[3] = {kTileK, kStep, 1};
+  if (!driver_encode_tiled(&f.dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.dy), dy_dims, dy_strides,
+                           dy_box, err) ||
+      !driver_encode_tiled(&f.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<int8_t*>(a.x.codes), c_dims,
+                           c_strides, c_box, err))
+    return cudaErrorInvalidValue;
+  f.tiles_k = static_cast<int>(cdiv(a.k, kTileK));
+  f.tiles_n = static_cast<int>(cdiv(a.n, kTileN));
+  const int64_t tiles = static_cast<int64_t>(f.tiles_k) * f.tiles_n;
+  // the largest split that leaves every cluster a place in the first wave
+  // (clusters of 8 fill about 128 of the 152 SMs) and every CTA some tokens
+  int split = 1;
+  for (int c : {2, 4, 8})
+    if (tiles * c <= (c == 8 ? 128 : 144) && cdiv(a.tokens, kStep) >= 2 * c) split = c;
+  if (split > 1 || tiles == 1) {
+    f.units = static_cast<int>(tiles);
+    return dw_dtype == 0 ? launch_tc<float, true>(f, split, s) : launch_tc<bf16, true>(f, split, s);
+  }
+  f.units = (f.tiles_k + 1) / 2 * f.tiles_n;
+  return dw_dtype == 0 ? launch_tc<float, false>(f, 2, s) : launch_tc<bf16, false>(f, 2, s);
+}
 
 cudaError_t launch_ckpt_wgrad_simt(const WgradArgs& a, int dy_dtype, int dw_dtype, cudaStream_t s) {
   const dim3 grid(static_cast<unsigned>(cdiv(a.k, 64)), static_cast<unsigned>(cdiv(a.n, 64)));
