@@ -129,22 +129,6 @@ template <int kSlots> struct Role {
   }
 };
 
-// D = A B^T over the head dimension: both tiles in shared memory.
-template <int DP>
-__device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b) {
-  constexpr uint32_t idesc = tc::idesc_bf16(kTile, kTile, 0, 0);
-#pragma unroll
-  for (int kk = 0; kk < DP / 16; ++kk) tc::mma_bf16(d, desc_cols(a, kk), desc_cols(b, kk), idesc, kk != 0);
-}
-// D (+)= A B over 128 rows of B: A in TMEM, its columns 64.. at +64.
-template <int DP>
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, bool first) {
-  constexpr uint32_t idesc = tc::idesc_bf16(kTile, DP, 0, 1);
-#pragma unroll
-  for (int kk = 0; kk < kTile / 16; ++kk)
-    tc::mma_bf16_ta(d, a + kk * 8 + (kk >= 4 ? 32 : 0), desc_rows(b, kk), idesc, !first || kk != 0);
-}
-
 // The end of both kernels: copies in flight land, TMEM is freed.
 template <int kSlots>
 __device__ __forceinline__ void finish(Bars<kSlots>* b, int warp) {
@@ -259,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
       if (!role.wait(&b->own_full[0], own)) break;
       int q = take(0);
       if (!role.ok) break;
-      if (lane == 0) {
+      if (tc::elect_one()) {
         product_ss<DP>(cS, k, tile(q));
         tc::mma_commit(&b->s_full[0]);
       }
@@ -268,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
       own ^= 1u;
       int o = take(0);
       if (!role.ok) break;
-      if (lane == 0) {
+      if (tc::elect_one()) {
         product_ss<DP>(cP, v, tile(o));
         tc::mma_commit(&b->dp_full);
         if (n == 1) tc::mma_commit(&b->own_empty);
@@ -280,15 +264,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         int q2 = 0, o2 = 0;
         if (!role.wait(&b->p_ready, p_phase)) break;
         p_phase ^= 1u;
-        if (lane == 0) {
-          product_ts<DP>(cV, cS, tile(o), i == 0);
+        if (tc::elect_one()) {
+          product_ts<DP>(cV, cS, tile(o), i == 0, 32);
           tc::mma_commit(&b->empty[o]);
         }
         __syncwarp();
         if (i + 1 < n) {
           q2 = take(i + 1);
           if (!role.ok) break;
-          if (lane == 0) {
+          if (tc::elect_one()) {
             product_ss<DP>(cS, k, tile(q2));
             tc::mma_commit(&b->s_full[0]);
           }
@@ -296,15 +280,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         }
         if (!role.wait(&b->ds_ready, ds_phase)) break;
         ds_phase ^= 1u;
-        if (lane == 0) {
-          product_ts<DP>(cK, cP, tile(q), i == 0);
+        if (tc::elect_one()) {
+          product_ts<DP>(cK, cP, tile(q), i == 0, 32);
           tc::mma_commit(&b->empty[q]);
         }
         __syncwarp();
         if (i + 1 < n) {
           o2 = take(i + 1);
           if (!role.ok) break;
-          if (lane == 0) {
+          if (tc::elect_one()) {
             product_ss<DP>(cP, v, tile(o2));
             tc::mma_commit(&b->dp_full);
             if (i + 2 == n) tc::mma_commit(&b->own_empty);
@@ -314,11 +298,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         q = q2;
         o = o2;
       }
-      if (role.ok && lane == 0) tc::mma_commit(&b->acc_full);
+      if (role.ok && tc::elect_one()) tc::mma_commit(&b->acc_full);
       __syncwarp();
     }
-    // every MMA issued by lane 0 has completed once `drain` fires
-    if (lane == 0) {
+    // every MMA issued has completed once `drain` fires
+    if (tc::elect_one()) {
       tc::mma_commit(&b->drain);
       volatile int never = 0;
       tc::mbar_wait(&b->drain, 0, &never);
@@ -510,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       if (!role.wait(&b->own_full[0], own)) break;
       int k = take_k(0);
       if (!role.ok) break;
-      if (lane == 0) {
+      if (tc::elect_one()) {
         product_ss<DP>(cS + 128 * buf, q, tile(k));
         tc::mma_commit(&b->s_full[buf]);
       }
@@ -521,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       // dP's columns are free once the previous item's last block has been read
       if (!role.wait(&b->dp_free, free_phase ^ 1u)) break;
       free_phase ^= 1u;
-      if (lane == 0) {
+      if (tc::elect_one()) {
         product_ss<DP>(cP, o, tile(v));
         tc::mma_commit(&b->dp_full);
         tc::mma_commit(&b->empty[v]);
@@ -535,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         if (j + 1 < n) {
           k2 = take_k(j + 1);
           if (!role.ok) break;
-          if (lane == 0) {
+          if (tc::elect_one()) {
             product_ss<DP>(cS + 128 * (buf ^ 1), q, tile(k2));
             tc::mma_commit(&b->s_full[buf ^ 1]);
           }
@@ -543,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
           v = role.take();
           if (!role.wait(&b->dp_free, free_phase ^ 1u)) break;
           free_phase ^= 1u;
-          if (lane == 0) {
+          if (tc::elect_one()) {
             product_ss<DP>(cP, o, tile(v));
             tc::mma_commit(&b->dp_full);
             tc::mma_commit(&b->empty[v]);
@@ -553,18 +537,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         }
         if (!role.wait(&b->ds_ready, ds_phase)) break;
         ds_phase ^= 1u;
-        if (lane == 0) {
-          product_ts<DP>(cQ, cS + 128 * buf, tile(k), j == 0);
+        if (tc::elect_one()) {
+          product_ts<DP>(cQ, cS + 128 * buf, tile(k), j == 0, 32);
           tc::mma_commit(&b->empty[k]);
         }
         __syncwarp();
         k = k2;
         buf ^= 1;
       }
-      if (role.ok && lane == 0) tc::mma_commit(&b->acc_full);
+      if (role.ok && tc::elect_one()) tc::mma_commit(&b->acc_full);
       __syncwarp();
     }
-    if (lane == 0) {
+    if (tc::elect_one()) {
       tc::mma_commit(&b->drain);
       volatile int never = 0;
       tc::mbar_wait(&b->drain, 0, &never);

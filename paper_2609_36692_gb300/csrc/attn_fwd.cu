@@ -174,8 +174,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       if (!ok && lane == 0) { *abort_flag = 1; raise_flag(f.a.flags, kFlagTimeout); }
     } else if (warp == 9) {
       // ---------------- MMA ----------------
-      constexpr uint32_t idesc_s = tc::idesc_bf16(kTile, kTile, 0, 0);
-      constexpr uint32_t idesc_o = tc::idesc_bf16(kTile, DP, 0, 1);
       int slot = 0;
       uint32_t phase = 0;
       uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, o_phase[2] = {0, 0};
@@ -192,11 +190,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
         return s;
       };
       auto scores = [&](int s, int kslot) {   // S_s = Q_s K^T
-        if (lane == 0) {
-          const uint32_t qa = tc::su32(sQ + s * kTileBytes), ka = tc::su32(sKV + kslot * kTileBytes);
-  #pragma unroll
-          for (int kk = 0; kk < DP / 16; ++kk)
-            tc::mma_bf16(s_col(s), desc_cols(qa, kk), desc_cols(ka, kk), idesc_s, kk != 0);
+        if (tc::elect_one()) {
+          product_ss<DP>(s_col(s), tc::su32(sQ + s * kTileBytes), tc::su32(sKV + kslot * kTileBytes));
           tc::mma_commit(&s_full[s]);
         }
         __syncwarp();
@@ -212,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           if (it.blk[s] == top) scores(s, kslot);
         }
         if (!ok) break;
-        if (lane == 0) {
+        if (tc::elect_one()) {
           tc::mma_commit(&kv_empty[kslot]);
           if (top == 0)
             for (int s = 0; s < 2; ++s)
@@ -235,11 +230,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
                 if (!wait(&o_empty[s], o_phase[s] ^ 1u)) break;
                 o_phase[s] ^= 1u;
               }
-              if (lane == 0) {   // O_s += P_s V
-                const uint32_t va = tc::su32(sKV + vslot * kTileBytes);
-  #pragma unroll
-                for (int kk = 0; kk < kTile / 16; ++kk)
-                  tc::mma_bf16_ta(o_col(s), s_col(s) + kk * 8, desc_rows(va, kk), idesc_o, j != it.blk[s] || kk != 0);
+              if (tc::elect_one()) {   // O_s += P_s V
+                product_ts<DP>(o_col(s), s_col(s), tc::su32(sKV + vslot * kTileBytes), j == it.blk[s], 0);
                 tc::mma_commit(&pv_done[s]);
               }
               __syncwarp();
@@ -247,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
             if (j > 0 && j - 1 <= it.blk[s]) scores(s, kslot);
           }
           if (!ok) break;
-          if (lane == 0) {
+          if (tc::elect_one()) {
             tc::mma_commit(&kv_empty[vslot]);
             if (j > 0) tc::mma_commit(&kv_empty[kslot]);
             if (j == 1)
@@ -258,8 +250,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
         }
       }
       if (!ok && lane == 0) { *abort_flag = 1; raise_flag(f.a.flags, kFlagTimeout); }
-      // every MMA issued by lane 0 has completed once `drain` fires
-      if (lane == 0) {
+      // every MMA issued has completed once `drain` fires
+      if (tc::elect_one()) {
         tc::mma_commit(drain);
         volatile int never = 0;
         tc::mbar_wait(drain, 0, &never);

@@ -32,13 +32,29 @@ __device__ __forceinline__ void load_rows(uint8_t* dst, const CUtensorMap* map, 
     tc::tma_load_3d(dst + c * kChunk, map, bar, 64 * c, static_cast<int>(row), head);
 }
 
-// Descriptor of a 16-deep K step of a tile read along its columns (K = head
-// dimension: K-major) or along its rows (K = tokens: MN-major).
-__device__ __forceinline__ uint64_t desc_cols(uint32_t tile, int kk) {
-  return tc::sdesc(tile + (kk >> 2) * kChunk + (kk & 3) * 32, 16, 1024);
+// Descriptor of a tile read along its columns (K = head dimension: K-major) or
+// along its rows (K = tokens: MN-major); step kk of 16 adds to the address.
+__device__ __forceinline__ uint64_t desc_cols(uint32_t tile) { return tc::sdesc(tile, 16, 1024); }
+__device__ __forceinline__ uint64_t desc_rows(uint32_t tile) { return tc::sdesc(tile, kChunk, 1024); }
+__host__ __device__ constexpr uint64_t cols_step(int kk) { return ((kk >> 2) * kChunk + (kk & 3) * 32) >> 4; }
+__host__ __device__ constexpr uint64_t rows_step(int kk) { return (kk * 2048) >> 4; }
+
+// D = A B^T over the head dimension: both tiles in shared memory.
+template <int DP>
+__device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b) {
+  constexpr uint32_t idesc = tc::idesc_bf16(kTile, kTile, 0, 0);
+  const uint64_t ad = desc_cols(a), bd = desc_cols(b);
+#pragma unroll
+  for (int kk = 0; kk < DP / 16; ++kk) tc::mma_bf16(d, ad + cols_step(kk), bd + cols_step(kk), idesc, kk != 0);
 }
-__device__ __forceinline__ uint64_t desc_rows(uint32_t tile, int kk) {
-  return tc::sdesc(tile + kk * 2048, kChunk, 1024);
+// D (+)= A B over 128 rows of B: A in TMEM, its columns 64 .. 127 `gap` columns further on.
+template <int DP>
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, bool first, int gap) {
+  constexpr uint32_t idesc = tc::idesc_bf16(kTile, DP, 0, 1);
+  const uint64_t bd = desc_rows(b);
+#pragma unroll
+  for (int kk = 0; kk < kTile / 16; ++kk)
+    tc::mma_bf16_ta(d, a + kk * 8 + (kk >= 4 ? gap : 0), bd + rows_step(kk), idesc, !first || kk != 0);
 }
 
 // Zeroes rows [rows, 128) of a tile in shared memory (one warp): what follows

@@ -233,12 +233,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
       for (int s = s0; s < s1; ++s) {
         if (!wait(&b->full[st], phase) || !wait(&b->xfull[xb], xphase)) break;
         tc::fence_after();
-        if (lane == 0) {
-          const uint32_t dy = tc::su32(ring + st * kStageBytes), x = tc::su32(xbuf + xb * kXBytes);
+        if (tc::elect_one()) {
+          const uint64_t dy = tc::sdesc(tc::su32(ring + st * kStageBytes), kBox, 1024);
+          const uint64_t x = tc::sdesc(tc::su32(xbuf + xb * kXBytes), kBox, 1024);
 #pragma unroll
           for (int kk = 0; kk < kStep / 16; ++kk)
-            tc::mma_bf16(tmem + 256 * acc, tc::sdesc(x + kk * 2048, kBox, 1024), tc::sdesc(dy + kk * 2048, kBox, 1024),
-                         idesc, s != s0 || kk != 0);
+            tc::mma_bf16(tmem + 256 * acc, x + kk * (2048 >> 4), dy + kk * (2048 >> 4), idesc, s != s0 || kk != 0);
           if (SPLIT) tc::mma_commit(&b->empty[st]);
           else tc::mma_commit_mc(&b->empty[st], 3);
           tc::mma_commit(&b->xempty[xb]);
@@ -248,13 +248,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
         if (++xb == kXbuf) { xb = 0; xphase ^= 1u; }
       }
       if (!ok) break;
-      if (lane == 0) tc::mma_commit(&b->tfull[acc]);
+      if (tc::elect_one()) tc::mma_commit(&b->tfull[acc]);
       __syncwarp();
       acc ^= 1;
       if (acc == 0) tphase ^= 1u;
     }
-    // every MMA issued by lane 0 has completed once `drain` fires
-    if (lane == 0) {
+    // every MMA issued has completed once `drain` fires
+    if (tc::elect_one()) {
       tc::mma_commit(&b->drain);
       volatile int never = 0;
       tc::mbar_wait(&b->drain, 0, &never);
