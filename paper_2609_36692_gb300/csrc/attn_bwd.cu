@@ -11,19 +11,23 @@
 // instead of 5.
 //
 // Both: one CTA per SM walks the work list; the owned tiles stay in shared
-// memory, the others pass through a ring filled by a TMA warp; one thread
-// issues the MMAs; eight softmax warps each take 32 rows x 64 columns of a
-// score tile, one thread per row.  P and dS go back to TMEM as bf16 over the
-// scores they came from (each warp group inside its own half of the columns)
-// and are the A operands of the products that follow.
+// memory, the others pass through a ring filled by a TMA warp; eight softmax
+// warps each take 32 rows x 64 columns of a score tile, one thread per row.  P
+// and dS go back to TMEM as bf16 over the scores they came from (each warp
+// group inside its own half of the columns) and are the A operands of the
+// products that follow.  Two warps issue the MMAs, each one of the two chains
+// below: a thread's MMAs run almost as it issues them, so that while it waits
+// the tensor cores need another's.
 //
 // k_attn_dkdv forms the transposed tiles S^T, dP^T (rows: keys), so that P^T
-// and dS^T lie in TMEM as the A operands of dV and dK.  TMEM at head_dim 128:
-// S^T 128, dP^T 128, dV 128, dK 128 columns.  The order dV(i), S(i+1), dK(i),
-// dP(i+1) keeps the tensor cores on two products while the softmax warps form
-// dS(i) and then P(i+1).
+// and dS^T lie in TMEM as the A operands of dV and dK.  Chains: P(i) -> dV(i),
+// S(i+1) and dS(i) -> dK(i), dP(i+1).  TMEM at head_dim 128: S^T 128, dP^T 128,
+// dV 128, dK 128 columns, all there is.
 // k_attn_dq: S in two buffers, dP, dQ; dS lies over S, so that dP(j+1) starts
-// as soon as dP(j) has been read.
+// as soon as dP(j) has been read.  Chains: dS(j) -> dQ(j), S(j+2) and dP(j).
+// Head dimensions up to 64 leave room for a second set of owned tiles and a
+// second set of accumulators, so that an item's start and end overlap its
+// neighbours.
 //
 // Roundings to bf16: P and dS once each (MMA operands), the gradients once.
 #include <algorithm>
@@ -33,14 +37,15 @@
 namespace normpre {
 namespace {
 
-constexpr int kThreads = 384;   // softmax 8 warps, TMA, MMA, statistics, padding rows
+constexpr int kThreads = 384;   // softmax 8 warps, TMA, MMA, statistics and sequence ends, MMA
 
 template <int DP> struct Bwd {
   static constexpr int kChunks = DP / 64;
   static constexpr int kTileBytes = kChunks * kChunk;
-  static constexpr int kSlots = DP == 128 ? 5 : 10;
-  static constexpr int kOther = 2048 + 512;            // statistics, barriers
-  static constexpr size_t kSmem = (2 + kSlots) * kTileBytes + kOther;
+  static constexpr int kSlots = DP == 128 ? 5 : 8;
+  static constexpr int kSets = DP == 128 ? 1 : 2;      // owned tiles, accumulators
+  static constexpr int kOther = 2048 + 768;            // statistics, barriers
+  static constexpr size_t kSmem = (2 * kSets + kSlots) * kTileBytes + kOther;
 };
 
 struct BwdArgs {
@@ -50,52 +55,74 @@ struct BwdArgs {
 
 // Barriers of both kernels.
 template <int kSlots> struct Bars {
-  uint64_t full[kSlots], empty[kSlots];    // ring
-  uint64_t own_full[2], own_empty;         // the owned tiles: one barrier each, freed together
+  // raw: a tile that ends its sequence lands here first; once its tail is
+  // zeroed it counts as full
+  uint64_t full[kSlots], empty[kSlots], raw[kSlots];
+  uint64_t own_full[2][2], own_empty[2];   // per set: the two owned tiles, freed together
   uint64_t s_full[2], dp_full, p_ready, ds_ready, dp_free;
-  uint64_t acc_full, acc_empty;
+  uint64_t acc_full[2], acc_empty[2];
   uint64_t stat_full[2], stat_empty[2];
-  uint64_t drain;
+  uint64_t drain[2];
   uint32_t tmem;
   int abort;
-  uint32_t issued[kSlots], own_issued[2];  // last parity + 1 of full and own_full
+  uint32_t issued[kSlots], raw_issued[kSlots], own_issued[2];  // loads so far
 };
 
+// `users`: MMA chains that read a ring tile, and that add to an accumulator set.
 template <int kSlots>
-__device__ __forceinline__ void init_bars(Bars<kSlots>* b) {
+__device__ __forceinline__ void init_bars(Bars<kSlots>* b, int users) {
   for (int i = 0; i < kSlots; ++i) {
     tc::mbar_init(&b->full[i], 1);
-    tc::mbar_init(&b->empty[i], 1);
-    b->issued[i] = 0;
+    tc::mbar_init(&b->empty[i], users);
+    tc::mbar_init(&b->raw[i], 1);
+    b->issued[i] = b->raw_issued[i] = 0;
   }
   for (int i = 0; i < 2; ++i) {
-    tc::mbar_init(&b->own_full[i], 1);
+    tc::mbar_init(&b->own_full[i][0], 1);
+    tc::mbar_init(&b->own_full[i][1], 1);
+    tc::mbar_init(&b->own_empty[i], 2);
     tc::mbar_init(&b->s_full[i], 1);
     tc::mbar_init(&b->stat_full[i], 1);
     tc::mbar_init(&b->stat_empty[i], 8);
+    tc::mbar_init(&b->acc_full[i], users);
+    tc::mbar_init(&b->acc_empty[i], 8);
+    tc::mbar_init(&b->drain[i], 1);
     b->own_issued[i] = 0;
   }
-  tc::mbar_init(&b->own_empty, 1);
   tc::mbar_init(&b->dp_full, 1);
   tc::mbar_init(&b->p_ready, 8);
   tc::mbar_init(&b->ds_ready, 8);
   tc::mbar_init(&b->dp_free, 8);
-  tc::mbar_init(&b->acc_full, 1);
-  tc::mbar_init(&b->acc_empty, 8);
-  tc::mbar_init(&b->drain, 1);
   b->abort = 0;
   tc::fence_barrier_init();
 }
 
-// What every role carries: the barriers and whether its waits still hold.
-template <int kSlots> struct Role {
+// Alternates over `sets` buffers; `parity` is of the current one's uses.
+template <int sets> struct Turn {
+  int i = 0;
+  uint32_t parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++i == sets) { i = 0; parity ^= 1u; }
+  }
+};
+
+// What a warp carries: the barriers, whether its waits still hold, and its
+// place in the ring.
+template <int kSlots> struct Warp {
   Bars<kSlots>* b;
   int lane;
   bool ok;
   int slot;
   uint32_t phase;
+  // all lanes of the warp
   __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
     ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, &b->abort));
+    tc::fence_after();
+    return ok;
+  }
+  // one thread
+  __device__ __forceinline__ bool wait1(uint64_t* bar, uint32_t parity) {
+    ok = ok && tc::mbar_wait(bar, parity, &b->abort);
     tc::fence_after();
     return ok;
   }
@@ -108,37 +135,69 @@ template <int kSlots> struct Role {
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(bar);
   }
-  // TMA warp: fills the next ring slot
+  // TMA thread: fills the next ring slot
   __device__ __forceinline__ void load(uint8_t* ring, int tile_bytes, const CUtensorMap* map, int64_t row, int head,
-                                       int chunks) {
-    if (!wait(&b->empty[slot], phase ^ 1u)) return;
-    if (lane == 0) {
-      tc::mbar_expect_tx(&b->full[slot], tile_bytes);
-      b->issued[slot] = phase + 1;
-      load_rows(ring + slot * tile_bytes, map, &b->full[slot], row, head, chunks);
-    }
-    __syncwarp();
+                                       int chunks, bool tail) {
+    if (!wait1(&b->empty[slot], phase ^ 1u)) return;
+    uint64_t* bar = tail ? &b->raw[slot] : &b->full[slot];
+    tc::mbar_expect_tx(bar, tile_bytes);
+    if (tail) ++b->raw_issued[slot];
+    else b->issued[slot] = phase + 1;
+    load_rows(ring + slot * tile_bytes, map, bar, row, head, chunks);
     next();
   }
-  // MMA warp: the next ring slot, once it is full
+  // TMA thread: the two owned tiles of a set
+  __device__ __forceinline__ bool load_own(uint8_t* tiles, int tile_bytes, int set, uint32_t parity,
+                                           const CUtensorMap* m0, const CUtensorMap* m1, int64_t row, int head,
+                                           int chunks) {
+    if (!wait1(&b->own_empty[set], parity ^ 1u)) return false;
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_expect_tx(&b->own_full[set][i], tile_bytes);
+      load_rows(tiles + (2 * set + i) * tile_bytes, i ? m1 : m0, &b->own_full[set][i], row, head, chunks);
+    }
+    ++b->own_issued[set];
+    return true;
+  }
+  // MMA thread: the ring slot `ahead` places on, once it is full
   __device__ __forceinline__ int take() {
     const int s = slot;
-    wait(&b->full[s], phase);
+    wait1(&b->full[s], phase);
     next();
     return s;
+  }
+  // warp: zeroes the end of a ring tile that just arrived, and passes it on
+  __device__ __forceinline__ bool end_tile(uint8_t* ring, int tile_bytes, int s, uint32_t& seen, int rows, int chunks) {
+    if (!wait(&b->raw[s], (seen >> s) & 1u)) return false;
+    seen ^= 1u << s;
+    zero_tail(ring + s * tile_bytes, rows, chunks, lane);
+    if (lane == 0) tc::mbar_arrive(&b->full[s]);
+    return true;
+  }
+  // MMA thread: every MMA issued has completed when this returns
+  __device__ __forceinline__ void drain(int i) {
+    int never = 0;
+    tc::mma_commit(&b->drain[i]);
+    tc::mbar_wait(&b->drain[i], 0, &never);
   }
 };
 
 // The end of both kernels: copies in flight land, TMEM is freed.
 template <int kSlots>
-__device__ __forceinline__ void finish(Bars<kSlots>* b, int warp) {
+__device__ __forceinline__ void finish(const Warp<kSlots>& w, int warp, int* flags) {
+  Bars<kSlots>* b = w.b;
+  if (!w.ok && w.lane == 0) {
+    *static_cast<volatile int*>(&b->abort) = 1;
+    raise_flag(flags, kFlagTimeout);
+  }
   __syncthreads();
   if (threadIdx.x == 0 && *static_cast<volatile int*>(&b->abort)) {
-    volatile int never = 0;
-    for (int i = 0; i < kSlots; ++i)
+    int never = 0;
+    for (int i = 0; i < kSlots; ++i) {
       if (b->issued[i]) tc::mbar_wait(&b->full[i], b->issued[i] - 1, &never);
-    for (int i = 0; i < 2; ++i)
-      if (b->own_issued[i]) tc::mbar_wait(&b->own_full[i], b->own_issued[i] - 1, &never);
+      if (b->raw_issued[i]) tc::mbar_wait(&b->raw[i], (b->raw_issued[i] - 1) & 1u, &never);
+    }
+    for (int i = 0; i < 4; ++i)
+      if (b->own_issued[i >> 1]) tc::mbar_wait(&b->own_full[i >> 1][i & 1], (b->own_issued[i >> 1] - 1) & 1u, &never);
   }
   __syncthreads();
   if (warp == 9) {
@@ -179,18 +238,17 @@ __device__ __forceinline__ bool get_item(const AttnArgs& a, const AttnBlock* lis
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_constant__ BwdArgs f) {
   using B = Bwd<DP>;
-  constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks;
+  constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks, kSets = B::kSets;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t* sK = smem;
-  uint8_t* sV = sK + kTileBytes;
-  uint8_t* ring = sV + kTileBytes;
+  uint8_t* own = smem;                                // [kSets] K, V
+  uint8_t* ring = own + 2 * kSets * kTileBytes;       // Q, dO, Q, dO ..
   float* stat = reinterpret_cast<float*>(ring + kSlots * kTileBytes);   // [2][-log2(e) lse, delta][128]
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(stat + 512);
-  static_assert(sizeof(Bars<kSlots>) <= 512, "barriers");
+  static_assert(sizeof(Bars<kSlots>) <= 768, "barriers");
   const AttnArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    init_bars(b);
+    init_bars(b, 2);
     for (const CUtensorMap* m : {&f.q, &f.k, &f.v, &f.dout}) tc::prefetch_map(m);
   }
   if (warp == 9) {
@@ -200,120 +258,108 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   }
   __syncthreads();
   tc::fence_after();
-  const uint32_t cS = b->tmem, cP = cS + 128, cV = cS + 256, cK = cV + DP;
-  Role<kSlots> role = {b, lane, true, 0, 0};
+  const uint32_t cS = b->tmem, cP = cS + 128, cAcc = cS + 256;     // per set: dV, dK
+  Warp<kSlots> w = {b, lane, true, 0, 0};
+  Turn<kSets> set;
   Item it;
 
   if (warp == 8) {
-    // ---------------- TMA ----------------
-    uint32_t own = 0;
-    for (int64_t r = 0; role.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r) {
-      if (!role.wait(&b->own_empty, own ^ 1u)) break;
-      const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
-      if (lane == 0) {
-        for (int i = 0; i < 2; ++i) {
-          tc::mbar_expect_tx(&b->own_full[i], kTileBytes);
-          b->own_issued[i] = own + 1;
-          load_rows(i ? sV : sK, i ? &f.v : &f.k, &b->own_full[i], row, it.head, kChunks);
-        }
+    // ---------------- TMA (one thread), then the rows past the sequences ----------------
+    if (tc::elect_one()) {
+      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r, set.next()) {
+        const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
+        if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.k, &f.v, row, it.head, kChunks)) break;
+        for (int g = 0; g < a.group && w.ok; ++g)
+          for (int i = it.blk; i * kTile < it.len && w.ok; ++i) {
+            const int64_t qrow = it.start + static_cast<int64_t>(kTile) * i;
+            const bool tail = kTile * (i + 1) > it.len;
+            w.load(ring, kTileBytes, &f.q, qrow, it.head * a.group + g, kChunks, tail);
+            if (w.ok) w.load(ring, kTileBytes, &f.dout, qrow, it.head * a.group + g, kChunks, tail);
+          }
       }
-      __syncwarp();
-      own ^= 1u;
-      for (int g = 0; g < a.group && role.ok; ++g)
-        for (int i = it.blk; i * kTile < it.len && role.ok; ++i) {
-          const int64_t qrow = it.start + static_cast<int64_t>(kTile) * i;
-          role.load(ring, kTileBytes, &f.q, qrow, it.head * a.group + g, kChunks);
-          if (role.ok) role.load(ring, kTileBytes, &f.dout, qrow, it.head * a.group + g, kChunks);
-        }
     }
+    w.ok = __all_sync(0xffffffffu, w.ok);
+    zero_padding(a, a.dk, a.kv_heads, blockIdx.x, gridDim.x, lane);
+    zero_padding(a, a.dv, a.kv_heads, blockIdx.x, gridDim.x, lane);
   } else if (warp == 9) {
-    // ---------------- MMA ----------------
-    uint32_t own = 0, p_phase = 0, ds_phase = 0, acc_phase = 0;
-    const uint32_t k = tc::su32(sK), v = tc::su32(sV);
-    auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-    for (int64_t r = 0; role.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r) {
-      const int nq = (it.len - 1) / kTile - it.blk + 1, n = nq * a.group;
-      const int last = it.len - kTile * (it.blk + nq - 1);     // rows of the last query block
-      // the tile's rows past the sequence's end become zeros
-      auto take = [&](int i) {
-        const int s = role.take();
-        if (role.ok && last < kTile && i % nq == nq - 1) zero_tail(ring + s * kTileBytes, last, kChunks, lane);
-        return s;
-      };
-      if (!role.wait(&b->own_full[0], own)) break;
-      int q = take(0);
-      if (!role.ok) break;
-      if (tc::elect_one()) {
+    // ---------------- MMA (one thread): dV(i), S(i + 1) ----------------
+    if (tc::elect_one()) {
+      uint32_t p_phase = 0;
+      auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
+      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r, set.next()) {
+        const int n = ((it.len - 1) / kTile - it.blk + 1) * a.group;
+        const uint32_t k = tc::su32(own + 2 * set.i * kTileBytes);
+        if (!w.wait1(&b->own_full[set.i][0], set.parity)) break;
+        int q = w.take();
+        if (!w.ok) break;
         product_ss<DP>(cS, k, tile(q));
         tc::mma_commit(&b->s_full[0]);
-      }
-      __syncwarp();
-      if (!role.wait(&b->own_full[1], own)) break;
-      own ^= 1u;
-      int o = take(0);
-      if (!role.ok) break;
-      if (tc::elect_one()) {
-        product_ss<DP>(cP, v, tile(o));
-        tc::mma_commit(&b->dp_full);
-        if (n == 1) tc::mma_commit(&b->own_empty);
-      }
-      __syncwarp();
-      if (!role.wait(&b->acc_empty, acc_phase ^ 1u)) break;
-      acc_phase ^= 1u;
-      for (int i = 0; i < n; ++i) {
-        int q2 = 0, o2 = 0;
-        if (!role.wait(&b->p_ready, p_phase)) break;
-        p_phase ^= 1u;
-        if (tc::elect_one()) {
-          product_ts<DP>(cV, cS, tile(o), i == 0, 32);
+        tc::mma_commit(&b->empty[q]);
+        if (n == 1) tc::mma_commit(&b->own_empty[set.i]);
+        if (!w.wait1(&b->acc_empty[set.i], set.parity ^ 1u)) break;
+        for (int i = 0; i < n; ++i) {
+          const int o = w.take();
+          if (!w.wait1(&b->p_ready, p_phase)) break;
+          p_phase ^= 1u;
+          product_ts<DP>(cAcc + 2 * DP * set.i, cS, tile(o), i == 0, 32);
           tc::mma_commit(&b->empty[o]);
-        }
-        __syncwarp();
-        if (i + 1 < n) {
-          q2 = take(i + 1);
-          if (!role.ok) break;
-          if (tc::elect_one()) {
-            product_ss<DP>(cS, k, tile(q2));
-            tc::mma_commit(&b->s_full[0]);
-          }
-          __syncwarp();
-        }
-        if (!role.wait(&b->ds_ready, ds_phase)) break;
-        ds_phase ^= 1u;
-        if (tc::elect_one()) {
-          product_ts<DP>(cK, cP, tile(q), i == 0, 32);
+          if (i + 1 == n) break;
+          q = w.take();
+          if (!w.ok) break;
+          product_ss<DP>(cS, k, tile(q));
+          tc::mma_commit(&b->s_full[0]);
           tc::mma_commit(&b->empty[q]);
+          if (i + 2 == n) tc::mma_commit(&b->own_empty[set.i]);
         }
-        __syncwarp();
-        if (i + 1 < n) {
-          o2 = take(i + 1);
-          if (!role.ok) break;
-          if (tc::elect_one()) {
-            product_ss<DP>(cP, v, tile(o2));
-            tc::mma_commit(&b->dp_full);
-            if (i + 2 == n) tc::mma_commit(&b->own_empty);
-          }
-          __syncwarp();
-        }
-        q = q2;
-        o = o2;
+        if (w.ok) tc::mma_commit(&b->acc_full[set.i]);
       }
-      if (role.ok && tc::elect_one()) tc::mma_commit(&b->acc_full);
-      __syncwarp();
-    }
-    // every MMA issued has completed once `drain` fires
-    if (tc::elect_one()) {
-      tc::mma_commit(&b->drain);
-      volatile int never = 0;
-      tc::mbar_wait(&b->drain, 0, &never);
+      w.drain(0);
     }
     __syncwarp();
+    w.ok = __all_sync(0xffffffffu, w.ok);
+  } else if (warp == 11) {
+    // ---------------- MMA (one thread): dK(i), dP(i + 1) ----------------
+    if (tc::elect_one()) {
+      uint32_t ds_phase = 0;
+      auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
+      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r, set.next()) {
+        const int n = ((it.len - 1) / kTile - it.blk + 1) * a.group;
+        const uint32_t v = tc::su32(own + (2 * set.i + 1) * kTileBytes);
+        if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
+        int q = w.take(), o = w.take();
+        if (!w.ok) break;
+        product_ss<DP>(cP, v, tile(o));
+        tc::mma_commit(&b->dp_full);
+        tc::mma_commit(&b->empty[o]);
+        if (n == 1) tc::mma_commit(&b->own_empty[set.i]);
+        if (!w.wait1(&b->acc_empty[set.i], set.parity ^ 1u)) break;
+        for (int i = 0; i < n; ++i) {
+          if (!w.wait1(&b->ds_ready, ds_phase)) break;
+          ds_phase ^= 1u;
+          product_ts<DP>(cAcc + 2 * DP * set.i + DP, cP, tile(q), i == 0, 32);
+          tc::mma_commit(&b->empty[q]);
+          if (i + 1 == n) break;
+          q = w.take();
+          o = w.take();
+          if (!w.ok) break;
+          product_ss<DP>(cP, v, tile(o));
+          tc::mma_commit(&b->dp_full);
+          tc::mma_commit(&b->empty[o]);
+          if (i + 2 == n) tc::mma_commit(&b->own_empty[set.i]);
+        }
+        if (w.ok) tc::mma_commit(&b->acc_full[set.i]);
+      }
+      w.drain(1);
+    }
+    __syncwarp();
+    w.ok = __all_sync(0xffffffffu, w.ok);
   } else if (warp == 10) {
-    // ---------------- log-sums and deltas of the query blocks ----------------
-    uint32_t phase = 0;
-    int st = 0;
-    for (int64_t r = 0; role.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r)
-      for (int g = 0; g < a.group && role.ok; ++g) {
+    // ---------------- log-sums and deltas of the query blocks, sequence ends ----------------
+    Turn<2> st;
+    uint32_t seen = 0;
+    int slot = 0;
+    for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r)
+      for (int g = 0; g < a.group && w.ok; ++g) {
         const int64_t base = static_cast<int64_t>(it.head * a.group + g) * a.tokens + it.start;
         for (int i = it.blk * kTile; i < it.len; i += kTile) {
           float ls[4], de[4];
@@ -323,38 +369,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
             ls[e] = j < it.len ? a.lse[base + j] * -kLog2e : -INFINITY;   // past the end: P = 0
             de[e] = j < it.len ? a.delta[base + j] : 0.f;
           }
-          if (!role.wait(&b->stat_empty[st], phase ^ 1u)) break;
+          const int s0 = slot, s1 = s0 + 1 == kSlots ? 0 : s0 + 1;
+          slot = s1 + 1 == kSlots ? 0 : s1 + 1;
+          if (it.len - i < kTile && (!w.end_tile(ring, kTileBytes, s0, seen, it.len - i, kChunks) ||
+                                     !w.end_tile(ring, kTileBytes, s1, seen, it.len - i, kChunks)))
+            break;
+          if (!w.wait(&b->stat_empty[st.i], st.parity ^ 1u)) break;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            stat[st * 256 + 32 * e + lane] = ls[e];
-            stat[st * 256 + 128 + 32 * e + lane] = de[e];
+            stat[st.i * 256 + 32 * e + lane] = ls[e];
+            stat[st.i * 256 + 128 + 32 * e + lane] = de[e];
           }
           __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&b->stat_full[st]);
-          st ^= 1;
-          if (st == 0) phase ^= 1u;
+          if (lane == 0) tc::mbar_arrive(&b->stat_full[st.i]);
+          st.next();
         }
       }
-  } else if (warp == 11) {
-    // ---------------- rows past the sequences ----------------
-    zero_padding(a, a.dk, a.kv_heads, blockIdx.x, gridDim.x, lane);
-    zero_padding(a, a.dv, a.kv_heads, blockIdx.x, gridDim.x, lane);
   } else {
     // ---------------- softmax ----------------
     const int half = warp >> 2, row = 32 * (warp & 3) + lane;    // columns 64 half .., row of the tile
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t mS = cS + lanes + 64 * half, mP = cP + lanes + 64 * half;
     const uint64_t c2 = tc::pack2(a.scale_log2, a.scale_log2);
-    uint32_t phase = 0, stat_phase = 0, acc_phase = 0;
-    int st = 0;
-    for (int64_t r = 0; role.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r) {
+    uint32_t phase = 0;
+    Turn<2> st;
+    for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r, set.next()) {
       const int nq = (it.len - 1) / kTile - it.blk + 1, n = nq * a.group;
       for (int i = 0; i < n; ++i) {
-        const float* ls = stat + st * 256 + 64 * half;
-        if (!role.wait(&b->stat_full[st], stat_phase) || !role.wait(&b->s_full[0], phase)) break;
+        const float* ls = stat + st.i * 256 + 64 * half;
+        if (!w.wait(&b->stat_full[st.i], st.parity) || !w.wait(&b->s_full[0], phase)) break;
         const bool diag = i % nq == 0;
         float p[64];
-        uint32_t w[32];
+        uint32_t pk[32];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t x[32];
@@ -376,11 +422,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
             if (64 * half + e < row) p[e] = 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) w[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
-        tc::tmem_st32(mS, w);
+        for (int e = 0; e < 32; ++e) pk[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
+        tc::tmem_st32(mS, pk);
         tc::tmem_st_drain();
-        role.arrive(&b->p_ready);
-        if (!role.wait(&b->dp_full, phase)) break;
+        w.arrive(&b->p_ready);
+        if (!w.wait(&b->dp_full, phase)) break;
         phase ^= 1u;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -392,56 +438,48 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
             const float4 de = *reinterpret_cast<const float4*>(ls + 128 + 32 * h + e);
             const float d4[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
-            for (int u = 0; u < 4; u += 2) {
-              float y0 = p[32 * h + e + u] * (__uint_as_float(x[e + u]) - d4[u]);
-              float y1 = p[32 * h + e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]);
-              w[16 * h + (e + u) / 2] = pack_bf16x2(y0, y1);
-            }
+            for (int u = 0; u < 4; u += 2)
+              pk[16 * h + (e + u) / 2] = pack_bf16x2(p[32 * h + e + u] * (__uint_as_float(x[e + u]) - d4[u]),
+                                                     p[32 * h + e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]));
           }
         }
         if (diag) {   // 0 * NaN in an unseen place
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
-            if (64 * half + 2 * e < row) w[e] &= 0xFFFF0000u;
-            if (64 * half + 2 * e + 1 < row) w[e] &= 0x0000FFFFu;
+            if (64 * half + 2 * e < row) pk[e] &= 0xFFFF0000u;
+            if (64 * half + 2 * e + 1 < row) pk[e] &= 0x0000FFFFu;
           }
         }
-        tc::tmem_st32(mP, w);
+        tc::tmem_st32(mP, pk);
         tc::tmem_st_drain();
-        role.arrive(&b->ds_ready);
-        if (lane == 0) tc::mbar_arrive(&b->stat_empty[st]);
-        st ^= 1;
-        if (st == 0) stat_phase ^= 1u;
+        w.arrive(&b->ds_ready);
+        if (lane == 0) tc::mbar_arrive(&b->stat_empty[st.i]);
+        st.next();
       }
-      if (!role.wait(&b->acc_full, acc_phase)) break;
-      acc_phase ^= 1u;
+      if (!w.wait(&b->acc_full[set.i], set.parity)) break;
       const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk + row;
       const bool in = kTile * it.blk + row < it.len;
-      store_acc<DP>(a.dv, cV + lanes, at, in, it.head, half, 1.f, a.dim);
-      store_acc<DP>(a.dk, cK + lanes, at, in, it.head, half, a.scale, a.dim);
-      role.arrive(&b->acc_empty);
+      const uint32_t acc = cAcc + 2 * DP * set.i + lanes;
+      store_acc<DP>(a.dv, acc, at, in, it.head, half, 1.f, a.dim);
+      store_acc<DP>(a.dk, acc + DP, at, in, it.head, half, a.scale, a.dim);
+      w.arrive(&b->acc_empty[set.i]);
     }
   }
-  if (!role.ok && lane == 0) {
-    *static_cast<volatile int*>(&b->abort) = 1;
-    raise_flag(a.flags, kFlagTimeout);
-  }
-  finish(b, warp);
+  finish(w, warp, a.flags);
 }
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constant__ BwdArgs f) {
   using B = Bwd<DP>;
-  constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks;
+  constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks, kSets = B::kSets;
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t* sQ = smem;
-  uint8_t* sO = sQ + kTileBytes;
-  uint8_t* ring = sO + kTileBytes;
+  uint8_t* own = smem;                                // [kSets] Q, dO
+  uint8_t* ring = own + 2 * kSets * kTileBytes;       // K, V, K, V ..
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(ring + kSlots * kTileBytes);
   const AttnArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    init_bars(b);
+    init_bars(b, 1);
     for (const CUtensorMap* m : {&f.q, &f.k, &f.v, &f.dout}) tc::prefetch_map(m);
   }
   if (warp == 9) {
@@ -451,132 +489,115 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
   }
   __syncthreads();
   tc::fence_after();
-  const uint32_t cS = b->tmem, cP = cS + 256, cQ = cS + 384;    // S: two buffers
-  Role<kSlots> role = {b, lane, true, 0, 0};
+  const uint32_t cS = b->tmem, cP = cS + 256, cAcc = cS + 384;    // S: two buffers; per set: dQ
+  Warp<kSlots> w = {b, lane, true, 0, 0};
+  Turn<kSets> set;
+  Turn<2> buf;                                                    // of S
   Item it;
 
   if (warp == 8) {
-    // ---------------- TMA ----------------
-    uint32_t own = 0;
-    for (int64_t r = 0; role.ok && get_item(a, a.by_query, a.heads, r, it); ++r) {
-      if (!role.wait(&b->own_empty, own ^ 1u)) break;
-      const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
-      if (lane == 0) {
-        for (int i = 0; i < 2; ++i) {
-          tc::mbar_expect_tx(&b->own_full[i], kTileBytes);
-          b->own_issued[i] = own + 1;
-          load_rows(i ? sO : sQ, i ? &f.dout : &f.q, &b->own_full[i], row, it.head, kChunks);
-        }
-      }
-      __syncwarp();
-      own ^= 1u;
-      for (int j = 0; j <= it.blk && role.ok; ++j) {
-        const int64_t krow = it.start + static_cast<int64_t>(kTile) * j;
-        role.load(ring, kTileBytes, &f.k, krow, it.head / a.group, kChunks);
-        if (role.ok) role.load(ring, kTileBytes, &f.v, krow, it.head / a.group, kChunks);
-      }
-    }
-  } else if (warp == 9) {
-    // ---------------- MMA ----------------
-    uint32_t own = 0, free_phase = 0, ds_phase = 0, acc_phase = 0;
-    int buf = 0;                                              // S buffer of block j
-    const uint32_t q = tc::su32(sQ), o = tc::su32(sO);
-    auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-    for (int64_t r = 0; role.ok && get_item(a, a.by_query, a.heads, r, it); ++r) {
-      const int n = it.blk + 1;
-      const int last = it.len - kTile * it.blk;               // keys of the diagonal block
-      // the keys past the sequence's end become zeros
-      auto take_k = [&](int j) {
-        const int s = role.take();
-        if (role.ok && last < kTile && j == it.blk) zero_tail(ring + s * kTileBytes, last, kChunks, lane);
-        return s;
-      };
-      if (!role.wait(&b->own_full[0], own)) break;
-      int k = take_k(0);
-      if (!role.ok) break;
-      if (tc::elect_one()) {
-        product_ss<DP>(cS + 128 * buf, q, tile(k));
-        tc::mma_commit(&b->s_full[buf]);
-      }
-      __syncwarp();
-      if (!role.wait(&b->own_full[1], own)) break;
-      own ^= 1u;
-      int v = role.take();
-      // dP's columns are free once the previous item's last block has been read
-      if (!role.wait(&b->dp_free, free_phase ^ 1u)) break;
-      free_phase ^= 1u;
-      if (tc::elect_one()) {
-        product_ss<DP>(cP, o, tile(v));
-        tc::mma_commit(&b->dp_full);
-        tc::mma_commit(&b->empty[v]);
-        if (n == 1) tc::mma_commit(&b->own_empty);
-      }
-      __syncwarp();
-      if (!role.wait(&b->acc_empty, acc_phase ^ 1u)) break;
-      acc_phase ^= 1u;
-      for (int j = 0; j < n; ++j) {
-        int k2 = 0;
-        if (j + 1 < n) {
-          k2 = take_k(j + 1);
-          if (!role.ok) break;
-          if (tc::elect_one()) {
-            product_ss<DP>(cS + 128 * (buf ^ 1), q, tile(k2));
-            tc::mma_commit(&b->s_full[buf ^ 1]);
-          }
-          __syncwarp();
-          v = role.take();
-          if (!role.wait(&b->dp_free, free_phase ^ 1u)) break;
-          free_phase ^= 1u;
-          if (tc::elect_one()) {
-            product_ss<DP>(cP, o, tile(v));
-            tc::mma_commit(&b->dp_full);
-            tc::mma_commit(&b->empty[v]);
-            if (j + 2 == n) tc::mma_commit(&b->own_empty);
-          }
-          __syncwarp();
-        }
-        if (!role.wait(&b->ds_ready, ds_phase)) break;
-        ds_phase ^= 1u;
-        if (tc::elect_one()) {
-          product_ts<DP>(cQ, cS + 128 * buf, tile(k), j == 0, 32);
-          tc::mma_commit(&b->empty[k]);
-        }
-        __syncwarp();
-        k = k2;
-        buf ^= 1;
-      }
-      if (role.ok && tc::elect_one()) tc::mma_commit(&b->acc_full);
-      __syncwarp();
-    }
+    // ---------------- TMA (one thread), then the rows past the sequences ----------------
     if (tc::elect_one()) {
-      tc::mma_commit(&b->drain);
-      volatile int never = 0;
-      tc::mbar_wait(&b->drain, 0, &never);
+      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r, set.next()) {
+        const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
+        if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.q, &f.dout, row, it.head, kChunks)) break;
+        for (int j = 0; j <= it.blk && w.ok; ++j) {
+          const int64_t krow = it.start + static_cast<int64_t>(kTile) * j;
+          w.load(ring, kTileBytes, &f.k, krow, it.head / a.group, kChunks, kTile * (j + 1) > it.len);
+          if (w.ok) w.load(ring, kTileBytes, &f.v, krow, it.head / a.group, kChunks, false);
+        }
+      }
+    }
+    w.ok = __all_sync(0xffffffffu, w.ok);
+    zero_padding(a, a.dq, a.heads, blockIdx.x, gridDim.x, lane);
+  } else if (warp == 9) {
+    // ---------------- MMA (one thread): dQ(j), S(j + 2) ----------------
+    if (tc::elect_one()) {
+      uint32_t ds_phase = 0;
+      auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
+      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r, set.next()) {
+        const int n = it.blk + 1;
+        const uint32_t q = tc::su32(own + 2 * set.i * kTileBytes);
+        int k[2] = {0, 0};                                        // ring slots of K(j), K(j + 1)
+        auto scores = [&](int j, int& slot) {
+          slot = w.take();
+          w.next();                                               // V is the other chain's
+          if (!w.ok) return;
+          product_ss<DP>(cS + 128 * (buf.i ^ (j & 1)), q, tile(slot));
+          tc::mma_commit(&b->s_full[buf.i ^ (j & 1)]);
+          if (j + 1 == n) tc::mma_commit(&b->own_empty[set.i]);
+        };
+        if (!w.wait1(&b->own_full[set.i][0], set.parity)) break;
+        scores(0, k[0]);
+        if (n > 1 && w.ok) scores(1, k[1]);
+        if (!w.wait1(&b->acc_empty[set.i], set.parity ^ 1u)) break;
+        for (int j = 0; j < n; ++j) {
+          if (!w.wait1(&b->ds_ready, ds_phase)) break;
+          ds_phase ^= 1u;
+          product_ts<DP>(cAcc + DP * set.i, cS + 128 * (buf.i ^ (j & 1)), tile(k[0]), j == 0, 32);
+          tc::mma_commit(&b->empty[k[0]]);
+          k[0] = k[1];
+          if (j + 2 < n) {
+            scores(j + 2, k[1]);
+            if (!w.ok) break;
+          }
+        }
+        buf.i ^= n & 1;
+        if (w.ok) tc::mma_commit(&b->acc_full[set.i]);
+      }
+      w.drain(0);
     }
     __syncwarp();
-  } else if (warp >= 10) {
-    // ---------------- rows past the sequences ----------------
-    zero_padding(a, a.dq, a.heads, 2 * static_cast<int64_t>(blockIdx.x) + warp - 10, 2 * static_cast<int64_t>(gridDim.x),
-                 lane);
+    w.ok = __all_sync(0xffffffffu, w.ok);
+  } else if (warp == 11) {
+    // ---------------- MMA (one thread): dP(j) ----------------
+    if (tc::elect_one()) {
+      uint32_t free_phase = 0;
+      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r, set.next()) {
+        const uint32_t o = tc::su32(own + (2 * set.i + 1) * kTileBytes);
+        if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
+        for (int j = 0; j <= it.blk; ++j) {
+          w.next();
+          const int v = w.take();
+          // free once the last block's dP has been read
+          if (!w.wait1(&b->dp_free, free_phase ^ 1u)) break;
+          free_phase ^= 1u;
+          product_ss<DP>(cP, o, tc::su32(ring + v * kTileBytes));
+          tc::mma_commit(&b->dp_full);
+          tc::mma_commit(&b->empty[v]);
+          if (j == it.blk) tc::mma_commit(&b->own_empty[set.i]);
+        }
+      }
+      w.drain(1);
+    }
+    __syncwarp();
+    w.ok = __all_sync(0xffffffffu, w.ok);
+  } else if (warp == 10) {
+    // ---------------- sequence ends: K's rows past them become zeros ----------------
+    uint32_t seen = 0;
+    int next = 0;                                                 // ring slot of the item's first tile
+    for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r) {
+      const int rows = it.len - kTile * it.blk;
+      if (rows < kTile) w.end_tile(ring, kTileBytes, (next + 2 * it.blk) % kSlots, seen, rows, kChunks);
+      next = (next + 2 * (it.blk + 1)) % kSlots;
+    }
   } else {
     // ---------------- softmax ----------------
     const int half = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint64_t c2 = tc::pack2(a.scale_log2, a.scale_log2);
-    uint32_t s_phase[2] = {0, 0}, dp_phase = 0, acc_phase = 0;
-    int buf = 0;
-    for (int64_t r = 0; role.ok && get_item(a, a.by_query, a.heads, r, it); ++r) {
+    uint32_t dp_phase = 0;
+    for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r, set.next()) {
       const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk + row;
       const bool in = kTile * it.blk + row < it.len;
       const int64_t si = static_cast<int64_t>(it.head) * a.tokens + at;
       const float ls = in ? a.lse[si] * -kLog2e : -INFINITY, de = in ? a.delta[si] : 0.f;
       const uint64_t ls2 = tc::pack2(ls, ls);
-      for (int j = 0; j <= it.blk; ++j) {
-        const uint32_t mS = cS + 128 * buf + lanes + 64 * half, mP = cP + lanes + 64 * half;
-        if (!role.wait(&b->s_full[buf], buf ? s_phase[1] : s_phase[0])) break;
-        if (buf) s_phase[1] ^= 1u; else s_phase[0] ^= 1u;
+      for (int j = 0; j <= it.blk; ++j, buf.next()) {
+        const uint32_t mS = cS + 128 * buf.i + lanes + 64 * half, mP = cP + lanes + 64 * half;
+        if (!w.wait(&b->s_full[buf.i], buf.parity)) break;
         float p[64];
-        uint32_t w[32];
+        uint32_t pk[32];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t x[32];
@@ -590,42 +611,36 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
             p[32 * h + e + 1] = tc::exp2_fast(y1);
           }
         }
-        if (!role.wait(&b->dp_full, dp_phase)) break;
+        if (!w.wait(&b->dp_full, dp_phase)) break;
         dp_phase ^= 1u;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t x[32];
           tc::tmem_ld32(mP + 32 * h, x);
           tc::tmem_ld_wait();
-          if (h == 1) role.arrive(&b->dp_free);
+          if (h == 1) w.arrive(&b->dp_free);
 #pragma unroll
           for (int e = 0; e < 32; e += 2)
-            w[16 * h + e / 2] = pack_bf16x2(p[32 * h + e] * (__uint_as_float(x[e]) - de),
-                                            p[32 * h + e + 1] * (__uint_as_float(x[e + 1]) - de));
+            pk[16 * h + e / 2] = pack_bf16x2(p[32 * h + e] * (__uint_as_float(x[e]) - de),
+                                             p[32 * h + e + 1] * (__uint_as_float(x[e + 1]) - de));
         }
         if (j == it.blk) {   // query `row` sees keys .. row
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
-            if (64 * half + 2 * e > row) w[e] &= 0xFFFF0000u;
-            if (64 * half + 2 * e + 1 > row) w[e] &= 0x0000FFFFu;
+            if (64 * half + 2 * e > row) pk[e] &= 0xFFFF0000u;
+            if (64 * half + 2 * e + 1 > row) pk[e] &= 0x0000FFFFu;
           }
         }
-        tc::tmem_st32(mS, w);
+        tc::tmem_st32(mS, pk);
         tc::tmem_st_drain();
-        role.arrive(&b->ds_ready);
-        buf ^= 1;
+        w.arrive(&b->ds_ready);
       }
-      if (!role.wait(&b->acc_full, acc_phase)) break;
-      acc_phase ^= 1u;
-      store_acc<DP>(a.dq, cQ + lanes, at, in, it.head, half, a.scale, a.dim);
-      role.arrive(&b->acc_empty);
+      if (!w.wait(&b->acc_full[set.i], set.parity)) break;
+      store_acc<DP>(a.dq, cAcc + DP * set.i + lanes, at, in, it.head, half, a.scale, a.dim);
+      w.arrive(&b->acc_empty[set.i]);
     }
   }
-  if (!role.ok && lane == 0) {
-    *static_cast<volatile int*>(&b->abort) = 1;
-    raise_flag(a.flags, kFlagTimeout);
-  }
-  finish(b, warp);
+  finish(w, warp, a.flags);
 }
 
 template <typename K>

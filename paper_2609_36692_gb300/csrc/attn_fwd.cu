@@ -30,14 +30,15 @@
 namespace normpre {
 namespace {
 
-constexpr int kThreads = 384;   // softmax 2 x 4 warps, TMA, MMA, two for the padding rows
+constexpr int kThreads = 384;   // softmax 2 x 4 warps, TMA, MMA of tile 0, sequence ends, MMA of tile 1
 constexpr float kGrow = 8.f;    // log2 of the growth that raises the maximum
 
 template <int DP> struct Fwd {
   static constexpr int kChunks = DP / 64;
   static constexpr int kTileBytes = kChunks * kChunk;
   static constexpr int kSlots = DP == 128 ? 5 : 10;    // K / V ring
-  static constexpr size_t kSmem = 1024 + (2 + kSlots) * kTileBytes + 512;
+  static constexpr int kAcc = DP == 128 ? 1 : 2;       // output accumulators of a tile
+  static constexpr size_t kSmem = (2 + kSlots) * kTileBytes + 1024;
 };
 
 struct FwdArgs {
@@ -48,11 +49,22 @@ struct FwdArgs {
   int pair_heads;  // the two tiles are two heads of a group
 };
 
+template <int kSlots> struct Bars {
+  // raw: a tile that ends its sequence lands here first; once its tail is
+  // zeroed it counts as full
+  uint64_t full[kSlots], empty[kSlots], raw[kSlots];
+  uint64_t q_full[2], q_empty[2], s_full[2], p_ready[2][2], pv_done[2], o_empty[2][2], drain[2];
+  uint32_t tmem;
+  int abort;
+  uint32_t issued[kSlots], raw_issued[kSlots], q_issued[2];   // last parity + 1
+};
+
 struct Item {
   int64_t start;   // the sequence's first row
   int len;
-  int blk[2];      // the tiles' block in the sequence, -1: no tile
-  int head[2];
+  int top;         // the topmost block of keys
+  int blk0, blk1;  // the tiles' block in the sequence, -1: no tile
+  int head0, head1;
   int kvh;
 };
 
@@ -64,72 +76,66 @@ __device__ __forceinline__ bool get_item(const FwdArgs& f, int64_t r, Item& it) 
   const int h = static_cast<int>(i % per);
   it.start = b.start;
   it.len = b.len;
+  it.blk0 = b.blk;
   if (f.pair_heads) {
-    it.blk[0] = it.blk[1] = b.blk;
-    it.head[0] = 2 * h;
-    it.head[1] = 2 * h + 1;
+    it.blk1 = b.blk;
+    it.head0 = 2 * h;
+    it.head1 = 2 * h + 1;
   } else {
-    it.blk[0] = b.blk;
-    it.blk[1] = (b.blk + 1) * kTile < b.len ? b.blk + 1 : -1;
-    it.head[0] = it.head[1] = h;
+    it.blk1 = (b.blk + 1) * kTile < b.len ? b.blk + 1 : -1;
+    it.head0 = it.head1 = h;
   }
-  it.kvh = it.head[0] / f.a.group;
+  it.top = max(it.blk0, it.blk1);
+  it.kvh = it.head0 / f.a.group;
   return true;
 }
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_constant__ FwdArgs f) {
   using F = Fwd<DP>;
-  constexpr int kSlots = F::kSlots, kTileBytes = F::kTileBytes, kChunks = F::kChunks;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  constexpr int kSlots = F::kSlots, kTileBytes = F::kTileBytes, kChunks = F::kChunks, kAcc = F::kAcc;
+  extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* sQ = smem;                          // [2]
-  uint8_t* sKV = smem + 2 * kTileBytes;        // [kSlots]
-  uint64_t* kv_full = reinterpret_cast<uint64_t*>(sKV + kSlots * kTileBytes);
-  uint64_t* kv_empty = kv_full + kSlots;
-  uint64_t* q_full = kv_empty + kSlots;        // [2], as the following ones
-  uint64_t* q_empty = q_full + 2;
-  uint64_t* s_full = q_empty + 2;
-  uint64_t* p_ready = s_full + 2;
-  uint64_t* pv_done = p_ready + 2;
-  uint64_t* o_empty = pv_done + 2;
-  uint64_t* drain = o_empty + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  uint32_t* issued = tmem_slot + 2;            // [kSlots + 2]: last parity + 1 of kv_full and q_full
+  uint8_t* ring = smem + 2 * kTileBytes;       // [kSlots]
+  Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(ring + kSlots * kTileBytes);
+  static_assert(sizeof(Bars<kSlots>) <= 1024, "barriers");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) {
-      tc::mbar_init(&kv_full[i], 1);
-      tc::mbar_init(&kv_empty[i], 1);
+      tc::mbar_init(&b->full[i], 1);
+      tc::mbar_init(&b->empty[i], 2);          // both tiles' MMAs
+      tc::mbar_init(&b->raw[i], 1);
+      b->issued[i] = b->raw_issued[i] = 0;
     }
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(&q_full[i], 1);
-      tc::mbar_init(&q_empty[i], 1);
-      tc::mbar_init(&s_full[i], 1);
-      tc::mbar_init(&p_ready[i], 4);
-      tc::mbar_init(&pv_done[i], 1);
-      tc::mbar_init(&o_empty[i], 4);
+      tc::mbar_init(&b->q_full[i], 1);
+      tc::mbar_init(&b->q_empty[i], 1);
+      tc::mbar_init(&b->s_full[i], 1);
+      tc::mbar_init(&b->p_ready[i][0], 4);
+      tc::mbar_init(&b->p_ready[i][1], 4);
+      tc::mbar_init(&b->pv_done[i], 1);
+      tc::mbar_init(&b->o_empty[i][0], 4);
+      tc::mbar_init(&b->o_empty[i][1], 4);
+      tc::mbar_init(&b->drain[i], 1);
+      b->q_issued[i] = 0;
     }
-    tc::mbar_init(drain, 1);
-    for (int i = 0; i < kSlots + 2; ++i) issued[i] = 0;
-    *abort_flag = 0;
+    b->abort = 0;
     tc::fence_barrier_init();
     tc::prefetch_map(&f.q);
     tc::prefetch_map(&f.k);
     tc::prefetch_map(&f.v);
   }
   if (warp == 9) {
-    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_alloc(&b->tmem, 512);
     tc::tmem_relinquish();
     tc::fence_before();
   }
   __syncthreads();
   tc::fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = b->tmem;
   auto s_col = [&](int s) { return tmem + static_cast<uint32_t>(128 * s); };
-  auto o_col = [&](int s) { return tmem + static_cast<uint32_t>(256 + DP * s); };
+  auto o_col = [&](int s, int acc) { return tmem + static_cast<uint32_t>(256 + DP * (kAcc * s + acc)); };
   bool ok = true;
   Item it;
 
@@ -137,133 +143,134 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
   if (warp >= 8) {
     tc::regs_fewer<96>();
     if (warp == 8) {
-      // ---------------- TMA ----------------
-      int slot = 0;
-      uint32_t phase = 0, q_phase[2] = {0, 0};
-      auto load_kv = [&](const CUtensorMap* map, int64_t row, int head) {
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(&kv_empty[slot], phase ^ 1u, abort_flag));
-        if (!ok) return;
-        if (lane == 0) {
-          tc::mbar_expect_tx(&kv_full[slot], kTileBytes);
-          issued[slot] = phase + 1;
-          load_rows(sKV + slot * kTileBytes, map, &kv_full[slot], row, head, kChunks);
-        }
-        __syncwarp();
-        if (++slot == kSlots) { slot = 0; phase ^= 1u; }
-      };
-      for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
-        for (int s = 0; s < 2 && ok; ++s) {
-          if (it.blk[s] < 0) continue;
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(&q_empty[s], q_phase[s] ^ 1u, abort_flag));
-          if (!ok) break;
-          if (lane == 0) {
-            tc::mbar_expect_tx(&q_full[s], kTileBytes);
-            issued[kSlots + s] = q_phase[s] + 1;
-            load_rows(sQ + s * kTileBytes, &f.q, &q_full[s], it.start + kTile * it.blk[s], it.head[s], kChunks);
-          }
-          __syncwarp();
-          q_phase[s] ^= 1u;
-          if (s == 0) load_kv(&f.k, it.start + static_cast<int64_t>(kTile) * max(it.blk[0], it.blk[1]), it.kvh);
-        }
-        for (int j = max(it.blk[0], it.blk[1]); j >= 0 && ok; --j) {
-          const int64_t row = it.start + static_cast<int64_t>(kTile) * j;
-          load_kv(&f.v, row, it.kvh);
-          if (j > 0 && ok) load_kv(&f.k, row - kTile, it.kvh);
-        }
-      }
-      if (!ok && lane == 0) { *abort_flag = 1; raise_flag(f.a.flags, kFlagTimeout); }
-    } else if (warp == 9) {
-      // ---------------- MMA ----------------
-      int slot = 0;
-      uint32_t phase = 0;
-      uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, o_phase[2] = {0, 0};
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, abort_flag));
-        tc::fence_after();
-        return ok;
-      };
-      // slot of the next tile of the ring, once it has arrived
-      auto take_kv = [&]() {
-        const int s = slot;
-        wait(&kv_full[s], phase);
-        if (++slot == kSlots) { slot = 0; phase ^= 1u; }
-        return s;
-      };
-      auto scores = [&](int s, int kslot) {   // S_s = Q_s K^T
-        if (tc::elect_one()) {
-          product_ss<DP>(s_col(s), tc::su32(sQ + s * kTileBytes), tc::su32(sKV + kslot * kTileBytes));
-          tc::mma_commit(&s_full[s]);
-        }
-        __syncwarp();
-      };
-      for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
-        const int top = max(it.blk[0], it.blk[1]);
-        const int krows = min(kTile, it.len - kTile * top);   // keys of the topmost block
-        int kslot = take_kv();
-        for (int s = 0; s < 2 && ok; ++s) {
-          if (it.blk[s] < 0) continue;
-          if (!wait(&q_full[s], q_phase[s])) break;
-          q_phase[s] ^= 1u;
-          if (it.blk[s] == top) scores(s, kslot);
-        }
-        if (!ok) break;
-        if (tc::elect_one()) {
-          tc::mma_commit(&kv_empty[kslot]);
-          if (top == 0)
-            for (int s = 0; s < 2; ++s)
-              if (it.blk[s] >= 0) tc::mma_commit(&q_empty[s]);
-        }
-        __syncwarp();
-        for (int j = top; j >= 0 && ok; --j) {
-          const int vslot = take_kv();
-          if (!ok) break;
-          if (j == top && krows < kTile) zero_tail(sKV + vslot * kTileBytes, krows, kChunks, lane);
-          if (j > 0) {
-            kslot = take_kv();
-            if (!ok) break;
-          }
-          for (int s = 0; s < 2 && ok; ++s) {
-            if (j <= it.blk[s]) {
-              if (!wait(&p_ready[s], p_phase[s])) break;
-              p_phase[s] ^= 1u;
-              if (j == it.blk[s]) {
-                if (!wait(&o_empty[s], o_phase[s] ^ 1u)) break;
-                o_phase[s] ^= 1u;
-              }
-              if (tc::elect_one()) {   // O_s += P_s V
-                product_ts<DP>(o_col(s), s_col(s), tc::su32(sKV + vslot * kTileBytes), j == it.blk[s], 0);
-                tc::mma_commit(&pv_done[s]);
-              }
-              __syncwarp();
-            }
-            if (j > 0 && j - 1 <= it.blk[s]) scores(s, kslot);
-          }
-          if (!ok) break;
-          if (tc::elect_one()) {
-            tc::mma_commit(&kv_empty[vslot]);
-            if (j > 0) tc::mma_commit(&kv_empty[kslot]);
-            if (j == 1)
-              for (int s = 0; s < 2; ++s)
-                if (it.blk[s] >= 0) tc::mma_commit(&q_empty[s]);
-          }
-          __syncwarp();
-        }
-      }
-      if (!ok && lane == 0) { *abort_flag = 1; raise_flag(f.a.flags, kFlagTimeout); }
-      // every MMA issued has completed once `drain` fires
+      // ---------------- TMA (one thread), then the rows past the sequences ----------------
       if (tc::elect_one()) {
-        tc::mma_commit(drain);
-        volatile int never = 0;
-        tc::mbar_wait(drain, 0, &never);
+        int slot = 0;
+        uint32_t phase = 0, q_phase[2] = {0, 0};
+        auto load = [&](const CUtensorMap* map, int64_t row, int head, bool tail) {
+          ok = ok && tc::mbar_wait(&b->empty[slot], phase ^ 1u, &b->abort);
+          if (!ok) return;
+          uint64_t* bar = tail ? &b->raw[slot] : &b->full[slot];
+          tc::mbar_expect_tx(bar, kTileBytes);
+          if (tail) ++b->raw_issued[slot];
+          else b->issued[slot] = phase + 1;
+          load_rows(ring + slot * kTileBytes, map, bar, row, head, kChunks);
+          if (++slot == kSlots) { slot = 0; phase ^= 1u; }
+        };
+        for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const int blk = s ? it.blk1 : it.blk0;
+            if (blk >= 0) {
+              ok = ok && tc::mbar_wait(&b->q_empty[s], q_phase[s] ^ 1u, &b->abort);
+              if (!ok) break;
+              tc::mbar_expect_tx(&b->q_full[s], kTileBytes);
+              b->q_issued[s] = q_phase[s] + 1;
+              load_rows(sQ + s * kTileBytes, &f.q, &b->q_full[s], it.start + kTile * blk, s ? it.head1 : it.head0, kChunks);
+              q_phase[s] ^= 1u;
+            }
+            if (s == 0) load(&f.k, it.start + static_cast<int64_t>(kTile) * it.top, it.kvh, false);
+          }
+          for (int j = it.top; j >= 0 && ok; --j) {
+            const int64_t row = it.start + static_cast<int64_t>(kTile) * j;
+            load(&f.v, row, it.kvh, kTile * (j + 1) > it.len);
+            if (j > 0) load(&f.k, row - kTile, it.kvh, false);
+          }
+        }
+      }
+      ok = __all_sync(0xffffffffu, ok);
+      zero_padding(f.a, f.a.o, f.a.heads, blockIdx.x, gridDim.x, lane);
+      const int64_t pad = f.a.tokens - f.a.total;
+      for (int64_t i = 32 * static_cast<int64_t>(blockIdx.x) + lane; i < pad * f.a.heads; i += 32 * static_cast<int64_t>(gridDim.x))
+        f.a.lse[(i / pad) * f.a.tokens + f.a.total + i % pad] = -INFINITY;
+    } else if (warp == 10) {
+      // ---------------- sequence ends: V's rows past them become zeros ----------------
+      int next = 0;             // ring slot of the item's first tile
+      uint32_t seen = 0;        // per slot, parity of its raw barrier
+      for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
+        const int rows = it.len - kTile * it.top;
+        if (rows < kTile) {
+          const int slot = next + 1 == kSlots ? 0 : next + 1;
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&b->raw[slot], (seen >> slot) & 1u, &b->abort));
+          seen ^= 1u << slot;
+          if (!ok) break;
+          zero_tail(ring + slot * kTileBytes, rows, kChunks, lane);
+          if (lane == 0) tc::mbar_arrive(&b->full[slot]);
+        }
+        next = (next + 2 * (it.top + 1)) % kSlots;
+      }
+    } else {
+      // ---------------- MMA of one tile (one thread) ----------------
+      // The two tiles are issued by two warps: a thread's MMAs run almost as it
+      // issues them, so that its waits leave the tensor cores to the other.
+      const int s = warp == 11;
+      if (tc::elect_one()) {
+        int slot = 0, acc = 0;
+        uint32_t phase = 0, q_phase = 0, p_phase = 0, o_phase = 0;
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+          ok = ok && tc::mbar_wait(bar, parity, &b->abort);
+          tc::fence_after();
+          return ok;
+        };
+        // next tile of the ring, once it has arrived
+        auto take = [&]() {
+          const int t = slot;
+          wait(&b->full[t], phase);
+          if (++slot == kSlots) { slot = 0; phase ^= 1u; }
+          return t;
+        };
+        auto scores = [&](int k) {   // S = Q K^T
+          product_ss<DP>(s_col(s), tc::su32(sQ + s * kTileBytes), tc::su32(ring + k * kTileBytes));
+          tc::mma_commit(&b->s_full[s]);
+          tc::mma_commit(&b->empty[k]);
+        };
+        for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
+          const int blk = s ? it.blk1 : it.blk0;
+          int k = take();
+          for (int j = it.top; ok; --j) {
+            // scores of block j
+            if (j <= blk) {
+              if (j == blk) {
+                if (!wait(&b->q_full[s], q_phase)) break;
+                q_phase ^= 1u;
+              }
+              scores(k);
+              if (j == 0) tc::mma_commit(&b->q_empty[s]);
+            } else {
+              tc::mbar_arrive(&b->empty[k]);
+            }
+            // O += P V of the block before it in the walk has been issued; this block's
+            const int v = take();
+            if (!ok) break;
+            if (j <= blk) {
+              if (j == blk) {
+                const uint32_t parity = kAcc == 2 ? (o_phase >> acc) & 1u : o_phase;
+                if (!wait(&b->o_empty[s][acc], parity ^ 1u)) break;
+                o_phase ^= kAcc == 2 ? 1u << acc : 1u;
+              }
+              const uint32_t o = o_col(s, acc), p = s_col(s);
+              if (!wait(&b->p_ready[s][0], p_phase)) break;
+              product_ts<DP, 0, 4>(o, p, tc::su32(ring + v * kTileBytes), j == blk, 0);
+              if (!wait(&b->p_ready[s][1], p_phase)) break;
+              product_ts<DP, 4, 8>(o, p, tc::su32(ring + v * kTileBytes), false, 0);
+              p_phase ^= 1u;
+              tc::mma_commit(&b->pv_done[s]);
+              tc::mma_commit(&b->empty[v]);
+            } else {
+              tc::mbar_arrive(&b->empty[v]);
+            }
+            if (j == 0) break;
+            k = take();
+          }
+          if (blk >= 0 && kAcc == 2) acc ^= 1;
+        }
+        // every MMA issued has completed once `drain` fires
+        tc::mma_commit(&b->drain[s]);
+        int never = 0;
+        tc::mbar_wait(&b->drain[s], 0, &never);
       }
       __syncwarp();
-    } else if (warp >= 10) {
-      // ---------------- rows past the sequences ----------------
-      const int64_t w = static_cast<int64_t>(blockIdx.x) * 2 + warp - 10, n = 2 * static_cast<int64_t>(gridDim.x);
-      zero_padding(f.a, f.a.o, f.a.heads, w, n, lane);
-      const int64_t pad = f.a.tokens - f.a.total;
-      for (int64_t i = w * 32 + lane; i < pad * f.a.heads; i += 32 * n)
-        f.a.lse[(i / pad) * f.a.tokens + f.a.total + i % pad] = -INFINITY;
+      ok = __all_sync(0xffffffffu, ok);
     }
   } else {
     // ---------------- softmax: warps 0-3 tile 0, warps 4-7 tile 1 ----------------
@@ -271,60 +278,50 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
     const int s = warp >> 2, q4 = warp & 3;
     const int row = 32 * q4 + lane;                       // of the tile
     const uint32_t lanes = static_cast<uint32_t>(q4 * 32) << 16;
-    const uint32_t sc = s_col(s) + lanes, oc = o_col(s) + lanes;
+    const uint32_t sc = s_col(s) + lanes;
     const float c = f.a.scale_log2;
-    uint32_t s_phase = 0, pv = 0;                         // score tiles seen, products P V before this block
+    const uint64_t c2 = tc::pack2(c, c);
+    uint32_t s_phase = 0, pv = 0;                         // products P V before this block
+    int acc = 0;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, abort_flag));
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, &b->abort));
       tc::fence_after();
       return ok;
     };
     for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
-      const int blk = it.blk[s];
+      const int blk = s ? it.blk1 : it.blk0;
       if (blk < 0) continue;
+      const uint32_t oc = o_col(s, acc) + lanes;
       float m = -INFINITY, l = 0.f;
       for (int j = blk; j >= 0; --j) {
-        if (!wait(&s_full[s], s_phase)) break;
+        if (!wait(&b->s_full[s], s_phase)) break;
         s_phase ^= 1u;
         uint32_t x[128];
 #pragma unroll
         for (int i = 0; i < 4; ++i) tc::tmem_ld32(sc + 32 * i, x + 32 * i);
         tc::tmem_ld_wait();
+        auto top = [&]() {
+          float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 128; i += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              t[e] = fmaxf(fmaxf(t[e], __uint_as_float(x[i + 2 * e])), __uint_as_float(x[i + 2 * e + 1]));
+          return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+        };
         if (j == blk) {
 #pragma unroll
           for (int i = 0; i < 128; ++i)
             if (i > row) x[i] = 0xFF800000u;
+          m = top();
         }
-        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int i = 0; i < 128; i += 8)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            t[e] = fmaxf(fmaxf(t[e], __uint_as_float(x[i + 2 * e])), __uint_as_float(x[i + 2 * e + 1]));
-        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-        if (j == blk) {
-          m = top;
-        } else if (__any_sync(0xffffffffu, (top - m) * c > kGrow)) {
-          const float up = fmaxf(m, top), keep = tc::exp2_fast((m - up) * c);
-          m = up;
-          l *= keep;
-          if (!wait(&pv_done[s], (pv - 1) & 1u)) break;
-#pragma unroll 1
-          for (int i = 0; i < DP; i += 32) {
-            uint32_t o[32];
-            tc::tmem_ld32(oc + i, o);
-            tc::tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-            tc::tmem_st32(oc + i, o);
-          }
-        }
-        const float mc = -m * c;
-        const uint64_t c2 = tc::pack2(c, c), mc2 = tc::pack2(mc, mc);
-        uint64_t sum[2] = {0, 0};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t p[32];
+        // half of the row's exponentials with the running maximum, into P
+        uint32_t p[32];
+        uint64_t sum[2];
+        auto half = [&](int h) {
+          const float mc = -m * c;
+          const uint64_t mc2 = tc::pack2(mc, mc);
+          sum[0] = sum[1] = 0;
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             float lo, hi;
@@ -335,22 +332,55 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
             sum[i & 1] = tc::add2(sum[i & 1], tc::pack2(lo, hi));
             p[i] = pack_bf16x2(lo, hi);
           }
+        };
+        auto add_sum = [&]() {
+          float lo, hi;
+          tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
+          l += lo + hi;
+        };
+        auto release = [&](int h) {
           tc::tmem_st32(sc + 32 * h, p);
+          tc::tmem_st_drain();
+          tc::fence_before();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&b->p_ready[s][h]);
+        };
+        // The maximum of a later block is needed only to see whether the
+        // running one must be raised, which is rare: its comparisons run in
+        // the shadow of the exponentials.
+        half(0);
+        if (j != blk) {
+          const float up = fmaxf(m, top());
+          if (__any_sync(0xffffffffu, (up - m) * c > kGrow)) {
+            const float keep = tc::exp2_fast((m - up) * c);
+            m = up;
+            l *= keep;
+            if (!wait(&b->pv_done[s], (pv - 1) & 1u)) break;
+#pragma unroll 1
+            for (int i = 0; i < DP; i += 32) {
+              uint32_t o[32];
+              tc::tmem_ld32(oc + i, o);
+              tc::tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+              tc::tmem_st32(oc + i, o);
+            }
+            half(0);
+          }
         }
-        tc::tmem_st_drain();
-        tc::fence_before();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&p_ready[s]);
-        float lo, hi;
-        tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
-        l += lo + hi;
+        add_sum();
+        release(0);
+        half(1);
+        release(1);
+        add_sum();
         ++pv;
       }
-      if (!ok || !wait(&pv_done[s], (pv - 1) & 1u)) break;
+      if (!ok || !wait(&b->pv_done[s], (pv - 1) & 1u)) break;
       const float inv = 1.f / l;
       const int i = kTile * blk + row;                    // of the sequence
       const int64_t at = it.start + i;
-      bf16* out = static_cast<bf16*>(f.a.o.p) + at * f.a.o.ts + it.head[s] * f.a.o.hs;
+      const int head = s ? it.head1 : it.head0;
+      bf16* out = static_cast<bf16*>(f.a.o.p) + at * f.a.o.ts + head * f.a.o.hs;
 #pragma unroll 1
       for (int d = 0; d < DP; d += 32) {
         uint32_t o[32];
@@ -360,18 +390,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       }
       tc::fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&o_empty[s]);
-      if (i < it.len) f.a.lse[static_cast<int64_t>(it.head[s]) * f.a.tokens + at] = (m * c + log2f(l)) * 0.6931471805599453f;
+      if (lane == 0) tc::mbar_arrive(&b->o_empty[s][acc]);
+      if (kAcc == 2) acc ^= 1;
+      if (i < it.len) f.a.lse[static_cast<int64_t>(head) * f.a.tokens + at] = (m * c + log2f(l)) * 0.6931471805599453f;
     }
-    if (!ok && lane == 0) { *abort_flag = 1; raise_flag(f.a.flags, kFlagTimeout); }
+  }
+  if (!ok && lane == 0) {
+    *static_cast<volatile int*>(&b->abort) = 1;
+    raise_flag(f.a.flags, kFlagTimeout);
   }
 
   __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag) {
+  if (threadIdx.x == 0 && *static_cast<volatile int*>(&b->abort)) {
     // let every TMA copy still in flight land before the CTA exits
-    volatile int never = 0;
-    for (int i = 0; i < kSlots + 2; ++i)
-      if (issued[i]) tc::mbar_wait(i < kSlots ? &kv_full[i] : &q_full[i - kSlots], issued[i] - 1, &never);
+    int never = 0;
+    for (int i = 0; i < kSlots; ++i) {
+      if (b->issued[i]) tc::mbar_wait(&b->full[i], b->issued[i] - 1, &never);
+      if (b->raw_issued[i]) tc::mbar_wait(&b->raw[i], (b->raw_issued[i] - 1) & 1u, &never);
+    }
+    for (int i = 0; i < 2; ++i)
+      if (b->q_issued[i]) tc::mbar_wait(&b->q_full[i], b->q_issued[i] - 1, &never);
   }
   __syncthreads();
   if (warp == 9) {

@@ -47,14 +47,15 @@ __device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b) {
 #pragma unroll
   for (int kk = 0; kk < DP / 16; ++kk) tc::mma_bf16(d, ad + cols_step(kk), bd + cols_step(kk), idesc, kk != 0);
 }
-// D (+)= A B over 128 rows of B: A in TMEM, its columns 64 .. 127 `gap` columns further on.
-template <int DP>
+// D (+)= A B over rows 16 K0 .. 16 K1 of B: A in TMEM, its columns 64 .. 127
+// `gap` columns further on.
+template <int DP, int K0 = 0, int K1 = 8>
 __device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, bool first, int gap) {
   constexpr uint32_t idesc = tc::idesc_bf16(kTile, DP, 0, 1);
   const uint64_t bd = desc_rows(b);
 #pragma unroll
-  for (int kk = 0; kk < kTile / 16; ++kk)
-    tc::mma_bf16_ta(d, a + kk * 8 + (kk >= 4 ? gap : 0), bd + rows_step(kk), idesc, !first || kk != 0);
+  for (int kk = K0; kk < K1; ++kk)
+    tc::mma_bf16_ta(d, a + kk * 8 + (kk >= 4 ? gap : 0), bd + rows_step(kk), idesc, !first || kk != K0);
 }
 
 // Zeroes rows [rows, 128) of a tile in shared memory (one warp): what follows

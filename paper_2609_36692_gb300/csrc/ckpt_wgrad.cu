@@ -223,17 +223,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
       }
     }
   } else if (warp == 13) {
-    // ---------------- MMA ----------------
-    constexpr uint32_t idesc = tc::idesc_bf16(kTileK, kTileN, 1, 1);
-    int st = 0, xb = 0, acc = 0;
-    uint32_t phase = 0, xphase = 0, tphase = 0;
-    for (int u = unit0; u < f.units && ok; u += nunits) {
-      if (!wait(&b->tempty[acc], tphase ^ 1u)) break;
-      tc::fence_after();
-      for (int s = s0; s < s1; ++s) {
-        if (!wait(&b->full[st], phase) || !wait(&b->xfull[xb], xphase)) break;
-        tc::fence_after();
-        if (tc::elect_one()) {
+    // ---------------- MMA (one thread) ----------------
+    if (tc::elect_one()) {
+      constexpr uint32_t idesc = tc::idesc_bf16(kTileK, kTileN, 1, 1);
+      int st = 0, xb = 0, acc = 0, never = 0;
+      uint32_t phase = 0, xphase = 0, tphase = 0;
+      auto wait1 = [&](uint64_t* bar, uint32_t parity) { return ok = ok && tc::mbar_wait(bar, parity, &b->abort); };
+      for (int u = unit0; u < f.units && ok; u += nunits) {
+        if (!wait1(&b->tempty[acc], tphase ^ 1u)) break;
+        for (int s = s0; s < s1; ++s) {
+          if (!wait1(&b->full[st], phase) || !wait1(&b->xfull[xb], xphase)) break;
+          tc::fence_after();
           const uint64_t dy = tc::sdesc(tc::su32(ring + st * kStageBytes), kBox, 1024);
           const uint64_t x = tc::sdesc(tc::su32(xbuf + xb * kXBytes), kBox, 1024);
 #pragma unroll
@@ -242,24 +242,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
           if (SPLIT) tc::mma_commit(&b->empty[st]);
           else tc::mma_commit_mc(&b->empty[st], 3);
           tc::mma_commit(&b->xempty[xb]);
+          if (++st == kRing) { st = 0; phase ^= 1u; }
+          if (++xb == kXbuf) { xb = 0; xphase ^= 1u; }
         }
-        __syncwarp();
-        if (++st == kRing) { st = 0; phase ^= 1u; }
-        if (++xb == kXbuf) { xb = 0; xphase ^= 1u; }
+        if (!ok) break;
+        tc::mma_commit(&b->tfull[acc]);
+        acc ^= 1;
+        if (acc == 0) tphase ^= 1u;
       }
-      if (!ok) break;
-      if (tc::elect_one()) tc::mma_commit(&b->tfull[acc]);
-      __syncwarp();
-      acc ^= 1;
-      if (acc == 0) tphase ^= 1u;
-    }
-    // every MMA issued has completed once `drain` fires
-    if (tc::elect_one()) {
+      // every MMA issued has completed once `drain` fires
       tc::mma_commit(&b->drain);
-      volatile int never = 0;
       tc::mbar_wait(&b->drain, 0, &never);
     }
     __syncwarp();
+    ok = __all_sync(0xffffffffu, ok);
   } else if (warp >= 4) {
     // ---------------- codes -> bf16 ----------------
     // 8 rows x 4 blocks per warp: lanes of 8 rows, whose 16-byte pieces the
