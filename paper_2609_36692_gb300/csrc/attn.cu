@@ -4,9 +4,13 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstring>
+#include <functional>
+#include <iterator>
 #include <memory>
 #include <new>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "../../include/normpre.h"
@@ -21,13 +25,26 @@ struct normpre_attn {
   int64_t max_blocks = 0;
   int n_blocks = 0, n_pairs = 0;
   int64_t total = 0;
-  void* lists = nullptr;       // three AttnBlock[max_blocks]
-  float* delta = nullptr;      // [n_heads][max_tokens]
+  // work lists of the current lengths, one block of memory: by_query, by_key,
+  // by_pair, then the walks
+  char* lists = nullptr;
+  char* staging = nullptr;         // pinned, the same size
+  cudaEvent_t copied = nullptr;    // the last copy out of `staging`
+  int64_t walk_at[3] = {-1, -1, -1};   // byte offsets of the walks, -1: none
+  float* delta = nullptr;          // [n_heads][max_tokens]
   int* flags = nullptr;
-  std::vector<AttnBlock> host; // staging of `lists`
 };
 
 namespace {
+
+// Up to this many items a kernel's items are dealt out to the CTAs on the host;
+// beyond it every CTA has dozens, and a fixed back-and-forth walk is as even.
+constexpr int64_t kMaxDealt = 8192;
+constexpr int64_t kWalkInts = kMaxDealt + 1024;   // most of one walk
+
+int64_t list_bytes(const normpre_attn* a) {
+  return 3 * (a->max_blocks * static_cast<int64_t>(sizeof(AttnBlock)) + kWalkInts * static_cast<int64_t>(sizeof(int)));
+}
 
 int fail(int code, const std::string& msg) {
   set_thread_error(msg);
@@ -39,6 +56,8 @@ int cuda_fail(cudaError_t e, const char* what) {
 
 void release(normpre_attn* a) {
   cudaFree(a->lists);
+  if (a->staging) cudaFreeHost(a->staging);
+  if (a->copied) cudaEventDestroy(a->copied);
   cudaFree(a->delta);
   cudaFree(a->flags);
   delete a;
@@ -73,10 +92,12 @@ int take(const normpre_attn* a, const normpre_heads* t, int64_t tokens, int head
 
 AttnArgs base_args(const normpre_attn* a, int64_t tokens) {
   AttnArgs g = {};
-  const AttnBlock* lists = static_cast<const AttnBlock*>(a->lists);
-  g.by_query = lists;
-  g.by_key = lists + a->max_blocks;
-  g.by_pair = lists + 2 * a->max_blocks;
+  g.by_query = reinterpret_cast<const AttnBlock*>(a->lists);
+  g.by_key = g.by_query + a->n_blocks;
+  g.by_pair = g.by_key + a->n_blocks;
+  const int** walks[3] = {&g.walk_fwd, &g.walk_dkdv, &g.walk_dq};
+  for (int i = 0; i < 3; ++i)
+    *walks[i] = a->walk_at[i] < 0 ? nullptr : reinterpret_cast<const int*>(a->lists + a->walk_at[i]);
   g.n_blocks = a->n_blocks;
   g.n_pairs = a->n_pairs;
   g.total = static_cast<int>(a->total);
@@ -98,6 +119,28 @@ int check_tokens(const normpre_attn* a, int64_t tokens) {
   return NORMPRE_OK;
 }
 
+// Deals out the items of a kernel, given in falling order of cost (`per` items
+// for each entry of `costs`): each goes to the CTA with the least so far.
+void deal(const std::vector<int>& costs, int per, std::vector<int>* out) {
+  const int64_t items = static_cast<int64_t>(costs.size()) * per;
+  const int grid = walk_grid(items);
+  std::vector<std::pair<int64_t, int>> heap;                 // load, CTA; the least on top
+  for (int c = 0; c < grid; ++c) heap.push_back({0, c});
+  const auto more = std::greater<std::pair<int64_t, int>>();
+  std::vector<int> owner(items), count(grid + 1, 0);
+  for (int64_t i = 0; i < items; ++i) {
+    std::pop_heap(heap.begin(), heap.end(), more);
+    owner[i] = heap.back().second;
+    heap.back().first += costs[i / per];
+    ++count[owner[i] + 1];
+    std::push_heap(heap.begin(), heap.end(), more);
+  }
+  for (int c = 0; c < grid; ++c) count[c + 1] += count[c];
+  out->assign(grid + 1 + items, 0);
+  std::copy(count.begin(), count.end(), out->begin());
+  for (int64_t i = 0; i < items; ++i) (*out)[grid + 1 + count[owner[i]]++] = static_cast<int>(i);
+}
+
 int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_t s) {
   int64_t total = 0;
   for (int i = 0; i < n_seqs; ++i) {
@@ -112,31 +155,49 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
       blocks.push_back(AttnBlock{static_cast<int>(start), static_cast<int>(lengths[i]), static_cast<int>(b), 0});
     start += lengths[i];
   }
-  const size_t n = blocks.size();
-  // longest work first: the last CTAs to start then have little to do
-  auto keys = [](const AttnBlock& b) { return b.blk; };
+  // longest work first
   auto queries = [](const AttnBlock& b) { return (b.len - 1) / 128 - b.blk; };
-  std::stable_sort(blocks.begin(), blocks.end(),
-                   [&](const AttnBlock& x, const AttnBlock& y) { return keys(x) > keys(y); });
-  std::copy(blocks.begin(), blocks.end(), a->host.begin());
-  const auto pairs_end = std::copy_if(blocks.begin(), blocks.end(), a->host.begin() + 2 * a->max_blocks,
-                                      [](const AttnBlock& b) { return b.blk % 2 == 0; });
-  const size_t n_pairs = static_cast<size_t>(pairs_end - (a->host.begin() + 2 * a->max_blocks));
-  std::stable_sort(blocks.begin(), blocks.end(),
+  std::stable_sort(blocks.begin(), blocks.end(), [](const AttnBlock& x, const AttnBlock& y) { return x.blk > y.blk; });
+  std::vector<AttnBlock> by_key = blocks, pairs;
+  std::stable_sort(by_key.begin(), by_key.end(),
                    [&](const AttnBlock& x, const AttnBlock& y) { return queries(x) > queries(y); });
-  std::copy(blocks.begin(), blocks.end(), a->host.begin() + a->max_blocks);
-  // pageable source: the runtime has taken its copy when the calls return
-  AttnBlock* dev = static_cast<AttnBlock*>(a->lists);
-  if (n) {
-    cudaError_t e = cudaMemcpyAsync(dev, a->host.data(), n * sizeof(AttnBlock), cudaMemcpyHostToDevice, s);
-    if (!e) e = cudaMemcpyAsync(dev + a->max_blocks, a->host.data() + a->max_blocks, n * sizeof(AttnBlock),
-                                cudaMemcpyHostToDevice, s);
-    if (!e) e = cudaMemcpyAsync(dev + 2 * a->max_blocks, a->host.data() + 2 * a->max_blocks,
-                                n_pairs * sizeof(AttnBlock), cudaMemcpyHostToDevice, s);
-    if (e) return cuda_fail(e, "cudaMemcpyAsync");
+  std::copy_if(blocks.begin(), blocks.end(), std::back_inserter(pairs), [](const AttnBlock& b) { return b.blk % 2 == 0; });
+  const int h = a->cfg.n_heads, hk = a->cfg.n_kv_heads, group = h / hk;
+  const int64_t n = static_cast<int64_t>(blocks.size());
+  std::vector<int> walk[3];
+  if (a->cfg.dtype == NORMPRE_BF16 && n && n * h <= kMaxDealt) {
+    // costs in tiles, with about what an item's start and end take
+    std::vector<int> fwd, dkdv, dq;
+    const bool heads = attn_pair_heads(group);
+    for (const AttnBlock& b : heads ? blocks : pairs)
+      fwd.push_back(2 * (b.blk + 1) + (heads ? 2 : (b.blk + 1) * 128 < b.len ? 4 : 2));
+    for (const AttnBlock& b : by_key) dkdv.push_back(group * (queries(b) + 1) + 1);
+    for (const AttnBlock& b : blocks) dq.push_back(b.blk + 2);
+    deal(fwd, heads ? h / 2 : h, &walk[0]);
+    deal(dkdv, hk, &walk[1]);
+    deal(dq, h, &walk[2]);
   }
+  // one copy; the staging memory is free once the last one has left it
+  cudaError_t e = cudaEventSynchronize(a->copied);
+  if (e) return cuda_fail(e, "cudaEventSynchronize");
+  int64_t at = 0, walk_at[3];
+  auto put = [&](const void* src, size_t bytes) {
+    if (bytes) std::memcpy(a->staging + at, src, bytes);
+    at += static_cast<int64_t>(bytes);
+  };
+  put(blocks.data(), blocks.size() * sizeof(AttnBlock));
+  put(by_key.data(), by_key.size() * sizeof(AttnBlock));
+  put(pairs.data(), pairs.size() * sizeof(AttnBlock));
+  for (int i = 0; i < 3; ++i) {
+    walk_at[i] = walk[i].empty() ? -1 : at;
+    put(walk[i].data(), walk[i].size() * sizeof(int));
+  }
+  if (at) e = cudaMemcpyAsync(a->lists, a->staging, static_cast<size_t>(at), cudaMemcpyHostToDevice, s);
+  if (!e) e = cudaEventRecord(a->copied, s);
+  if (e) return cuda_fail(e, "cudaMemcpyAsync");
   a->n_blocks = static_cast<int>(n);
-  a->n_pairs = static_cast<int>(n_pairs);
+  a->n_pairs = static_cast<int>(pairs.size());
+  std::copy(walk_at, walk_at + 3, a->walk_at);
   a->total = total;
   return NORMPRE_OK;
 }
@@ -162,9 +223,10 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out) {
     a->cfg = *cfg;
     if (a->cfg.scale == 0.f) a->cfg.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(cfg->head_dim)));
     a->max_blocks = cfg->max_tokens / 128 + std::min<int64_t>(cfg->max_seqs, cfg->max_tokens);
-    a->host.resize(3 * a->max_blocks);
     cudaError_t e = cudaGetDevice(&a->device);
-    if (!e) e = cudaMalloc(&a->lists, 3 * a->max_blocks * sizeof(AttnBlock));
+    if (!e) e = cudaMalloc(&a->lists, list_bytes(a.get()));
+    if (!e) e = cudaHostAlloc(&a->staging, list_bytes(a.get()), cudaHostAllocDefault);
+    if (!e) e = cudaEventCreateWithFlags(&a->copied, cudaEventDisableTiming);
     if (!e) e = cudaMalloc(&a->delta, static_cast<size_t>(cfg->n_heads) * cfg->max_tokens * sizeof(float));
     if (!e) e = cudaMalloc(&a->flags, sizeof(int));
     if (!e) e = cudaMemset(a->flags, 0, sizeof(int));

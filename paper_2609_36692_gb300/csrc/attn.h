@@ -6,6 +6,8 @@
 
 #include <string>
 
+#include "internal.h"
+
 namespace normpre {
 
 // 128 rows of one sequence: rows start + 128 blk .. of the pack, of which the
@@ -31,6 +33,8 @@ struct AttnArgs {
   const AttnBlock* by_key;   // blocks, the ones seen by the most queries first
   const AttnBlock* by_pair;  // the blocks of even index, in by_query's order
   int n_blocks, n_pairs;
+  // items of each CTA of the tensor-core kernels (null: see walk_item)
+  const int *walk_fwd, *walk_dkdv, *walk_dq;
   int total;                 // rows that belong to sequences
   int tokens;
   int heads, kv_heads, group, dim;
@@ -38,6 +42,15 @@ struct AttnArgs {
   float scale_log2;          // c log2(e): exp(c x) = exp2(scale_log2 x)
   int* flags;
 };
+
+// The forward kernel's two query tiles are two heads of a group; otherwise two
+// neighbouring tiles of one head.
+inline bool attn_pair_heads(int group) { return group % 2 == 0; }
+
+// CTAs of a tensor-core kernel.
+inline int walk_grid(int64_t items) {
+  return static_cast<int>(items < 1 ? 1 : items < device_sm_count() ? items : device_sm_count());
+}
 
 // fp32 kernels, one CTA per 64 rows and head (attn_simt.cu).
 cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t s);

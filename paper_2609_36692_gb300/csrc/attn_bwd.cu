@@ -30,8 +30,6 @@
 // neighbours.
 //
 // Roundings to bf16: P and dS once each (MMA operands), the gradients once.
-#include <algorithm>
-
 #include "attn_tc.cuh"
 
 namespace normpre {
@@ -61,14 +59,15 @@ template <int kSlots> struct Bars {
   uint64_t own_full[2][2], own_empty[2];   // per set: the two owned tiles, freed together
   uint64_t s_full[2], dp_full, p_ready, ds_ready, dp_free;
   uint64_t acc_full[2], acc_empty[2];
-  uint64_t stat_full[2], stat_empty[2];
+  uint64_t stat_empty[2];
   uint64_t drain[2];
   uint32_t tmem;
   int abort;
   uint32_t issued[kSlots], raw_issued[kSlots], own_issued[2];  // loads so far
 };
 
-// `users`: MMA chains that read a ring tile, and that add to an accumulator set.
+// `users`: MMA chains that read a ring tile, and that add to an accumulator set
+// (two in dK, dV, one in dQ).
 template <int kSlots>
 __device__ __forceinline__ void init_bars(Bars<kSlots>* b, int users) {
   for (int i = 0; i < kSlots; ++i) {
@@ -81,8 +80,7 @@ __device__ __forceinline__ void init_bars(Bars<kSlots>* b, int users) {
     tc::mbar_init(&b->own_full[i][0], 1);
     tc::mbar_init(&b->own_full[i][1], 1);
     tc::mbar_init(&b->own_empty[i], 2);
-    tc::mbar_init(&b->s_full[i], 1);
-    tc::mbar_init(&b->stat_full[i], 1);
+    tc::mbar_init(&b->s_full[i], users);             // dK, dV: the scores and their statistics
     tc::mbar_init(&b->stat_empty[i], 8);
     tc::mbar_init(&b->acc_full[i], users);
     tc::mbar_init(&b->acc_empty[i], 8);
@@ -224,9 +222,10 @@ struct Item {
   int64_t start;
   int len, blk, head;
 };
-__device__ __forceinline__ bool get_item(const AttnArgs& a, const AttnBlock* list, int heads, int64_t r, Item& it) {
-  const int64_t i = walk_item(r);
-  if (i >= static_cast<int64_t>(a.n_blocks) * heads) return false;
+__device__ __forceinline__ bool get_item(const AttnArgs& a, const AttnBlock* list, const int* walk, int heads,
+                                         int64_t r, Item& it) {
+  const int64_t i = walk_item(walk, r, static_cast<int64_t>(a.n_blocks) * heads);
+  if (i < 0) return false;
   const AttnBlock b = list[i / heads];
   it.start = b.start;
   it.len = b.len;
@@ -266,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   if (warp == 8) {
     // ---------------- TMA (one thread), then the rows past the sequences ----------------
     if (tc::elect_one()) {
-      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r, set.next()) {
         const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
         if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.k, &f.v, row, it.head, kChunks)) break;
         for (int g = 0; g < a.group && w.ok; ++g)
@@ -285,15 +284,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     // ---------------- MMA (one thread): dV(i), S(i + 1) ----------------
     if (tc::elect_one()) {
       uint32_t p_phase = 0;
+      int st = 0;                                                 // parity of the block in the walk
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r, set.next()) {
         const int n = ((it.len - 1) / kTile - it.blk + 1) * a.group;
         const uint32_t k = tc::su32(own + 2 * set.i * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][0], set.parity)) break;
         int q = w.take();
         if (!w.ok) break;
         product_ss<DP>(cS, k, tile(q));
-        tc::mma_commit(&b->s_full[0]);
+        tc::mma_commit(&b->s_full[st]);
+        st ^= 1;
         tc::mma_commit(&b->empty[q]);
         if (n == 1) tc::mma_commit(&b->own_empty[set.i]);
         if (!w.wait1(&b->acc_empty[set.i], set.parity ^ 1u)) break;
@@ -307,7 +308,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
           q = w.take();
           if (!w.ok) break;
           product_ss<DP>(cS, k, tile(q));
-          tc::mma_commit(&b->s_full[0]);
+          tc::mma_commit(&b->s_full[st]);
+          st ^= 1;
           tc::mma_commit(&b->empty[q]);
           if (i + 2 == n) tc::mma_commit(&b->own_empty[set.i]);
         }
@@ -322,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     if (tc::elect_one()) {
       uint32_t ds_phase = 0;
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r, set.next()) {
         const int n = ((it.len - 1) / kTile - it.blk + 1) * a.group;
         const uint32_t v = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
@@ -358,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     Turn<2> st;
     uint32_t seen = 0;
     int slot = 0;
-    for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r)
+    for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r)
       for (int g = 0; g < a.group && w.ok; ++g) {
         const int64_t base = static_cast<int64_t>(it.head * a.group + g) * a.tokens + it.start;
         for (int i = it.blk * kTile; i < it.len; i += kTile) {
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
             stat[st.i * 256 + 128 + 32 * e + lane] = de[e];
           }
           __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&b->stat_full[st.i]);
+          if (lane == 0) tc::mbar_arrive(&b->s_full[st.i]);
           st.next();
         }
       }
@@ -393,28 +395,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     const uint64_t c2 = tc::pack2(a.scale_log2, a.scale_log2);
     uint32_t phase = 0;
     Turn<2> st;
-    for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.kv_heads, r, it); ++r, set.next()) {
+    for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r, set.next()) {
       const int nq = (it.len - 1) / kTile - it.blk + 1, n = nq * a.group;
       for (int i = 0; i < n; ++i) {
         const float* ls = stat + st.i * 256 + 64 * half;
-        if (!w.wait(&b->stat_full[st.i], st.parity) || !w.wait(&b->s_full[0], phase)) break;
+        if (!w.wait(&b->s_full[st.i], st.parity)) break;
         const bool diag = i % nq == 0;
         float p[64];
         uint32_t pk[32];
+        uint32_t x[64];
+        tc::tmem_ld32(mS, x);
+        tc::tmem_ld32(mS + 32, x + 32);
+        tc::tmem_ld_wait();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t x[32];
-          tc::tmem_ld32(mS + 32 * h, x);
-          tc::tmem_ld_wait();
+        for (int e = 0; e < 64; e += 4) {
+          const ulonglong2 l2 = *reinterpret_cast<const ulonglong2*>(ls + e);
+          float y[4];
+          tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, l2.x), y[0], y[1]);
+          tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), c2, l2.y), y[2], y[3]);
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            const ulonglong2 l2 = *reinterpret_cast<const ulonglong2*>(ls + 32 * h + e);
-            float y[4];
-            tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, l2.x), y[0], y[1]);
-            tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), c2, l2.y), y[2], y[3]);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) p[32 * h + e + u] = tc::exp2_fast(y[u]);
-          }
+          for (int u = 0; u < 4; ++u) p[e + u] = tc::exp2_fast(y[u]);
         }
         if (diag) {   // key `row` is seen by queries row ..
 #pragma unroll
@@ -423,25 +423,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) pk[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
-        tc::tmem_st32(mS, pk);
+        tc::tmem_put32(mS, pk);
         tc::tmem_st_drain();
         w.arrive(&b->p_ready);
         if (!w.wait(&b->dp_full, phase)) break;
         phase ^= 1u;
+        tc::tmem_ld32(mP, x);
+        tc::tmem_ld32(mP + 32, x + 32);
+        tc::tmem_ld_wait();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t x[32];
-          tc::tmem_ld32(mP + 32 * h, x);
-          tc::tmem_ld_wait();
+        for (int e = 0; e < 64; e += 4) {
+          const float4 de = *reinterpret_cast<const float4*>(ls + 128 + e);
+          const float d4[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            const float4 de = *reinterpret_cast<const float4*>(ls + 128 + 32 * h + e);
-            const float d4[4] = {de.x, de.y, de.z, de.w};
-#pragma unroll
-            for (int u = 0; u < 4; u += 2)
-              pk[16 * h + (e + u) / 2] = pack_bf16x2(p[32 * h + e + u] * (__uint_as_float(x[e + u]) - d4[u]),
-                                                     p[32 * h + e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]));
-          }
+          for (int u = 0; u < 4; u += 2)
+            pk[(e + u) / 2] = pack_bf16x2(p[e + u] * (__uint_as_float(x[e + u]) - d4[u]),
+                                          p[e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]));
         }
         if (diag) {   // 0 * NaN in an unseen place
 #pragma unroll
@@ -450,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
             if (64 * half + 2 * e + 1 < row) pk[e] &= 0x0000FFFFu;
           }
         }
-        tc::tmem_st32(mP, pk);
+        tc::tmem_put32(mP, pk);
         tc::tmem_st_drain();
         w.arrive(&b->ds_ready);
         if (lane == 0) tc::mbar_arrive(&b->stat_empty[st.i]);
@@ -498,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
   if (warp == 8) {
     // ---------------- TMA (one thread), then the rows past the sequences ----------------
     if (tc::elect_one()) {
-      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r, set.next()) {
         const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
         if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.q, &f.dout, row, it.head, kChunks)) break;
         for (int j = 0; j <= it.blk && w.ok; ++j) {
@@ -515,7 +512,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     if (tc::elect_one()) {
       uint32_t ds_phase = 0;
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r, set.next()) {
         const int n = it.blk + 1;
         const uint32_t q = tc::su32(own + 2 * set.i * kTileBytes);
         int k[2] = {0, 0};                                        // ring slots of K(j), K(j + 1)
@@ -553,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     // ---------------- MMA (one thread): dP(j) ----------------
     if (tc::elect_one()) {
       uint32_t free_phase = 0;
-      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r, set.next()) {
         const uint32_t o = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
         for (int j = 0; j <= it.blk; ++j) {
@@ -576,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     // ---------------- sequence ends: K's rows past them become zeros ----------------
     uint32_t seen = 0;
     int next = 0;                                                 // ring slot of the item's first tile
-    for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r) {
+    for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r) {
       const int rows = it.len - kTile * it.blk;
       if (rows < kTile) w.end_tile(ring, kTileBytes, (next + 2 * it.blk) % kSlots, seen, rows, kChunks);
       next = (next + 2 * (it.blk + 1)) % kSlots;
@@ -587,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint64_t c2 = tc::pack2(a.scale_log2, a.scale_log2);
     uint32_t dp_phase = 0;
-    for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.heads, r, it); ++r, set.next()) {
+    for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r, set.next()) {
       const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk + row;
       const bool in = kTile * it.blk + row < it.len;
       const int64_t si = static_cast<int64_t>(it.head) * a.tokens + at;
@@ -598,32 +595,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         if (!w.wait(&b->s_full[buf.i], buf.parity)) break;
         float p[64];
         uint32_t pk[32];
+        uint32_t x[64];
+        tc::tmem_ld32(mS, x);
+        tc::tmem_ld32(mS + 32, x + 32);
+        tc::tmem_ld_wait();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t x[32];
-          tc::tmem_ld32(mS + 32 * h, x);
-          tc::tmem_ld_wait();
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            float y0, y1;
-            tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, ls2), y0, y1);
-            p[32 * h + e] = tc::exp2_fast(y0);
-            p[32 * h + e + 1] = tc::exp2_fast(y1);
-          }
+        for (int e = 0; e < 64; e += 2) {
+          float y0, y1;
+          tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, ls2), y0, y1);
+          p[e] = tc::exp2_fast(y0);
+          p[e + 1] = tc::exp2_fast(y1);
         }
         if (!w.wait(&b->dp_full, dp_phase)) break;
         dp_phase ^= 1u;
+        tc::tmem_ld32(mP, x);
+        tc::tmem_ld32(mP + 32, x + 32);
+        tc::tmem_ld_wait();
+        w.arrive(&b->dp_free);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t x[32];
-          tc::tmem_ld32(mP + 32 * h, x);
-          tc::tmem_ld_wait();
-          if (h == 1) w.arrive(&b->dp_free);
-#pragma unroll
-          for (int e = 0; e < 32; e += 2)
-            pk[16 * h + e / 2] = pack_bf16x2(p[32 * h + e] * (__uint_as_float(x[e]) - de),
-                                             p[32 * h + e + 1] * (__uint_as_float(x[e + 1]) - de));
-        }
+        for (int e = 0; e < 64; e += 2)
+          pk[e / 2] = pack_bf16x2(p[e] * (__uint_as_float(x[e]) - de), p[e + 1] * (__uint_as_float(x[e + 1]) - de));
         if (j == it.blk) {   // query `row` sees keys .. row
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
@@ -631,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
             if (64 * half + 2 * e + 1 > row) pk[e] &= 0x0000FFFFu;
           }
         }
-        tc::tmem_st32(mS, pk);
+        tc::tmem_put32(mS, pk);
         tc::tmem_st_drain();
         w.arrive(&b->ds_ready);
       }
@@ -647,8 +638,7 @@ template <typename K>
 cudaError_t launch(K* kernel, const BwdArgs& f, int heads, size_t smem, cudaStream_t s) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e) return e;
-  const int64_t items = std::max<int64_t>(1, static_cast<int64_t>(f.a.n_blocks) * heads);
-  kernel<<<static_cast<int>(std::min<int64_t>(items, device_sm_count())), kThreads, smem, s>>>(f);
+  kernel<<<walk_grid(static_cast<int64_t>(f.a.n_blocks) * heads), kThreads, smem, s>>>(f);
   return cudaGetLastError();
 }
 

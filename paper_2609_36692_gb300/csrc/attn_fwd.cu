@@ -25,6 +25,8 @@
 //
 // Roundings to bf16: P once (the MMA operand; l sums the unrounded values) and
 // the output once.
+#include <type_traits>
+
 #include "attn_tc.cuh"
 
 namespace normpre {
@@ -53,7 +55,7 @@ template <int kSlots> struct Bars {
   // raw: a tile that ends its sequence lands here first; once its tail is
   // zeroed it counts as full
   uint64_t full[kSlots], empty[kSlots], raw[kSlots];
-  uint64_t q_full[2], q_empty[2], s_full[2], p_ready[2][2], pv_done[2], o_empty[2][2], drain[2];
+  uint64_t q_full[2], q_empty[2], s_full[2], p_ready[2][2], pv_done[2], o_empty[2][2], turn[2], drain[2];
   uint32_t tmem;
   int abort;
   uint32_t issued[kSlots], raw_issued[kSlots], q_issued[2];   // last parity + 1
@@ -70,8 +72,8 @@ struct Item {
 
 __device__ __forceinline__ bool get_item(const FwdArgs& f, int64_t r, Item& it) {
   const int per = f.pair_heads ? f.a.heads / 2 : f.a.heads;
-  const int64_t i = walk_item(r);
-  if (i >= static_cast<int64_t>(f.n_list) * per) return false;
+  const int64_t i = walk_item(f.a.walk_fwd, r, static_cast<int64_t>(f.n_list) * per);
+  if (i < 0) return false;
   const AttnBlock b = f.list[i / per];
   const int h = static_cast<int>(i % per);
   it.start = b.start;
@@ -117,6 +119,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       tc::mbar_init(&b->pv_done[i], 1);
       tc::mbar_init(&b->o_empty[i][0], 4);
       tc::mbar_init(&b->o_empty[i][1], 4);
+      tc::mbar_init(&b->turn[i], 1);
       tc::mbar_init(&b->drain[i], 1);
       b->q_issued[i] = 0;
     }
@@ -201,17 +204,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       }
     } else {
       // ---------------- MMA of one tile (one thread) ----------------
-      // The two tiles are issued by two warps: a thread's MMAs run almost as it
-      // issues them, so that its waits leave the tensor cores to the other.
+      // A thread's MMAs run almost as it issues them, so that its waits would
+      // idle the tensor cores: the two tiles are issued by two warps.  They
+      // take turns, a tile's P V and next scores at a time, which keeps one
+      // tile's softmax beside the other's products (left alone they fall into
+      // step).  The turn passes before the last MMAs, to cover its latency.
       const int s = warp == 11;
       if (tc::elect_one()) {
         int slot = 0, acc = 0;
-        uint32_t phase = 0, q_phase = 0, p_phase = 0, o_phase = 0;
+        uint32_t phase = 0, q_phase = 0, p_phase = 0, o_phase = 0, t_phase = s ? 0 : 1;
+        const uint32_t sq = tc::su32(sQ + s * kTileBytes);
+        auto tile = [&](int t) { return tc::su32(ring + t * kTileBytes); };
         auto wait = [&](uint64_t* bar, uint32_t parity) {
           ok = ok && tc::mbar_wait(bar, parity, &b->abort);
           tc::fence_after();
           return ok;
         };
+        auto my_turn = [&]() {
+          wait(&b->turn[s], t_phase);
+          t_phase ^= 1u;
+          return ok;
+        };
+        auto pass_turn = [&]() { tc::mbar_arrive(&b->turn[s ^ 1]); };
         // next tile of the ring, once it has arrived
         auto take = [&]() {
           const int t = slot;
@@ -219,48 +233,55 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           if (++slot == kSlots) { slot = 0; phase ^= 1u; }
           return t;
         };
-        auto scores = [&](int k) {   // S = Q K^T
-          product_ss<DP>(s_col(s), tc::su32(sQ + s * kTileBytes), tc::su32(ring + k * kTileBytes));
+        // S = Q K^T, and the turn is over
+        auto scores = [&](int k) {
+          product_ss<DP, 0, DP / 32>(s_col(s), sq, tile(k));
+          pass_turn();
+          product_ss<DP, DP / 32, DP / 16>(s_col(s), sq, tile(k));
           tc::mma_commit(&b->s_full[s]);
           tc::mma_commit(&b->empty[k]);
         };
         for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
           const int blk = s ? it.blk1 : it.blk0;
           int k = take();
-          for (int j = it.top; ok; --j) {
-            // scores of block j
-            if (j <= blk) {
-              if (j == blk) {
-                if (!wait(&b->q_full[s], q_phase)) break;
-                q_phase ^= 1u;
-              }
-              scores(k);
-              if (j == 0) tc::mma_commit(&b->q_empty[s]);
-            } else {
-              tc::mbar_arrive(&b->empty[k]);
-            }
-            // O += P V of the block before it in the walk has been issued; this block's
+          if (blk >= 0 && !wait(&b->q_full[s], q_phase)) break;
+          if (blk >= 0) q_phase ^= 1u;
+          if (!ok || !my_turn()) break;
+          if (it.top == blk) {
+            scores(k);
+            if (blk == 0) tc::mma_commit(&b->q_empty[s]);
+          } else {
+            tc::mbar_arrive(&b->empty[k]);
+            pass_turn();
+          }
+          for (int j = it.top; j >= 0; --j) {
             const int v = take();
+            if (j > 0) k = take();
             if (!ok) break;
+            const uint32_t o = o_col(s, acc), p = s_col(s);
             if (j <= blk) {
               if (j == blk) {
-                const uint32_t parity = kAcc == 2 ? (o_phase >> acc) & 1u : o_phase;
-                if (!wait(&b->o_empty[s][acc], parity ^ 1u)) break;
-                o_phase ^= kAcc == 2 ? 1u << acc : 1u;
+                if (!wait(&b->o_empty[s][acc], ((o_phase >> acc) & 1u) ^ 1u)) break;
+                o_phase ^= 1u << acc;
               }
-              const uint32_t o = o_col(s, acc), p = s_col(s);
-              if (!wait(&b->p_ready[s][0], p_phase)) break;
-              product_ts<DP, 0, 4>(o, p, tc::su32(ring + v * kTileBytes), j == blk, 0);
+              if (!wait(&b->p_ready[s][0], p_phase) || !my_turn()) break;
+              product_ts<DP, 0, 6>(o, p, tile(v), j == blk, 0);
               if (!wait(&b->p_ready[s][1], p_phase)) break;
-              product_ts<DP, 4, 8>(o, p, tc::su32(ring + v * kTileBytes), false, 0);
+              product_ts<DP, 6, 8>(o, p, tile(v), false, 0);
               p_phase ^= 1u;
               tc::mma_commit(&b->pv_done[s]);
               tc::mma_commit(&b->empty[v]);
             } else {
+              if (!my_turn()) break;
               tc::mbar_arrive(&b->empty[v]);
             }
-            if (j == 0) break;
-            k = take();
+            if (j > 0 && j - 1 <= blk) {
+              scores(k);
+              if (j == 1) tc::mma_commit(&b->q_empty[s]);
+            } else {
+              if (j > 0) tc::mbar_arrive(&b->empty[k]);
+              pass_turn();
+            }
           }
           if (blk >= 0 && kAcc == 2) acc ^= 1;
         }
@@ -315,40 +336,41 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
             if (i > row) x[i] = 0xFF800000u;
           m = top();
         }
-        // half of the row's exponentials with the running maximum, into P
-        uint32_t p[32];
+        // exponentials of columns 2 I0 .. 2 I1 with the running maximum, into P
+        uint32_t p[64];
         uint64_t sum[2];
-        auto half = [&](int h) {
+        auto exps = [&](auto first, auto last) {
           const float mc = -m * c;
           const uint64_t mc2 = tc::pack2(mc, mc);
           sum[0] = sum[1] = 0;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
+          for (int i = decltype(first)::value; i < decltype(last)::value; ++i) {
             float lo, hi;
-            const int e = 64 * h + 2 * i;
-            tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, mc2), lo, hi);
+            tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), c2, mc2), lo, hi);
             lo = tc::exp2_fast(lo);
             hi = tc::exp2_fast(hi);
             sum[i & 1] = tc::add2(sum[i & 1], tc::pack2(lo, hi));
             p[i] = pack_bf16x2(lo, hi);
           }
         };
+        using I0 = std::integral_constant<int, 0>;
+        using I48 = std::integral_constant<int, 48>;
+        using I64 = std::integral_constant<int, 64>;
         auto add_sum = [&]() {
           float lo, hi;
           tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
           l += lo + hi;
         };
-        auto release = [&](int h) {
-          tc::tmem_st32(sc + 32 * h, p);
+        auto release = [&](int part) {
           tc::tmem_st_drain();
           tc::fence_before();
           __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&b->p_ready[s][h]);
+          if (lane == 0) tc::mbar_arrive(&b->p_ready[s][part]);
         };
         // The maximum of a later block is needed only to see whether the
         // running one must be raised, which is rare: its comparisons run in
         // the shadow of the exponentials.
-        half(0);
+        exps(I0{}, I48{});
         if (j != blk) {
           const float up = fmaxf(m, top());
           if (__any_sync(0xffffffffu, (up - m) * c > kGrow)) {
@@ -363,14 +385,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
               tc::tmem_ld_wait();
 #pragma unroll
               for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-              tc::tmem_st32(oc + i, o);
+              tc::tmem_put32(oc + i, o);
             }
-            half(0);
+            exps(I0{}, I48{});
           }
         }
         add_sum();
+        // three quarters of P first: the products on them cover the rest
+        tc::tmem_put32(sc, p);
+        tc::tmem_put16(sc + 32, p + 32);
         release(0);
-        half(1);
+        exps(I48{}, I64{});
+        tc::tmem_put16(sc + 48, p + 48);
         release(1);
         add_sum();
         ++pv;
@@ -425,8 +451,7 @@ static cudaError_t launch(const FwdArgs& f, int64_t items, cudaStream_t s) {
   cudaError_t e = cudaFuncSetAttribute(k_attn_fwd_tc<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        static_cast<int>(Fwd<DP>::kSmem));
   if (e) return e;
-  const int grid = static_cast<int>(std::min<int64_t>(std::max<int64_t>(items, 1), device_sm_count()));
-  k_attn_fwd_tc<DP><<<grid, kThreads, Fwd<DP>::kSmem, s>>>(f);
+  k_attn_fwd_tc<DP><<<walk_grid(items), kThreads, Fwd<DP>::kSmem, s>>>(f);
   return cudaGetLastError();
 }
 
@@ -436,7 +461,7 @@ cudaError_t launch_attn_forward_tc(const AttnArgs& a, cudaStream_t s, std::strin
   if (!rows_map(&f.q, a.q, a.tokens, a.heads, a.dim, err) || !rows_map(&f.k, a.k, a.tokens, a.kv_heads, a.dim, err) ||
       !rows_map(&f.v, a.v, a.tokens, a.kv_heads, a.dim, err))
     return cudaErrorInvalidValue;
-  f.pair_heads = a.group % 2 == 0;
+  f.pair_heads = attn_pair_heads(a.group);
   f.list = f.pair_heads ? a.by_query : a.by_pair;
   f.n_list = f.pair_heads ? a.n_blocks : a.n_pairs;
   const int64_t items = static_cast<int64_t>(f.n_list) * (f.pair_heads ? a.heads / 2 : a.heads);

@@ -17,11 +17,18 @@ constexpr int kTile = 128;                 // rows and keys of a tile
 constexpr int kChunk = kTile * 128;        // bytes of 128 rows of 64 bf16: one TMA box, 128-byte swizzle
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Position r of the work list's walk by CTA c of g: back and forth, so that
-// with items in falling order of cost every CTA's total is about the same.
-__device__ __forceinline__ int64_t walk_item(int64_t r) {
+// The r-th item of this CTA, -1 past its last.  With a plan's lists: ids from
+// walk[gridDim.x + 1 + walk[c]] up to walk[gridDim.x + 1 + walk[c + 1]].  Without
+// (many items per CTA): the items in falling order of cost, back and forth over
+// the CTAs.
+__device__ __forceinline__ int64_t walk_item(const int* walk, int64_t r, int64_t items) {
   const int64_t g = gridDim.x, c = blockIdx.x;
-  return r * g + ((r & 1) ? g - 1 - c : c);
+  if (walk) {
+    const int64_t i = walk[c] + r;
+    return i < walk[c + 1] ? walk[g + 1 + i] : -1;
+  }
+  const int64_t i = r * g + ((r & 1) ? g - 1 - c : c);
+  return i < items ? i : -1;
 }
 
 // One tile of `chunks` 64-wide column chunks: 128 rows from `row` of a head.
@@ -39,13 +46,14 @@ __device__ __forceinline__ uint64_t desc_rows(uint32_t tile) { return tc::sdesc(
 __host__ __device__ constexpr uint64_t cols_step(int kk) { return ((kk >> 2) * kChunk + (kk & 3) * 32) >> 4; }
 __host__ __device__ constexpr uint64_t rows_step(int kk) { return (kk * 2048) >> 4; }
 
-// D = A B^T over the head dimension: both tiles in shared memory.
-template <int DP>
+// D = A B^T over columns 16 K0 .. 16 K1 of the head dimension: both tiles in
+// shared memory.
+template <int DP, int K0 = 0, int K1 = DP / 16>
 __device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b) {
   constexpr uint32_t idesc = tc::idesc_bf16(kTile, kTile, 0, 0);
   const uint64_t ad = desc_cols(a), bd = desc_cols(b);
 #pragma unroll
-  for (int kk = 0; kk < DP / 16; ++kk) tc::mma_bf16(d, ad + cols_step(kk), bd + cols_step(kk), idesc, kk != 0);
+  for (int kk = K0; kk < K1; ++kk) tc::mma_bf16(d, ad + cols_step(kk), bd + cols_step(kk), idesc, kk != 0);
 }
 // D (+)= A B over rows 16 K0 .. 16 K1 of B: A in TMEM, its columns 64 .. 127
 // `gap` columns further on.
