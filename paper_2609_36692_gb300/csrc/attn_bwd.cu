@@ -257,6 +257,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   }
   __syncthreads();
   tc::fence_after();
+  tc::grid_wait();      // the deltas; what came before them
+  tc::grid_release();   // k_attn_dq may take the SMs that run out of work here
   const uint32_t cS = b->tmem, cP = cS + 128, cAcc = cS + 256;     // per set: dV, dK
   Warp<kSlots> w = {b, lane, true, 0, 0};
   Turn<kSets> set;
@@ -632,14 +634,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     }
   }
   finish(w, warp, a.flags);
+  // It started beside k_attn_dkdv, which had waited for the deltas, and shares
+  // nothing with it; but what follows in the stream follows both.
+  tc::grid_wait();
 }
 
+// Launched as a programmatic dependent of the kernel before it in the stream.
 template <typename K>
 cudaError_t launch(K* kernel, const BwdArgs& f, int heads, size_t smem, cudaStream_t s) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e) return e;
-  kernel<<<walk_grid(static_cast<int64_t>(f.a.n_blocks) * heads), kThreads, smem, s>>>(f);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  cfg.gridDim = dim3(walk_grid(static_cast<int64_t>(f.a.n_blocks) * heads));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, f);
 }
 
 }  // namespace

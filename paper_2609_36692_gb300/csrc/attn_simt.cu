@@ -20,6 +20,7 @@
 #include "attn.h"
 #include "common.cuh"
 #include "internal.h"
+#include "tc.cuh"
 
 namespace normpre {
 namespace {
@@ -362,26 +363,25 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(const __grid_constant__ At
   store_tile<T, DP>(a.dq, row0, rows, head, a.dim, ty, tx, dq, c);
 }
 
-// One warp per row and head.
-template <typename T>
+// LANES (8 or 16) lanes per row and head, 8 columns each.
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ AttnArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;   // token-major
+  tc::grid_release();   // the backward kernel sets itself up meanwhile
+  const int lane = threadIdx.x % LANES;
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) / LANES;   // token-major
   const int64_t row = i / a.heads;
   const int head = static_cast<int>(i - row * a.heads);
-  if (row >= a.total) return;
-  const T* o = static_cast<const T*>(a.o.p) + row * a.o.ts + head * a.o.hs;
-  const T* d = static_cast<const T*>(a.dout.p) + row * a.dout.ts + head * a.dout.hs;
   float s = 0.f;
-  if (lane * 8 < a.dim) {
+  if (row < a.total && lane * 8 < a.dim) {
     float x[8], y[8];
-    load8(o + lane * 8, x);
-    load8(d + lane * 8, y);
+    load8(static_cast<const T*>(a.o.p) + row * a.o.ts + head * a.o.hs + lane * 8, x);
+    load8(static_cast<const T*>(a.dout.p) + row * a.dout.ts + head * a.dout.hs + lane * 8, y);
 #pragma unroll
     for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
   }
-  s = warp_sum(s);
-  if (lane == 0) a.delta[static_cast<int64_t>(head) * a.tokens + row] = s;
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0 && row < a.total) a.delta[static_cast<int64_t>(head) * a.tokens + row] = s;
 }
 
 template <typename K>
@@ -416,13 +416,18 @@ cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s) {
   return a.dim <= 64 ? backward<float, 64>(a, s) : backward<float, 128>(a, s);
 }
 
-cudaError_t launch_attn_delta(const AttnArgs& a, int dtype, cudaStream_t s) {
-  const int64_t warps = static_cast<int64_t>(a.total) * a.heads;
-  if (!warps) return cudaSuccess;
-  const unsigned grid = static_cast<unsigned>((warps + 7) / 8);
-  if (dtype == 0) k_attn_delta<float><<<grid, 256, 0, s>>>(a);
-  else k_attn_delta<bf16><<<grid, 256, 0, s>>>(a);
+template <typename T>
+static cudaError_t delta(const AttnArgs& a, cudaStream_t s) {
+  const int lanes = a.dim <= 64 ? 8 : 16;
+  const int64_t ctas = cdiv(static_cast<int64_t>(a.total) * a.heads, 256 / lanes);
+  if (!ctas) return cudaSuccess;
+  if (lanes == 8) k_attn_delta<T, 8><<<static_cast<unsigned>(ctas), 256, 0, s>>>(a);
+  else k_attn_delta<T, 16><<<static_cast<unsigned>(ctas), 256, 0, s>>>(a);
   return cudaGetLastError();
+}
+
+cudaError_t launch_attn_delta(const AttnArgs& a, int dtype, cudaStream_t s) {
+  return dtype == 0 ? delta<float>(a, s) : delta<bf16>(a, s);
 }
 
 }  // namespace normpre

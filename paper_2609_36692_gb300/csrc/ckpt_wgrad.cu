@@ -6,7 +6,7 @@
 // 128 features x 256 outputs (the transposed piece of dW: a TMEM lane is a
 // feature, so that a warp stores 32 consecutive elements of a row of dW) is
 // summed 64 tokens at a time: TMA brings the codes and the dY boxes into a
-// ring, eight warps turn codes into swizzled bf16 tiles (a byte becomes an
+// ring, sixteen warps turn codes into swizzled bf16 tiles (a byte becomes an
 // fp32 by permutation into 2^23 + byte, one packed FMA takes off the offset
 // and scales, one conversion packs two), one thread issues the MMAs, and four
 // warps drain a finished accumulator (two in TMEM) while the next tile runs.
@@ -84,8 +84,9 @@ constexpr int kRing = 4, kXbuf = 3;
 constexpr int kBox = 64 * 128;                           // bytes of 64 rows of 64 bf16
 constexpr int kDyBytes = 4 * kBox, kCodeBytes = kStep * kTileK, kXBytes = 2 * kBox;
 constexpr int kStageBytes = kDyBytes + kCodeBytes;
-constexpr int kConvert = 8;                              // converting warps
-constexpr int kTcThreads = 32 * (4 + kConvert + 2);      // drain, convert, TMA, MMA
+constexpr int kConvert = 8, kGroups = 2;                 // converting warps of a step; groups that take turns
+constexpr int kTma = 4 + kGroups * kConvert, kMma = kTma + 1, kSteps = kTma + 2;   // warps: drain, convert, these
+constexpr int kTcThreads = 32 * (kSteps + 1);
 constexpr size_t kTcSmem = kRing * kStageBytes + kXbuf * kXBytes + kRing * kStep * 4 + 512;
 
 struct WgradTcArgs {
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   }
   __syncthreads();
   tc::cluster_sync();   // the peer's barriers exist before a multicast reaches them
-  if (warp == 13) {
+  if (warp == kMma) {
     tc::tmem_alloc(&b->tmem, 512);
     tc::tmem_relinquish();
     tc::fence_before();
@@ -190,39 +191,51 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   auto tile_k = [&](int u) { return SPLIT ? u % f.tiles_k : 2 * (u % ((f.tiles_k + 1) / 2)) + static_cast<int>(rank); };
   auto tile_n = [&](int u) { return SPLIT ? u / f.tiles_k : u / ((f.tiles_k + 1) / 2); };
 
-  if (warp == 12) {
-    // ---------------- TMA, and the step words by plain asynchronous copies ----------------
+  if (warp == kTma) {
+    // ---------------- TMA (one thread) ----------------
+    if (tc::elect_one()) {
+      int st = 0;
+      uint32_t phase = 0;
+      for (int u = unit0; u < f.units && ok; u += nunits) {
+        const int k0 = tile_k(u) * kTileK, n0 = tile_n(u) * kTileN;
+        for (int s = s0; s < s1; ++s) {
+          if (!(ok = tc::mbar_wait(&b->empty[st], phase ^ 1u, &b->abort))) break;
+          uint8_t* dst = ring + st * kStageBytes;
+          tc::mbar_expect_tx(&b->full[st], kStageBytes);
+          b->issued[st] = phase + 1;
+          tc::tma_load_3d(dst + kDyBytes, &f.codes, &b->full[st], k0, s * kStep, 0);
+          if (SPLIT) {
+            for (int i = 0; i < 4; ++i) tc::tma_load_3d(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, s * kStep, 0);
+          } else {
+            for (int i = 2 * rank; i < 2 * static_cast<int>(rank) + 2; ++i)
+              tc::tma_load_3d_mc(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, s * kStep, 0, 3);
+          }
+          if (++st == kRing) { st = 0; phase ^= 1u; }
+        }
+      }
+    }
+    __syncwarp();
+    ok = __all_sync(0xffffffffu, ok);
+  } else if (warp == kSteps) {
+    // ---------------- step words, by plain asynchronous copies ----------------
     int st = 0;
     uint32_t phase = 0;
     for (int u = unit0; u < f.units && ok; u += nunits) {
-      const int tk = tile_k(u), n0 = tile_n(u) * kTileN;
+      const int tk = tile_k(u);
       const uint32_t* words = a.x.steps + static_cast<int64_t>(tk) * a.tokens;
       for (int s = s0; s < s1; ++s) {
         if (!wait(&b->empty[st], phase ^ 1u)) break;
-        uint8_t* dst = ring + st * kStageBytes;
-        const int t0 = s * kStep;
-        if (lane == 0) {
-          tc::mbar_expect_tx(&b->full[st], kStageBytes);
-          b->issued[st] = phase + 1;
-          if (SPLIT) {
-            for (int i = 0; i < 4; ++i) tc::tma_load_3d(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, t0, 0);
-          } else {
-            for (int i = 2 * rank; i < 2 * static_cast<int>(rank) + 2; ++i)
-              tc::tma_load_3d_mc(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, t0, 0, 3);
-          }
-          tc::tma_load_3d(dst + kDyBytes, &f.codes, &b->full[st], tk * kTileK, t0, 0);
-        }
-        __syncwarp();
 #pragma unroll
         for (int i = lane; i < kStep; i += 32) {
-          const bool in = tk < f.tiles_k && t0 + i < a.tokens;
-          copy4_async(steps + st * kStep + i, in ? words + t0 + i : a.x.steps, in);
+          const int64_t t = static_cast<int64_t>(s) * kStep + i;
+          const bool in = tk < f.tiles_k && t < a.tokens;
+          copy4_async(steps + st * kStep + i, in ? words + t : a.x.steps, in);
         }
         copies_arrive(&b->full[st]);
         if (++st == kRing) { st = 0; phase ^= 1u; }
       }
     }
-  } else if (warp == 13) {
+  } else if (warp == kMma) {
     // ---------------- MMA (one thread) ----------------
     if (tc::elect_one()) {
       constexpr uint32_t idesc = tc::idesc_bf16(kTileK, kTileN, 1, 1);
@@ -258,37 +271,42 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     ok = __all_sync(0xffffffffu, ok);
   } else if (warp >= 4) {
     // ---------------- codes -> bf16 ----------------
-    // 8 rows x 4 blocks per warp: lanes of 8 rows, whose 16-byte pieces the
-    // swizzle spreads over all banks
-    const int row = 8 * (warp - 4) + (lane & 7), blk = lane >> 3, sw = row & 7;
-    int st = 0, xb = 0;
+    // The groups take the steps in turn, so that a group's waits have another
+    // step's time.  8 rows x 4 blocks per warp: lanes of 8 rows, whose 16-byte
+    // pieces the swizzle spreads over all banks.
+    const int group = (warp - 4) / kConvert;
+    const int row = 8 * ((warp - 4) % kConvert) + (lane & 7), blk = lane >> 3, sw = row & 7;
+    int st = 0, xb = 0, turn = 0;
     uint32_t phase = 0, xphase = 0;
     for (int u = unit0; u < f.units && ok; u += nunits)
       for (int s = s0; s < s1; ++s) {
-        if (!wait(&b->full[st], phase)) break;
-        const uint8_t* src = ring + st * kStageBytes + kDyBytes + row * kTileK;
-        uint4 c[2];
+        if (turn == group) {
+          if (!wait(&b->full[st], phase)) break;
+          const uint8_t* src = ring + st * kStageBytes + kDyBytes + row * kTileK;
+          uint4 c[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) c[i] = *reinterpret_cast<const uint4*>(src + (((2 * blk + i) ^ sw) << 4));
-        const float step = ckpt_step(steps[st * kStep + row], blk);
-        const float off = -8388736.f * step;             // -(2^23 + 128) step
-        const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
-        if (!wait(&b->xempty[xb], xphase ^ 1u)) break;
-        uint8_t* dst = xbuf + xb * kXBytes + (blk >> 1) * kBox + row * 128;
+          for (int i = 0; i < 2; ++i) c[i] = *reinterpret_cast<const uint4*>(src + (((2 * blk + i) ^ sw) << 4));
+          const float step = ckpt_step(steps[st * kStep + row], blk);
+          const float off = -8388736.f * step;             // -(2^23 + 128) step
+          const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
+          if (!wait(&b->xempty[xb], xphase ^ 1u)) break;
+          uint8_t* dst = xbuf + xb * kXBytes + (blk >> 1) * kBox + row * 128;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint4 v;
-            convert4(w[2 * h], step2, off2, v.x, v.y);
-            convert4(w[2 * h + 1], step2, off2, v.z, v.w);
-            *reinterpret_cast<uint4*>(dst + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
+            for (int h = 0; h < 2; ++h) {
+              uint4 v;
+              convert4(w[2 * h], step2, off2, v.x, v.y);
+              convert4(w[2 * h + 1], step2, off2, v.z, v.w);
+              *reinterpret_cast<uint4*>(dst + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
+            }
           }
+          tc::fence_smem_async();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&b->xfull[xb]);
         }
-        tc::fence_smem_async();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&b->xfull[xb]);
+        if (++turn == kGroups) turn = 0;
         if (++st == kRing) { st = 0; phase ^= 1u; }
         if (++xb == kXbuf) { xb = 0; xphase ^= 1u; }
       }
@@ -342,10 +360,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     }
     __syncthreads();
     tc::cluster_sync();
-    const int k0 = tile_k(unit0) * kTileK, n0 = tile_n(unit0) * kTileN, rows = kTileN / csize;
+    const int k0 = tile_k(unit0) * kTileK, n0 = tile_n(unit0) * kTileN, rows = (kTileN + csize - 1) / csize;
     for (int i = threadIdx.x; i < rows * (kTileK / 4); i += kTcThreads) {
       const int n = rank * rows + i / (kTileK / 4), k = 4 * (i % (kTileK / 4));
-      if (n0 + n >= a.n || k0 + k >= a.k) continue;
+      if (n >= kTileN || n0 + n >= a.n || k0 + k >= a.k) continue;
       float v[4] = {};
       for (uint32_t q = 0; q < csize; ++q) {
         if (static_cast<int64_t>(total) * q / csize == static_cast<int64_t>(total) * (q + 1) / csize) continue;   // no tokens
@@ -373,41 +391,67 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   // no CTA exits while the other may still multicast into it, arrive on its
   // barriers or read its partial tile
   tc::cluster_sync();
-  if (warp == 13) {
+  if (warp == kMma) {
     tc::fence_after();
     tc::tmem_dealloc(tmem, 512);
   }
 }
 
-template <typename TW, bool SPLIT>
-cudaError_t launch_tc(WgradTcArgs f, int cluster, cudaStream_t s) {
-  auto kernel = k_wgrad_tc<TW, SPLIT>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kTcSmem));
-  if (e) return e;
+struct ClusterLaunch {
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
-  cfg.blockDim = dim3(kTcThreads);
-  cfg.dynamicSmemBytes = kTcSmem;
-  cfg.stream = s;
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cluster;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  int clusters = f.units;
-  if (!SPLIT) {
-    // how many pairs run at once: a GPC with an odd number of SMs leaves one out
-    static std::atomic<int> known{0};
-    int fit = known.load(std::memory_order_relaxed);
-    if (!fit) {
-      cfg.gridDim = dim3(2 * std::max(1, device_sm_count() / 2));
-      if ((e = cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg))) return e;
-      known.store(fit = std::max(1, fit), std::memory_order_relaxed);
-    }
-    clusters = std::min(clusters, fit);
+  ClusterLaunch(int cluster, int clusters, cudaStream_t s) {
+    cfg.gridDim = dim3(cluster * clusters);
+    cfg.blockDim = dim3(kTcThreads);
+    cfg.dynamicSmemBytes = kTcSmem;
+    cfg.stream = s;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
   }
-  cfg.gridDim = dim3(clusters * cluster);
-  return cudaLaunchKernelEx(&cfg, kernel, f);
+};
+
+// Clusters of a size that the GPU holds at once (a cluster stays within a GPC,
+// so that some SMs are left over).
+template <typename TW, bool SPLIT>
+cudaError_t clusters_at_once(int cluster, int* fit) {
+  static std::atomic<int> known[9];
+  *fit = known[cluster].load(std::memory_order_relaxed);
+  if (*fit) return cudaSuccess;
+  ClusterLaunch l(cluster, std::max(1, device_sm_count() / cluster), nullptr);
+  cudaError_t e = cudaFuncSetAttribute(k_wgrad_tc<TW, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(kTcSmem));
+  if (!e) e = cudaOccupancyMaxActiveClusters(fit, k_wgrad_tc<TW, SPLIT>, &l.cfg);
+  if (!e) known[cluster].store(*fit = std::max(1, *fit), std::memory_order_relaxed);
+  return e;
+}
+
+template <typename TW>
+cudaError_t launch_tc(WgradTcArgs f, cudaStream_t s) {
+  const int64_t tiles = static_cast<int64_t>(f.tiles_k) * f.tiles_n, steps = cdiv(f.a.tokens, kStep);
+  // The largest split of the tokens whose clusters all run at once, each CTA
+  // with at least two steps: half the tokens a CTA and twice the CTAs halve the
+  // time until the join (about four steps) weighs in.
+  int split = tiles == 1 ? 1 : 0, fit = 0;
+  for (int c = 2; c <= 8 && steps >= 2 * c && tiles * c <= device_sm_count(); ++c) {
+    const cudaError_t e = clusters_at_once<TW, true>(c, &fit);
+    if (e) return e;
+    if (tiles <= fit) split = c;
+  }
+  if (split) {
+    f.units = static_cast<int>(tiles);
+    const cudaError_t e = clusters_at_once<TW, true>(split, &fit);
+    if (e) return e;
+    ClusterLaunch l(split, f.units, s);
+    return cudaLaunchKernelEx(&l.cfg, k_wgrad_tc<TW, true>, f);
+  }
+  f.units = (f.tiles_k + 1) / 2 * f.tiles_n;
+  const cudaError_t e = clusters_at_once<TW, false>(2, &fit);
+  if (e) return e;
+  ClusterLaunch l(2, std::min(f.units, fit), s);
+  return cudaLaunchKernelEx(&l.cfg, k_wgrad_tc<TW, false>, f);
 }
 
 }  // namespace
@@ -429,18 +473,7 @@ cudaError_t launch_ckpt_wgrad_tc(const WgradArgs& a, int dw_dtype, cudaStream_t 
     return cudaErrorInvalidValue;
   f.tiles_k = static_cast<int>(cdiv(a.k, kTileK));
   f.tiles_n = static_cast<int>(cdiv(a.n, kTileN));
-  const int64_t tiles = static_cast<int64_t>(f.tiles_k) * f.tiles_n;
-  // the largest split that leaves every cluster a place in the first wave
-  // (clusters of 8 fill about 128 of the 152 SMs) and every CTA some tokens
-  int split = 1;
-  for (int c : {2, 4, 8})
-    if (tiles * c <= (c == 8 ? 128 : 144) && cdiv(a.tokens, kStep) >= 2 * c) split = c;
-  if (split > 1 || tiles == 1) {
-    f.units = static_cast<int>(tiles);
-    return dw_dtype == 0 ? launch_tc<float, true>(f, split, s) : launch_tc<bf16, true>(f, split, s);
-  }
-  f.units = (f.tiles_k + 1) / 2 * f.tiles_n;
-  return dw_dtype == 0 ? launch_tc<float, false>(f, 2, s) : launch_tc<bf16, false>(f, 2, s);
+  return dw_dtype == 0 ? launch_tc<float>(f, s) : launch_tc<bf16>(f, s);
 }
 
 cudaError_t launch_ckpt_wgrad_simt(const WgradArgs& a, int dy_dtype, int dw_dtype, cudaStream_t s) {
