@@ -640,9 +640,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
 }
 
 // Launched as a programmatic dependent of the kernel before it in the stream.
-template <typename K>
-cudaError_t launch(K* kernel, const BwdArgs& f, int heads, size_t smem, cudaStream_t s) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+template <auto kernel>
+cudaError_t launch(const BwdArgs& f, int heads, size_t smem, cudaStream_t s) {
+  const cudaError_t e = allow_smem<kernel>(smem);
   if (e) return e;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
@@ -668,11 +668,11 @@ cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t s, std::stri
     return cudaErrorInvalidValue;
   cudaError_t e;
   if (a.dim <= 64) {
-    e = launch(k_attn_dkdv_tc<64>, f, a.kv_heads, Bwd<64>::kSmem, s);
-    return e ? e : launch(k_attn_dq_tc<64>, f, a.heads, Bwd<64>::kSmem, s);
+    e = launch<k_attn_dkdv_tc<64>>(f, a.kv_heads, Bwd<64>::kSmem, s);
+    return e ? e : launch<k_attn_dq_tc<64>>(f, a.heads, Bwd<64>::kSmem, s);
   }
-  e = launch(k_attn_dkdv_tc<128>, f, a.kv_heads, Bwd<128>::kSmem, s);
-  return e ? e : launch(k_attn_dq_tc<128>, f, a.heads, Bwd<128>::kSmem, s);
+  e = launch<k_attn_dkdv_tc<128>>(f, a.kv_heads, Bwd<128>::kSmem, s);
+  return e ? e : launch<k_attn_dq_tc<128>>(f, a.heads, Bwd<128>::kSmem, s);
 }
 
 }  // namespace normpre

@@ -448,8 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
 
 template <int DP>
 static cudaError_t launch(const FwdArgs& f, int64_t items, cudaStream_t s) {
-  cudaError_t e = cudaFuncSetAttribute(k_attn_fwd_tc<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(Fwd<DP>::kSmem));
+  const cudaError_t e = allow_smem<k_attn_fwd_tc<DP>>(Fwd<DP>::kSmem);
   if (e) return e;
   k_attn_fwd_tc<DP><<<walk_grid(items), kThreads, Fwd<DP>::kSmem, s>>>(f);
   return cudaGetLastError();

@@ -384,9 +384,9 @@ __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ Attn
   if (lane == 0 && row < a.total) a.delta[static_cast<int64_t>(head) * a.tokens + row] = s;
 }
 
-template <typename K>
-cudaError_t run(K* kernel, const AttnArgs& a, int heads, size_t smem, cudaStream_t s) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+template <auto kernel>
+cudaError_t run(const AttnArgs& a, int heads, size_t smem, cudaStream_t s) {
+  const cudaError_t e = allow_smem<kernel>(smem);
   if (e) return e;
   const int64_t tail = (a.tokens - a.total + kB - 1) / kB;
   const dim3 grid(static_cast<unsigned>(2 * static_cast<int64_t>(a.n_blocks) + tail), static_cast<unsigned>(heads));
@@ -401,15 +401,15 @@ template <int DP> constexpr size_t dq_smem() { return sizeof(float) * (4 * kB * 
 
 template <typename T, int DP>
 cudaError_t backward(const AttnArgs& a, cudaStream_t s) {
-  cudaError_t e = run(k_attn_dkdv<T, DP>, a, a.kv_heads, dkdv_smem<DP>(), s);
-  return e ? e : run(k_attn_dq<T, DP>, a, a.heads, dq_smem<DP>(), s);
+  cudaError_t e = run<k_attn_dkdv<T, DP>>(a, a.kv_heads, dkdv_smem<DP>(), s);
+  return e ? e : run<k_attn_dq<T, DP>>(a, a.heads, dq_smem<DP>(), s);
 }
 
 }  // namespace
 
 cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t s) {
-  return a.dim <= 64 ? run(k_attn_fwd<float, 64>, a, a.heads, fwd_smem<64>(), s)
-                     : run(k_attn_fwd<float, 128>, a, a.heads, fwd_smem<128>(), s);
+  return a.dim <= 64 ? run<k_attn_fwd<float, 64>>(a, a.heads, fwd_smem<64>(), s)
+                     : run<k_attn_fwd<float, 128>>(a, a.heads, fwd_smem<128>(), s);
 }
 
 cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s) {

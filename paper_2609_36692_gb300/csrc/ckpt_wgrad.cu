@@ -421,8 +421,7 @@ cudaError_t clusters_at_once(int cluster, int* fit) {
   *fit = known[cluster].load(std::memory_order_relaxed);
   if (*fit) return cudaSuccess;
   ClusterLaunch l(cluster, std::max(1, device_sm_count() / cluster), nullptr);
-  cudaError_t e = cudaFuncSetAttribute(k_wgrad_tc<TW, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(kTcSmem));
+  cudaError_t e = allow_smem<k_wgrad_tc<TW, SPLIT>>(kTcSmem);
   if (!e) e = cudaOccupancyMaxActiveClusters(fit, k_wgrad_tc<TW, SPLIT>, &l.cfg);
   if (!e) known[cluster].store(*fit = std::max(1, *fit), std::memory_order_relaxed);
   return e;

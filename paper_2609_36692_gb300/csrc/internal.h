@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <string>
 #include <vector>
 
@@ -347,6 +348,19 @@ class DeviceGuard {
   int prev_ = 0;
   bool changed_ = false;
 };
+
+// Allows a kernel its dynamic shared memory, once per device.
+template <auto kernel>
+cudaError_t allow_smem(size_t bytes) {
+  static std::atomic<uint64_t> done{0};   // one bit per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (e || (done.load(std::memory_order_relaxed) & bit)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (!e) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 // Device properties cached per process.
 int device_sm_count();

@@ -9,22 +9,35 @@ the differentiable forms.
 """
 from __future__ import annotations
 
+import ctypes
 from typing import Optional, Sequence, Tuple
 
 import torch
 
 from . import normpre as C
-from .optim import _dtype_code
+
+_CODES = {torch.float32: C.NORMPRE_F32, torch.bfloat16: C.NORMPRE_BF16}
+# The handle of a device's current stream, without the Stream object around it
+# (a tenth of a microsecond instead of two).
+_current_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 
-def _stream(x: torch.Tensor, stream=None) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream(x.device)).cuda_stream
+def _dtype_code(x: torch.Tensor) -> int:
+    code = _CODES.get(x.dtype)
+    if code is None:
+        raise TypeError("unsupported dtype %s (float32 or bfloat16)" % x.dtype)
+    return code
 
 
-def _cuda(x: torch.Tensor, name: str) -> torch.Tensor:
-    if not x.is_cuda:
-        raise ValueError("%s must be a CUDA tensor" % name)
-    return x
+def _on(device: torch.device, f, *args) -> None:
+    """f(*args, stream) with `device` current, on its current stream."""
+    index = device.index
+    if _current_device() == index:
+        f(*args, _current_stream(index))
+    else:
+        with torch.cuda.device(index):
+            f(*args, _current_stream(index))
 
 
 def _used_on(stream, *tensors) -> None:
@@ -53,9 +66,10 @@ class PackedAttention:
 
     def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, max_tokens: int, max_seqs: int,
                  dtype: torch.dtype = torch.bfloat16, scale: float = 0.0, device=None):
-        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        index = None if device is None else torch.device(device).index
+        self.device = torch.device("cuda", torch.cuda.current_device() if index is None else index)
         self.dtype, self.n_heads, self.n_kv_heads, self.head_dim = dtype, n_heads, n_kv_heads, head_dim
-        code = {torch.float32: C.NORMPRE_F32, torch.bfloat16: C.NORMPRE_BF16}.get(dtype)
+        code = _CODES.get(dtype)
         if code is None:
             raise TypeError("unsupported dtype %s (float32 or bfloat16)" % dtype)
         self.plan = None
@@ -68,55 +82,63 @@ class PackedAttention:
             s = stream if stream is not None else torch.cuda.current_stream()
             C.normpre_attn_set_lengths(self.plan, lengths, s.cuda_stream)
 
-    def _heads(self, x: torch.Tensor, heads: int, name: str, tokens: Optional[int] = None) -> C.normpre_heads:
+    def _check(self, x: torch.Tensor, name: str, tokens: int, heads: int):
         if x.device != self.device:
             raise ValueError("%s must be on %s" % (name, self.device))
         if x.dtype != self.dtype:
             raise TypeError("%s must be %s" % (name, self.dtype))
-        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.head_dim or \
-                (tokens is not None and x.shape[0] != tokens):
-            raise ValueError("%s must be [%s, %d, %d] (got %s)" % (name, tokens if tokens is not None else "tokens",
-                                                                   heads, self.head_dim, tuple(x.shape)))
-        if x.shape[0] and x.stride(2) != 1:
+        if x.shape != (tokens, heads, self.head_dim):
+            raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, tokens, heads, self.head_dim, tuple(x.shape)))
+        st, sh, sd = x.stride()
+        if sd != 1 and tokens:
             raise ValueError("%s: the last dimension must be contiguous" % name)
-        return C.normpre_heads(x.data_ptr(), x.stride(0), x.stride(1))
+        return x.data_ptr(), st, sh
 
     def _lse(self, lse: torch.Tensor, tokens: int) -> int:
         if lse.device != self.device or lse.dtype != torch.float32 or not lse.is_contiguous() or \
-                tuple(lse.shape) != (self.n_heads, tokens):
+                lse.shape != (self.n_heads, tokens):
             raise ValueError("lse must be a contiguous float32 [%d, %d] tensor on %s" % (self.n_heads, tokens, self.device))
         return lse.data_ptr()
 
-    def _new(self, given, tokens: int, heads: int, stream):
-        if given is None:
-            given = torch.empty(tokens, heads, self.head_dim, dtype=self.dtype, device=self.device)
-            _used_on(stream, given)
-        return given
+    def _new(self, tokens: int, heads: int, stream):
+        x = torch.empty((tokens, heads, self.head_dim), dtype=self.dtype, device=self.device)
+        _used_on(stream, x)
+        return x
 
     def forward(self, q, k, v, out=None, lse=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """(out, lse): [tokens, n_heads, head_dim] and the fp32 log-sums
         [n_heads, tokens] that ``backward`` reads."""
-        t = q.shape[0]
-        args = [self._heads(q, self.n_heads, "q"), self._heads(k, self.n_kv_heads, "k", t),
-                self._heads(v, self.n_kv_heads, "v", t)]
-        out = self._new(out, t, self.n_heads, stream)
+        t, h, hk = q.shape[0], self.n_heads, self.n_kv_heads
+        check = self._check
+        args = (*check(q, "q", t, h), *check(k, "k", t, hk), *check(v, "v", t, hk))
+        if out is None:
+            out = self._new(t, h, stream)
         if lse is None:
-            lse = torch.empty(self.n_heads, t, dtype=torch.float32, device=self.device)
+            lse = torch.empty((h, t), dtype=torch.float32, device=self.device)
             _used_on(stream, lse)
-        C.normpre_attn_forward(self.plan, t, *args, self._heads(out, self.n_heads, "out", t), self._lse(lse, t),
-                               _stream(q, stream))
+        heads = (ctypes.c_int64 * 12)(*args, *check(out, "out", t, h))
+        at = ctypes.addressof(heads)
+        C.normpre_attn_forward(self.plan, t, at, at + 24, at + 48, at + 72, self._lse(lse, t),
+                               _current_stream(self.device.index) if stream is None else stream.cuda_stream)
         return out, lse
 
     def backward(self, q, k, v, out, lse, dout, dq=None, dk=None, dv=None, stream=None):
         """(dq, dk, dv) for the forward pass that gave ``out`` and ``lse``."""
-        t = q.shape[0]
-        h, hk = self.n_heads, self.n_kv_heads
-        args = [self._heads(q, h, "q"), self._heads(k, hk, "k", t), self._heads(v, hk, "v", t),
-                self._heads(out, h, "out", t)]
-        do = self._heads(dout, h, "dout", t)
-        dq, dk, dv = self._new(dq, t, h, stream), self._new(dk, t, hk, stream), self._new(dv, t, hk, stream)
-        C.normpre_attn_backward(self.plan, t, *args, self._lse(lse, t), do, self._heads(dq, h, "dq", t),
-                                self._heads(dk, hk, "dk", t), self._heads(dv, hk, "dv", t), _stream(q, stream))
+        t, h, hk = q.shape[0], self.n_heads, self.n_kv_heads
+        check = self._check
+        args = (*check(q, "q", t, h), *check(k, "k", t, hk), *check(v, "v", t, hk), *check(out, "out", t, h),
+                *check(dout, "dout", t, h))
+        if dq is None:
+            dq = self._new(t, h, stream)
+        if dk is None:
+            dk = self._new(t, hk, stream)
+        if dv is None:
+            dv = self._new(t, hk, stream)
+        heads = (ctypes.c_int64 * 24)(*args, *check(dq, "dq", t, h), *check(dk, "dk", t, hk), *check(dv, "dv", t, hk))
+        at = ctypes.addressof(heads)
+        C.normpre_attn_backward(self.plan, t, at, at + 24, at + 48, at + 72, self._lse(lse, t), at + 96, at + 120,
+                                at + 144, at + 168,
+                                _current_stream(self.device.index) if stream is None else stream.cuda_stream)
         return dq, dk, dv
 
     def __call__(self, q, k, v) -> torch.Tensor:
@@ -169,56 +191,66 @@ class _Attention(torch.autograd.Function):
 # 8-bit activation checkpoints
 # ---------------------------------------------------------------------------
 class Checkpoint:
-    """A [tokens, features] matrix kept in 8 bits (``normpre_ckpt_pack``)."""
+    """A [tokens, features] matrix kept in 8 bits (``normpre_ckpt_pack``):
+    ``codes`` and ``steps`` in one allocation."""
 
-    def __init__(self, codes: torch.Tensor, steps: torch.Tensor, tokens: int, features: int, dtype: torch.dtype):
-        self.codes, self.steps, self.tokens, self.features, self.dtype = codes, steps, tokens, features, dtype
+    __slots__ = ("data", "tokens", "features", "dtype", "device", "nbytes", "codes_ptr", "steps_ptr")
 
-    @classmethod
-    def empty(cls, tokens: int, features: int, dtype: torch.dtype, device) -> "Checkpoint":
-        nc, ns = C.normpre_ckpt_bytes(tokens, features)
-        return cls(torch.empty(nc, dtype=torch.int8, device=device), torch.empty(ns, dtype=torch.uint8, device=device),
-                   tokens, features, dtype)
+    def __init__(self, tokens: int, features: int, dtype: torch.dtype, device: torch.device,
+                 data: Optional[torch.Tensor] = None):
+        # the sizes of normpre_ckpt_bytes; the codes' is a multiple of 32, so the steps are aligned too
+        codes = tokens * ((features + 31) // 32 * 32)
+        self.nbytes = codes + 4 * tokens * ((features + 127) // 128)
+        self.data = torch.empty(self.nbytes, dtype=torch.uint8, device=device) if data is None else data
+        self.tokens, self.features, self.dtype, self.device = tokens, features, dtype, device
+        self.codes_ptr = self.data.data_ptr()
+        self.steps_ptr = self.codes_ptr + codes
 
     @property
-    def nbytes(self) -> int:
-        return self.codes.numel() + self.steps.numel()
+    def codes(self) -> torch.Tensor:
+        return self.data[:self.steps_ptr - self.codes_ptr].view(torch.int8)
+
+    @property
+    def steps(self) -> torch.Tensor:
+        return self.data[self.steps_ptr - self.codes_ptr:]
 
     def restore(self, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The values it stands for, in the dtype of what was packed by default."""
         if out is None:
-            out = torch.empty(self.tokens, self.features, dtype=dtype or self.dtype, device=self.codes.device)
+            out = torch.empty((self.tokens, self.features), dtype=dtype or self.dtype, device=self.device)
         elif dtype is not None and out.dtype != dtype:
             raise TypeError("out must be %s" % dtype)
-        ld = _matrix(out, "out", (self.tokens, self.features))
-        with torch.cuda.device(out.device):
-            C.normpre_ckpt_restore(self.tokens, self.features, self.codes.data_ptr(), self.steps.data_ptr(),
-                                   out.data_ptr(), _dtype_code(out), ld, _stream(out))
+        ld = _matrix(out, "out", (self.tokens, self.features), self.device)
+        _on(self.device, C.normpre_ckpt_restore, self.tokens, self.features, self.codes_ptr, self.steps_ptr,
+            out.data_ptr(), _dtype_code(out), ld)
         return out
 
 
 def _matrix(x: torch.Tensor, name: str, shape=None, device=None) -> int:
     """Checks a 2-D tensor and returns its row stride."""
-    _cuda(x, name)
-    if x.dim() != 2 or (shape is not None and tuple(x.shape) != tuple(shape)):
+    if not x.is_cuda:
+        raise ValueError("%s must be a CUDA tensor" % name)
+    if x.dim() != 2 or (shape is not None and x.shape != shape):
         raise ValueError("%s must be %s (got %s)" % (name, list(shape) if shape is not None else "a matrix", tuple(x.shape)))
     if device is not None and x.device != device:
         raise ValueError("%s must be on %s" % (name, device))
-    if x.shape[1] > 1 and x.stride(1) != 1:
+    rows, cols = x.shape
+    ld, step = x.stride()
+    if cols > 1 and step != 1:
         raise ValueError("%s: rows must be contiguous" % name)
-    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+    if rows <= 1:
+        return cols
+    if ld < cols:
         raise ValueError("%s: rows must not overlap" % name)
-    _dtype_code(x)
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return ld
 
 
 def ckpt_pack(x: torch.Tensor) -> Checkpoint:
     """The 8-bit checkpoint of a [tokens, features] matrix (fp32 or bf16)."""
-    ld = _matrix(x, "x")
-    ck = Checkpoint.empty(x.shape[0], x.shape[1], x.dtype, x.device)
-    with torch.cuda.device(x.device):
-        C.normpre_ckpt_pack(ck.tokens, ck.features, x.data_ptr(), _dtype_code(x), ld, ck.codes.data_ptr(),
-                            ck.steps.data_ptr(), _stream(x))
+    ld, code = _matrix(x, "x"), _dtype_code(x)
+    t, f = x.shape
+    ck = Checkpoint(t, f, x.dtype, x.device)
+    _on(ck.device, C.normpre_ckpt_pack, t, f, x.data_ptr(), code, ld, ck.codes_ptr, ck.steps_ptr)
     return ck
 
 
@@ -226,18 +258,17 @@ def ckpt_wgrad(dy: torch.Tensor, ck: Checkpoint, dtype: Optional[torch.dtype] = 
                out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
     """dW = dY^T xhat, [out_features, features]: the weight gradient of
     y = x W^T from x's checkpoint; added to ``out`` with ``accumulate``."""
-    ld = _matrix(dy, "dy", (ck.tokens, dy.shape[1] if dy.dim() == 2 else -1), ck.codes.device)
+    ld = _matrix(dy, "dy", (ck.tokens, dy.shape[1] if dy.dim() == 2 else -1), ck.device)
     shape = (dy.shape[1], ck.features)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty(shape, dtype=dtype or dy.dtype, device=dy.device)
+        out = torch.empty(shape, dtype=dtype or dy.dtype, device=ck.device)
     elif dtype is not None and out.dtype != dtype:
         raise TypeError("out must be %s" % dtype)
-    out_ld = _matrix(out, "out", shape, dy.device)
-    with torch.cuda.device(dy.device):
-        C.normpre_ckpt_wgrad(ck.tokens, shape[0], shape[1], dy.data_ptr(), _dtype_code(dy), ld, ck.codes.data_ptr(),
-                             ck.steps.data_ptr(), out.data_ptr(), _dtype_code(out), out_ld, accumulate, _stream(dy))
+    out_ld = _matrix(out, "out", shape, ck.device)
+    _on(ck.device, C.normpre_ckpt_wgrad, ck.tokens, shape[0], shape[1], dy.data_ptr(), _dtype_code(dy), ld,
+        ck.codes_ptr, ck.steps_ptr, out.data_ptr(), _dtype_code(out), out_ld, accumulate)
     return out
 
 
@@ -247,29 +278,25 @@ def ckpt_swiglu(gate: torch.Tensor, up: torch.Tensor):
     ul = _matrix(up, "up", gate.shape, gate.device)
     if up.dtype != gate.dtype:
         raise TypeError("gate and up must have one dtype")
+    code, device = _dtype_code(gate), gate.device
     t, f = gate.shape
-    h = torch.empty(t, f, dtype=gate.dtype, device=gate.device)
-    cg = Checkpoint.empty(t, f, gate.dtype, gate.device)
-    cu = Checkpoint.empty(t, f, gate.dtype, gate.device)
-    with torch.cuda.device(gate.device):
-        C.normpre_ckpt_swiglu(t, f, _dtype_code(gate), gate.data_ptr(), gl, up.data_ptr(), ul, h.data_ptr(), f,
-                              cg.codes.data_ptr(), cg.steps.data_ptr(), cu.codes.data_ptr(), cu.steps.data_ptr(),
-                              _stream(gate))
+    h = torch.empty((t, f), dtype=gate.dtype, device=device)
+    cg, cu = Checkpoint(t, f, gate.dtype, device), Checkpoint(t, f, gate.dtype, device)
+    _on(device, C.normpre_ckpt_swiglu, t, f, code, gate.data_ptr(), gl, up.data_ptr(), ul, h.data_ptr(), f,
+        cg.codes_ptr, cg.steps_ptr, cu.codes_ptr, cu.steps_ptr)
     return h, cg, cu
 
 
 def ckpt_swiglu_backward(gate: Checkpoint, up: Checkpoint, dh: torch.Tensor):
     """(dgate, dup) from the checkpoints that ``ckpt_swiglu`` gave."""
     t, f = gate.tokens, gate.features
-    if (up.tokens, up.features) != (t, f):
-        raise ValueError("the checkpoints' shapes differ")
-    ld = _matrix(dh, "dh", (t, f), gate.codes.device)
-    dgate, dup = torch.empty_like(dh, memory_format=torch.contiguous_format), \
-        torch.empty_like(dh, memory_format=torch.contiguous_format)
-    with torch.cuda.device(dh.device):
-        C.normpre_ckpt_swiglu_backward(t, f, _dtype_code(dh), gate.codes.data_ptr(), gate.steps.data_ptr(),
-                                       up.codes.data_ptr(), up.steps.data_ptr(), dh.data_ptr(), ld, dgate.data_ptr(),
-                                       f, dup.data_ptr(), f, _stream(dh))
+    if (up.tokens, up.features) != (t, f) or up.device != gate.device:
+        raise ValueError("the checkpoints' shapes or devices differ")
+    ld, code = _matrix(dh, "dh", (t, f), gate.device), _dtype_code(dh)
+    dgate = torch.empty((t, f), dtype=dh.dtype, device=gate.device)
+    dup = torch.empty((t, f), dtype=dh.dtype, device=gate.device)
+    _on(gate.device, C.normpre_ckpt_swiglu_backward, t, f, code, gate.codes_ptr, gate.steps_ptr, up.codes_ptr,
+        up.steps_ptr, dh.data_ptr(), ld, dgate.data_ptr(), f, dup.data_ptr(), f)
     return dgate, dup
 
 

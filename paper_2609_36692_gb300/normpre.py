@@ -120,7 +120,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.normpre_normalize_cols_noalloc.restype = ctypes.c_int
     lib.normpre_sketch_omega.argtypes = [ctypes.c_uint64, ctypes.c_int, i64, i64, ctypes.c_int, P, P, P, P]
     lib.normpre_sketch_omega.restype = ctypes.c_int
-    HP = ctypes.POINTER(normpre_heads)
+    HP = P       # normpre_heads by reference or by address
     i32 = ctypes.c_int
     lib.normpre_attn_init.argtypes = [ctypes.POINTER(normpre_attn_config), ctypes.POINTER(P)]
     lib.normpre_attn_set_lengths.argtypes = [P, i32, ctypes.POINTER(i64), P]
@@ -265,18 +265,22 @@ def normpre_attn_set_lengths(plan: int, lengths: Sequence[int], stream: int = 0)
     return _check(load_library().normpre_attn_set_lengths(plan, len(lengths), arr, stream))
 
 
-def normpre_attn_forward(plan: int, tokens: int, q: normpre_heads, k: normpre_heads, v: normpre_heads,
-                         out: normpre_heads, lse_ptr: int, stream: int = 0) -> int:
-    r = ctypes.byref
-    return _check(load_library().normpre_attn_forward(plan, int(tokens), r(q), r(k), r(v), r(out), lse_ptr, stream))
+def _by_ref(x):
+    return ctypes.byref(x) if isinstance(x, normpre_heads) else x
 
 
-def normpre_attn_backward(plan: int, tokens: int, q: normpre_heads, k: normpre_heads, v: normpre_heads,
-                          out: normpre_heads, lse_ptr: int, dout: normpre_heads, dq: normpre_heads,
-                          dk: normpre_heads, dv: normpre_heads, stream: int = 0) -> int:
-    r = ctypes.byref
-    return _check(load_library().normpre_attn_backward(plan, int(tokens), r(q), r(k), r(v), r(out), lse_ptr, r(dout),
-                                                       r(dq), r(dk), r(dv), stream))
+def normpre_attn_forward(plan: int, tokens: int, q, k, v, out, lse_ptr: int, stream: int = 0) -> int:
+    """q, k, v, out: ``normpre_heads`` or their addresses."""
+    return _check(load_library().normpre_attn_forward(plan, tokens, _by_ref(q), _by_ref(k), _by_ref(v), _by_ref(out),
+                                                      lse_ptr, stream))
+
+
+def normpre_attn_backward(plan: int, tokens: int, q, k, v, out, lse_ptr: int, dout, dq, dk, dv,
+                          stream: int = 0) -> int:
+    """q .. dv: ``normpre_heads`` or their addresses."""
+    return _check(load_library().normpre_attn_backward(plan, tokens, _by_ref(q), _by_ref(k), _by_ref(v), _by_ref(out),
+                                                       lse_ptr, _by_ref(dout), _by_ref(dq), _by_ref(dk), _by_ref(dv),
+                                                       stream))
 
 
 def normpre_attn_sync_status(plan: int, stream: int = 0, raise_on_error: bool = True) -> int:
