@@ -11,10 +11,10 @@
 // instead of 5.
 //
 // Both: one CTA per SM walks the work list; the owned tiles stay in shared
-// memory, the others pass through a ring filled by a TMA warp; eight softmax
-// warps each take 32 rows x 64 columns of a score tile, one thread per row.  P
+// memory, the others pass through a ring filled by a TMA warp; sixteen softmax
+// warps each take 32 rows x 32 columns of a score tile, one row a thread.  P
 // and dS go back to TMEM as bf16 over the scores they came from (each warp
-// group inside its own half of the columns) and are the A operands of the
+// group inside its own quarter of the columns) and are the A operands of the
 // products that follow.  Two warps issue the MMAs, each one of the two chains
 // below: a thread's MMAs run almost as it issues them, so that while it waits
 // the tensor cores need another's.
@@ -35,14 +35,16 @@
 namespace normpre {
 namespace {
 
-constexpr int kThreads = 384;   // softmax 8 warps, TMA, MMA, statistics and sequence ends, MMA
+constexpr int kSoftmax = 16;    // warps
+constexpr int kTma = 16, kMmaA = 17, kStats = 18, kMmaB = 19;   // warps: TMA, MMA, statistics and sequence ends, MMA
+constexpr int kThreads = 640;
 
 template <int DP> struct Bwd {
   static constexpr int kChunks = DP / 64;
   static constexpr int kTileBytes = kChunks * kChunk;
   static constexpr int kSlots = DP == 128 ? 5 : 8;
   static constexpr int kSets = DP == 128 ? 1 : 2;      // owned tiles, accumulators
-  static constexpr int kOther = 2048 + 768;            // statistics, barriers
+  static constexpr int kOther = 2048 + 512 + 512;      // statistics, barriers, items
   static constexpr size_t kSmem = (2 * kSets + kSlots) * kTileBytes + kOther;
 };
 
@@ -81,16 +83,16 @@ __device__ __forceinline__ void init_bars(Bars<kSlots>* b, int users) {
     tc::mbar_init(&b->own_full[i][1], 1);
     tc::mbar_init(&b->own_empty[i], 2);
     tc::mbar_init(&b->s_full[i], users);             // dK, dV: the scores and their statistics
-    tc::mbar_init(&b->stat_empty[i], 8);
+    tc::mbar_init(&b->stat_empty[i], kSoftmax);
     tc::mbar_init(&b->acc_full[i], users);
-    tc::mbar_init(&b->acc_empty[i], 8);
+    tc::mbar_init(&b->acc_empty[i], kSoftmax);
     tc::mbar_init(&b->drain[i], 1);
     b->own_issued[i] = 0;
   }
   tc::mbar_init(&b->dp_full, 1);
-  tc::mbar_init(&b->p_ready, 8);
-  tc::mbar_init(&b->ds_ready, 8);
-  tc::mbar_init(&b->dp_free, 8);
+  tc::mbar_init(&b->p_ready, kSoftmax);
+  tc::mbar_init(&b->ds_ready, kSoftmax);
+  tc::mbar_init(&b->dp_free, kSoftmax);
   b->abort = 0;
   tc::fence_barrier_init();
 }
@@ -198,39 +200,48 @@ __device__ __forceinline__ void finish(const Warp<kSlots>& w, int warp, int* fla
       if (b->own_issued[i >> 1]) tc::mbar_wait(&b->own_full[i >> 1][i & 1], (b->own_issued[i >> 1] - 1) & 1u, &never);
   }
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kMmaA) {
     tc::fence_after();
     tc::tmem_dealloc(b->tmem, 512);
   }
 }
 
-// A warp's 32 rows x (DP / 2) columns of an accumulator, scaled, to global memory.
+// A warp's 32 rows x (DP / 4) columns of an accumulator, scaled, to the tile
+// at row `row`, of which `rows` exist.
 template <int DP>
-__device__ __forceinline__ void store_acc(const AttnTensor& t, uint32_t acc, int64_t row, bool in, int head, int half,
-                                          float w, int dim) {
-  bf16* p = static_cast<bf16*>(t.p) + row * t.ts + head * t.hs;
-#pragma unroll 1
-  for (int d = half * (DP / 2); d < (half + 1) * (DP / 2); d += 32) {
-    uint32_t o[32];
-    tc::tmem_ld32(acc + d, o);
-    tc::tmem_ld_wait();
-    if (in) store_row32(p, o, w, d, dim);
-  }
+__device__ __forceinline__ void store_acc(const AttnTensor& t, uint32_t acc, int64_t row, int rows, int head, int warp,
+                                          float w, int dim, int lane) {
+  constexpr int kCols = DP / 4;
+  const int part = warp >> 2;
+  uint32_t o[kCols];
+  if constexpr (kCols == 32) tc::tmem_ld32(acc + kCols * part, o);
+  else tc::tmem_ld16(acc + kCols * part, o);
+  tc::tmem_ld_wait();
+  store_rows<kCols>(static_cast<bf16*>(t.p) + row * t.ts + head * t.hs, t.ts, o, w, 32 * (warp & 3), rows, kCols * part,
+                    dim, lane);
 }
 
 struct Item {
   int64_t start;
   int len, blk, head;
 };
-__device__ __forceinline__ bool get_item(const AttnArgs& a, const AttnBlock* list, const int* walk, int heads,
-                                         int64_t r, Item& it) {
+
+constexpr int kCached = 32;
+
+__device__ __forceinline__ ItemRef find_item(const AttnArgs& a, const AttnBlock* list, const int* walk, int heads,
+                                             int64_t r) {
   const int64_t i = walk_item(walk, r, static_cast<int64_t>(a.n_blocks) * heads);
-  if (i < 0) return false;
+  if (i < 0) return ItemRef{0, 0, -1, 0};
   const AttnBlock b = list[i / heads];
+  return ItemRef{b.start, b.len, b.blk, static_cast<int>(i % heads)};
+}
+
+__device__ __forceinline__ bool get_item(const ItemRef& b, Item& it) {
+  if (b.blk < 0) return false;
   it.start = b.start;
   it.len = b.len;
   it.blk = b.blk;
-  it.head = static_cast<int>(i % heads);
+  it.head = b.head;
   return true;
 }
 
@@ -243,14 +254,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   uint8_t* ring = own + 2 * kSets * kTileBytes;       // Q, dO, Q, dO ..
   float* stat = reinterpret_cast<float*>(ring + kSlots * kTileBytes);   // [2][-log2(e) lse, delta][128]
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(stat + 512);
-  static_assert(sizeof(Bars<kSlots>) <= 768, "barriers");
+  static_assert(sizeof(Bars<kSlots>) <= 512, "barriers");
+  ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
   const AttnArgs& a = f.a;
+  auto find = [&](int64_t r) { return find_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r); };
+  auto item = [&](int64_t r) { return r < kCached ? items[r] : find(r); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     init_bars(b, 2);
     for (const CUtensorMap* m : {&f.q, &f.k, &f.v, &f.dout}) tc::prefetch_map(m);
   }
-  if (warp == 9) {
+  if (warp == 2) items[lane] = find(lane);
+  if (warp == kMmaA) {
     tc::tmem_alloc(&b->tmem, 512);
     tc::tmem_relinquish();
     tc::fence_before();
@@ -264,10 +279,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   Turn<kSets> set;
   Item it;
 
-  if (warp == 8) {
+  if (warp == kTma) {
     // ---------------- TMA (one thread), then the rows past the sequences ----------------
     if (tc::elect_one()) {
-      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
         if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.k, &f.v, row, it.head, kChunks)) break;
         for (int g = 0; g < a.group && w.ok; ++g)
@@ -282,13 +297,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     w.ok = __all_sync(0xffffffffu, w.ok);
     zero_padding(a, a.dk, a.kv_heads, blockIdx.x, gridDim.x, lane);
     zero_padding(a, a.dv, a.kv_heads, blockIdx.x, gridDim.x, lane);
-  } else if (warp == 9) {
+  } else if (warp == kMmaA) {
     // ---------------- MMA (one thread): dV(i), S(i + 1) ----------------
     if (tc::elect_one()) {
       uint32_t p_phase = 0;
       int st = 0;                                                 // parity of the block in the walk
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int n = ((it.len - 1) / kTile - it.blk + 1) * a.group;
         const uint32_t k = tc::su32(own + 2 * set.i * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][0], set.parity)) break;
@@ -304,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
           const int o = w.take();
           if (!w.wait1(&b->p_ready, p_phase)) break;
           p_phase ^= 1u;
-          product_ts<DP>(cAcc + 2 * DP * set.i, cS, tile(o), i == 0, 32);
+          product_ts<DP, 4>(cAcc + 2 * DP * set.i, cS, tile(o), i == 0);
           tc::mma_commit(&b->empty[o]);
           if (i + 1 == n) break;
           q = w.take();
@@ -321,12 +336,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     }
     __syncwarp();
     w.ok = __all_sync(0xffffffffu, w.ok);
-  } else if (warp == 11) {
+  } else if (warp == kMmaB) {
     // ---------------- MMA (one thread): dK(i), dP(i + 1) ----------------
     if (tc::elect_one()) {
       uint32_t ds_phase = 0;
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-      for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int n = ((it.len - 1) / kTile - it.blk + 1) * a.group;
         const uint32_t v = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
@@ -340,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         for (int i = 0; i < n; ++i) {
           if (!w.wait1(&b->ds_ready, ds_phase)) break;
           ds_phase ^= 1u;
-          product_ts<DP>(cAcc + 2 * DP * set.i + DP, cP, tile(q), i == 0, 32);
+          product_ts<DP, 4>(cAcc + 2 * DP * set.i + DP, cP, tile(q), i == 0);
           tc::mma_commit(&b->empty[q]);
           if (i + 1 == n) break;
           q = w.take();
@@ -357,12 +372,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     }
     __syncwarp();
     w.ok = __all_sync(0xffffffffu, w.ok);
-  } else if (warp == 10) {
+  } else if (warp == kStats) {
     // ---------------- log-sums and deltas of the query blocks, sequence ends ----------------
     Turn<2> st;
     uint32_t seen = 0;
     int slot = 0;
-    for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r)
+    for (int64_t r = 0; w.ok && get_item(item(r), it); ++r)
       for (int g = 0; g < a.group && w.ok; ++g) {
         const int64_t base = static_cast<int64_t>(it.head * a.group + g) * a.tokens + it.start;
         for (int i = it.blk * kTile; i < it.len; i += kTile) {
@@ -391,26 +406,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
       }
   } else {
     // ---------------- softmax ----------------
-    const int half = warp >> 2, row = 32 * (warp & 3) + lane;    // columns 64 half .., row of the tile
+    const int part = warp >> 2, row = 32 * (warp & 3) + lane;    // columns 32 part .., row of the tile
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t mS = cS + lanes + 64 * half, mP = cP + lanes + 64 * half;
+    const uint32_t mS = cS + lanes + 32 * part, mP = cP + lanes + 32 * part;
     const uint64_t c2 = tc::pack2(a.scale_log2, a.scale_log2);
     uint32_t phase = 0;
     Turn<2> st;
-    for (int64_t r = 0; w.ok && get_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r, it); ++r, set.next()) {
+    for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
       const int nq = (it.len - 1) / kTile - it.blk + 1, n = nq * a.group;
       for (int i = 0; i < n; ++i) {
-        const float* ls = stat + st.i * 256 + 64 * half;
+        const float* ls = stat + st.i * 256 + 32 * part;
         if (!w.wait(&b->s_full[st.i], st.parity)) break;
         const bool diag = i % nq == 0;
-        float p[64];
-        uint32_t pk[32];
-        uint32_t x[64];
+        float p[32];
+        uint32_t pk[16];
+        uint32_t x[32];
         tc::tmem_ld32(mS, x);
-        tc::tmem_ld32(mS + 32, x + 32);
         tc::tmem_ld_wait();
 #pragma unroll
-        for (int e = 0; e < 64; e += 4) {
+        for (int e = 0; e < 32; e += 4) {
           const ulonglong2 l2 = *reinterpret_cast<const ulonglong2*>(ls + e);
           float y[4];
           tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, l2.x), y[0], y[1]);
@@ -420,21 +434,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         }
         if (diag) {   // key `row` is seen by queries row ..
 #pragma unroll
-          for (int e = 0; e < 64; ++e)
-            if (64 * half + e < row) p[e] = 0.f;
+          for (int e = 0; e < 32; ++e)
+            if (32 * part + e < row) p[e] = 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) pk[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
-        tc::tmem_put32(mS, pk);
+        for (int e = 0; e < 16; ++e) pk[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
+        tc::tmem_put16(mS, pk);
         tc::tmem_st_drain();
         w.arrive(&b->p_ready);
         if (!w.wait(&b->dp_full, phase)) break;
         phase ^= 1u;
         tc::tmem_ld32(mP, x);
-        tc::tmem_ld32(mP + 32, x + 32);
         tc::tmem_ld_wait();
 #pragma unroll
-        for (int e = 0; e < 64; e += 4) {
+        for (int e = 0; e < 32; e += 4) {
           const float4 de = *reinterpret_cast<const float4*>(ls + 128 + e);
           const float d4[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
@@ -444,23 +457,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         }
         if (diag) {   // 0 * NaN in an unseen place
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            if (64 * half + 2 * e < row) pk[e] &= 0xFFFF0000u;
-            if (64 * half + 2 * e + 1 < row) pk[e] &= 0x0000FFFFu;
+          for (int e = 0; e < 16; ++e) {
+            if (32 * part + 2 * e < row) pk[e] &= 0xFFFF0000u;
+            if (32 * part + 2 * e + 1 < row) pk[e] &= 0x0000FFFFu;
           }
         }
-        tc::tmem_put32(mP, pk);
+        tc::tmem_put16(mP, pk);
         tc::tmem_st_drain();
         w.arrive(&b->ds_ready);
         if (lane == 0) tc::mbar_arrive(&b->stat_empty[st.i]);
         st.next();
       }
       if (!w.wait(&b->acc_full[set.i], set.parity)) break;
-      const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk + row;
-      const bool in = kTile * it.blk + row < it.len;
+      const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk;
+      const int rows = it.len - kTile * it.blk;
       const uint32_t acc = cAcc + 2 * DP * set.i + lanes;
-      store_acc<DP>(a.dv, acc, at, in, it.head, half, 1.f, a.dim);
-      store_acc<DP>(a.dk, acc + DP, at, in, it.head, half, a.scale, a.dim);
+      store_acc<DP>(a.dv, acc, at, rows, it.head, warp, 1.f, a.dim, lane);
+      store_acc<DP>(a.dk, acc + DP, at, rows, it.head, warp, a.scale, a.dim, lane);
       w.arrive(&b->acc_empty[set.i]);
     }
   }
@@ -475,13 +488,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
   uint8_t* own = smem;                                // [kSets] Q, dO
   uint8_t* ring = own + 2 * kSets * kTileBytes;       // K, V, K, V ..
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(ring + kSlots * kTileBytes);
+  ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
   const AttnArgs& a = f.a;
+  auto find = [&](int64_t r) { return find_item(a, a.by_query, a.walk_dq, a.heads, r); };
+  auto item = [&](int64_t r) { return r < kCached ? items[r] : find(r); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     init_bars(b, 1);
     for (const CUtensorMap* m : {&f.q, &f.k, &f.v, &f.dout}) tc::prefetch_map(m);
   }
-  if (warp == 9) {
+  if (warp == 2) items[lane] = find(lane);
+  if (warp == kMmaA) {
     tc::tmem_alloc(&b->tmem, 512);
     tc::tmem_relinquish();
     tc::fence_before();
@@ -494,10 +511,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
   Turn<2> buf;                                                    // of S
   Item it;
 
-  if (warp == 8) {
+  if (warp == kTma) {
     // ---------------- TMA (one thread), then the rows past the sequences ----------------
     if (tc::elect_one()) {
-      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
         if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.q, &f.dout, row, it.head, kChunks)) break;
         for (int j = 0; j <= it.blk && w.ok; ++j) {
@@ -509,12 +526,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     }
     w.ok = __all_sync(0xffffffffu, w.ok);
     zero_padding(a, a.dq, a.heads, blockIdx.x, gridDim.x, lane);
-  } else if (warp == 9) {
+  } else if (warp == kMmaA) {
     // ---------------- MMA (one thread): dQ(j), S(j + 2) ----------------
     if (tc::elect_one()) {
       uint32_t ds_phase = 0;
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int n = it.blk + 1;
         const uint32_t q = tc::su32(own + 2 * set.i * kTileBytes);
         int k[2] = {0, 0};                                        // ring slots of K(j), K(j + 1)
@@ -533,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         for (int j = 0; j < n; ++j) {
           if (!w.wait1(&b->ds_ready, ds_phase)) break;
           ds_phase ^= 1u;
-          product_ts<DP>(cAcc + DP * set.i, cS + 128 * (buf.i ^ (j & 1)), tile(k[0]), j == 0, 32);
+          product_ts<DP, 4>(cAcc + DP * set.i, cS + 128 * (buf.i ^ (j & 1)), tile(k[0]), j == 0);
           tc::mma_commit(&b->empty[k[0]]);
           k[0] = k[1];
           if (j + 2 < n) {
@@ -548,11 +565,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     }
     __syncwarp();
     w.ok = __all_sync(0xffffffffu, w.ok);
-  } else if (warp == 11) {
+  } else if (warp == kMmaB) {
     // ---------------- MMA (one thread): dP(j) ----------------
     if (tc::elect_one()) {
       uint32_t free_phase = 0;
-      for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const uint32_t o = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
         for (int j = 0; j <= it.blk; ++j) {
@@ -571,38 +588,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     }
     __syncwarp();
     w.ok = __all_sync(0xffffffffu, w.ok);
-  } else if (warp == 10) {
+  } else if (warp == kStats) {
     // ---------------- sequence ends: K's rows past them become zeros ----------------
     uint32_t seen = 0;
     int next = 0;                                                 // ring slot of the item's first tile
-    for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r) {
+    for (int64_t r = 0; w.ok && get_item(item(r), it); ++r) {
       const int rows = it.len - kTile * it.blk;
       if (rows < kTile) w.end_tile(ring, kTileBytes, (next + 2 * it.blk) % kSlots, seen, rows, kChunks);
       next = (next + 2 * (it.blk + 1)) % kSlots;
     }
   } else {
     // ---------------- softmax ----------------
-    const int half = warp >> 2, row = 32 * (warp & 3) + lane;
+    const int part = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint64_t c2 = tc::pack2(a.scale_log2, a.scale_log2);
     uint32_t dp_phase = 0;
-    for (int64_t r = 0; w.ok && get_item(a, a.by_query, a.walk_dq, a.heads, r, it); ++r, set.next()) {
-      const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk + row;
-      const bool in = kTile * it.blk + row < it.len;
-      const int64_t si = static_cast<int64_t>(it.head) * a.tokens + at;
+    for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
+      const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk;
+      const int rows = it.len - kTile * it.blk;
+      const bool in = row < rows;
+      const int64_t si = static_cast<int64_t>(it.head) * a.tokens + at + row;
       const float ls = in ? a.lse[si] * -kLog2e : -INFINITY, de = in ? a.delta[si] : 0.f;
       const uint64_t ls2 = tc::pack2(ls, ls);
       for (int j = 0; j <= it.blk; ++j, buf.next()) {
-        const uint32_t mS = cS + 128 * buf.i + lanes + 64 * half, mP = cP + lanes + 64 * half;
+        const uint32_t mS = cS + 128 * buf.i + lanes + 32 * part, mP = cP + lanes + 32 * part;
         if (!w.wait(&b->s_full[buf.i], buf.parity)) break;
-        float p[64];
-        uint32_t pk[32];
-        uint32_t x[64];
+        float p[32];
+        uint32_t pk[16];
+        uint32_t x[32];
         tc::tmem_ld32(mS, x);
-        tc::tmem_ld32(mS + 32, x + 32);
         tc::tmem_ld_wait();
 #pragma unroll
-        for (int e = 0; e < 64; e += 2) {
+        for (int e = 0; e < 32; e += 2) {
           float y0, y1;
           tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, ls2), y0, y1);
           p[e] = tc::exp2_fast(y0);
@@ -611,25 +628,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         if (!w.wait(&b->dp_full, dp_phase)) break;
         dp_phase ^= 1u;
         tc::tmem_ld32(mP, x);
-        tc::tmem_ld32(mP + 32, x + 32);
         tc::tmem_ld_wait();
         w.arrive(&b->dp_free);
 #pragma unroll
-        for (int e = 0; e < 64; e += 2)
+        for (int e = 0; e < 32; e += 2)
           pk[e / 2] = pack_bf16x2(p[e] * (__uint_as_float(x[e]) - de), p[e + 1] * (__uint_as_float(x[e + 1]) - de));
         if (j == it.blk) {   // query `row` sees keys .. row
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            if (64 * half + 2 * e > row) pk[e] &= 0xFFFF0000u;
-            if (64 * half + 2 * e + 1 > row) pk[e] &= 0x0000FFFFu;
+          for (int e = 0; e < 16; ++e) {
+            if (32 * part + 2 * e > row) pk[e] &= 0xFFFF0000u;
+            if (32 * part + 2 * e + 1 > row) pk[e] &= 0x0000FFFFu;
           }
         }
-        tc::tmem_put32(mS, pk);
+        tc::tmem_put16(mS, pk);
         tc::tmem_st_drain();
         w.arrive(&b->ds_ready);
       }
       if (!w.wait(&b->acc_full[set.i], set.parity)) break;
-      store_acc<DP>(a.dq, cAcc + DP * set.i + lanes, at, in, it.head, half, a.scale, a.dim);
+      store_acc<DP>(a.dq, cAcc + DP * set.i + lanes, at, rows, it.head, warp, a.scale, a.dim, lane);
       w.arrive(&b->acc_empty[set.i]);
     }
   }

@@ -40,7 +40,7 @@ template <int DP> struct Fwd {
   static constexpr int kTileBytes = kChunks * kChunk;
   static constexpr int kSlots = DP == 128 ? 5 : 10;    // K / V ring
   static constexpr int kAcc = DP == 128 ? 1 : 2;       // output accumulators of a tile
-  static constexpr size_t kSmem = (2 + kSlots) * kTileBytes + 1024;
+  static constexpr size_t kSmem = (2 + kSlots) * kTileBytes + 2048;
 };
 
 struct FwdArgs {
@@ -70,22 +70,29 @@ struct Item {
   int kvh;
 };
 
-__device__ __forceinline__ bool get_item(const FwdArgs& f, int64_t r, Item& it) {
+constexpr int kCached = 64;
+
+__device__ __forceinline__ ItemRef find_item(const FwdArgs& f, int64_t r) {
   const int per = f.pair_heads ? f.a.heads / 2 : f.a.heads;
   const int64_t i = walk_item(f.a.walk_fwd, r, static_cast<int64_t>(f.n_list) * per);
-  if (i < 0) return false;
+  if (i < 0) return ItemRef{0, 0, -1, 0};
   const AttnBlock b = f.list[i / per];
-  const int h = static_cast<int>(i % per);
+  return ItemRef{b.start, b.len, b.blk, static_cast<int>(i % per)};
+}
+
+__device__ __forceinline__ bool get_item(const FwdArgs& f, const ItemRef* cached, int64_t r, Item& it) {
+  const ItemRef b = r < kCached ? cached[r] : find_item(f, r);
+  if (b.blk < 0) return false;
   it.start = b.start;
   it.len = b.len;
   it.blk0 = b.blk;
   if (f.pair_heads) {
     it.blk1 = b.blk;
-    it.head0 = 2 * h;
-    it.head1 = 2 * h + 1;
+    it.head0 = 2 * b.head;
+    it.head1 = 2 * b.head + 1;
   } else {
     it.blk1 = (b.blk + 1) * kTile < b.len ? b.blk + 1 : -1;
-    it.head0 = it.head1 = h;
+    it.head0 = it.head1 = b.head;
   }
   it.top = max(it.blk0, it.blk1);
   it.kvh = it.head0 / f.a.group;
@@ -101,6 +108,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
   uint8_t* ring = smem + 2 * kTileBytes;       // [kSlots]
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(ring + kSlots * kTileBytes);
   static_assert(sizeof(Bars<kSlots>) <= 1024, "barriers");
+  ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 1024);   // [kCached]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -129,6 +137,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
     tc::prefetch_map(&f.k);
     tc::prefetch_map(&f.v);
   }
+  if (threadIdx.x >= 64 && threadIdx.x < 64 + kCached) items[threadIdx.x - 64] = find_item(f, threadIdx.x - 64);
   if (warp == 9) {
     tc::tmem_alloc(&b->tmem, 512);
     tc::tmem_relinquish();
@@ -160,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           load_rows(ring + slot * kTileBytes, map, bar, row, head, kChunks);
           if (++slot == kSlots) { slot = 0; phase ^= 1u; }
         };
-        for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
+        for (int64_t r = 0; ok && get_item(f, items, r, it); ++r) {
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             const int blk = s ? it.blk1 : it.blk0;
@@ -190,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       // ---------------- sequence ends: V's rows past them become zeros ----------------
       int next = 0;             // ring slot of the item's first tile
       uint32_t seen = 0;        // per slot, parity of its raw barrier
-      for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
+      for (int64_t r = 0; ok && get_item(f, items, r, it); ++r) {
         const int rows = it.len - kTile * it.top;
         if (rows < kTile) {
           const int slot = next + 1 == kSlots ? 0 : next + 1;
@@ -241,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           tc::mma_commit(&b->s_full[s]);
           tc::mma_commit(&b->empty[k]);
         };
-        for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
+        for (int64_t r = 0; ok && get_item(f, items, r, it); ++r) {
           const int blk = s ? it.blk1 : it.blk0;
           int k = take();
           if (blk >= 0 && !wait(&b->q_full[s], q_phase)) break;
@@ -265,9 +274,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
                 o_phase ^= 1u << acc;
               }
               if (!wait(&b->p_ready[s][0], p_phase) || !my_turn()) break;
-              product_ts<DP, 0, 6>(o, p, tile(v), j == blk, 0);
+              product_ts<DP, 1, 0, 6>(o, p, tile(v), j == blk);
               if (!wait(&b->p_ready[s][1], p_phase)) break;
-              product_ts<DP, 6, 8>(o, p, tile(v), false, 0);
+              product_ts<DP, 1, 6, 8>(o, p, tile(v), false);
               p_phase ^= 1u;
               tc::mma_commit(&b->pv_done[s]);
               tc::mma_commit(&b->empty[v]);
@@ -309,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       tc::fence_after();
       return ok;
     };
-    for (int64_t r = 0; ok && get_item(f, r, it); ++r) {
+    for (int64_t r = 0; ok && get_item(f, items, r, it); ++r) {
       const int blk = s ? it.blk1 : it.blk0;
       if (blk < 0) continue;
       const uint32_t oc = o_col(s, acc) + lanes;
@@ -403,8 +412,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       }
       if (!ok || !wait(&b->pv_done[s], (pv - 1) & 1u)) break;
       const float inv = 1.f / l;
-      const int i = kTile * blk + row;                    // of the sequence
-      const int64_t at = it.start + i;
+      const int rows = it.len - kTile * blk;              // of the tile
+      const int64_t at = it.start + static_cast<int64_t>(kTile) * blk;
       const int head = s ? it.head1 : it.head0;
       bf16* out = static_cast<bf16*>(f.a.o.p) + at * f.a.o.ts + head * f.a.o.hs;
 #pragma unroll 1
@@ -412,13 +421,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
         uint32_t o[32];
         tc::tmem_ld32(oc + d, o);
         tc::tmem_ld_wait();
-        if (i < it.len) store_row32(out, o, inv, d, f.a.dim);
+        store_rows<32>(out, f.a.o.ts, o, inv, 32 * q4, rows, d, f.a.dim, lane);
       }
       tc::fence_before();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&b->o_empty[s][acc]);
       if (kAcc == 2) acc ^= 1;
-      if (i < it.len) f.a.lse[static_cast<int64_t>(head) * f.a.tokens + at] = (m * c + log2f(l)) * 0.6931471805599453f;
+      if (row < rows)
+        f.a.lse[static_cast<int64_t>(head) * f.a.tokens + at + row] = (m * c + log2f(l)) * 0.6931471805599453f;
     }
   }
   if (!ok && lane == 0) {

@@ -55,15 +55,17 @@ __device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b) {
 #pragma unroll
   for (int kk = K0; kk < K1; ++kk) tc::mma_bf16(d, ad + cols_step(kk), bd + cols_step(kk), idesc, kk != 0);
 }
-// D (+)= A B over rows 16 K0 .. 16 K1 of B: A in TMEM, its columns 64 .. 127
-// `gap` columns further on.
-template <int DP, int K0 = 0, int K1 = 8>
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, bool first, int gap) {
+// D (+)= A B over rows 16 K0 .. 16 K1 of B: A in TMEM as bf16, two a column;
+// `spread` (1, 2, 4): its columns lie in that many parts, each at the start of
+// its share of 128 columns.
+template <int DP, int spread, int K0 = 0, int K1 = 8>
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, bool first) {
   constexpr uint32_t idesc = tc::idesc_bf16(kTile, DP, 0, 1);
   const uint64_t bd = desc_rows(b);
 #pragma unroll
   for (int kk = K0; kk < K1; ++kk)
-    tc::mma_bf16_ta(d, a + kk * 8 + (kk >= 4 ? gap : 0), bd + rows_step(kk), idesc, !first || kk != K0);
+    tc::mma_bf16_ta(d, a + 8 * kk + (kk * spread / 8) * (spread == 1 ? 0 : 64 / spread), bd + rows_step(kk), idesc,
+                    !first || kk != K0);
 }
 
 // Zeroes rows [rows, 128) of a tile in shared memory (one warp): what follows
@@ -88,17 +90,49 @@ __device__ __forceinline__ void zero_padding(const AttnArgs& a, const AttnTensor
   }
 }
 
-// 32 fp32 columns of a thread's row, scaled, as bf16 at p (columns c .. of `dim`).
-__device__ __forceinline__ void store_row32(bf16* p, const uint32_t* r, float w, int c, int dim) {
+// A warp's 32 rows x N (16 or 32) fp32 columns, one row a thread, scaled, to
+// global memory as bf16: columns c .. of rows row0 .. of a tile whose first
+// `rows` exist.  The lanes of 2 or 4 rows exchange their 16-byte pieces first,
+// so that a row's piece of 2 N bytes leaves in one instruction: scattered
+// 16-byte stores took several microseconds a tile.
+template <int N>
+__device__ __forceinline__ void store_rows(bf16* tile, int64_t ts, const uint32_t* r, float w, int row0, int rows, int c,
+                                           int dim, int lane) {
+  constexpr int kPieces = N / 8;
+  static_assert(kPieces == 2 || kPieces == 4, "pieces");
+  uint32_t v[kPieces][4];
 #pragma unroll
-  for (int i = 0; i < 32; i += 8) {
-    uint32_t v[4];
+  for (int i = 0; i < kPieces; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      v[e] = pack_bf16x2(__uint_as_float(r[i + 2 * e]) * w, __uint_as_float(r[i + 2 * e + 1]) * w);
-    if (c + i < dim) *reinterpret_cast<uint4*>(p + c + i) = make_uint4(v[0], v[1], v[2], v[3]);
-  }
+      v[i][e] = pack_bf16x2(__uint_as_float(r[8 * i + 2 * e]) * w, __uint_as_float(r[8 * i + 2 * e + 1]) * w);
+  // piece i of row (lane & ~(kPieces - 1)) + k comes to lane i of the group, as its v[k]
+#pragma unroll
+  for (int o = 1; o < kPieces; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (!(i & o)) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t give = up ? v[i][e] : v[i | o][e];
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, give, o);
+          if (up) v[i][e] = got; else v[i | o][e] = got;
+        }
+      }
+  const int piece = lane & (kPieces - 1), first = row0 + (lane & ~(kPieces - 1));
+  bf16* p = tile + first * ts + c + 8 * piece;
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k)
+    if (first + k < rows && c + 8 * piece < dim)
+      *reinterpret_cast<uint4*>(p + k * ts) = make_uint4(v[k][0], v[k][1], v[k][2], v[k][3]);
 }
+
+// The first items of a CTA, resolved once into shared memory: looking one up
+// is two dependent global loads, a microsecond between two items otherwise.
+struct ItemRef {
+  int start, len, blk, head;   // blk -1: no item
+};
 
 // Map of a [tokens][heads][dim] bf16 tensor for boxes of 128 rows x 64 columns.
 inline bool rows_map(CUtensorMap* m, const AttnTensor& t, int tokens, int heads, int dim, std::string* err) {
