@@ -23,10 +23,8 @@
 // 2^8 relative to the row's maximum, which bf16 and the fp32 sums hold as
 // precisely, and the rescale, which has to wait for P V, is rare.
 //
-// Roundings to bf16: P once (the MMA operand; l sums the unrounded values) and
-// the output once.
-#include <type_traits>
-
+// Roundings to bf16: P once (the MMA operand; l sums the uncut values) and the
+// output once.
 #include "attn_tc.cuh"
 
 namespace normpre {
@@ -34,6 +32,14 @@ namespace {
 
 constexpr int kThreads = 384;   // softmax 2 x 4 warps, TMA, MMA of tile 0, sequence ends, MMA of tile 1
 constexpr float kGrow = 8.f;    // log2 of the growth that raises the maximum
+// P is cut to bf16, not rounded: the pack instruction that cuts two values runs
+// beside the exponentials, while a rounding conversion takes their pipe.  A cut
+// loses between nothing and 2^-7 of a number's leading bit, 0.0028 (2^-8 / (2
+// ln 2)) of the number on average; P is therefore formed 1.0028 times as large,
+// which leaves the cut values right on average (their spread is that of
+// rounding), and the row's sum, of uncut values, is divided by it.
+constexpr float kUnbias = 0.0040596f;           // log2(1.0028179)
+constexpr float kUnbiasScale = 0.9971900f;      // 1 / 1.0028179
 
 template <int DP> struct Fwd {
   static constexpr int kChunks = DP / 64;
@@ -273,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
                 if (!wait(&b->o_empty[s][acc], ((o_phase >> acc) & 1u) ^ 1u)) break;
                 o_phase ^= 1u << acc;
               }
-              if (!wait(&b->p_ready[s][0], p_phase) || !my_turn()) break;
+              if (!my_turn() || !wait(&b->p_ready[s][0], p_phase)) break;
               product_ts<DP, 1, 0, 6>(o, p, tile(v), j == blk);
               if (!wait(&b->p_ready[s][1], p_phase)) break;
               product_ts<DP, 1, 6, 8>(o, p, tile(v), false);
@@ -326,49 +332,40 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       for (int j = blk; j >= 0; --j) {
         if (!wait(&b->s_full[s], s_phase)) break;
         s_phase ^= 1u;
-        uint32_t x[128];
+        uint32_t x[32];                 // a quarter of the row's scores
+        uint32_t p[48];
+        uint64_t sum[2] = {0, 0};
+        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto load = [&](int q) {
+          tc::tmem_ld32(sc + 32 * q, x);
+          tc::tmem_ld_wait();
+        };
+        auto mask = [&](int q) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tc::tmem_ld32(sc + 32 * i, x + 32 * i);
-        tc::tmem_ld_wait();
-        auto top = [&]() {
-          float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          for (int i = 0; i < 32; ++i)
+            if (32 * q + i > row) x[i] = 0xFF800000u;
+        };
+        auto compare = [&]() {
 #pragma unroll
-          for (int i = 0; i < 128; i += 8)
+          for (int i = 0; i < 32; i += 8)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               t[e] = fmaxf(fmaxf(t[e], __uint_as_float(x[i + 2 * e])), __uint_as_float(x[i + 2 * e + 1]));
-          return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
         };
-        if (j == blk) {
-#pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i > row) x[i] = 0xFF800000u;
-          m = top();
-        }
-        // exponentials of columns 2 I0 .. 2 I1 with the running maximum, into P
-        uint32_t p[64];
-        uint64_t sum[2];
-        auto exps = [&](auto first, auto last) {
-          const float mc = -m * c;
+        auto top = [&]() { return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])); };
+        // the quarter's exponentials with the running maximum, as P and into the sum
+        auto exps = [&](uint32_t* to) {
+          const float mc = fmaf(-m, c, kUnbias);
           const uint64_t mc2 = tc::pack2(mc, mc);
-          sum[0] = sum[1] = 0;
 #pragma unroll
-          for (int i = decltype(first)::value; i < decltype(last)::value; ++i) {
+          for (int i = 0; i < 16; ++i) {
             float lo, hi;
             tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), c2, mc2), lo, hi);
             lo = tc::exp2_fast(lo);
             hi = tc::exp2_fast(hi);
             sum[i & 1] = tc::add2(sum[i & 1], tc::pack2(lo, hi));
-            p[i] = pack_bf16x2(lo, hi);
+            to[i] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
           }
-        };
-        using I0 = std::integral_constant<int, 0>;
-        using I48 = std::integral_constant<int, 48>;
-        using I64 = std::integral_constant<int, 64>;
-        auto add_sum = [&]() {
-          float lo, hi;
-          tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
-          l += lo + hi;
         };
         auto release = [&](int part) {
           tc::tmem_st_drain();
@@ -376,11 +373,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(&b->p_ready[s][part]);
         };
-        // The maximum of a later block is needed only to see whether the
-        // running one must be raised, which is rare: its comparisons run in
-        // the shadow of the exponentials.
-        exps(I0{}, I48{});
-        if (j != blk) {
+        // Three quarters of P go first: the products on them cover the rest.
+        if (j == blk) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            load(q);
+            mask(q);
+            compare();
+          }
+          m = top();
+#pragma unroll
+          for (int q = 0; q < 3; ++q) {
+            load(q);
+            mask(q);
+            exps(p + 16 * q);
+          }
+          load(3);
+          mask(3);
+        } else {
+          // A later block's maximum is needed only to see whether the running
+          // one must be raised, which is rare: its comparisons run in the
+          // shadow of the exponentials.
+#pragma unroll
+          for (int q = 0; q < 3; ++q) {
+            load(q);
+            compare();
+            exps(p + 16 * q);
+          }
+          load(3);
+          compare();
           const float up = fmaxf(m, top());
           if (__any_sync(0xffffffffu, (up - m) * c > kGrow)) {
             const float keep = tc::exp2_fast((m - up) * c);
@@ -396,21 +417,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
               for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
               tc::tmem_put32(oc + i, o);
             }
-            exps(I0{}, I48{});
+            sum[0] = sum[1] = 0;
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+              load(q);
+              exps(p + 16 * q);
+            }
+            load(3);
           }
         }
-        add_sum();
-        // three quarters of P first: the products on them cover the rest
         tc::tmem_put32(sc, p);
         tc::tmem_put16(sc + 32, p + 32);
         release(0);
-        exps(I48{}, I64{});
-        tc::tmem_put16(sc + 48, p + 48);
+        exps(p);
+        tc::tmem_put16(sc + 48, p);
         release(1);
-        add_sum();
+        float lo, hi;
+        tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
+        l += lo + hi;
         ++pv;
       }
       if (!ok || !wait(&b->pv_done[s], (pv - 1) & 1u)) break;
+      l *= kUnbiasScale;
       const float inv = 1.f / l;
       const int rows = it.len - kTile * blk;              // of the tile
       const int64_t at = it.start + static_cast<int64_t>(kTile) * blk;

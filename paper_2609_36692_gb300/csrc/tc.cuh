@@ -53,17 +53,17 @@ constexpr uint64_t kWaitNs = 2000000000ull;
 // The global timer is read only after many tries: reading it costs
 // microseconds, more than most waits last.
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  if (mbar_try_wait(bar, parity)) return true;
   uint64_t t0 = 0;
-  for (uint32_t i = 1;; ++i) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if ((i & 255u) == 0) {
+  uint32_t i = 0;
+  while (!mbar_try_wait(bar, parity)) {
+    if ((++i & 255u) == 0) {
       if (*abort_flag) return false;
       const uint64_t t = globaltimer();
       if (t0 == 0) t0 = t;
       if (t - t0 > kWaitNs) return false;
     }
   }
+  return true;
 }
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0,
                                             int c1, int c2) {
