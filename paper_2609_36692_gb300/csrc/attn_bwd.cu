@@ -29,7 +29,8 @@
 // second set of accumulators, so that an item's start and end overlap its
 // neighbours.
 //
-// Roundings to bf16: P and dS once each (MMA operands), the gradients once.
+// Roundings to bf16: P and dS once each (MMA operands; kUnbias), the gradients
+// once.
 #include "attn_tc.cuh"
 
 namespace normpre {
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* own = smem;                                // [kSets] K, V
   uint8_t* ring = own + 2 * kSets * kTileBytes;       // Q, dO, Q, dO ..
-  float* stat = reinterpret_cast<float*>(ring + kSlots * kTileBytes);   // [2][-log2(e) lse, delta][128]
+  float* stat = reinterpret_cast<float*>(ring + kSlots * kTileBytes);   // [2][log2(1.0028) - log2(e) lse, delta][128]
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(stat + 512);
   static_assert(sizeof(Bars<kSlots>) <= 512, "barriers");
   ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int j = i + 32 * e + lane;
-            ls[e] = j < it.len ? a.lse[base + j] * -kLog2e : -INFINITY;   // past the end: P = 0
+            ls[e] = j < it.len ? fmaf(a.lse[base + j], -kLog2e, kUnbias) : -INFINITY;   // past the end: P = 0
             de[e] = j < it.len ? a.delta[base + j] : 0.f;
           }
           const int s0 = slot, s1 = s0 + 1 == kSlots ? 0 : s0 + 1;
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
             if (32 * part + e < row) p[e] = 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) pk[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
+        for (int e = 0; e < 16; ++e) pk[e] = cut_bf16x2(p[2 * e], p[2 * e + 1]);
         tc::tmem_put16(mS, pk);
         tc::tmem_st_drain();
         w.arrive(&b->p_ready);
@@ -452,8 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
           const float d4[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
           for (int u = 0; u < 4; u += 2)
-            pk[(e + u) / 2] = pack_bf16x2(p[e + u] * (__uint_as_float(x[e + u]) - d4[u]),
-                                          p[e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]));
+            pk[(e + u) / 2] = cut_bf16x2(p[e + u] * (__uint_as_float(x[e + u]) - d4[u]),
+                                         p[e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]));
         }
         if (diag) {   // 0 * NaN in an unseen place
 #pragma unroll
@@ -608,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       const int rows = it.len - kTile * it.blk;
       const bool in = row < rows;
       const int64_t si = static_cast<int64_t>(it.head) * a.tokens + at + row;
-      const float ls = in ? a.lse[si] * -kLog2e : -INFINITY, de = in ? a.delta[si] : 0.f;
+      const float ls = in ? fmaf(a.lse[si], -kLog2e, kUnbias) : -INFINITY, de = in ? a.delta[si] : 0.f;
       const uint64_t ls2 = tc::pack2(ls, ls);
       for (int j = 0; j <= it.blk; ++j, buf.next()) {
         const uint32_t mS = cS + 128 * buf.i + lanes + 32 * part, mP = cP + lanes + 32 * part;
@@ -632,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         w.arrive(&b->dp_free);
 #pragma unroll
         for (int e = 0; e < 32; e += 2)
-          pk[e / 2] = pack_bf16x2(p[e] * (__uint_as_float(x[e]) - de), p[e + 1] * (__uint_as_float(x[e + 1]) - de));
+          pk[e / 2] = cut_bf16x2(p[e] * (__uint_as_float(x[e]) - de), p[e + 1] * (__uint_as_float(x[e + 1]) - de));
         if (j == it.blk) {   // query `row` sees keys .. row
 #pragma unroll
           for (int e = 0; e < 16; ++e) {

@@ -32,14 +32,6 @@ namespace {
 
 constexpr int kThreads = 384;   // softmax 2 x 4 warps, TMA, MMA of tile 0, sequence ends, MMA of tile 1
 constexpr float kGrow = 8.f;    // log2 of the growth that raises the maximum
-// P is cut to bf16, not rounded: the pack instruction that cuts two values runs
-// beside the exponentials, while a rounding conversion takes their pipe.  A cut
-// loses between nothing and 2^-7 of a number's leading bit, 0.0028 (2^-8 / (2
-// ln 2)) of the number on average; P is therefore formed 1.0028 times as large,
-// which leaves the cut values right on average (their spread is that of
-// rounding), and the row's sum, of uncut values, is divided by it.
-constexpr float kUnbias = 0.0040596f;           // log2(1.0028179)
-constexpr float kUnbiasScale = 0.9971900f;      // 1 / 1.0028179
 
 template <int DP> struct Fwd {
   static constexpr int kChunks = DP / 64;
@@ -364,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
             lo = tc::exp2_fast(lo);
             hi = tc::exp2_fast(hi);
             sum[i & 1] = tc::add2(sum[i & 1], tc::pack2(lo, hi));
-            to[i] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+            to[i] = cut_bf16x2(lo, hi);
           }
         };
         auto release = [&](int part) {
