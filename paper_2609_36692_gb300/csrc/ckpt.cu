@@ -21,17 +21,50 @@ namespace {
 constexpr int kRows = 64;        // rows of a CTA
 constexpr int kThreads = 256;
 
-// 16 consecutive elements; `n` of them exist.
-template <bool VEC, typename T>
-__device__ __forceinline__ void load16(const T* p, int n, float (&v)[16]) {
-  if (VEC && n >= 16) {
-    load8(p, v);
-    load8(p + 8, v + 8);
-  } else {
+// 16 consecutive elements as they lie in memory, `n` of which exist.  A thread
+// fetches all that it will work on before it converts any of it, so that its
+// reads are in flight together.
+template <bool VEC, typename T> struct Raw16 {
+  uint4 q[sizeof(T)];   // 16 elements: 16 sizeof(T) bytes
+  __device__ __forceinline__ void fetch(const T* p, int n) {
+    if (VEC && n >= 16) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
+      for (int i = 0; i < static_cast<int>(sizeof(T)); ++i) q[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    } else {
+      T v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = i < n ? p[i] : from_f32<T>(0.f);
+#pragma unroll
+      for (int i = 0; i < static_cast<int>(sizeof(T)); ++i) q[i] = pack(v + 16 / sizeof(T) * i);
+    }
   }
-}
+  __device__ __forceinline__ void values(float (&v)[16]) const {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T)); ++i) {
+      const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) {
+          v[4 * i + e] = __uint_as_float(w[e]);
+        } else {
+          v[8 * i + 2 * e] = bf16lo(w[e]);
+          v[8 * i + 2 * e + 1] = bf16hi(w[e]);
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float* v) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+  }
+  static __device__ __forceinline__ uint4 pack(const bf16* v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      w[e] = static_cast<uint32_t>(__bfloat16_as_ushort(v[2 * e])) |
+             (static_cast<uint32_t>(__bfloat16_as_ushort(v[2 * e + 1])) << 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
 template <bool VEC, typename T>
 __device__ __forceinline__ void store16(T* p, int n, const float (&v)[16]) {
   if (VEC && n >= 16) {
@@ -107,31 +140,56 @@ struct PackArgs {
   uint32_t* steps;
 };
 
+constexpr int kPasses = kRows / 32;
+
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_ckpt_pack(const __grid_constant__ PackArgs a) {
+  Place p[kPasses];
+  Raw16<VEC, T> x[kPasses];
 #pragma unroll
-  for (int pass = 0; pass < kRows / 32; ++pass) {
-    const Place p = place(a.tokens, a.features, a.ld, pass);
+  for (int i = 0; i < kPasses; ++i) {
+    p[i] = place(a.tokens, a.features, a.ld, i);
+    x[i].fetch(static_cast<const T*>(a.x) + p[i].row * a.x_ld + p[i].feature, p[i].n);
+  }
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
     float v[16];
-    load16<VEC>(static_cast<const T*>(a.x) + p.row * a.x_ld + p.feature, p.n, v);
+    x[i].values(v);
     uint4 codes;
     const uint32_t word = encode16(v, codes);
-    if (p.codes) *reinterpret_cast<uint4*>(a.codes + p.row * a.ld + p.feature) = codes;
-    if ((threadIdx.x & 7) == 0 && p.row < a.tokens) a.steps[p.word] = word;
+    if (p[i].codes) *reinterpret_cast<uint4*>(a.codes + p[i].row * a.ld + p[i].feature) = codes;
+    if ((threadIdx.x & 7) == 0 && p[i].row < a.tokens) a.steps[p[i].word] = word;
   }
 }
 
+// The codes and step of a lane's 16 elements.
+struct Coded {
+  uint4 codes;
+  uint32_t word;
+  __device__ __forceinline__ void fetch(const int8_t* codes_, const uint32_t* steps, int64_t ld, const Place& p) {
+    codes = make_uint4(0, 0, 0, 0);
+    word = 0;
+    if (!p.n) return;
+    codes = __ldcs(reinterpret_cast<const uint4*>(codes_ + p.row * ld + p.feature));
+    word = __ldg(steps + p.word);
+  }
+  __device__ __forceinline__ void values(float (&v)[16]) const { decode16(codes, ckpt_step(word, (threadIdx.x & 7) >> 1), v); }
+};
+
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_ckpt_restore(const __grid_constant__ PackArgs a, T* y) {
+  Place p[kPasses];
+  Coded c[kPasses];
 #pragma unroll
-  for (int pass = 0; pass < kRows / 32; ++pass) {
-    const Place p = place(a.tokens, a.features, a.ld, pass);
-    if (!p.n) continue;
-    const uint4 codes = __ldg(reinterpret_cast<const uint4*>(a.codes + p.row * a.ld + p.feature));
-    const uint32_t word = __ldg(a.steps + p.word);
+  for (int i = 0; i < kPasses; ++i) {
+    p[i] = place(a.tokens, a.features, a.ld, i);
+    c[i].fetch(a.codes, a.steps, a.ld, p[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
     float v[16];
-    decode16(codes, ckpt_step(word, (threadIdx.x & 7) >> 1), v);
-    store16<VEC>(y + p.row * a.x_ld + p.feature, p.n, v);
+    c[i].values(v);
+    if (p[i].n) store16<VEC>(y + p[i].row * a.x_ld + p[i].feature, p[i].n, v);
   }
 }
 
@@ -148,48 +206,61 @@ __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f +
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_ckpt_swiglu(const __grid_constant__ SwigluArgs a) {
+  Place p[kPasses];
+  Raw16<VEC, T> gr[kPasses], ur[kPasses];
 #pragma unroll
-  for (int pass = 0; pass < kRows / 32; ++pass) {
-    const Place p = place(a.tokens, a.features, a.ld, pass);
+  for (int i = 0; i < kPasses; ++i) {
+    p[i] = place(a.tokens, a.features, a.ld, i);
+    gr[i].fetch(static_cast<const T*>(a.gate) + p[i].row * a.gate_ld + p[i].feature, p[i].n);
+    ur[i].fetch(static_cast<const T*>(a.up) + p[i].row * a.up_ld + p[i].feature, p[i].n);
+  }
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
     float g[16], u[16];
-    load16<VEC>(static_cast<const T*>(a.gate) + p.row * a.gate_ld + p.feature, p.n, g);
-    load16<VEC>(static_cast<const T*>(a.up) + p.row * a.up_ld + p.feature, p.n, u);
+    gr[i].values(g);
+    ur[i].values(u);
     uint4 gc, uc;
     const uint32_t gw = encode16(g, gc), uw = encode16(u, uc);
-    if (p.codes) {
-      *reinterpret_cast<uint4*>(a.gate_codes + p.row * a.ld + p.feature) = gc;
-      *reinterpret_cast<uint4*>(a.up_codes + p.row * a.ld + p.feature) = uc;
+    if (p[i].codes) {
+      *reinterpret_cast<uint4*>(a.gate_codes + p[i].row * a.ld + p[i].feature) = gc;
+      *reinterpret_cast<uint4*>(a.up_codes + p[i].row * a.ld + p[i].feature) = uc;
     }
-    if ((threadIdx.x & 7) == 0 && p.row < a.tokens) {
-      a.gate_steps[p.word] = gw;
-      a.up_steps[p.word] = uw;
+    if ((threadIdx.x & 7) == 0 && p[i].row < a.tokens) {
+      a.gate_steps[p[i].word] = gw;
+      a.up_steps[p[i].word] = uw;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) u[i] *= g[i] * sigmoid(g[i]);
-    store16<VEC>(static_cast<T*>(a.h) + p.row * a.h_ld + p.feature, p.n, u);
+    for (int e = 0; e < 16; ++e) u[e] *= g[e] * sigmoid(g[e]);
+    store16<VEC>(static_cast<T*>(a.h) + p[i].row * a.h_ld + p[i].feature, p[i].n, u);
   }
 }
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_ckpt_swiglu_bwd(const __grid_constant__ SwigluArgs a) {
+  Place p[kPasses];
+  Raw16<VEC, T> dr[kPasses];
+  Coded gr[kPasses], ur[kPasses];
 #pragma unroll
-  for (int pass = 0; pass < kRows / 32; ++pass) {
-    const Place p = place(a.tokens, a.features, a.ld, pass);
-    if (!p.n) continue;
-    const int block = (threadIdx.x & 7) >> 1;
-    const int64_t at = p.row * a.ld + p.feature;
+  for (int i = 0; i < kPasses; ++i) {
+    p[i] = place(a.tokens, a.features, a.ld, i);
+    dr[i].fetch(static_cast<const T*>(a.dh) + p[i].row * a.dh_ld + p[i].feature, p[i].n);
+    gr[i].fetch(a.gate_codes, a.gate_steps, a.ld, p[i]);
+    ur[i].fetch(a.up_codes, a.up_steps, a.ld, p[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
     float g[16], u[16], d[16];
-    load16<VEC>(static_cast<const T*>(a.dh) + p.row * a.dh_ld + p.feature, p.n, d);
-    decode16(__ldg(reinterpret_cast<const uint4*>(a.gate_codes + at)), ckpt_step(__ldg(a.gate_steps + p.word), block), g);
-    decode16(__ldg(reinterpret_cast<const uint4*>(a.up_codes + at)), ckpt_step(__ldg(a.up_steps + p.word), block), u);
+    dr[i].values(d);
+    gr[i].values(g);
+    ur[i].values(u);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float s = sigmoid(g[i]);
-      u[i] *= d[i] * s * fmaf(g[i], 1.f - s, 1.f);
-      g[i] *= d[i] * s;
+    for (int e = 0; e < 16; ++e) {
+      const float s = sigmoid(g[e]);
+      u[e] *= d[e] * s * fmaf(g[e], 1.f - s, 1.f);
+      g[e] *= d[e] * s;
     }
-    store16<VEC>(static_cast<T*>(a.dgate) + p.row * a.dgate_ld + p.feature, p.n, u);
-    store16<VEC>(static_cast<T*>(a.dup) + p.row * a.dup_ld + p.feature, p.n, g);
+    store16<VEC>(static_cast<T*>(a.dgate) + p[i].row * a.dgate_ld + p[i].feature, p[i].n, u);
+    store16<VEC>(static_cast<T*>(a.dup) + p[i].row * a.dup_ld + p[i].feature, p[i].n, g);
   }
 }
 
