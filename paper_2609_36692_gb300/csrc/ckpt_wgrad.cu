@@ -79,27 +79,31 @@ __global__ void __launch_bounds__(256) k_wgrad_simt(const __grid_constant__ Wgra
     }
 }
 
-constexpr int kTileK = 128, kTileN = 256, kStep = 64;   // features, outputs, tokens of a step
-constexpr int kRing = 4, kXbuf = 3;
+constexpr int kTileK = 128, kTileN = 256, kStep = 64;   // features, outputs (at most), tokens of a step
+// dY and the codes have rings of their own: codes are given back as soon as
+// they are converted, so that conversion runs ahead and only dY's load latency
+// stands between the rings and the tensor cores.
+constexpr int kRing = 4;
 constexpr int kBox = 64 * 128;                           // bytes of 64 rows of 64 bf16
 constexpr int kDyBytes = 4 * kBox, kCodeBytes = kStep * kTileK, kXBytes = 2 * kBox;
-constexpr int kStageBytes = kDyBytes + kCodeBytes;
 constexpr int kConvert = 8, kGroups = 2;                 // converting warps of a step; groups that take turns
-constexpr int kTma = 4 + kGroups * kConvert, kMma = kTma + 1, kSteps = kTma + 2;   // warps: drain, convert, these
-constexpr int kTcThreads = 32 * (kSteps + 1);
-constexpr size_t kTcSmem = kRing * kStageBytes + kXbuf * kXBytes + kRing * kStep * 4 + 512;
+constexpr int kTma = 4 + kGroups * kConvert, kMma = kTma + 1, kCodes = kTma + 2;   // warps: drain, convert, these
+constexpr int kTcThreads = 32 * (kCodes + 1);
+constexpr size_t kTcSmem = kRing * (kDyBytes + kXBytes + kCodeBytes + kStep * 4) + 512;
 
 struct WgradTcArgs {
   WgradArgs a;
   CUtensorMap dy, codes;
   int tiles_k, tiles_n, units;   // units: tiles, or pairs of feature tiles
+  int tile_n;                    // outputs of a tile
 };
 
 struct WgradBars {
-  uint64_t full[kRing], empty[kRing], xfull[kXbuf], xempty[kXbuf], tfull[2], tempty[2], drain;
+  // of dY, the codes and their steps, the converted tiles, the accumulators
+  uint64_t full[kRing], empty[kRing], cfull[kRing], cempty[kRing], xfull[kRing], xempty[kRing], tfull[2], tempty[2], drain;
   uint32_t tmem;
   int abort;
-  uint32_t issued[kRing];   // last parity + 1 of full
+  uint32_t issued[kRing], cissued[kRing];   // last parity + 1 of full and cfull
 };
 
 // 4 bytes from global to shared memory (zero if !in), and the arrival of the
@@ -137,9 +141,10 @@ __device__ __forceinline__ void convert4(uint32_t w, uint64_t step2, uint64_t of
 template <typename TW, bool SPLIT>
 __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constant__ WgradTcArgs f) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t* ring = smem;                                   // [kRing] dY boxes, codes
-  uint8_t* xbuf = ring + kRing * kStageBytes;             // [kXbuf]
-  uint32_t* steps = reinterpret_cast<uint32_t*>(xbuf + kXbuf * kXBytes);   // [kRing][kStep]
+  uint8_t* ring = smem;                                   // [kRing] dY boxes
+  uint8_t* xbuf = ring + kRing * kDyBytes;                // [kRing] the codes as bf16
+  uint8_t* codes = xbuf + kRing * kXBytes;                // [kRing]
+  uint32_t* steps = reinterpret_cast<uint32_t*>(codes + kRing * kCodeBytes);   // [kRing][kStep]
   WgradBars* b = reinterpret_cast<WgradBars*>(steps + kRing * kStep);
   static_assert(sizeof(WgradBars) <= 512, "barriers");
   const WgradArgs& a = f.a;
@@ -154,13 +159,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kRing; ++i) {
-      tc::mbar_init(&b->full[i], 1 + 32);
+      tc::mbar_init(&b->full[i], 1);
       tc::mbar_init(&b->empty[i], SPLIT ? 1 : 2);
-      b->issued[i] = 0;
-    }
-    for (int i = 0; i < kXbuf; ++i) {
+      tc::mbar_init(&b->cfull[i], 1 + 32);
+      tc::mbar_init(&b->cempty[i], kConvert);
       tc::mbar_init(&b->xfull[i], kConvert);
       tc::mbar_init(&b->xempty[i], 1);
+      b->issued[i] = b->cissued[i] = 0;
     }
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(&b->tfull[i], 1);
@@ -187,76 +192,78 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, &b->abort));
     return ok;
   };
-  // feature tile and output tile of a unit
+  auto wait1 = [&](uint64_t* bar, uint32_t parity) { return ok = ok && tc::mbar_wait(bar, parity, &b->abort); };
+  // feature tile and first output of a unit
   auto tile_k = [&](int u) { return SPLIT ? u % f.tiles_k : 2 * (u % ((f.tiles_k + 1) / 2)) + static_cast<int>(rank); };
-  auto tile_n = [&](int u) { return SPLIT ? u / f.tiles_k : u / ((f.tiles_k + 1) / 2); };
+  auto first_n = [&](int u) { return (SPLIT ? u / f.tiles_k : u / ((f.tiles_k + 1) / 2)) * f.tile_n; };
+  int st = 0;            // place in the rings, and the parity of its uses
+  uint32_t phase = 0;
+  auto next = [&]() {
+    if (++st == kRing) { st = 0; phase ^= 1u; }
+  };
 
   if (warp == kTma) {
-    // ---------------- TMA (one thread) ----------------
+    // ---------------- dY by TMA (one thread) ----------------
     if (tc::elect_one()) {
-      int st = 0;
-      uint32_t phase = 0;
       for (int u = unit0; u < f.units && ok; u += nunits) {
-        const int k0 = tile_k(u) * kTileK, n0 = tile_n(u) * kTileN;
-        for (int s = s0; s < s1; ++s) {
-          if (!(ok = tc::mbar_wait(&b->empty[st], phase ^ 1u, &b->abort))) break;
-          uint8_t* dst = ring + st * kStageBytes;
-          tc::mbar_expect_tx(&b->full[st], kStageBytes);
+        const int n0 = first_n(u);
+        for (int s = s0; s < s1; ++s, next()) {
+          if (!wait1(&b->empty[st], phase ^ 1u)) break;
+          uint8_t* dst = ring + st * kDyBytes;
+          tc::mbar_expect_tx(&b->full[st], kDyBytes);
           b->issued[st] = phase + 1;
-          tc::tma_load_3d(dst + kDyBytes, &f.codes, &b->full[st], k0, s * kStep, 0);
           if (SPLIT) {
             for (int i = 0; i < 4; ++i) tc::tma_load_3d(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, s * kStep, 0);
           } else {
             for (int i = 2 * rank; i < 2 * static_cast<int>(rank) + 2; ++i)
               tc::tma_load_3d_mc(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, s * kStep, 0, 3);
           }
-          if (++st == kRing) { st = 0; phase ^= 1u; }
         }
       }
     }
     __syncwarp();
     ok = __all_sync(0xffffffffu, ok);
-  } else if (warp == kSteps) {
-    // ---------------- step words, by plain asynchronous copies ----------------
-    int st = 0;
-    uint32_t phase = 0;
+  } else if (warp == kCodes) {
+    // ---------------- codes by TMA, step words by plain asynchronous copies ----------------
     for (int u = unit0; u < f.units && ok; u += nunits) {
       const int tk = tile_k(u);
       const uint32_t* words = a.x.steps + static_cast<int64_t>(tk) * a.tokens;
-      for (int s = s0; s < s1; ++s) {
-        if (!wait(&b->empty[st], phase ^ 1u)) break;
+      for (int s = s0; s < s1; ++s, next()) {
+        if (!wait(&b->cempty[st], phase ^ 1u)) break;
+        if (lane == 0) {
+          tc::mbar_expect_tx(&b->cfull[st], kCodeBytes);
+          b->cissued[st] = phase + 1;
+          tc::tma_load_3d(codes + st * kCodeBytes, &f.codes, &b->cfull[st], tk * kTileK, s * kStep, 0);
+        }
+        __syncwarp();
 #pragma unroll
         for (int i = lane; i < kStep; i += 32) {
           const int64_t t = static_cast<int64_t>(s) * kStep + i;
           const bool in = tk < f.tiles_k && t < a.tokens;
           copy4_async(steps + st * kStep + i, in ? words + t : a.x.steps, in);
         }
-        copies_arrive(&b->full[st]);
-        if (++st == kRing) { st = 0; phase ^= 1u; }
+        copies_arrive(&b->cfull[st]);
       }
     }
   } else if (warp == kMma) {
     // ---------------- MMA (one thread) ----------------
     if (tc::elect_one()) {
-      constexpr uint32_t idesc = tc::idesc_bf16(kTileK, kTileN, 1, 1);
-      int st = 0, xb = 0, acc = 0, never = 0;
-      uint32_t phase = 0, xphase = 0, tphase = 0;
-      auto wait1 = [&](uint64_t* bar, uint32_t parity) { return ok = ok && tc::mbar_wait(bar, parity, &b->abort); };
+      const uint32_t idesc = tc::idesc_bf16(kTileK, f.tile_n, 1, 1);
+      int acc = 0, never = 0;
+      uint32_t tphase = 0;
       for (int u = unit0; u < f.units && ok; u += nunits) {
         if (!wait1(&b->tempty[acc], tphase ^ 1u)) break;
-        for (int s = s0; s < s1; ++s) {
-          if (!wait1(&b->full[st], phase) || !wait1(&b->xfull[xb], xphase)) break;
+        for (int s = s0; s < s1; ++s, next()) {
+          if (!wait1(&b->full[st], phase) || !wait1(&b->xfull[st], phase)) break;
           tc::fence_after();
-          const uint64_t dy = tc::sdesc(tc::su32(ring + st * kStageBytes), kBox, 1024);
-          const uint64_t x = tc::sdesc(tc::su32(xbuf + xb * kXBytes), kBox, 1024);
+          const uint64_t dy = tc::sdesc(tc::su32(ring + st * kDyBytes), kBox, 1024);
+          const uint64_t x = tc::sdesc(tc::su32(xbuf + st * kXBytes), kBox, 1024);
 #pragma unroll
           for (int kk = 0; kk < kStep / 16; ++kk)
             tc::mma_bf16(tmem + 256 * acc, x + kk * (2048 >> 4), dy + kk * (2048 >> 4), idesc, s != s0 || kk != 0);
           if (SPLIT) tc::mma_commit(&b->empty[st]);
           else tc::mma_commit_mc(&b->empty[st], 3);
-          tc::mma_commit(&b->xempty[xb]);
-          if (++st == kRing) { st = 0; phase ^= 1u; }
-          if (++xb == kXbuf) { xb = 0; xphase ^= 1u; }
+          tc::mma_commit(&b->xempty[st]);
         }
         if (!ok) break;
         tc::mma_commit(&b->tfull[acc]);
@@ -276,58 +283,57 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     // pieces the swizzle spreads over all banks.
     const int group = (warp - 4) / kConvert;
     const int row = 8 * ((warp - 4) % kConvert) + (lane & 7), blk = lane >> 3, sw = row & 7;
-    int st = 0, xb = 0, turn = 0;
-    uint32_t phase = 0, xphase = 0;
+    int turn = 0;
     for (int u = unit0; u < f.units && ok; u += nunits)
-      for (int s = s0; s < s1; ++s) {
-        if (turn == group) {
-          if (!wait(&b->full[st], phase)) break;
-          const uint8_t* src = ring + st * kStageBytes + kDyBytes + row * kTileK;
-          uint4 c[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) c[i] = *reinterpret_cast<const uint4*>(src + (((2 * blk + i) ^ sw) << 4));
-          const float step = ckpt_step(steps[st * kStep + row], blk);
-          const float off = -8388736.f * step;             // -(2^23 + 128) step
-          const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
-          if (!wait(&b->xempty[xb], xphase ^ 1u)) break;
-          uint8_t* dst = xbuf + xb * kXBytes + (blk >> 1) * kBox + row * 128;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint4 v;
-              convert4(w[2 * h], step2, off2, v.x, v.y);
-              convert4(w[2 * h + 1], step2, off2, v.z, v.w);
-              *reinterpret_cast<uint4*>(dst + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
-            }
-          }
-          tc::fence_smem_async();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&b->xfull[xb]);
-        }
+      for (int s = s0; s < s1; ++s, next()) {
+        const bool mine = turn == group;
         if (++turn == kGroups) turn = 0;
-        if (++st == kRing) { st = 0; phase ^= 1u; }
-        if (++xb == kXbuf) { xb = 0; xphase ^= 1u; }
+        if (!mine) continue;
+        if (!wait(&b->cfull[st], phase)) break;
+        const uint8_t* src = codes + st * kCodeBytes + row * kTileK;
+        uint4 c[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) c[i] = *reinterpret_cast<const uint4*>(src + (((2 * blk + i) ^ sw) << 4));
+        const float step = ckpt_step(steps[st * kStep + row], blk);
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&b->cempty[st]);
+        const float off = -8388736.f * step;             // -(2^23 + 128) step
+        const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
+        if (!wait(&b->xempty[st], phase ^ 1u)) break;
+        uint8_t* dst = xbuf + st * kXBytes + (blk >> 1) * kBox + row * 128;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint4 v;
+            convert4(w[2 * h], step2, off2, v.x, v.y);
+            convert4(w[2 * h + 1], step2, off2, v.z, v.w);
+            *reinterpret_cast<uint4*>(dst + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
+          }
+        }
+        tc::fence_smem_async();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&b->xfull[st]);
       }
   } else if (!SPLIT) {
-    // ---------------- drain: warp's 32 features x 256 outputs ----------------
+    // ---------------- drain: warp's 32 features x a tile's outputs ----------------
     int acc = 0;
     uint32_t tphase = 0;
     for (int u = unit0; u < f.units && ok; u += nunits) {
       if (!wait(&b->tfull[acc], tphase)) break;
       tc::fence_after();
-      const int k = tile_k(u) * kTileK + 32 * warp + lane, n0 = tile_n(u) * kTileN;
+      const int k = tile_k(u) * kTileK + 32 * warp + lane, n0 = first_n(u), n1 = min(f.tile_n, a.n - n0);
       TW* dw = static_cast<TW*>(a.dw) + static_cast<int64_t>(n0) * a.dw_ld + k;
 #pragma unroll 1
-      for (int c = 0; c < kTileN && n0 + c < a.n; c += 32) {
+      for (int c = 0; c < n1; c += 32) {
         uint32_t r[32];
         tc::tmem_ld32(tmem + 256 * acc + c + (static_cast<uint32_t>(32 * warp) << 16), r);
         tc::tmem_ld_wait();
         if (k < a.k) {
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (n0 + c + e < a.n) {
+            if (c + e < n1) {
               TW* p = dw + (c + e) * a.dw_ld;
               const float v = __uint_as_float(r[e]);
               *p = from_f32<TW>(a.accumulate ? to_f32(*p) + v : v);
@@ -360,7 +366,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     }
     __syncthreads();
     tc::cluster_sync();
-    const int k0 = tile_k(unit0) * kTileK, n0 = tile_n(unit0) * kTileN, rows = (kTileN + csize - 1) / csize;
+    const int k0 = tile_k(unit0) * kTileK, n0 = first_n(unit0), rows = (kTileN + csize - 1) / csize;
     for (int i = threadIdx.x; i < rows * (kTileK / 4); i += kTcThreads) {
       const int n = rank * rows + i / (kTileK / 4), k = 4 * (i % (kTileK / 4));
       if (n >= kTileN || n0 + n >= a.n || k0 + k >= a.k) continue;
@@ -384,8 +390,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   if (threadIdx.x == 0 && *static_cast<volatile int*>(&b->abort)) {
     // let every TMA copy still in flight land before the CTA exits
     volatile int never = 0;
-    for (int i = 0; i < kRing; ++i)
+    for (int i = 0; i < kRing; ++i) {
       if (b->issued[i]) tc::mbar_wait(&b->full[i], b->issued[i] - 1, &never);
+      if (b->cissued[i]) tc::mbar_wait(&b->cfull[i], b->cissued[i] - 1, &never);
+    }
   }
   __syncthreads();
   // no CTA exits while the other may still multicast into it, arrive on its
@@ -429,10 +437,13 @@ cudaError_t clusters_at_once(int cluster, int* fit) {
 
 template <typename TW>
 cudaError_t launch_tc(WgradTcArgs f, cudaStream_t s) {
+  f.tiles_k = static_cast<int>(cdiv(f.a.k, kTileK));
+  f.tile_n = kTileN;
+  f.tiles_n = static_cast<int>(cdiv(f.a.n, kTileN));
   const int64_t tiles = static_cast<int64_t>(f.tiles_k) * f.tiles_n, steps = cdiv(f.a.tokens, kStep);
   // The largest split of the tokens whose clusters all run at once, each CTA
-  // with at least two steps: half the tokens a CTA and twice the CTAs halve the
-  // time until the join (about four steps) weighs in.
+  // with at least two steps: twice the CTAs halve the time until the join
+  // (about four steps) weighs in.
   int split = tiles == 1 ? 1 : 0, fit = 0;
   for (int c = 2; c <= 8 && steps >= 2 * c && tiles * c <= device_sm_count(); ++c) {
     const cudaError_t e = clusters_at_once<TW, true>(c, &fit);
@@ -446,9 +457,18 @@ cudaError_t launch_tc(WgradTcArgs f, cudaStream_t s) {
     ClusterLaunch l(split, f.units, s);
     return cudaLaunchKernelEx(&l.cfg, k_wgrad_tc<TW, true>, f);
   }
-  f.units = (f.tiles_k + 1) / 2 * f.tiles_n;
   const cudaError_t e = clusters_at_once<TW, false>(2, &fit);
   if (e) return e;
+  // The tile width whose rounds over the clusters take least: 2 cycles an
+  // output and step, about 100 a step beside them.
+  int64_t least = -1;
+  for (int tn = kTileN; tn >= 192; tn -= 16) {
+    const int64_t units = (f.tiles_k + 1) / 2 * cdiv(f.a.n, tn), cost = cdiv(units, fit) * (2 * tn + 100);
+    if (least >= 0 && cost >= least) continue;
+    least = cost;
+    f.tile_n = tn;
+    f.units = static_cast<int>(units);
+  }
   ClusterLaunch l(2, std::min(f.units, fit), s);
   return cudaLaunchKernelEx(&l.cfg, k_wgrad_tc<TW, false>, f);
 }
@@ -470,8 +490,6 @@ cudaError_t launch_ckpt_wgrad_tc(const WgradArgs& a, int dw_dtype, cudaStream_t 
       !driver_encode_tiled(&f.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<int8_t*>(a.x.codes), c_dims,
                            c_strides, c_box, err))
     return cudaErrorInvalidValue;
-  f.tiles_k = static_cast<int>(cdiv(a.k, kTileK));
-  f.tiles_n = static_cast<int>(cdiv(a.n, kTileN));
   return dw_dtype == 0 ? launch_tc<float>(f, s) : launch_tc<bf16>(f, s);
 }
 
