@@ -8,7 +8,7 @@
 // summed 64 tokens at a time: TMA brings the codes and the dY boxes into a
 // ring, sixteen warps turn codes into swizzled bf16 tiles (a byte becomes an
 // fp32 by permutation into 2^23 + byte, one packed FMA takes off the offset
-// and scales, one conversion packs two), one thread issues the MMAs, and four
+// and scales, a permutation packs two), one thread issues the MMAs, and four
 // warps drain a finished accumulator (two in TMEM) while the next tile runs.
 // Both operands are read along their rows (MN-major), as they lie in memory:
 // nothing is transposed.  The 128 side is the converted one: it costs about
@@ -86,7 +86,7 @@ constexpr int kTileK = 128, kTileN = 256, kStep = 64;   // features, outputs (at
 constexpr int kRing = 4;
 constexpr int kBox = 64 * 128;                           // bytes of 64 rows of 64 bf16
 constexpr int kDyBytes = 4 * kBox, kCodeBytes = kStep * kTileK, kXBytes = 2 * kBox;
-constexpr int kConvert = 8, kGroups = 2;                 // converting warps of a step; groups that take turns
+constexpr int kConvert = 4, kGroups = 4;                 // converting warps of a step; groups that take turns
 constexpr int kTma = 4 + kGroups * kConvert, kMma = kTma + 1, kCodes = kTma + 2;   // warps: drain, convert, these
 constexpr int kTcThreads = 32 * (kCodes + 1);
 constexpr size_t kTcSmem = kRing * (kDyBytes + kXBytes + kCodeBytes + kStep * 4) + 512;
@@ -130,10 +130,11 @@ __device__ __forceinline__ void convert4(uint32_t w, uint64_t step2, uint64_t of
 #pragma unroll
   for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 + i));   // 2^23 + code + 128
   float lo, hi;
+  // the values are bf16 numbers: their upper halves are all of them
   tc::unpack2(tc::fma2(tc::pack2(f[0], f[1]), step2, off2), lo, hi);
-  p0 = pack_bf16x2(lo, hi);
+  p0 = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
   tc::unpack2(tc::fma2(tc::pack2(f[2], f[3]), step2, off2), lo, hi);
-  p1 = pack_bf16x2(lo, hi);
+  p1 = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
 }
 
 // SPLIT: the cluster's CTAs share a tile and split its tokens; otherwise a
@@ -278,11 +279,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     ok = __all_sync(0xffffffffu, ok);
   } else if (warp >= 4) {
     // ---------------- codes -> bf16 ----------------
-    // The groups take the steps in turn, so that a group's waits have another
-    // step's time.  8 rows x 4 blocks per warp: lanes of 8 rows, whose 16-byte
-    // pieces the swizzle spreads over all banks.
+    // The groups take the steps in turn: a group's waits, which outweigh its
+    // work, then have other steps' time.  8 rows x 4 blocks per warp at a time:
+    // lanes of 8 rows, whose 16-byte pieces the swizzle spreads over all banks.
     const int group = (warp - 4) / kConvert;
-    const int row = 8 * ((warp - 4) % kConvert) + (lane & 7), blk = lane >> 3, sw = row & 7;
+    const int row0 = 8 * ((warp - 4) % kConvert) + (lane & 7), blk = lane >> 3, sw = row0 & 7;
     int turn = 0;
     for (int u = unit0; u < f.units && ok; u += nunits)
       for (int s = s0; s < s1; ++s, next()) {
@@ -290,26 +291,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
         if (++turn == kGroups) turn = 0;
         if (!mine) continue;
         if (!wait(&b->cfull[st], phase)) break;
-        const uint8_t* src = codes + st * kCodeBytes + row * kTileK;
-        uint4 c[2];
+        uint4 c[kStep / (8 * kConvert)][2];
+        uint32_t word[kStep / (8 * kConvert)];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) c[i] = *reinterpret_cast<const uint4*>(src + (((2 * blk + i) ^ sw) << 4));
-        const float step = ckpt_step(steps[st * kStep + row], blk);
+        for (int r = 0; r < kStep / (8 * kConvert); ++r) {
+          const int row = row0 + 8 * kConvert * r;
+          const uint8_t* src = codes + st * kCodeBytes + row * kTileK;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) c[r][i] = *reinterpret_cast<const uint4*>(src + (((2 * blk + i) ^ sw) << 4));
+          word[r] = steps[st * kStep + row];
+        }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&b->cempty[st]);
-        const float off = -8388736.f * step;             // -(2^23 + 128) step
-        const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
         if (!wait(&b->xempty[st], phase ^ 1u)) break;
-        uint8_t* dst = xbuf + st * kXBytes + (blk >> 1) * kBox + row * 128;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+        for (int r = 0; r < kStep / (8 * kConvert); ++r) {
+          const float step = ckpt_step(word[r], blk), off = -8388736.f * step;   // -(2^23 + 128) step
+          const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
+          uint8_t* dst = xbuf + st * kXBytes + (blk >> 1) * kBox + (row0 + 8 * kConvert * r) * 128;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint4 v;
-            convert4(w[2 * h], step2, off2, v.x, v.y);
-            convert4(w[2 * h + 1], step2, off2, v.z, v.w);
-            *reinterpret_cast<uint4*>(dst + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t w[4] = {c[r][i].x, c[r][i].y, c[r][i].z, c[r][i].w};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint4 v;
+              convert4(w[2 * h], step2, off2, v.x, v.y);
+              convert4(w[2 * h + 1], step2, off2, v.z, v.w);
+              *reinterpret_cast<uint4*>(dst + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
+            }
           }
         }
         tc::fence_smem_async();
