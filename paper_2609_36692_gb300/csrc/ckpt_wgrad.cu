@@ -16,6 +16,11 @@
 //   Two CTAs of a cluster take two neighbouring feature tiles of the same
 // outputs and each multicasts half of their dY boxes to both (24 KB instead of
 // 40 KB of L2 reads a step).
+//   What bounds it: 40 KB a step enter an SM, multicast or not, at 60 of the 64
+// bytes a cycle of its L2 port: 660 cycles a step against the MMAs' 512.  256 x
+// 192 tiles take in fewer bytes an MMA, but their conversion (4 cycles an
+// element and SM sub-partition, byte permutations at half rate) then takes
+// 1000 cycles of the MMAs' 768.  16384 x 6144 x 2048: 0.305 ms, 1350 TFLOP/s.
 //   With too few tiles for the SMs, clusters of 2, 4 or 8 CTAs split a tile's
 // tokens instead and join through distributed shared memory: each CTA lays its
 // accumulator out in its (then idle) ring and sums one slice of the outputs
@@ -89,7 +94,7 @@ constexpr int kDyBytes = 4 * kBox, kCodeBytes = kStep * kTileK, kXBytes = 2 * kB
 constexpr int kConvert = 4, kGroups = 4;                 // converting warps of a step; groups that take turns
 constexpr int kTma = 4 + kGroups * kConvert, kMma = kTma + 1, kCodes = kTma + 2;   // warps: drain, convert, these
 constexpr int kTcThreads = 32 * (kCodes + 1);
-constexpr size_t kTcSmem = kRing * (kDyBytes + kXBytes + kCodeBytes + kStep * 4) + 512;
+constexpr size_t kTcSmem = kRing * (kDyBytes + kXBytes + kCodeBytes) + 512;
 
 struct WgradTcArgs {
   WgradArgs a;
@@ -99,21 +104,13 @@ struct WgradTcArgs {
 };
 
 struct WgradBars {
-  // of dY, the codes and their steps, the converted tiles, the accumulators
+  // of dY, the codes, the converted tiles, the accumulators
   uint64_t full[kRing], empty[kRing], cfull[kRing], cempty[kRing], xfull[kRing], xempty[kRing], tfull[2], tempty[2], drain;
   uint32_t tmem;
   int abort;
   uint32_t issued[kRing], cissued[kRing];   // last parity + 1 of full and cfull
 };
 
-// 4 bytes from global to shared memory (zero if !in), and the arrival of the
-// thread's copies so far on a barrier.
-__device__ __forceinline__ void copy4_async(uint32_t* dst, const uint32_t* src, bool in) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(tc::su32(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(tc::su32(bar)) : "memory");
-}
 // A float of another CTA's shared memory in the cluster.
 __device__ __forceinline__ float4 remote_float4(uint32_t addr, uint32_t rank) {
   uint32_t r;
@@ -145,8 +142,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   uint8_t* ring = smem;                                   // [kRing] dY boxes
   uint8_t* xbuf = ring + kRing * kDyBytes;                // [kRing] the codes as bf16
   uint8_t* codes = xbuf + kRing * kXBytes;                // [kRing]
-  uint32_t* steps = reinterpret_cast<uint32_t*>(codes + kRing * kCodeBytes);   // [kRing][kStep]
-  WgradBars* b = reinterpret_cast<WgradBars*>(steps + kRing * kStep);
+  WgradBars* b = reinterpret_cast<WgradBars*>(codes + kRing * kCodeBytes);
   static_assert(sizeof(WgradBars) <= 512, "barriers");
   const WgradArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -162,7 +158,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     for (int i = 0; i < kRing; ++i) {
       tc::mbar_init(&b->full[i], 1);
       tc::mbar_init(&b->empty[i], SPLIT ? 1 : 2);
-      tc::mbar_init(&b->cfull[i], 1 + 32);
+      tc::mbar_init(&b->cfull[i], 1);
       tc::mbar_init(&b->cempty[i], kConvert);
       tc::mbar_init(&b->xfull[i], kConvert);
       tc::mbar_init(&b->xempty[i], 1);
@@ -225,27 +221,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     __syncwarp();
     ok = __all_sync(0xffffffffu, ok);
   } else if (warp == kCodes) {
-    // ---------------- codes by TMA, step words by plain asynchronous copies ----------------
-    for (int u = unit0; u < f.units && ok; u += nunits) {
-      const int tk = tile_k(u);
-      const uint32_t* words = a.x.steps + static_cast<int64_t>(tk) * a.tokens;
-      for (int s = s0; s < s1; ++s, next()) {
-        if (!wait(&b->cempty[st], phase ^ 1u)) break;
-        if (lane == 0) {
+    // ---------------- codes by TMA (one thread) ----------------
+    if (tc::elect_one()) {
+      for (int u = unit0; u < f.units && ok; u += nunits) {
+        const int k0 = tile_k(u) * kTileK;
+        for (int s = s0; s < s1; ++s, next()) {
+          if (!wait1(&b->cempty[st], phase ^ 1u)) break;
           tc::mbar_expect_tx(&b->cfull[st], kCodeBytes);
           b->cissued[st] = phase + 1;
-          tc::tma_load_3d(codes + st * kCodeBytes, &f.codes, &b->cfull[st], tk * kTileK, s * kStep, 0);
+          tc::tma_load_3d(codes + st * kCodeBytes, &f.codes, &b->cfull[st], k0, s * kStep, 0);
         }
-        __syncwarp();
-#pragma unroll
-        for (int i = lane; i < kStep; i += 32) {
-          const int64_t t = static_cast<int64_t>(s) * kStep + i;
-          const bool in = tk < f.tiles_k && t < a.tokens;
-          copy4_async(steps + st * kStep + i, in ? words + t : a.x.steps, in);
-        }
-        copies_arrive(&b->cfull[st]);
       }
     }
+    __syncwarp();
+    ok = __all_sync(0xffffffffu, ok);
   } else if (warp == kMma) {
     // ---------------- MMA (one thread) ----------------
     if (tc::elect_one()) {
@@ -280,51 +269,82 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   } else if (warp >= 4) {
     // ---------------- codes -> bf16 ----------------
     // The groups take the steps in turn: a group's waits, which outweigh its
-    // work, then have other steps' time.  8 rows x 4 blocks per warp at a time:
-    // lanes of 8 rows, whose 16-byte pieces the swizzle spreads over all banks.
+    // work, then have other steps' time.  A group always works in the same
+    // place of the rings, where it waits for its own last step, never two uses
+    // ahead (a barrier's parity would lie there).  8 rows x 4 blocks per warp at
+    // a time: lanes of 8 rows, whose 16-byte pieces the swizzle spreads over all
+    // banks.
+    static_assert(kGroups == kRing, "a group's place in the rings");
+    constexpr int kPer = kStep / (8 * kConvert);   // rows of a lane
     const int group = (warp - 4) / kConvert;
-    const int row0 = 8 * ((warp - 4) % kConvert) + (lane & 7), blk = lane >> 3, sw = row0 & 7;
-    int turn = 0;
-    for (int u = unit0; u < f.units && ok; u += nunits)
-      for (int s = s0; s < s1; ++s, next()) {
-        const bool mine = turn == group;
-        if (++turn == kGroups) turn = 0;
-        if (!mine) continue;
-        if (!wait(&b->cfull[st], phase)) break;
-        uint4 c[kStep / (8 * kConvert)][2];
-        uint32_t word[kStep / (8 * kConvert)];
+    const int row = 8 * ((warp - 4) % kConvert) + (lane & 7), blk = lane >> 3, sw = row & 7;
+    const uint8_t* src = codes + group * kCodeBytes + row * kTileK;
+    uint8_t* dst = xbuf + group * kXBytes + (blk >> 1) * kBox + row * 128;
+    // The rows' step words come from global memory, a group's turn ahead.
+    uint32_t word[kPer], ahead[kPer];
+    const uint32_t* words = nullptr;       // of the unit's panel, if it has one
+    int s = s0 + group, u = unit0;         // the group's next step
+    uint32_t parity = 0;
+    auto enter = [&]() {
+      const int tk = tile_k(u);
+      words = u < f.units && tk < f.tiles_k ? a.x.steps + static_cast<int64_t>(tk) * a.tokens : nullptr;
+    };
+    auto settle = [&]() {                  // in this unit, or that far into one after it
+      while (s >= s1 && u < f.units) {
+        s -= s1 - s0;
+        u += nunits;
+        enter();
+      }
+    };
+    auto fetch = [&]() {
 #pragma unroll
-        for (int r = 0; r < kStep / (8 * kConvert); ++r) {
-          const int row = row0 + 8 * kConvert * r;
-          const uint8_t* src = codes + st * kCodeBytes + row * kTileK;
+      for (int r = 0; r < kPer; ++r) {
+        const int64_t t = static_cast<int64_t>(s) * kStep + row + 8 * kConvert * r;
+        ahead[r] = words && t < a.tokens ? __ldg(words + t) : 0u;
+      }
+    };
+    if (s0 >= s1) u = f.units;
+    if (u < f.units) {
+      enter();
+      settle();
+      fetch();
+    }
+    for (; u < f.units; parity ^= 1u) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) c[r][i] = *reinterpret_cast<const uint4*>(src + (((2 * blk + i) ^ sw) << 4));
-          word[r] = steps[st * kStep + row];
-        }
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&b->cempty[st]);
-        if (!wait(&b->xempty[st], phase ^ 1u)) break;
+      for (int r = 0; r < kPer; ++r) word[r] = ahead[r];
+      s += kGroups;
+      settle();
+      fetch();
+      if (!wait(&b->cfull[group], parity)) break;
+      uint4 c[kPer][2];
 #pragma unroll
-        for (int r = 0; r < kStep / (8 * kConvert); ++r) {
-          const float step = ckpt_step(word[r], blk), off = -8388736.f * step;   // -(2^23 + 128) step
-          const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
-          uint8_t* dst = xbuf + st * kXBytes + (blk >> 1) * kBox + (row0 + 8 * kConvert * r) * 128;
+      for (int r = 0; r < kPer; ++r)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t w[4] = {c[r][i].x, c[r][i].y, c[r][i].z, c[r][i].w};
+        for (int i = 0; i < 2; ++i)
+          c[r][i] = *reinterpret_cast<const uint4*>(src + 8 * kConvert * kTileK * r + (((2 * blk + i) ^ sw) << 4));
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&b->cempty[group]);
+      if (!wait(&b->xempty[group], parity ^ 1u)) break;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              uint4 v;
-              convert4(w[2 * h], step2, off2, v.x, v.y);
-              convert4(w[2 * h + 1], step2, off2, v.z, v.w);
-              *reinterpret_cast<uint4*>(dst + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
-            }
+      for (int r = 0; r < kPer; ++r) {
+        const float step = ckpt_step(word[r], blk), off = -8388736.f * step;   // -(2^23 + 128) step
+        const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t w[4] = {c[r][i].x, c[r][i].y, c[r][i].z, c[r][i].w};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint4 v;
+            convert4(w[2 * h], step2, off2, v.x, v.y);
+            convert4(w[2 * h + 1], step2, off2, v.z, v.w);
+            *reinterpret_cast<uint4*>(dst + 8 * kConvert * 128 * r + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
           }
         }
-        tc::fence_smem_async();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&b->xfull[st]);
       }
+      tc::fence_smem_async();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&b->xfull[group]);
+    }
   } else if (!SPLIT) {
     // ---------------- drain: warp's 32 features x a tile's outputs ----------------
     int acc = 0;
@@ -360,16 +380,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     // one unit per cluster; each CTA's partial tile goes to its ring as
     // [outputs][features], free once the accumulator is complete
     float* part = reinterpret_cast<float*>(ring);
-    if (warp < 4) {
+    if (warp >= 4 && warp < 4 + kGroups * kConvert) {   // idle by now: 4 warps a lane quarter, 64 outputs each
+      const int q = warp & 3, c0 = 64 * ((warp - 4) >> 2);
       if (s1 > s0 && wait(&b->tfull[0], 0)) {
         tc::fence_after();
 #pragma unroll 1
-        for (int c = 0; c < kTileN; c += 32) {
+        for (int c = c0; c < c0 + 64; c += 32) {
           uint32_t r[32];
-          tc::tmem_ld32(tmem + c + (static_cast<uint32_t>(32 * warp) << 16), r);
+          tc::tmem_ld32(tmem + c + (static_cast<uint32_t>(32 * q) << 16), r);
           tc::tmem_ld_wait();
 #pragma unroll
-          for (int e = 0; e < 32; ++e) part[(c + e) * kTileK + 32 * warp + lane] = __uint_as_float(r[e]);
+          for (int e = 0; e < 32; ++e) part[(c + e) * kTileK + 32 * q + lane] = __uint_as_float(r[e]);
         }
       }
     }
@@ -379,11 +400,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     for (int i = threadIdx.x; i < rows * (kTileK / 4); i += kTcThreads) {
       const int n = rank * rows + i / (kTileK / 4), k = 4 * (i % (kTileK / 4));
       if (n >= kTileN || n0 + n >= a.n || k0 + k >= a.k) continue;
+      // all ranks' pieces are fetched before any is added
+      float4 piece[8];
+#pragma unroll
+      for (uint32_t q = 0; q < 8; ++q) {
+        piece[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (q < csize && static_cast<int64_t>(total) * q / csize != static_cast<int64_t>(total) * (q + 1) / csize)
+          piece[q] = remote_float4(tc::su32(part + n * kTileK + k), q);
+      }
       float v[4] = {};
-      for (uint32_t q = 0; q < csize; ++q) {
-        if (static_cast<int64_t>(total) * q / csize == static_cast<int64_t>(total) * (q + 1) / csize) continue;   // no tokens
-        const float4 w = remote_float4(tc::su32(part + n * kTileK + k), q);
-        v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        v[0] += piece[q].x; v[1] += piece[q].y; v[2] += piece[q].z; v[3] += piece[q].w;
       }
       TW* p = static_cast<TW*>(a.dw) + static_cast<int64_t>(n0 + n) * a.dw_ld + k0 + k;
 #pragma unroll
