@@ -5,10 +5,10 @@
 // starting with the block on the diagonal (where every row sees at least
 // itself, so the running maximum is finite from the first block on), with the
 // running maximum and sum of the softmax; one pass over K and V.
-// Backward: P is formed again from the log-sum.  Two kernels, one owning 64
-// keys (dK, dV summed over the query heads of the group and the later query
-// blocks), one owning 64 queries (dQ): each output is summed by one CTA in a
-// fixed order, at the price of forming the scores twice.
+// Backward: P is formed again from the log-sum.  Half of the CTAs own 64 keys
+// (dK, dV summed over the query heads of the group and the later query blocks),
+// half 64 queries (dQ): each output is summed by one CTA in a fixed order, at
+// the price of forming the scores twice.
 //
 // A thread holds a 4 x 4 piece of a 64 x 64 score tile (rows ty + 16 r, columns
 // tx + 16 c) and a 4 x (D / 16) piece of a 64 x D product; tiles lie in shared
@@ -33,17 +33,44 @@ template <int DP> __host__ __device__ constexpr int ld() { return DP + 4; }
 
 // 64 rows from `row0` of a head into shared memory; rows at or past `rows` and
 // columns at or past `dim` are zero.
+template <typename T, int DP> struct Tile {
+  static constexpr int kEach = kB * (DP / 8) / kThreads;   // groups of 8 elements of a thread
+  float v[kEach][8];
+  __device__ __forceinline__ void fetch(const AttnTensor& t, int64_t row0, int rows, int head, int dim) {
+    const T* src = static_cast<const T*>(t.p) + row0 * t.ts + head * t.hs;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int e = threadIdx.x + kThreads * i, r = e / (DP / 8), c = (e % (DP / 8)) * 8;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[i][k] = 0.f;
+      if (r < rows && c < dim) load8(src + r * t.ts + c, v[i]);
+    }
+  }
+  __device__ __forceinline__ void put(float* dst) const {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int e = threadIdx.x + kThreads * i, r = e / (DP / 8), c = (e % (DP / 8)) * 8;
+#pragma unroll
+      for (int k = 0; k < 8; k += 4)
+        *reinterpret_cast<float4*>(dst + r * ld<DP>() + c + k) = make_float4(v[i][k], v[i][k + 1], v[i][k + 2], v[i][k + 3]);
+    }
+  }
+};
 template <typename T, int DP>
 __device__ __forceinline__ void load_tile(float* dst, const AttnTensor& t, int64_t row0, int rows, int head, int dim) {
-  const T* src = static_cast<const T*>(t.p) + row0 * t.ts + head * t.hs;
-  for (int e = threadIdx.x; e < kB * (DP / 8); e += kThreads) {
-    const int r = e / (DP / 8), c = (e % (DP / 8)) * 8;
-    float v[8] = {};
-    if (r < rows && c < dim) load8(src + r * t.ts + c, v);
-#pragma unroll
-    for (int i = 0; i < 8; i += 4)
-      *reinterpret_cast<float4*>(dst + r * ld<DP>() + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-  }
+  Tile<T, DP> x;
+  x.fetch(t, row0, rows, head, dim);
+  x.put(dst);
+}
+// Two tiles of the same rows, their reads in flight together.
+template <typename T, int DP>
+__device__ __forceinline__ void load_tiles(float* dst0, const AttnTensor& t0, float* dst1, const AttnTensor& t1,
+                                           int64_t row0, int rows, int head, int dim) {
+  Tile<T, DP> x, y;
+  x.fetch(t0, row0, rows, head, dim);
+  y.fetch(t1, row0, rows, head, dim);
+  x.put(dst0);
+  y.put(dst1);
 }
 
 // s[r][c] = <A row ty + 16 r, B row tx + 16 c>
@@ -154,9 +181,9 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
   float* Q = sm;
   float* KV = Q + kB * ld<DP>();
   float* P = KV + kB * ld<DP>();
-  const int head = blockIdx.y, kvh = head / a.group;
+  const int head = static_cast<int>(blockIdx.x % a.heads), kvh = head / a.group;
   Rows w;
-  if (!rows_of(a, a.by_query, blockIdx.x, w)) return;
+  if (!rows_of(a, a.by_query, blockIdx.x / a.heads, w)) return;
   const int64_t row0 = w.seq + w.first;
   float* lse = a.lse + static_cast<int64_t>(head) * a.tokens + row0;
   if (!w.len) {
@@ -261,18 +288,15 @@ __device__ __forceinline__ void load_stats(const AttnArgs& a, float* lse, float*
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads) k_attn_dkdv(const __grid_constant__ AttnArgs a) {
-  extern __shared__ float sm[];
+__device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int kvh, float* sm, float* lse, float* delta) {
   float* K = sm;
   float* V = K + kB * ld<DP>();
   float* Q = V + kB * ld<DP>();
   float* dO = Q + kB * ld<DP>();
   float* Pt = dO + kB * ld<DP>();   // P^T, then dS^T: [key][query]
   float* St = Pt + kB * kPs;
-  __shared__ float lse[kB], delta[kB];
-  const int kvh = blockIdx.y;
   Rows w;
-  if (!rows_of(a, a.by_key, blockIdx.x, w)) return;
+  if (!rows_of(a, a.by_key, item, w)) return;
   const int64_t row0 = w.seq + w.first;
   if (!w.len) {
     const int rows = static_cast<int>(min(static_cast<int64_t>(kB), a.tokens - row0));
@@ -282,8 +306,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkdv(const __grid_constant__ 
   }
   const int rows = min(kB, w.len - w.first);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  load_tile<T, DP>(K, a.k, row0, rows, kvh, a.dim);
-  load_tile<T, DP>(V, a.v, row0, rows, kvh, a.dim);
+  load_tiles<T, DP>(K, a.k, V, a.v, row0, rows, kvh, a.dim);
   float4 dk[4][DP / 64], dv[4][DP / 64];
 #pragma unroll
   for (int r = 0; r < 4; ++r)
@@ -294,8 +317,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkdv(const __grid_constant__ 
     for (int i0 = w.first; i0 < w.len; i0 += kB) {
       const int qrows = min(kB, w.len - i0);
       __syncthreads();
-      load_tile<T, DP>(Q, a.q, w.seq + i0, qrows, head, a.dim);
-      load_tile<T, DP>(dO, a.dout, w.seq + i0, qrows, head, a.dim);
+      load_tiles<T, DP>(Q, a.q, dO, a.dout, w.seq + i0, qrows, head, a.dim);
       load_stats(a, lse, delta, head, w.seq + i0, qrows);
       __syncthreads();
       float p[4][4], s[4][4];
@@ -318,17 +340,15 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkdv(const __grid_constant__ 
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads) k_attn_dq(const __grid_constant__ AttnArgs a) {
-  extern __shared__ float sm[];
+__device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, int head, float* sm, float* lse, float* delta) {
   float* Q = sm;
   float* dO = Q + kB * ld<DP>();
   float* K = dO + kB * ld<DP>();
   float* V = K + kB * ld<DP>();
   float* S = V + kB * ld<DP>();
-  __shared__ float lse[kB], delta[kB];
-  const int head = blockIdx.y, kvh = head / a.group;
+  const int kvh = head / a.group;
   Rows w;
-  if (!rows_of(a, a.by_query, blockIdx.x, w)) return;
+  if (!rows_of(a, a.by_query, item, w)) return;
   const int64_t row0 = w.seq + w.first;
   if (!w.len) {
     zero_rows<T>(a.dq, row0, static_cast<int>(min(static_cast<int64_t>(kB), a.tokens - row0)), head, a.dim);
@@ -336,8 +356,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(const __grid_constant__ At
   }
   const int rows = min(kB, w.len - w.first);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  load_tile<T, DP>(Q, a.q, row0, rows, head, a.dim);
-  load_tile<T, DP>(dO, a.dout, row0, rows, head, a.dim);
+  load_tiles<T, DP>(Q, a.q, dO, a.dout, row0, rows, head, a.dim);
   load_stats(a, lse, delta, head, row0, rows);
   float4 dq[4][DP / 64];
 #pragma unroll
@@ -347,8 +366,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(const __grid_constant__ At
   for (int j0 = 0; j0 <= w.first; j0 += kB) {
     const int krows = min(kB, w.len - j0);
     __syncthreads();
-    load_tile<T, DP>(K, a.k, w.seq + j0, krows, kvh, a.dim);
-    load_tile<T, DP>(V, a.v, w.seq + j0, krows, kvh, a.dim);
+    load_tiles<T, DP>(K, a.k, V, a.v, w.seq + j0, krows, kvh, a.dim);
     __syncthreads();
     float p[4][4], s[4][4];
     grad_scores<DP>(a, Q, K, dO, V, lse, delta, w.first, j0, w.len, ty, tx, p, s);
@@ -361,6 +379,19 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(const __grid_constant__ At
   }
   const float c[4] = {a.scale, a.scale, a.scale, a.scale};
   store_tile<T, DP>(a.dq, row0, rows, head, a.dim, ty, tx, dq, c);
+}
+
+// Both kinds of work in one launch, side by side for each 64 rows, so that the
+// SMs that run out of the one take the other.  At head dimensions up to 64 two
+// CTAs share an SM.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) k_attn_bwd(const __grid_constant__ AttnArgs a) {
+  extern __shared__ float sm[];
+  __shared__ float lse[kB], delta[kB];
+  const int all = a.kv_heads + a.heads, which = static_cast<int>(blockIdx.x % all);
+  const int64_t item = blockIdx.x / all;
+  if (which < a.kv_heads) owned_keys<T, DP>(a, item, which, sm, lse, delta);
+  else owned_queries<T, DP>(a, item, which - a.kv_heads, sm, lse, delta);
 }
 
 // LANES (8 or 16) lanes per row and head, 8 columns each.
@@ -384,26 +415,20 @@ __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ Attn
   if (lane == 0 && row < a.total) a.delta[static_cast<int64_t>(head) * a.tokens + row] = s;
 }
 
+// `each`: CTAs for every 64 rows.
 template <auto kernel>
-cudaError_t run(const AttnArgs& a, int heads, size_t smem, cudaStream_t s) {
+cudaError_t run(const AttnArgs& a, int each, size_t smem, cudaStream_t s) {
   const cudaError_t e = allow_smem<kernel>(smem);
   if (e) return e;
-  const int64_t tail = (a.tokens - a.total + kB - 1) / kB;
-  const dim3 grid(static_cast<unsigned>(2 * static_cast<int64_t>(a.n_blocks) + tail), static_cast<unsigned>(heads));
-  if (!grid.x) return cudaSuccess;
-  kernel<<<grid, kThreads, smem, s>>>(a);
+  const int64_t ctas = (2 * static_cast<int64_t>(a.n_blocks) + cdiv(a.tokens - a.total, kB)) * each;
+  if (!ctas) return cudaSuccess;
+  if (ctas >= (int64_t(1) << 31)) return cudaErrorInvalidConfiguration;
+  kernel<<<static_cast<unsigned>(ctas), kThreads, smem, s>>>(a);
   return cudaGetLastError();
 }
 
 template <int DP> constexpr size_t fwd_smem() { return sizeof(float) * (2 * kB * ld<DP>() + kB * kPs); }
-template <int DP> constexpr size_t dkdv_smem() { return sizeof(float) * (4 * kB * ld<DP>() + 2 * kB * kPs); }
-template <int DP> constexpr size_t dq_smem() { return sizeof(float) * (4 * kB * ld<DP>() + kB * kPs); }
-
-template <typename T, int DP>
-cudaError_t backward(const AttnArgs& a, cudaStream_t s) {
-  cudaError_t e = run<k_attn_dkdv<T, DP>>(a, a.kv_heads, dkdv_smem<DP>(), s);
-  return e ? e : run<k_attn_dq<T, DP>>(a, a.heads, dq_smem<DP>(), s);
-}
+template <int DP> constexpr size_t bwd_smem() { return sizeof(float) * (4 * kB * ld<DP>() + 2 * kB * kPs); }
 
 }  // namespace
 
@@ -413,7 +438,9 @@ cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t s) {
 }
 
 cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s) {
-  return a.dim <= 64 ? backward<float, 64>(a, s) : backward<float, 128>(a, s);
+  const int each = a.kv_heads + a.heads;
+  return a.dim <= 64 ? run<k_attn_bwd<float, 64>>(a, each, bwd_smem<64>(), s)
+                     : run<k_attn_bwd<float, 128>>(a, each, bwd_smem<128>(), s);
 }
 
 template <typename T>
