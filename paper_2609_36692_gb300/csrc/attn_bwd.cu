@@ -29,8 +29,14 @@
 // second set of accumulators, so that an item's start and end overlap its
 // neighbours.
 //
-// Roundings to bf16: P and dS once each (MMA operands; kUnbias), the gradients
-// once.
+// Reductions to bf16: P and dS once each (MMA operands, cut with kUnbias), the
+// gradients once.
+//
+// What bounds it: the products.  16384 tokens, 16 / 8 heads of 128: 2.38 ms
+// alone, 2.52 ms in a loop, where the seven products run at 1530 TFLOP/s and the
+// clock falls with the power limit.  Short sequences add the items' ends (the
+// gradients' way from TMEM to memory, 2000 cycles against 2050 an iteration of
+// dK, dV at head_dim 64): 8 x 1024 tokens, 12 heads of 64, 0.080 ms.
 #include "attn_tc.cuh"
 
 namespace normpre {

@@ -6,7 +6,9 @@
 // features each, so that a warp reads and writes whole 32-byte sectors of 4
 // rows, the maximum of a 32-element block needs one shuffle, and the steps of
 // consecutive rows (one 32-bit word per row and panel) leave in whole sectors.
-// Bound by HBM.
+// Bound by HBM: 16384 x 6144 bf16, pack and restore 0.102 ms (6.0 TB/s), the
+// gated activation and its gradient 0.268 ms (6.1 TB/s; a copy runs at 6.8).
+// Small calls are bound by the launch.
 #include <atomic>
 #include <string>
 

@@ -331,7 +331,10 @@ class _Linear(torch.autograd.Function):
 
 def linear(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
     """Differentiable y = x W^T that keeps x in 8 bits for its backward pass;
-    the weight gradient comes in the weight's dtype."""
+    the weight gradient comes in the weight's dtype.  Nothing is kept where
+    there will be none."""
+    if not (torch.is_grad_enabled() and weight.requires_grad):
+        return x @ weight.to(x.dtype).t()
     return _Linear.apply(x, weight)
 
 
