@@ -13,14 +13,16 @@
 // Both operands are read along their rows (MN-major), as they lie in memory:
 // nothing is transposed.  The 128 side is the converted one: half the bytes to
 // convert of the 256 side.
-//   Two CTAs of a cluster take two neighbouring feature tiles of the same
-// outputs and each multicasts half of their dY boxes to both (24 KB instead of
-// 40 KB of L2 reads a step).
-//   What bounds it: 40 KB a step enter an SM, multicast or not, at 60 of the 64
-// bytes a cycle of its L2 port: 660 cycles a step against the MMAs' 512.  256 x
-// 192 tiles take in fewer bytes an MMA, but their conversion (4 cycles an
-// element and SM sub-partition, byte permutations at half rate) then takes
-// 1000 cycles of the MMAs' 768.  16384 x 6144 x 2048: 0.305 ms, 1350 TFLOP/s.
+//   A pair of CTAs takes two neighbouring feature tiles of the same outputs as
+// one product of 256 features: each converts its own 128 features and loads the
+// dY of 128 outputs, and a thread of the even CTA issues the MMAs that read both.
+//   What bounds it: an SM takes in 24 KB a step, 375 cycles of its L2 port's 64
+// bytes a cycle, under the MMAs' 512 (40 KB, 660 cycles, when each CTA works for
+// itself; a multicast saves L2 reads but not the port).  256 x 192 tiles of one
+// CTA take in fewer bytes too, but their conversion (4 cycles an element and SM
+// sub-partition, byte permutations at half rate) then takes 1000 cycles of the
+// MMAs' 768.  16384 x 6144 x 2048: 0.248 ms (1660 TFLOP/s), 0.274 ms in a long
+// loop, where the clock falls with the power limit.
 //   With too few tiles for the SMs, clusters of 2 to 8 CTAs split a tile's
 // tokens instead and join through distributed shared memory: each CTA lays its
 // accumulator out in its (then idle) ring and sums one slice of the outputs
@@ -91,11 +93,12 @@ constexpr int kTileK = 128, kTileN = 256, kStep = 64;   // features, outputs (at
 // stands between the rings and the tensor cores.
 constexpr int kRing = 4;
 constexpr int kBox = 64 * 128;                           // bytes of 64 rows of 64 bf16
-constexpr int kDyBytes = 4 * kBox, kCodeBytes = kStep * kTileK, kXBytes = 2 * kBox;
+constexpr int kCodeBytes = kStep * kTileK, kXBytes = 2 * kBox;
+constexpr int kDyRingBytes = 16 * kBox;                  // 4 places of 4 boxes, or 8 of a pair's 2
 constexpr int kConvert = 4, kGroups = 4;                 // converting warps of a step; groups that take turns
 constexpr int kTma = 4 + kGroups * kConvert, kMma = kTma + 1, kCodes = kTma + 2;   // warps: drain, convert, these
 constexpr int kTcThreads = 32 * (kCodes + 1);
-constexpr size_t kTcSmem = kRing * (kDyBytes + kXBytes + kCodeBytes) + 512;
+constexpr size_t kTcSmem = kDyRingBytes + kRing * (kXBytes + kCodeBytes) + 512;
 
 struct WgradTcArgs {
   WgradArgs a;
@@ -105,11 +108,13 @@ struct WgradTcArgs {
 };
 
 struct WgradBars {
-  // of dY, the codes, the converted tiles, the accumulators
-  uint64_t full[kRing], empty[kRing], cfull[kRing], cempty[kRing], xfull[kRing], xempty[kRing], tfull[2], tempty[2], drain;
+  // of dY, the codes, the converted tiles (of this CTA, and both operands of the
+  // pair's other), the accumulators
+  uint64_t full[8], empty[8], cfull[kRing], cempty[kRing], xfull[kRing], xempty[kRing], ofull[kRing];
+  uint64_t tfull[2], tempty[2], drain;
   uint32_t tmem;
   int abort;
-  uint32_t issued[kRing], cissued[kRing];   // last parity + 1 of full and cfull
+  uint32_t issued[8], cissued[kRing];   // last parity + 1 of full and cfull
 };
 
 // A float of another CTA's shared memory in the cluster.
@@ -135,13 +140,15 @@ __device__ __forceinline__ void convert4(uint32_t w, uint64_t step2, uint64_t of
   p1 = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
 }
 
-// SPLIT: the cluster's CTAs share a tile and split its tokens; otherwise a
-// cluster of two takes two feature tiles and shares dY.
+// SPLIT: the cluster's CTAs share a tile and split its tokens; otherwise a pair
+// of CTAs takes two feature tiles, each with half of dY's columns, and one thread
+// of the even CTA issues the MMAs of both.
 template <typename TW, bool SPLIT>
 __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constant__ WgradTcArgs f) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  uint8_t* ring = smem;                                   // [kRing] dY boxes
-  uint8_t* xbuf = ring + kRing * kDyBytes;                // [kRing] the codes as bf16
+  constexpr int kDyRing = SPLIT ? 4 : 8, kDyBytes = kDyRingBytes / kDyRing;
+  uint8_t* ring = smem;                                   // [kDyRing] dY boxes
+  uint8_t* xbuf = ring + kDyRingBytes;                    // [kRing] the codes as bf16
   uint8_t* codes = xbuf + kRing * kXBytes;                // [kRing]
   WgradBars* b = reinterpret_cast<WgradBars*>(codes + kRing * kCodeBytes);
   static_assert(sizeof(WgradBars) <= 512, "barriers");
@@ -156,18 +163,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   const int s1 = SPLIT ? static_cast<int>(static_cast<int64_t>(total) * (rank + 1) / csize) : total;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kRing; ++i) {
+    for (int i = 0; i < kDyRing; ++i) {
       tc::mbar_init(&b->full[i], 1);
-      tc::mbar_init(&b->empty[i], SPLIT ? 1 : 2);
+      tc::mbar_init(&b->empty[i], 1);
+      b->issued[i] = 0;
+    }
+    for (int i = 0; i < kRing; ++i) {
+      tc::mbar_init(&b->ofull[i], 1);
       tc::mbar_init(&b->cfull[i], 1);
       tc::mbar_init(&b->cempty[i], kConvert);
       tc::mbar_init(&b->xfull[i], kConvert);
       tc::mbar_init(&b->xempty[i], 1);
-      b->issued[i] = b->cissued[i] = 0;
+      b->cissued[i] = 0;
     }
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(&b->tfull[i], 1);
-      tc::mbar_init(&b->tempty[i], 4);
+      tc::mbar_init(&b->tempty[i], SPLIT ? 4 : 8);
     }
     tc::mbar_init(&b->drain, 1);
     b->abort = 0;
@@ -176,13 +187,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     tc::prefetch_map(&f.codes);
   }
   __syncthreads();
-  tc::cluster_sync();   // the peer's barriers exist before a multicast reaches them
+  tc::cluster_sync();   // the peer's barriers exist before an arrival reaches them
   if (warp == kMma) {
-    tc::tmem_alloc(&b->tmem, 512);
-    tc::tmem_relinquish();
+    if (SPLIT) {
+      tc::tmem_alloc(&b->tmem, 512);
+      tc::tmem_relinquish();
+    } else {
+      tc::tmem_alloc_pair(&b->tmem, 512);
+      tc::tmem_relinquish_pair();
+    }
     tc::fence_before();
   }
   __syncthreads();
+  if (!SPLIT) tc::cluster_sync();   // both have their accumulators
   tc::fence_after();
   const uint32_t tmem = b->tmem;
   bool ok = true;
@@ -194,28 +211,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   // feature tile and first output of a unit
   auto tile_k = [&](int u) { return SPLIT ? u % f.tiles_k : 2 * (u % ((f.tiles_k + 1) / 2)) + static_cast<int>(rank); };
   auto first_n = [&](int u) { return (SPLIT ? u / f.tiles_k : u / ((f.tiles_k + 1) / 2)) * f.tile_n; };
-  int st = 0;            // place in the rings, and the parity of its uses
-  uint32_t phase = 0;
-  auto next = [&]() {
-    if (++st == kRing) { st = 0; phase ^= 1u; }
+  struct Place {         // in a ring of N, and the parity of its uses
+    int at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int n) {
+      if (++at == n) { at = 0; phase ^= 1u; }
+    }
   };
+  Place y, x;            // of dY's ring and the others
 
   if (warp == kTma) {
     // ---------------- dY by TMA (one thread) ----------------
     if (tc::elect_one()) {
       for (int u = unit0; u < f.units && ok; u += nunits) {
-        const int n0 = first_n(u);
-        for (int s = s0; s < s1; ++s, next()) {
-          if (!wait1(&b->empty[st], phase ^ 1u)) break;
-          uint8_t* dst = ring + st * kDyBytes;
-          tc::mbar_expect_tx(&b->full[st], kDyBytes);
-          b->issued[st] = phase + 1;
-          if (SPLIT) {
-            for (int i = 0; i < 4; ++i) tc::tma_load_3d(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, s * kStep, 0);
-          } else {
-            for (int i = 2 * rank; i < 2 * static_cast<int>(rank) + 2; ++i)
-              tc::tma_load_3d_mc(dst + i * kBox, &f.dy, &b->full[st], n0 + 64 * i, s * kStep, 0, 3);
-          }
+        const int n0 = first_n(u) + (SPLIT ? 0 : static_cast<int>(rank) * f.tile_n / 2);
+        for (int s = s0; s < s1; ++s, y.next(kDyRing)) {
+          if (!wait1(&b->empty[y.at], y.phase ^ 1u)) break;
+          uint8_t* dst = ring + y.at * kDyBytes;
+          tc::mbar_expect_tx(&b->full[y.at], kDyBytes);
+          b->issued[y.at] = y.phase + 1;
+          for (int i = 0; i < kDyBytes / kBox; ++i)
+            tc::tma_load_3d(dst + i * kBox, &f.dy, &b->full[y.at], n0 + 64 * i, s * kStep, 0);
         }
       }
     }
@@ -226,11 +242,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     if (tc::elect_one()) {
       for (int u = unit0; u < f.units && ok; u += nunits) {
         const int k0 = tile_k(u) * kTileK;
-        for (int s = s0; s < s1; ++s, next()) {
-          if (!wait1(&b->cempty[st], phase ^ 1u)) break;
-          tc::mbar_expect_tx(&b->cfull[st], kCodeBytes);
-          b->cissued[st] = phase + 1;
-          tc::tma_load_3d(codes + st * kCodeBytes, &f.codes, &b->cfull[st], k0, s * kStep, 0);
+        for (int s = s0; s < s1; ++s, x.next(kRing)) {
+          if (!wait1(&b->cempty[x.at], x.phase ^ 1u)) break;
+          tc::mbar_expect_tx(&b->cfull[x.at], kCodeBytes);
+          b->cissued[x.at] = x.phase + 1;
+          tc::tma_load_3d(codes + x.at * kCodeBytes, &f.codes, &b->cfull[x.at], k0, s * kStep, 0);
         }
       }
     }
@@ -238,31 +254,54 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
     ok = __all_sync(0xffffffffu, ok);
   } else if (warp == kMma) {
     // ---------------- MMA (one thread) ----------------
-    if (tc::elect_one()) {
-      const uint32_t idesc = tc::idesc_bf16(kTileK, f.tile_n, 1, 1);
+    if (!SPLIT && rank != 0) {
+      // The pair's other CTA: its operands are in place.  The tensor cores of
+      // this SM read them, no thread elsewhere does, so that the arrival need not
+      // order them for the cluster (a release and acquire at that scope take 2100
+      // cycles a step, all others together 600).
+      if (tc::elect_one()) {
+        for (int u = unit0; u < f.units && ok; u += nunits)
+          for (int s = s0; s < s1; ++s, y.next(kDyRing), x.next(kRing)) {
+            if (!wait1(&b->full[y.at], y.phase) || !wait1(&b->xfull[x.at], x.phase)) break;
+            tc::mbar_arrive_remote(&b->ofull[x.at], 0);
+          }
+        // the issuing thread's last arrival: none is under way after it
+        int never = 0;
+        tc::mbar_wait(&b->drain, 0, &never);
+      }
+    } else if (tc::elect_one()) {
+      const uint32_t idesc = tc::idesc_bf16(SPLIT ? kTileK : 2 * kTileK, f.tile_n, 1, 1);
+      auto commit = [&](uint64_t* bar) {   // in both CTAs of a pair
+        if (SPLIT) tc::mma_commit(bar);
+        else tc::mma_commit_pair(bar, 3);
+      };
       int acc = 0, never = 0;
       uint32_t tphase = 0;
       for (int u = unit0; u < f.units && ok; u += nunits) {
         if (!wait1(&b->tempty[acc], tphase ^ 1u)) break;
-        for (int s = s0; s < s1; ++s, next()) {
-          if (!wait1(&b->full[st], phase) || !wait1(&b->xfull[st], phase)) break;
+        for (int s = s0; s < s1; ++s, y.next(kDyRing), x.next(kRing)) {
+          if (!wait1(&b->full[y.at], y.phase) || !wait1(&b->xfull[x.at], x.phase)) break;
+          if (!SPLIT && !wait1(&b->ofull[x.at], x.phase)) break;
           tc::fence_after();
-          const uint64_t dy = tc::sdesc(tc::su32(ring + st * kDyBytes), kBox, 1024);
-          const uint64_t x = tc::sdesc(tc::su32(xbuf + st * kXBytes), kBox, 1024);
+          const uint64_t bd = tc::sdesc(tc::su32(ring + y.at * kDyBytes), kBox, 1024);
+          const uint64_t ad = tc::sdesc(tc::su32(xbuf + x.at * kXBytes), kBox, 1024);
 #pragma unroll
-          for (int kk = 0; kk < kStep / 16; ++kk)
-            tc::mma_bf16(tmem + 256 * acc, x + kk * (2048 >> 4), dy + kk * (2048 >> 4), idesc, s != s0 || kk != 0);
-          if (SPLIT) tc::mma_commit(&b->empty[st]);
-          else tc::mma_commit_mc(&b->empty[st], 3);
-          tc::mma_commit(&b->xempty[st]);
+          for (int kk = 0; kk < kStep / 16; ++kk) {
+            const uint32_t d = tmem + 256 * acc, add = s != s0 || kk != 0;
+            if (SPLIT) tc::mma_bf16(d, ad + kk * (2048 >> 4), bd + kk * (2048 >> 4), idesc, add);
+            else tc::mma_bf16_pair(d, ad + kk * (2048 >> 4), bd + kk * (2048 >> 4), idesc, add);
+          }
+          commit(&b->empty[y.at]);
+          commit(&b->xempty[x.at]);
         }
         if (!ok) break;
-        tc::mma_commit(&b->tfull[acc]);
+        commit(&b->tfull[acc]);
         acc ^= 1;
         if (acc == 0) tphase ^= 1u;
       }
       // every MMA issued has completed once `drain` fires
-      tc::mma_commit(&b->drain);
+      // every MMA issued has completed once `drain` fires
+      commit(&b->drain);
       tc::mbar_wait(&b->drain, 0, &never);
     }
     __syncwarp();
@@ -372,7 +411,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
       }
       tc::fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&b->tempty[acc]);
+      if (lane == 0) tc::mbar_arrive_remote(&b->tempty[acc], 0);   // where the MMAs are issued
       acc ^= 1;
       if (acc == 0) tphase ^= 1u;
     }
@@ -428,18 +467,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   if (threadIdx.x == 0 && *static_cast<volatile int*>(&b->abort)) {
     // let every TMA copy still in flight land before the CTA exits
     volatile int never = 0;
-    for (int i = 0; i < kRing; ++i) {
+    for (int i = 0; i < kDyRing; ++i)
       if (b->issued[i]) tc::mbar_wait(&b->full[i], b->issued[i] - 1, &never);
+    for (int i = 0; i < kRing; ++i)
       if (b->cissued[i]) tc::mbar_wait(&b->cfull[i], b->cissued[i] - 1, &never);
-    }
   }
   __syncthreads();
-  // no CTA exits while the other may still multicast into it, arrive on its
-  // barriers or read its partial tile
+  // no CTA exits while the other may still arrive on its barriers, work on its
+  // operands or read its partial tile
   tc::cluster_sync();
   if (warp == kMma) {
     tc::fence_after();
-    tc::tmem_dealloc(tmem, 512);
+    if (SPLIT) tc::tmem_dealloc(tmem, 512);
+    else tc::tmem_dealloc_pair(tmem, 512);
   }
 }
 
@@ -500,7 +540,7 @@ cudaError_t launch_tc(WgradTcArgs f, cudaStream_t s) {
   // The tile width whose rounds over the clusters take least: 2 cycles an
   // output and step, about 100 a step beside them.
   int64_t least = -1;
-  for (int tn = kTileN; tn >= 192; tn -= 16) {
+  for (int tn = kTileN; tn >= 192; tn -= 32) {
     const int64_t units = (f.tiles_k + 1) / 2 * cdiv(f.a.n, tn), cost = cdiv(units, fit) * (2 * tn + 100);
     if (least >= 0 && cost >= least) continue;
     least = cost;
