@@ -16,9 +16,11 @@
 //   A pair of CTAs takes two neighbouring feature tiles of the same outputs as
 // one product of 256 features: each converts its own 128 features and loads the
 // dY of 128 outputs, and a thread of the even CTA issues the MMAs that read both.
-//   What bounds it: an SM takes in 24 KB a step, 375 cycles of its L2 port's 64
-// bytes a cycle, under the MMAs' 512 (40 KB, 660 cycles, when each CTA works for
-// itself; a multicast saves L2 reads but not the port).  256 x 192 tiles of one
+//   What bounds it: shared memory, whose 128 bytes a cycle pass 80 KB a step (24
+// KB in, 24 KB through the conversion, 32 KB of MMA operands: 625 cycles against
+// the MMAs' 512).  From L2 an SM takes in 24 KB, 375 cycles of its port's 64 bytes
+// a cycle (40 KB, 660 cycles, when each CTA works for itself; a multicast saves
+// L2 reads but not the port).  256 x 192 tiles of one
 // CTA take in fewer bytes too, but their conversion (4 cycles an element and SM
 // sub-partition, byte permutations at half rate) then takes 1000 cycles of the
 // MMAs' 768.  16384 x 6144 x 2048: 0.248 ms (1660 TFLOP/s), 0.274 ms in a long
@@ -537,11 +539,14 @@ cudaError_t launch_tc(WgradTcArgs f, cudaStream_t s) {
   }
   const cudaError_t e = clusters_at_once<TW, false>(2, &fit);
   if (e) return e;
-  // The tile width whose rounds over the clusters take least: 2 cycles an
-  // output and step, about 100 a step beside them.
+  // The tile width whose rounds over the clusters take least.  Shared memory
+  // serves a step's 64 KB and 64 bytes an output at about 128 bytes a cycle, so
+  // that a narrower tile gains little (16384 x 4096 x 2432, three rounds each:
+  // 252 us at 256, 248 at 224, 238 at 192) and a further round costs all of it
+  // (16384 x 6912 x 2048: 266 us at 256, 327 at 224).
   int64_t least = -1;
   for (int tn = kTileN; tn >= 192; tn -= 32) {
-    const int64_t units = (f.tiles_k + 1) / 2 * cdiv(f.a.n, tn), cost = cdiv(units, fit) * (2 * tn + 100);
+    const int64_t units = (f.tiles_k + 1) / 2 * cdiv(f.a.n, tn), cost = cdiv(units, fit) * (512 + tn / 2);
     if (least >= 0 && cost >= least) continue;
     least = cost;
     f.tile_n = tn;
