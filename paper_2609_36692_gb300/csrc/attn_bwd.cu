@@ -66,7 +66,10 @@ template <int kSlots> struct Bars {
   // zeroed it counts as full
   uint64_t full[kSlots], empty[kSlots], raw[kSlots];
   uint64_t own_full[2][2], own_empty[2];   // per set: the two owned tiles, freed together
-  uint64_t s_full[2], dp_full, p_ready, ds_ready, dp_free;
+  // ds_ready, dQ: one per buffer of S.  The softmax warps can be done with both
+  // buffers before the MMA thread looks: on one barrier that would be two phases
+  // ahead, which its parity cannot tell from none.
+  uint64_t s_full[2], dp_full, p_ready, ds_ready[2], dp_free;
   uint64_t acc_full[2], acc_empty[2];
   uint64_t stat_empty[2];
   uint64_t drain[2];
@@ -98,7 +101,7 @@ __device__ __forceinline__ void init_bars(Bars<kSlots>* b, int users) {
   }
   tc::mbar_init(&b->dp_full, 1);
   tc::mbar_init(&b->p_ready, kSoftmax);
-  tc::mbar_init(&b->ds_ready, kSoftmax);
+  for (int i = 0; i < 2; ++i) tc::mbar_init(&b->ds_ready[i], kSoftmax);
   tc::mbar_init(&b->dp_free, kSoftmax);
   b->abort = 0;
   tc::fence_barrier_init();
@@ -360,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         if (n == 1) tc::mma_commit(&b->own_empty[set.i]);
         if (!w.wait1(&b->acc_empty[set.i], set.parity ^ 1u)) break;
         for (int i = 0; i < n; ++i) {
-          if (!w.wait1(&b->ds_ready, ds_phase)) break;
+          if (!w.wait1(&b->ds_ready[0], ds_phase)) break;
           ds_phase ^= 1u;
           product_ts<DP, 4>(cAcc + 2 * DP * set.i + DP, cP, tile(q), i == 0);
           tc::mma_commit(&b->empty[q]);
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         }
         tc::tmem_put16(mP, pk);
         tc::tmem_st_drain();
-        w.arrive(&b->ds_ready);
+        w.arrive(&b->ds_ready[0]);
         if (lane == 0) tc::mbar_arrive(&b->stat_empty[st.i]);
         st.next();
       }
@@ -536,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
   } else if (warp == kMmaA) {
     // ---------------- MMA (one thread): dQ(j), S(j + 2) ----------------
     if (tc::elect_one()) {
-      uint32_t ds_phase = 0;
+      uint32_t ds_phase = 0;                                      // a bit per buffer
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int n = it.blk + 1;
@@ -555,9 +558,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         if (n > 1 && w.ok) scores(1, k[1]);
         if (!w.wait1(&b->acc_empty[set.i], set.parity ^ 1u)) break;
         for (int j = 0; j < n; ++j) {
-          if (!w.wait1(&b->ds_ready, ds_phase)) break;
-          ds_phase ^= 1u;
-          product_ts<DP, 4>(cAcc + DP * set.i, cS + 128 * (buf.i ^ (j & 1)), tile(k[0]), j == 0);
+          const int at = buf.i ^ (j & 1);
+          if (!w.wait1(&b->ds_ready[at], (ds_phase >> at) & 1u)) break;
+          ds_phase ^= 1u << at;
+          product_ts<DP, 4>(cAcc + DP * set.i, cS + 128 * at, tile(k[0]), j == 0);
           tc::mma_commit(&b->empty[k[0]]);
           k[0] = k[1];
           if (j + 2 < n) {
@@ -649,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         }
         tc::tmem_put16(mS, pk);
         tc::tmem_st_drain();
-        w.arrive(&b->ds_ready);
+        w.arrive(&b->ds_ready[buf.i]);
       }
       if (!w.wait(&b->acc_full[set.i], set.parity)) break;
       store_acc<DP>(a.dq, cAcc + DP * set.i + lanes, at, rows, it.head, warp, a.scale, a.dim, lane);

@@ -35,6 +35,24 @@ def test_sequences_of_one_token(dtype):
     check_backward(plan, q, k, v, do, out, lse, ref, [1] * n, dtype)
 
 
+def test_many_backward_passes_in_a_row():
+    """No wait gives up and the bits stay the same over a long queue of passes,
+    whose kernels start beside the ends of those before them."""
+    import torch
+    for h, hk, d, lengths in ((32, 8, 64, [2048] * 2), (8, 4, 128, [1700, 1, 900])):
+        q, k, v, do = make(2, sum(lengths), h, hk, d, "bf16")
+        plan = plan_for(h, hk, d, sum(lengths), lengths, "bf16")
+        out, lse = plan.forward(q, k, v)
+        first = plan.backward(q, k, v, out, lse, do)
+        grads = [torch.empty_like(x) for x in first]
+        for _ in range(6):
+            for _ in range(250):
+                plan.backward(q, k, v, out, lse, do, *grads)
+            assert plan.status() == 0
+            for a, b in zip(first, grads):
+                assert torch.equal(a, b)
+
+
 # tiles of 128 features x 256 outputs: 18, 25, 30, 36, 49 and 66 of them leave
 # room for 8, 6, 5, 4, 3 and 2 CTAs each
 @pytest.mark.parametrize("tiles", [(3, 6), (5, 5), (5, 6), (6, 6), (7, 7), (6, 11), (1, 1)], ids=str)
