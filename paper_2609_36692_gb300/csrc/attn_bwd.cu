@@ -36,7 +36,7 @@
 // alone, 2.52 ms in a loop, where the seven products run at 1530 TFLOP/s and the
 // clock falls with the power limit.  Short sequences add the items' ends (the
 // gradients' way from TMEM to memory, 2000 cycles against 2050 an iteration of
-// dK, dV at head_dim 64): 8 x 1024 tokens, 12 heads of 64, 0.080 ms.
+// dK, dV at head_dim 64): 8 x 1024 tokens, 12 heads of 64, 0.090 ms.
 #include "attn_tc.cuh"
 
 namespace normpre {
@@ -282,8 +282,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   }
   __syncthreads();
   tc::fence_after();
-  tc::grid_wait();      // the deltas; what came before them
-  tc::grid_release();   // k_attn_dq may take the SMs that run out of work here
   const uint32_t cS = b->tmem, cP = cS + 128, cAcc = cS + 256;     // per set: dV, dK
   Warp<kSlots> w = {b, lane, true, 0, 0};
   Turn<kSets> set;
@@ -661,27 +659,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     }
   }
   finish(w, warp, a.flags);
-  // It started beside k_attn_dkdv, which had waited for the deltas, and shares
-  // nothing with it; but what follows in the stream follows both.
-  tc::grid_wait();
 }
 
-// Launched as a programmatic dependent of the kernel before it in the stream.
 template <auto kernel>
 cudaError_t launch(const BwdArgs& f, int heads, size_t smem, cudaStream_t s) {
   const cudaError_t e = allow_smem<kernel>(smem);
   if (e) return e;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[1];
-  cfg.gridDim = dim3(walk_grid(static_cast<int64_t>(f.a.n_blocks) * heads));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, f);
+  kernel<<<walk_grid(static_cast<int64_t>(f.a.n_blocks) * heads), kThreads, smem, s>>>(f);
+  return cudaGetLastError();
 }
 
 }  // namespace

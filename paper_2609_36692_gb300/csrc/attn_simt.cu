@@ -400,7 +400,6 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) k_attn_bwd(const _
 // LANES (8 or 16) lanes per row and head, 8 columns each.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ AttnArgs a) {
-  tc::grid_release();   // the backward kernel sets itself up meanwhile
   const int lane = threadIdx.x % LANES;
   const int64_t i = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) / LANES;   // token-major
   const int64_t row = i / a.heads;

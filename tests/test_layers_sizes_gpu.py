@@ -36,8 +36,7 @@ def test_sequences_of_one_token(dtype):
 
 
 def test_many_backward_passes_in_a_row():
-    """No wait gives up and the bits stay the same over a long queue of passes,
-    whose kernels start beside the ends of those before them."""
+    """No wait gives up and the bits stay the same over a long queue of passes."""
     import torch
     for h, hk, d, lengths in ((32, 8, 64, [2048] * 2), (8, 4, 128, [1700, 1, 900])):
         q, k, v, do = make(2, sum(lengths), h, hk, d, "bf16")
