@@ -7,9 +7,9 @@
 // feature, so that a warp stores 32 consecutive elements of a row of dW) is
 // summed 64 tokens at a time: TMA brings the codes and the dY boxes into a
 // ring, sixteen warps turn codes into swizzled bf16 tiles (a byte becomes an
-// fp32 by permutation into 2^23 + byte, one packed FMA takes off the offset
-// and scales, a permutation packs two), one thread issues the MMAs, and four
-// warps drain a finished accumulator (two in TMEM) while the next tile runs.
+// fp32 by permutation into 2^23 + byte, a packed addition takes off the offset,
+// a packed product scales, a permutation packs two), one thread issues the MMAs,
+// and four warps drain a finished accumulator (two in TMEM) while the next tile runs.
 // Both operands are read along their rows (MN-major), as they lie in memory:
 // nothing is transposed.  The 128 side is the converted one: half the bytes to
 // convert of the 256 side.
@@ -128,17 +128,19 @@ __device__ __forceinline__ float4 remote_float4(uint32_t addr, uint32_t rank) {
   return v;
 }
 
-// Four codes -> two bf16 pairs, code * step.
-__device__ __forceinline__ void convert4(uint32_t w, uint64_t step2, uint64_t off2, uint32_t& p0, uint32_t& p1) {
+// Four codes -> two bf16 pairs, code * step.  The offset comes off before the
+// product, exactly: a multiple of a large step by 2^23 is beyond fp32.
+__device__ __forceinline__ void convert4(uint32_t w, uint64_t step2, uint32_t& p0, uint32_t& p1) {
   w ^= 0x80808080u;   // code + 128
   float f[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440 + i));   // 2^23 + code + 128
+  const uint64_t off2 = tc::pack2(-8388736.f, -8388736.f);                                       // -(2^23 + 128)
   float lo, hi;
   // the values are bf16 numbers: their upper halves are all of them
-  tc::unpack2(tc::fma2(tc::pack2(f[0], f[1]), step2, off2), lo, hi);
+  tc::unpack2(tc::mul2(tc::add2(tc::pack2(f[0], f[1]), off2), step2), lo, hi);
   p0 = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
-  tc::unpack2(tc::fma2(tc::pack2(f[2], f[3]), step2, off2), lo, hi);
+  tc::unpack2(tc::mul2(tc::add2(tc::pack2(f[2], f[3]), off2), step2), lo, hi);
   p1 = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
 }
 
@@ -369,16 +371,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
       if (!wait(&b->xempty[group], parity ^ 1u)) break;
 #pragma unroll
       for (int r = 0; r < kPer; ++r) {
-        const float step = ckpt_step(word[r], blk), off = -8388736.f * step;   // -(2^23 + 128) step
-        const uint64_t step2 = tc::pack2(step, step), off2 = tc::pack2(off, off);
+        const float step = ckpt_step(word[r], blk);
+        const uint64_t step2 = tc::pack2(step, step);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const uint32_t w[4] = {c[r][i].x, c[r][i].y, c[r][i].z, c[r][i].w};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             uint4 v;
-            convert4(w[2 * h], step2, off2, v.x, v.y);
-            convert4(w[2 * h + 1], step2, off2, v.z, v.w);
+            convert4(w[2 * h], step2, v.x, v.y);
+            convert4(w[2 * h + 1], step2, v.z, v.w);
             *reinterpret_cast<uint4*>(dst + 8 * kConvert * 128 * r + (((4 * (blk & 1) + 2 * i + h) ^ sw) << 4)) = v;
           }
         }
