@@ -385,8 +385,8 @@ typedef struct normpre_attn_config {
   int max_seqs;        /* most sequences of one pack, in [1, 65536] */
   int64_t max_tokens;  /* most rows of one call, in [1, 2^24] */
   int dtype;           /* normpre_dtype of Q, K, V, O and the gradients.  BF16: products on the tensor
-                          cores, bf16 operands (the probabilities and ds cut to bf16 once each, scaled
-                          so that the cut is right on average), fp32 accumulation and softmax statistics.
+                          cores, bf16 operands (the probabilities and ds rounded to bf16 once each), fp32
+                          accumulation and softmax statistics.
                           F32: everything in fp32 */
   float scale;         /* c, finite and > 0; 0 selects 1 / sqrt(head_dim) */
 } normpre_attn_config;

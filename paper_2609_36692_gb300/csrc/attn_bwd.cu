@@ -1,6 +1,6 @@
 // Packed causal attention, backward, bf16 on tcgen05 tensor cores.
 //
-//   P = exp2(c S - log2(e) lse),  dS = P (dP - delta),  S = Q K^T, dP = dO V^T,
+//   P = exp2(log2(e) (scale S - lse)),  dS = P (dP - delta),  S = Q K^T, dP = dO V^T,
 //   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
 //
 // Two kernels: k_attn_dkdv owns 128 keys and walks the queries that see them
@@ -29,8 +29,11 @@
 // second set of accumulators, so that an item's start and end overlap its
 // neighbours.
 //
-// Reductions to bf16: P and dS once each (MMA operands, cut with kUnbias), the
-// gradients once.
+// scale S - lse is one FMA, rounded once and where it matters small: scaled by
+// log2(e) beforehand, scale S and lse would each carry a rounding of their own
+// size into the exponent.
+//
+// Roundings to bf16: P and dS once each (MMA operands), the gradients once.
 //
 // What bounds it: the products.  16384 tokens, 16 / 8 heads of 128: 2.38 ms
 // alone, 2.52 ms in a loop, where the seven products run at 1530 TFLOP/s and the
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* own = smem;                                // [kSets] K, V
   uint8_t* ring = own + 2 * kSets * kTileBytes;       // Q, dO, Q, dO ..
-  float* stat = reinterpret_cast<float*>(ring + kSlots * kTileBytes);   // [2][log2(1.0028) - log2(e) lse, delta][128]
+  float* stat = reinterpret_cast<float*>(ring + kSlots * kTileBytes);   // [2][-lse, delta][128]
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(stat + 512);
   static_assert(sizeof(Bars<kSlots>) <= 512, "barriers");
   ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
@@ -393,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int j = i + 32 * e + lane;
-            ls[e] = j < it.len ? fmaf(a.lse[base + j], -kLog2e, kUnbias) : -INFINITY;   // past the end: P = 0
+            ls[e] = j < it.len ? -a.lse[base + j] : -INFINITY;   // past the end: P = 0
             de[e] = j < it.len ? a.delta[base + j] : 0.f;
           }
           const int s0 = slot, s1 = s0 + 1 == kSlots ? 0 : s0 + 1;
@@ -417,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     const int part = warp >> 2, row = 32 * (warp & 3) + lane;    // columns 32 part .., row of the tile
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t mS = cS + lanes + 32 * part, mP = cP + lanes + 32 * part;
-    const uint64_t c2 = tc::pack2(a.scale_log2, a.scale_log2);
+    const uint64_t c2 = tc::pack2(a.scale, a.scale), log2e2 = tc::pack2(kLog2e, kLog2e);
     uint32_t phase = 0;
     Turn<2> st;
     for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
@@ -435,8 +438,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         for (int e = 0; e < 32; e += 4) {
           const ulonglong2 l2 = *reinterpret_cast<const ulonglong2*>(ls + e);
           float y[4];
-          tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, l2.x), y[0], y[1]);
-          tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), c2, l2.y), y[2], y[3]);
+          tc::unpack2(tc::mul2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, l2.x), log2e2), y[0], y[1]);
+          tc::unpack2(tc::mul2(tc::fma2(tc::pack2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), c2, l2.y), log2e2), y[2], y[3]);
 #pragma unroll
           for (int u = 0; u < 4; ++u) p[e + u] = tc::exp2_fast(y[u]);
         }
@@ -446,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
             if (32 * part + e < row) p[e] = 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) pk[e] = cut_bf16x2(p[2 * e], p[2 * e + 1]);
+        for (int e = 0; e < 16; ++e) pk[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
         tc::tmem_put16(mS, pk);
         tc::tmem_st_drain();
         w.arrive(&b->p_ready);
@@ -460,8 +463,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
           const float d4[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
           for (int u = 0; u < 4; u += 2)
-            pk[(e + u) / 2] = cut_bf16x2(p[e + u] * (__uint_as_float(x[e + u]) - d4[u]),
-                                         p[e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]));
+            pk[(e + u) / 2] = pack_bf16x2(p[e + u] * (__uint_as_float(x[e + u]) - d4[u]),
+                                          p[e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]));
         }
         if (diag) {   // 0 * NaN in an unseen place
 #pragma unroll
@@ -610,14 +613,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     // ---------------- softmax ----------------
     const int part = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint64_t c2 = tc::pack2(a.scale_log2, a.scale_log2);
+    const uint64_t c2 = tc::pack2(a.scale, a.scale), log2e2 = tc::pack2(kLog2e, kLog2e);
     uint32_t dp_phase = 0;
     for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
       const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk;
       const int rows = it.len - kTile * it.blk;
       const bool in = row < rows;
       const int64_t si = static_cast<int64_t>(it.head) * a.tokens + at + row;
-      const float ls = in ? fmaf(a.lse[si], -kLog2e, kUnbias) : -INFINITY, de = in ? a.delta[si] : 0.f;
+      const float ls = in ? -a.lse[si] : -INFINITY, de = in ? a.delta[si] : 0.f;
       const uint64_t ls2 = tc::pack2(ls, ls);
       for (int j = 0; j <= it.blk; ++j, buf.next()) {
         const uint32_t mS = cS + 128 * buf.i + lanes + 32 * part, mP = cP + lanes + 32 * part;
@@ -630,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
           float y0, y1;
-          tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, ls2), y0, y1);
+          tc::unpack2(tc::mul2(tc::fma2(tc::pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, ls2), log2e2), y0, y1);
           p[e] = tc::exp2_fast(y0);
           p[e + 1] = tc::exp2_fast(y1);
         }
@@ -641,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         w.arrive(&b->dp_free);
 #pragma unroll
         for (int e = 0; e < 32; e += 2)
-          pk[e / 2] = cut_bf16x2(p[e] * (__uint_as_float(x[e]) - de), p[e + 1] * (__uint_as_float(x[e + 1]) - de));
+          pk[e / 2] = pack_bf16x2(p[e] * (__uint_as_float(x[e]) - de), p[e + 1] * (__uint_as_float(x[e + 1]) - de));
         if (j == it.blk) {   // query `row` sees keys .. row
 #pragma unroll
           for (int e = 0; e < 16; ++e) {

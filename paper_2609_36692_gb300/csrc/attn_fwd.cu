@@ -23,12 +23,16 @@
 // 2^8 relative to the row's maximum, which bf16 and the fp32 sums hold as
 // precisely, and the rescale, which has to wait for P V, is rare.
 //
-// Reductions to bf16: P once (the MMA operand, cut with kUnbias; l sums the
-// uncut values) and the output once.
+// S - m' is formed before the scale: near the maximum it is exact however large
+// the scores, while c S - c m' would carry the rounding of c m' (0.002 in the
+// exponent at scores of 3e4).  It costs a packed addition beside the product.
+//
+// Roundings to bf16: P once (the MMA operand; l sums the unrounded values) and
+// the output once.
 //
 // What bounds it: a step (two tiles x 128 keys) costs the tensor cores 2 x 2 x
 // 512 cycles and a scheduler's two softmax warps 2 x 128 exponentials of 4
-// cycles beside their scaling, sums and cuts, about as much; the two stay within
+// cycles beside their scaling, sums and conversions, about as much; the two stay within
 // a fifth of each other.  Under load the clock falls with the power limit.
 // 16384 tokens, 16 / 8 heads of 128: 0.612 ms alone (1800 TFLOP/s), 0.70 ms in a
 // loop; 8192 tokens in seven sequences 0.089 ms (1100 TFLOP/s: the CTAs' last
@@ -355,16 +359,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
         auto top = [&]() { return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])); };
         // the quarter's exponentials with the running maximum, as P and into the sum
         auto exps = [&](uint32_t* to) {
-          const float mc = fmaf(-m, c, kUnbias);
-          const uint64_t mc2 = tc::pack2(mc, mc);
+          const uint64_t m2 = tc::pack2(-m, -m);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float lo, hi;
-            tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), c2, mc2), lo, hi);
+            tc::unpack2(tc::mul2(tc::add2(tc::pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), m2), c2), lo, hi);
             lo = tc::exp2_fast(lo);
             hi = tc::exp2_fast(hi);
             sum[i & 1] = tc::add2(sum[i & 1], tc::pack2(lo, hi));
-            to[i] = cut_bf16x2(lo, hi);
+            to[i] = pack_bf16x2(lo, hi);
           }
         };
         auto release = [&](int part) {
@@ -438,7 +441,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
         ++pv;
       }
       if (!ok || !wait(&b->pv_done[s], (pv - 1) & 1u)) break;
-      l *= kUnbiasScale;
       const float inv = 1.f / l;
       const int rows = it.len - kTile * blk;              // of the tile
       const int64_t at = it.start + static_cast<int64_t>(kTile) * blk;
@@ -456,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       if (lane == 0) tc::mbar_arrive(&b->o_empty[s][acc]);
       if (kAcc == 2) acc ^= 1;
       if (row < rows)
-        f.a.lse[static_cast<int64_t>(head) * f.a.tokens + at + row] = (m * c + log2f(l)) * 0.6931471805599453f;
+        f.a.lse[static_cast<int64_t>(head) * f.a.tokens + at + row] = fmaf(m, f.a.scale, log2f(l) * 0.6931471805599453f);
     }
   }
   if (!ok && lane == 0) {

@@ -17,18 +17,6 @@ constexpr int kTile = 128;                 // rows and keys of a tile
 constexpr int kChunk = kTile * 128;        // bytes of 128 rows of 64 bf16: one TMA box, 128-byte swizzle
 constexpr float kLog2e = 1.4426950408889634f;
 
-// P and dS are cut to bf16, not rounded: the byte permutation that cuts two
-// values runs beside the exponentials, while a rounding conversion takes their
-// pipe.  A cut loses between nothing and 2^-7 of a number's leading bit, 0.0028
-// (2^-8 / (2 ln 2)) of the number on average; P is therefore formed 1.0028
-// times as large, which leaves the cut values right on average (their spread
-// is that of rounding); sums of uncut values are divided by it.
-constexpr float kUnbias = 0.0040596f;           // log2(1.0028179)
-constexpr float kUnbiasScale = 0.9971900f;      // 1 / 1.0028179
-__device__ __forceinline__ uint32_t cut_bf16x2(float lo, float hi) {
-  return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
-}
-
 // The r-th item of this CTA, -1 past its last.  With a plan's lists: ids from
 // walk[gridDim.x + 1 + walk[c]] up to walk[gridDim.x + 1 + walk[c + 1]].  Without
 // (many items per CTA): the items in falling order of cost, back and forth over

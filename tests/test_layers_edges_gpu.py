@@ -1,10 +1,11 @@
 """The layer operators at the ends of their ranges: steps near the largest fp32
-number in the weight gradient.
+number in the weight gradient, large scores in attention.
 
 References are in 64 bits; each test derives its tolerance.
 """
 import pytest
 
+from test_attention_gpu import TOL, err, plan_for, reference
 from test_checkpoint_gpu import dt, rel, sample
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +34,53 @@ def test_weight_gradient_of_large_steps(shape, dy_dtype):
     assert L.ckpt_status() == 0
     for k in range(0, f, 32):
         assert rel(dw[:, k:k + 32], ref[:, k:k + 32]) <= 1e-5, k
+
+
+def exact_scores(seed, n, h, hk, dtype, base, spread=0):
+    """q, k, v, dout of n rows with head_dim 64 whose scores are computed
+    without rounding: whole numbers, and a scale of 1/8.  The scores are `base`
+    (a multiple of 504), plus up to `spread` eighths."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    q, k = torch.full((n, h, 64), 64.0, device="cuda"), torch.full((n, hk, 64), float(base // 504), device="cuda")
+    whole = lambda m, *shape: torch.randint(-m, m + 1, shape, generator=g, device="cuda").float()  # noqa: E731
+    q[..., 0] = whole(2, n, h) if spread else 0.0
+    k[..., 0] = whole(max(1, spread // 2), n, hk)
+    v, do = (torch.randn(n, x, 64, generator=g, device="cuda") for x in (hk, h))
+    return [x.to(dt(dtype)) for x in (q, k, v, do)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("base", [504 * 2, 504 * 64, 504 * 124, -504 * 124], ids=str)
+def test_one_key_however_large_the_score(base, dtype):
+    """p = 1 and the log-sum is the score itself, a number that fp32 holds: the
+    output is the value and dv the output's gradient, to the bit."""
+    import torch
+    n, h, hk = 200, 2, 2
+    q, k, v, do = exact_scores(1, n, h, hk, dtype, base)
+    plan = plan_for(h, hk, 64, n, [1] * n, dtype)
+    out, lse = plan.forward(q, k, v)
+    dv = plan.backward(q, k, v, out, lse, do)[2]
+    assert plan.status() == 0
+    assert torch.equal(lse, torch.full_like(lse, float(base)))
+    assert torch.equal(out, v) and torch.equal(dv, do)
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("base", [504 * 64, 504 * 124], ids=str)
+def test_many_keys_of_large_scores(base, dtype):
+    """Scores around 32256 and 62496 that differ by up to 4.  Tolerances of
+    ordinary scores; the fp32 log-sum adds half of its last place, 2^-10 or 2^-9,
+    to the exponent of the backward pass."""
+    n, h, hk, lengths = 700, 4, 2, [300, 1, 399]
+    q, k, v, do = exact_scores(2, n, h, hk, dtype, base, 16)
+    plan = plan_for(h, hk, 64, n, lengths, dtype)
+    ref = reference(q, k, v, do, lengths)
+    out, lse = plan.forward(q, k, v)
+    grads = plan.backward(q, k, v, out, lse, do)
+    assert plan.status() == 0
+    half = 2.0 ** (-10 if base < 2 ** 15 else -9)
+    assert float((lse.double() - ref[1]).abs().max()) <= 1.01 * half
+    assert err(out, ref[0]) <= TOL[dtype, "fwd"]
+    for x, r, m in zip(grads, ref[2:5], ref[5]):
+        assert err(x, r, m) <= TOL[dtype, "bwd"] + half
