@@ -9,6 +9,8 @@
 // (dK, dV summed over the query heads of the group and the later query blocks),
 // half 64 queries (dQ): each output is summed by one CTA in a fixed order, at
 // the price of forming the scores twice.
+// Differences of scores are taken before the factor log2(e) of the exponentials:
+// that factor's rounding then is one of the difference, not of the score.
 //
 // A thread holds a 4 x 4 piece of a 64 x 64 score tile (rows ty + 16 r, columns
 // tx + 16 c) and a 4 x (D / 16) piece of a 64 x D product; tiles lie in shared
@@ -31,6 +33,7 @@ namespace {
 constexpr int kB = 64;              // rows and keys of a tile
 constexpr int kThreads = 256;
 constexpr int kPs = kB + 4;         // row stride of a score tile
+constexpr float kLog2e = 1.4426950408889634f;
 
 template <int DP> __host__ __device__ constexpr int ld() { return DP + 4; }
 
@@ -220,17 +223,17 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
       float mx = -INFINITY;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        s[r][c] = jb == diag && tx + 16 * c > ty + 16 * r ? -INFINITY : s[r][c] * a.scale_log2;
+        s[r][c] = jb == diag && tx + 16 * c > ty + 16 * r ? -INFINITY : s[r][c] * a.scale;
         mx = fmaxf(mx, s[r][c]);
       }
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
       mx = fmaxf(mx, m[r]);
-      const float keep = exp2f(m[r] - mx);
+      const float keep = exp2f((m[r] - mx) * kLog2e);
       float sum = 0.f;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const float p = jb == diag && tx + 16 * c > ty + 16 * r ? 0.f : exp2f(s[r][c] - mx);
+        const float p = jb == diag && tx + 16 * c > ty + 16 * r ? 0.f : exp2f((s[r][c] - mx) * kLog2e);
         P[(ty + 16 * r) * kPs + tx + 16 * c] = p;
         sum += p;
       }
@@ -252,7 +255,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     inv[r] = 1.f / l[r];
-    if (tx == 0 && ty + 16 * r < rows) lse[ty + 16 * r] = (m[r] + log2f(l[r])) * 0.6931471805599453f;
+    if (tx == 0 && ty + 16 * r < rows) lse[ty + 16 * r] = fmaf(log2f(l[r]), 0.6931471805599453f, m[r]);
   }
   store_tile<T, DP>(a.o, row0, rows, head, a.dim, ty, tx, acc, inv);
 }
@@ -270,11 +273,11 @@ __device__ __forceinline__ void grad_scores(const AttnArgs& a, const float* Q, c
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int i = i0 + ty + 16 * r;
-    const float ls = lse[ty + 16 * r] * 1.4426950408889634f, de = delta[ty + 16 * r];
+    const float ls = lse[ty + 16 * r], de = delta[ty + 16 * r];
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const bool seen = i < len && j0 + tx + 16 * c <= i;
-      p[r][c] = seen ? exp2f(fmaf(t[r][c], a.scale_log2, -ls)) : 0.f;
+      p[r][c] = seen ? exp2f(fmaf(t[r][c], a.scale, -ls) * kLog2e) : 0.f;
       s[r][c] = seen ? p[r][c] * (s[r][c] - de) : 0.f;
     }
   }

@@ -50,7 +50,7 @@ def exact_scores(seed, n, h, hk, dtype, base, spread=0):
     return [x.to(dt(dtype)) for x in (q, k, v, do)]
 
 
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("base", [504 * 2, 504 * 64, 504 * 124, -504 * 124], ids=str)
 def test_one_key_however_large_the_score(base, dtype):
     """p = 1 and the log-sum is the score itself, a number that fp32 holds: the
@@ -66,7 +66,7 @@ def test_one_key_however_large_the_score(base, dtype):
     assert torch.equal(out, v) and torch.equal(dv, do)
 
 
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("base", [504 * 64, 504 * 124], ids=str)
 def test_many_keys_of_large_scores(base, dtype):
     """Scores around 32256 and 62496 that differ by up to 4.  Tolerances of
