@@ -204,7 +204,18 @@ struct SwigluArgs {
   uint32_t *gate_steps, *up_steps;
 };
 
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+// 1 / (1 + exp(-x)).  fp32: to a few units in the last place, from exp(-|x|),
+// which cannot overflow.  bf16: the hardware's exponential, whose relative error
+// (1e-5 at |x| = 88) is far below the rounding that follows; the exact one makes
+// the kernels 12 % slower (16384 x 6144, both passes: 301 us, not 268).
+template <typename T> __device__ __forceinline__ float sigmoid(float x) {
+  if constexpr (sizeof(T) == 4) {
+    const float e = expf(-fabsf(x));
+    return (x < 0.f ? e : 1.f) / (1.f + e);
+  } else {
+    return __fdividef(1.f, 1.f + __expf(-x));
+  }
+}
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_ckpt_swiglu(const __grid_constant__ SwigluArgs a) {
@@ -232,7 +243,7 @@ __global__ void __launch_bounds__(kThreads) k_ckpt_swiglu(const __grid_constant_
       a.up_steps[p[i].word] = uw;
     }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) u[e] *= g[e] * sigmoid(g[e]);
+    for (int e = 0; e < 16; ++e) u[e] *= g[e] * sigmoid<T>(g[e]);
     store16<VEC>(static_cast<T*>(a.h) + p[i].row * a.h_ld + p[i].feature, p[i].n, u);
   }
 }
@@ -257,8 +268,9 @@ __global__ void __launch_bounds__(kThreads) k_ckpt_swiglu_bwd(const __grid_const
     ur[i].values(u);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float s = sigmoid(g[e]);
-      u[e] *= d[e] * s * fmaf(g[e], 1.f - s, 1.f);
+      const float s = sigmoid<T>(g[e]);
+      // 1 - s, in fp32 without its cancellation
+      u[e] *= d[e] * s * fmaf(g[e], sizeof(T) == 4 ? sigmoid<T>(-g[e]) : 1.f - s, 1.f);
       g[e] *= d[e] * s;
     }
     store16<VEC>(static_cast<T*>(a.dgate) + p[i].row * a.dgate_ld + p[i].feature, p[i].n, u);

@@ -1,5 +1,5 @@
 """The layer operators at the ends of their ranges: steps near the largest fp32
-number in the weight gradient, large scores in attention.
+number in the weight gradient, large scores in attention, large gates.
 
 References are in 64 bits; each test derives its tolerance.
 """
@@ -84,3 +84,27 @@ def test_many_keys_of_large_scores(base, dtype):
     assert err(out, ref[0]) <= TOL[dtype, "fwd"]
     for x, r, m in zip(grads, ref[2:5], ref[5]):
         assert err(x, r, m) <= TOL[dtype, "bwd"] + half
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_swiglu_element_by_element(dtype):
+    """Gates from -87 (below, exp(gate) leaves fp32's normal numbers) to 100,
+    each element against its own size.  fp32: an exponential of 2 units in the
+    last place, a quotient of 2, and three other roundings of a half, 5.5 *
+    2^-23 = 6.6e-7; the backward pass has two roundings more and is measured
+    against its terms before they cancel.  bf16: one rounding, 2^-8, besides."""
+    import torch
+    from paper_2609_36692_gb300 import layers as L
+    tol = 8e-7 + (2.0 ** -8 if dtype == "bf16" else 0)
+    gate = torch.linspace(-87, 100, 64 * 96, device="cuda").view(64, 96).to(dt(dtype))
+    up, dh = (sample(i, 64, 96, dtype) for i in (1, 2))
+    h, cg, cu = L.ckpt_swiglu(gate, up)
+    g, u = gate.double(), up.double()
+    ref = g * torch.sigmoid(g) * u
+    assert bool(((h.double() - ref).abs() <= tol * ref.abs() + 2.0 ** -126).all())
+    g, u, d = cg.restore(torch.float32).double(), cu.restore(torch.float32).double(), dh.double()
+    s = torch.sigmoid(g)
+    dgate, dup = (x.double() for x in L.ckpt_swiglu_backward(cg, cu, dh))
+    assert bool(((dup - d * g * s).abs() <= tol * (d * g * s).abs() + 2.0 ** -126).all())
+    terms = (d * u * s).abs() * (1 + g.abs() * (1 - s))
+    assert bool(((dgate - d * u * s * (1 + g * (1 - s))).abs() <= tol * terms + 2.0 ** -126).all())
