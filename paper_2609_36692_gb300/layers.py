@@ -5,7 +5,8 @@ Like ``optim``, this only checks tensors and hands their pointers and the
 current CUDA stream to the C ABI (``normpre_attn_*``, ``normpre_ckpt_*`` in
 ``include/normpre.h``, which has the definitions); all arithmetic runs in the
 library's kernels.  ``PackedAttention.__call__``, ``linear`` and ``swiglu`` are
-the differentiable forms.
+the differentiable forms; they have first derivatives only, and asking for
+another one raises.
 """
 from __future__ import annotations
 
@@ -13,6 +14,7 @@ import ctypes
 from typing import Optional, Sequence, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import normpre as C
 
@@ -181,6 +183,7 @@ class _Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse = ctx.saved_tensors
         # autograd may hand over an expanded gradient
@@ -321,6 +324,7 @@ class _Linear(torch.autograd.Function):
         return x @ weight.to(x.dtype).t()
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         weight, = ctx.saved_tensors
         dy = _rows(dy)
@@ -345,6 +349,7 @@ class _SwiGLU(torch.autograd.Function):
         return h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh):
         return ckpt_swiglu_backward(ctx.gate, ctx.up, _rows(dh))
 

@@ -1,5 +1,6 @@
 """The layer operators at the ends of their ranges: steps near the largest fp32
-number in the weight gradient, large scores in attention, large gates.
+number in the weight gradient, large scores in attention, large gates; and what
+the differentiable forms refuse.
 
 References are in 64 bits; each test derives its tolerance.
 """
@@ -108,3 +109,18 @@ def test_swiglu_element_by_element(dtype):
     assert bool(((dup - d * g * s).abs() <= tol * (d * g * s).abs() + 2.0 ** -126).all())
     terms = (d * u * s).abs() * (1 + g.abs() * (1 - s))
     assert bool(((dgate - d * u * s * (1 + g * (1 - s))).abs() <= tol * terms + 2.0 ** -126).all())
+
+
+def test_second_derivatives_are_refused():
+    """The backward passes fill their results outside autograd: a second
+    derivative would miss their terms without a word."""
+    import torch
+    from paper_2609_36692_gb300 import layers as L
+    leaf = lambda *shape: torch.randn(*shape, device="cuda").to(torch.bfloat16).requires_grad_()  # noqa: E731
+    q, k, v = leaf(40, 2, 64), leaf(40, 1, 64), leaf(40, 1, 64)
+    plan = plan_for(2, 1, 64, 40, [40], "bf16")
+    for f, leaves in ((plan, (q, k, v)), (L.linear, (leaf(40, 64), leaf(32, 64))), (L.swiglu, (leaf(40, 64), leaf(40, 64)))):
+        grads = torch.autograd.grad((f(*leaves) ** 2).sum(), leaves, create_graph=True)
+        for g in grads:
+            with pytest.raises(RuntimeError, match="once_differentiable"):
+                (g ** 2).sum().backward(retain_graph=True)
