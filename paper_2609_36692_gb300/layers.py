@@ -74,15 +74,17 @@ class PackedAttention:
         code = _CODES.get(dtype)
         if code is None:
             raise TypeError("unsupported dtype %s (float32 or bfloat16)" % dtype)
-        self.plan = None
+        self.plan, self.lengths = None, ()
         cfg = C.normpre_attn_config(n_heads, n_kv_heads, head_dim, max_seqs, max_tokens, code, scale)
         with torch.cuda.device(self.device):
             self.plan = C.normpre_attn_init(cfg)
 
     def set_lengths(self, lengths: Sequence[int], stream=None) -> None:
+        lengths = tuple(int(n) for n in lengths)
         with torch.cuda.device(self.device):
             s = stream if stream is not None else torch.cuda.current_stream()
             C.normpre_attn_set_lengths(self.plan, lengths, s.cuda_stream)
+        self.lengths = lengths
 
     def _check(self, x: torch.Tensor, name: str, tokens: int, heads: int):
         if x.device != self.device:
@@ -144,8 +146,8 @@ class PackedAttention:
         return dq, dk, dv
 
     def __call__(self, q, k, v) -> torch.Tensor:
-        """Differentiable attention.  The lengths must not change between a
-        call and its backward pass."""
+        """Differentiable attention.  A backward pass runs with the plan's
+        lengths: they must be its call's (else it raises)."""
         return _Attention.apply(self, q, k, v)
 
     def status(self, stream=None, raise_on_error: bool = True) -> int:
@@ -178,7 +180,7 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, plan, q, k, v):
         out, lse = plan.forward(q, k, v)
-        ctx.plan = plan
+        ctx.plan, ctx.lengths = plan, plan.lengths
         ctx.save_for_backward(q, k, v, out, lse)
         return out
 
@@ -186,6 +188,9 @@ class _Attention(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse = ctx.saved_tensors
+        if ctx.lengths != ctx.plan.lengths:
+            raise RuntimeError("the plan's lengths changed between an attention call and its backward pass; give "
+                               "set_lengths the call's lengths again, or use a plan for each batch in flight")
         # autograd may hand over an expanded gradient
         return (None, *ctx.plan.backward(q, k, v, out, lse, _aligned(dout)))
 

@@ -6,7 +6,7 @@ References are in 64 bits; each test derives its tolerance.
 """
 import pytest
 
-from test_attention_gpu import TOL, err, plan_for, reference
+from test_attention_gpu import TOL, err, make, plan_for, reference
 from test_checkpoint_gpu import dt, rel, sample
 
 pytestmark = pytest.mark.gpu
@@ -124,3 +124,18 @@ def test_second_derivatives_are_refused():
         for g in grads:
             with pytest.raises(RuntimeError, match="once_differentiable"):
                 (g ** 2).sum().backward(retain_graph=True)
+
+
+def test_backward_pass_of_other_lengths_is_refused():
+    import torch
+    q, k, v, do = make(3, 64, 2, 1, 64, "bf16")
+    plan = plan_for(2, 1, 64, 64, [40, 24], "bf16")
+    want = plan.backward(q, k, v, *plan.forward(q, k, v), do)
+    leaves = [x.clone().requires_grad_() for x in (q, k, v)]
+    out = plan(*leaves)
+    plan.set_lengths([24, 40])
+    with pytest.raises(RuntimeError, match="lengths changed"):
+        torch.autograd.grad(out, leaves, do, retain_graph=True)
+    plan.set_lengths(torch.tensor([40, 24]))           # the call's lengths again
+    for x, y in zip(torch.autograd.grad(out, leaves, do), want):
+        assert torch.equal(x, y)
