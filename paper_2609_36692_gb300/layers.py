@@ -43,11 +43,24 @@ def _on(device: torch.device, f, *args) -> None:
 
 
 def _used_on(stream, *tensors) -> None:
-    # tensors allocated here belong to the current stream's allocator pool;
-    # tell it about another stream that works on them
+    # the memory of a tensor that is freed while another stream than its own
+    # still works on it must wait for that stream before it is given out again
     if stream is not None:
         for t in tensors:
-            t.record_stream(stream)
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _empty(shape, dtype, device: torch.device, stream) -> torch.Tensor:
+    """An output that work on `stream` (None: the current one) writes.  It comes
+    from that stream's own pool: memory of the current stream's may still be
+    read or written by what was queued there before."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        x = torch.empty(shape, dtype=dtype, device=device)
+    x.record_stream(torch.cuda.current_stream(device))
+    return x
 
 
 # ---------------------------------------------------------------------------
@@ -64,6 +77,10 @@ class PackedAttention:
     v [tokens, n_kv_heads, head_dim]: any views whose last dimension is
     contiguous and whose strides are multiples of 16 bytes.  Rows past the last
     sequence give zero outputs and gradients.
+
+    With `stream`, a call's work runs there instead of on the current stream;
+    the caller orders it after what wrote its inputs and lengths, and before
+    what reads its outputs.
     """
 
     def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, max_tokens: int, max_seqs: int,
@@ -105,9 +122,7 @@ class PackedAttention:
         return lse.data_ptr()
 
     def _new(self, tokens: int, heads: int, stream):
-        x = torch.empty((tokens, heads, self.head_dim), dtype=self.dtype, device=self.device)
-        _used_on(stream, x)
-        return x
+        return _empty((tokens, heads, self.head_dim), self.dtype, self.device, stream)
 
     def forward(self, q, k, v, out=None, lse=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """(out, lse): [tokens, n_heads, head_dim] and the fp32 log-sums
@@ -115,11 +130,11 @@ class PackedAttention:
         t, h, hk = q.shape[0], self.n_heads, self.n_kv_heads
         check = self._check
         args = (*check(q, "q", t, h), *check(k, "k", t, hk), *check(v, "v", t, hk))
+        _used_on(stream, q, k, v, out, lse)
         if out is None:
             out = self._new(t, h, stream)
         if lse is None:
-            lse = torch.empty((h, t), dtype=torch.float32, device=self.device)
-            _used_on(stream, lse)
+            lse = _empty((h, t), torch.float32, self.device, stream)
         heads = (ctypes.c_int64 * 12)(*args, *check(out, "out", t, h))
         at = ctypes.addressof(heads)
         C.normpre_attn_forward(self.plan, t, at, at + 24, at + 48, at + 72, self._lse(lse, t),
@@ -132,6 +147,7 @@ class PackedAttention:
         check = self._check
         args = (*check(q, "q", t, h), *check(k, "k", t, hk), *check(v, "v", t, hk), *check(out, "out", t, h),
                 *check(dout, "dout", t, h))
+        _used_on(stream, q, k, v, out, lse, dout, dq, dk, dv)
         if dq is None:
             dq = self._new(t, h, stream)
         if dk is None:

@@ -139,3 +139,40 @@ def test_backward_pass_of_other_lengths_is_refused():
     plan.set_lengths(torch.tensor([40, 24]))           # the call's lengths again
     for x, y in zip(torch.autograd.grad(out, leaves, do), want):
         assert torch.equal(x, y)
+
+
+def test_stream_argument():
+    """Work on a stream given by argument: the same bits, and outputs that do
+    not lie where the current stream still has work to do."""
+    import torch
+    n, h, hk = 1024, 2, 1
+    q, k, v, do = make(4, n, h, hk, 64, "bf16")
+    plan = plan_for(h, hk, 64, n, [1000], "bf16")
+    out, lse = plan.forward(q, k, v)
+    grads = plan.backward(q, k, v, out, lse, do)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    def while_memory_is_in_use(shapes, f):
+        held = [torch.full(s, 3.0, dtype=t, device="cuda") for s, t in shapes]
+        torch.cuda._sleep(200_000_000)               # a tenth of a second
+        copies = [x.clone() for x in held]
+        del held                                     # what is still to be copied is free for others
+        got = f()
+        torch.cuda.synchronize()
+        for x in copies:
+            assert bool((x == 3.0).all())
+        return got
+    o2, l2 = while_memory_is_in_use([(out.shape, out.dtype), (lse.shape, lse.dtype)],
+                                    lambda: plan.forward(q, k, v, stream=side))
+    g2 = while_memory_is_in_use([(x.shape, x.dtype) for x in grads],
+                                lambda: plan.backward(q, k, v, out, lse, do, stream=side))
+    assert plan.status(side) == 0
+    for x, y in zip((o2, l2, *g2), (out, lse, *grads)):
+        assert torch.equal(x, y)
+    o3, g3 = torch.empty_like(out), torch.empty_like(grads[0])   # given outputs
+    side.wait_stream(torch.cuda.current_stream())
+    assert plan.forward(q, k, v, out=o3, stream=side)[0] is o3
+    assert plan.backward(q, k, v, out, lse, do, dq=g3, stream=side)[0] is g3
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(o3, out) and torch.equal(g3, grads[0])
