@@ -35,7 +35,6 @@
 // dW, 16 tokens at a time through shared memory, a 4 x 4 piece per thread; any
 // dtype, stride and size.  Bound by the fp32 FMA pipe.
 #include <algorithm>
-#include <atomic>
 
 #include "ckpt.h"
 #include "common.cuh"
@@ -503,18 +502,19 @@ struct ClusterLaunch {
   }
 };
 
-// Clusters of a size that the GPU holds at once (a cluster stays within a GPC,
-// so that some SMs are left over).
+// Clusters of a size that the current device holds at once (a cluster stays
+// within a GPC, so that some SMs are left over).  The kernel is allowed its
+// shared memory there first; a launch of it follows such a question.
 template <typename TW, bool SPLIT>
 cudaError_t clusters_at_once(int cluster, int* fit) {
-  static std::atomic<int> known[9];
-  *fit = known[cluster].load(std::memory_order_relaxed);
-  if (*fit) return cudaSuccess;
-  ClusterLaunch l(cluster, std::max(1, device_sm_count() / cluster), nullptr);
-  cudaError_t e = allow_smem<k_wgrad_tc<TW, SPLIT>>(kTcSmem);
-  if (!e) e = cudaOccupancyMaxActiveClusters(fit, k_wgrad_tc<TW, SPLIT>, &l.cfg);
-  if (!e) known[cluster].store(*fit = std::max(1, *fit), std::memory_order_relaxed);
-  return e;
+  static PerDevice known[9];
+  return known[cluster].get(fit, [cluster](int* n) {
+    ClusterLaunch l(cluster, std::max(1, device_sm_count() / cluster), nullptr);
+    cudaError_t e = allow_smem<k_wgrad_tc<TW, SPLIT>>(kTcSmem);
+    if (!e) e = cudaOccupancyMaxActiveClusters(n, k_wgrad_tc<TW, SPLIT>, &l.cfg);
+    if (!e) *n = std::max(1, *n);
+    return e;
+  });
 }
 
 template <typename TW>

@@ -362,6 +362,30 @@ cudaError_t allow_smem(size_t bytes) {
   return e;
 }
 
+// What a query says about the current device, asked once per device.
+class PerDevice {
+ public:
+  template <typename Query>   // cudaError_t query(int* value), value >= 0
+  cudaError_t get(int* value, Query query) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e) return e;
+    const bool kept = dev >= 0 && dev < kMax;
+    const int seen = kept ? known_[dev].load(std::memory_order_relaxed) : 0;
+    if (seen) {
+      *value = seen - 1;
+      return cudaSuccess;
+    }
+    e = query(value);
+    if (!e && kept) known_[dev].store(*value + 1, std::memory_order_relaxed);
+    return e;
+  }
+
+ private:
+  static constexpr int kMax = 64;
+  std::atomic<int> known_[kMax] = {};   // value + 1; 0: not asked yet
+};
+
 // Device properties cached per process.
 int device_sm_count();
 bool driver_encode_tiled(CUtensorMap* map, CUtensorMapDataType dt, uint32_t rank, void* addr,
