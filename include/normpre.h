@@ -389,6 +389,9 @@ typedef struct normpre_attn_config {
                           accumulation and softmax statistics.
                           F32: everything in fp32 */
   float scale;         /* c, finite and > 0; 0 selects 1 / sqrt(head_dim) */
+  int test_stall;      /* tests only, 0 otherwise.  1: one CTA of the BF16 forward pass issues no copies, so
+                          that its bounded waits give up after about two seconds (TIMEOUT; the context stays
+                          usable) */
 } normpre_attn_config;
 
 /* One [tokens][heads][head_dim] tensor on the device; the last dimension is
@@ -425,7 +428,10 @@ int normpre_attn_set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths
  *   out  written in full.
  *   lse  device fp32 [n_heads][tokens], written in full; natural logarithm.
  * Asynchronous on `stream`; allocates nothing.
- * Errors: ARG, SHAPE, ALIGN, CUDA.
+ * Errors: ARG, SHAPE, ALIGN, CUDA; TIMEOUT: a bounded wait of an earlier
+ * forward or backward pass of the plan gave up, and normpre_attn_sync_status
+ * has not been called since.  (A call does not wait for the ones before it: what
+ * they are still doing shows up in a later call, or in normpre_attn_sync_status.)
  */
 int normpre_attn_forward(normpre_attn* a, int64_t tokens, const normpre_heads* q, const normpre_heads* k,
                          const normpre_heads* v, const normpre_heads* out, float* lse, void* stream);
@@ -435,15 +441,15 @@ int normpre_attn_forward(normpre_attn* a, int64_t tokens, const normpre_heads* q
  * tensors and dout.  Sums run in a fixed order: the same inputs give the same
  * bits.  The plan's workspace is used, so two backward passes of one plan must
  * not run concurrently.  Asynchronous on `stream`; allocates nothing.
- * Errors: ARG, SHAPE, ALIGN, CUDA.
+ * Errors: ARG, SHAPE, ALIGN, CUDA, TIMEOUT (as the forward pass).
  */
 int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* q, const normpre_heads* k,
                           const normpre_heads* v, const normpre_heads* out, const float* lse,
                           const normpre_heads* dout, const normpre_heads* dq, const normpre_heads* dk,
                           const normpre_heads* dv, void* stream);
 
-/* Synchronizes `stream`, then reports and clears the plan's device flag:
- * TIMEOUT if a bounded wait gave up since the last call, else OK. */
+/* Synchronizes `stream`, then reports and clears the plan's flag: TIMEOUT if a
+ * bounded wait gave up since the last call, else OK. */
 int normpre_attn_sync_status(normpre_attn* a, void* stream);
 
 /* Synchronizes the plan's device and releases the plan.  NULL is ignored. */
@@ -489,7 +495,9 @@ int normpre_ckpt_restore(int64_t tokens, int64_t features, const void* codes, co
  * rows on 16-byte boundaries runs on the tensor cores; fp32 dY, and rows off
  * those boundaries, on an fp32 kernel.  The sums' order is fixed.
  * Out_features in [1, 2^20].  A device-side timeout is reported by
- * normpre_ckpt_sync_status.
+ * normpre_ckpt_sync_status; until then it makes the device's next weight
+ * gradients fail with TIMEOUT.  The process's first call allocates a few
+ * pinned words for that.
  */
 int normpre_ckpt_wgrad(int64_t tokens, int64_t out_features, int64_t features, const void* dy, int dy_dtype,
                        int64_t dy_ld, const void* codes, const void* steps, void* dw, int dw_dtype, int64_t dw_ld,

@@ -32,7 +32,7 @@ struct normpre_attn {
   cudaEvent_t copied = nullptr;    // the last copy out of `staging`
   int64_t walk_at[3] = {-1, -1, -1};   // byte offsets of the walks, -1: none
   float* delta = nullptr;          // [n_heads][max_tokens]
-  int* flags = nullptr;
+  int* flags = nullptr;            // pinned: set by kernels, read here between calls
 };
 
 namespace {
@@ -59,7 +59,7 @@ void release(normpre_attn* a) {
   if (a->staging) cudaFreeHost(a->staging);
   if (a->copied) cudaEventDestroy(a->copied);
   cudaFree(a->delta);
-  cudaFree(a->flags);
+  if (a->flags) cudaFreeHost(a->flags);
   delete a;
 }
 struct Release {
@@ -110,10 +110,16 @@ AttnArgs base_args(const normpre_attn* a, int64_t tokens) {
   g.scale_log2 = a->cfg.scale * 1.4426950408889634f;
   g.delta = a->delta;
   g.flags = a->flags;
+  g.test_stall = a->cfg.test_stall;
   return g;
 }
 
-int check_tokens(const normpre_attn* a, int64_t tokens) {
+int flags_of(const normpre_attn* a) { return *static_cast<const volatile int*>(a->flags); }
+
+int check_call(const normpre_attn* a, int64_t tokens) {
+  if (flags_of(a) & kFlagTimeout)
+    return fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait of an earlier call of this plan gave up: what that call wrote "
+                                     "has no meaning (normpre_attn_sync_status clears this)");
   if (tokens < a->total || tokens > a->cfg.max_tokens)
     return fail(NORMPRE_ERR_SHAPE, "tokens must be between the sum of the lengths and max_tokens");
   return NORMPRE_OK;
@@ -218,6 +224,7 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out) {
   if (cfg->max_tokens < 1 || cfg->max_tokens > (int64_t(1) << 24) || cfg->max_seqs < 1 || cfg->max_seqs > 65536)
     return fail(NORMPRE_ERR_SHAPE, "max_tokens must be in [1, 2^24] and max_seqs in [1, 65536]");
   if (!std::isfinite(cfg->scale) || cfg->scale < 0.f) return fail(NORMPRE_ERR_ARG, "scale must be finite and >= 0");
+  if (cfg->test_stall != 0 && cfg->test_stall != 1) return fail(NORMPRE_ERR_ARG, "test_stall must be 0 or 1");
   try {
     std::unique_ptr<normpre_attn, Release> a(new normpre_attn());
     a->cfg = *cfg;
@@ -228,9 +235,9 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out) {
     if (!e) e = cudaHostAlloc(&a->staging, list_bytes(a.get()), cudaHostAllocDefault);
     if (!e) e = cudaEventCreateWithFlags(&a->copied, cudaEventDisableTiming);
     if (!e) e = cudaMalloc(&a->delta, static_cast<size_t>(cfg->n_heads) * cfg->max_tokens * sizeof(float));
-    if (!e) e = cudaMalloc(&a->flags, sizeof(int));
-    if (!e) e = cudaMemset(a->flags, 0, sizeof(int));
+    if (!e) e = cudaHostAlloc(&a->flags, sizeof(int), cudaHostAllocDefault);
     if (e) return cuda_fail(e, "normpre_attn_init");
+    *a->flags = 0;
     *out = a.release();
   } catch (const std::bad_alloc&) {
     return fail(NORMPRE_ERR_CUDA, "out of host memory");
@@ -253,7 +260,7 @@ int normpre_attn_set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths
 int normpre_attn_forward(normpre_attn* a, int64_t tokens, const normpre_heads* q, const normpre_heads* k,
                          const normpre_heads* v, const normpre_heads* out, float* lse, void* stream) {
   if (!a) return fail(NORMPRE_ERR_ARG, "null plan");
-  int rc = check_tokens(a, tokens);
+  int rc = check_call(a, tokens);
   if (rc || !tokens) return rc;
   AttnArgs g = base_args(a, tokens);
   const int h = a->cfg.n_heads, hk = a->cfg.n_kv_heads;
@@ -275,7 +282,7 @@ int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* 
                           const normpre_heads* dout, const normpre_heads* dq, const normpre_heads* dk,
                           const normpre_heads* dv, void* stream) {
   if (!a) return fail(NORMPRE_ERR_ARG, "null plan");
-  int rc = check_tokens(a, tokens);
+  int rc = check_call(a, tokens);
   if (rc || !tokens) return rc;
   AttnArgs g = base_args(a, tokens);
   const int h = a->cfg.n_heads, hk = a->cfg.n_kv_heads;
@@ -297,11 +304,10 @@ int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* 
 int normpre_attn_sync_status(normpre_attn* a, void* stream) {
   if (!a) return fail(NORMPRE_ERR_ARG, "null plan");
   DeviceGuard device_guard(a->device);
-  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
-  int flags = 0;
-  if (!e) e = cudaMemcpy(&flags, a->flags, sizeof(int), cudaMemcpyDeviceToHost);
-  if (!e && flags) e = cudaMemset(a->flags, 0, sizeof(int));
+  const cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   if (e) return cuda_fail(e, "normpre_attn_sync_status");
+  const int flags = flags_of(a);
+  if (flags) *static_cast<volatile int*>(a->flags) = 0;
   return flags & kFlagTimeout ? fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait gave up") : NORMPRE_OK;
 }
 

@@ -40,7 +40,8 @@ struct AttnArgs {
   int heads, kv_heads, group, dim;
   float scale;               // c
   float scale_log2;          // c log2(e): exp(c x) = exp2(scale_log2 x)
-  int* flags;
+  int* flags;                // pinned host memory
+  int test_stall;
 };
 
 // The forward kernel's two query tiles are two heads of a group; otherwise two

@@ -200,7 +200,7 @@ __device__ __forceinline__ void finish(const Warp<kSlots>& w, int warp, int* fla
   Bars<kSlots>* b = w.b;
   if (!w.ok && w.lane == 0) {
     *static_cast<volatile int*>(&b->abort) = 1;
-    raise_flag(flags, kFlagTimeout);
+    raise_host_flag(flags, kFlagTimeout);
   }
   __syncthreads();
   if (threadIdx.x == 0 && *static_cast<volatile int*>(&b->abort)) {

@@ -169,6 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       if (tc::elect_one()) {
         int slot = 0;
         uint32_t phase = 0, q_phase[2] = {0, 0};
+        const bool stall = f.a.test_stall && blockIdx.x == 0;   // nothing is loaded: the others' waits run out
         auto load = [&](const CUtensorMap* map, int64_t row, int head, bool tail) {
           ok = ok && tc::mbar_wait(&b->empty[slot], phase ^ 1u, &b->abort);
           if (!ok) return;
@@ -179,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           load_rows(ring + slot * kTileBytes, map, bar, row, head, kChunks);
           if (++slot == kSlots) { slot = 0; phase ^= 1u; }
         };
-        for (int64_t r = 0; ok && get_item(f, items, r, it); ++r) {
+        for (int64_t r = 0; ok && !stall && get_item(f, items, r, it); ++r) {
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             const int blk = s ? it.blk1 : it.blk0;
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
   }
   if (!ok && lane == 0) {
     *static_cast<volatile int*>(&b->abort) = 1;
-    raise_flag(f.a.flags, kFlagTimeout);
+    raise_host_flag(f.a.flags, kFlagTimeout);
   }
 
   __syncthreads();

@@ -10,6 +10,7 @@
 // gated activation and its gradient 0.268 ms (6.1 TB/s; a copy runs at 6.8).
 // Small calls are bound by the launch.
 #include <atomic>
+#include <cstring>
 #include <string>
 
 #include "../../include/normpre.h"
@@ -278,25 +279,35 @@ __global__ void __launch_bounds__(kThreads) k_ckpt_swiglu_bwd(const __grid_const
   }
 }
 
-__device__ int d_ckpt_flags;
+// A word of flags per device in pinned memory: kernels set it, the entry points
+// read it.  The first call of a process that needs one allocates them (also
+// within a stream capture, where an allocation otherwise counts as unsafe).
+constexpr int kMaxDevices = 64;
+std::atomic<int*> g_flags{nullptr};
 
-// The current device's flag word; its address is looked up once per device.
 cudaError_t ckpt_flags(int** out) {
-  constexpr int kMaxDevices = 64;
-  static std::atomic<int*> known[kMaxDevices];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e) return e;
-  int* p = dev < kMaxDevices ? known[dev].load(std::memory_order_acquire) : nullptr;
+  if (dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  int* p = g_flags.load(std::memory_order_acquire);
   if (!p) {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    if ((e = cudaThreadExchangeStreamCaptureMode(&mode))) return e;
     void* v = nullptr;
-    if ((e = cudaGetSymbolAddress(&v, d_ckpt_flags))) return e;
-    p = static_cast<int*>(v);
-    if (dev < kMaxDevices) known[dev].store(p, std::memory_order_release);
+    e = cudaHostAlloc(&v, kMaxDevices * sizeof(int), cudaHostAllocPortable);
+    if (!e) {
+      std::memset(v, 0, kMaxDevices * sizeof(int));
+      if (g_flags.compare_exchange_strong(p, static_cast<int*>(v), std::memory_order_acq_rel)) p = static_cast<int*>(v);
+      else cudaFreeHost(v);   // another thread was first: p is its words
+    }
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (e) return e;
   }
-  *out = p;
+  *out = p + dev;
   return cudaSuccess;
 }
+int flags_now(const int* p) { return *static_cast<const volatile int*>(p); }
 
 int fail(int code, const std::string& msg) {
   set_thread_error(msg);
@@ -432,6 +443,9 @@ int normpre_ckpt_wgrad(int64_t tokens, int64_t out_features, int64_t features, c
   a.k = static_cast<int>(features);
   a.accumulate = accumulate;
   cudaError_t e = ckpt_flags(&a.flags);
+  if (!e && (flags_now(a.flags) & kFlagTimeout))
+    return fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait of an earlier weight gradient gave up: what that call wrote has "
+                                     "no meaning (normpre_ckpt_sync_status clears this)");
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   std::string err;
   if (!e) e = tokens && dy_dtype == NORMPRE_BF16 && vec_rows(dy_ld, dy_dtype)
@@ -498,13 +512,12 @@ int normpre_ckpt_swiglu_backward(int64_t tokens, int64_t features, int dtype, co
 }
 
 int normpre_ckpt_sync_status(void* stream) {
-  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   int* flags = nullptr;
-  int v = 0;
+  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   if (!e) e = ckpt_flags(&flags);
-  if (!e) e = cudaMemcpy(&v, flags, sizeof(int), cudaMemcpyDeviceToHost);
-  if (!e && v) e = cudaMemset(flags, 0, sizeof(int));
   if (e) return done(e, "normpre_ckpt_sync_status");
+  const int v = flags_now(flags);
+  if (v) *static_cast<volatile int*>(flags) = 0;
   return v & kFlagTimeout ? fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait gave up") : NORMPRE_OK;
 }
 

@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   }
   if (!ok && lane == 0) {
     *static_cast<volatile int*>(&b->abort) = 1;
-    raise_flag(a.flags, kFlagTimeout);
+    raise_host_flag(a.flags, kFlagTimeout);
   }
   __syncthreads();
   if (threadIdx.x == 0 && *static_cast<volatile int*>(&b->abort)) {

@@ -10,6 +10,8 @@ namespace normpre {
 __device__ __forceinline__ void raise_flag(int* flags, int bit) {
   if (flags) atomicOr(flags, bit);
 }
+// For a word in pinned host memory, which the host reads between calls.
+__device__ __forceinline__ void raise_host_flag(int* flags, int bit) { atomicOr_system(flags, bit); }
 
 typedef __nv_bfloat16 bf16;
 

@@ -167,6 +167,8 @@ class PackedAttention:
         return _Attention.apply(self, q, k, v)
 
     def status(self, stream=None, raise_on_error: bool = True) -> int:
+        """Synchronizes, and reports and clears what the plan's kernels flagged.
+        A flag that is not cleared makes the plan's next call raise."""
         s = stream if stream is not None else torch.cuda.current_stream(self.device)
         return C.normpre_attn_sync_status(self.plan, s.cuda_stream, raise_on_error)
 
@@ -325,7 +327,8 @@ def ckpt_swiglu_backward(gate: Checkpoint, up: Checkpoint, dh: torch.Tensor):
 
 
 def ckpt_status(stream=None, raise_on_error: bool = True) -> int:
-    """Synchronizes and reports the checkpoint kernels' device flag."""
+    """Synchronizes, and reports and clears the checkpoint kernels' flag.  A flag
+    that is not cleared makes the next weight gradient raise."""
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.normpre_ckpt_sync_status(s.cuda_stream, raise_on_error)
 

@@ -60,6 +60,7 @@ class normpre_attn_config(ctypes.Structure):
         ("max_tokens", ctypes.c_int64),
         ("dtype", ctypes.c_int),
         ("scale", ctypes.c_float),
+        ("test_stall", ctypes.c_int),
     ]
 
 

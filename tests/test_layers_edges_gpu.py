@@ -176,3 +176,60 @@ def test_stream_argument():
     assert plan.backward(q, k, v, out, lse, do, dq=g3, stream=side)[0] is g3
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(o3, out) and torch.equal(g3, grads[0])
+
+
+def test_a_wait_that_gave_up_is_reported_by_the_next_call():
+    """With test_stall one CTA loads nothing: its waits give up after two seconds
+    and the kernel ends.  No call of the plan then passes, the differentiable
+    form's neither, until its status has been asked."""
+    import torch
+    from paper_2609_36692_gb300 import normpre as C
+    q, k, v, do = make(6, 500, 2, 1, 64, "bf16")
+    plan = plan_for(2, 1, 64, 500, [300, 200], "bf16")
+    out, lse = plan.forward(q, k, v)
+    plan.close()
+    plan.plan = C.normpre_attn_init(C.normpre_attn_config(2, 1, 64, 2, 500, C.NORMPRE_BF16, 0.0, 1))
+    plan.set_lengths([300, 200])
+    leaves = [x.clone().requires_grad_() for x in (q, k, v)]
+    got = plan(*leaves)                       # asynchronous: nothing to report yet
+    torch.cuda.synchronize()
+    for f in (lambda: got.backward(do), lambda: plan(*leaves), lambda: plan.backward(q, k, v, out, lse, do)):
+        with pytest.raises(C.NormPreError, match="gave up") as e:
+            f()
+        assert e.value.status == C.NORMPRE_ERR_TIMEOUT
+    assert plan.status(raise_on_error=False) == C.NORMPRE_ERR_TIMEOUT
+    assert plan.status() == C.NORMPRE_OK
+    grads = plan.backward(q, k, v, out, lse, do)   # the context is usable, and the plan too
+    assert plan.status() == C.NORMPRE_OK
+    for x, r, m in zip(grads, *(lambda ref: (ref[2:5], ref[5]))(reference(q, k, v, do, [300, 200]))):
+        assert err(x, r, m) <= TOL["bf16", "bwd"]
+
+
+def test_checkpoint_capture_in_a_graph():
+    """Pack, weight gradient, restore and SwiGLU captured in a process that has
+    made no call of theirs before."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2609_36692_gb300 import layers as L
+x, dy, up = (torch.randn(300, n, device="cuda").to(torch.bfloat16) for n in (256, 136, 256))
+def calls():
+    ck = L.ckpt_pack(x)
+    h, cg, cu = L.ckpt_swiglu(x, up)
+    return (ck.restore(), L.ckpt_wgrad(dy, ck), h, *L.ckpt_swiglu_backward(cg, cu, x))
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    got = calls()
+for _ in range(2):
+    for y in got:
+        y.zero_()
+    g.replay()
+assert L.ckpt_status() == 0
+assert all(torch.equal(a, b) for a, b in zip(got, calls()))
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
