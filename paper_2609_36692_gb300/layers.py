@@ -343,7 +343,7 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight):
-        ctx.ck = ckpt_pack(_rows(x))
+        ctx.ck = ckpt_pack(_rows(x.reshape(-1, x.shape[-1])))
         ctx.save_for_backward(weight)
         return x @ weight.to(x.dtype).t()
 
@@ -351,16 +351,16 @@ class _Linear(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         weight, = ctx.saved_tensors
-        dy = _rows(dy)
         dx = dy @ weight.to(dy.dtype) if ctx.needs_input_grad[0] else None
-        dw = ckpt_wgrad(dy, ctx.ck, dtype=weight.dtype) if ctx.needs_input_grad[1] else None
+        dw = ckpt_wgrad(_rows(dy.reshape(-1, dy.shape[-1])), ctx.ck, dtype=weight.dtype) if ctx.needs_input_grad[1] else None
         return dx, dw
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
-    """Differentiable y = x W^T that keeps x in 8 bits for its backward pass;
-    the weight gradient comes in the weight's dtype.  Nothing is kept where
-    there will be none."""
+    """Differentiable y = x W^T, x [..., features], that keeps x in 8 bits for
+    its backward pass; the weight gradient comes in the weight's dtype.  Nothing
+    is kept where there will be none.  The weight gradient is this library's
+    kernel; y and x's gradient are torch's matrix products."""
     if not (torch.is_grad_enabled() and weight.requires_grad):
         return x @ weight.to(x.dtype).t()
     return _Linear.apply(x, weight)

@@ -233,3 +233,30 @@ assert all(torch.equal(a, b) for a, b in zip(got, calls()))
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("shape", [(96,), (3, 40, 96), (2, 0, 96)], ids=str)
+def test_linear_of_any_leading_dimensions(shape):
+    """As many dimensions as the call takes when no gradient is kept; the bits of
+    the same rows as a matrix."""
+    import torch
+    from paper_2609_36692_gb300 import layers as L
+    x = torch.randn(*shape, device="cuda").to(torch.bfloat16)
+    w = torch.randn(64, 96, device="cuda").requires_grad_()
+    rows = [x.reshape(-1, 96).clone().requires_grad_(), w.detach().clone().requires_grad_()]
+    y2 = L.linear(*rows)
+    x.requires_grad_()
+    y = L.linear(x, w)
+    with torch.no_grad():
+        assert y.shape == L.linear(x, w).shape == (*shape[:-1], 64)
+    dy = torch.randn_like(y)
+    y.backward(dy)
+    y2.backward(dy.reshape(-1, 64))
+    assert torch.equal(w.grad, rows[1].grad)
+    # the library's products of other shapes may sum in another order
+    assert x.grad.shape == x.shape and rel(x.grad.reshape(-1, 96), rows[0].grad.double()) <= 2.0 ** -8
+    # a gradient that is expanded, or has its rows elsewhere
+    w.grad = None
+    L.linear(x, w).sum().backward()
+    ref = torch.ones(64, 1, device="cuda").double() @ L.ckpt_pack(x.detach().reshape(-1, 96)).restore().double().sum(0, keepdim=True)
+    assert rel(w.grad, ref) <= 1e-5
