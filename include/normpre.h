@@ -416,9 +416,12 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out);
 /*
  * The lengths of the next pack: lengths[s] >= 0 rows for sequence s (host
  * array; zero-length sequences are allowed, n_seqs = 0 is an empty pack).
- * Work lists are rebuilt on the host and copied on `stream`, so calls queued
- * on that stream before it still use the old lengths; once per batch, not per
- * layer.  Not for use during stream capture.
+ * Work lists are rebuilt on the host and copied on `stream`: calls made before
+ * it use the old lengths and calls made after it the new ones, whatever their
+ * streams.  Calls on `stream` need nothing for that; one on another stream waits
+ * for the copy there, and after such a call, or when `stream` changes, this call
+ * waits for the device.  Once per batch, not per layer.  Not for use during
+ * stream capture; captured calls belong to the lengths they were captured with.
  * Errors: ARG, SHAPE (more than the plan's max_seqs / max_tokens), CUDA.
  */
 int normpre_attn_set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, void* stream);

@@ -30,6 +30,8 @@ struct normpre_attn {
   char* lists = nullptr;
   char* staging = nullptr;         // pinned, the same size
   cudaEvent_t copied = nullptr;    // the last copy out of `staging`
+  cudaStream_t list_stream = nullptr;   // where it ran; calls there are in order with it
+  bool used = false, elsewhere = false;   // calls since: any, on other streams
   int64_t walk_at[3] = {-1, -1, -1};   // byte offsets of the walks, -1: none
   float* delta = nullptr;          // [n_heads][max_tokens]
   int* flags = nullptr;            // pinned: set by kernels, read here between calls
@@ -116,6 +118,23 @@ AttnArgs base_args(const normpre_attn* a, int64_t tokens) {
 
 int flags_of(const normpre_attn* a) { return *static_cast<const volatile int*>(a->flags); }
 
+// Puts a call's stream behind the copy of the lists.
+cudaError_t order(normpre_attn* a, cudaStream_t s) {
+  a->used = true;
+  if (s == a->list_stream) return cudaSuccess;
+  a->elsewhere = true;
+  cudaStreamCaptureStatus capture;
+  cudaError_t e = cudaStreamIsCapturing(s, &capture);
+  if (e) return e;
+  if (capture == cudaStreamCaptureStatusNone) return cudaStreamWaitEvent(s, a->copied, 0);
+  // a capture cannot depend on work outside it: the copy is waited for here
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  if ((e = cudaThreadExchangeStreamCaptureMode(&mode))) return e;
+  e = cudaEventSynchronize(a->copied);
+  const cudaError_t back = cudaThreadExchangeStreamCaptureMode(&mode);
+  return e ? e : back;
+}
+
 int check_call(const normpre_attn* a, int64_t tokens) {
   if (flags_of(a) & kFlagTimeout)
     return fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait of an earlier call of this plan gave up: what that call wrote "
@@ -183,9 +202,13 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
     deal(dkdv, hk, &walk[1]);
     deal(dq, h, &walk[2]);
   }
-  // one copy; the staging memory is free once the last one has left it
+  // one copy; the staging memory is free once the last one has left it, the
+  // lists once the calls that read them are done
   cudaError_t e = cudaEventSynchronize(a->copied);
-  if (e) return cuda_fail(e, "cudaEventSynchronize");
+  if (!e && (a->elsewhere || (a->used && s != a->list_stream))) e = cudaDeviceSynchronize();
+  if (e) return cuda_fail(e, "normpre_attn_set_lengths");
+  a->list_stream = s;
+  a->used = a->elsewhere = false;
   int64_t at = 0, walk_at[3];
   auto put = [&](const void* src, size_t bytes) {
     if (bytes) std::memcpy(a->staging + at, src, bytes);
@@ -272,8 +295,8 @@ int normpre_attn_forward(normpre_attn* a, int64_t tokens, const normpre_heads* q
   DeviceGuard device_guard(a->device);
   std::string err;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = a->cfg.dtype == NORMPRE_BF16 ? launch_attn_forward_tc(g, s, &err)
-                                                     : launch_attn_forward_simt(g, s);
+  cudaError_t e = order(a, s);
+  if (!e) e = a->cfg.dtype == NORMPRE_BF16 ? launch_attn_forward_tc(g, s, &err) : launch_attn_forward_simt(g, s);
   return e ? cuda_fail(e, err.empty() ? "attention forward" : err.c_str()) : NORMPRE_OK;
 }
 
@@ -295,7 +318,8 @@ int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* 
   g.lse = const_cast<float*>(lse);
   DeviceGuard device_guard(a->device);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_attn_delta(g, a->cfg.dtype, s);
+  cudaError_t e = order(a, s);
+  if (!e) e = launch_attn_delta(g, a->cfg.dtype, s);
   std::string err;
   if (!e) e = a->cfg.dtype == NORMPRE_BF16 ? launch_attn_backward_tc(g, s, &err) : launch_attn_backward_simt(g, s);
   return e ? cuda_fail(e, err.empty() ? "attention backward" : err.c_str()) : NORMPRE_OK;

@@ -260,3 +260,42 @@ def test_linear_of_any_leading_dimensions(shape):
     L.linear(x, w).sum().backward()
     ref = torch.ones(64, 1, device="cuda").double() @ L.ckpt_pack(x.detach().reshape(-1, 96)).restore().double().sum(0, keepdim=True)
     assert rel(w.grad, ref) <= 1e-5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_lengths_and_calls_on_different_streams(dtype):
+    """A call uses the lengths that were set before it, on whatever stream, and
+    not those that are set while it waits for its turn."""
+    import torch
+    n, h, hk = 600, 2, 1
+    packs = ([600], [37] * 16, [1, 300, 299])
+    q, k, v, do = make(7, n, h, hk, 64, dtype)
+    plan = plan_for(h, hk, 64, n, packs[1], dtype)
+
+    def both(stream=None):
+        out, lse = plan.forward(q, k, v, stream=stream)
+        return (out, lse, *plan.backward(q, k, v, out, lse, do, stream=stream))
+    want = []
+    for lengths in packs:
+        plan.set_lengths(lengths)
+        want.append(both())
+    side = torch.cuda.Stream()
+    got = []
+    for lengths in packs:
+        torch.cuda._sleep(20_000_000)                  # the copy of the lengths waits on the current stream
+        plan.set_lengths(lengths)
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)              # and the calls on theirs
+        got.append(both(side))
+    # lengths copied on the other stream, calls on the current one
+    side.wait_stream(torch.cuda.current_stream())
+    for lengths in packs:
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        plan.set_lengths(lengths, stream=side)
+        got.append(both())
+    torch.cuda.synchronize()
+    assert plan.status() == 0
+    for i, outs in enumerate(got):
+        for x, y in zip(outs, want[i % 3]):
+            assert torch.equal(x, y), i
