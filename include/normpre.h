@@ -421,7 +421,10 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out);
  * streams.  Calls on `stream` need nothing for that; one on another stream waits
  * for the copy there, and after such a call, or when `stream` changes, this call
  * waits for the device.  Once per batch, not per layer.  Not for use during
- * stream capture; captured calls belong to the lengths they were captured with.
+ * stream capture.  Captured calls belong to the lengths they were captured with:
+ * replayed under others they stay within the call's rows, but their outputs have
+ * no meaning; where the lists show it, that is reported as ARG, in the way of
+ * TIMEOUT.
  * Errors: ARG, SHAPE (more than the plan's max_seqs / max_tokens), CUDA.
  */
 int normpre_attn_set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, void* stream);
@@ -451,8 +454,9 @@ int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* 
                           const normpre_heads* dout, const normpre_heads* dq, const normpre_heads* dk,
                           const normpre_heads* dv, void* stream);
 
-/* Synchronizes `stream`, then reports and clears the plan's flag: TIMEOUT if a
- * bounded wait gave up since the last call, else OK. */
+/* Synchronizes `stream`, then reports and clears the plan's flags: TIMEOUT if a
+ * bounded wait gave up since the last call, ARG if a captured call met the lists
+ * of other lengths, else OK. */
 int normpre_attn_sync_status(normpre_attn* a, void* stream);
 
 /* Synchronizes the plan's device and releases the plan.  NULL is ignored. */

@@ -118,6 +118,8 @@ AttnArgs base_args(const normpre_attn* a, int64_t tokens) {
 
 int flags_of(const normpre_attn* a) { return *static_cast<const volatile int*>(a->flags); }
 
+constexpr char kOtherLists[] = "a captured call ran with the lists of other lengths than its own; its outputs have no meaning";
+
 // Puts a call's stream behind the copy of the lists.
 cudaError_t order(normpre_attn* a, cudaStream_t s) {
   a->used = true;
@@ -139,6 +141,7 @@ int check_call(const normpre_attn* a, int64_t tokens) {
   if (flags_of(a) & kFlagTimeout)
     return fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait of an earlier call of this plan gave up: what that call wrote "
                                      "has no meaning (normpre_attn_sync_status clears this)");
+  if (flags_of(a) & kFlagLists) return fail(NORMPRE_ERR_ARG, kOtherLists);
   if (tokens < a->total || tokens > a->cfg.max_tokens)
     return fail(NORMPRE_ERR_SHAPE, "tokens must be between the sum of the lengths and max_tokens");
   return NORMPRE_OK;
@@ -332,7 +335,9 @@ int normpre_attn_sync_status(normpre_attn* a, void* stream) {
   if (e) return cuda_fail(e, "normpre_attn_sync_status");
   const int flags = flags_of(a);
   if (flags) *static_cast<volatile int*>(a->flags) = 0;
-  return flags & kFlagTimeout ? fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait gave up") : NORMPRE_OK;
+  if (flags & kFlagTimeout) return fail(NORMPRE_ERR_TIMEOUT, "a bounded device wait gave up");
+  if (flags & kFlagLists) return fail(NORMPRE_ERR_ARG, kOtherLists);
+  return NORMPRE_OK;
 }
 
 void normpre_attn_free(normpre_attn* a) {

@@ -19,6 +19,15 @@ struct AttnBlock {
   int pad;
 };
 
+// Whether an entry of the lists fits into `total` rows.  The lists are rebuilt for
+// other lengths in place, and a call that was captured before then walks them
+// with counts of its own: every entry is checked before anything is addressed
+// by it, so that such a call ends with a flag and not out of range.
+__host__ __device__ inline bool block_fits(const AttnBlock& b, int total) {
+  return b.start >= 0 && b.start <= total && b.len > 0 && b.len <= total - b.start && b.blk >= 0 &&
+         b.blk <= (b.len - 1) / 128;
+}
+
 // A [tokens][heads][head_dim] tensor, strides in elements.
 struct AttnTensor {
   void* p;

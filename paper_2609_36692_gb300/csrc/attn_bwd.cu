@@ -241,14 +241,6 @@ struct Item {
 
 constexpr int kCached = 32;
 
-__device__ __forceinline__ ItemRef find_item(const AttnArgs& a, const AttnBlock* list, const int* walk, int heads,
-                                             int64_t r) {
-  const int64_t i = walk_item(walk, r, static_cast<int64_t>(a.n_blocks) * heads);
-  if (i < 0) return ItemRef{0, 0, -1, 0};
-  const AttnBlock b = list[i / heads];
-  return ItemRef{b.start, b.len, b.blk, static_cast<int>(i % heads)};
-}
-
 __device__ __forceinline__ bool get_item(const ItemRef& b, Item& it) {
   if (b.blk < 0) return false;
   it.start = b.start;
@@ -270,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   static_assert(sizeof(Bars<kSlots>) <= 512, "barriers");
   ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
   const AttnArgs& a = f.a;
-  auto find = [&](int64_t r) { return find_item(a, a.by_key, a.walk_dkdv, a.kv_heads, r); };
+  auto find = [&](int64_t r) { return list_item(a, a.by_key, a.n_blocks, a.walk_dkdv, a.kv_heads, r); };
   auto item = [&](int64_t r) { return r < kCached ? items[r] : find(r); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -501,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(ring + kSlots * kTileBytes);
   ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
   const AttnArgs& a = f.a;
-  auto find = [&](int64_t r) { return find_item(a, a.by_query, a.walk_dq, a.heads, r); };
+  auto find = [&](int64_t r) { return list_item(a, a.by_query, a.n_blocks, a.walk_dq, a.heads, r); };
   auto item = [&](int64_t r) { return r < kCached ? items[r] : find(r); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {

@@ -83,11 +83,7 @@ struct Item {
 constexpr int kCached = 64;
 
 __device__ __forceinline__ ItemRef find_item(const FwdArgs& f, int64_t r) {
-  const int per = f.pair_heads ? f.a.heads / 2 : f.a.heads;
-  const int64_t i = walk_item(f.a.walk_fwd, r, static_cast<int64_t>(f.n_list) * per);
-  if (i < 0) return ItemRef{0, 0, -1, 0};
-  const AttnBlock b = f.list[i / per];
-  return ItemRef{b.start, b.len, b.blk, static_cast<int>(i % per)};
+  return list_item(f.a, f.list, f.n_list, f.a.walk_fwd, f.pair_heads ? f.a.heads / 2 : f.a.heads, r);
 }
 
 __device__ __forceinline__ bool get_item(const FwdArgs& f, const ItemRef* cached, int64_t r, Item& it) {

@@ -171,6 +171,10 @@ struct Rows {
 __device__ __forceinline__ bool rows_of(const AttnArgs& a, const AttnBlock* list, int64_t i, Rows& w) {
   if (i < 2 * static_cast<int64_t>(a.n_blocks)) {
     const AttnBlock b = list[i >> 1];
+    if (!block_fits(b, a.total)) {
+      if (threadIdx.x == 0) raise_host_flag(a.flags, kFlagLists);
+      return false;
+    }
     w.seq = b.start;
     w.first = 128 * b.blk + 64 * static_cast<int>(i & 1);
     w.len = b.len;

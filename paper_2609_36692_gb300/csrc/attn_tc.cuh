@@ -20,12 +20,19 @@ constexpr float kLog2e = 1.4426950408889634f;
 // The r-th item of this CTA, -1 past its last.  With a plan's lists: ids from
 // walk[gridDim.x + 1 + walk[c]] up to walk[gridDim.x + 1 + walk[c + 1]].  Without
 // (many items per CTA): the items in falling order of cost, back and forth over
-// the CTAs.
-__device__ __forceinline__ int64_t walk_item(const int* walk, int64_t r, int64_t items) {
+// the CTAs.  What does not fit the call (see block_fits) is flagged and ends the
+// CTA's walk.
+__device__ __forceinline__ int64_t walk_item(const int* walk, int64_t r, int64_t items, int* flags) {
   const int64_t g = gridDim.x, c = blockIdx.x;
   if (walk) {
-    const int64_t i = walk[c] + r;
-    return i < walk[c + 1] ? walk[g + 1 + i] : -1;
+    const int64_t i = walk[c] + r, end = walk[c + 1];
+    if (i >= 0 && end <= items) {
+      if (i >= end) return -1;
+      const int64_t id = walk[g + 1 + i];
+      if (id >= 0 && id < items) return id;
+    }
+    raise_host_flag(flags, kFlagLists);
+    return -1;
   }
   const int64_t i = r * g + ((r & 1) ? g - 1 - c : c);
   return i < items ? i : -1;
@@ -133,6 +140,20 @@ __device__ __forceinline__ void store_rows(bf16* tile, int64_t ts, const uint32_
 struct ItemRef {
   int start, len, blk, head;   // blk -1: no item
 };
+
+// The r-th item of this CTA from a list of blocks with `per` items each.
+__device__ __forceinline__ ItemRef list_item(const AttnArgs& a, const AttnBlock* list, int blocks, const int* walk, int per,
+                                             int64_t r) {
+  const ItemRef none = {0, 0, -1, 0};
+  const int64_t i = walk_item(walk, r, static_cast<int64_t>(blocks) * per, a.flags);
+  if (i < 0) return none;
+  const AttnBlock b = list[i / per];
+  if (!block_fits(b, a.total)) {
+    raise_host_flag(a.flags, kFlagLists);
+    return none;
+  }
+  return ItemRef{b.start, b.len, b.blk, static_cast<int>(i % per)};
+}
 
 // Map of a [tokens][heads][dim] bf16 tensor for boxes of 128 rows x 64 columns.
 inline bool rows_map(CUtensorMap* m, const AttnTensor& t, int tokens, int heads, int dim, std::string* err) {

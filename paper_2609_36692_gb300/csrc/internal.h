@@ -15,6 +15,7 @@ namespace normpre {
 constexpr int kFlagNonfinite = 1;
 constexpr int kFlagNumeric = 2;
 constexpr int kFlagTimeout = 4;
+constexpr int kFlagLists = 8;    // attention: work lists of other lengths than the call's
 
 constexpr int kMaxBatch = 32;    // matrices served by one normalize/apply launch
 constexpr int kMaxGroups = 7;    // shape groups served by one Newton-Schulz GEMM launch (its arguments within 4 KB)

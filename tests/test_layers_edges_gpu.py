@@ -299,3 +299,45 @@ def test_lengths_and_calls_on_different_streams(dtype):
     for i, outs in enumerate(got):
         for x, y in zip(outs, want[i % 3]):
             assert torch.equal(x, y), i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_replay_under_other_lengths_stays_in_range(dtype):
+    """A captured call knows the number of blocks of its own lengths.  Replayed
+    with the lists of others it writes no row but the call's, ends, and gives the
+    right bits again once its lengths are back."""
+    import torch
+    h, hk, d, n, room = 4, 2, 64, 700, 64
+    own, others = [123, 277], [[700], [1] * 100, [5] * 140, [0, 400], []]
+    # a process whose plans take up to 700 rows; the call's are 400, with rows around them that nobody owns
+    names = [("q", h), ("k", hk), ("v", hk), ("o", h), ("do", h), ("dq", h), ("dk", hk), ("dv", hk)]
+    big = {name: torch.full((400 + 2 * room, x, d), 7.0, device="cuda", dtype=dt(dtype)) for name, x in names}
+    t = {name: x[room:room + 400] for name, x in big.items()}
+    for name, x in zip(("q", "k", "v", "do"), make(8, 400, h, hk, d, dtype)):
+        t[name].copy_(x)
+    lse = torch.full((h, 400), 7.0, device="cuda")
+    plan = plan_for(h, hk, d, n, [1] * 140, dtype)
+    plan.set_lengths(own)
+
+    def calls():
+        plan.forward(t["q"], t["k"], t["v"], out=t["o"], lse=lse)
+        plan.backward(t["q"], t["k"], t["v"], t["o"], lse, t["do"], t["dq"], t["dk"], t["dv"])
+    calls()
+    torch.cuda.synchronize()
+    want = {name: x.clone() for name, x in big.items()}
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls()
+    for lengths in others:
+        plan.set_lengths(lengths)
+        g.replay()
+        torch.cuda.synchronize()
+        plan.status(raise_on_error=False)
+        for name, x in big.items():
+            assert bool((x[:room] == 7.0).all()) and bool((x[room + 400:] == 7.0).all()), name
+        plan.set_lengths(own)
+        g.replay()
+        torch.cuda.synchronize()
+        assert plan.status() == 0
+        for name, x in big.items():
+            assert torch.equal(x, want[name]), name
