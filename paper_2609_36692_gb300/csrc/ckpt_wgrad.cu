@@ -258,10 +258,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
   } else if (warp == kMma) {
     // ---------------- MMA (one thread) ----------------
     if (!SPLIT && rank != 0) {
-      // The pair's other CTA: its operands are in place.  The tensor cores of
-      // this SM read them, no thread elsewhere does, so that the arrival need not
-      // order them for the cluster (a release and acquire at that scope take 2100
-      // cycles a step, all others together 600).
+      // The pair's other CTA: its operands are in place.  The converting warps
+      // handed their writes to the asynchronous proxy and to this thread; its
+      // arrival releases them to the thread that issues the MMAs.
       if (tc::elect_one()) {
         for (int u = unit0; u < f.units && ok; u += nunits)
           for (int s = s0; s < s1; ++s, y.next(kDyRing), x.next(kRing)) {
@@ -278,13 +277,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
         if (SPLIT) tc::mma_commit(bar);
         else tc::mma_commit_pair(bar, 3);
       };
+      // arrivals of both CTAs
+      auto wait_pair = [&](uint64_t* bar, uint32_t parity) { return ok = ok && tc::mbar_wait<!SPLIT>(bar, parity, &b->abort); };
       int acc = 0, never = 0;
       uint32_t tphase = 0;
       for (int u = unit0; u < f.units && ok; u += nunits) {
-        if (!wait1(&b->tempty[acc], tphase ^ 1u)) break;
+        if (!wait_pair(&b->tempty[acc], tphase ^ 1u)) break;
         for (int s = s0; s < s1; ++s, y.next(kDyRing), x.next(kRing)) {
           if (!wait1(&b->full[y.at], y.phase) || !wait1(&b->xfull[x.at], x.phase)) break;
-          if (!SPLIT && !wait1(&b->ofull[x.at], x.phase)) break;
+          if (!SPLIT && !wait_pair(&b->ofull[x.at], x.phase)) break;
           tc::fence_after();
           const uint64_t bd = tc::sdesc(tc::su32(ring + y.at * kDyBytes), kBox, 1024);
           const uint64_t ad = tc::sdesc(tc::su32(xbuf + x.at * kXBytes), kBox, 1024);
@@ -302,7 +303,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_wgrad_tc(const __grid_constan
         acc ^= 1;
         if (acc == 0) tphase ^= 1u;
       }
-      // every MMA issued has completed once `drain` fires
       // every MMA issued has completed once `drain` fires
       commit(&b->drain);
       tc::mbar_wait(&b->drain, 0, &never);

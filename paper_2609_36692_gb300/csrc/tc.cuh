@@ -36,26 +36,42 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(su32(bar)) : "memory");
 }
+// CLUSTER: for arrivals from another CTA of the cluster, without their acquire
+// (see mbar_wait).
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(su32(bar)), "r"(parity)
-      : "memory");
+  if constexpr (CLUSTER) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(su32(bar)), "r"(parity)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(su32(bar)), "r"(parity)
+        : "memory");
+  }
   return ok != 0;
 }
 // Bounded wait: gives up after ~2 s (no tile takes a fraction of that) or as
 // soon as another role of the CTA has given up.
 constexpr uint64_t kWaitNs = 2000000000ull;
 // The global timer is read only after many tries: reading it costs
-// microseconds, more than most waits last.
+// microseconds, more than most waits last.  CLUSTER: acquires what other CTAs of
+// the cluster released before they arrived (mbar_arrive_remote), as far as it
+// lies in shared memory.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
   uint64_t t0 = 0;
   uint32_t i = 0;
-  while (!mbar_try_wait(bar, parity)) {
+  while (!mbar_try_wait<CLUSTER>(bar, parity)) {
     if ((++i & 255u) == 0) {
       if (*abort_flag) return false;
       const uint64_t t = globaltimer();
@@ -63,6 +79,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
       if (t - t0 > kWaitNs) return false;
     }
   }
+  if constexpr (CLUSTER) asm volatile("fence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory");
   return true;
 }
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int c0,
@@ -157,11 +174,14 @@ __device__ __forceinline__ void mma_commit_pair(uint64_t* bar, uint16_t mask) {
                "h"(mask)
                : "memory");
 }
-// Arrives on the barrier at the same place of another CTA of the cluster.
+// Arrives on the barrier at the same place of another CTA of the cluster, and
+// releases this CTA's shared memory to it (mbar_wait<true> acquires).  The fence is
+// restricted to shared memory: one over all memory takes 2000 cycles.
 __device__ __forceinline__ void mbar_arrive_remote(uint64_t* bar, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(su32(bar)), "r"(rank));
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(r) : "memory");
+  asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(r) : "memory");
 }
 // TMA load multicast to the CTAs of the cluster named in `mask`: the box lands
 // at offset `dst` of each one's shared memory and completes on the barrier at

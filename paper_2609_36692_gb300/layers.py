@@ -283,7 +283,10 @@ def ckpt_pack(x: torch.Tensor) -> Checkpoint:
 def ckpt_wgrad(dy: torch.Tensor, ck: Checkpoint, dtype: Optional[torch.dtype] = None,
                out: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
     """dW = dY^T xhat, [out_features, features]: the weight gradient of
-    y = x W^T from x's checkpoint; added to ``out`` with ``accumulate``."""
+    y = x W^T from x's checkpoint; added to ``out`` with ``accumulate``.  bf16 dY
+    whose rows start on 16-byte boundaries runs on the tensor cores; fp32 dY and
+    other row strides (an odd out_features) on fp32 units, an order of magnitude
+    slower."""
     ld = _matrix(dy, "dy", (ck.tokens, dy.shape[1] if dy.dim() == 2 else -1), ck.device)
     shape = (dy.shape[1], ck.features)
     if out is None:
