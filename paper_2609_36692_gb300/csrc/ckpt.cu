@@ -205,17 +205,18 @@ struct SwigluArgs {
   uint32_t *gate_steps, *up_steps;
 };
 
-// 1 / (1 + exp(-x)).  fp32: to a few units in the last place, from exp(-|x|),
-// which cannot overflow.  bf16: the hardware's exponential, whose relative error
-// (1e-5 at |x| = 88) is far below the rounding that follows; the exact one makes
-// the kernels 12 % slower (16384 x 6144, both passes: 301 us, not 268).
+// s = 1 / (1 + exp(-x)) in x, 1 - s in y, to a few units in the last place: from
+// exp(-|x|), which cannot overflow, and a divisor in [1, 2].
+__device__ __forceinline__ float2 sigmoids(float x) {
+  const float e = expf(-fabsf(x)), r = __fdividef(1.f, 1.f + e);
+  return x < 0.f ? make_float2(e * r, r) : make_float2(r, e * r);
+}
+// bf16 takes the hardware's exponential, whose relative error (1e-5 at |x| = 88)
+// is far below the rounding that follows; the exact one makes its kernels 12 %
+// slower (16384 x 6144, both passes: 301 us, not 268).
 template <typename T> __device__ __forceinline__ float sigmoid(float x) {
-  if constexpr (sizeof(T) == 4) {
-    const float e = expf(-fabsf(x));
-    return (x < 0.f ? e : 1.f) / (1.f + e);
-  } else {
-    return __fdividef(1.f, 1.f + __expf(-x));
-  }
+  if constexpr (sizeof(T) == 4) return sigmoids(x).x;
+  else return __fdividef(1.f, 1.f + __expf(-x));
 }
 
 template <typename T, bool VEC>
@@ -270,8 +271,7 @@ __global__ void __launch_bounds__(kThreads) k_ckpt_swiglu_bwd(const __grid_const
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const float s = sigmoid<T>(g[e]);
-      // 1 - s, in fp32 without its cancellation
-      u[e] *= d[e] * s * fmaf(g[e], sizeof(T) == 4 ? sigmoid<T>(-g[e]) : 1.f - s, 1.f);
+      u[e] *= d[e] * s * fmaf(g[e], sizeof(T) == 4 ? sigmoids(g[e]).y : 1.f - s, 1.f);
       g[e] *= d[e] * s;
     }
     store16<VEC>(static_cast<T*>(a.dgate) + p[i].row * a.dgate_ld + p[i].feature, p[i].n, u);
