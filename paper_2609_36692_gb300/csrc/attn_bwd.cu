@@ -35,11 +35,14 @@
 //
 // Roundings to bf16: P and dS once each (MMA operands), the gradients once.
 //
-// What bounds it: the products.  16384 tokens, 16 / 8 heads of 128: 2.38 ms
-// alone, 2.52 ms in a loop, where the seven products run at 1530 TFLOP/s and the
-// clock falls with the power limit.  Short sequences add the items' ends (the
+// What bounds it: the products.  16384 tokens, 16 / 8 heads of 128: 2.5 ms alone,
+// 2.58 ms in a loop, where the seven products run at 1490 TFLOP/s and the clock
+// falls with the power limit.  Short sequences add the items' ends (the
 // gradients' way from TMEM to memory, 2000 cycles against 2050 an iteration of
-// dK, dV at head_dim 64): 8 x 1024 tokens, 12 heads of 64, 0.090 ms.
+// dK, dV at head_dim 64): 8 x 1024 tokens, 12 heads of 64, 0.091 ms.  With few key
+// / value heads the key blocks of a long sequence do not fill the GPU: one of 4096
+// tokens, 8 / 1 heads of 128, is 32 items of dK, dV, 0.45 ms (190 TFLOP/s of the
+// five products that are needed).
 #include "attn_tc.cuh"
 
 namespace normpre {

@@ -25,7 +25,8 @@
 //
 // S - m' is formed before the scale: near the maximum it is exact however large
 // the scores, while c S - c m' would carry the rounding of c m' (0.002 in the
-// exponent at scores of 3e4).  It costs a packed addition beside the product.
+// exponent at scores of 3e4).  That addition and P's conversion, which shares the
+// exponentials' pipe, cost 3 % against one FMA and a cut.
 //
 // Roundings to bf16: P once (the MMA operand; l sums the unrounded values) and
 // the output once.
@@ -34,9 +35,9 @@
 // 512 cycles and a scheduler's two softmax warps 2 x 128 exponentials of 4
 // cycles beside their scaling, sums and conversions, about as much; the two stay within
 // a fifth of each other.  Under load the clock falls with the power limit.
-// 16384 tokens, 16 / 8 heads of 128: 0.612 ms alone (1800 TFLOP/s), 0.70 ms in a
-// loop; 8192 tokens in seven sequences 0.089 ms (1100 TFLOP/s: the CTAs' last
-// items).
+// 16384 tokens, 16 / 8 heads of 128: 0.62 ms alone (1760 TFLOP/s), 0.70 ms in a
+// loop; 8192 tokens in seven sequences 0.074 ms with everything in L2 (1320
+// TFLOP/s: the CTAs' last items), 0.090 to 0.098 ms otherwise.
 #include "attn_tc.cuh"
 
 namespace normpre {

@@ -23,7 +23,7 @@
 // L2 reads but not the port).  256 x 192 tiles of one
 // CTA take in fewer bytes too, but their conversion (4 cycles an element and SM
 // sub-partition, byte permutations at half rate) then takes 1000 cycles of the
-// MMAs' 768.  16384 x 6144 x 2048: 0.248 ms (1660 TFLOP/s), 0.274 ms in a long
+// MMAs' 768.  16384 x 6144 x 2048: 0.251 ms (1640 TFLOP/s), 0.28 ms in a long
 // loop, where the clock falls with the power limit.
 //   With too few tiles for the SMs, clusters of 2 to 8 CTAs split a tile's
 // tokens instead and join through distributed shared memory: each CTA lays its
@@ -33,7 +33,9 @@
 //
 // k_wgrad_simt: fp32 arithmetic, one CTA of 256 threads per 64 x 64 piece of
 // dW, 16 tokens at a time through shared memory, a 4 x 4 piece per thread; any
-// dtype, stride and size.  Bound by the fp32 FMA pipe.
+// dtype, stride and size.  Loads and products take turns, and a CTA walks all
+// tokens: 8192 x 768 x 768 with fp32 dY 0.73 ms (13 TFLOP/s, 144 CTAs), 16384 x
+// 6144 x 2048 16.7 ms (25).
 #include <algorithm>
 
 #include "ckpt.h"
@@ -541,11 +543,10 @@ cudaError_t launch_tc(WgradTcArgs f, cudaStream_t s) {
   }
   const cudaError_t e = clusters_at_once<TW, false>(2, &fit);
   if (e) return e;
-  // The tile width whose rounds over the clusters take least.  Shared memory
-  // serves a step's 64 KB and 64 bytes an output at about 128 bytes a cycle, so
-  // that a narrower tile gains little (16384 x 4096 x 2432, three rounds each:
-  // 252 us at 256, 248 at 224, 238 at 192) and a further round costs all of it
-  // (16384 x 6912 x 2048: 266 us at 256, 327 at 224).
+  // The tile width whose rounds over the clusters take least.  A step's time goes
+  // as 512 + tn / 2, so that a narrower tile gains little (16384 x 4096 x 2432,
+  // three rounds each: 252 us at 256, 248 at 224, 238 at 192) and a further round
+  // costs all of it (16384 x 6912 x 2048: 266 us at 256, 327 at 224).
   int64_t least = -1;
   for (int tn = kTileN; tn >= 192; tn -= 32) {
     const int64_t units = (f.tiles_k + 1) / 2 * cdiv(f.a.n, tn), cost = cdiv(units, fit) * (512 + tn / 2);
