@@ -535,6 +535,112 @@ int normpre_ckpt_swiglu_backward(int64_t tokens, int64_t features, int dtype, co
  * call, else OK. */
 int normpre_ckpt_sync_status(void* stream);
 
+/*
+ * Norms of queries and keys with the rotation of their positions: what lies
+ * between a layer's fused projection and its attention.  For a row x (the
+ * head_dim values of one head and token) with weight w and position p:
+ *   r = 1 / sqrt(mean(x^2) + eps),  y = x r w
+ * and then the first rotary_dim values of y in pairs (a, b), the pairs being
+ * (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with interleaved = 1:
+ *   a' = a cos(p f_i) - b sin(p f_i),  b' = a sin(p f_i) + b cos(p f_i)
+ * The other values pass.  Backward, with g the rotation of dz by -p f_i,
+ * u = g w and xh = x r:
+ *   dx = r (u - xh mean(u xh)),  dw = sum of g xh over tokens and heads
+ * One weight of head_dim values serves all query heads, one all key heads; a
+ * null weight is one of ones.  fp32 arithmetic (rows whose squares leave its
+ * range are scaled first), results rounded once; angles are exact to 2^-53 of a
+ * turn per position, whatever the position.
+ * Rows from `used` on (padding) are written as zeros and add nothing to the
+ * weights' gradients, whatever they hold.  A row that is not finite reaches its
+ * own results and the weights' gradients.
+ */
+typedef struct normpre_qkrot normpre_qkrot;
+
+typedef struct normpre_qkrot_config {
+  int n_heads;      /* query heads, in [1, 65535] */
+  int n_kv_heads;   /* key heads, in [1, 65535] */
+  int head_dim;     /* a multiple of 8, in [8, 128] */
+  int rotary_dim;   /* even, in [0, head_dim]; 0: norms only */
+  int interleaved;  /* 1: pairs of neighbours */
+  int norm;         /* 0: rotation only (weights are null), 1: norms and rotation */
+  int dtype;        /* normpre_dtype of queries, keys and their gradients */
+  float eps;        /* finite, >= 1e-30 (norm = 1) */
+} normpre_qkrot_config;
+
+/*
+ * A plan: host memory only, so that one may serve any number of calls at once,
+ * on any device.  frequencies: host array of rotary_dim / 2 angles per
+ * position in radians, f_i (at most 1e6 in absolute value); usually
+ * base^(-2 i / rotary_dim).
+ * Errors (message from normpre_last_error(NULL), as for every normpre_qkrot_*
+ * call): ARG, SHAPE, DTYPE.
+ */
+int normpre_qkrot_init(const normpre_qkrot_config* cfg, const double* frequencies, normpre_qkrot** out);
+
+/* Bytes of a backward call's workspace (its contents need not be kept or cleared). */
+int normpre_qkrot_bytes(const normpre_qkrot* p, int64_t* bytes);
+
+/*
+ * q, k, q_out, k_out: see normpre_heads; an output may be its input itself.
+ * positions: device, one whole number per token, of 4 or 8 bytes
+ * (position_bytes); not read where rotary_dim = 0.  weights: device, head_dim
+ * contiguous values of weight_dtype.  tokens in [0, 2^31).
+ * Asynchronous on `stream`, on the current device; allocates nothing.
+ * Errors: ARG, SHAPE, DTYPE, ALIGN, CUDA.
+ */
+int normpre_qkrot_forward(const normpre_qkrot* p, int64_t tokens, int64_t used, const normpre_heads* q,
+                          const normpre_heads* k, const void* positions, int position_bytes, const void* q_weight,
+                          const void* k_weight, int weight_dtype, const normpre_heads* q_out, const normpre_heads* k_out,
+                          void* stream);
+
+/*
+ * dq_out, dk_out: gradients of the forward call's results; dq, dk: of its
+ * inputs (either may be the former itself).  dq_weight, dk_weight: head_dim
+ * values of weight_dtype each, or null where no gradient is wanted (a null
+ * weight has none); then no workspace is needed.  The sums run in a fixed
+ * order: the same inputs give the same bits.
+ */
+int normpre_qkrot_backward(const normpre_qkrot* p, int64_t tokens, int64_t used, const normpre_heads* q,
+                           const normpre_heads* k, const void* positions, int position_bytes, const void* q_weight,
+                           const void* k_weight, int weight_dtype, const normpre_heads* dq_out,
+                           const normpre_heads* dk_out, const normpre_heads* dq, const normpre_heads* dk,
+                           void* dq_weight, void* dk_weight, void* workspace, void* stream);
+
+/* NULL is ignored. */
+void normpre_qkrot_free(normpre_qkrot* p);
+
+/*
+ * The norm of n gradients taken as one vector, and clipping by it:
+ *   norm = sqrt(sum of all g^2),  c = min(1, max_norm / (norm + eps)),  g' = c g
+ * n in [0, 2^20].  grads[i]: device, sizes[i] >= 0 contiguous values of dtypes[i]
+ * (normpre_dtype), aligned to its elements, at most 2^40 values in all; arrays of pointers, sizes and dtypes are host memory
+ * and are read before the call returns.  fp32 products; sums of squares in fp32
+ * over 64 bytes of values (fp64 where they would leave its range), fp64 beyond,
+ * in a fixed order: the same inputs give the same bits.
+ *   norm       device, one fp32 value, written.  A gradient that holds a NaN
+ *              gives NaN, one that holds an infinity infinity.
+ *   workspace  device, 16-byte aligned, normpre_grad_bytes(n) bytes, whose
+ *              contents need not be kept or cleared; calls that may overlap on
+ *              the GPU need one each.
+ * Asynchronous on `stream`, on the current device; allocates no device memory.
+ * Errors (message from normpre_last_error(NULL)): ARG, SHAPE, DTYPE, ALIGN, CUDA.
+ */
+int normpre_grad_bytes(int n, int64_t* bytes);
+
+int normpre_grad_norm(int n, const void* const* grads, const int* dtypes, const int64_t* sizes, float* norm,
+                      void* workspace, void* stream);
+
+/*
+ * out[i], of out_dtypes[i], receives the clipped gradient (rounded once).  It
+ * may be grads[i] itself with the same dtype: if all are, and c = 1, nothing is
+ * written.  An output that shares memory with another tensor of the call is
+ * refused (ARG): a tensor listed twice would be clipped twice.  With a norm of
+ * infinity c is 0, with NaN every result is NaN.
+ *   max_norm  finite, >= 0.    eps  finite, >= 0 (a common choice is 1e-6).
+ */
+int normpre_grad_clip(int n, const void* const* grads, const int* dtypes, const int64_t* sizes, void* const* out,
+                      const int* out_dtypes, float max_norm, float eps, float* norm, void* workspace, void* stream);
+
 /* Releases the handle made by normpre_init and every device buffer it owns
  * (the caller's W, G and M, which carry the optimizer's state across the steps
  * of Algorithm 1, are untouched).  NULL is ignored. */

@@ -68,28 +68,9 @@ struct Release {
   void operator()(normpre_attn* a) const { release(a); }
 };
 
-// Checks one tensor argument and copies it; a stride that no address uses (a
-// single row or head) is replaced by a valid one.
 int take(const normpre_attn* a, const normpre_heads* t, int64_t tokens, int heads, const char* name, bool output,
          AttnTensor* out) {
-  if (!t || !t->data) return fail(NORMPRE_ERR_ARG, std::string(name) + ": null");
-  const int64_t d = a->cfg.head_dim, per16 = a->cfg.dtype == NORMPRE_BF16 ? 8 : 4;
-  int64_t ts = tokens > 1 ? t->token_stride : 0, hs = heads > 1 ? t->head_stride : 0;
-  if (tokens > 1 && (ts < d || ts > (int64_t(1) << 30)))
-    return fail(NORMPRE_ERR_SHAPE, std::string(name) + ": token stride must be in [head_dim, 2^30]");
-  if (heads > 1 && (hs < d || hs > (int64_t(1) << 36)))
-    return fail(NORMPRE_ERR_SHAPE, std::string(name) + ": head stride must be in [head_dim, 2^36]");
-  if ((reinterpret_cast<uintptr_t>(t->data) & 15u) || ts % per16 || hs % per16)
-    return fail(NORMPRE_ERR_ALIGN, std::string(name) + ": data and strides must be multiples of 16 bytes");
-  if (output && tokens > 1 && heads > 1) {
-    const bool by_token = ts >= hs;   // rows outermost, or heads
-    const int64_t inner = by_token ? (heads - 1) * hs + d : (tokens - 1) * ts + d;
-    if ((by_token ? ts : hs) < inner) return fail(NORMPRE_ERR_SHAPE, std::string(name) + ": overlapping strides");
-  }
-  if (!ts) ts = round_up(d, 8);
-  if (!hs) hs = round_up(d, 8);
-  *out = AttnTensor{t->data, ts, hs};
-  return NORMPRE_OK;
+  return take_heads(t, tokens, heads, a->cfg.head_dim, a->cfg.dtype, name, output, out);
 }
 
 AttnArgs base_args(const normpre_attn* a, int64_t tokens) {

@@ -6,6 +6,7 @@
 
 #include <string>
 
+#include "heads.h"
 #include "internal.h"
 
 namespace normpre {
@@ -28,11 +29,7 @@ __host__ __device__ inline bool block_fits(const AttnBlock& b, int total) {
          b.blk <= (b.len - 1) / 128;
 }
 
-// A [tokens][heads][head_dim] tensor, strides in elements.
-struct AttnTensor {
-  void* p;
-  int64_t ts, hs;
-};
+typedef HeadsView AttnTensor;
 
 struct AttnArgs {
   AttnTensor q, k, v, o, dout, dq, dk, dv;

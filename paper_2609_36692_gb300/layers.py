@@ -1,16 +1,18 @@
 """Training operators around the optimizer step, on torch tensors: packed
-causal attention and 8-bit activation checkpoints.
+causal attention, the norms and rotation of queries and keys before it, and 8-bit
+activation checkpoints.
 
 Like ``optim``, this only checks tensors and hands their pointers and the
-current CUDA stream to the C ABI (``normpre_attn_*``, ``normpre_ckpt_*`` in
-``include/normpre.h``, which has the definitions); all arithmetic runs in the
-library's kernels.  ``PackedAttention.__call__``, ``linear`` and ``swiglu`` are
-the differentiable forms; they have first derivatives only, and asking for
-another one raises.
+current CUDA stream to the C ABI (``normpre_attn_*``, ``normpre_qkrot_*``,
+``normpre_ckpt_*`` in ``include/normpre.h``, which has the definitions); all
+arithmetic runs in the library's kernels.  ``PackedAttention.__call__``,
+``QKNormRotary.__call__``, ``linear`` and ``swiglu`` are the differentiable forms;
+they have first derivatives only, and asking for another one raises.
 """
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -32,14 +34,14 @@ def _dtype_code(x: torch.Tensor) -> int:
     return code
 
 
-def _on(device: torch.device, f, *args) -> None:
-    """f(*args, stream) with `device` current, on its current stream."""
+def _on(device: torch.device, f, *args, stream=None) -> None:
+    """f(*args, stream) with `device` current, on its current stream or the one given."""
     index = device.index
     if _current_device() == index:
-        f(*args, _current_stream(index))
+        f(*args, _current_stream(index) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(index):
-            f(*args, _current_stream(index))
+            f(*args, _current_stream(index) if stream is None else stream.cuda_stream)
 
 
 def _used_on(stream, *tensors) -> None:
@@ -211,6 +213,154 @@ class _Attention(torch.autograd.Function):
                                "set_lengths the call's lengths again, or use a plan for each batch in flight")
         # autograd may hand over an expanded gradient
         return (None, *ctx.plan.backward(q, k, v, out, lse, _aligned(dout)))
+
+
+# ---------------------------------------------------------------------------
+# norms of queries and keys, rotation of their positions
+# ---------------------------------------------------------------------------
+class QKNormRotary:
+    """What lies between a layer's fused projection and its attention: the RMS
+    norm of each query and key head with a weight of ``head_dim`` values, and the
+    rotation of the first ``rotary_dim`` values by the token's position, in one
+    pass (``normpre_qkrot_forward`` has the formulas).
+
+    ``rotary_dim`` None: all of ``head_dim``; 0: norms only.  The pairs that turn
+    are (i, i + rotary_dim / 2), or neighbours with ``interleaved``; pair i turns
+    by ``frequencies[i]`` radians per position, base^(-2 i / rotary_dim) unless
+    they are given.  ``norm`` False: rotation only, without weights.
+
+    q is [tokens, n_heads, head_dim], k [tokens, n_kv_heads, head_dim]: views as
+    ``PackedAttention`` takes them.  positions: whole numbers [tokens], int32 or
+    int64.  Weights: [head_dim], fp32 or bf16; None: ones.  used: rows from there
+    on are padding, and get zero outputs and gradients.  One object may serve any
+    number of calls at once, on any device and stream.
+    """
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, rotary_dim: Optional[int] = None,
+                 base: float = 10000.0, interleaved: bool = False, eps: float = 1e-6, norm: bool = True,
+                 dtype: torch.dtype = torch.bfloat16, frequencies: Optional[Sequence[float]] = None):
+        code = _CODES.get(dtype)
+        if code is None:
+            raise TypeError("unsupported dtype %s (float32 or bfloat16)" % dtype)
+        self.n_heads, self.n_kv_heads, self.head_dim, self.dtype = n_heads, n_kv_heads, head_dim, dtype
+        self.rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        self.plan = None
+        if frequencies is None:
+            if not 0.0 < base < math.inf:
+                raise ValueError("base must be finite and > 0")
+            frequencies = [base ** (-2.0 * i / self.rotary_dim) for i in range(max(0, self.rotary_dim // 2))]
+        cfg = C.normpre_qkrot_config(n_heads, n_kv_heads, head_dim, self.rotary_dim, int(interleaved), int(norm), code, eps)
+        self.plan = C.normpre_qkrot_init(cfg, frequencies)
+        self._bytes = C.normpre_qkrot_bytes(self.plan)
+
+    def _check(self, x: torch.Tensor, name: str, tokens: int, heads: int, device: torch.device):
+        if x.device != device or not x.is_cuda:
+            raise ValueError("%s must be on %s" % (name, "a CUDA device" if device.type != "cuda" else device))
+        if x.dtype != self.dtype:
+            raise TypeError("%s must be %s" % (name, self.dtype))
+        if x.shape != (tokens, heads, self.head_dim):
+            raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, tokens, heads, self.head_dim, tuple(x.shape)))
+        st, sh, sd = x.stride()
+        if sd != 1 and tokens:
+            raise ValueError("%s: the last dimension must be contiguous" % name)
+        return x.data_ptr(), st, sh
+
+    def _rest(self, positions, q_weight, k_weight, tokens, device):
+        """Positions' pointer and bytes, weights' pointers and dtype code."""
+        at, size = 0, 8
+        if self.rotary_dim:
+            if positions is None or positions.device != device or positions.shape != (tokens,) or \
+                    positions.dtype not in (torch.int64, torch.int32) or (tokens > 1 and positions.stride(0) != 1):
+                raise ValueError("positions must be a contiguous int32 or int64 [%d] tensor on %s" % (tokens, device))
+            at, size = positions.data_ptr(), positions.element_size()
+        pointers, code = [], None
+        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is None:
+                pointers.append(0)
+                continue
+            if w.device != device or w.shape != (self.head_dim,) or w.stride(0) != 1:
+                raise ValueError("%s must be a contiguous [%d] tensor on %s" % (name, self.head_dim, device))
+            if code is not None and _dtype_code(w) != code:
+                raise TypeError("q_weight and k_weight must have one dtype")
+            code = _dtype_code(w)
+            pointers.append(w.data_ptr())
+        return at, size, pointers[0], pointers[1], code or 0
+
+    def forward(self, q, k, positions=None, q_weight=None, k_weight=None, q_out=None, k_out=None,
+                used: Optional[int] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """The normed and rotated (q, k).  An output may be its input itself."""
+        t, h, hk, device = q.shape[0], self.n_heads, self.n_kv_heads, q.device
+        check = self._check
+        args = (*check(q, "q", t, h, device), *check(k, "k", t, hk, device))
+        rest = self._rest(positions, q_weight, k_weight, t, device)
+        _used_on(stream, q, k, positions, q_weight, k_weight, q_out, k_out)
+        if q_out is None:
+            q_out = _empty((t, h, self.head_dim), self.dtype, device, stream)
+        if k_out is None:
+            k_out = _empty((t, hk, self.head_dim), self.dtype, device, stream)
+        heads = (ctypes.c_int64 * 12)(*args, *check(q_out, "q_out", t, h, device), *check(k_out, "k_out", t, hk, device))
+        at = ctypes.addressof(heads)
+        _on(device, C.normpre_qkrot_forward, self.plan, t, t if used is None else used, at, at + 24, *rest, at + 48, at + 72,
+            stream=stream)
+        return q_out, k_out
+
+    def backward(self, q, k, positions, dq_out, dk_out, q_weight=None, k_weight=None, dq=None, dk=None,
+                 used: Optional[int] = None, weights: bool = True, stream=None):
+        """(dq, dk, dq_weight, dk_weight) from the gradients of ``forward``'s
+        results.  A weight that is None has no gradient (None); with ``weights``
+        False neither has."""
+        t, h, hk, device = q.shape[0], self.n_heads, self.n_kv_heads, q.device
+        check = self._check
+        args = (*check(q, "q", t, h, device), *check(k, "k", t, hk, device), *check(dq_out, "dq_out", t, h, device),
+                *check(dk_out, "dk_out", t, hk, device))
+        rest = self._rest(positions, q_weight, k_weight, t, device)
+        _used_on(stream, q, k, positions, dq_out, dk_out, q_weight, k_weight, dq, dk)
+        if dq is None:
+            dq = _empty((t, h, self.head_dim), self.dtype, device, stream)
+        if dk is None:
+            dk = _empty((t, hk, self.head_dim), self.dtype, device, stream)
+        new = lambda w: None if w is None or not weights else _empty((self.head_dim,), w.dtype, device, stream)  # noqa: E731
+        dqw, dkw = new(q_weight), new(k_weight)
+        work = None
+        if dqw is not None or dkw is not None:
+            work = _empty((self._bytes,), torch.uint8, device, stream)
+        heads = (ctypes.c_int64 * 18)(*args, *check(dq, "dq", t, h, device), *check(dk, "dk", t, hk, device))
+        at = ctypes.addressof(heads)
+        ptr = lambda x: 0 if x is None else x.data_ptr()  # noqa: E731
+        _on(device, C.normpre_qkrot_backward, self.plan, t, t if used is None else used, at, at + 24, *rest, at + 48,
+            at + 72, at + 96, at + 120, ptr(dqw), ptr(dkw), ptr(work), stream=stream)
+        return dq, dk, dqw, dkw
+
+    def __call__(self, q, k, positions=None, q_weight=None, k_weight=None, used: Optional[int] = None):
+        """The differentiable form."""
+        return _QKNormRotary.apply(self, q, k, positions, q_weight, k_weight, used)
+
+    def close(self) -> None:
+        if self.plan:
+            C.normpre_qkrot_free(self.plan)
+            self.plan = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class _QKNormRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, plan, q, k, positions, q_weight, k_weight, used):
+        ctx.plan, ctx.used = plan, used
+        ctx.save_for_backward(q, k, positions, q_weight, k_weight)
+        return plan.forward(q, k, positions, q_weight, k_weight, used=used)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        q, k, positions, q_weight, k_weight = ctx.saved_tensors
+        dq, dk, dqw, dkw = ctx.plan.backward(q, k, positions, _aligned(dq_out), _aligned(dk_out), q_weight, k_weight,
+                                             used=ctx.used, weights=any(ctx.needs_input_grad[4:6]))
+        return None, dq, dk, None, dqw, dkw, None
 
 
 # ---------------------------------------------------------------------------

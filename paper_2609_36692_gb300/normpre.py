@@ -72,6 +72,19 @@ class normpre_heads(ctypes.Structure):
     ]
 
 
+class normpre_qkrot_config(ctypes.Structure):
+    _fields_ = [
+        ("n_heads", ctypes.c_int),
+        ("n_kv_heads", ctypes.c_int),
+        ("head_dim", ctypes.c_int),
+        ("rotary_dim", ctypes.c_int),
+        ("interleaved", ctypes.c_int),
+        ("norm", ctypes.c_int),
+        ("dtype", ctypes.c_int),
+        ("eps", ctypes.c_float),
+    ]
+
+
 class NormPreError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__("%s: %s" % (STATUS_NAMES.get(status, status), message))
@@ -141,6 +154,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                  "ckpt_sync_status"):
         getattr(lib, "normpre_" + name).restype = ctypes.c_int
     lib.normpre_attn_free.restype = None
+    lib.normpre_qkrot_init.argtypes = [ctypes.POINTER(normpre_qkrot_config), ctypes.POINTER(ctypes.c_double),
+                                       ctypes.POINTER(P)]
+    lib.normpre_qkrot_bytes.argtypes = [P, ctypes.POINTER(i64)]
+    lib.normpre_qkrot_forward.argtypes = [P, i64, i64, HP, HP, P, i32, P, P, i32, HP, HP, P]
+    lib.normpre_qkrot_backward.argtypes = [P, i64, i64, HP, HP, P, i32, P, P, i32, HP, HP, HP, HP, P, P, P, P]
+    lib.normpre_qkrot_free.argtypes = [P]
+    lib.normpre_qkrot_free.restype = None
+    lib.normpre_grad_bytes.argtypes = [i32, ctypes.POINTER(i64)]
+    lib.normpre_grad_norm.argtypes = [i32, P, P, P, P, P, P]
+    lib.normpre_grad_clip.argtypes = [i32, P, P, P, P, P, ctypes.c_float, ctypes.c_float, P, P, P]
+    for name in ("qkrot_init", "qkrot_bytes", "qkrot_forward", "qkrot_backward", "grad_bytes", "grad_norm", "grad_clip"):
+        getattr(lib, "normpre_" + name).restype = ctypes.c_int
     lib.normpre_free.argtypes = [P]
     lib.normpre_free.restype = None
     lib.normpre_last_error.argtypes = [P]
@@ -336,6 +361,66 @@ def normpre_ckpt_swiglu_backward(tokens: int, features: int, dtype: int, gate_co
 def normpre_ckpt_sync_status(stream: int = 0, raise_on_error: bool = True) -> int:
     rc = load_library().normpre_ckpt_sync_status(stream)
     return _check(rc) if raise_on_error else rc
+
+
+def normpre_qkrot_init(cfg: normpre_qkrot_config, frequencies: Sequence[float]) -> int:
+    h = ctypes.c_void_p()
+    f = (ctypes.c_double * max(1, len(frequencies)))(*[float(x) for x in frequencies])
+    if len(frequencies) != max(0, cfg.rotary_dim // 2):
+        raise ValueError("rotary_dim / 2 = %d frequencies are needed (got %d)" % (cfg.rotary_dim // 2, len(frequencies)))
+    _check(load_library().normpre_qkrot_init(ctypes.byref(cfg), f, ctypes.byref(h)))
+    return h.value
+
+
+def normpre_qkrot_bytes(plan: int) -> int:
+    n = ctypes.c_int64()
+    _check(load_library().normpre_qkrot_bytes(plan, ctypes.byref(n)))
+    return n.value
+
+
+def normpre_qkrot_forward(plan: int, tokens: int, used: int, q, k, positions: int, position_bytes: int, q_weight: int,
+                          k_weight: int, weight_dtype: int, q_out, k_out, stream: int = 0) -> int:
+    """q, k, q_out, k_out: ``normpre_heads`` or their addresses."""
+    return _check(load_library().normpre_qkrot_forward(plan, tokens, used, _by_ref(q), _by_ref(k), positions,
+                                                       position_bytes, q_weight, k_weight, weight_dtype,
+                                                       _by_ref(q_out), _by_ref(k_out), stream))
+
+
+def normpre_qkrot_backward(plan: int, tokens: int, used: int, q, k, positions: int, position_bytes: int, q_weight: int,
+                           k_weight: int, weight_dtype: int, dq_out, dk_out, dq, dk, dq_weight: int, dk_weight: int,
+                           workspace: int, stream: int = 0) -> int:
+    """q, k, dq_out .. dk: ``normpre_heads`` or their addresses."""
+    return _check(load_library().normpre_qkrot_backward(plan, tokens, used, _by_ref(q), _by_ref(k), positions,
+                                                        position_bytes, q_weight, k_weight, weight_dtype,
+                                                        _by_ref(dq_out), _by_ref(dk_out), _by_ref(dq), _by_ref(dk),
+                                                        dq_weight, dk_weight, workspace, stream))
+
+
+def normpre_qkrot_free(plan: int) -> None:
+    if plan:
+        load_library().normpre_qkrot_free(plan)
+
+
+def normpre_grad_bytes(n: int) -> int:
+    b = ctypes.c_int64()
+    _check(load_library().normpre_grad_bytes(n, ctypes.byref(b)))
+    return b.value
+
+
+def normpre_grad_norm(grads: Sequence[int], dtypes: Sequence[int], sizes: Sequence[int], norm_ptr: int,
+                      workspace: int, stream: int = 0) -> int:
+    n = len(grads)
+    return _check(load_library().normpre_grad_norm(n, (ctypes.c_void_p * n)(*grads), (ctypes.c_int * n)(*dtypes),
+                                                   (ctypes.c_int64 * n)(*sizes), norm_ptr, workspace, stream))
+
+
+def normpre_grad_clip(grads: Sequence[int], dtypes: Sequence[int], sizes: Sequence[int], out: Sequence[int],
+                      out_dtypes: Sequence[int], max_norm: float, eps: float, norm_ptr: int, workspace: int,
+                      stream: int = 0) -> int:
+    n = len(grads)
+    P, I = ctypes.c_void_p * n, ctypes.c_int * n
+    return _check(load_library().normpre_grad_clip(n, P(*grads), I(*dtypes), (ctypes.c_int64 * n)(*sizes), P(*out),
+                                                   I(*out_dtypes), max_norm, eps, norm_ptr, workspace, stream))
 
 
 def normpre_free(handle: int) -> None:

@@ -3,6 +3,8 @@
 ``NormPre`` keeps one library handle for a fixed list of matrices and turns
 lists of torch tensors into the pointer arrays the ABI takes (and the current
 CUDA stream into its ``stream`` argument).  It does no arithmetic of its own.
+``clip_grad_norm_``, ``clip_grads`` and ``grad_norm`` are the global norm of
+gradients before the step.
 """
 from __future__ import annotations
 
@@ -204,6 +206,85 @@ class NormPreOptimizer(_torch_optimizer_base()):
                 plan.close()
             except Exception:
                 pass
+
+
+def _dense(x) -> bool:
+    """Whether a tensor fills its memory without gaps, in whatever order."""
+    if x.is_contiguous():
+        return True
+    order = sorted(range(x.dim()), key=x.stride, reverse=True)
+    return x.permute(order).is_contiguous()
+
+
+def _grad_lists(grads, name: str = "gradient"):
+    """Checks gradients and returns their pointers, dtype codes and sizes."""
+    import torch
+    codes = {torch.float32: C.NORMPRE_F32, torch.bfloat16: C.NORMPRE_BF16}
+    device = grads[0].device
+    for i, g in enumerate(grads):
+        if not g.is_cuda or g.device != device or g.layout != torch.strided:
+            raise ValueError("%s %d: all must be dense CUDA tensors on one device" % (name, i))
+        if g.dtype not in codes:
+            raise TypeError("%s %d: unsupported dtype %s (float32 or bfloat16)" % (name, i, g.dtype))
+        if not _dense(g):
+            raise ValueError("%s %d: its memory must have no gaps" % (name, i))
+    return [g.data_ptr() for g in grads], [codes[g.dtype] for g in grads], [g.numel() for g in grads]
+
+
+def _grad_call(device, f, *args):
+    """f(*args, norm, workspace, stream) on the gradients' device; returns the norm."""
+    import torch
+    with torch.cuda.device(device):
+        norm = torch.empty((), dtype=torch.float32, device=device)
+        work = torch.empty(C.normpre_grad_bytes(len(args[0])), dtype=torch.uint8, device=device)
+        f(*args, norm.data_ptr(), work.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    return norm
+
+
+def grad_norm(grads):
+    """The norm of a list of CUDA tensors (fp32 or bf16) taken as one vector, as
+    an fp32 scalar on their device.  Nothing is waited for."""
+    import torch
+    grads = list(grads)
+    if not grads:
+        return torch.zeros((), dtype=torch.float32, device="cuda")
+    return _grad_call(grads[0].device, C.normpre_grad_norm, *_grad_lists(grads))
+
+
+def clip_grads(grads, max_norm: float, eps: float = 1e-6, out=None):
+    """Scales gradients by min(1, max_norm / (norm + eps)) and returns their norm
+    (``grad_norm``) before that.  In place, or into the tensors of ``out`` (their
+    dtypes may differ: gradients summed in fp32, clipped ones in bf16 for the
+    step).  In place nothing is written where the norm is below the limit.  A
+    tensor may be listed once only."""
+    import torch
+    grads = list(grads)
+    if not grads:
+        return torch.zeros((), dtype=torch.float32, device="cuda")
+    lists = _grad_lists(grads)
+    if out is None:
+        to = lists
+    else:
+        out = list(out)
+        if len(out) != len(grads):
+            raise ValueError("out must have a tensor for each gradient")
+        to = _grad_lists(out, "out")
+        for i, (g, o) in enumerate(zip(grads, out)):
+            if o.shape != g.shape or o.device != g.device:
+                raise ValueError("out %d must have its gradient's shape and device" % i)
+            if o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()):
+                raise ValueError("out %d must have its gradient's strides" % i)
+    return _grad_call(grads[0].device, C.normpre_grad_clip, *lists, to[0], to[1], float(max_norm), float(eps))
+
+
+def clip_grad_norm_(parameters, max_norm: float, eps: float = 1e-6):
+    """Clips the gradients of parameters (or one) in place by their global norm,
+    and returns it: ``clip_grads`` of their ``.grad``, between the backward pass
+    and the optimizers' steps."""
+    import torch
+    if isinstance(parameters, torch.Tensor):
+        parameters = [parameters]
+    return clip_grads([p.grad for p in parameters if p.grad is not None], max_norm, eps)
 
 
 def newton_schulz(X, **config):
