@@ -414,6 +414,18 @@ typedef struct normpre_heads {
 int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out);
 
 /*
+ * A plan whose rows see a window of the rows before them and the sequence's
+ * first rows: j runs over the rows up to i with i - j < window or j < sinks (rows
+ * counted from the sequence's first).  window = 0: all rows up to i, as
+ * normpre_attn_init; sinks then change nothing.  All other calls are the same.
+ * The work grows with window + sinks instead of the sequence's length.  A
+ * non-finite value of token j reaches, besides the rows that see it, the rows of
+ * every aligned block of 128 rows that has a row which sees one of j's block.
+ * Errors: as normpre_attn_init; ARG for a negative window or sinks.
+ */
+int normpre_attn_init_window(const normpre_attn_config* cfg, int64_t window, int64_t sinks, normpre_attn** out);
+
+/*
  * The lengths of the next pack: lengths[s] >= 0 rows for sequence s (host
  * array; zero-length sequences are allowed, n_seqs = 0 is an empty pack).
  * Work lists are rebuilt on the host and copied on `stream`: calls made before

@@ -31,6 +31,8 @@ struct normpre_attn {
   char* staging = nullptr;         // pinned, the same size
   cudaEvent_t copied = nullptr;    // the last copy out of `staging`
   cudaStream_t list_stream = nullptr;   // where it ran; calls there are in order with it
+  int window = 0, sinks = 0;       // of the plan (0: none), and what the current lengths need of them
+  int now_window = kNoWindow, now_sinks = 0;
   bool used = false, elsewhere = false;   // calls since: any, on other streams
   int64_t walk_at[3] = {-1, -1, -1};   // byte offsets of the walks, -1: none
   float* delta = nullptr;          // [n_heads][max_tokens]
@@ -89,6 +91,8 @@ AttnArgs base_args(const normpre_attn* a, int64_t tokens) {
   g.kv_heads = a->cfg.n_kv_heads;
   g.group = a->cfg.n_heads / a->cfg.n_kv_heads;
   g.dim = a->cfg.head_dim;
+  g.window = a->now_window;
+  g.sinks = a->now_sinks;
   g.scale = a->cfg.scale;
   g.scale_log2 = a->cfg.scale * 1.4426950408889634f;
   g.delta = a->delta;
@@ -157,6 +161,11 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
     if (lengths[i] > a->cfg.max_tokens - total) return fail(NORMPRE_ERR_SHAPE, "the lengths exceed max_tokens");
     total += lengths[i];
   }
+  // a window that no sequence is longer than hides nothing
+  int64_t longest = 0;
+  for (int i = 0; i < n_seqs; ++i) longest = std::max(longest, lengths[i]);
+  const bool windowed = a->window && a->window < longest;
+  const int window = windowed ? a->window : kNoWindow, sinks = windowed ? a->sinks : 0;
   std::vector<AttnBlock> blocks;
   int64_t start = 0;
   for (int i = 0; i < n_seqs; ++i) {
@@ -165,8 +174,10 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
     start += lengths[i];
   }
   // longest work first
-  auto queries = [](const AttnBlock& b) { return (b.len - 1) / 128 - b.blk; };
-  std::stable_sort(blocks.begin(), blocks.end(), [](const AttnBlock& x, const AttnBlock& y) { return x.blk > y.blk; });
+  auto keys = [&](const AttnBlock& b, int top) { return key_span(b.blk, window, sinks).count(top); };
+  auto queries = [&](const AttnBlock& b) { return last_query(b.blk, b.len, window, sinks) - b.blk; };
+  std::stable_sort(blocks.begin(), blocks.end(),
+                   [&](const AttnBlock& x, const AttnBlock& y) { return keys(x, x.blk) > keys(y, y.blk); });
   std::vector<AttnBlock> by_key = blocks, pairs;
   std::stable_sort(by_key.begin(), by_key.end(),
                    [&](const AttnBlock& x, const AttnBlock& y) { return queries(x) > queries(y); });
@@ -179,9 +190,9 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
     std::vector<int> fwd, dkdv, dq;
     const bool heads = attn_pair_heads(group);
     for (const AttnBlock& b : heads ? blocks : pairs)
-      fwd.push_back(2 * (b.blk + 1) + (heads ? 2 : (b.blk + 1) * 128 < b.len ? 4 : 2));
+      fwd.push_back(2 * keys(b, heads || (b.blk + 1) * 128 >= b.len ? b.blk : b.blk + 1) + 2);
     for (const AttnBlock& b : by_key) dkdv.push_back(group * (queries(b) + 1) + 1);
-    for (const AttnBlock& b : blocks) dq.push_back(b.blk + 2);
+    for (const AttnBlock& b : blocks) dq.push_back(keys(b, b.blk) + 1);
     deal(fwd, heads ? h / 2 : h, &walk[0]);
     deal(dkdv, hk, &walk[1]);
     deal(dq, h, &walk[2]);
@@ -212,6 +223,8 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
   a->n_pairs = static_cast<int>(pairs.size());
   std::copy(walk_at, walk_at + 3, a->walk_at);
   a->total = total;
+  a->now_window = window;
+  a->now_sinks = sinks;
   return NORMPRE_OK;
 }
 
@@ -220,6 +233,10 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
 extern "C" {
 
 int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out) {
+  return normpre_attn_init_window(cfg, 0, 0, out);
+}
+
+int normpre_attn_init_window(const normpre_attn_config* cfg, int64_t window, int64_t sinks, normpre_attn** out) {
   if (!cfg || !out) return fail(NORMPRE_ERR_ARG, "null argument");
   *out = nullptr;
   if (cfg->dtype != NORMPRE_F32 && cfg->dtype != NORMPRE_BF16)
@@ -231,10 +248,14 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out) {
   if (cfg->max_tokens < 1 || cfg->max_tokens > (int64_t(1) << 24) || cfg->max_seqs < 1 || cfg->max_seqs > 65536)
     return fail(NORMPRE_ERR_SHAPE, "max_tokens must be in [1, 2^24] and max_seqs in [1, 65536]");
   if (!std::isfinite(cfg->scale) || cfg->scale < 0.f) return fail(NORMPRE_ERR_ARG, "scale must be finite and >= 0");
+  if (window < 0 || sinks < 0) return fail(NORMPRE_ERR_ARG, "window and sinks must be >= 0");
   if (cfg->test_stall != 0 && cfg->test_stall != 1) return fail(NORMPRE_ERR_ARG, "test_stall must be 0 or 1");
   try {
     std::unique_ptr<normpre_attn, Release> a(new normpre_attn());
     a->cfg = *cfg;
+    // beyond max_tokens there is nothing that a window hides or a sink shows
+    a->window = window < cfg->max_tokens ? static_cast<int>(window) : 0;
+    a->sinks = a->window ? static_cast<int>(std::min(sinks, cfg->max_tokens)) : 0;
     if (a->cfg.scale == 0.f) a->cfg.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(cfg->head_dim)));
     a->max_blocks = cfg->max_tokens / 128 + std::min<int64_t>(cfg->max_seqs, cfg->max_tokens);
     cudaError_t e = cudaGetDevice(&a->device);

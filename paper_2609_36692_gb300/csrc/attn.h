@@ -29,6 +29,32 @@ __host__ __device__ inline bool block_fits(const AttnBlock& b, int total) {
          b.blk <= (b.len - 1) / 128;
 }
 
+// Which blocks of 128 keys a block of 128 queries meets, and the other way
+// round.  Row i sees keys j <= i with i - j < window or j < sinks: a query block
+// meets the sinks' blocks [0, sink) and then [lo, blk] (sink <= lo), a key block
+// the query blocks blk .. last.  Without a window (kNoWindow): all up to blk.
+constexpr int kNoWindow = 1 << 25;   // beyond every distance of two rows
+struct KeySpan {
+  int lo, sink;
+  __host__ __device__ int count(int blk) const { return blk - lo + 1 + sink; }
+  // the block before j, on the way down; -1: none
+  __host__ __device__ int down(int j) const { return j > lo || j <= sink ? j - 1 : sink - 1; }
+  // the block after j, on the way up
+  __host__ __device__ int up(int j) const { return j + 1 == sink ? lo : j + 1; }
+  __host__ __device__ int first() const { return sink ? 0 : lo; }
+};
+__host__ __device__ inline KeySpan key_span(int blk, int window, int sinks) {
+  KeySpan s;
+  const int below = 128 * blk - window + 1, ends = (sinks + 127) / 128;
+  s.lo = below > 0 ? below / 128 : 0;
+  s.sink = ends < s.lo ? ends : s.lo;
+  return s;
+}
+__host__ __device__ inline int last_query(int blk, int len, int window, int sinks) {
+  const int last = (len - 1) / 128, in = (128 * blk + 126 + window) / 128;
+  return 128 * blk < sinks || last < in ? last : in;
+}
+
 typedef HeadsView AttnTensor;
 
 struct AttnArgs {
@@ -44,6 +70,7 @@ struct AttnArgs {
   int total;                 // rows that belong to sequences
   int tokens;
   int heads, kv_heads, group, dim;
+  int window, sinks;         // kNoWindow, 0: none, or none that the lengths reach
   float scale;               // c
   float scale_log2;          // c log2(e): exp(c x) = exp2(scale_log2 x)
   int* flags;                // pinned host memory

@@ -253,7 +253,8 @@ __device__ __forceinline__ bool get_item(const ItemRef& b, Item& it) {
   return true;
 }
 
-template <int DP>
+// WIN: the rows have a window.
+template <int DP, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_constant__ BwdArgs f) {
   using B = Bwd<DP>;
   constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks, kSets = B::kSets;
@@ -265,6 +266,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   static_assert(sizeof(Bars<kSlots>) <= 512, "barriers");
   ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
   const AttnArgs& a = f.a;
+  // query blocks of an item and head
+  auto queries = [&](const Item& it) {
+    return (WIN ? last_query(it.blk, it.len, a.window, a.sinks) : (it.len - 1) / kTile) - it.blk + 1;
+  };
   auto find = [&](int64_t r) { return list_item(a, a.by_key, a.n_blocks, a.walk_dkdv, a.kv_heads, r); };
   auto item = [&](int64_t r) { return r < kCached ? items[r] : find(r); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -291,8 +296,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
         if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.k, &f.v, row, it.head, kChunks)) break;
+        const int end = it.blk + queries(it);
         for (int g = 0; g < a.group && w.ok; ++g)
-          for (int i = it.blk; i * kTile < it.len && w.ok; ++i) {
+          for (int i = it.blk; i < end && w.ok; ++i) {
             const int64_t qrow = it.start + static_cast<int64_t>(kTile) * i;
             const bool tail = kTile * (i + 1) > it.len;
             w.load(ring, kTileBytes, &f.q, qrow, it.head * a.group + g, kChunks, tail);
@@ -310,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
       int st = 0;                                                 // parity of the block in the walk
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
-        const int n = ((it.len - 1) / kTile - it.blk + 1) * a.group;
+        const int n = queries(it) * a.group;
         const uint32_t k = tc::su32(own + 2 * set.i * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][0], set.parity)) break;
         int q = w.take();
@@ -348,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
       uint32_t ds_phase = 0;
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
-        const int n = ((it.len - 1) / kTile - it.blk + 1) * a.group;
+        const int n = queries(it) * a.group;
         const uint32_t v = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
         int q = w.take(), o = w.take();
@@ -383,10 +389,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     Turn<2> st;
     uint32_t seen = 0;
     int slot = 0;
-    for (int64_t r = 0; w.ok && get_item(item(r), it); ++r)
+    for (int64_t r = 0; w.ok && get_item(item(r), it); ++r) {
+      const int end = min(it.len, kTile * (it.blk + queries(it)));
       for (int g = 0; g < a.group && w.ok; ++g) {
         const int64_t base = static_cast<int64_t>(it.head * a.group + g) * a.tokens + it.start;
-        for (int i = it.blk * kTile; i < it.len; i += kTile) {
+        for (int i = it.blk * kTile; i < end; i += kTile) {
           float ls[4], de[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -410,6 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
           st.next();
         }
       }
+    }
   } else {
     // ---------------- softmax ----------------
     const int part = warp >> 2, row = 32 * (warp & 3) + lane;    // columns 32 part .., row of the tile
@@ -419,11 +427,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     uint32_t phase = 0;
     Turn<2> st;
     for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
-      const int nq = (it.len - 1) / kTile - it.blk + 1, n = nq * a.group;
+      const int nq = queries(it), n = nq * a.group;
       for (int i = 0; i < n; ++i) {
         const float* ls = stat + st.i * 256 + 32 * part;
         if (!w.wait(&b->s_full[st.i], st.parity)) break;
-        const bool diag = i % nq == 0;
+        const int up = i % nq;                   // blocks between the keys and the queries
+        const bool diag = up == 0;
+        // the window's end crosses the tile, and not only over sinks
+        const bool edge = WIN && kTile * (up + 1) > a.window && kTile * (it.blk + 1) > a.sinks;
+        // the tile's queries that do not see key `row`, a bit for each column
+        uint32_t hide = 0;
+        if (WIN && (diag || edge)) {
+          hide = below_bits(row - kTile * up - 32 * part);
+          if (kTile * it.blk + row >= a.sinks) hide |= ~below_bits(row + a.window - kTile * up - 32 * part);
+        }
         float p[32];
         uint32_t pk[16];
         uint32_t x[32];
@@ -438,7 +455,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
 #pragma unroll
           for (int u = 0; u < 4; ++u) p[e + u] = tc::exp2_fast(y[u]);
         }
-        if (diag) {   // key `row` is seen by queries row ..
+        if constexpr (WIN) {
+          if (diag || edge) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (hide >> e & 1u) p[e] = 0.f;
+          }
+        } else if (diag) {   // key `row` is seen by queries row ..
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             if (32 * part + e < row) p[e] = 0.f;
@@ -461,7 +484,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
             pk[(e + u) / 2] = pack_bf16x2(p[e + u] * (__uint_as_float(x[e + u]) - d4[u]),
                                           p[e + u + 1] * (__uint_as_float(x[e + u + 1]) - d4[u + 1]));
         }
-        if (diag) {   // 0 * NaN in an unseen place
+        if constexpr (WIN) {
+          if (diag || edge) {   // 0 * NaN in an unseen place
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              if (hide >> (2 * e) & 1u) pk[e] &= 0xFFFF0000u;
+              if (hide >> (2 * e + 1) & 1u) pk[e] &= 0x0000FFFFu;
+            }
+          }
+        } else if (diag) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             if (32 * part + 2 * e < row) pk[e] &= 0xFFFF0000u;
@@ -486,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   finish(w, warp, a.flags);
 }
 
-template <int DP>
+template <int DP, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constant__ BwdArgs f) {
   using B = Bwd<DP>;
   constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks, kSets = B::kSets;
@@ -496,6 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(ring + kSlots * kTileBytes);
   ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
   const AttnArgs& a = f.a;
+  auto keys = [&](const Item& it) { return WIN ? key_span(it.blk, a.window, a.sinks) : KeySpan{0, 0}; };
   auto find = [&](int64_t r) { return list_item(a, a.by_query, a.n_blocks, a.walk_dq, a.heads, r); };
   auto item = [&](int64_t r) { return r < kCached ? items[r] : find(r); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -523,7 +555,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
         if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.q, &f.dout, row, it.head, kChunks)) break;
-        for (int j = 0; j <= it.blk && w.ok; ++j) {
+        const KeySpan span = keys(it);
+        for (int j = span.first(); j <= it.blk && w.ok; j = WIN ? span.up(j) : j + 1) {
           const int64_t krow = it.start + static_cast<int64_t>(kTile) * j;
           w.load(ring, kTileBytes, &f.k, krow, it.head / a.group, kChunks, kTile * (j + 1) > it.len);
           if (w.ok) w.load(ring, kTileBytes, &f.v, krow, it.head / a.group, kChunks, false);
@@ -538,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       uint32_t ds_phase = 0;                                      // a bit per buffer
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
-        const int n = it.blk + 1;
+        const int n = keys(it).count(it.blk);
         const uint32_t q = tc::su32(own + 2 * set.i * kTileBytes);
         int k[2] = {0, 0};                                        // ring slots of K(j), K(j + 1)
         auto scores = [&](int j, int& slot) {
@@ -579,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const uint32_t o = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
-        for (int j = 0; j <= it.blk; ++j) {
+        for (int n = keys(it).count(it.blk); n > 0; --n) {
           w.next();
           const int v = w.take();
           // free once the last block's dP has been read
@@ -588,7 +621,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
           product_ss<DP>(cP, o, tc::su32(ring + v * kTileBytes));
           tc::mma_commit(&b->dp_full);
           tc::mma_commit(&b->empty[v]);
-          if (j == it.blk) tc::mma_commit(&b->own_empty[set.i]);
+          if (n == 1) tc::mma_commit(&b->own_empty[set.i]);
         }
       }
       w.drain(1);
@@ -600,9 +633,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     uint32_t seen = 0;
     int next = 0;                                                 // ring slot of the item's first tile
     for (int64_t r = 0; w.ok && get_item(item(r), it); ++r) {
-      const int rows = it.len - kTile * it.blk;
-      if (rows < kTile) w.end_tile(ring, kTileBytes, (next + 2 * it.blk) % kSlots, seen, rows, kChunks);
-      next = (next + 2 * (it.blk + 1)) % kSlots;
+      const int rows = it.len - kTile * it.blk, n = keys(it).count(it.blk);
+      if (rows < kTile) w.end_tile(ring, kTileBytes, (next + 2 * (n - 1)) % kSlots, seen, rows, kChunks);
+      next = (next + 2 * n) % kSlots;
     }
   } else {
     // ---------------- softmax ----------------
@@ -617,7 +650,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       const int64_t si = static_cast<int64_t>(it.head) * a.tokens + at + row;
       const float ls = in ? -a.lse[si] : -INFINITY, de = in ? a.delta[si] : 0.f;
       const uint64_t ls2 = tc::pack2(ls, ls);
-      for (int j = 0; j <= it.blk; ++j, buf.next()) {
+      const KeySpan span = keys(it);
+      for (int j = span.first(); j <= it.blk; j = WIN ? span.up(j) : j + 1, buf.next()) {
         const uint32_t mS = cS + 128 * buf.i + lanes + 32 * part, mP = cP + lanes + 32 * part;
         if (!w.wait(&b->s_full[buf.i], buf.parity)) break;
         float p[32];
@@ -640,7 +674,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
 #pragma unroll
         for (int e = 0; e < 32; e += 2)
           pk[e / 2] = pack_bf16x2(p[e] * (__uint_as_float(x[e]) - de), p[e + 1] * (__uint_as_float(x[e + 1]) - de));
-        if (j == it.blk) {   // query `row` sees keys .. row
+        if constexpr (WIN) {
+          if (kTile * (it.blk - j + 1) > a.window || j == it.blk) {
+            const int up = kTile * (it.blk - j) - 32 * part;
+            const uint32_t hide = hidden_bits(up + row, up + row - a.window + 1, a.sinks - kTile * j - 32 * part);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              if (hide >> (2 * e) & 1u) pk[e] &= 0xFFFF0000u;
+              if (hide >> (2 * e + 1) & 1u) pk[e] &= 0x0000FFFFu;
+            }
+          }
+        } else if (j == it.blk) {   // query `row` sees keys .. row
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             if (32 * part + 2 * e > row) pk[e] &= 0xFFFF0000u;
@@ -667,6 +711,12 @@ cudaError_t launch(const BwdArgs& f, int heads, size_t smem, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+template <int DP, bool WIN>
+cudaError_t both(const BwdArgs& f, cudaStream_t s) {
+  const cudaError_t e = launch<k_attn_dkdv_tc<DP, WIN>>(f, f.a.kv_heads, Bwd<DP>::kSmem, s);
+  return e ? e : launch<k_attn_dq_tc<DP, WIN>>(f, f.a.heads, Bwd<DP>::kSmem, s);
+}
+
 }  // namespace
 
 cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t s, std::string* err) {
@@ -676,13 +726,8 @@ cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t s, std::stri
       !rows_map(&f.v, a.v, a.tokens, a.kv_heads, a.dim, err) ||
       !rows_map(&f.dout, a.dout, a.tokens, a.heads, a.dim, err))
     return cudaErrorInvalidValue;
-  cudaError_t e;
-  if (a.dim <= 64) {
-    e = launch<k_attn_dkdv_tc<64>>(f, a.kv_heads, Bwd<64>::kSmem, s);
-    return e ? e : launch<k_attn_dq_tc<64>>(f, a.heads, Bwd<64>::kSmem, s);
-  }
-  e = launch<k_attn_dkdv_tc<128>>(f, a.kv_heads, Bwd<128>::kSmem, s);
-  return e ? e : launch<k_attn_dq_tc<128>>(f, a.heads, Bwd<128>::kSmem, s);
+  if (a.window < kNoWindow) return a.dim <= 64 ? both<64, true>(f, s) : both<128, true>(f, s);
+  return a.dim <= 64 ? both<64, false>(f, s) : both<128, false>(f, s);
 }
 
 }  // namespace normpre

@@ -76,6 +76,7 @@ struct Item {
   int64_t start;   // the sequence's first row
   int len;
   int top;         // the topmost block of keys
+  KeySpan span;    // below it: the blocks that tile 0 meets, which include tile 1's
   int blk0, blk1;  // the tiles' block in the sequence, -1: no tile
   int head0, head1;
   int kvh;
@@ -102,11 +103,14 @@ __device__ __forceinline__ bool get_item(const FwdArgs& f, const ItemRef* cached
     it.head0 = it.head1 = b.head;
   }
   it.top = max(it.blk0, it.blk1);
+  it.span = key_span(it.blk0, f.a.window, f.a.sinks);
   it.kvh = it.head0 / f.a.group;
   return true;
 }
 
-template <int DP>
+// WIN: the rows have a window (else the spans are whole and nothing is hidden
+// but by the diagonal).
+template <int DP, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_constant__ FwdArgs f) {
   using F = Fwd<DP>;
   constexpr int kSlots = F::kSlots, kTileBytes = F::kTileBytes, kChunks = F::kChunks, kAcc = F::kAcc;
@@ -191,10 +195,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
             }
             if (s == 0) load(&f.k, it.start + static_cast<int64_t>(kTile) * it.top, it.kvh, false);
           }
-          for (int j = it.top; j >= 0 && ok; --j) {
-            const int64_t row = it.start + static_cast<int64_t>(kTile) * j;
-            load(&f.v, row, it.kvh, kTile * (j + 1) > it.len);
-            if (j > 0) load(&f.k, row - kTile, it.kvh, false);
+          for (int j = it.top, next; j >= 0 && ok; j = next) {
+            next = WIN ? it.span.down(j) : j - 1;
+            load(&f.v, it.start + static_cast<int64_t>(kTile) * j, it.kvh, kTile * (j + 1) > it.len);
+            if (next >= 0) load(&f.k, it.start + static_cast<int64_t>(kTile) * next, it.kvh, false);
           }
         }
       }
@@ -217,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           zero_tail(ring + slot * kTileBytes, rows, kChunks, lane);
           if (lane == 0) tc::mbar_arrive(&b->full[slot]);
         }
-        next = (next + 2 * (it.top + 1)) % kSlots;
+        next = (next + 2 * (WIN ? it.span.count(it.top) : it.top + 1)) % kSlots;
       }
     } else {
       // ---------------- MMA of one tile (one thread) ----------------
@@ -260,23 +264,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
         };
         for (int64_t r = 0; ok && get_item(f, items, r, it); ++r) {
           const int blk = s ? it.blk1 : it.blk0;
+          // this tile's own span, which may leave out the lowest of tile 0's window,
+          // and the last block that it meets
+          const KeySpan own = WIN && blk >= 0 ? key_span(blk, f.a.window, f.a.sinks) : KeySpan{0, 0};
+          const int last = WIN ? own.first() : 0;
+          auto meets = [&](int j) { return j <= blk && (!WIN || j >= own.lo || j < own.sink); };
           int k = take();
           if (blk >= 0 && !wait(&b->q_full[s], q_phase)) break;
           if (blk >= 0) q_phase ^= 1u;
           if (!ok || !my_turn()) break;
           if (it.top == blk) {
             scores(k);
-            if (blk == 0) tc::mma_commit(&b->q_empty[s]);
+            if (blk == last) tc::mma_commit(&b->q_empty[s]);
           } else {
             tc::mbar_arrive(&b->empty[k]);
             pass_turn();
           }
-          for (int j = it.top; j >= 0; --j) {
+          for (int j = it.top, next; j >= 0; j = next) {
+            next = WIN ? it.span.down(j) : j - 1;
             const int v = take();
-            if (j > 0) k = take();
+            if (next >= 0) k = take();
             if (!ok) break;
             const uint32_t o = o_col(s, acc), p = s_col(s);
-            if (j <= blk) {
+            if (meets(j)) {
               if (j == blk) {
                 if (!wait(&b->o_empty[s][acc], ((o_phase >> acc) & 1u) ^ 1u)) break;
                 o_phase ^= 1u << acc;
@@ -292,11 +302,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
               if (!my_turn()) break;
               tc::mbar_arrive(&b->empty[v]);
             }
-            if (j > 0 && j - 1 <= blk) {
+            if (next >= 0 && meets(next)) {
               scores(k);
-              if (j == 1) tc::mma_commit(&b->q_empty[s]);
+              if (next == last) tc::mma_commit(&b->q_empty[s]);
             } else {
-              if (j > 0) tc::mbar_arrive(&b->empty[k]);
+              if (next >= 0) tc::mbar_arrive(&b->empty[k]);
               pass_turn();
             }
           }
@@ -331,7 +341,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       if (blk < 0) continue;
       const uint32_t oc = o_col(s, acc) + lanes;
       float m = -INFINITY, l = 0.f;
-      for (int j = blk; j >= 0; --j) {
+      const KeySpan own = WIN ? key_span(blk, f.a.window, f.a.sinks) : KeySpan{0, 0};
+      for (int j = blk; j >= 0; j = WIN ? own.down(j) : j - 1) {
         if (!wait(&b->s_full[s], s_phase)) break;
         s_phase ^= 1u;
         uint32_t x[32];                 // a quarter of the row's scores
@@ -342,10 +353,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           tc::tmem_ld32(sc + 32 * q, x);
           tc::tmem_ld_wait();
         };
+        // the window's end crosses the block for some row, and not only over sinks
+        const bool edge = WIN && kTile * (blk - j + 1) > f.a.window && kTile * (j + 1) > f.a.sinks;
         auto mask = [&](int q) {
+          if constexpr (WIN) {
+            if (j != blk && !edge) return;
+            const uint32_t hide = hidden_bits(kTile * (blk - j) + row - 32 * q,
+                                              kTile * (blk - j) + row - f.a.window + 1 - 32 * q, f.a.sinks - kTile * j - 32 * q);
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (32 * q + i > row) x[i] = 0xFF800000u;
+            for (int i = 0; i < 32; ++i)
+              if (hide >> i & 1u) x[i] = 0xFF800000u;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * q + i > row) x[i] = 0xFF800000u;
+          }
         };
         auto compare = [&]() {
 #pragma unroll
@@ -398,10 +420,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
 #pragma unroll
           for (int q = 0; q < 3; ++q) {
             load(q);
+            if (WIN) mask(q);
             compare();
             exps(p + 16 * q);
           }
           load(3);
+          if (WIN) mask(3);
           compare();
           const float up = fmaxf(m, top());
           if (__any_sync(0xffffffffu, (up - m) * c > kGrow)) {
@@ -422,9 +446,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
               load(q);
+              if (WIN) mask(q);
               exps(p + 16 * q);
             }
             load(3);
+            if (WIN) mask(3);
           }
         }
         tc::tmem_put32(sc, p);
@@ -484,11 +510,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
 
 }  // namespace
 
-template <int DP>
+template <int DP, bool WIN>
 static cudaError_t launch(const FwdArgs& f, int64_t items, cudaStream_t s) {
-  const cudaError_t e = allow_smem<k_attn_fwd_tc<DP>>(Fwd<DP>::kSmem);
+  const cudaError_t e = allow_smem<k_attn_fwd_tc<DP, WIN>>(Fwd<DP>::kSmem);
   if (e) return e;
-  k_attn_fwd_tc<DP><<<walk_grid(items), kThreads, Fwd<DP>::kSmem, s>>>(f);
+  k_attn_fwd_tc<DP, WIN><<<walk_grid(items), kThreads, Fwd<DP>::kSmem, s>>>(f);
   return cudaGetLastError();
 }
 
@@ -502,7 +528,8 @@ cudaError_t launch_attn_forward_tc(const AttnArgs& a, cudaStream_t s, std::strin
   f.list = f.pair_heads ? a.by_query : a.by_pair;
   f.n_list = f.pair_heads ? a.n_blocks : a.n_pairs;
   const int64_t items = static_cast<int64_t>(f.n_list) * (f.pair_heads ? a.heads / 2 : a.heads);
-  return a.dim <= 64 ? launch<64>(f, items, s) : launch<128>(f, items, s);
+  if (a.window < kNoWindow) return a.dim <= 64 ? launch<64, true>(f, items, s) : launch<128, true>(f, items, s);
+  return a.dim <= 64 ? launch<64, false>(f, items, s) : launch<128, false>(f, items, s);
 }
 
 }  // namespace normpre

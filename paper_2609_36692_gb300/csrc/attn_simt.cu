@@ -1,6 +1,9 @@
 // Packed causal attention in fp32 arithmetic: one CTA of 256 threads per 64
 // rows of one sequence and head.
 //
+// With a window both walk only the tiles that the rows see: the window's, and
+// those of the sequence's first rows that stay visible.
+//
 // Forward: the CTA's 64 query rows meet the sequence's keys 64 at a time,
 // starting with the block on the diagonal (where every row sees at least
 // itself, so the running maximum is finite from the first block on), with the
@@ -215,20 +218,25 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
 #pragma unroll
     for (int k = 0; k < DP / 64; ++k) acc[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  const int diag = w.first / kB;
-  for (int jb = diag; jb >= 0; --jb) {
+  const int diag = w.first / kB, lo = max(0, w.first - a.window + 1) / kB, sink = min(lo, (a.sinks + kB - 1) / kB);
+  for (int jb = diag; jb >= 0; jb = jb > lo || jb <= sink ? jb - 1 : sink - 1) {
     const int krows = min(kB, w.len - jb * kB);
     __syncthreads();
     load_tile<T, DP>(KV, a.k, w.seq + jb * kB, krows, kvh, a.dim);
     __syncthreads();
     float s[4][4];
     scores<DP>(Q, KV, ty, tx, s);
+    const int up = kB * (diag - jb);
+    auto hidden = [&](int r, int c) {
+      const int far = up + ty + 16 * r - tx - 16 * c;        // rows between the two
+      return far < 0 || (far >= a.window && kB * jb + tx + 16 * c >= a.sinks);
+    };
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float mx = -INFINITY;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        s[r][c] = jb == diag && tx + 16 * c > ty + 16 * r ? -INFINITY : s[r][c] * a.scale;
+        s[r][c] = hidden(r, c) ? -INFINITY : s[r][c] * a.scale;
         mx = fmaxf(mx, s[r][c]);
       }
 #pragma unroll
@@ -238,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
       float sum = 0.f;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const float p = jb == diag && tx + 16 * c > ty + 16 * r ? 0.f : exp2f((s[r][c] - mx) * kLog2e);
+        const float p = hidden(r, c) ? 0.f : exp2f((s[r][c] - mx) * kLog2e);
         P[(ty + 16 * r) * kPs + tx + 16 * c] = p;
         sum += p;
       }
@@ -281,7 +289,8 @@ __device__ __forceinline__ void grad_scores(const AttnArgs& a, const float* Q, c
     const float ls = lse[ty + 16 * r], de = delta[ty + 16 * r];
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const bool seen = i < len && j0 + tx + 16 * c <= i;
+      const int j = j0 + tx + 16 * c;
+      const bool seen = i < len && j <= i && (i - j < a.window || j < a.sinks);
       p[r][c] = seen ? exp2f(fmaf(t[r][c], a.scale, -ls) * kLog2e) : 0.f;
       s[r][c] = seen ? p[r][c] * (s[r][c] - de) : 0.f;
     }
@@ -323,9 +332,11 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int k = 0; k < DP / 64; ++k) dk[r][k] = dv[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  // rows past the last one that sees any of these keys
+  const int end = w.first < a.sinks ? w.len : min(w.len, w.first + kB - 1 + a.window);
   for (int g = 0; g < a.group; ++g) {
     const int head = kvh * a.group + g;
-    for (int i0 = w.first; i0 < w.len; i0 += kB) {
+    for (int i0 = w.first; i0 < end; i0 += kB) {
       const int qrows = min(kB, w.len - i0);
       __syncthreads();
       load_tiles<T, DP>(Q, a.q, dO, a.dout, w.seq + i0, qrows, head, a.dim);
@@ -374,7 +385,8 @@ __device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, i
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int k = 0; k < DP / 64; ++k) dq[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j0 = 0; j0 <= w.first; j0 += kB) {
+  const int lo = max(0, w.first - a.window + 1) / kB * kB, sink = min(lo, (a.sinks + kB - 1) / kB * kB);
+  for (int j0 = sink ? 0 : lo; j0 <= w.first; j0 = j0 + kB == sink ? lo : j0 + kB) {
     const int krows = min(kB, w.len - j0);
     __syncthreads();
     load_tiles<T, DP>(K, a.k, V, a.v, w.seq + j0, krows, kvh, a.dim);

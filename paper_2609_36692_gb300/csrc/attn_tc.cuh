@@ -135,6 +135,13 @@ __device__ __forceinline__ void store_rows(bf16* tile, int64_t ts, const uint32_
       *reinterpret_cast<uint4*>(p + k * ts) = make_uint4(v[k][0], v[k][1], v[k][2], v[k][3]);
 }
 
+// Which of 32 columns c = 0 .. are hidden from a row that sees c <= top, and of
+// those only c >= low and c < sinks: a bit each.
+__device__ __forceinline__ uint32_t below_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t hidden_bits(int top, int low, int sinks) {
+  return ~below_bits(top + 1) | (below_bits(low) & ~below_bits(sinks));
+}
+
 // The first items of a CTA, resolved once into shared memory: looking one up
 // is two dependent global loads, a microsecond between two items otherwise.
 struct ItemRef {

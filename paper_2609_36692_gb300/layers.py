@@ -80,13 +80,17 @@ class PackedAttention:
     contiguous and whose strides are multiples of 16 bytes.  Rows past the last
     sequence give zero outputs and gradients.
 
+    With ``window``, a row sees the ``window`` rows up to itself and, with
+    ``sinks``, its sequence's first ``sinks`` rows however far they are; 0: all
+    rows up to itself.
+
     With `stream`, a call's work runs there instead of on the current stream;
     the caller orders it after what wrote its inputs and lengths, and before
     what reads its outputs.
     """
 
     def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, max_tokens: int, max_seqs: int,
-                 dtype: torch.dtype = torch.bfloat16, scale: float = 0.0, device=None):
+                 dtype: torch.dtype = torch.bfloat16, scale: float = 0.0, device=None, window: int = 0, sinks: int = 0):
         index = None if device is None else torch.device(device).index
         self.device = torch.device("cuda", torch.cuda.current_device() if index is None else index)
         self.dtype, self.n_heads, self.n_kv_heads, self.head_dim = dtype, n_heads, n_kv_heads, head_dim
@@ -96,7 +100,7 @@ class PackedAttention:
         self.plan, self.lengths = None, ()
         cfg = C.normpre_attn_config(n_heads, n_kv_heads, head_dim, max_seqs, max_tokens, code, scale)
         with torch.cuda.device(self.device):
-            self.plan = C.normpre_attn_init(cfg)
+            self.plan = C.normpre_attn_init_window(cfg, window, sinks)
 
     def set_lengths(self, lengths: Sequence[int], stream=None) -> None:
         lengths = tuple(int(n) for n in lengths)

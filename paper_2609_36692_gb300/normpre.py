@@ -137,6 +137,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     HP = P       # normpre_heads by reference or by address
     i32 = ctypes.c_int
     lib.normpre_attn_init.argtypes = [ctypes.POINTER(normpre_attn_config), ctypes.POINTER(P)]
+    lib.normpre_attn_init_window.argtypes = [ctypes.POINTER(normpre_attn_config), i64, i64, ctypes.POINTER(P)]
     lib.normpre_attn_set_lengths.argtypes = [P, i32, ctypes.POINTER(i64), P]
     lib.normpre_attn_forward.argtypes = [P, i64, HP, HP, HP, HP, P, P]
     lib.normpre_attn_backward.argtypes = [P, i64, HP, HP, HP, HP, P, HP, HP, HP, HP, P]
@@ -149,7 +150,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.normpre_ckpt_swiglu.argtypes = [i64, i64, i32, P, i64, P, i64, P, i64, P, P, P, P, P]
     lib.normpre_ckpt_swiglu_backward.argtypes = [i64, i64, i32, P, P, P, P, P, i64, P, i64, P, i64, P]
     lib.normpre_ckpt_sync_status.argtypes = [P]
-    for name in ("attn_init", "attn_set_lengths", "attn_forward", "attn_backward", "attn_sync_status",
+    for name in ("attn_init", "attn_init_window", "attn_set_lengths", "attn_forward", "attn_backward", "attn_sync_status",
                  "ckpt_bytes", "ckpt_pack", "ckpt_restore", "ckpt_wgrad", "ckpt_swiglu", "ckpt_swiglu_backward",
                  "ckpt_sync_status"):
         getattr(lib, "normpre_" + name).restype = ctypes.c_int
@@ -283,6 +284,12 @@ def normpre_sketch_omega(seed: int, matrix_id: int, t: int, n_a: int, l: int, om
 def normpre_attn_init(cfg: normpre_attn_config) -> int:
     h = ctypes.c_void_p()
     _check(load_library().normpre_attn_init(ctypes.byref(cfg), ctypes.byref(h)))
+    return h.value
+
+
+def normpre_attn_init_window(cfg: normpre_attn_config, window: int, sinks: int) -> int:
+    h = ctypes.c_void_p()
+    _check(load_library().normpre_attn_init_window(ctypes.byref(cfg), window, sinks, ctypes.byref(h)))
     return h.value
 
 

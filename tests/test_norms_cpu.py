@@ -1,6 +1,9 @@
 """Host-side checks of the query and key norms and of gradient clipping: arguments are refused before any CUDA call."""
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import pytest
 
@@ -88,3 +91,57 @@ def test_clip_arguments(C):
 @pytest.mark.parametrize("struct", ["normpre_qkrot_config"])
 def test_structs(C, struct):
     base.test_structs_mirror_the_header(C, struct)
+
+
+@pytest.mark.parametrize("window, sinks", [(-1, 0), (0, -1), (100, -5)])
+def test_window_arguments(C, window, sinks):
+    cfg = C.normpre_attn_config(4, 2, 64, 8, 1024, C.NORMPRE_BF16, 0.0)
+    refused(C, C.NORMPRE_ERR_ARG, C.normpre_attn_init_window, cfg, window, sinks)
+    cfg.head_dim = 12
+    refused(C, C.NORMPRE_ERR_SHAPE, C.normpre_attn_init_window, cfg, 10, 1)
+    assert C.load_library().normpre_attn_init_window(None, 0, 0, None) == C.NORMPRE_ERR_ARG
+
+
+SPANS = r"""
+#include <algorithm>
+#include <cstdio>
+#include "attn.h"
+using namespace normpre;
+// whether some row of the query block sees some key of the key block
+static bool meets(int i, int j, int len, int w, int s) {
+  for (int q = 128 * i; q < std::min(len, 128 * i + 128); ++q)
+    for (int k = 128 * j; k < std::min(len, 128 * j + 128); ++k)
+      if (k <= q && (q - k < w || k < s)) return true;
+  return false;
+}
+int main() {
+  int bad = 0;
+  for (int len : {1, 128, 129, 600, 1025})
+    for (int w : {1, 2, 127, 128, 129, 256, 300, 1 << 25})
+      for (int s : {0, 1, 128, 129, 300, 2000})
+        for (int b = 0, n = (len + 127) / 128; b < n; ++b) {
+          const KeySpan k = key_span(b, w, s);
+          int down = 0, up = 0, last = b;
+          for (int j = b; j >= 0; j = k.down(j), ++down) bad += !meets(b, j, 1 << 20, w, s);
+          for (int j = k.first(); j <= b; j = k.up(j), ++up) bad += !meets(b, j, 1 << 20, w, s);
+          int all = 0;
+          for (int j = 0; j <= b; ++j) all += meets(b, j, 1 << 20, w, s);
+          bad += all != down || all != up || all != k.count(b);
+          for (int i = b; i < n; ++i)
+            if (meets(i, b, 1 << 20, w, s)) last = i;
+          bad += last_query(b, len, w, s) != last;
+        }
+  std::printf("%d\n", bad);
+}
+"""
+
+
+@pytest.mark.skipif(not shutil.which("g++") or not os.path.exists("/usr/local/cuda/include/cuda_runtime.h"),
+                    reason="needs g++ and the CUDA headers")
+def test_spans(tmp_path):
+    """Which blocks of keys and queries meet, against all their pairs of rows."""
+    src, exe = tmp_path / "t.cpp", tmp_path / "t"
+    src.write_text(SPANS)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I/usr/local/cuda/include",
+                    "-I" + os.path.join(base.ROOT, "paper_2609_36692_gb300", "csrc"), str(src), "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.strip() == "0"

@@ -1,0 +1,327 @@
+"""Packed attention with a window and sinks, against the definition in 64 bits.
+
+Tolerances are those of attention without a window, derived in
+test_attention_gpu: a window only leaves terms out.  Blocks of 64 rows are also
+checked one by one, at twice the tolerance: it takes a rounding for 2^-9, as it is
+in the root mean square over many values, where 2^-8 is the most.
+"""
+import math
+
+import pytest
+
+import test_attention_gpu as A
+from test_attention_gpu import TOL, dt, err, make, plan_for
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(q, k, v, do, lengths, window, sinks):
+    """As test_attention_gpu's, of the pairs that a window and sinks leave; the sums
+    of the terms' squares by rows, for the output and the gradients."""
+    import torch
+    t, h, d = q.shape
+    hk = k.shape[1]
+    g, scale, dev = h // hk, 1.0 / math.sqrt(d), q.device
+    z = lambda n: torch.zeros(t, n, d, dtype=torch.float64, device=dev)  # noqa: E731
+    out, dq, dk, dv = z(h), z(h), z(hk), z(hk)
+    lse = torch.full((h, t), -math.inf, dtype=torch.float64, device=dev)
+    terms = {n: torch.zeros(t, dtype=torch.float64, device=dev) for n in ("out", "dq", "dk", "dv")}
+    at = 0
+    for n in lengths:
+        for r0 in range(0, n, 2000):
+            i = torch.arange(r0, min(n, r0 + 2000), device=dev)
+            j = torch.arange(int(i[-1]) + 1, device=dev)
+            j = j[(j > r0 - window) | (j < sinks)]
+            far = i[:, None] - j
+            hide = (far < 0) | ((far >= window) & (j >= sinks))
+            r, c = at + i, at + j
+            for a in range(h):
+                qq, kk, vv, dd = (x.double() for x in (q[r, a], k[c, a // g], v[c, a // g], do[r, a]))
+                s = (scale * qq @ kk.T).masked_fill(hide, -math.inf)
+                lse[a, r] = torch.logsumexp(s, 1)
+                p = torch.exp(s - lse[a, r, None])
+                o = p @ vv
+                dp, delta = dd @ vv.T, (dd * o).sum(1, keepdim=True)
+                ds = p * (dp - delta)
+                size = (p * (dp.abs() + delta.abs())) ** 2
+                terms["out"][r] += (p ** 2 @ vv ** 2).sum(1)
+                terms["dq"][r] += scale ** 2 * (size @ kk ** 2).sum(1)
+                terms["dk"].index_add_(0, c, scale ** 2 * (size.T @ qq ** 2).sum(1))
+                terms["dv"].index_add_(0, c, (p.T ** 2 @ dd ** 2).sum(1))
+                out[r, a], dq[r, a] = o, scale * ds @ kk
+                dk[:, a // g].index_add_(0, c, scale * ds.T @ qq)
+                dv[:, a // g].index_add_(0, c, p.T @ dd)
+        at += n
+    return out, lse, dq, dk, dv, terms
+
+
+def check(layout, lengths, window, sinks, dtype, seed=0, pad=3, scale=1.0):
+    import torch
+    h, hk, d = layout
+    n = sum(lengths)
+    q, k, v, do = make(seed + n + window, n + pad, h, hk, d, dtype, scale)
+    plan = plan_for(h, hk, d, n + pad, lengths, dtype, window=window, sinks=sinks)
+    ref = reference(q, k, v, do, lengths, window, sinks)
+    out, lse = plan.forward(q, k, v)
+    grads = plan.backward(q, k, v, out, lse, do)
+    assert plan.status() == 0
+    for name, x, r in zip(("out", "dq", "dk", "dv"), (out, *grads), (ref[0], *ref[2:5])):
+        tol, terms = TOL[dtype, "fwd" if name == "out" else "bwd"], ref[5][name]
+        assert err(x, r, float(terms.sum()) ** 0.5) <= tol, name
+        assert not bool(x[n:].any()), name
+        for r0 in range(0, n, 64):
+            rows = slice(r0, min(n, r0 + 64))
+            assert err(x[rows], r[rows], float(terms[rows].sum()) ** 0.5) <= 2 * tol, (name, r0)
+    assert bool((lse[:, n:] == -math.inf).all())
+    if n:
+        assert float((lse[:, :n].double() - ref[1][:, :n]).abs().max()) <= 2e-5 * max(1.0, float(ref[1][:, :n].abs().max()))
+    return plan, (q, k, v, do), (out, lse, *grads)
+
+
+LAYOUTS = [(2, 2, 64), (4, 2, 128), (6, 2, 96), (3, 1, 64), (1, 1, 8), (3, 3, 128)]
+WINDOWS = [(1, 0), (1, 1), (2, 300), (16, 2), (64, 64), (100, 0), (127, 129), (128, 4), (129, 0), (200, 128), (300, 1),
+           (511, 600), (700, 4), (5000, 2)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", LAYOUTS, ids=str)
+@pytest.mark.parametrize("window, sinks", WINDOWS)
+def test_forward_and_backward(window, sinks, layout, dtype):
+    check(layout, [700, 0, 1, 129, 255, 64], window, sinks, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lengths", [[1], [0], [128], [129], [1500], [384, 383, 385], [5] * 60, []], ids=str)
+@pytest.mark.parametrize("window, sinks", [(1, 3), (130, 0), (130, 200), (256, 2)])
+def test_lengths(lengths, window, sinks, dtype):
+    check((3, 1, 64), lengths, window, sinks, dtype)
+    check((4, 2, 128), lengths, window, sinks, dtype, pad=0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("window, sinks", [(3, 2), (1000, 5), (1, 300), (2500, 0)])
+def test_long(window, sinks, dtype):
+    """Many more blocks than the window has, more items than CTAs."""
+    check((2, 1, 64), [5000, 37], window, sinks, dtype)
+    check((1, 1, 128), [4100], window, sinks, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_very_long(dtype):
+    """Lists too long to be dealt out one by one."""
+    check((3, 3, 64), [40000] if dtype == "bf16" else [9000], 70, 5, dtype)
+    if dtype == "bf16":
+        check((70, 70, 8), [9000, 7000], 200, 1, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", [(4, 2, 64), (3, 1, 128)], ids=str)
+def test_a_window_that_hides_nothing(layout, dtype):
+    """The bits of a plan without one."""
+    import torch
+    h, hk, d = layout
+    lengths = [300, 1, 411]
+    q, k, v, do = make(1, 720, h, hk, d, dtype)
+    outs = []
+    for window, sinks in ((0, 0), (0, 50), (411, 3), (1 << 40, 1 << 40)):
+        plan = plan_for(h, hk, d, 720, lengths, dtype, window=window, sinks=sinks)
+        out, lse = plan.forward(q, k, v)
+        outs.append((out, lse, *plan.backward(q, k, v, out, lse, do)))
+        assert plan.status() == 0
+    for other in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(other, outs[0]))
+    # all rows are sinks: the same numbers, by the windowed kernels
+    plan = plan_for(h, hk, d, 720, lengths, dtype, window=5, sinks=411)
+    out, lse = plan.forward(q, k, v)
+    for a, b in zip((out, *plan.backward(q, k, v, out, lse, do)), (outs[0][0], *outs[0][2:])):
+        assert err(a, b.double()) <= TOL[dtype, "bwd"]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -3.3e38])
+def test_other_rows_do_not_reach_a_sequence(dtype, bad):
+    import torch
+    h, hk, d, lengths = 4, 2, 128, [330, 277, 400]
+    tokens = sum(lengths) + 140
+    q, k, v, do = (x.contiguous() for x in make(8, tokens, h, hk, d, dtype))
+    plan = plan_for(h, hk, d, tokens, lengths, dtype, window=100, sinks=3)
+    out, lse = plan.forward(q, k, v)
+    grads = plan.backward(q, k, v, out, lse, do)
+    q2, k2, v2, do2 = (x.clone() for x in (q, k, v, do))
+    for x in (q2, k2, v2, do2):
+        x[330:607] = bad
+        x[1007:] = bad
+    out2, lse2 = plan.forward(q2, k2, v2)
+    out2[1007:] = bad
+    lse2[:, 1007:] = bad
+    grads2 = plan.backward(q2, k2, v2, out2, lse2, do2)
+    assert plan.status() == 0
+    keep = torch.cat([torch.arange(0, 330), torch.arange(607, 1007)]).cuda()
+    assert torch.equal(out2[keep], out[keep]) and torch.equal(lse2[:, keep], lse[:, keep])
+    for a, b in zip(grads2, grads):
+        assert torch.equal(a[keep], b[keep])
+        assert not bool(a[1007:].any())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_what_the_window_hides_does_not_matter(dtype):
+    """A token that is not finite, beyond the window of all rows of a block."""
+    import torch
+    h, hk, d, n = 2, 1, 64, 1000
+    q, k, v, do = (x.contiguous() for x in make(9, n, h, hk, d, dtype))
+    plan = plan_for(h, hk, d, n, [n], dtype, window=200, sinks=2)
+    out, lse = plan.forward(q, k, v)
+    dq, dk, dv = plan.backward(q, k, v, out, lse, do)
+    k2, v2 = k.clone(), v.clone()
+    k2[300], v2[301] = math.nan, math.inf     # block 2; rows to 500 see them, rows from 640 no row of the block
+    out2, lse2 = plan.forward(q, k2, v2)
+    got = plan.backward(q, k2, v2, out2, lse2, do)
+    assert plan.status() == 0
+    assert bool(torch.isnan(out2[301:500]).all()) and torch.equal(out2[:256], out[:256])
+    assert torch.equal(out2[640:], out[640:]) and torch.equal(lse2[:, 640:], lse[:, 640:])
+    assert torch.equal(got[0][640:], dq[640:])
+    # keys that only rows from 640 on see; the sinks' own gradients take all rows
+    assert torch.equal(got[1][640:], dk[640:]) and torch.equal(got[2][640:], dv[640:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sharp_scores(dtype):
+    """Scores of up to a hundred that grow towards a sequence's end, or towards
+    its sinks, so that the running maximum moves at every block."""
+    import torch
+    h, hk, d, n = 2, 2, 64, 900
+    q, k, v, do = (x.contiguous() for x in make(6, n, h, hk, d, dtype, scale=3.0))
+    q[:, 0, 0], k[:, :, 0] = 4.0, torch.linspace(0, 60, n, device="cuda").to(k.dtype)[:, None]
+    q[:, 1, 0] = -4.0
+    plan = plan_for(h, hk, d, n, [n], dtype, window=300, sinks=7)
+    ref = reference(q, k, v, do, [n], 300, 7)
+    out, lse = plan.forward(q, k, v)
+    assert err(out, ref[0]) <= TOL[dtype, "fwd"]
+    assert float((lse.double() - ref[1]).abs().max()) <= 2e-5 * float(ref[1].abs().max())
+    # errors of the log-sum grow with the scores: 2^-24 * 100 in the exponent
+    for x, r in zip(plan.backward(q, k, v, out, lse, do), ref[2:5]):
+        assert err(x, r) <= (4e-5 if dtype == "f32" else 2e-2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layouts_streams_and_capture(dtype):
+    import torch
+    h, hk, d, lengths = 4, 2, 64, [650, 33, 200]
+    q, k, v, do = make(10, 890, h, hk, d, dtype)
+    plan = plan_for(h, hk, d, 890, lengths, dtype, window=150, sinks=4)
+    c = [x.contiguous() for x in (q, k, v, do)]
+    out, lse = plan.forward(*c[:3])
+    want = (out, lse, *plan.backward(*c[:3], out, lse, c[3]))
+    hm = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v, do)]
+
+    def calls(ins, stream=None):
+        o, l = plan.forward(*ins[:3], stream=stream)
+        return (o, l, *plan.backward(*ins[:3], o, l, ins[3], stream=stream))
+    torch.cuda.synchronize()
+    got = [calls((q, k, v, do)), calls(hm), calls(c, torch.cuda.Stream())]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got.append(calls(c))
+    for _ in range(2):
+        g.replay()
+    torch.cuda.synchronize()
+    assert plan.status() == 0
+    for outs in got:
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    # other lengths, and these again: nothing of the others is left
+    for other in ([890], [10] * 3, []):
+        plan.set_lengths(other)
+        calls(c)
+        plan.set_lengths(lengths)
+        assert all(torch.equal(a, b) for a, b in zip(calls(c), want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_replay_under_other_lengths_stays_in_range(dtype):
+    """As without a window; the graph's own lengths need none of the window, or
+    all of it, where the others' do not."""
+    import torch
+    h, hk, d, n, room = 4, 2, 64, 1100, 64
+    names = [("q", h), ("k", hk), ("v", hk), ("o", h), ("do", h), ("dq", h), ("dk", hk), ("dv", hk)]
+    for own in ([40, 90, 270], [400]):
+        big = {name: torch.full((400 + 2 * room, x, d), 7.0, device="cuda", dtype=dt(dtype)) for name, x in names}
+        t = {name: x[room:room + 400] for name, x in big.items()}
+        for name, x in zip(("q", "k", "v", "do"), make(8, 400, h, hk, d, dtype)):
+            t[name].copy_(x)
+        lse = torch.full((h, 400), 7.0, device="cuda")
+        plan = plan_for(h, hk, d, n, [1] * 140, dtype, window=280, sinks=5)
+        plan.set_lengths(own)
+
+        def calls():
+            plan.forward(t["q"], t["k"], t["v"], out=t["o"], lse=lse)
+            plan.backward(t["q"], t["k"], t["v"], t["o"], lse, t["do"], t["dq"], t["dk"], t["dv"])
+        calls()
+        torch.cuda.synchronize()
+        want = {name: x.clone() for name, x in big.items()}
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            calls()
+        for lengths in ([1100], [1] * 100, [5] * 140, [0, 400], [399], []):
+            plan.set_lengths(lengths)
+            g.replay()
+            torch.cuda.synchronize()
+            plan.status(raise_on_error=False)
+            for name, x in big.items():
+                assert bool((x[:room] == 7.0).all()) and bool((x[room + 400:] == 7.0).all()), name
+            plan.set_lengths(own)
+            g.replay()
+            torch.cuda.synchronize()
+            assert plan.status() == 0
+            for name, x in big.items():
+                assert torch.equal(x, want[name]), name
+
+
+def test_gradient_against_differences():
+    """As test_attention_gpu's."""
+    import torch
+    h, hk, d, lengths = 2, 1, 64, [90, 23]
+    q, k, v, w = (x.contiguous() for x in make(14, 113, h, hk, d, "f32"))
+    plan = plan_for(h, hk, d, 113, lengths, "f32", window=9, sinks=2)
+    loss = lambda *x: float((plan.forward(*x)[0].double() * w.double()).sum())  # noqa: E731
+    out, lse = plan.forward(q, k, v)
+    for i, grad in enumerate(plan.backward(q, k, v, out, lse, w)):
+        u = grad / grad.norm()
+        step = 2.0 ** -6
+        x = [q, k, v]
+        hi, lo = ([y + sign * step * u if j == i else y for j, y in enumerate(x)] for sign in (1, -1))
+        slope = (loss(*hi) - loss(*lo)) / (2 * step)
+        assert abs(slope - float((grad.double() * u.double()).sum())) <= 2e-3 * abs(slope)
+
+
+def test_autograd():
+    import torch
+    h, hk, d, lengths = 4, 2, 64, [300, 28]
+    q, k, v, do = (x.contiguous() for x in make(15, 328, h, hk, d, "bf16"))
+    plan = plan_for(h, hk, d, 328, lengths, "bf16", window=40, sinks=4)
+    ref = reference(q, k, v, do, lengths, 40, 4)
+    leaves = [x.clone().requires_grad_() for x in (q, k, v)]
+    (plan(*leaves) * do).sum().backward()
+    for x, r in zip(leaves, ref[2:5]):
+        assert err(x.grad, r) <= TOL["bf16", "bwd"]
+    out = plan(*leaves)
+    plan.set_lengths([328])
+    with pytest.raises(RuntimeError, match="lengths changed"):
+        out.backward(do)
+
+
+@pytest.mark.parametrize("window, sinks", [(-1, 0), (5, -1)])
+def test_refusals(window, sinks):
+    from paper_2609_36692_gb300 import normpre as C
+    with pytest.raises(C.NormPreError) as e:
+        plan_for(4, 2, 64, 64, [64], "bf16", window=window, sinks=sinks)
+    assert e.value.status == C.NORMPRE_ERR_ARG
+
+
+def test_sizes_are_the_reference_without_a_window():
+    """This file's reference is test_attention_gpu's where the window hides
+    nothing."""
+    import torch
+    q, k, v, do = make(3, 150, 4, 2, 64, "f32")
+    for a, b in zip(reference(q, k, v, do, [100, 40], 200, 3)[:5], A.reference(q, k, v, do, [100, 40])[:5]):
+        assert bool(torch.isclose(a, b, rtol=1e-12, atol=1e-12).all())
