@@ -63,88 +63,110 @@ __device__ __forceinline__ int find(const Table<N>& t, uint32_t chunk) {
   return lo;
 }
 
-template <int N>
-__device__ __forceinline__ double squares(const float (&x)[N]) {
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) s = fmaf(x[i], x[i], s);
-  if (s > 0x1p-100f && s < 0x1p120f) return s;
-  // squares near the ends of fp32's range
-  double d = 0.;
-  if (s == 0.f) {
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[i]));
-    if (top == 0.f) return 0.;
+// Sixteen bytes of a tensor as fp32 values.
+template <typename T> struct Piece {
+  static constexpr int kN = 16 / sizeof(T);
+  uint32_t w[4];
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
   }
+  // elements i .. of the tensor's n, i a multiple of 16 bytes' worth before its
+  // first one or behind it: zeros outside
+  __device__ __forceinline__ void load(const T* p, int64_t i, int64_t n) {
+    if (i >= 0 && i + kN <= n) {
+      const uint4 q = __ldg(reinterpret_cast<const uint4*>(p + i));
+      w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    } else {
 #pragma unroll
-  for (int i = 0; i < N; ++i) d = fma(static_cast<double>(x[i]), static_cast<double>(x[i]), d);
-  return d;
-}
-
-// A thread's share of a chunk of n values: 64 bytes.  With 16-byte accesses
-// where `vec`, else one value at a time, neighbours in neighbouring threads.
-template <typename T, bool VEC> struct Share {
-  static constexpr int kEach = 64 / sizeof(T);
-  static constexpr int kPer16 = 16 / sizeof(T);
-  float v[kEach];
-  static __device__ __forceinline__ int index(int i) {
-    return VEC ? (i / kPer16 * kThreads + static_cast<int>(threadIdx.x)) * kPer16 + i % kPer16
-               : i * kThreads + static_cast<int>(threadIdx.x);
-  }
-  __device__ __forceinline__ void load(const T* p, int n) {
+      for (int e = 0; e < 4; ++e) w[e] = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; i += VEC ? kPer16 : 1) {
-      const int at = index(i);
-      if constexpr (VEC) {
-        if (at + kPer16 <= n) {
-          const uint4 q = __ldg(reinterpret_cast<const uint4*>(p + at));
-          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 4) {
-              v[i + e] = __uint_as_float(w[e]);
-            } else {
-              v[i + 2 * e] = bf16lo(w[e]);
-              v[i + 2 * e + 1] = bf16hi(w[e]);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < kPer16; ++e) v[i + e] = at + e < n ? to_f32(p[at + e]) : 0.f;
+      for (int e = 0; e < kN; ++e)
+        if (i + e >= 0 && i + e < n) {
+          if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(__ldg(p + i + e));
+          else w[e >> 1] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const unsigned short*>(p) + i + e)) << (16 * (e & 1));
         }
-      } else {
-        v[i] = at < n ? to_f32(p[at]) : 0.f;
-      }
     }
   }
-  template <typename U> __device__ __forceinline__ void store(U* p, int n, float c) const {
+  template <typename U> __device__ __forceinline__ void store(U* p, int64_t i, int64_t n, float c, bool aligned) const {
+    if (i >= 0 && i + kN <= n && aligned) {
+      uint32_t o[kN * sizeof(U) / 4];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int at = index(i);
-      if (at < n) p[at] = from_f32<U>(v[i] * c);
+      for (int e = 0; e < kN; e += 2) {
+        if constexpr (sizeof(U) == 4) {
+          o[e] = __float_as_uint(at(e) * c);
+          o[e + 1] = __float_as_uint(at(e + 1) * c);
+        } else {
+          o[e >> 1] = pack_bf16x2(at(e) * c, at(e + 1) * c);
+        }
+      }
+      if constexpr (kN * sizeof(U) == 8) {
+        *reinterpret_cast<uint2*>(p + i) = make_uint2(o[0], o[1]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < static_cast<int>(kN * sizeof(U) / 4); e += 4)
+          *reinterpret_cast<uint4*>(p + i + e * (4 / sizeof(U))) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kN; ++e)
+        if (i + e >= 0 && i + e < n) p[i + e] = from_f32<U>(at(e) * c);
     }
+  }
+};
+
+// A thread's share of a chunk: four pieces, neighbours in neighbouring threads.
+// Chunks start on 16-byte boundaries, the first one at or before the tensor.
+template <typename T> struct Share {
+  Piece<T> q[4];
+  static __device__ __forceinline__ int64_t index(const Entry& e, uint32_t chunk, int i) {
+    const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(e.in) % 16 / sizeof(T));
+    return (static_cast<int64_t>(chunk - e.first) * (kChunkBytes / 16) + i * kThreads + static_cast<int>(threadIdx.x)) *
+               Piece<T>::kN - lead;
+  }
+  __device__ __forceinline__ void load(const Entry& e, uint32_t chunk) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i].load(static_cast<const T*>(e.in), index(e, chunk, i), e.size);
+  }
+  __device__ __forceinline__ double squares() const {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < Piece<T>::kN; ++e) s = fmaf(q[i].at(e), q[i].at(e), s);
+    if (s > 0x1p-100f && s < 0x1p120f) return s;
+    // squares near the ends of fp32's range
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= q[i].w[e];
+    if (!any) return 0.;
+    double d = 0.;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < Piece<T>::kN; ++e) d = fma(static_cast<double>(q[i].at(e)), static_cast<double>(q[i].at(e)), d);
+    return d;
+  }
+  template <typename U> __device__ __forceinline__ void store(const Entry& e, uint32_t chunk, float c) const {
+    constexpr int kOut = Piece<T>::kN * sizeof(U) < 16 ? 8 : 16;
+    // whether the output's pieces start on their boundaries too
+    const bool aligned = reinterpret_cast<uintptr_t>(static_cast<U*>(e.out) + index(e, e.first, 0)) % kOut == 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i].store(static_cast<U*>(e.out), index(e, chunk, i), e.size, c, aligned);
   }
 };
 
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const Entry& e, uint32_t chunk) {
-  constexpr int kElems = kChunkBytes / sizeof(T);
-  const int64_t at = static_cast<int64_t>(chunk - e.first) * kElems;
-  const T* p = static_cast<const T*>(e.in) + at;
-  const int n = static_cast<int>(min(static_cast<int64_t>(kElems), e.size - at));
-  if (reinterpret_cast<uintptr_t>(e.in) % 16 == 0) {
-    Share<T, true> x;
-    x.load(p, n);
-    return squares(x.v);
-  }
-  Share<T, false> x;
-  x.load(p, n);
-  return squares(x.v);
+  Share<T> x;
+  x.load(e, chunk);
+  return x.squares();
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant__ Table<N> t, double* part) {
+__global__ void __launch_bounds__(kThreads, kPerSm) k_grad_squares(const __grid_constant__ Table<N> t, double* part) {
   __shared__ double red[kThreads / 32];
   uint32_t c = static_cast<uint32_t>(static_cast<uint64_t>(t.chunks) * blockIdx.x / gridDim.x);
   const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(t.chunks) * (blockIdx.x + 1) / gridDim.x);
@@ -167,23 +189,15 @@ __device__ __forceinline__ double fold(const double* part, int parts, double* re
   return block_sum(sum, red);
 }
 
-template <typename T, typename U, bool VEC>
-__device__ __forceinline__ void scale_share(const Entry& e, int64_t at, int n, float c) {
-  Share<T, VEC> x;
-  x.load(static_cast<const T*>(e.in) + at, n);
-  x.store(static_cast<U*>(e.out) + at, n, c);
-}
 template <typename T, typename U>
 __device__ __forceinline__ void scale_chunk(const Entry& e, uint32_t chunk, float c) {
-  constexpr int kElems = kChunkBytes / sizeof(T);
-  const int64_t at = static_cast<int64_t>(chunk - e.first) * kElems;
-  const int n = static_cast<int>(min(static_cast<int64_t>(kElems), e.size - at));
-  if (reinterpret_cast<uintptr_t>(e.in) % 16 == 0) scale_share<T, U, true>(e, at, n, c);
-  else scale_share<T, U, false>(e, at, n, c);
+  Share<T> x;
+  x.load(e, chunk);
+  x.template store<U>(e, chunk, c);
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreads) k_grad_scale(const __grid_constant__ Table<N> t, const double* part, int parts,
+__global__ void __launch_bounds__(kThreads, kPerSm) k_grad_scale(const __grid_constant__ Table<N> t, const double* part, int parts,
                                                          float max_norm, float eps, int in_place, float* norm) {
   __shared__ double red[kThreads / 32];
   __shared__ float factor;
@@ -291,7 +305,8 @@ void fill(Table<N>* t, int first, int n, const void* const* grads, const int* dt
     const int in_bf16 = dtypes[i] == NORMPRE_BF16;
     t->e[t->n++] = Entry{grads[i], out ? out[i] : nullptr, sizes[i], static_cast<uint32_t>(chunks), static_cast<uint16_t>(in_bf16),
                          static_cast<uint16_t>(out && out_dtypes[i] == NORMPRE_BF16)};
-    chunks += static_cast<uint64_t>(cdiv(sizes[i], kChunkBytes / (in_bf16 ? 2 : 4)));
+    const int64_t lead = static_cast<int64_t>(reinterpret_cast<uintptr_t>(grads[i]) % 16);
+    chunks += static_cast<uint64_t>(cdiv(lead + sizes[i] * (in_bf16 ? 2 : 4), kChunkBytes));
   }
   t->chunks = static_cast<uint32_t>(chunks);
 }

@@ -8,7 +8,9 @@ cannot be loaded, importing the functions raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+from array import array
 from typing import Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -408,26 +410,29 @@ def normpre_qkrot_free(plan: int) -> None:
         load_library().normpre_qkrot_free(plan)
 
 
+@functools.lru_cache(maxsize=64)
 def normpre_grad_bytes(n: int) -> int:
     b = ctypes.c_int64()
     _check(load_library().normpre_grad_bytes(n, ctypes.byref(b)))
     return b.value
 
 
+def _at(values: array) -> int:
+    return values.buffer_info()[0]
+
+
 def normpre_grad_norm(grads: Sequence[int], dtypes: Sequence[int], sizes: Sequence[int], norm_ptr: int,
                       workspace: int, stream: int = 0) -> int:
-    n = len(grads)
-    return _check(load_library().normpre_grad_norm(n, (ctypes.c_void_p * n)(*grads), (ctypes.c_int * n)(*dtypes),
-                                                   (ctypes.c_int64 * n)(*sizes), norm_ptr, workspace, stream))
+    p, t, n = array("Q", grads), array("i", dtypes), array("q", sizes)
+    return _check(load_library().normpre_grad_norm(len(p), _at(p), _at(t), _at(n), norm_ptr, workspace, stream))
 
 
 def normpre_grad_clip(grads: Sequence[int], dtypes: Sequence[int], sizes: Sequence[int], out: Sequence[int],
                       out_dtypes: Sequence[int], max_norm: float, eps: float, norm_ptr: int, workspace: int,
                       stream: int = 0) -> int:
-    n = len(grads)
-    P, I = ctypes.c_void_p * n, ctypes.c_int * n
-    return _check(load_library().normpre_grad_clip(n, P(*grads), I(*dtypes), (ctypes.c_int64 * n)(*sizes), P(*out),
-                                                   I(*out_dtypes), max_norm, eps, norm_ptr, workspace, stream))
+    p, t, n, o, u = array("Q", grads), array("i", dtypes), array("q", sizes), array("Q", out), array("i", out_dtypes)
+    return _check(load_library().normpre_grad_clip(len(p), _at(p), _at(t), _at(n), _at(o), _at(u), max_norm, eps,
+                                                   norm_ptr, workspace, stream))
 
 
 def normpre_free(handle: int) -> None:

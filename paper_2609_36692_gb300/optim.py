@@ -210,8 +210,6 @@ class NormPreOptimizer(_torch_optimizer_base()):
 
 def _dense(x) -> bool:
     """Whether a tensor fills its memory without gaps, in whatever order."""
-    if x.is_contiguous():
-        return True
     order = sorted(range(x.dim()), key=x.stride, reverse=True)
     return x.permute(order).is_contiguous()
 
@@ -220,24 +218,33 @@ def _grad_lists(grads, name: str = "gradient"):
     """Checks gradients and returns their pointers, dtype codes and sizes."""
     import torch
     codes = {torch.float32: C.NORMPRE_F32, torch.bfloat16: C.NORMPRE_BF16}
-    device = grads[0].device
+    strided, index = torch.strided, grads[0].get_device()
+    pointers, types, sizes = [], [], []
     for i, g in enumerate(grads):
-        if not g.is_cuda or g.device != device or g.layout != torch.strided:
+        if g.layout != strided or index < 0 or g.get_device() != index:
             raise ValueError("%s %d: all must be dense CUDA tensors on one device" % (name, i))
-        if g.dtype not in codes:
+        code = codes.get(g.dtype)
+        if code is None:
             raise TypeError("%s %d: unsupported dtype %s (float32 or bfloat16)" % (name, i, g.dtype))
-        if not _dense(g):
+        if not (g.is_contiguous() or _dense(g)):
             raise ValueError("%s %d: its memory must have no gaps" % (name, i))
-    return [g.data_ptr() for g in grads], [codes[g.dtype] for g in grads], [g.numel() for g in grads]
+        pointers.append(g.data_ptr())
+        types.append(code)
+        sizes.append(g.numel())
+    return pointers, types, sizes
 
 
 def _grad_call(device, f, *args):
     """f(*args, norm, workspace, stream) on the gradients' device; returns the norm."""
     import torch
-    with torch.cuda.device(device):
-        norm = torch.empty((), dtype=torch.float32, device=device)
-        work = torch.empty(C.normpre_grad_bytes(len(args[0])), dtype=torch.uint8, device=device)
-        f(*args, norm.data_ptr(), work.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    work = torch.empty(C.normpre_grad_bytes(len(args[0])), dtype=torch.uint8, device=device)
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    if torch._C._cuda_getDevice() == device.index:
+        f(*args, norm.data_ptr(), work.data_ptr(), stream)
+    else:
+        with torch.cuda.device(device):
+            f(*args, norm.data_ptr(), work.data_ptr(), stream)
     return norm
 
 
@@ -270,9 +277,9 @@ def clip_grads(grads, max_norm: float, eps: float = 1e-6, out=None):
             raise ValueError("out must have a tensor for each gradient")
         to = _grad_lists(out, "out")
         for i, (g, o) in enumerate(zip(grads, out)):
-            if o.shape != g.shape or o.device != g.device:
+            if o.shape != g.shape or (i == 0 and o.device != g.device):
                 raise ValueError("out %d must have its gradient's shape and device" % i)
-            if o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()):
+            if not (o.is_contiguous() and g.is_contiguous()) and o.stride() != g.stride():
                 raise ValueError("out %d must have its gradient's strides" % i)
     return _grad_call(grads[0].device, C.normpre_grad_clip, *lists, to[0], to[1], float(max_norm), float(eps))
 
