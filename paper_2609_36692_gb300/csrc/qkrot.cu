@@ -9,11 +9,12 @@
 // A row stays in registers between the sums and the result, so that every value
 // is read once and written once: bound by HBM.
 //
-// A lane holds eight pairs of its row (16 values) and with them the pairs' cos
-// and sin, which it forms once per token and uses for all of its heads; 1 to 16
-// lanes share a row.  Half-split pairs (i, i + R/2) are two runs of up to eight
-// values, read V at a time (V: the largest of 8, 4, 2, 1 that divides R/2, so
-// that no access leaves its alignment); interleaved pairs two runs of eight.
+// A lane holds four pairs of a row (8 values), of two heads at once: with them
+// the pairs' cos and sin, which it forms once per token and uses for all of its
+// heads; 1 to 32 lanes share a row, and the rows' sums of both heads travel
+// through the lanes together.  Half-split pairs (i, i + R/2) are two runs of up to
+// four values, read V at a time (V: the largest of 4, 2, 1 that divides R/2, so
+// that no access leaves its alignment); interleaved pairs two runs of four.
 //
 // Angles: a position is a whole number p, and a frequency is kept as a 64-bit
 // fraction F of a turn.  p F mod 2^64 is the angle's fraction of a turn, exact
@@ -85,211 +86,300 @@ struct Unit {
 template <bool INTER>
 __device__ __forceinline__ Unit unit_of(const RotArgs& g, int u) {
   Unit t;
-  if constexpr (INTER) {
-    t.a = 16 * u;
-    t.b = 16 * u + 8;
-    t.na = max(0, min(8, g.dim - t.a));
-    t.nb = max(0, min(8, g.dim - t.b));
-  } else if (u < g.rot_units) {
-    t.a = 8 * u;
-    t.b = g.half + 8 * u;
-    t.na = t.nb = min(8, g.half - 8 * u);
+  if (!INTER && u < g.rot_units) {
+    t.a = 4 * u;
+    t.b = g.half + 4 * u;
+    t.na = t.nb = min(4, g.half - 4 * u);
   } else {
-    t.a = 2 * g.half + 16 * (u - g.rot_units);
-    t.b = t.a + 8;
-    t.na = max(0, min(8, g.dim - t.a));
-    t.nb = max(0, min(8, g.dim - t.b));
+    t.a = INTER ? 8 * u : 2 * g.half + 8 * (u - g.rot_units);
+    t.b = t.a + 4;
+    t.na = max(0, min(4, g.dim - t.a));
+    t.nb = max(0, min(4, g.dim - t.b));
   }
   return t;
+}
+// The e-th of the lane's values: where it lies in the row, -1: nowhere.
+__device__ __forceinline__ int place(const Unit& t, int e) {
+  return e < 4 ? (e < t.na ? t.a + e : -1) : (e - 4 < t.nb ? t.b + e - 4 : -1);
 }
 
 template <typename T, int V> struct alignas(V * sizeof(T)) Vec { T v[V]; };
 
-// Runs of values between memory and registers, V at a time; values past the
-// run are zero.
-template <typename T, int V>
-__device__ __forceinline__ void load_run(const T* p, int n, float* v) {
-  constexpr int L = V * sizeof(T) > 16 ? 16 / sizeof(T) : V;
-#pragma unroll
-  for (int i = 0; i < 8; i += L) {
-    Vec<T, L> x;
-    if (i < n) {
-      x = *reinterpret_cast<const Vec<T, L>*>(p + i);
-#pragma unroll
-      for (int e = 0; e < L; ++e) v[i + e] = to_f32(x.v[e]);
+// A lane's 8 values between memory and registers, V at a time; values past a run
+// are zero, and not written.
+template <typename T, int V> struct Raw {
+  uint32_t w[8 * sizeof(T) / 4];
+  // the V values at p into words i ..
+  __device__ __forceinline__ void get(const T* p, int i) {
+    constexpr int kBytes = V * sizeof(T);
+    const int at = i * static_cast<int>(sizeof(T)) / 4;
+    if constexpr (kBytes == 16) {
+      const uint4 q = *reinterpret_cast<const uint4*>(p);
+      w[at] = q.x; w[at + 1] = q.y; w[at + 2] = q.z; w[at + 3] = q.w;
+    } else if constexpr (kBytes == 8) {
+      const uint2 q = *reinterpret_cast<const uint2*>(p);
+      w[at] = q.x; w[at + 1] = q.y;
+    } else if constexpr (kBytes == 4) {
+      w[at] = *reinterpret_cast<const uint32_t*>(p);
     } else {
-#pragma unroll
-      for (int e = 0; e < L; ++e) v[i + e] = 0.f;
+      w[at] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p)) << (16 * (i & 1));
     }
   }
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_run(T* p, int n, const float* v) {
-  constexpr int L = V * sizeof(T) > 16 ? 16 / sizeof(T) : V;
+  __device__ __forceinline__ void load(const T* p, const Unit& t, bool live) {
 #pragma unroll
-  for (int i = 0; i < 8; i += L)
-    if (i < n) {
-      Vec<T, L> x;
+    for (int i = 0; i < static_cast<int>(8 * sizeof(T) / 4); ++i) w[i] = 0;
 #pragma unroll
-      for (int e = 0; e < L; ++e) x.v[e] = from_f32<T>(v[i + e]);
-      *reinterpret_cast<Vec<T, L>*>(p + i) = x;
-    }
-}
-
-// The lane's 16 values turned by its angles (`back`: by minus them).
-template <bool INTER>
-__device__ __forceinline__ void turn(float (&y)[16], const float (&c)[8], const float (&s)[8], uint32_t turned, bool back) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float& p = INTER ? y[2 * e] : y[e];
-    float& q = INTER ? y[2 * e + 1] : y[8 + e];
-    const float sn = back ? -s[e] : s[e];
-    const float u = p * c[e] - q * sn, v = p * sn + q * c[e];
-    if (turned >> e & 1u) {
-      p = u;
-      q = v;
+    for (int i = 0; i < 4; i += V) {
+      if (live && i < t.na) get(p + t.a + i, i);
+      if (live && i < t.nb) get(p + t.b + i, 4 + i);
     }
   }
+  __device__ __forceinline__ void unpack(float (&v)[8]) {
+    // the words stay words until here: converted where they are loaded, they
+    // would be waited for there
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(8 * sizeof(T) / 4); ++i) asm volatile("" : "+r"(w[i]));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      v[i] = sizeof(T) == 4 ? __uint_as_float(w[i]) : i & 1 ? bf16hi(w[i / 2]) : bf16lo(w[i / 2]);
+  }
+  static __device__ __forceinline__ void store(T* p, const Unit& t, const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; i += V) {
+      Vec<T, V> x, y;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        x.v[e] = from_f32<T>(v[i + e]);
+        y.v[e] = from_f32<T>(v[4 + i + e]);
+      }
+      if (i < t.na) *reinterpret_cast<Vec<T, V>*>(p + t.a + i) = x;
+      if (i < t.nb) *reinterpret_cast<Vec<T, V>*>(p + t.b + i) = y;
+    }
+  }
+};
+
+// The e-th pair of a lane's values.
+template <bool INTER> __device__ constexpr int first_of(int e) { return INTER ? 2 * e : e; }
+template <bool INTER> __device__ constexpr int second_of(int e) { return INTER ? 2 * e + 1 : 4 + e; }
+
+// Sums over the lanes of a row, of several values at once.
+template <int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int lanes) {
+  for (int o = 1; o < lanes; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
-__device__ __forceinline__ float row_sum(float v, int lanes) {
-  for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-__device__ __forceinline__ float squares(const float (&x)[16]) {
+__device__ __forceinline__ float dot(const float (&x)[8], const float (&y)[8]) {
   float sum = 0.f;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) sum = fmaf(x[e], x[e], sum);
+  for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
   return sum;
 }
 
-// x becomes xh; returns the factor r that did it (0 where x has no finite norm).
-__device__ __forceinline__ float normalize(float (&x)[16], const RotArgs& g) {
-  float sum = row_sum(squares(x), g.lanes), scale = 1.f;
-  // Where squares leave fp32's range the row is scaled by a power of two first.
-  const bool large = !(sum < 0x1p126f);
-  if (__any_sync(0xffffffffu, large)) {
-    scale = large ? 0x1p-96f : 1.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] *= scale;
-    sum = row_sum(squares(x), g.lanes);
-  }
-  const float m = fmaf(sum, g.inv_dim, g.eps * scale * scale);
-  float r = rsqrtf(m);
+// 1 / sqrt(sum / dim + eps)
+__device__ __forceinline__ float inverse_root(float sum, const RotArgs& g, float eps) {
+  const float m = fmaf(sum, g.inv_dim, eps);
+  const float r = rsqrtf(m);
   // one Newton step: rsqrtf may be off by two units in the last place
-  if (m < INFINITY) r = fmaf(0.5f * r, fmaf(-m * r, r, 1.f), r);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) x[e] *= r;
-  return r * scale;
+  return m < INFINITY ? fmaf(0.5f * r, fmaf(-m * r, r, 1.f), r) : r;
 }
+// Rows whose squares leave fp32's range are scaled by a power of two first.
+constexpr float kLargeSum = 0x1p126f, kDown = 0x1p-96f;
 
-// Each warp walks its share of the (token group, head) units: 32 / lanes tokens
-// of a head at once.  BWD: gradients.
+// CTAs per SM, which the registers are bounded for.
+template <typename T, bool BWD> constexpr int per_sm() { return BWD ? 2 : 3; }
+
+// Each warp walks its share of the (token group, two heads) units: 32 / lanes
+// tokens at once.  The next unit is on its way while one is worked on.  BWD:
+// gradients.
 template <typename T, int V, bool INTER, bool BWD>
-__global__ void __launch_bounds__(kThreads) k_qkrot(const __grid_constant__ RotArgs g) {
+__global__ void __launch_bounds__(kThreads, per_sm<T, BWD>()) k_qkrot(const __grid_constant__ RotArgs g) {
   const int side = blockIdx.x >= g.ctas;
   const int cta = side ? blockIdx.x - g.ctas : blockIdx.x, ctas = side ? gridDim.x - g.ctas : g.ctas;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int u = lane & (g.lanes - 1), rows = 32 / g.lanes, sub = lane / g.lanes;
   const Unit t = unit_of<INTER>(g, u);
-  const int heads = g.heads[side];
-  const int64_t units = (g.tokens + rows - 1) / rows * heads;
+  const int heads = g.heads[side], twos = (heads + 1) / 2;
+  const int64_t units = (g.tokens + rows - 1) / rows * twos;
   const int64_t n_warps = static_cast<int64_t>(ctas) * kWarps, w = static_cast<int64_t>(cta) * kWarps + warp;
-  int64_t unit = units * w / n_warps, group = unit / heads;
+  int64_t unit = units * w / n_warps;
   const int64_t end = units * (w + 1) / n_warps;
-  int head = static_cast<int>(unit - group * heads);
   uint32_t turned = 0;
+  float wt[8], dw[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (8 * u + e < g.half && (INTER || u < g.rot_units)) turned |= 1u << e;
-  float wt[16], dw[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const bool in = e < 8 ? e < t.na : e - 8 < t.nb;
-    wt[e] = in ? weight(g, side, e < 8 ? t.a + e : t.b + e - 8) : 0.f;
+  for (int e = 0; e < 8; ++e) {
+    if (e < 4 && 4 * u + e < g.half && (INTER || u < g.rot_units)) turned |= 1u << e;
+    const int at = place(t, e);
+    wt[e] = at < 0 ? 0.f : weight(g, side, at);
     dw[e] = 0.f;
   }
-  float c[8], s[8];
-  bool fresh = true;
-  for (; unit < end; ++unit) {
-    const int64_t token = group * rows + sub;
+
+  // the unit on its way: its place, values and position
+  int64_t token = unit / twos * rows + sub, next_pos = 0;
+  int head = 2 * static_cast<int>(unit % twos);
+  Raw<T, V> nx[2], nz[2];
+  const bool want_x = !BWD || g.norm;
+  auto fetch = [&](bool position) {
     const bool live = token < g.used;
-    if (fresh) {
-      int64_t p = 0;
-      if (turned && live) p = g.pos64 ? static_cast<const int64_t*>(g.pos)[token] : static_cast<const int*>(g.pos)[token];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+    for (int i = 0; i < 2; ++i) {
+      const bool in = live && head + i < heads;
+      if (want_x) nx[i].load(static_cast<const T*>(g.x[side].p) + token * g.x[side].ts + (head + i) * g.x[side].hs, t, in);
+      if constexpr (BWD)
+        nz[i].load(static_cast<const T*>(g.dz[side].p) + token * g.dz[side].ts + (head + i) * g.dz[side].hs, t, in);
+    }
+    if (position) {
+      next_pos = 0;
+      if (turned && live) next_pos = g.pos64 ? static_cast<const int64_t*>(g.pos)[token] : static_cast<const int*>(g.pos)[token];
+    }
+  };
+  float c[4], s[4];
+  bool fresh = true;
+  if (unit < end) fetch(true);
+  while (unit < end) {
+    float x[2][8], y[2][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (want_x) nx[i].unpack(x[i]);
+      if constexpr (BWD) nz[i].unpack(y[i]);
+    }
+    if (fresh) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
         c[e] = 1.f;
         s[e] = 0.f;
-        if (turned >> e & 1u) circle(static_cast<uint64_t>(p) * g.turns[8 * u + e], c[e], s[e]);
+        if (turned >> e & 1u) circle(static_cast<uint64_t>(next_pos) * g.turns[4 * u + e], c[e], s[e]);
       }
-      fresh = false;
     }
-    const int na = live ? t.na : 0, nb = live ? t.nb : 0;
-    float x[16], y[16];
-    float r = 1.f;
-    if (!BWD || g.norm) {
-      const T* px = static_cast<const T*>(g.x[side].p) + token * g.x[side].ts + head * g.x[side].hs;
-      load_run<T, V>(px + t.a, na, x);
-      load_run<T, V>(px + t.b, nb, x + 8);
-      if (g.norm) r = normalize(x, g);
-    }
-    if constexpr (BWD) {
-      const T* pz = static_cast<const T*>(g.dz[side].p) + token * g.dz[side].ts + head * g.dz[side].hs;
-      load_run<T, V>(pz + t.a, na, y);
-      load_run<T, V>(pz + t.b, nb, y + 8);
-      turn<INTER>(y, c, s, turned, true);
-      if (g.norm) {
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          dw[e] = fmaf(y[e], x[e], dw[e]);
-          y[e] *= wt[e];
-          sum = fmaf(y[e], x[e], sum);
-        }
-        const float m = row_sum(sum, g.lanes) * g.inv_dim;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) y[e] = r * fmaf(-x[e], m, y[e]);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = x[e] * wt[e];
-      turn<INTER>(y, c, s, turned, false);
-    }
-    if (!live) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = 0.f;
-    }
-    if (token < g.tokens) {
-      T* po = static_cast<T*>(g.out[side].p) + token * g.out[side].ts + head * g.out[side].hs;
-      store_run<T, V>(po + t.a, t.na, y);
-      store_run<T, V>(po + t.b, t.nb, y + 8);
-    }
-    if (++head == heads) {
+    const int64_t here = token;
+    const int at = head;
+    ++unit;
+    head += 2;
+    fresh = head >= heads;
+    if (fresh) {
       head = 0;
-      ++group;
-      fresh = true;
+      token += rows;
+    }
+    if (unit < end) fetch(fresh);
+
+    if constexpr (!BWD) {
+      float r[2] = {1.f, 1.f};
+      if (g.norm) {
+        float sum[2] = {dot(x[0], x[0]), dot(x[1], x[1])};
+        row_sums(sum, g.lanes);
+        if (__any_sync(0xffffffffu, !(sum[0] < kLargeSum && sum[1] < kLargeSum))) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float scale = sum[i] < kLargeSum ? 1.f : kDown;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] *= scale;
+            float again[1] = {dot(x[i], x[i])};
+            row_sums(again, g.lanes);
+            r[i] = inverse_root(again[0], g, g.eps * scale * scale);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) r[i] = inverse_root(sum[i], g, g.eps);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int p = first_of<INTER>(e), q = second_of<INTER>(e);
+          const float a = x[i][p] * r[i] * wt[p], b = x[i][q] * r[i] * wt[q];
+          y[i][p] = fmaf(a, c[e], -(b * s[e]));
+          y[i][q] = fmaf(a, s[e], b * c[e]);
+        }
+    } else {
+      // g in place of dz
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int p = first_of<INTER>(e), q = second_of<INTER>(e);
+          const float a = y[i][p], b = y[i][q];
+          y[i][p] = fmaf(a, c[e], b * s[e]);
+          y[i][q] = fmaf(b, c[e], -(a * s[e]));
+        }
+      if (g.norm) {
+        float sum[4], r[2], m[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sum[i] = dot(x[i], x[i]);
+          sum[2 + i] = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[2 + i] = fmaf(y[i][e] * wt[e], x[i][e], sum[2 + i]);
+        }
+        row_sums(sum, g.lanes);
+        const bool fits = sum[0] < kLargeSum && sum[1] < kLargeSum && fabsf(sum[2]) < INFINITY && fabsf(sum[3]) < INFINITY;
+        if (__any_sync(0xffffffffu, !fits)) {
+          // <u, x> may be out of range with x: from xh instead
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float scale = sum[i] < kLargeSum ? 1.f : kDown;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] *= scale;
+            float again[1] = {dot(x[i], x[i])};
+            row_sums(again, g.lanes);
+            r[i] = inverse_root(again[0], g, g.eps * scale * scale);
+            again[0] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              x[i][e] *= r[i];
+              again[0] = fmaf(y[i][e] * wt[e], x[i][e], again[0]);
+            }
+            row_sums(again, g.lanes);
+            m[i] = again[0] * g.inv_dim;
+            r[i] *= scale;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            r[i] = inverse_root(sum[i], g, g.eps);
+            m[i] = sum[2 + i] * g.inv_dim * r[i];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] *= r[i];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            dw[e] = fmaf(y[i][e], x[i][e], dw[e]);
+            y[i][e] = r[i] * fmaf(-x[i][e], m[i], y[i][e] * wt[e]);
+          }
+      }
+    }
+    if (here >= g.used) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[i][e] = 0.f;
+    }
+    if (here < g.tokens) {
+      T* po = static_cast<T*>(g.out[side].p) + here * g.out[side].ts + at * g.out[side].hs;
+      Raw<T, V>::store(po, t, y[0]);
+      if (at + 1 < heads) Raw<T, V>::store(po + g.out[side].hs, t, y[1]);
     }
   }
   if constexpr (BWD) {
     // the CTA's weight gradients: over the rows of a warp, then over the warps
     if (!g.part) return;
-    __shared__ float sm[kWarps][16 * 16];
+    __shared__ float sm[kWarps][8 * 32];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
+    for (int e = 0; e < 8; ++e) {
       for (int o = g.lanes; o < 32; o <<= 1) dw[e] += __shfl_xor_sync(0xffffffffu, dw[e], o);
-      if (sub == 0) sm[warp][16 * u + e] = dw[e];
+      if (sub == 0) sm[warp][8 * u + e] = dw[e];
     }
     __syncthreads();
-    if (threadIdx.x < 16 * g.lanes) {
-      const Unit m = unit_of<INTER>(g, threadIdx.x >> 4);
-      const int e = threadIdx.x & 15;
+    if (threadIdx.x < 8 * g.lanes) {
+      const int to = place(unit_of<INTER>(g, threadIdx.x >> 3), threadIdx.x & 7);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) sum += sm[i][threadIdx.x];
-      if (e < 8 ? e < m.na : e - 8 < m.nb)
-        g.part[static_cast<int64_t>(blockIdx.x) * g.dim + (e < 8 ? m.a + e : m.b + e - 8)] = sum;
+      if (to >= 0) g.part[static_cast<int64_t>(blockIdx.x) * g.dim + to] = sum;
     }
   }
 }
@@ -324,13 +414,25 @@ int done(cudaError_t e, const char* what) {
   return e ? fail(NORMPRE_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e)) : NORMPRE_OK;
 }
 
+// Shares the CTAs out by heads, every warp at least one unit; returns their number.
+unsigned share(RotArgs* g, int per_sm) {
+  const int64_t groups = cdiv(g->tokens, 32 / g->lanes);
+  const int64_t most = std::min<int64_t>(kMaxCtas, static_cast<int64_t>(device_sm_count()) * per_sm);
+  const int64_t twos[2] = {cdiv(g->heads[0], 2), cdiv(g->heads[1], 2)};
+  const int64_t q = std::max<int64_t>(1, most * twos[0] / (twos[0] + twos[1])), k = std::max<int64_t>(1, most - q);
+  g->ctas = static_cast<int>(std::min(q, cdiv(groups * twos[0], kWarps)));
+  return static_cast<unsigned>(g->ctas + std::min(k, cdiv(groups * twos[1], kWarps)));
+}
+
+// Returns the number of CTAs.
 template <typename T, bool BWD>
-void launch(const RotArgs& g, int v, bool inter, unsigned ctas, cudaStream_t s) {
-  if (inter) k_qkrot<T, 8, true, BWD><<<ctas, kThreads, 0, s>>>(g);
-  else if (v == 8) k_qkrot<T, 8, false, BWD><<<ctas, kThreads, 0, s>>>(g);
-  else if (v == 4) k_qkrot<T, 4, false, BWD><<<ctas, kThreads, 0, s>>>(g);
-  else if (v == 2) k_qkrot<T, 2, false, BWD><<<ctas, kThreads, 0, s>>>(g);
-  else k_qkrot<T, 1, false, BWD><<<ctas, kThreads, 0, s>>>(g);
+unsigned launch(RotArgs* g, int v, bool inter, cudaStream_t s) {
+  const unsigned ctas = share(g, per_sm<T, BWD>());
+  if (inter) k_qkrot<T, 4, true, BWD><<<ctas, kThreads, 0, s>>>(*g);
+  else if (v == 4) k_qkrot<T, 4, false, BWD><<<ctas, kThreads, 0, s>>>(*g);
+  else if (v == 2) k_qkrot<T, 2, false, BWD><<<ctas, kThreads, 0, s>>>(*g);
+  else k_qkrot<T, 1, false, BWD><<<ctas, kThreads, 0, s>>>(*g);
+  return ctas;
 }
 
 // What both directions take; fills in all but the gradients.
@@ -372,26 +474,15 @@ int base(const normpre_qkrot* p, int64_t tokens, int64_t used, const normpre_hea
   g->norm = c.norm;
   g->eps = c.eps;
   g->inv_dim = 1.f / static_cast<float>(c.head_dim);
-  g->rot_units = static_cast<int>(cdiv(p->half, 8));
-  const int units = c.interleaved ? static_cast<int>(cdiv(c.head_dim, 16))
-                                  : g->rot_units + static_cast<int>(cdiv(c.head_dim - 2 * p->half, 16));
+  g->rot_units = static_cast<int>(cdiv(p->half, 4));
+  const int units = c.interleaved ? c.head_dim / 8 : g->rot_units + static_cast<int>(cdiv(c.head_dim - 2 * p->half, 8));
   for (g->lanes = 1; g->lanes < units;) g->lanes *= 2;
   for (int i = 0; i < p->half; ++i) g->turns[i] = p->turns[i];
   return NORMPRE_OK;
 }
 
-// Shares the CTAs out by heads, every warp at least one unit; returns their number.
-unsigned share(RotArgs* g, int per_sm) {
-  const int64_t groups = cdiv(g->tokens, 32 / g->lanes);
-  const int64_t most = std::min<int64_t>(kMaxCtas, static_cast<int64_t>(device_sm_count()) * per_sm);
-  const int64_t all = g->heads[0] + g->heads[1];
-  const int64_t q = std::max<int64_t>(1, most * g->heads[0] / all), k = std::max<int64_t>(1, most - q);
-  g->ctas = static_cast<int>(std::min(q, cdiv(groups * g->heads[0], kWarps)));
-  return static_cast<unsigned>(g->ctas + std::min(k, cdiv(groups * g->heads[1], kWarps)));
-}
-
 // The most values that one access may take: of a run that starts at a multiple of half.
-int width(int half) { return half % 8 == 0 ? 8 : half % 4 == 0 ? 4 : half % 2 == 0 ? 2 : 1; }
+int width(int half) { return half % 4 == 0 ? 4 : half % 2 == 0 ? 2 : 1; }
 
 }  // namespace
 }  // namespace normpre
@@ -444,9 +535,8 @@ int normpre_qkrot_forward(const normpre_qkrot* p, int64_t tokens, int64_t used, 
       (rc = take_heads(k_out, tokens, c.n_kv_heads, c.head_dim, c.dtype, "k_out", true, &g.out[1])))
     return rc;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const unsigned ctas = share(&g, 4);
-  if (c.dtype == NORMPRE_BF16) launch<bf16, false>(g, width(p->half), c.interleaved, ctas, s);
-  else launch<float, false>(g, width(p->half), c.interleaved, ctas, s);
+  if (c.dtype == NORMPRE_BF16) launch<bf16, false>(&g, width(p->half), c.interleaved, s);
+  else launch<float, false>(&g, width(p->half), c.interleaved, s);
   return done(cudaGetLastError(), "query and key norms");
 }
 
@@ -479,9 +569,8 @@ int normpre_qkrot_backward(const normpre_qkrot* p, int64_t tokens, int64_t used,
         (rc = take_heads(dk, tokens, c.n_kv_heads, c.head_dim, c.dtype, "dk", true, &g.out[1])))
       return rc;
     g.part = weights ? static_cast<float*>(workspace) : nullptr;
-    ctas = share(&g, 2);
-    if (c.dtype == NORMPRE_BF16) launch<bf16, true>(g, width(p->half), c.interleaved, ctas, s);
-    else launch<float, true>(g, width(p->half), c.interleaved, ctas, s);
+    ctas = c.dtype == NORMPRE_BF16 ? launch<bf16, true>(&g, width(p->half), c.interleaved, s)
+                                   : launch<float, true>(&g, width(p->half), c.interleaved, s);
   }
   if (weights)
     k_qkrot_fold<<<dim3(static_cast<unsigned>(cdiv(c.head_dim, 32)), 2), dim3(32, 32), 0, s>>>(
