@@ -596,7 +596,7 @@ int normpre_qkrot_bytes(const normpre_qkrot* p, int64_t* bytes);
  * q, k, q_out, k_out: see normpre_heads; an output may be its input itself.
  * positions: device, one whole number per token, of 4 or 8 bytes
  * (position_bytes); not read where rotary_dim = 0.  weights: device, head_dim
- * contiguous values of weight_dtype.  tokens in [0, 2^31).
+ * contiguous values of weight_dtype.  tokens in [0, 2^30].
  * Asynchronous on `stream`, on the current device; allocates nothing.
  * Errors: ARG, SHAPE, DTYPE, ALIGN, CUDA.
  */

@@ -9,10 +9,10 @@
 // A row stays in registers between the sums and the result, so that every value
 // is read once and written once: bound by HBM.
 //
-// A lane holds four pairs of a row (8 values), of two heads at once: with them
+// A lane holds four pairs of a row (8 values), (bf16: of two heads at once): with them
 // the pairs' cos and sin, which it forms once per token and uses for all of its
-// heads; 1 to 32 lanes share a row, and the rows' sums of both heads travel
-// through the lanes together.  Half-split pairs (i, i + R/2) are two runs of up to
+// heads; 1 to 32 lanes share a row, and all sums of a unit travel through the
+// lanes together.  Half-split pairs (i, i + R/2) are two runs of up to
 // four values, read V at a time (V: the largest of 4, 2, 1 that divides R/2, so
 // that no access leaves its alignment); interleaved pairs two runs of four.
 //
@@ -29,6 +29,7 @@
 #include "common.cuh"
 #include "heads.h"
 #include "internal.h"
+#include "tc.cuh"
 
 using namespace normpre;
 
@@ -65,14 +66,22 @@ __device__ __forceinline__ float weight(const RotArgs& a, int side, int i) {
   return a.w_bf16 ? to_f32(static_cast<const bf16*>(a.w[side])[i]) : static_cast<const float*>(a.w[side])[i];
 }
 
-// cos and sin of `turns` 2^-64 turns: to the nearest eighth of a turn first, so
-// that the rest, at most 1/8, keeps all of its 24 bits.
+// cos and sin of `turns` 2^-64 turns: to the nearest quarter of a turn first, so
+// that the rest x, at most 1/4 of a half turn, keeps all of its 24 bits.  Then
+// sin(pi x) = x P(x^2) and cos(pi x) = 1 + x^2 Q(x^2), P and Q of third degree
+// through the Chebyshev points of [0, 1/16]: within 2.2 and 1.4 units of 2^-24 of
+// their values over all x.
 __device__ __forceinline__ void circle(uint64_t turns, float& c, float& s) {
   const uint64_t u = turns + (uint64_t(1) << 61);
   const int quarter = static_cast<int>(u >> 62);
   const int64_t rest = static_cast<int64_t>(u & ((uint64_t(1) << 62) - 1)) - (int64_t(1) << 61);
-  float cc, ss;
-  sincospif(static_cast<float>(static_cast<int>(rest >> 30)) * 0x1p-33f, &ss, &cc);
+  const float x = static_cast<float>(static_cast<int>(rest >> 30)) * 0x1p-33f, z = x * x;
+  float ss = fmaf(z, -0.5890750885009766f, 2.549767017364502f);
+  ss = fmaf(z, ss, -5.167707920074463f);
+  ss = x * fmaf(z, ss, 3.1415927410125732f);
+  float cc = fmaf(z, 0.2321254163980484f, -1.3351378440856934f);
+  cc = fmaf(z, cc, 4.05871057510376f);
+  cc = fmaf(z, fmaf(z, cc, -4.934802055358887f), 1.f);
   c = quarter & 1 ? ss : cc;
   s = quarter & 1 ? cc : ss;
   if (quarter == 1 || quarter == 2) c = -c;
@@ -98,18 +107,25 @@ __device__ __forceinline__ Unit unit_of(const RotArgs& g, int u) {
   }
   return t;
 }
-// The e-th of the lane's values: where it lies in the row, -1: nowhere.
+// The e-th of the lane's values, its pairs' first ones and then their second
+// ones: where it lies in the row, -1: nowhere.
+template <bool INTER>
 __device__ __forceinline__ int place(const Unit& t, int e) {
-  return e < 4 ? (e < t.na ? t.a + e : -1) : (e - 4 < t.nb ? t.b + e - 4 : -1);
+  const int m = !INTER ? e : e < 4 ? 2 * e : 2 * (e - 4) + 1;
+  return m < 4 ? (m < t.na ? t.a + m : -1) : (m - 4 < t.nb ? t.b + m - 4 : -1);
 }
 
 template <typename T, int V> struct alignas(V * sizeof(T)) Vec { T v[V]; };
 
-// A lane's 8 values between memory and registers, V at a time; values past a run
-// are zero, and not written.
+// A lane's 8 values as they lie in memory, read and written V at a time.
 template <typename T, int V> struct Raw {
-  uint32_t w[8 * sizeof(T) / 4];
-  // the V values at p into words i ..
+  static constexpr int kWords = 8 * sizeof(T) / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+  }
+  // the V values at p become the i-th ..
   __device__ __forceinline__ void get(const T* p, int i) {
     constexpr int kBytes = V * sizeof(T);
     const int at = i * static_cast<int>(sizeof(T)) / 4;
@@ -122,59 +138,77 @@ template <typename T, int V> struct Raw {
     } else if constexpr (kBytes == 4) {
       w[at] = *reinterpret_cast<const uint32_t*>(p);
     } else {
-      w[at] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p)) << (16 * (i & 1));
+      const uint32_t v = *reinterpret_cast<const uint16_t*>(p);
+      w[at] = i & 1 ? (w[at] & 0xFFFFu) | v << 16 : v;
     }
   }
-  __device__ __forceinline__ void load(const T* p, const Unit& t, bool live) {
-#pragma unroll
-    for (int i = 0; i < static_cast<int>(8 * sizeof(T) / 4); ++i) w[i] = 0;
+  // a: the lane's first run.  What lies past a run stays as it is.
+  __device__ __forceinline__ void load(const T* a, const Unit& t) {
 #pragma unroll
     for (int i = 0; i < 4; i += V) {
-      if (live && i < t.na) get(p + t.a + i, i);
-      if (live && i < t.nb) get(p + t.b + i, 4 + i);
+      if (i < t.na) get(a + i, i);
+      if (i < t.nb) get(a + (t.b - t.a) + i, 4 + i);
     }
   }
-  __device__ __forceinline__ void unpack(float (&v)[8]) {
+  // Pairs of values: 0, 1 the pairs' first ones, 2, 3 their second ones.
+  template <bool INTER> __device__ __forceinline__ void unpack(uint64_t (&v)[4]) {
     // the words stay words until here: converted where they are loaded, they
     // would be waited for there
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(8 * sizeof(T) / 4); ++i) asm volatile("" : "+r"(w[i]));
+    for (int i = 0; i < kWords; ++i) asm volatile("" : "+r"(w[i]));
+    auto at = [&](int m) {
+      return sizeof(T) == 4 ? __uint_as_float(w[m]) : m & 1 ? bf16hi(w[m / 2]) : bf16lo(w[m / 2]);
+    };
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      v[i] = sizeof(T) == 4 ? __uint_as_float(w[i]) : i & 1 ? bf16hi(w[i / 2]) : bf16lo(w[i / 2]);
+    for (int i = 0; i < 2; ++i) {
+      v[i] = INTER ? tc::pack2(at(4 * i), at(4 * i + 2)) : tc::pack2(at(2 * i), at(2 * i + 1));
+      v[2 + i] = INTER ? tc::pack2(at(4 * i + 1), at(4 * i + 3)) : tc::pack2(at(4 + 2 * i), at(4 + 2 * i + 1));
+    }
   }
-  static __device__ __forceinline__ void store(T* p, const Unit& t, const float (&v)[8]) {
+  template <bool INTER> static __device__ __forceinline__ void store(T* a, const Unit& t, const uint64_t (&v)[4]) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = INTER ? (i < 2 ? 4 * i : 4 * i - 7) : 2 * i;
+      tc::unpack2(v[i], f[e], f[e + (INTER ? 2 : 1)]);
+    }
 #pragma unroll
     for (int i = 0; i < 4; i += V) {
       Vec<T, V> x, y;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x.v[e] = from_f32<T>(v[i + e]);
-        y.v[e] = from_f32<T>(v[4 + i + e]);
+        x.v[e] = from_f32<T>(f[i + e]);
+        y.v[e] = from_f32<T>(f[4 + i + e]);
       }
-      if (i < t.na) *reinterpret_cast<Vec<T, V>*>(p + t.a + i) = x;
-      if (i < t.nb) *reinterpret_cast<Vec<T, V>*>(p + t.b + i) = y;
+      if (i < t.na) *reinterpret_cast<Vec<T, V>*>(a + i) = x;
+      if (i < t.nb) *reinterpret_cast<Vec<T, V>*>(a + (t.b - t.a) + i) = y;
     }
   }
 };
 
-// The e-th pair of a lane's values.
-template <bool INTER> __device__ constexpr int first_of(int e) { return INTER ? 2 * e : e; }
-template <bool INTER> __device__ constexpr int second_of(int e) { return INTER ? 2 * e + 1 : 4 + e; }
-
 // Sums over the lanes of a row, of several values at once.
 template <int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], int lanes) {
-  for (int o = 1; o < lanes; o <<= 1)
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  for (int o = 1; o < 32; o <<= 1)
+    if (o < lanes) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
 }
 
-__device__ __forceinline__ float dot(const float (&x)[8], const float (&y)[8]) {
-  float sum = 0.f;
+__device__ __forceinline__ float dot(const uint64_t (&x)[4], const uint64_t (&y)[4]) {
+  uint64_t sum = tc::mul2(x[0], y[0]);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
-  return sum;
+  for (int e = 1; e < 4; ++e) sum = tc::fma2(x[e], y[e], sum);
+  float lo, hi;
+  tc::unpack2(sum, lo, hi);
+  return lo + hi;
+}
+__device__ __forceinline__ void scale(uint64_t (&x)[4], float f) {
+  const uint64_t f2 = tc::pack2(f, f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = tc::mul2(x[e], f2);
 }
 
 // 1 / sqrt(sum / dim + eps)
@@ -190,178 +224,252 @@ constexpr float kLargeSum = 0x1p126f, kDown = 0x1p-96f;
 // CTAs per SM, which the registers are bounded for.
 template <typename T, bool BWD> constexpr int per_sm() { return BWD ? 2 : 3; }
 
-// Each warp walks its share of the (token group, two heads) units: 32 / lanes
-// tokens at once.  The next unit is on its way while one is worked on.  BWD:
-// gradients.
-template <typename T, int V, bool INTER, bool BWD>
-__global__ void __launch_bounds__(kThreads, per_sm<T, BWD>()) k_qkrot(const __grid_constant__ RotArgs g) {
-  const int side = blockIdx.x >= g.ctas;
+// Heads of a unit: fp32 has no registers for two on their way.
+template <typename T> constexpr int kUnitHeads = sizeof(T) == 2 ? 2 : 1;
+
+// Each warp walks its share of the (token group, heads) units: 32 / lanes tokens
+// at once.  The next unit is on its way while one is worked on.  BWD:
+// gradients.  side: 0 queries, 1 keys, known to the compiler so that what the
+// launch's arguments hold for it needs no registers.
+template <typename T, int V, bool INTER, bool BWD, int side>
+__device__ __forceinline__ void walk(const RotArgs& g) {
+  constexpr int H = kUnitHeads<T>;
+  using tc::fma2;
+  using tc::mul2;
   const int cta = side ? blockIdx.x - g.ctas : blockIdx.x, ctas = side ? gridDim.x - g.ctas : g.ctas;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int u = lane & (g.lanes - 1), rows = 32 / g.lanes, sub = lane / g.lanes;
   const Unit t = unit_of<INTER>(g, u);
-  const int heads = g.heads[side], twos = (heads + 1) / 2;
-  const int64_t units = (g.tokens + rows - 1) / rows * twos;
+  const int heads = g.heads[side], parts = (heads + H - 1) / H;
+  const int64_t units = (g.tokens + rows - 1) / rows * parts;
   const int64_t n_warps = static_cast<int64_t>(ctas) * kWarps, w = static_cast<int64_t>(cta) * kWarps + warp;
-  int64_t unit = units * w / n_warps;
-  const int64_t end = units * (w + 1) / n_warps;
+  const int64_t begin = units * w / n_warps;
+  int left = static_cast<int>(units * (w + 1) / n_warps - begin);
   uint32_t turned = 0;
-  float wt[8], dw[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (e < 4 && 4 * u + e < g.half && (INTER || u < g.rot_units)) turned |= 1u << e;
-    const int at = place(t, e);
-    wt[e] = at < 0 ? 0.f : weight(g, side, at);
-    dw[e] = 0.f;
+  for (int e = 0; e < 4; ++e)
+    if (4 * u + e < g.half && (INTER || u < g.rot_units)) turned |= 1u << e;
+  __shared__ __align__(16) float sw[8 * 32];   // the weights by lane
+  if (threadIdx.x < 8 * g.lanes) {
+    const int at = place<INTER>(unit_of<INTER>(g, threadIdx.x >> 3), threadIdx.x & 7);
+    sw[threadIdx.x] = at < 0 ? 0.f : weight(g, side, at);
+  }
+  __syncthreads();
+  auto weights = [&](int e) { return reinterpret_cast<const uint64_t*>(sw)[4 * u + e]; };
+  uint64_t wt[4], dw[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    wt[e] = BWD ? weights(e) : 0;
+    dw[e] = 0;
   }
 
   // the unit on its way: its place, values and position
-  int64_t token = unit / twos * rows + sub, next_pos = 0;
-  int head = 2 * static_cast<int>(unit % twos);
-  Raw<T, V> nx[2], nz[2];
   const bool want_x = !BWD || g.norm;
-  auto fetch = [&](bool position) {
-    const bool live = token < g.used;
+  int token = static_cast<int>(begin / parts) * rows + sub;   // at most 2^30 + 31
+  int head = H * static_cast<int>(begin % parts);
+  int64_t pos = 0;
+  const T *px = nullptr, *pz = nullptr;      // its first head's row, from this lane's first run on
+  T* po = nullptr;
+  bool live = false, exists = false, all = false;   // its token counts, is a row of the call; all of the warp's count
+  Raw<T, V> nx[H], nz[H];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const bool in = live && head + i < heads;
-      if (want_x) nx[i].load(static_cast<const T*>(g.x[side].p) + token * g.x[side].ts + (head + i) * g.x[side].hs, t, in);
-      if constexpr (BWD)
-        nz[i].load(static_cast<const T*>(g.dz[side].p) + token * g.dz[side].ts + (head + i) * g.dz[side].hs, t, in);
-    }
-    if (position) {
-      next_pos = 0;
-      if (turned && live) next_pos = g.pos64 ? static_cast<const int64_t*>(g.pos)[token] : static_cast<const int*>(g.pos)[token];
-    }
+  for (int i = 0; i < H; ++i) {
+    nx[i].clear();
+    nz[i].clear();
+  }
+  auto enter = [&]() {
+    auto row = [&](const HeadsView& v) { return static_cast<T*>(v.p) + token * v.ts + (head * v.hs + t.a); };
+    if (want_x) px = row(g.x[side]);
+    if (BWD) pz = row(g.dz[side]);
+    po = row(g.out[side]);
+    live = token < g.used;
+    exists = token < g.tokens;
+    all = token - sub + rows <= g.used;
+    pos = 0;
+    if (turned && live) pos = g.pos64 ? static_cast<const int64_t*>(g.pos)[token] : static_cast<const int*>(g.pos)[token];
   };
-  float c[4], s[4];
-  bool fresh = true;
-  if (unit < end) fetch(true);
-  while (unit < end) {
-    float x[2][8], y[2][8];
+  auto fetch = [&]() {
+    if (!all || head + H > heads) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (want_x) nx[i].unpack(x[i]);
-      if constexpr (BWD) nz[i].unpack(y[i]);
+      for (int i = 0; i < H; ++i) {
+        nx[i].clear();
+        nz[i].clear();
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+      if (live && (i == 0 || head + i < heads)) {
+        if (want_x) nx[i].load(px + i * g.x[side].hs, t);
+        if (BWD) nz[i].load(pz + i * g.dz[side].hs, t);
+      }
+  };
+  // cos, sin of the pairs' angles; forward with the weights: first = x1 k0 + x2 k1, second = x1 k2 + x2 k3
+  uint64_t k0[2], k1[2], k2[2], k3[2];
+  bool fresh = true;
+  if (left) {
+    enter();
+    fetch();
+  }
+  while (left) {
+    uint64_t x[H][4], y[H][4];
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      if (want_x) nx[i].template unpack<INTER>(x[i]);
+      if (BWD) nz[i].template unpack<INTER>(y[i]);
     }
     if (fresh) {
+      float c[4], s[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         c[e] = 1.f;
         s[e] = 0.f;
-        if (turned >> e & 1u) circle(static_cast<uint64_t>(next_pos) * g.turns[4 * u + e], c[e], s[e]);
+        if (turned >> e & 1u) circle(static_cast<uint64_t>(pos) * g.turns[4 * u + e], c[e], s[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint64_t c2 = tc::pack2(c[2 * e], c[2 * e + 1]), s2 = tc::pack2(s[2 * e], s[2 * e + 1]);
+        const uint64_t n2 = tc::pack2(-s[2 * e], -s[2 * e + 1]);
+        const uint64_t w0 = BWD ? 0 : weights(e), w1 = BWD ? 0 : weights(2 + e);
+        k0[e] = BWD ? c2 : mul2(c2, w0);
+        k1[e] = BWD ? s2 : mul2(n2, w1);
+        k2[e] = BWD ? n2 : mul2(s2, w0);
+        k3[e] = BWD ? c2 : mul2(c2, w1);
       }
     }
-    const int64_t here = token;
-    const int at = head;
-    ++unit;
-    head += 2;
+    T* const to = po;
+    const int here = heads - head;             // heads from the unit's first one on
+    const bool count = live, write = exists, whole = all;
+    head += H;
     fresh = head >= heads;
-    if (fresh) {
-      head = 0;
-      token += rows;
+    if (--left) {
+      if (fresh) {
+        head = 0;
+        token += rows;
+        enter();
+      } else {
+        if (want_x) px += H * g.x[side].hs;
+        if (BWD) pz += H * g.dz[side].hs;
+        po += H * g.out[side].hs;
+      }
+      fetch();
     }
-    if (unit < end) fetch(fresh);
 
-    if constexpr (!BWD) {
-      float r[2] = {1.f, 1.f};
-      if (g.norm) {
-        float sum[2] = {dot(x[0], x[0]), dot(x[1], x[1])};
-        row_sums(sum, g.lanes);
-        if (__any_sync(0xffffffffu, !(sum[0] < kLargeSum && sum[1] < kLargeSum))) {
+    // the pairs turned, or turned back
+    auto turn = [&](uint64_t (&v)[4]) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float scale = sum[i] < kLargeSum ? 1.f : kDown;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] *= scale;
-            float again[1] = {dot(x[i], x[i])};
-            row_sums(again, g.lanes);
-            r[i] = inverse_root(again[0], g, g.eps * scale * scale);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) r[i] = inverse_root(sum[i], g, g.eps);
-        }
+      for (int e = 0; e < 2; ++e) {
+        const uint64_t a = v[e], b = v[2 + e];
+        v[e] = fma2(a, k0[e], mul2(b, k1[e]));
+        v[2 + e] = fma2(a, k2[e], mul2(b, k3[e]));
       }
+    };
+    if (!g.norm) {
+      // rotation only: what does not turn passes as it is, infinities too
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < H; ++i) {
+        uint64_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = y[i][e] = BWD ? y[i][e] : x[i][e];
+        turn(y[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int p = first_of<INTER>(e), q = second_of<INTER>(e);
-          const float a = x[i][p] * r[i] * wt[p], b = x[i][q] * r[i] * wt[q];
-          y[i][p] = fmaf(a, c[e], -(b * s[e]));
-          y[i][q] = fmaf(a, s[e], b * c[e]);
+          float was[2], is[2];
+          tc::unpack2(v[e], was[0], was[1]);
+          tc::unpack2(y[i][e], is[0], is[1]);
+          const uint32_t both = turned >> (2 * (e & 1));
+          y[i][e] = tc::pack2(both & 1u ? is[0] : was[0], both & 2u ? is[1] : was[1]);
         }
+      }
+    } else if constexpr (!BWD) {
+      float sum[H], r[H];
+      bool fits = true;
+#pragma unroll
+      for (int i = 0; i < H; ++i) sum[i] = dot(x[i], x[i]);
+      row_sums(sum, g.lanes);
+#pragma unroll
+      for (int i = 0; i < H; ++i) fits = fits && sum[i] < kLargeSum;
+      if (__any_sync(0xffffffffu, !fits)) {
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          const float down = sum[i] < kLargeSum ? 1.f : kDown;
+          scale(x[i], down);
+          float again[1] = {dot(x[i], x[i])};
+          row_sums(again, g.lanes);
+          r[i] = inverse_root(again[0], g, g.eps * down * down);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < H; ++i) r[i] = inverse_root(sum[i], g, g.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < H; ++i) {
+        turn(x[i]);
+        scale(x[i], r[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[i][e] = x[i][e];
+      }
     } else {
-      // g in place of dz
+      float sum[2 * H], r[H], m[H];
+      bool fits = true;
+      auto slope = [&](int i) {                 // <u, x>
+        uint64_t v[4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+        for (int e = 0; e < 4; ++e) v[e] = mul2(y[i][e], wt[e]);
+        return dot(v, x[i]);
+      };
+#pragma unroll
+      for (int i = 0; i < H; ++i) {
+        turn(y[i]);
+        sum[i] = dot(x[i], x[i]);
+        sum[H + i] = slope(i);
+      }
+      row_sums(sum, g.lanes);
+#pragma unroll
+      for (int i = 0; i < H; ++i) fits = fits && sum[i] < kLargeSum && fabsf(sum[H + i]) < INFINITY;
+      if (__any_sync(0xffffffffu, !fits)) {
+        // <u, x> may be out of range with x: from xh instead
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          const float down = sum[i] < kLargeSum ? 1.f : kDown;
+          scale(x[i], down);
+          float again[1] = {dot(x[i], x[i])};
+          row_sums(again, g.lanes);
+          r[i] = inverse_root(again[0], g, g.eps * down * down);
+          scale(x[i], r[i]);
+          again[0] = slope(i);
+          row_sums(again, g.lanes);
+          m[i] = again[0] * g.inv_dim;
+          r[i] *= down;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          r[i] = inverse_root(sum[i], g, g.eps);
+          m[i] = sum[H + i] * g.inv_dim * r[i];
+          scale(x[i], r[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < H; ++i) {
+        const uint64_t m2 = tc::pack2(-m[i], -m[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int p = first_of<INTER>(e), q = second_of<INTER>(e);
-          const float a = y[i][p], b = y[i][q];
-          y[i][p] = fmaf(a, c[e], b * s[e]);
-          y[i][q] = fmaf(b, c[e], -(a * s[e]));
+          dw[e] = fma2(y[i][e], x[i][e], dw[e]);
+          y[i][e] = fma2(x[i][e], m2, mul2(y[i][e], wt[e]));
         }
-      if (g.norm) {
-        float sum[4], r[2], m[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          sum[i] = dot(x[i], x[i]);
-          sum[2 + i] = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum[2 + i] = fmaf(y[i][e] * wt[e], x[i][e], sum[2 + i]);
-        }
-        row_sums(sum, g.lanes);
-        const bool fits = sum[0] < kLargeSum && sum[1] < kLargeSum && fabsf(sum[2]) < INFINITY && fabsf(sum[3]) < INFINITY;
-        if (__any_sync(0xffffffffu, !fits)) {
-          // <u, x> may be out of range with x: from xh instead
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float scale = sum[i] < kLargeSum ? 1.f : kDown;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] *= scale;
-            float again[1] = {dot(x[i], x[i])};
-            row_sums(again, g.lanes);
-            r[i] = inverse_root(again[0], g, g.eps * scale * scale);
-            again[0] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              x[i][e] *= r[i];
-              again[0] = fmaf(y[i][e] * wt[e], x[i][e], again[0]);
-            }
-            row_sums(again, g.lanes);
-            m[i] = again[0] * g.inv_dim;
-            r[i] *= scale;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            r[i] = inverse_root(sum[i], g, g.eps);
-            m[i] = sum[2 + i] * g.inv_dim * r[i];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] *= r[i];
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            dw[e] = fmaf(y[i][e], x[i][e], dw[e]);
-            y[i][e] = r[i] * fmaf(-x[i][e], m[i], y[i][e] * wt[e]);
-          }
+        scale(y[i], r[i]);
       }
     }
-    if (here >= g.used) {
+    if (!whole && !count) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < H; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[i][e] = 0.f;
+        for (int e = 0; e < 4; ++e) y[i][e] = 0;
     }
-    if (here < g.tokens) {
-      T* po = static_cast<T*>(g.out[side].p) + here * g.out[side].ts + at * g.out[side].hs;
-      Raw<T, V>::store(po, t, y[0]);
-      if (at + 1 < heads) Raw<T, V>::store(po + g.out[side].hs, t, y[1]);
+    if (write) {
+#pragma unroll
+      for (int i = 0; i < H; ++i)
+        if (i == 0 || i < here) Raw<T, V>::template store<INTER>(to + i * g.out[side].hs, t, y[i]);
     }
   }
   if constexpr (BWD) {
@@ -369,19 +477,30 @@ __global__ void __launch_bounds__(kThreads, per_sm<T, BWD>()) k_qkrot(const __gr
     if (!g.part) return;
     __shared__ float sm[kWarps][8 * 32];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      for (int o = g.lanes; o < 32; o <<= 1) dw[e] += __shfl_xor_sync(0xffffffffu, dw[e], o);
-      if (sub == 0) sm[warp][8 * u + e] = dw[e];
+    for (int e = 0; e < 4; ++e) {
+      float v[2];
+      tc::unpack2(dw[e], v[0], v[1]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        for (int o = g.lanes; o < 32; o <<= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        if (sub == 0) sm[warp][8 * u + 2 * e + i] = v[i];
+      }
     }
     __syncthreads();
     if (threadIdx.x < 8 * g.lanes) {
-      const int to = place(unit_of<INTER>(g, threadIdx.x >> 3), threadIdx.x & 7);
+      const int to = place<INTER>(unit_of<INTER>(g, threadIdx.x >> 3), threadIdx.x & 7);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) sum += sm[i][threadIdx.x];
       if (to >= 0) g.part[static_cast<int64_t>(blockIdx.x) * g.dim + to] = sum;
     }
   }
+}
+
+template <typename T, int V, bool INTER, bool BWD>
+__global__ void __launch_bounds__(kThreads, per_sm<T, BWD>()) k_qkrot(const __grid_constant__ RotArgs g) {
+  if (blockIdx.x < g.ctas) walk<T, V, INTER, BWD, 0>(g);
+  else walk<T, V, INTER, BWD, 1>(g);
 }
 
 // Sums the CTAs' weight gradients in a fixed order: 32 columns of one weight.
@@ -415,19 +534,19 @@ int done(cudaError_t e, const char* what) {
 }
 
 // Shares the CTAs out by heads, every warp at least one unit; returns their number.
-unsigned share(RotArgs* g, int per_sm) {
+unsigned share(RotArgs* g, int per_sm, int unit) {
   const int64_t groups = cdiv(g->tokens, 32 / g->lanes);
   const int64_t most = std::min<int64_t>(kMaxCtas, static_cast<int64_t>(device_sm_count()) * per_sm);
-  const int64_t twos[2] = {cdiv(g->heads[0], 2), cdiv(g->heads[1], 2)};
-  const int64_t q = std::max<int64_t>(1, most * twos[0] / (twos[0] + twos[1])), k = std::max<int64_t>(1, most - q);
-  g->ctas = static_cast<int>(std::min(q, cdiv(groups * twos[0], kWarps)));
-  return static_cast<unsigned>(g->ctas + std::min(k, cdiv(groups * twos[1], kWarps)));
+  const int64_t parts[2] = {cdiv(g->heads[0], unit), cdiv(g->heads[1], unit)};
+  const int64_t q = std::max<int64_t>(1, most * parts[0] / (parts[0] + parts[1])), k = std::max<int64_t>(1, most - q);
+  g->ctas = static_cast<int>(std::min(q, cdiv(groups * parts[0], kWarps)));
+  return static_cast<unsigned>(g->ctas + std::min(k, cdiv(groups * parts[1], kWarps)));
 }
 
 // Returns the number of CTAs.
 template <typename T, bool BWD>
 unsigned launch(RotArgs* g, int v, bool inter, cudaStream_t s) {
-  const unsigned ctas = share(g, per_sm<T, BWD>());
+  const unsigned ctas = share(g, per_sm<T, BWD>(), kUnitHeads<T>);
   if (inter) k_qkrot<T, 4, true, BWD><<<ctas, kThreads, 0, s>>>(*g);
   else if (v == 4) k_qkrot<T, 4, false, BWD><<<ctas, kThreads, 0, s>>>(*g);
   else if (v == 2) k_qkrot<T, 2, false, BWD><<<ctas, kThreads, 0, s>>>(*g);
@@ -440,7 +559,7 @@ int base(const normpre_qkrot* p, int64_t tokens, int64_t used, const normpre_hea
          const void* positions, int position_bytes, const void* qw, const void* kw, int w_dtype, RotArgs* g) {
   if (!p) return fail(NORMPRE_ERR_ARG, "null plan");
   const normpre_qkrot_config& c = p->cfg;
-  if (tokens < 0 || tokens >= (int64_t(1) << 31)) return fail(NORMPRE_ERR_SHAPE, "tokens must be in [0, 2^31)");
+  if (tokens < 0 || tokens > (int64_t(1) << 30)) return fail(NORMPRE_ERR_SHAPE, "tokens must be in [0, 2^30]");
   if (used < 0 || used > tokens) return fail(NORMPRE_ERR_SHAPE, "used must be in [0, tokens]");
   if (position_bytes != 4 && position_bytes != 8) return fail(NORMPRE_ERR_DTYPE, "positions must have 4 or 8 bytes");
   if (w_dtype != NORMPRE_F32 && w_dtype != NORMPRE_BF16)

@@ -47,7 +47,7 @@ def test_rotary_call_arguments(C):
     good = dict(plan=plan, tokens=5, used=5, q=q, k=k, positions=A, position_bytes=8, q_weight=A, k_weight=A, weight_dtype=0,
                 q_out=q, k_out=k)
     more = dict(dq_out=q, dk_out=k, dq=q, dk=k, dq_weight=A, dk_weight=A, workspace=A)
-    bad = [("SHAPE", dict(tokens=-1)), ("SHAPE", dict(tokens=1 << 31)), ("SHAPE", dict(used=6)), ("SHAPE", dict(used=-1)),
+    bad = [("SHAPE", dict(tokens=-1)), ("SHAPE", dict(tokens=(1 << 30) + 1)), ("SHAPE", dict(used=6)), ("SHAPE", dict(used=-1)),
            ("DTYPE", dict(position_bytes=2)), ("DTYPE", dict(weight_dtype=2)), ("ARG", dict(positions=0)),
            ("ALIGN", dict(positions=A + 4)), ("ALIGN", dict(q_weight=A + 2)), ("ARG", dict(q=C.normpre_heads(0, 256, 64))),
            ("ALIGN", dict(q=C.normpre_heads(A + 8, 256, 64))), ("ALIGN", dict(k=C.normpre_heads(A, 132, 64))),
