@@ -18,9 +18,9 @@
 // from and is the A operand of P V.  Q stays in shared memory for the item; K
 // and V tiles pass through one ring that a TMA warp fills.
 //
-// The running maximum is only raised when it would grow by more than 2^8
-// (O and l then are rescaled by the softmax warps themselves): P stays below
-// 2^8 relative to the row's maximum, which bf16 and the fp32 sums hold as
+// The running maximum is only raised when it would grow by more than 2^8 (with a
+// window 2^24; O and l then are rescaled by the softmax warps themselves): P stays
+// below that relative to the row's maximum, which bf16 and the fp32 sums hold as
 // precisely, and the rescale, which has to wait for P V, is rare.
 //
 // S - m' is formed before the scale: near the maximum it is exact however large
@@ -44,7 +44,11 @@ namespace normpre {
 namespace {
 
 constexpr int kThreads = 384;   // softmax 2 x 4 warps, TMA, MMA of tile 0, sequence ends, MMA of tile 1
-constexpr float kGrow = 8.f;    // log2 of the growth that raises the maximum
+// log2 of the growth that raises the maximum.  With a window an item has few
+// blocks, and the diagonal one shows its upper rows few keys, so that a larger
+// maximum in the next is common where scores are sharp: at a standard deviation of
+// 3 raising cost a fourth of the time at 2^8.
+constexpr float kGrow = 8.f, kGrowWindow = 24.f;
 
 template <int DP> struct Fwd {
   static constexpr int kChunks = DP / 64;
@@ -114,6 +118,7 @@ template <int DP, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_constant__ FwdArgs f) {
   using F = Fwd<DP>;
   constexpr int kSlots = F::kSlots, kTileBytes = F::kTileBytes, kChunks = F::kChunks, kAcc = F::kAcc;
+  constexpr float kRaise = WIN ? kGrowWindow : kGrow;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* sQ = smem;                          // [2]
   uint8_t* ring = smem + 2 * kTileBytes;       // [kSlots]
@@ -357,7 +362,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
         const bool edge = WIN && kTile * (blk - j + 1) > f.a.window && kTile * (j + 1) > f.a.sinks;
         auto mask = [&](int q) {
           if constexpr (WIN) {
-            if (j != blk && !edge) return;
             const uint32_t hide = hidden_bits(kTile * (blk - j) + row - 32 * q,
                                               kTile * (blk - j) + row - f.a.window + 1 - 32 * q, f.a.sinks - kTile * j - 32 * q);
 #pragma unroll
@@ -396,15 +400,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(&b->p_ready[s][part]);
         };
+        // Raises the maximum to `up`: l and O, once the products so far are in it.
+        auto raise = [&](float up) {
+          const float keep = tc::exp2_fast((m - up) * c);
+          m = up;
+          l *= keep;
+          if (!wait(&b->pv_done[s], (pv - 1) & 1u)) return false;
+#pragma unroll 1
+          for (int i = 0; i < DP; i += 32) {
+            uint32_t o[32];
+            tc::tmem_ld32(oc + i, o);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+            tc::tmem_put32(oc + i, o);
+          }
+          return true;
+        };
         // Three quarters of P go first: the products on them cover the rest.
-        if (j == blk) {
+        if (j == blk || (WIN && edge)) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             load(q);
             mask(q);
             compare();
           }
-          m = top();
+          const float up = fmaxf(m, top());
+          if (!WIN || j == blk) m = up;
+          else if (__any_sync(0xffffffffu, (up - m) * c > kRaise) && !raise(up)) break;
 #pragma unroll
           for (int q = 0; q < 3; ++q) {
             load(q);
@@ -420,37 +443,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
 #pragma unroll
           for (int q = 0; q < 3; ++q) {
             load(q);
-            if (WIN) mask(q);
             compare();
             exps(p + 16 * q);
           }
           load(3);
-          if (WIN) mask(3);
           compare();
           const float up = fmaxf(m, top());
-          if (__any_sync(0xffffffffu, (up - m) * c > kGrow)) {
-            const float keep = tc::exp2_fast((m - up) * c);
-            m = up;
-            l *= keep;
-            if (!wait(&b->pv_done[s], (pv - 1) & 1u)) break;
-#pragma unroll 1
-            for (int i = 0; i < DP; i += 32) {
-              uint32_t o[32];
-              tc::tmem_ld32(oc + i, o);
-              tc::tmem_ld_wait();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-              tc::tmem_put32(oc + i, o);
-            }
+          if (__any_sync(0xffffffffu, (up - m) * c > kRaise)) {
+            if (!raise(up)) break;
             sum[0] = sum[1] = 0;
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
               load(q);
-              if (WIN) mask(q);
               exps(p + 16 * q);
             }
             load(3);
-            if (WIN) mask(3);
           }
         }
         tc::tmem_put32(sc, p);
