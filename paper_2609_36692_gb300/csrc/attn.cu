@@ -23,10 +23,10 @@ struct normpre_attn {
   normpre_attn_config cfg;
   int device = 0;
   int64_t max_blocks = 0;
-  int n_blocks = 0, n_pairs = 0;
+  int n_blocks = 0, n_pairs = 0, n_keys = 0, n_split = 0;
   int64_t total = 0;
   // work lists of the current lengths, one block of memory: by_query, by_key,
-  // by_pair, then the walks
+  // by_pair, by_split, then the walks
   char* lists = nullptr;
   char* staging = nullptr;         // pinned, the same size
   cudaEvent_t copied = nullptr;    // the last copy out of `staging`
@@ -36,6 +36,9 @@ struct normpre_attn {
   bool used = false, elsewhere = false;   // calls since: any, on other streams
   int64_t walk_at[3] = {-1, -1, -1};   // byte offsets of the walks, -1: none
   float* delta = nullptr;          // [n_heads][max_tokens]
+  int chunk = 0, slots = 0;        // of split key blocks (see KeyPart): the least part, the most slots
+  int now_chunk = 0;               // part of the current lengths
+  float* partial = nullptr;
   int* flags = nullptr;            // pinned: set by kernels, read here between calls
 };
 
@@ -47,7 +50,33 @@ constexpr int64_t kMaxDealt = 8192;
 constexpr int64_t kWalkInts = kMaxDealt + 1024;   // most of one walk
 
 int64_t list_bytes(const normpre_attn* a) {
-  return 3 * (a->max_blocks * static_cast<int64_t>(sizeof(AttnBlock)) + kWalkInts * static_cast<int64_t>(sizeof(int)));
+  return (3 * a->max_blocks + 2 * a->slots) * static_cast<int64_t>(sizeof(AttnBlock)) +
+         3 * kWalkInts * static_cast<int64_t>(sizeof(int));
+}
+
+// Most memory of the partial sums.
+constexpr int64_t kMaxPartial = int64_t(64) << 20;
+
+int64_t slot_bytes(const normpre_attn* a) {
+  return static_cast<int64_t>(a->cfg.n_kv_heads) * 2 * 128 * a->cfg.head_dim * static_cast<int64_t>(sizeof(float));
+}
+
+// Parts of split key blocks: as long as a window's own walk, but long enough to
+// be worth an item, and few enough for their memory.
+void plan_parts(normpre_attn* a) {
+  if (!a->window || !a->sinks) return;
+  const int64_t most = std::min<int64_t>(kMaxSlots, kMaxPartial / slot_bytes(a));
+  const int64_t blocks = cdiv(a->cfg.max_tokens, 128), sinks = std::min<int64_t>(cdiv(a->sinks, 128), blocks);
+  // fp32 items are many and small: half an item's tiles are one query block
+  for (int64_t chunk = std::max<int64_t>(a->cfg.dtype == NORMPRE_BF16 ? 8 : 2, (126 + a->window) / 128 + 1); chunk < blocks;
+       chunk *= 2) {
+    // a sequence of n > chunk blocks has at most 2 n / chunk parts for each of its sink blocks
+    const int64_t slots = sinks * 2 * (blocks + blocks / chunk + 1) / chunk;
+    if (slots > most) continue;
+    a->chunk = static_cast<int>(chunk);
+    a->slots = static_cast<int>(slots);
+    return;
+  }
 }
 
 int fail(int code, const std::string& msg) {
@@ -63,6 +92,7 @@ void release(normpre_attn* a) {
   if (a->staging) cudaFreeHost(a->staging);
   if (a->copied) cudaEventDestroy(a->copied);
   cudaFree(a->delta);
+  cudaFree(a->partial);
   if (a->flags) cudaFreeHost(a->flags);
   delete a;
 }
@@ -79,12 +109,18 @@ AttnArgs base_args(const normpre_attn* a, int64_t tokens) {
   AttnArgs g = {};
   g.by_query = reinterpret_cast<const AttnBlock*>(a->lists);
   g.by_key = g.by_query + a->n_blocks;
-  g.by_pair = g.by_key + a->n_blocks;
+  g.by_pair = g.by_key + a->n_keys;
+  g.by_split = g.by_pair + a->n_pairs;
   const int** walks[3] = {&g.walk_fwd, &g.walk_dkdv, &g.walk_dq};
   for (int i = 0; i < 3; ++i)
     *walks[i] = a->walk_at[i] < 0 ? nullptr : reinterpret_cast<const int*>(a->lists + a->walk_at[i]);
   g.n_blocks = a->n_blocks;
   g.n_pairs = a->n_pairs;
+  g.n_keys = a->n_keys;
+  g.n_split = a->n_split;
+  g.chunk = a->now_chunk;
+  g.slots = a->slots;
+  g.partial = a->partial;
   g.total = static_cast<int>(a->total);
   g.tokens = static_cast<int>(tokens);
   g.heads = a->cfg.n_heads;
@@ -178,20 +214,46 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
   auto queries = [&](const AttnBlock& b) { return last_query(b.blk, b.len, window, sinks) - b.blk; };
   std::stable_sort(blocks.begin(), blocks.end(),
                    [&](const AttnBlock& x, const AttnBlock& y) { return keys(x, x.blk) > keys(y, y.blk); });
-  std::vector<AttnBlock> by_key = blocks, pairs;
+  // A block that is no more than about half of what a CTA gets in all is dealt
+  // out well as it is: 8 x 2432 tokens, window 1024, 450 us without parts, 475 with.
+  int chunk = 0, slots = 0;
+  if (windowed && a->chunk) {
+    int64_t all = 0;
+    for (const AttnBlock& b : blocks) all += queries(b) + 1;
+    const int64_t ctas = device_sm_count() * (a->cfg.dtype == NORMPRE_BF16 ? 1 : 2);
+    chunk = static_cast<int>(std::max<int64_t>(a->chunk, all * a->cfg.n_kv_heads / (2 * ctas)));
+  }
+  std::vector<AttnBlock> by_key, pairs, by_split;
+  for (AttnBlock b : blocks) {
+    const int count = queries(b) + 1, parts = chunk ? key_parts(count, chunk) : 1;
+    if (128 * b.blk >= sinks || parts < 2 || slots + parts > a->slots) {
+      by_key.push_back(b);
+      continue;
+    }
+    b.part = slots;
+    by_split.push_back(b);
+    for (int i = 0; i < parts; ++i) {
+      b.part = i << 12 | (slots++ + 1);
+      by_key.push_back(b);
+    }
+  }
+  auto walked = [&](const AttnBlock& b) {
+    const KeyPart p = key_part(b, window, sinks, chunk, a->slots);
+    return p.end - p.first;
+  };
   std::stable_sort(by_key.begin(), by_key.end(),
-                   [&](const AttnBlock& x, const AttnBlock& y) { return queries(x) > queries(y); });
+                   [&](const AttnBlock& x, const AttnBlock& y) { return walked(x) > walked(y); });
   std::copy_if(blocks.begin(), blocks.end(), std::back_inserter(pairs), [](const AttnBlock& b) { return b.blk % 2 == 0; });
   const int h = a->cfg.n_heads, hk = a->cfg.n_kv_heads, group = h / hk;
   const int64_t n = static_cast<int64_t>(blocks.size());
   std::vector<int> walk[3];
-  if (a->cfg.dtype == NORMPRE_BF16 && n && n * h <= kMaxDealt) {
+  if (a->cfg.dtype == NORMPRE_BF16 && n && n * h <= kMaxDealt && static_cast<int64_t>(by_key.size()) * hk <= kMaxDealt) {
     // costs in tiles, with about what an item's start and end take
     std::vector<int> fwd, dkdv, dq;
     const bool heads = attn_pair_heads(group);
     for (const AttnBlock& b : heads ? blocks : pairs)
       fwd.push_back(2 * keys(b, heads || (b.blk + 1) * 128 >= b.len ? b.blk : b.blk + 1) + 2);
-    for (const AttnBlock& b : by_key) dkdv.push_back(group * (queries(b) + 1) + 1);
+    for (const AttnBlock& b : by_key) dkdv.push_back(group * walked(b) + 1);
     for (const AttnBlock& b : blocks) dq.push_back(keys(b, b.blk) + 1);
     deal(fwd, heads ? h / 2 : h, &walk[0]);
     deal(dkdv, hk, &walk[1]);
@@ -212,6 +274,7 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
   put(blocks.data(), blocks.size() * sizeof(AttnBlock));
   put(by_key.data(), by_key.size() * sizeof(AttnBlock));
   put(pairs.data(), pairs.size() * sizeof(AttnBlock));
+  put(by_split.data(), by_split.size() * sizeof(AttnBlock));
   for (int i = 0; i < 3; ++i) {
     walk_at[i] = walk[i].empty() ? -1 : at;
     put(walk[i].data(), walk[i].size() * sizeof(int));
@@ -221,8 +284,11 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
   if (e) return cuda_fail(e, "cudaMemcpyAsync");
   a->n_blocks = static_cast<int>(n);
   a->n_pairs = static_cast<int>(pairs.size());
+  a->n_keys = static_cast<int>(by_key.size());
+  a->n_split = static_cast<int>(by_split.size());
   std::copy(walk_at, walk_at + 3, a->walk_at);
   a->total = total;
+  a->now_chunk = chunk;
   a->now_window = window;
   a->now_sinks = sinks;
   return NORMPRE_OK;
@@ -258,11 +324,13 @@ int normpre_attn_init_window(const normpre_attn_config* cfg, int64_t window, int
     a->sinks = a->window ? static_cast<int>(std::min(sinks, cfg->max_tokens)) : 0;
     if (a->cfg.scale == 0.f) a->cfg.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(cfg->head_dim)));
     a->max_blocks = cfg->max_tokens / 128 + std::min<int64_t>(cfg->max_seqs, cfg->max_tokens);
+    plan_parts(a.get());
     cudaError_t e = cudaGetDevice(&a->device);
     if (!e) e = cudaMalloc(&a->lists, list_bytes(a.get()));
     if (!e) e = cudaHostAlloc(&a->staging, list_bytes(a.get()), cudaHostAllocDefault);
     if (!e) e = cudaEventCreateWithFlags(&a->copied, cudaEventDisableTiming);
     if (!e) e = cudaMalloc(&a->delta, static_cast<size_t>(cfg->n_heads) * cfg->max_tokens * sizeof(float));
+    if (!e && a->slots) e = cudaMalloc(&a->partial, static_cast<size_t>(a->slots) * slot_bytes(a.get()));
     if (!e) e = cudaHostAlloc(&a->flags, sizeof(int), cudaHostAllocDefault);
     if (e) return cuda_fail(e, "normpre_attn_init");
     *a->flags = 0;
@@ -327,6 +395,7 @@ int normpre_attn_backward(normpre_attn* a, int64_t tokens, const normpre_heads* 
   if (!e) e = launch_attn_delta(g, a->cfg.dtype, s);
   std::string err;
   if (!e) e = a->cfg.dtype == NORMPRE_BF16 ? launch_attn_backward_tc(g, s, &err) : launch_attn_backward_simt(g, s);
+  if (!e) e = launch_attn_join(g, a->cfg.dtype, s);
   return e ? cuda_fail(e, err.empty() ? "attention backward" : err.c_str()) : NORMPRE_OK;
 }
 

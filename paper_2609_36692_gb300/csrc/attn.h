@@ -17,7 +17,7 @@ struct AttnBlock {
   int start;   // the sequence's first row
   int len;     // the sequence's rows
   int blk;     // index of the block in the sequence
-  int pad;
+  int part;    // of a key block whose queries are split: its place (see KeyPart); by_split: the first place
 };
 
 // Whether an entry of the lists fits into `total` rows.  The lists are rebuilt for
@@ -55,6 +55,36 @@ __host__ __device__ inline int last_query(int blk, int len, int window, int sink
   return 128 * blk < sinks || last < in ? last : in;
 }
 
+// The sinks' key blocks meet all later query blocks, however short the window.
+// They are split into parts of about `chunk` query blocks, each an item of its
+// own, whose sums over queries (dk, dv in fp32) lie in a slot of the workspace
+// until they are added up in the parts' order.  part = index of the part * 2^12 +
+// slot + 1; 0: not split.
+constexpr int kMaxSlots = 4000;
+__host__ __device__ inline int key_parts(int count, int chunk) { return (count + chunk - 1) / chunk; }
+struct KeyPart {
+  int first, end;    // query blocks
+  int slot;          // -1: not split
+  bool fits;         // whether the entry is one of this call's (see block_fits)
+};
+__host__ __device__ inline KeyPart key_part(const AttnBlock& b, int window, int sinks, int chunk, int slots) {
+  KeyPart p;
+  const int count = last_query(b.blk, b.len, window, sinks) - b.blk + 1;
+  p.first = b.blk;
+  p.end = b.blk + count;
+  p.slot = (b.part & 4095) - 1;
+  p.fits = true;
+  if (b.part) {
+    const int n = chunk > 0 ? key_parts(count, chunk) : 0, i = b.part >> 12;
+    p.fits = i >= 0 && i < n && n < 4096 && p.slot >= 0 && p.slot < slots;
+    if (p.fits) {
+      p.first = b.blk + static_cast<int>(static_cast<int64_t>(count) * i / n);
+      p.end = b.blk + static_cast<int>(static_cast<int64_t>(count) * (i + 1) / n);
+    }
+  }
+  return p;
+}
+
 typedef HeadsView AttnTensor;
 
 struct AttnArgs {
@@ -64,7 +94,11 @@ struct AttnArgs {
   const AttnBlock* by_query; // blocks, the ones that see the most keys first
   const AttnBlock* by_key;   // blocks, the ones seen by the most queries first
   const AttnBlock* by_pair;  // the blocks of even index, in by_query's order
+  const AttnBlock* by_split; // key blocks whose queries are split
   int n_blocks, n_pairs;
+  int n_keys, n_split;       // entries of by_key (a split block has several), of by_split
+  int chunk, slots;          // see KeyPart
+  float* partial;            // [slots][kv_heads][dk, dv][128][dim]
   // items of each CTA of the tensor-core kernels (null: see walk_item)
   const int *walk_fwd, *walk_dkdv, *walk_dq;
   int total;                 // rows that belong to sequences
@@ -92,6 +126,8 @@ cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s);
 // Tensor-core kernels, bf16 (attn_fwd.cu, attn_bwd.cu).
 cudaError_t launch_attn_forward_tc(const AttnArgs& a, cudaStream_t s, std::string* err);
 cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t s, std::string* err);
+// Adds up the parts of split key blocks, if there are any.
+cudaError_t launch_attn_join(const AttnArgs& a, int dtype, cudaStream_t s);
 // delta_i = <do_i, o_i>; zero for rows outside the sequences.
 cudaError_t launch_attn_delta(const AttnArgs& a, int dtype, cudaStream_t s);
 

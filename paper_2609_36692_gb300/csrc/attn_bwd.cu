@@ -237,12 +237,54 @@ __device__ __forceinline__ void store_acc(const AttnTensor& t, uint32_t acc, int
                     dim, lane);
 }
 
+// An accumulator's 32 rows x (DP / 4) columns of a warp to a part's fp32 sums.
+template <int DP>
+__device__ __forceinline__ void store_part(float* to, uint32_t acc, int warp, int dim, int lane) {
+  constexpr int kCols = DP / 4;
+  const int c = kCols * (warp >> 2);
+  uint32_t o[kCols];
+  if constexpr (kCols == 32) tc::tmem_ld32(acc + c, o);
+  else tc::tmem_ld16(acc + c, o);
+  tc::tmem_ld_wait();
+  float* p = to + static_cast<int64_t>(32 * (warp & 3) + lane) * dim + c;
+#pragma unroll
+  for (int i = 0; i < kCols; i += 4)
+    if (c + i < dim) *reinterpret_cast<uint4*>(p + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+}
+
 struct Item {
   int64_t start;
   int len, blk, head;
 };
 
 constexpr int kCached = 32;
+
+// An item of dK, dV: a key block and head, and the query blocks first .. end.
+struct alignas(16) KeyItem {
+  int start, len, blk, head, first, end, slot, pad;   // blk -1: no item
+};
+constexpr int kKeyCached = 16;                        // 512 bytes
+static_assert(kKeyCached * sizeof(KeyItem) <= 512, "items");
+// Not inlined: in every role of the kernel, for the few items past the cached
+// ones, it would push the roles' loops apart in the instruction cache (4 % of a
+// pass over short items).  The same for the items of dQ.
+template <bool WIN>
+__device__ __noinline__ KeyItem key_item(const AttnArgs& a, int64_t r) {
+  KeyItem k = {0, 0, -1, 0, 0, 0, -1, 0};
+  const int64_t i = walk_item(a.walk_dkdv, r, static_cast<int64_t>(a.n_keys) * a.kv_heads, a.flags);
+  if (i < 0) return k;
+  const AttnBlock b = a.by_key[i / a.kv_heads];
+  KeyPart p = {b.blk, (b.len - 1) / kTile + 1, -1, b.part == 0};
+  if (WIN && block_fits(b, a.total)) p = key_part(b, a.window, a.sinks, a.chunk, a.slots);
+  if (!block_fits(b, a.total) || !p.fits) {
+    raise_host_flag(a.flags, kFlagLists);
+    return k;
+  }
+  return KeyItem{b.start, b.len, b.blk, static_cast<int>(i % a.kv_heads), p.first, p.end, p.slot, 0};
+}
+__device__ __noinline__ ItemRef query_item(const AttnArgs& a, int64_t r) {
+  return list_item(a, a.by_query, a.n_blocks, a.walk_dq, a.heads, r);
+}
 
 __device__ __forceinline__ bool get_item(const ItemRef& b, Item& it) {
   if (b.blk < 0) return false;
@@ -264,20 +306,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   float* stat = reinterpret_cast<float*>(ring + kSlots * kTileBytes);   // [2][-lse, delta][128]
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(stat + 512);
   static_assert(sizeof(Bars<kSlots>) <= 512, "barriers");
-  ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
+  KeyItem* items = reinterpret_cast<KeyItem*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kKeyCached]
   const AttnArgs& a = f.a;
-  // query blocks of an item and head
-  auto queries = [&](const Item& it) {
-    return (WIN ? last_query(it.blk, it.len, a.window, a.sinks) : (it.len - 1) / kTile) - it.blk + 1;
+  auto get = [&](int64_t r, KeyItem& it) {
+    it = r < kKeyCached ? items[r] : key_item<WIN>(a, r);
+    return it.blk >= 0;
   };
-  auto find = [&](int64_t r) { return list_item(a, a.by_key, a.n_blocks, a.walk_dkdv, a.kv_heads, r); };
-  auto item = [&](int64_t r) { return r < kCached ? items[r] : find(r); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     init_bars(b, 2);
     for (const CUtensorMap* m : {&f.q, &f.k, &f.v, &f.dout}) tc::prefetch_map(m);
   }
-  if (warp == 2) items[lane] = find(lane);
+  if (warp == 2 && lane < kKeyCached) items[lane] = key_item<WIN>(a, lane);
   if (warp == kMmaA) {
     tc::tmem_alloc(&b->tmem, 512);
     tc::tmem_relinquish();
@@ -288,17 +328,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   const uint32_t cS = b->tmem, cP = cS + 128, cAcc = cS + 256;     // per set: dV, dK
   Warp<kSlots> w = {b, lane, true, 0, 0};
   Turn<kSets> set;
-  Item it;
+  KeyItem it;
 
   if (warp == kTma) {
     // ---------------- TMA (one thread), then the rows past the sequences ----------------
     if (tc::elect_one()) {
-      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
+      for (int64_t r = 0; w.ok && get(r, it); ++r, set.next()) {
         const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
         if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.k, &f.v, row, it.head, kChunks)) break;
-        const int end = it.blk + queries(it);
         for (int g = 0; g < a.group && w.ok; ++g)
-          for (int i = it.blk; i < end && w.ok; ++i) {
+          for (int i = it.first; i < it.end && w.ok; ++i) {
             const int64_t qrow = it.start + static_cast<int64_t>(kTile) * i;
             const bool tail = kTile * (i + 1) > it.len;
             w.load(ring, kTileBytes, &f.q, qrow, it.head * a.group + g, kChunks, tail);
@@ -315,8 +354,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
       uint32_t p_phase = 0;
       int st = 0;                                                 // parity of the block in the walk
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
-        const int n = queries(it) * a.group;
+      for (int64_t r = 0; w.ok && get(r, it); ++r, set.next()) {
+        const int n = (it.end - it.first) * a.group;
         const uint32_t k = tc::su32(own + 2 * set.i * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][0], set.parity)) break;
         int q = w.take();
@@ -353,8 +392,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     if (tc::elect_one()) {
       uint32_t ds_phase = 0;
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
-      for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
-        const int n = queries(it) * a.group;
+      for (int64_t r = 0; w.ok && get(r, it); ++r, set.next()) {
+        const int n = (it.end - it.first) * a.group;
         const uint32_t v = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
         int q = w.take(), o = w.take();
@@ -389,11 +428,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     Turn<2> st;
     uint32_t seen = 0;
     int slot = 0;
-    for (int64_t r = 0; w.ok && get_item(item(r), it); ++r) {
-      const int end = min(it.len, kTile * (it.blk + queries(it)));
+    for (int64_t r = 0; w.ok && get(r, it); ++r) {
+      const int end = min(it.len, kTile * it.end);
       for (int g = 0; g < a.group && w.ok; ++g) {
         const int64_t base = static_cast<int64_t>(it.head * a.group + g) * a.tokens + it.start;
-        for (int i = it.blk * kTile; i < end; i += kTile) {
+        for (int i = it.first * kTile; i < end; i += kTile) {
           float ls[4], de[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -426,20 +465,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
     const uint64_t c2 = tc::pack2(a.scale, a.scale), log2e2 = tc::pack2(kLog2e, kLog2e);
     uint32_t phase = 0;
     Turn<2> st;
-    for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
-      const int nq = queries(it), n = nq * a.group;
+    for (int64_t r = 0; w.ok && get(r, it); ++r, set.next()) {
+      // what the loop needs of the item; the rest is fetched again after it
+      const int nq = it.end - it.first, n = nq * a.group, gap = it.first - it.blk;
+      const int sinks = WIN ? a.sinks - kTile * it.blk : 0;    // among these keys
       for (int i = 0; i < n; ++i) {
         const float* ls = stat + st.i * 256 + 32 * part;
         if (!w.wait(&b->s_full[st.i], st.parity)) break;
-        const int up = i % nq;                   // blocks between the keys and the queries
+        const int up = gap + i % nq;   // blocks between the keys and the queries
         const bool diag = up == 0;
         // the window's end crosses the tile, and not only over sinks
-        const bool edge = WIN && kTile * (up + 1) > a.window && kTile * (it.blk + 1) > a.sinks;
+        const bool edge = WIN && kTile * (up + 1) > a.window && sinks < kTile;
         // the tile's queries that do not see key `row`, a bit for each column
         uint32_t hide = 0;
         if (WIN && (diag || edge)) {
           hide = below_bits(row - kTile * up - 32 * part);
-          if (kTile * it.blk + row >= a.sinks) hide |= ~below_bits(row + a.window - kTile * up - 32 * part);
+          if (row >= sinks) hide |= ~below_bits(row + a.window - kTile * up - 32 * part);
         }
         float p[32];
         uint32_t pk[16];
@@ -505,12 +546,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         if (lane == 0) tc::mbar_arrive(&b->stat_empty[st.i]);
         st.next();
       }
-      if (!w.wait(&b->acc_full[set.i], set.parity)) break;
+      if (!w.wait(&b->acc_full[set.i], set.parity) || !get(r, it)) break;
       const int64_t at = it.start + static_cast<int64_t>(kTile) * it.blk;
       const int rows = it.len - kTile * it.blk;
       const uint32_t acc = cAcc + 2 * DP * set.i + lanes;
-      store_acc<DP>(a.dv, acc, at, rows, it.head, warp, 1.f, a.dim, lane);
-      store_acc<DP>(a.dk, acc + DP, at, rows, it.head, warp, a.scale, a.dim, lane);
+      if (WIN && it.slot >= 0) {
+        float* to = a.partial + (static_cast<int64_t>(it.slot) * a.kv_heads + it.head) * 2 * kTile * a.dim;
+        store_part<DP>(to, acc + DP, warp, a.dim, lane);
+        store_part<DP>(to + kTile * a.dim, acc, warp, a.dim, lane);
+      } else {
+        store_acc<DP>(a.dv, acc, at, rows, it.head, warp, 1.f, a.dim, lane);
+        store_acc<DP>(a.dk, acc + DP, at, rows, it.head, warp, a.scale, a.dim, lane);
+      }
       w.arrive(&b->acc_empty[set.i]);
     }
   }
@@ -528,14 +575,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
   ItemRef* items = reinterpret_cast<ItemRef*>(reinterpret_cast<uint8_t*>(b) + 512);   // [kCached]
   const AttnArgs& a = f.a;
   auto keys = [&](const Item& it) { return WIN ? key_span(it.blk, a.window, a.sinks) : KeySpan{0, 0}; };
-  auto find = [&](int64_t r) { return list_item(a, a.by_query, a.n_blocks, a.walk_dq, a.heads, r); };
-  auto item = [&](int64_t r) { return r < kCached ? items[r] : find(r); };
+  auto item = [&](int64_t r) { return r < kCached ? items[r] : query_item(a, r); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     init_bars(b, 1);
     for (const CUtensorMap* m : {&f.q, &f.k, &f.v, &f.dout}) tc::prefetch_map(m);
   }
-  if (warp == 2) items[lane] = find(lane);
+  if (warp == 2) items[lane] = query_item(a, lane);
   if (warp == kMmaA) {
     tc::tmem_alloc(&b->tmem, 512);
     tc::tmem_relinquish();
@@ -704,17 +750,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
 }
 
 template <auto kernel>
-cudaError_t launch(const BwdArgs& f, int heads, size_t smem, cudaStream_t s) {
+cudaError_t launch(const BwdArgs& f, int64_t items, size_t smem, cudaStream_t s) {
   const cudaError_t e = allow_smem<kernel>(smem);
   if (e) return e;
-  kernel<<<walk_grid(static_cast<int64_t>(f.a.n_blocks) * heads), kThreads, smem, s>>>(f);
+  kernel<<<walk_grid(items), kThreads, smem, s>>>(f);
   return cudaGetLastError();
 }
 
 template <int DP, bool WIN>
 cudaError_t both(const BwdArgs& f, cudaStream_t s) {
-  const cudaError_t e = launch<k_attn_dkdv_tc<DP, WIN>>(f, f.a.kv_heads, Bwd<DP>::kSmem, s);
-  return e ? e : launch<k_attn_dq_tc<DP, WIN>>(f, f.a.heads, Bwd<DP>::kSmem, s);
+  const cudaError_t e = launch<k_attn_dkdv_tc<DP, WIN>>(f, static_cast<int64_t>(f.a.n_keys) * f.a.kv_heads, Bwd<DP>::kSmem, s);
+  return e ? e : launch<k_attn_dq_tc<DP, WIN>>(f, static_cast<int64_t>(f.a.n_blocks) * f.a.heads, Bwd<DP>::kSmem, s);
 }
 
 }  // namespace

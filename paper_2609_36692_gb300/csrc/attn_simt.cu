@@ -171,10 +171,11 @@ struct Rows {
   int64_t seq;     // the sequence's first row
   int first;       // this CTA's first row in the sequence
   int len;         // the sequence's rows; 0: rows that belong to no sequence
+  AttnBlock block;
 };
-__device__ __forceinline__ bool rows_of(const AttnArgs& a, const AttnBlock* list, int64_t i, Rows& w) {
-  if (i < 2 * static_cast<int64_t>(a.n_blocks)) {
-    const AttnBlock b = list[i >> 1];
+__device__ __forceinline__ bool rows_of(const AttnArgs& a, const AttnBlock* list, int blocks, int64_t i, Rows& w) {
+  if (i < 2 * static_cast<int64_t>(blocks)) {
+    const AttnBlock b = w.block = list[i >> 1];
     if (!block_fits(b, a.total)) {
       if (threadIdx.x == 0) raise_host_flag(a.flags, kFlagLists);
       return false;
@@ -184,7 +185,7 @@ __device__ __forceinline__ bool rows_of(const AttnArgs& a, const AttnBlock* list
     w.len = b.len;
     return w.first < w.len;
   }
-  w.seq = a.total + 64 * (i - 2 * static_cast<int64_t>(a.n_blocks));
+  w.seq = a.total + 64 * (i - 2 * static_cast<int64_t>(blocks));
   w.first = w.len = 0;
   return w.seq < a.tokens;
 }
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
   float* P = KV + kB * ld<DP>();
   const int head = static_cast<int>(blockIdx.x % a.heads), kvh = head / a.group;
   Rows w;
-  if (!rows_of(a, a.by_query, blockIdx.x / a.heads, w)) return;
+  if (!rows_of(a, a.by_query, a.n_blocks, blockIdx.x / a.heads, w)) return;
   const int64_t row0 = w.seq + w.first;
   float* lse = a.lse + static_cast<int64_t>(head) * a.tokens + row0;
   if (!w.len) {
@@ -316,12 +317,17 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
   float* Pt = dO + kB * ld<DP>();   // P^T, then dS^T: [key][query]
   float* St = Pt + kB * kPs;
   Rows w;
-  if (!rows_of(a, a.by_key, item, w)) return;
+  if (!rows_of(a, a.by_key, a.n_keys, item, w)) return;
   const int64_t row0 = w.seq + w.first;
   if (!w.len) {
     const int rows = static_cast<int>(min(static_cast<int64_t>(kB), a.tokens - row0));
     zero_rows<T>(a.dk, row0, rows, kvh, a.dim);
     zero_rows<T>(a.dv, row0, rows, kvh, a.dim);
+    return;
+  }
+  const KeyPart part = key_part(w.block, a.window, a.sinks, a.chunk, a.slots);
+  if (!part.fits) {
+    if (threadIdx.x == 0) raise_host_flag(a.flags, kFlagLists);
     return;
   }
   const int rows = min(kB, w.len - w.first);
@@ -333,10 +339,11 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
 #pragma unroll
     for (int k = 0; k < DP / 64; ++k) dk[r][k] = dv[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
   // rows past the last one that sees any of these keys
-  const int end = w.first < a.sinks ? w.len : min(w.len, w.first + kB - 1 + a.window);
+  const int last = w.first < a.sinks ? w.len : min(w.len, w.first + kB - 1 + a.window);
+  const int begin = max(w.first, 128 * part.first), end = min(last, 128 * part.end);
   for (int g = 0; g < a.group; ++g) {
     const int head = kvh * a.group + g;
-    for (int i0 = w.first; i0 < end; i0 += kB) {
+    for (int i0 = begin; i0 < end; i0 += kB) {
       const int qrows = min(kB, w.len - i0);
       __syncthreads();
       load_tiles<T, DP>(Q, a.q, dO, a.dout, w.seq + i0, qrows, head, a.dim);
@@ -357,6 +364,14 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
     }
   }
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, c[4] = {a.scale, a.scale, a.scale, a.scale};
+  if (part.slot >= 0) {
+    // 128 rows of the slot, these the first or second 64
+    float* p = a.partial + ((static_cast<int64_t>(part.slot) * a.kv_heads + kvh) * 2 * 128 + (w.first & 127)) * a.dim;
+    const AttnTensor pk = {p, a.dim, 0}, pv = {p + 128 * a.dim, a.dim, 0};
+    store_tile<float, DP>(pk, 0, rows, 0, a.dim, ty, tx, dk, one);
+    store_tile<float, DP>(pv, 0, rows, 0, a.dim, ty, tx, dv, one);
+    return;
+  }
   store_tile<T, DP>(a.dk, row0, rows, kvh, a.dim, ty, tx, dk, c);
   store_tile<T, DP>(a.dv, row0, rows, kvh, a.dim, ty, tx, dv, one);
 }
@@ -370,7 +385,7 @@ __device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, i
   float* S = V + kB * ld<DP>();
   const int kvh = head / a.group;
   Rows w;
-  if (!rows_of(a, a.by_query, item, w)) return;
+  if (!rows_of(a, a.by_query, a.n_blocks, item, w)) return;
   const int64_t row0 = w.seq + w.first;
   if (!w.len) {
     zero_rows<T>(a.dq, row0, static_cast<int>(min(static_cast<int64_t>(kB), a.tokens - row0)), head, a.dim);
@@ -442,7 +457,7 @@ template <auto kernel>
 cudaError_t run(const AttnArgs& a, int each, size_t smem, cudaStream_t s) {
   const cudaError_t e = allow_smem<kernel>(smem);
   if (e) return e;
-  const int64_t ctas = (2 * static_cast<int64_t>(a.n_blocks) + cdiv(a.tokens - a.total, kB)) * each;
+  const int64_t ctas = (2 * static_cast<int64_t>(each == a.heads ? a.n_blocks : max(a.n_blocks, a.n_keys)) + cdiv(a.tokens - a.total, kB)) * each;
   if (!ctas) return cudaSuccess;
   if (ctas >= (int64_t(1) << 31)) return cudaErrorInvalidConfiguration;
   kernel<<<static_cast<unsigned>(ctas), kThreads, smem, s>>>(a);
@@ -463,6 +478,44 @@ cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s) {
   const int each = a.kv_heads + a.heads;
   return a.dim <= 64 ? run<k_attn_bwd<float, 64>>(a, each, bwd_smem<64>(), s)
                      : run<k_attn_bwd<float, 128>>(a, each, bwd_smem<128>(), s);
+}
+
+// One CTA for 16 rows of a split key block and head: 16 lanes a row, eight
+// columns each.
+template <typename T>
+static __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ AttnArgs a) {
+  const int head = blockIdx.y, row = 16 * (blockIdx.x & 7) + threadIdx.x / 16, c = 8 * (threadIdx.x & 15);
+  const AttnBlock b = a.by_split[blockIdx.x >> 3];
+  int n = 0;
+  if (block_fits(b, a.total) && 128 * b.blk + 128 <= b.len)
+    n = key_parts(last_query(b.blk, b.len, a.window, a.sinks) - b.blk + 1, a.chunk);
+  if (n < 2 || b.part < 0 || n > a.slots - b.part) {
+    if (threadIdx.x == 0) raise_host_flag(a.flags, kFlagLists);
+    return;
+  }
+  if (c >= a.dim) return;
+  for (int which = 0; which < 2; ++which) {
+    float sum[8] = {};
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      float v[8];
+      load8(a.partial + (((static_cast<int64_t>(b.part + i) * a.kv_heads + head) * 2 + which) * 128 + row) * a.dim + c, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += v[e];
+    }
+    const AttnTensor& t = which ? a.dv : a.dk;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] *= which ? 1.f : a.scale;
+    store8(static_cast<T*>(t.p) + (static_cast<int64_t>(b.start) + 128 * b.blk + row) * t.ts + head * t.hs + c, sum);
+  }
+}
+
+cudaError_t launch_attn_join(const AttnArgs& a, int dtype, cudaStream_t s) {
+  if (!a.n_split) return cudaSuccess;
+  const dim3 grid(static_cast<unsigned>(8 * a.n_split), static_cast<unsigned>(a.kv_heads));
+  if (dtype == 0) k_attn_join<float><<<grid, 256, 0, s>>>(a);
+  else k_attn_join<bf16><<<grid, 256, 0, s>>>(a);
+  return cudaGetLastError();
 }
 
 template <typename T>

@@ -101,9 +101,13 @@ def test_lengths(lengths, window, sinks, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("window, sinks", [(3, 2), (1000, 5), (1, 300), (2500, 0)])
 def test_long(window, sinks, dtype):
-    """Many more blocks than the window has, more items than CTAs."""
-    check((2, 1, 64), [5000, 37], window, sinks, dtype)
-    check((1, 1, 128), [4100], window, sinks, dtype)
+    """Many more blocks than the window has, so that the sinks' gradients come
+    from parts of the queries; the same bits again."""
+    import torch
+    for layout, lengths in (((2, 1, 64), [5000, 37]), ((1, 1, 128), [4100]), ((4, 2, 24), [2000, 1999, 1100])):
+        plan, (q, k, v, do), (out, lse, *grads) = check(layout, lengths, window, sinks, dtype)
+        for a, b in zip(plan.backward(q, k, v, out, lse, do), grads):
+            assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
