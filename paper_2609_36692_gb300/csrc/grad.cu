@@ -16,7 +16,7 @@
 // share backwards, from what it read last.
 //
 // Range and precision: a thread sums 16 KB / 256 threads = 64 bytes of values
-// in fp32, where squares cannot overflow or vanish, else in fp64; everything
+// in fp32, four sums of 16 bytes side by side, where squares cannot overflow or vanish, else in fp64; everything
 // beyond is fp64.
 #include <algorithm>
 #include <cmath>
@@ -129,11 +129,14 @@ template <typename T> struct Share {
     for (int i = 0; i < 4; ++i) q[i].load(static_cast<const T*>(e.in), index(e, chunk, i), e.size);
   }
   __device__ __forceinline__ double squares() const {
-    float s = 0.f;
+    float p[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      p[i] = q[i].at(0) * q[i].at(0);
 #pragma unroll
-      for (int e = 0; e < Piece<T>::kN; ++e) s = fmaf(q[i].at(e), q[i].at(e), s);
+      for (int e = 1; e < Piece<T>::kN; ++e) p[i] = fmaf(q[i].at(e), q[i].at(e), p[i]);
+    }
+    const float s = (p[0] + p[1]) + (p[2] + p[3]);
     if (s > 0x1p-100f && s < 0x1p120f) return s;
     // squares near the ends of fp32's range
     uint32_t any = 0;
@@ -189,6 +192,12 @@ __device__ __forceinline__ double fold(const double* part, int parts, double* re
   return block_sum(sum, red);
 }
 
+// The root of a sum in fp32: where its range allows, of the sum rounded to fp32,
+// off by 1.5 units of 2^-24 (the fp64 root takes a microsecond).
+__device__ __forceinline__ float root(double sum) {
+  return sum > 0x1p-120 && sum < 0x1p120 ? sqrtf(static_cast<float>(sum)) : static_cast<float>(sqrt(sum));
+}
+
 template <typename T, typename U>
 __device__ __forceinline__ void scale_chunk(const Entry& e, uint32_t chunk, float c) {
   Share<T> x;
@@ -203,10 +212,16 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_grad_scale(const __grid_co
   __shared__ float factor;
   const double sum = fold(part, parts, red);
   if (threadIdx.x == 0) {
-    const double n = sqrt(sum), to = n + static_cast<double>(eps);
+    float n = root(sum);
     // all zeros are left as they are; a norm that is NaN gives NaN
-    factor = to <= static_cast<double>(max_norm) ? 1.f : static_cast<float>(static_cast<double>(max_norm) / to);
-    if (norm && blockIdx.x == 0) *norm = static_cast<float>(n);
+    if (n > 0x1p-60f && n < 0x1p100f) {
+      const float to = n + eps;
+      factor = to <= max_norm ? 1.f : max_norm / to;
+    } else {
+      const double to = sqrt(sum) + static_cast<double>(eps);
+      factor = to <= static_cast<double>(max_norm) ? 1.f : static_cast<float>(static_cast<double>(max_norm) / to);
+    }
+    if (norm && blockIdx.x == 0) *norm = n;
   }
   __syncthreads();
   const float f = factor;
@@ -231,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_grad_scale(const __grid_co
 __global__ void __launch_bounds__(kThreads) k_grad_norm(const double* part, int parts, float* norm) {
   __shared__ double red[kThreads / 32];
   const double sum = fold(part, parts, red);
-  if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(sum));
+  if (threadIdx.x == 0) *norm = root(sum);
 }
 
 int fail(int code, const std::string& msg) {
@@ -248,18 +263,18 @@ int check_list(int n, const void* const* grads, const int* dtypes, const int64_t
   if (n < 0 || n > (1 << 20)) return fail(NORMPRE_ERR_ARG, "the number of gradients must be in [0, 2^20]");
   if (n && (!grads || !dtypes || !sizes)) return fail(NORMPRE_ERR_ARG, "null argument");
   int64_t total = 0;
+  auto refuse = [](int code, int i, const char* what) { return fail(code, "gradient " + std::to_string(i) + what); };
   for (int i = 0; i < n; ++i) {
-    const std::string name = "gradient " + std::to_string(i);
     if (dtypes[i] != NORMPRE_F32 && dtypes[i] != NORMPRE_BF16)
-      return fail(NORMPRE_ERR_DTYPE, name + ": dtype must be NORMPRE_F32 or NORMPRE_BF16");
+      return refuse(NORMPRE_ERR_DTYPE, i, ": dtype must be NORMPRE_F32 or NORMPRE_BF16");
     // a table's chunks are counted in 32 bits
     if (sizes[i] < 0 || sizes[i] > (int64_t(1) << 40) - total)
-      return fail(NORMPRE_ERR_SHAPE, name + ": size must be >= 0, and all together at most 2^40");
+      return refuse(NORMPRE_ERR_SHAPE, i, ": size must be >= 0, and all together at most 2^40");
     total += sizes[i];
     if (!sizes[i]) continue;
-    if (!grads[i]) return fail(NORMPRE_ERR_ARG, name + ": null");
+    if (!grads[i]) return refuse(NORMPRE_ERR_ARG, i, ": null");
     if (reinterpret_cast<uintptr_t>(grads[i]) % (dtypes[i] == NORMPRE_BF16 ? 2 : 4))
-      return fail(NORMPRE_ERR_ALIGN, name + " must be aligned to its elements");
+      return refuse(NORMPRE_ERR_ALIGN, i, " must be aligned to its elements");
   }
   return NORMPRE_OK;
 }

@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from array import array
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -21,6 +22,7 @@ from torch.autograd.function import once_differentiable
 from . import normpre as C
 
 _CODES = {torch.float32: C.NORMPRE_F32, torch.bfloat16: C.NORMPRE_BF16}
+_POSITIONS = {torch.int64: 8, torch.int32: 4}
 # The handle of a device's current stream, without the Stream object around it
 # (a tenth of a microsecond instead of two).
 _current_stream = torch._C._cuda_getCurrentRawStream
@@ -34,14 +36,19 @@ def _dtype_code(x: torch.Tensor) -> int:
     return code
 
 
-def _on(device: torch.device, f, *args, stream=None) -> None:
-    """f(*args, stream) with `device` current, on its current stream or the one given."""
-    index = device.index
+def _on(device: torch.device, f, *args) -> None:
+    """f(*args, stream) with `device` current, on its current stream."""
+    _on_index(device.index, f, *args)
+
+
+def _on_index(index: int, f, *args, stream=None) -> None:
+    """The same, or on the stream given."""
+    s = _current_stream(index) if stream is None else stream.cuda_stream
     if _current_device() == index:
-        f(*args, _current_stream(index) if stream is None else stream.cuda_stream)
+        f(*args, s)
     else:
         with torch.cuda.device(index):
-            f(*args, _current_stream(index) if stream is None else stream.cuda_stream)
+            f(*args, s)
 
 
 def _used_on(stream, *tensors) -> None:
@@ -257,55 +264,63 @@ class QKNormRotary:
         self.plan = C.normpre_qkrot_init(cfg, frequencies)
         self._bytes = C.normpre_qkrot_bytes(self.plan)
 
-    def _check(self, x: torch.Tensor, name: str, tokens: int, heads: int, device: torch.device):
-        if x.device != device or not x.is_cuda:
-            raise ValueError("%s must be on %s" % (name, "a CUDA device" if device.type != "cuda" else device))
-        if x.dtype != self.dtype:
-            raise TypeError("%s must be %s" % (name, self.dtype))
-        if x.shape != (tokens, heads, self.head_dim):
-            raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, tokens, heads, self.head_dim, tuple(x.shape)))
-        st, sh, sd = x.stride()
-        if sd != 1 and tokens:
-            raise ValueError("%s: the last dimension must be contiguous" % name)
-        return x.data_ptr(), st, sh
+    def _views(self, index: int, tokens: int, *views) -> array:
+        """Pointers and strides of (tensor, name, heads) after checking them."""
+        dtype, d = self.dtype, self.head_dim
+        out = array("q")
+        for x, name, heads in views:
+            if x.get_device() != index or index < 0:
+                raise ValueError("%s must be on %s" % (name, "a CUDA device" if index < 0 else "cuda:%d" % index))
+            if x.dtype is not dtype:
+                raise TypeError("%s must be %s" % (name, dtype))
+            if x.shape != (tokens, heads, d):
+                raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, tokens, heads, d, tuple(x.shape)))
+            st, sh, sd = x.stride()
+            if sd != 1 and tokens:
+                raise ValueError("%s: the last dimension must be contiguous" % name)
+            out.extend((x.data_ptr(), st, sh))
+        return out
 
-    def _rest(self, positions, q_weight, k_weight, tokens, device):
+    def _rest(self, positions, q_weight, k_weight, tokens, index):
         """Positions' pointer and bytes, weights' pointers and dtype code."""
         at, size = 0, 8
         if self.rotary_dim:
-            if positions is None or positions.device != device or positions.shape != (tokens,) or \
-                    positions.dtype not in (torch.int64, torch.int32) or (tokens > 1 and positions.stride(0) != 1):
-                raise ValueError("positions must be a contiguous int32 or int64 [%d] tensor on %s" % (tokens, device))
-            at, size = positions.data_ptr(), positions.element_size()
-        pointers, code = [], None
-        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            if w is None:
-                pointers.append(0)
-                continue
-            if w.device != device or w.shape != (self.head_dim,) or w.stride(0) != 1:
-                raise ValueError("%s must be a contiguous [%d] tensor on %s" % (name, self.head_dim, device))
-            if code is not None and _dtype_code(w) != code:
+            if positions is not None:
+                size = _POSITIONS.get(positions.dtype)
+            if positions is None or size is None or positions.get_device() != index or positions.shape != (tokens,) or \
+                    not positions.is_contiguous():
+                raise ValueError("positions must be a contiguous int32 or int64 [%d] tensor on cuda:%d" % (tokens, index))
+            at = positions.data_ptr()
+        code = qw = kw = 0
+        if q_weight is not None:
+            qw, code = self._weight(q_weight, "q_weight", index), _dtype_code(q_weight)
+        if k_weight is not None:
+            kw, kc = self._weight(k_weight, "k_weight", index), _dtype_code(k_weight)
+            if q_weight is not None and kc != code:
                 raise TypeError("q_weight and k_weight must have one dtype")
-            code = _dtype_code(w)
-            pointers.append(w.data_ptr())
-        return at, size, pointers[0], pointers[1], code or 0
+            code = kc
+        return at, size, qw, kw, code
+
+    def _weight(self, w, name: str, index: int) -> int:
+        if w.get_device() != index or w.shape != (self.head_dim,) or not w.is_contiguous():
+            raise ValueError("%s must be a contiguous [%d] tensor on cuda:%d" % (name, self.head_dim, index))
+        return w.data_ptr()
 
     def forward(self, q, k, positions=None, q_weight=None, k_weight=None, q_out=None, k_out=None,
                 used: Optional[int] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """The normed and rotated (q, k).  An output may be its input itself."""
-        t, h, hk, device = q.shape[0], self.n_heads, self.n_kv_heads, q.device
-        check = self._check
-        args = (*check(q, "q", t, h, device), *check(k, "k", t, hk, device))
-        rest = self._rest(positions, q_weight, k_weight, t, device)
+        t, h, hk, index = q.shape[0], self.n_heads, self.n_kv_heads, q.get_device()
+        views = self._views(index, t, (q, "q", h), (k, "k", hk))
+        rest = self._rest(positions, q_weight, k_weight, t, index)
         _used_on(stream, q, k, positions, q_weight, k_weight, q_out, k_out)
         if q_out is None:
-            q_out = _empty((t, h, self.head_dim), self.dtype, device, stream)
+            q_out = _empty((t, h, self.head_dim), self.dtype, q.device, stream)
         if k_out is None:
-            k_out = _empty((t, hk, self.head_dim), self.dtype, device, stream)
-        heads = (ctypes.c_int64 * 12)(*args, *check(q_out, "q_out", t, h, device), *check(k_out, "k_out", t, hk, device))
-        at = ctypes.addressof(heads)
-        _on(device, C.normpre_qkrot_forward, self.plan, t, t if used is None else used, at, at + 24, *rest, at + 48, at + 72,
-            stream=stream)
+            k_out = _empty((t, hk, self.head_dim), self.dtype, q.device, stream)
+        views += self._views(index, t, (q_out, "q_out", h), (k_out, "k_out", hk))
+        at = views.buffer_info()[0]
+        _on_index(index, C.normpre_qkrot_forward, self.plan, t, t if used is None else used, at, at + 24, *rest, at + 48,
+                  at + 72, stream=stream)
         return q_out, k_out
 
     def backward(self, q, k, positions, dq_out, dk_out, q_weight=None, k_weight=None, dq=None, dk=None,
@@ -313,26 +328,30 @@ class QKNormRotary:
         """(dq, dk, dq_weight, dk_weight) from the gradients of ``forward``'s
         results.  A weight that is None has no gradient (None); with ``weights``
         False neither has."""
-        t, h, hk, device = q.shape[0], self.n_heads, self.n_kv_heads, q.device
-        check = self._check
-        args = (*check(q, "q", t, h, device), *check(k, "k", t, hk, device), *check(dq_out, "dq_out", t, h, device),
-                *check(dk_out, "dk_out", t, hk, device))
-        rest = self._rest(positions, q_weight, k_weight, t, device)
+        t, h, hk, index = q.shape[0], self.n_heads, self.n_kv_heads, q.get_device()
+        views = self._views(index, t, (q, "q", h), (k, "k", hk), (dq_out, "dq_out", h), (dk_out, "dk_out", hk))
+        rest = self._rest(positions, q_weight, k_weight, t, index)
         _used_on(stream, q, k, positions, dq_out, dk_out, q_weight, k_weight, dq, dk)
+        device = q.device
         if dq is None:
             dq = _empty((t, h, self.head_dim), self.dtype, device, stream)
         if dk is None:
             dk = _empty((t, hk, self.head_dim), self.dtype, device, stream)
-        new = lambda w: None if w is None or not weights else _empty((self.head_dim,), w.dtype, device, stream)  # noqa: E731
-        dqw, dkw = new(q_weight), new(k_weight)
-        work = None
-        if dqw is not None or dkw is not None:
-            work = _empty((self._bytes,), torch.uint8, device, stream)
-        heads = (ctypes.c_int64 * 18)(*args, *check(dq, "dq", t, h, device), *check(dk, "dk", t, hk, device))
-        at = ctypes.addressof(heads)
-        ptr = lambda x: 0 if x is None else x.data_ptr()  # noqa: E731
-        _on(device, C.normpre_qkrot_backward, self.plan, t, t if used is None else used, at, at + 24, *rest, at + 48,
-            at + 72, at + 96, at + 120, ptr(dqw), ptr(dkw), ptr(work), stream=stream)
+        views += self._views(index, t, (dq, "dq", h), (dk, "dk", hk))
+        dqw = dkw = None
+        to_q = to_k = work = 0
+        if weights and (q_weight is not None or k_weight is not None):
+            if q_weight is not None:
+                dqw = _empty((self.head_dim,), q_weight.dtype, device, stream)
+                to_q = dqw.data_ptr()
+            if k_weight is not None:
+                dkw = _empty((self.head_dim,), k_weight.dtype, device, stream)
+                to_k = dkw.data_ptr()
+            space = _empty((self._bytes,), torch.uint8, device, stream)
+            work = space.data_ptr()
+        at = views.buffer_info()[0]
+        _on_index(index, C.normpre_qkrot_backward, self.plan, t, t if used is None else used, at, at + 24, *rest, at + 48,
+                  at + 72, at + 96, at + 120, to_q, to_k, work, stream=stream)
         return dq, dk, dqw, dkw
 
     def __call__(self, q, k, positions=None, q_weight=None, k_weight=None, used: Optional[int] = None):

@@ -390,19 +390,19 @@ def normpre_qkrot_bytes(plan: int) -> int:
 def normpre_qkrot_forward(plan: int, tokens: int, used: int, q, k, positions: int, position_bytes: int, q_weight: int,
                           k_weight: int, weight_dtype: int, q_out, k_out, stream: int = 0) -> int:
     """q, k, q_out, k_out: ``normpre_heads`` or their addresses."""
-    return _check(load_library().normpre_qkrot_forward(plan, tokens, used, _by_ref(q), _by_ref(k), positions,
-                                                       position_bytes, q_weight, k_weight, weight_dtype,
-                                                       _by_ref(q_out), _by_ref(k_out), stream))
+    rc = load_library().normpre_qkrot_forward(plan, tokens, used, _by_ref(q), _by_ref(k), positions, position_bytes,
+                                              q_weight, k_weight, weight_dtype, _by_ref(q_out), _by_ref(k_out), stream)
+    return rc if rc == NORMPRE_OK else _check(rc)
 
 
 def normpre_qkrot_backward(plan: int, tokens: int, used: int, q, k, positions: int, position_bytes: int, q_weight: int,
                            k_weight: int, weight_dtype: int, dq_out, dk_out, dq, dk, dq_weight: int, dk_weight: int,
                            workspace: int, stream: int = 0) -> int:
     """q, k, dq_out .. dk: ``normpre_heads`` or their addresses."""
-    return _check(load_library().normpre_qkrot_backward(plan, tokens, used, _by_ref(q), _by_ref(k), positions,
-                                                        position_bytes, q_weight, k_weight, weight_dtype,
-                                                        _by_ref(dq_out), _by_ref(dk_out), _by_ref(dq), _by_ref(dk),
-                                                        dq_weight, dk_weight, workspace, stream))
+    rc = load_library().normpre_qkrot_backward(plan, tokens, used, _by_ref(q), _by_ref(k), positions, position_bytes,
+                                               q_weight, k_weight, weight_dtype, _by_ref(dq_out), _by_ref(dk_out),
+                                               _by_ref(dq), _by_ref(dk), dq_weight, dk_weight, workspace, stream)
+    return rc if rc == NORMPRE_OK else _check(rc)
 
 
 def normpre_qkrot_free(plan: int) -> None:

@@ -215,23 +215,26 @@ def _dense(x) -> bool:
 
 
 def _grad_lists(grads, name: str = "gradient"):
-    """Checks gradients and returns their pointers, dtype codes and sizes."""
+    """Checks gradients and returns their pointers, dtype codes and sizes, and
+    whether all are contiguous."""
     import torch
-    codes = {torch.float32: C.NORMPRE_F32, torch.bfloat16: C.NORMPRE_BF16}
-    strided, index = torch.strided, grads[0].get_device()
+    code_of = {torch.float32: C.NORMPRE_F32, torch.bfloat16: C.NORMPRE_BF16}.get
+    strided, index, plain = torch.strided, grads[0].get_device(), True
     pointers, types, sizes = [], [], []
     for i, g in enumerate(grads):
-        if g.layout != strided or index < 0 or g.get_device() != index:
-            raise ValueError("%s %d: all must be dense CUDA tensors on one device" % (name, i))
-        code = codes.get(g.dtype)
+        code = code_of(g.dtype)
         if code is None:
             raise TypeError("%s %d: unsupported dtype %s (float32 or bfloat16)" % (name, i, g.dtype))
-        if not (g.is_contiguous() or _dense(g)):
-            raise ValueError("%s %d: its memory must have no gaps" % (name, i))
+        if index < 0 or g.get_device() != index or g.layout is not strided:
+            raise ValueError("%s %d: all must be dense CUDA tensors on one device" % (name, i))
+        if not g.is_contiguous():
+            if not _dense(g):
+                raise ValueError("%s %d: its memory must have no gaps" % (name, i))
+            plain = False
         pointers.append(g.data_ptr())
         types.append(code)
         sizes.append(g.numel())
-    return pointers, types, sizes
+    return (pointers, types, sizes), plain
 
 
 def _grad_call(device, f, *args):
@@ -255,7 +258,7 @@ def grad_norm(grads):
     grads = list(grads)
     if not grads:
         return torch.zeros((), dtype=torch.float32, device="cuda")
-    return _grad_call(grads[0].device, C.normpre_grad_norm, *_grad_lists(grads))
+    return _grad_call(grads[0].device, C.normpre_grad_norm, *_grad_lists(grads)[0])
 
 
 def clip_grads(grads, max_norm: float, eps: float = 1e-6, out=None):
@@ -268,18 +271,19 @@ def clip_grads(grads, max_norm: float, eps: float = 1e-6, out=None):
     grads = list(grads)
     if not grads:
         return torch.zeros((), dtype=torch.float32, device="cuda")
-    lists = _grad_lists(grads)
-    if out is None:
-        to = lists
-    else:
+    lists, plain = _grad_lists(grads)
+    to = lists
+    if out is not None:
         out = list(out)
         if len(out) != len(grads):
             raise ValueError("out must have a tensor for each gradient")
-        to = _grad_lists(out, "out")
+        to, plain_out = _grad_lists(out, "out")
+        if out[0].device != grads[0].device:
+            raise ValueError("out must be on its gradients' device")
         for i, (g, o) in enumerate(zip(grads, out)):
-            if o.shape != g.shape or (i == 0 and o.device != g.device):
-                raise ValueError("out %d must have its gradient's shape and device" % i)
-            if not (o.is_contiguous() and g.is_contiguous()) and o.stride() != g.stride():
+            if o.shape != g.shape:
+                raise ValueError("out %d must have its gradient's shape" % i)
+            if not (plain and plain_out) and not (o.is_contiguous() and g.is_contiguous()) and o.stride() != g.stride():
                 raise ValueError("out %d must have its gradient's strides" % i)
     return _grad_call(grads[0].device, C.normpre_grad_clip, *lists, to[0], to[1], float(max_norm), float(eps))
 
