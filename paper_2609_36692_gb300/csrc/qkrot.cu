@@ -211,11 +211,30 @@ __device__ __forceinline__ void scale(uint64_t (&x)[4], float f) {
   for (int e = 0; e < 4; ++e) x[e] = tc::mul2(x[e], f2);
 }
 
-// 1 / sqrt(sum / dim + eps)
+// The sums of two heads over the lanes of a row (two or more): the row's upper
+// half of lanes ends with the second head's, the lower half with the first's, in
+// one shuffle a step instead of two.  (Forward only: backward it takes registers
+// that are not there, 71 us against 68.)
+__device__ __forceinline__ float split_sum(float first, float second, int lanes, bool upper) {
+  float mine = (upper ? second : first) + __shfl_xor_sync(0xffffffffu, upper ? first : second, lanes >> 1);
+#pragma unroll
+  for (int o = 8; o; o >>= 1)
+    if (o < lanes >> 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  return mine;
+}
+// A value of each half's head, for all lanes.
+__device__ __forceinline__ void join_halves(float mine, int lanes, bool upper, float (&both)[2]) {
+  const float other = __shfl_xor_sync(0xffffffffu, mine, lanes >> 1);
+  both[0] = upper ? other : mine;
+  both[1] = upper ? mine : other;
+}
+
+// 1 / sqrt(sum / dim + eps); that sum is a normal number or infinite.
 __device__ __forceinline__ float inverse_root(float sum, const RotArgs& g, float eps) {
   const float m = fmaf(sum, g.inv_dim, eps);
-  const float r = rsqrtf(m);
-  // one Newton step: rsqrtf may be off by two units in the last place
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(m));
+  // one Newton step: the approximation may be off by two units in the last place
   return m < INFINITY ? fmaf(0.5f * r, fmaf(-m * r, r, 1.f), r) : r;
 }
 // Rows whose squares leave fp32's range are scaled by a power of two first.
@@ -245,6 +264,7 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
   const int64_t n_warps = static_cast<int64_t>(ctas) * kWarps, w = static_cast<int64_t>(cta) * kWarps + warp;
   const int64_t begin = units * w / n_warps;
   int left = static_cast<int>(units * (w + 1) / n_warps - begin);
+  const bool upper = u >= g.lanes >> 1;
   uint32_t turned = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -381,14 +401,21 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
         }
       }
     } else if constexpr (!BWD) {
-      float sum[H], r[H];
+      float sum[H], r[H], mine = 0.f;
       bool fits = true;
 #pragma unroll
       for (int i = 0; i < H; ++i) sum[i] = dot(x[i], x[i]);
-      row_sums(sum, g.lanes);
+      const bool split = H == 2 && g.lanes > 1;
+      if (split) {
+        mine = split_sum(sum[0], sum[H - 1], g.lanes, upper);
+        fits = mine < kLargeSum;
+      } else {
+        row_sums(sum, g.lanes);
 #pragma unroll
-      for (int i = 0; i < H; ++i) fits = fits && sum[i] < kLargeSum;
+        for (int i = 0; i < H; ++i) fits = fits && sum[i] < kLargeSum;
+      }
       if (__any_sync(0xffffffffu, !fits)) {
+        if (split) row_sums(sum, g.lanes);
 #pragma unroll
         for (int i = 0; i < H; ++i) {
           const float down = sum[i] < kLargeSum ? 1.f : kDown;
@@ -397,6 +424,8 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
           row_sums(again, g.lanes);
           r[i] = inverse_root(again[0], g, g.eps * down * down);
         }
+      } else if (split) {
+        if constexpr (H == 2) join_halves(inverse_root(mine, g, g.eps), g.lanes, upper, r);
       } else {
 #pragma unroll
         for (int i = 0; i < H; ++i) r[i] = inverse_root(sum[i], g, g.eps);
