@@ -55,6 +55,10 @@ __host__ __device__ inline int last_query(int blk, int len, int window, int sink
   return 128 * blk < sinks || last < in ? last : in;
 }
 
+// Whether every row sees itself alone: then p = 1 whatever the scores, and ds = 0
+// is written as such, where the difference of two equal sums would leave noise.
+__host__ __device__ inline bool sees_itself(int window, int sinks) { return window == 1 && sinks == 0; }
+
 // The sinks' key blocks meet all later query blocks, however short the window.
 // They are split into parts of about `chunk` query blocks, each an item of its
 // own, whose sums over queries (dk, dv in fp32) lie in a slot of the workspace

@@ -527,6 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
         }
         if constexpr (WIN) {
           if (diag || edge) {   // 0 * NaN in an unseen place
+            if (sees_itself(a.window, a.sinks)) hide = ~0u;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               if (hide >> (2 * e) & 1u) pk[e] &= 0xFFFF0000u;
@@ -723,7 +724,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
         if constexpr (WIN) {
           if (kTile * (it.blk - j + 1) > a.window || j == it.blk) {
             const int up = kTile * (it.blk - j) - 32 * part;
-            const uint32_t hide = hidden_bits(up + row, up + row - a.window + 1, a.sinks - kTile * j - 32 * part);
+            uint32_t hide = hidden_bits(up + row, up + row - a.window + 1, a.sinks - kTile * j - 32 * part);
+            if (sees_itself(a.window, a.sinks)) hide = ~0u;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               if (hide >> (2 * e) & 1u) pk[e] &= 0xFFFF0000u;

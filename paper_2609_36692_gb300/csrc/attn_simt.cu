@@ -293,7 +293,7 @@ __device__ __forceinline__ void grad_scores(const AttnArgs& a, const float* Q, c
       const int j = j0 + tx + 16 * c;
       const bool seen = i < len && j <= i && (i - j < a.window || j < a.sinks);
       p[r][c] = seen ? exp2f(fmaf(t[r][c], a.scale, -ls) * kLog2e) : 0.f;
-      s[r][c] = seen ? p[r][c] * (s[r][c] - de) : 0.f;
+      s[r][c] = seen && !sees_itself(a.window, a.sinks) ? p[r][c] * (s[r][c] - de) : 0.f;
     }
   }
 }

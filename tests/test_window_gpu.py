@@ -111,6 +111,24 @@ def test_long(window, sinks, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", [(4, 2, 64), (2, 1, 128)], ids=str)
+def test_rows_that_see_themselves_alone(layout, dtype):
+    """p = 1: the output is the value, and no gradient reaches queries and keys."""
+    import torch
+    h, hk, d = layout
+    lengths = [300, 1, 211]
+    q, k, v, do = make(4, 520, h, hk, d, dtype)
+    plan = plan_for(h, hk, d, 520, lengths, dtype, window=1, sinks=0)
+    out, lse = plan.forward(q, k, v)
+    dq, dk, dv = plan.backward(q, k, v, out, lse, do)
+    assert plan.status() == 0
+    assert torch.equal(out[:512], v[:512].repeat_interleave(h // hk, 1))
+    assert not bool(dq.any()) and not bool(dk.any())
+    ref = do[:512].double().view(512, hk, h // hk, d).sum(2)
+    assert err(dv[:512], ref) <= TOL[dtype, "bwd"]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_very_long(dtype):
     """Lists too long to be dealt out one by one."""
     check((3, 3, 64), [40000] if dtype == "bf16" else [9000], 70, 5, dtype)
