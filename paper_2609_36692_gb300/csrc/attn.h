@@ -42,6 +42,8 @@ struct KeySpan {
   // the block after j, on the way up
   __host__ __device__ int up(int j) const { return j + 1 == sink ? lo : j + 1; }
   __host__ __device__ int first() const { return sink ? 0 : lo; }
+  // the block of which only the first 32 keys or fewer are seen, as sinks; -1: none
+  __host__ __device__ int narrow(int sinks) const { return sink && sinks - 128 * (sink - 1) <= 32 ? sink - 1 : -1; }
 };
 __host__ __device__ inline KeySpan key_span(int blk, int window, int sinks) {
   KeySpan s;

@@ -23,6 +23,9 @@
 // and dS^T lie in TMEM as the A operands of dV and dK.  Chains: P(i) -> dV(i),
 // S(i+1) and dS(i) -> dK(i), dP(i+1).  TMEM at head_dim 128: S^T 128, dP^T 128,
 // dV 128, dK 128 columns, all there is.
+// With a window, the walks are those of the rows that see each other; of the
+// last sink block that a query block meets, k_attn_dq takes 32 keys only where no
+// more are visible.
 // k_attn_dq: S in two buffers, dP, dQ; dS lies over S, so that dP(j+1) starts
 // as soon as dP(j) has been read.  Chains: dS(j) -> dQ(j), S(j+2) and dP(j).
 // Head dimensions up to 64 leave room for a second set of owned tiles and a
@@ -619,13 +622,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int n = keys(it).count(it.blk);
+        const int narrow = WIN ? keys(it).narrow(a.sinks) : -1;     // a block's number in the walk too: the sinks' come first
         const uint32_t q = tc::su32(own + 2 * set.i * kTileBytes);
         int k[2] = {0, 0};                                        // ring slots of K(j), K(j + 1)
         auto scores = [&](int j, int& slot) {
           slot = w.take();
           w.next();                                               // V is the other chain's
           if (!w.ok) return;
-          product_ss<DP>(cS + 128 * (buf.i ^ (j & 1)), q, tile(slot));
+          if (WIN && j == narrow) product_ss<DP, 0, DP / 16, 32>(cS + 128 * (buf.i ^ (j & 1)), q, tile(slot));
+          else product_ss<DP>(cS + 128 * (buf.i ^ (j & 1)), q, tile(slot));
           tc::mma_commit(&b->s_full[buf.i ^ (j & 1)]);
           if (j + 1 == n) tc::mma_commit(&b->own_empty[set.i]);
         };
@@ -637,7 +642,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
           const int at = buf.i ^ (j & 1);
           if (!w.wait1(&b->ds_ready[at], (ds_phase >> at) & 1u)) break;
           ds_phase ^= 1u << at;
-          product_ts<DP, 4>(cAcc + DP * set.i, cS + 128 * at, tile(k[0]), j == 0);
+          if (WIN && j == narrow) product_ts<DP, 4, 0, 2>(cAcc + DP * set.i, cS + 128 * at, tile(k[0]), j == 0);
+          else product_ts<DP, 4>(cAcc + DP * set.i, cS + 128 * at, tile(k[0]), j == 0);
           tc::mma_commit(&b->empty[k[0]]);
           k[0] = k[1];
           if (j + 2 < n) {
@@ -659,13 +665,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const uint32_t o = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
-        for (int n = keys(it).count(it.blk); n > 0; --n) {
+        const int all = keys(it).count(it.blk), narrow = WIN ? keys(it).narrow(a.sinks) : -1;
+        for (int n = all; n > 0; --n) {
           w.next();
           const int v = w.take();
           // free once the last block's dP has been read
           if (!w.wait1(&b->dp_free, free_phase ^ 1u)) break;
           free_phase ^= 1u;
-          product_ss<DP>(cP, o, tc::su32(ring + v * kTileBytes));
+          if (WIN && all - n == narrow) product_ss<DP, 0, DP / 16, 32>(cP, o, tc::su32(ring + v * kTileBytes));
+          else product_ss<DP>(cP, o, tc::su32(ring + v * kTileBytes));
           tc::mma_commit(&b->dp_full);
           tc::mma_commit(&b->empty[v]);
           if (n == 1) tc::mma_commit(&b->own_empty[set.i]);
@@ -698,7 +706,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       const float ls = in ? -a.lse[si] : -INFINITY, de = in ? a.delta[si] : 0.f;
       const uint64_t ls2 = tc::pack2(ls, ls);
       const KeySpan span = keys(it);
+      const int narrow = WIN ? span.narrow(a.sinks) : -1;
       for (int j = span.first(); j <= it.blk; j = WIN ? span.up(j) : j + 1, buf.next()) {
+        if (WIN && j == narrow && part) {                         // no columns of this part are seen
+          if (!w.wait(&b->s_full[buf.i], buf.parity) || !w.wait(&b->dp_full, dp_phase)) break;
+          dp_phase ^= 1u;
+          w.arrive(&b->dp_free);
+          w.arrive(&b->ds_ready[buf.i]);
+          continue;
+        }
         const uint32_t mS = cS + 128 * buf.i + lanes + 32 * part, mP = cP + lanes + 32 * part;
         if (!w.wait(&b->s_full[buf.i], buf.parity)) break;
         float p[32];

@@ -8,6 +8,10 @@
 // first: every row sees itself there, so m is finite from then on, and no
 // other block needs a mask (a sequence's end lies in its last diagonal block).
 //
+// With a window, the blocks are those of the window and then the sinks'; of the
+// last of these only 32 keys go through the products and the softmax where no more
+// are visible (a few sinks are the common case).
+//
 // One CTA per SM walks the work list.  An item is two query tiles that read
 // the same keys: two heads of a group, or with an odd group two neighbouring
 // tiles of one head.  Each has its own 128 columns of scores and its output
@@ -260,10 +264,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           return t;
         };
         // S = Q K^T, and the turn is over
-        auto scores = [&](int k) {
-          product_ss<DP, 0, DP / 32>(s_col(s), sq, tile(k));
-          pass_turn();
-          product_ss<DP, DP / 32, DP / 16>(s_col(s), sq, tile(k));
+        auto scores = [&](int k, bool few) {
+          if (WIN && few) {
+            pass_turn();
+            product_ss<DP, 0, DP / 16, 32>(s_col(s), sq, tile(k));
+          } else {
+            product_ss<DP, 0, DP / 32>(s_col(s), sq, tile(k));
+            pass_turn();
+            product_ss<DP, DP / 32, DP / 16>(s_col(s), sq, tile(k));
+          }
           tc::mma_commit(&b->s_full[s]);
           tc::mma_commit(&b->empty[k]);
         };
@@ -273,13 +282,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           // and the last block that it meets
           const KeySpan own = WIN && blk >= 0 ? key_span(blk, f.a.window, f.a.sinks) : KeySpan{0, 0};
           const int last = WIN ? own.first() : 0;
+          const int narrow = WIN && blk >= 0 ? own.narrow(f.a.sinks) : -1;
           auto meets = [&](int j) { return j <= blk && (!WIN || j >= own.lo || j < own.sink); };
           int k = take();
           if (blk >= 0 && !wait(&b->q_full[s], q_phase)) break;
           if (blk >= 0) q_phase ^= 1u;
           if (!ok || !my_turn()) break;
           if (it.top == blk) {
-            scores(k);
+            scores(k, false);
             if (blk == last) tc::mma_commit(&b->q_empty[s]);
           } else {
             tc::mbar_arrive(&b->empty[k]);
@@ -297,9 +307,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
                 o_phase ^= 1u << acc;
               }
               if (!my_turn() || !wait(&b->p_ready[s][0], p_phase)) break;
-              product_ts<DP, 1, 0, 6>(o, p, tile(v), j == blk);
-              if (!wait(&b->p_ready[s][1], p_phase)) break;
-              product_ts<DP, 1, 6, 8>(o, p, tile(v), false);
+              if (WIN && j == narrow) {
+                product_ts<DP, 1, 0, 2>(o, p, tile(v), false);
+                if (!wait(&b->p_ready[s][1], p_phase)) break;
+              } else {
+                product_ts<DP, 1, 0, 6>(o, p, tile(v), j == blk);
+                if (!wait(&b->p_ready[s][1], p_phase)) break;
+                product_ts<DP, 1, 6, 8>(o, p, tile(v), false);
+              }
               p_phase ^= 1u;
               tc::mma_commit(&b->pv_done[s]);
               tc::mma_commit(&b->empty[v]);
@@ -308,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
               tc::mbar_arrive(&b->empty[v]);
             }
             if (next >= 0 && meets(next)) {
-              scores(k);
+              scores(k, next == narrow);
               if (next == last) tc::mma_commit(&b->q_empty[s]);
             } else {
               if (next >= 0) tc::mbar_arrive(&b->empty[k]);
@@ -347,6 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       const uint32_t oc = o_col(s, acc) + lanes;
       float m = -INFINITY, l = 0.f;
       const KeySpan own = WIN ? key_span(blk, f.a.window, f.a.sinks) : KeySpan{0, 0};
+      const int narrow = WIN ? own.narrow(f.a.sinks) : -1;
       for (int j = blk; j >= 0; j = WIN ? own.down(j) : j - 1) {
         if (!wait(&b->s_full[s], s_phase)) break;
         s_phase ^= 1u;
@@ -417,6 +433,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           }
           return true;
         };
+        if (WIN && j == narrow) {
+          // a quarter is all there is
+          load(0);
+          mask(0);
+          compare();
+          const float up = fmaxf(m, top());
+          if (__any_sync(0xffffffffu, (up - m) * c > kRaise) && !raise(up)) break;
+          exps(p);
+          tc::tmem_put16(sc, p);
+          release(0);
+          release(1);
+          float lo, hi;
+          tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
+          l += lo + hi;
+          ++pv;
+          continue;
+        }
         // Three quarters of P go first: the products on them cover the rest.
         if (j == blk || (WIN && edge)) {
 #pragma unroll

@@ -53,11 +53,11 @@ __device__ __forceinline__ uint64_t desc_rows(uint32_t tile) { return tc::sdesc(
 __host__ __device__ constexpr uint64_t cols_step(int kk) { return ((kk >> 2) * kChunk + (kk & 3) * 32) >> 4; }
 __host__ __device__ constexpr uint64_t rows_step(int kk) { return (kk * 2048) >> 4; }
 
-// D = A B^T over columns 16 K0 .. 16 K1 of the head dimension: both tiles in
-// shared memory.
-template <int DP, int K0 = 0, int K1 = DP / 16>
+// D = A B^T over columns 16 K0 .. 16 K1 of the head dimension, of B's first N
+// rows: both tiles in shared memory.
+template <int DP, int K0 = 0, int K1 = DP / 16, int N = kTile>
 __device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b) {
-  constexpr uint32_t idesc = tc::idesc_bf16(kTile, kTile, 0, 0);
+  constexpr uint32_t idesc = tc::idesc_bf16(kTile, N, 0, 0);
   const uint64_t ad = desc_cols(a), bd = desc_cols(b);
 #pragma unroll
   for (int kk = K0; kk < K1; ++kk) tc::mma_bf16(d, ad + cols_step(kk), bd + cols_step(kk), idesc, kk != 0);
