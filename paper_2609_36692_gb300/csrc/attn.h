@@ -121,6 +121,17 @@ struct AttnArgs {
 // neighbouring tiles of one head.
 inline bool attn_pair_heads(int group) { return group % 2 == 0; }
 
+// Kinds of tensor-core kernels: no window; one; one whose narrow sink block (see
+// KeySpan::narrow) has a path of its own.  That path pays where it is a good part
+// of the walk, and its code costs 4 % everywhere (forward, one H of 128 or 64: window
+// 256 with 4 sinks 39.6 -> 38.7 and 62.7 -> 58.6 us, window 1024 54.0 -> 55.0 and 88.9 ->
+// 90.1), so that only short windows take it.
+enum WindowKind { kWhole = 0, kWindow = 1, kWindowNarrow = 2 };
+inline int window_kind(const AttnArgs& a) {
+  if (a.window >= kNoWindow) return kWhole;
+  return a.window <= 512 && a.sinks > 0 && (a.sinks - 1) % 128 < 32 ? kWindowNarrow : kWindow;
+}
+
 // CTAs of a tensor-core kernel.
 inline int walk_grid(int64_t items) {
   return static_cast<int>(items < 1 ? 1 : items < device_sm_count() ? items : device_sm_count());

@@ -568,8 +568,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   finish(w, warp, a.flags);
 }
 
-template <int DP, bool WIN>
+template <int DP, int KIND>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constant__ BwdArgs f) {
+  constexpr bool WIN = KIND != kWhole, kFew = KIND == kWindowNarrow;
   using B = Bwd<DP>;
   constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks, kSets = B::kSets;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -622,14 +623,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       auto tile = [&](int s) { return tc::su32(ring + s * kTileBytes); };
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const int n = keys(it).count(it.blk);
-        const int narrow = WIN ? keys(it).narrow(a.sinks) : -1;     // a block's number in the walk too: the sinks' come first
+        const int narrow = kFew ? keys(it).narrow(a.sinks) : -1;     // a block's number in the walk too: the sinks' come first
         const uint32_t q = tc::su32(own + 2 * set.i * kTileBytes);
         int k[2] = {0, 0};                                        // ring slots of K(j), K(j + 1)
         auto scores = [&](int j, int& slot) {
           slot = w.take();
           w.next();                                               // V is the other chain's
           if (!w.ok) return;
-          if (WIN && j == narrow) product_ss<DP, 0, DP / 16, 32>(cS + 128 * (buf.i ^ (j & 1)), q, tile(slot));
+          if (kFew && j == narrow) product_ss<DP, 0, DP / 16, 32>(cS + 128 * (buf.i ^ (j & 1)), q, tile(slot));
           else product_ss<DP>(cS + 128 * (buf.i ^ (j & 1)), q, tile(slot));
           tc::mma_commit(&b->s_full[buf.i ^ (j & 1)]);
           if (j + 1 == n) tc::mma_commit(&b->own_empty[set.i]);
@@ -642,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
           const int at = buf.i ^ (j & 1);
           if (!w.wait1(&b->ds_ready[at], (ds_phase >> at) & 1u)) break;
           ds_phase ^= 1u << at;
-          if (WIN && j == narrow) product_ts<DP, 4, 0, 2>(cAcc + DP * set.i, cS + 128 * at, tile(k[0]), j == 0);
+          if (kFew && j == narrow) product_ts<DP, 4, 0, 2>(cAcc + DP * set.i, cS + 128 * at, tile(k[0]), j == 0);
           else product_ts<DP, 4>(cAcc + DP * set.i, cS + 128 * at, tile(k[0]), j == 0);
           tc::mma_commit(&b->empty[k[0]]);
           k[0] = k[1];
@@ -665,14 +666,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       for (int64_t r = 0; w.ok && get_item(item(r), it); ++r, set.next()) {
         const uint32_t o = tc::su32(own + (2 * set.i + 1) * kTileBytes);
         if (!w.wait1(&b->own_full[set.i][1], set.parity)) break;
-        const int all = keys(it).count(it.blk), narrow = WIN ? keys(it).narrow(a.sinks) : -1;
+        const int all = keys(it).count(it.blk), narrow = kFew ? keys(it).narrow(a.sinks) : -1;
         for (int n = all; n > 0; --n) {
           w.next();
           const int v = w.take();
           // free once the last block's dP has been read
           if (!w.wait1(&b->dp_free, free_phase ^ 1u)) break;
           free_phase ^= 1u;
-          if (WIN && all - n == narrow) product_ss<DP, 0, DP / 16, 32>(cP, o, tc::su32(ring + v * kTileBytes));
+          if (kFew && all - n == narrow) product_ss<DP, 0, DP / 16, 32>(cP, o, tc::su32(ring + v * kTileBytes));
           else product_ss<DP>(cP, o, tc::su32(ring + v * kTileBytes));
           tc::mma_commit(&b->dp_full);
           tc::mma_commit(&b->empty[v]);
@@ -706,9 +707,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       const float ls = in ? -a.lse[si] : -INFINITY, de = in ? a.delta[si] : 0.f;
       const uint64_t ls2 = tc::pack2(ls, ls);
       const KeySpan span = keys(it);
-      const int narrow = WIN ? span.narrow(a.sinks) : -1;
+      const int narrow = kFew ? span.narrow(a.sinks) : -1;
       for (int j = span.first(); j <= it.blk; j = WIN ? span.up(j) : j + 1, buf.next()) {
-        if (WIN && j == narrow && part) {                         // no columns of this part are seen
+        if (kFew && j == narrow && part) {                         // no columns of this part are seen
           if (!w.wait(&b->s_full[buf.i], buf.parity) || !w.wait(&b->dp_full, dp_phase)) break;
           dp_phase ^= 1u;
           w.arrive(&b->dp_free);
@@ -775,10 +776,10 @@ cudaError_t launch(const BwdArgs& f, int64_t items, size_t smem, cudaStream_t s)
   return cudaGetLastError();
 }
 
-template <int DP, bool WIN>
+template <int DP, int KIND>
 cudaError_t both(const BwdArgs& f, cudaStream_t s) {
-  const cudaError_t e = launch<k_attn_dkdv_tc<DP, WIN>>(f, static_cast<int64_t>(f.a.n_keys) * f.a.kv_heads, Bwd<DP>::kSmem, s);
-  return e ? e : launch<k_attn_dq_tc<DP, WIN>>(f, static_cast<int64_t>(f.a.n_blocks) * f.a.heads, Bwd<DP>::kSmem, s);
+  const cudaError_t e = launch<k_attn_dkdv_tc<DP, KIND != kWhole>>(f, static_cast<int64_t>(f.a.n_keys) * f.a.kv_heads, Bwd<DP>::kSmem, s);
+  return e ? e : launch<k_attn_dq_tc<DP, KIND>>(f, static_cast<int64_t>(f.a.n_blocks) * f.a.heads, Bwd<DP>::kSmem, s);
 }
 
 }  // namespace
@@ -790,8 +791,11 @@ cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t s, std::stri
       !rows_map(&f.v, a.v, a.tokens, a.kv_heads, a.dim, err) ||
       !rows_map(&f.dout, a.dout, a.tokens, a.heads, a.dim, err))
     return cudaErrorInvalidValue;
-  if (a.window < kNoWindow) return a.dim <= 64 ? both<64, true>(f, s) : both<128, true>(f, s);
-  return a.dim <= 64 ? both<64, false>(f, s) : both<128, false>(f, s);
+  switch (window_kind(a)) {
+    case kWindow: return a.dim <= 64 ? both<64, kWindow>(f, s) : both<128, kWindow>(f, s);
+    case kWindowNarrow: return a.dim <= 64 ? both<64, kWindowNarrow>(f, s) : both<128, kWindowNarrow>(f, s);
+    default: return a.dim <= 64 ? both<64, kWhole>(f, s) : both<128, kWhole>(f, s);
+  }
 }
 
 }  // namespace normpre

@@ -116,12 +116,13 @@ __device__ __forceinline__ bool get_item(const FwdArgs& f, const ItemRef* cached
   return true;
 }
 
-// WIN: the rows have a window (else the spans are whole and nothing is hidden
+// KIND: see WindowKind (without a window the spans are whole and nothing is hidden
 // but by the diagonal).
-template <int DP, bool WIN>
+template <int DP, int KIND>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_constant__ FwdArgs f) {
   using F = Fwd<DP>;
   constexpr int kSlots = F::kSlots, kTileBytes = F::kTileBytes, kChunks = F::kChunks, kAcc = F::kAcc;
+  constexpr bool WIN = KIND != kWhole, kFew = KIND == kWindowNarrow;
   constexpr float kRaise = WIN ? kGrowWindow : kGrow;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* sQ = smem;                          // [2]
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
         };
         // S = Q K^T, and the turn is over
         auto scores = [&](int k, bool few) {
-          if (WIN && few) {
+          if (kFew && few) {
             pass_turn();
             product_ss<DP, 0, DP / 16, 32>(s_col(s), sq, tile(k));
           } else {
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           // and the last block that it meets
           const KeySpan own = WIN && blk >= 0 ? key_span(blk, f.a.window, f.a.sinks) : KeySpan{0, 0};
           const int last = WIN ? own.first() : 0;
-          const int narrow = WIN && blk >= 0 ? own.narrow(f.a.sinks) : -1;
+          const int narrow = kFew && blk >= 0 ? own.narrow(f.a.sinks) : -1;
           auto meets = [&](int j) { return j <= blk && (!WIN || j >= own.lo || j < own.sink); };
           int k = take();
           if (blk >= 0 && !wait(&b->q_full[s], q_phase)) break;
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
                 o_phase ^= 1u << acc;
               }
               if (!my_turn() || !wait(&b->p_ready[s][0], p_phase)) break;
-              if (WIN && j == narrow) {
+              if (kFew && j == narrow) {
                 product_ts<DP, 1, 0, 2>(o, p, tile(v), false);
                 if (!wait(&b->p_ready[s][1], p_phase)) break;
               } else {
@@ -362,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       const uint32_t oc = o_col(s, acc) + lanes;
       float m = -INFINITY, l = 0.f;
       const KeySpan own = WIN ? key_span(blk, f.a.window, f.a.sinks) : KeySpan{0, 0};
-      const int narrow = WIN ? own.narrow(f.a.sinks) : -1;
+      const int narrow = kFew ? own.narrow(f.a.sinks) : -1;
       for (int j = blk; j >= 0; j = WIN ? own.down(j) : j - 1) {
         if (!wait(&b->s_full[s], s_phase)) break;
         s_phase ^= 1u;
@@ -433,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
           }
           return true;
         };
-        if (WIN && j == narrow) {
+        if (kFew && j == narrow) {
           // a quarter is all there is
           load(0);
           mask(0);
@@ -550,11 +551,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
 
 }  // namespace
 
-template <int DP, bool WIN>
+template <int DP, int KIND>
 static cudaError_t launch(const FwdArgs& f, int64_t items, cudaStream_t s) {
-  const cudaError_t e = allow_smem<k_attn_fwd_tc<DP, WIN>>(Fwd<DP>::kSmem);
+  const cudaError_t e = allow_smem<k_attn_fwd_tc<DP, KIND>>(Fwd<DP>::kSmem);
   if (e) return e;
-  k_attn_fwd_tc<DP, WIN><<<walk_grid(items), kThreads, Fwd<DP>::kSmem, s>>>(f);
+  k_attn_fwd_tc<DP, KIND><<<walk_grid(items), kThreads, Fwd<DP>::kSmem, s>>>(f);
   return cudaGetLastError();
 }
 
@@ -568,8 +569,11 @@ cudaError_t launch_attn_forward_tc(const AttnArgs& a, cudaStream_t s, std::strin
   f.list = f.pair_heads ? a.by_query : a.by_pair;
   f.n_list = f.pair_heads ? a.n_blocks : a.n_pairs;
   const int64_t items = static_cast<int64_t>(f.n_list) * (f.pair_heads ? a.heads / 2 : a.heads);
-  if (a.window < kNoWindow) return a.dim <= 64 ? launch<64, true>(f, items, s) : launch<128, true>(f, items, s);
-  return a.dim <= 64 ? launch<64, false>(f, items, s) : launch<128, false>(f, items, s);
+  switch (window_kind(a)) {
+    case kWindow: return a.dim <= 64 ? launch<64, kWindow>(f, items, s) : launch<128, kWindow>(f, items, s);
+    case kWindowNarrow: return a.dim <= 64 ? launch<64, kWindowNarrow>(f, items, s) : launch<128, kWindowNarrow>(f, items, s);
+    default: return a.dim <= 64 ? launch<64, kWhole>(f, items, s) : launch<128, kWhole>(f, items, s);
+  }
 }
 
 }  // namespace normpre

@@ -432,24 +432,37 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) k_attn_bwd(const _
   else owned_queries<T, DP>(a, item, which - a.kv_heads, sm, lse, delta);
 }
 
-// LANES (8 or 16) lanes per row and head, 8 columns each.
-template <typename T, int LANES>
+// LANES (8 or 16) lanes per row and head, 8 columns each; EACH rows and heads a
+// thread, whose loads are in flight together, where there are enough.  Index: type
+// of the number of rows and heads, 32 bits where they do (the division took most of
+// the time).  Bound by HBM: 8192 rows, 16 heads of 128 in bf16, 67 MB in 11 us.
+template <typename T, int LANES, int EACH, typename Index>
 __global__ void __launch_bounds__(256) k_attn_delta(const __grid_constant__ AttnArgs a) {
+  constexpr int kStep = 256 / LANES;
   const int lane = threadIdx.x % LANES;
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) / LANES;   // token-major
-  const int64_t row = i / a.heads;
-  const int head = static_cast<int>(i - row * a.heads);
-  float s = 0.f;
-  if (row < a.total && lane * 8 < a.dim) {
-    float x[8], y[8];
-    load8(static_cast<const T*>(a.o.p) + row * a.o.ts + head * a.o.hs + lane * 8, x);
-    load8(static_cast<const T*>(a.dout.p) + row * a.dout.ts + head * a.dout.hs + lane * 8, y);
+  float s[EACH];
+  Index row[EACH];
+  int head[EACH];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
+  for (int u = 0; u < EACH; ++u) {
+    const Index i = (static_cast<Index>(blockIdx.x) * EACH + u) * kStep + threadIdx.x / LANES;   // token-major
+    row[u] = i / static_cast<Index>(a.heads);
+    head[u] = static_cast<int>(i - row[u] * a.heads);
+    s[u] = 0.f;
+    if (row[u] < a.total && lane * 8 < a.dim) {
+      float x[8], y[8];
+      load8(static_cast<const T*>(a.o.p) + row[u] * a.o.ts + head[u] * a.o.hs + lane * 8, x);
+      load8(static_cast<const T*>(a.dout.p) + row[u] * a.dout.ts + head[u] * a.dout.hs + lane * 8, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[u] = fmaf(x[e], y[e], s[u]);
+    }
   }
 #pragma unroll
-  for (int o = LANES / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (lane == 0 && row < a.total) a.delta[static_cast<int64_t>(head) * a.tokens + row] = s;
+  for (int u = 0; u < EACH; ++u) {
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) s[u] += __shfl_xor_sync(0xffffffffu, s[u], o);
+    if (lane == 0 && row[u] < a.total) a.delta[static_cast<int64_t>(head[u]) * a.tokens + row[u]] = s[u];
+  }
 }
 
 // `each`: CTAs for every 64 rows.
@@ -480,8 +493,8 @@ cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s) {
                      : run<k_attn_bwd<float, 128>>(a, each, bwd_smem<128>(), s);
 }
 
-// One CTA for 16 rows of a split key block and head: 16 lanes a row, eight
-// columns each.
+// One CTA for 16 rows of dk or dv of a split key block and head: 16 lanes a row,
+// eight columns each.  Bound by the latency of its few loads.
 template <typename T>
 static __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ AttnArgs a) {
   const int head = blockIdx.y, row = 16 * (blockIdx.x & 7) + threadIdx.x / 16, c = 8 * (threadIdx.x & 15);
@@ -494,38 +507,45 @@ static __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant_
     return;
   }
   if (c >= a.dim) return;
-  for (int which = 0; which < 2; ++which) {
-    float sum[8] = {};
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      float v[8];
-      load8(a.partial + (((static_cast<int64_t>(b.part + i) * a.kv_heads + head) * 2 + which) * 128 + row) * a.dim + c, v);
+  const int which = blockIdx.z;
+  float sum[8] = {};
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    float v[8];
+    load8(a.partial + (((static_cast<int64_t>(b.part + i) * a.kv_heads + head) * 2 + which) * 128 + row) * a.dim + c, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[e];
-    }
-    const AttnTensor& t = which ? a.dv : a.dk;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] *= which ? 1.f : a.scale;
-    store8(static_cast<T*>(t.p) + (static_cast<int64_t>(b.start) + 128 * b.blk + row) * t.ts + head * t.hs + c, sum);
+    for (int e = 0; e < 8; ++e) sum[e] += v[e];
   }
+  const AttnTensor& t = which ? a.dv : a.dk;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum[e] *= which ? 1.f : a.scale;
+  store8(static_cast<T*>(t.p) + (static_cast<int64_t>(b.start) + 128 * b.blk + row) * t.ts + head * t.hs + c, sum);
 }
 
 cudaError_t launch_attn_join(const AttnArgs& a, int dtype, cudaStream_t s) {
   if (!a.n_split) return cudaSuccess;
-  const dim3 grid(static_cast<unsigned>(8 * a.n_split), static_cast<unsigned>(a.kv_heads));
+  const dim3 grid(static_cast<unsigned>(8 * a.n_split), static_cast<unsigned>(a.kv_heads), 2);
   if (dtype == 0) k_attn_join<float><<<grid, 256, 0, s>>>(a);
   else k_attn_join<bf16><<<grid, 256, 0, s>>>(a);
   return cudaGetLastError();
 }
 
+template <typename T, int LANES>
+static cudaError_t delta(const AttnArgs& a, cudaStream_t s) {
+  const int64_t rows = static_cast<int64_t>(a.total) * a.heads, each = 256 / LANES;
+  if (!rows) return cudaSuccess;
+  const bool many = rows > 8 * each * device_sm_count();
+  const int64_t ctas = cdiv(rows, many ? 4 * each : each);
+  if (ctas >= (int64_t(1) << 31)) return cudaErrorInvalidConfiguration;
+  const unsigned grid = static_cast<unsigned>(ctas);
+  if (!many) k_attn_delta<T, LANES, 1, int><<<grid, 256, 0, s>>>(a);
+  else if (rows < (int64_t(1) << 30)) k_attn_delta<T, LANES, 4, int><<<grid, 256, 0, s>>>(a);
+  else k_attn_delta<T, LANES, 4, int64_t><<<grid, 256, 0, s>>>(a);
+  return cudaGetLastError();
+}
 template <typename T>
 static cudaError_t delta(const AttnArgs& a, cudaStream_t s) {
-  const int lanes = a.dim <= 64 ? 8 : 16;
-  const int64_t ctas = cdiv(static_cast<int64_t>(a.total) * a.heads, 256 / lanes);
-  if (!ctas) return cudaSuccess;
-  if (lanes == 8) k_attn_delta<T, 8><<<static_cast<unsigned>(ctas), 256, 0, s>>>(a);
-  else k_attn_delta<T, 16><<<static_cast<unsigned>(ctas), 256, 0, s>>>(a);
-  return cudaGetLastError();
+  return a.dim <= 64 ? delta<T, 8>(a, s) : delta<T, 16>(a, s);
 }
 
 cudaError_t launch_attn_delta(const AttnArgs& a, int dtype, cudaStream_t s) {
