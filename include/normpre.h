@@ -418,7 +418,8 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out);
  * first rows: j runs over the rows up to i with i - j < window or j < sinks (rows
  * counted from the sequence's first).  window = 0: all rows up to i, as
  * normpre_attn_init; sinks then change nothing.  All other calls are the same.
- * The work grows with window + sinks instead of the sequence's length.  A
+ * The work grows with window + sinks instead of the sequence's length; with sinks
+ * the plan's workspace has up to 64 MiB more.  A
  * non-finite value of token j reaches, besides the rows that see it, the rows of
  * every aligned block of 128 rows that has a row which sees one of j's block.
  * Errors: as normpre_attn_init; ARG for a negative window or sinks.

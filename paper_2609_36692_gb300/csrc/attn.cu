@@ -168,14 +168,21 @@ int check_call(const normpre_attn* a, int64_t tokens) {
   return NORMPRE_OK;
 }
 
-// Deals out the items of a kernel, given in falling order of cost (`per` items
-// for each entry of `costs`): each goes to the CTA with the least so far.
-void deal(const std::vector<int>& costs, int per, std::vector<int>* out) {
+// Deals out the items of a walk, given in falling order of cost (`per` items
+// for each entry of `costs`): each goes to the CTA with the least so far.  loads:
+// what the CTAs have already, a pair of load and CTA for each.
+typedef std::vector<std::pair<int64_t, int>> Loads;
+Loads no_loads(int grid) {
+  Loads loads;
+  for (int c = 0; c < grid; ++c) loads.push_back({0, c});
+  return loads;
+}
+void deal(const std::vector<int>& costs, int per, Loads* loads, std::vector<int>* out) {
   const int64_t items = static_cast<int64_t>(costs.size()) * per;
-  const int grid = walk_grid(items);
-  std::vector<std::pair<int64_t, int>> heap;                 // load, CTA; the least on top
-  for (int c = 0; c < grid; ++c) heap.push_back({0, c});
+  Loads& heap = *loads;                                      // the least on top
+  const int grid = static_cast<int>(heap.size());
   const auto more = std::greater<std::pair<int64_t, int>>();
+  std::make_heap(heap.begin(), heap.end(), more);
   std::vector<int> owner(items), count(grid + 1, 0);
   for (int64_t i = 0; i < items; ++i) {
     std::pop_heap(heap.begin(), heap.end(), more);
@@ -253,11 +260,18 @@ int set_lengths(normpre_attn* a, int n_seqs, const int64_t* lengths, cudaStream_
     const bool heads = attn_pair_heads(group);
     for (const AttnBlock& b : heads ? blocks : pairs)
       fwd.push_back(2 * keys(b, heads || (b.blk + 1) * 128 >= b.len ? b.blk : b.blk + 1) + 2);
-    for (const AttnBlock& b : by_key) dkdv.push_back(group * walked(b) + 1);
-    for (const AttnBlock& b : blocks) dq.push_back(keys(b, b.blk) + 1);
-    deal(fwd, heads ? h / 2 : h, &walk[0]);
-    deal(dkdv, hk, &walk[1]);
-    deal(dq, h, &walk[2]);
+    // four products a tile against three
+    for (const AttnBlock& b : by_key) dkdv.push_back(5 * (group * walked(b) + 1));
+    for (const AttnBlock& b : blocks) dq.push_back(4 * (keys(b, b.blk) + 1));
+    const int64_t of_fwd = static_cast<int64_t>(fwd.size()) * (heads ? h / 2 : h), of_keys = static_cast<int64_t>(by_key.size()) * hk;
+    const int64_t of_queries = n * h;
+    Loads loads = no_loads(walk_grid(of_fwd));
+    deal(fwd, heads ? h / 2 : h, &loads, &walk[0]);
+    // with a window the two walks of the backward pass are one launch
+    loads = no_loads(walk_grid(windowed ? std::max(of_keys, of_queries) : of_keys));
+    deal(dkdv, hk, &loads, &walk[1]);
+    if (!windowed) loads = no_loads(walk_grid(of_queries));
+    deal(dq, h, &loads, &walk[2]);
   }
   // one copy; the staging memory is free once the last one has left it, the
   // lists once the calls that read them are done

@@ -3,8 +3,8 @@
 //   P = exp2(log2(e) (scale S - lse)),  dS = P (dP - delta),  S = Q K^T, dP = dO V^T,
 //   dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K
 //
-// Two kernels: k_attn_dkdv owns 128 keys and walks the queries that see them
-// (over the heads of the group and the later blocks), k_attn_dq owns 128
+// Two walks: one (k_attn_dkdv) owns 128 keys and walks the queries that see them
+// (over the heads of the group and the later blocks), one (k_attn_dq) owns 128
 // queries and walks their keys.  Every gradient is then summed by one CTA in
 // one accumulator in a fixed order, without atomics or fp32 partials in global
 // memory; the price is that S and dP are formed twice, 7 products of a tile
@@ -46,6 +46,8 @@
 // / value heads the key blocks of a long sequence do not fill the GPU: one of 4096
 // tokens, 8 / 1 heads of 128, is 32 items of dK, dV, 0.45 ms (190 TFLOP/s of the
 // five products that are needed).
+#include <algorithm>
+
 #include "attn_tc.cuh"
 
 namespace normpre {
@@ -200,16 +202,17 @@ template <int kSlots> struct Warp {
   }
 };
 
-// The end of both kernels: copies in flight land, TMEM is freed.
+// The end of both walks: copies in flight land.  False if a wait gave up.
 template <int kSlots>
-__device__ __forceinline__ void finish(const Warp<kSlots>& w, int warp, int* flags) {
+__device__ __forceinline__ bool finish(const Warp<kSlots>& w, int* flags) {
   Bars<kSlots>* b = w.b;
   if (!w.ok && w.lane == 0) {
     *static_cast<volatile int*>(&b->abort) = 1;
     raise_host_flag(flags, kFlagTimeout);
   }
   __syncthreads();
-  if (threadIdx.x == 0 && *static_cast<volatile int*>(&b->abort)) {
+  const bool gave_up = *static_cast<volatile int*>(&b->abort);
+  if (threadIdx.x == 0 && gave_up) {
     int never = 0;
     for (int i = 0; i < kSlots; ++i) {
       if (b->issued[i]) tc::mbar_wait(&b->full[i], b->issued[i] - 1, &never);
@@ -219,9 +222,12 @@ __device__ __forceinline__ void finish(const Warp<kSlots>& w, int warp, int* fla
       if (b->own_issued[i >> 1]) tc::mbar_wait(&b->own_full[i >> 1][i & 1], (b->own_issued[i >> 1] - 1) & 1u, &never);
   }
   __syncthreads();
-  if (warp == kMmaA) {
+  return !gave_up;
+}
+__device__ __forceinline__ void free_tmem(uint32_t tmem) {
+  if (threadIdx.x >> 5 == kMmaA) {
     tc::fence_after();
-    tc::tmem_dealloc(b->tmem, 512);
+    tc::tmem_dealloc(tmem, 512);
   }
 }
 
@@ -298,12 +304,11 @@ __device__ __forceinline__ bool get_item(const ItemRef& b, Item& it) {
   return true;
 }
 
-// WIN: the rows have a window.
+// dK, dV.  WIN: the rows have a window.  Allocates all of TMEM.
 template <int DP, bool WIN>
-__global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_constant__ BwdArgs f) {
+__device__ __forceinline__ bool walk_dkdv(const BwdArgs& f, uint8_t* smem, uint32_t& tmem) {
   using B = Bwd<DP>;
   constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks, kSets = B::kSets;
-  extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* own = smem;                                // [kSets] K, V
   uint8_t* ring = own + 2 * kSets * kTileBytes;       // Q, dO, Q, dO ..
   float* stat = reinterpret_cast<float*>(ring + kSlots * kTileBytes);   // [2][-lse, delta][128]
@@ -328,7 +333,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
   }
   __syncthreads();
   tc::fence_after();
-  const uint32_t cS = b->tmem, cP = cS + 128, cAcc = cS + 256;     // per set: dV, dK
+  tmem = b->tmem;
+  const uint32_t cS = tmem, cP = cS + 128, cAcc = cS + 256;     // per set: dV, dK
   Warp<kSlots> w = {b, lane, true, 0, 0};
   Turn<kSets> set;
   KeyItem it;
@@ -565,15 +571,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_const
       w.arrive(&b->acc_empty[set.i]);
     }
   }
-  finish(w, warp, a.flags);
+  return finish(w, a.flags);
 }
 
-template <int DP, int KIND>
-__global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constant__ BwdArgs f) {
+// dQ.  FIRST: allocates TMEM, else `tmem` is its address.  Its barriers lie where
+// the other walk has its statistics: none of those that arrived there are touched.
+template <int DP, int KIND, bool FIRST>
+__device__ __forceinline__ void walk_dq(const BwdArgs& f, uint8_t* smem, uint32_t& tmem) {
   constexpr bool WIN = KIND != kWhole, kFew = KIND == kWindowNarrow;
   using B = Bwd<DP>;
   constexpr int kSlots = B::kSlots, kTileBytes = B::kTileBytes, kChunks = B::kChunks, kSets = B::kSets;
-  extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* own = smem;                                // [kSets] Q, dO
   uint8_t* ring = own + 2 * kSets * kTileBytes;       // K, V, K, V ..
   Bars<kSlots>* b = reinterpret_cast<Bars<kSlots>*>(ring + kSlots * kTileBytes);
@@ -587,14 +594,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
     for (const CUtensorMap* m : {&f.q, &f.k, &f.v, &f.dout}) tc::prefetch_map(m);
   }
   if (warp == 2) items[lane] = query_item(a, lane);
-  if (warp == kMmaA) {
+  if (FIRST && warp == kMmaA) {
     tc::tmem_alloc(&b->tmem, 512);
     tc::tmem_relinquish();
     tc::fence_before();
   }
   __syncthreads();
   tc::fence_after();
-  const uint32_t cS = b->tmem, cP = cS + 256, cAcc = cS + 384;    // S: two buffers; per set: dQ
+  if (FIRST) tmem = b->tmem;
+  const uint32_t cS = tmem, cP = cS + 256, cAcc = cS + 384;    // S: two buffers; per set: dQ
   Warp<kSlots> w = {b, lane, true, 0, 0};
   Turn<kSets> set;
   Turn<2> buf;                                                    // of S
@@ -765,7 +773,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constan
       w.arrive(&b->acc_empty[set.i]);
     }
   }
-  finish(w, warp, a.flags);
+  finish(w, a.flags);
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1) k_attn_dkdv_tc(const __grid_constant__ BwdArgs f) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint32_t tmem;
+  walk_dkdv<DP, false>(f, smem, tmem);
+  free_tmem(tmem);
+}
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1) k_attn_dq_tc(const __grid_constant__ BwdArgs f) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint32_t tmem;
+  walk_dq<DP, kWhole, true>(f, smem, tmem);
+  free_tmem(tmem);
+}
+
+// With a window both walks run in one launch, one after the other in each CTA and
+// dealt out together: items are short, so that a second launch's start and the
+// walks' uneven ends show.  (Without one the two launches of before remain.)
+template <int DP, int KIND>
+__global__ void __launch_bounds__(kThreads, 1) k_attn_bwd_tc(const __grid_constant__ BwdArgs f) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint32_t tmem;
+  if (walk_dkdv<DP, true>(f, smem, tmem)) {
+    // tiles whose tails were zeroed through the generic proxy are loaded over
+    tc::fence_smem_async();
+    __syncthreads();
+    walk_dq<DP, KIND, false>(f, smem, tmem);
+  }
+  free_tmem(tmem);
 }
 
 template <auto kernel>
@@ -776,10 +815,16 @@ cudaError_t launch(const BwdArgs& f, int64_t items, size_t smem, cudaStream_t s)
   return cudaGetLastError();
 }
 
-template <int DP, int KIND>
+template <int DP>
 cudaError_t both(const BwdArgs& f, cudaStream_t s) {
-  const cudaError_t e = launch<k_attn_dkdv_tc<DP, KIND != kWhole>>(f, static_cast<int64_t>(f.a.n_keys) * f.a.kv_heads, Bwd<DP>::kSmem, s);
-  return e ? e : launch<k_attn_dq_tc<DP, KIND>>(f, static_cast<int64_t>(f.a.n_blocks) * f.a.heads, Bwd<DP>::kSmem, s);
+  const int64_t by_key = static_cast<int64_t>(f.a.n_keys) * f.a.kv_heads, by_query = static_cast<int64_t>(f.a.n_blocks) * f.a.heads;
+  switch (window_kind(f.a)) {
+    case kWindow: return launch<k_attn_bwd_tc<DP, kWindow>>(f, std::max(by_key, by_query), Bwd<DP>::kSmem, s);
+    case kWindowNarrow: return launch<k_attn_bwd_tc<DP, kWindowNarrow>>(f, std::max(by_key, by_query), Bwd<DP>::kSmem, s);
+    default: break;
+  }
+  const cudaError_t e = launch<k_attn_dkdv_tc<DP>>(f, by_key, Bwd<DP>::kSmem, s);
+  return e ? e : launch<k_attn_dq_tc<DP>>(f, by_query, Bwd<DP>::kSmem, s);
 }
 
 }  // namespace
@@ -791,11 +836,7 @@ cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t s, std::stri
       !rows_map(&f.v, a.v, a.tokens, a.kv_heads, a.dim, err) ||
       !rows_map(&f.dout, a.dout, a.tokens, a.heads, a.dim, err))
     return cudaErrorInvalidValue;
-  switch (window_kind(a)) {
-    case kWindow: return a.dim <= 64 ? both<64, kWindow>(f, s) : both<128, kWindow>(f, s);
-    case kWindowNarrow: return a.dim <= 64 ? both<64, kWindowNarrow>(f, s) : both<128, kWindowNarrow>(f, s);
-    default: return a.dim <= 64 ? both<64, kWhole>(f, s) : both<128, kWhole>(f, s);
-  }
+  return a.dim <= 64 ? both<64>(f, s) : both<128>(f, s);
 }
 
 }  // namespace normpre

@@ -72,6 +72,24 @@ def _empty(shape, dtype, device: torch.device, stream) -> torch.Tensor:
     return x
 
 
+def _views(dtype: torch.dtype, dim: int, index: int, tokens: int, *views) -> array:
+    """Pointers and strides of (tensor, name, heads), each [tokens, heads, dim] on
+    device `index`, after checking them: an array of ``normpre_heads``."""
+    out = array("q")
+    for x, name, heads in views:
+        if x.get_device() != index or index < 0:
+            raise ValueError("%s must be on %s" % (name, "a CUDA device" if index < 0 else "cuda:%d" % index))
+        if x.dtype is not dtype:
+            raise TypeError("%s must be %s" % (name, dtype))
+        if x.shape != (tokens, heads, dim):
+            raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, tokens, heads, dim, tuple(x.shape)))
+        st, sh, sd = x.stride()
+        if sd != 1 and tokens:
+            raise ValueError("%s: the last dimension must be contiguous" % name)
+        out.extend((x.data_ptr(), st, sh))
+    return out
+
+
 # ---------------------------------------------------------------------------
 # packed causal attention
 # ---------------------------------------------------------------------------
@@ -90,6 +108,9 @@ class PackedAttention:
     With ``window``, a row sees the ``window`` rows up to itself and, with
     ``sinks``, its sequence's first ``sinks`` rows however far they are; 0: all
     rows up to itself.
+
+    A plan has one workspace for its backward passes: they run one after the
+    other, in whatever streams and graphs they are.
 
     With `stream`, a call's work runs there instead of on the current stream;
     the caller orders it after what wrote its inputs and lengths, and before
@@ -116,62 +137,43 @@ class PackedAttention:
             C.normpre_attn_set_lengths(self.plan, lengths, s.cuda_stream)
         self.lengths = lengths
 
-    def _check(self, x: torch.Tensor, name: str, tokens: int, heads: int):
-        if x.device != self.device:
-            raise ValueError("%s must be on %s" % (name, self.device))
-        if x.dtype != self.dtype:
-            raise TypeError("%s must be %s" % (name, self.dtype))
-        if x.shape != (tokens, heads, self.head_dim):
-            raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, tokens, heads, self.head_dim, tuple(x.shape)))
-        st, sh, sd = x.stride()
-        if sd != 1 and tokens:
-            raise ValueError("%s: the last dimension must be contiguous" % name)
-        return x.data_ptr(), st, sh
-
     def _lse(self, lse: torch.Tensor, tokens: int) -> int:
-        if lse.device != self.device or lse.dtype != torch.float32 or not lse.is_contiguous() or \
+        if lse.get_device() != self.device.index or lse.dtype is not torch.float32 or not lse.is_contiguous() or \
                 lse.shape != (self.n_heads, tokens):
             raise ValueError("lse must be a contiguous float32 [%d, %d] tensor on %s" % (self.n_heads, tokens, self.device))
         return lse.data_ptr()
 
-    def _new(self, tokens: int, heads: int, stream):
-        return _empty((tokens, heads, self.head_dim), self.dtype, self.device, stream)
-
     def forward(self, q, k, v, out=None, lse=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """(out, lse): [tokens, n_heads, head_dim] and the fp32 log-sums
         [n_heads, tokens] that ``backward`` reads."""
-        t, h, hk = q.shape[0], self.n_heads, self.n_kv_heads
-        check = self._check
-        args = (*check(q, "q", t, h), *check(k, "k", t, hk), *check(v, "v", t, hk))
+        t, h, hk, d, index = q.shape[0], self.n_heads, self.n_kv_heads, self.head_dim, self.device.index
+        views = _views(self.dtype, d, index, t, (q, "q", h), (k, "k", hk), (v, "v", hk))
         _used_on(stream, q, k, v, out, lse)
         if out is None:
-            out = self._new(t, h, stream)
+            out = _empty((t, h, d), self.dtype, self.device, stream)
         if lse is None:
             lse = _empty((h, t), torch.float32, self.device, stream)
-        heads = (ctypes.c_int64 * 12)(*args, *check(out, "out", t, h))
-        at = ctypes.addressof(heads)
+        views += _views(self.dtype, d, index, t, (out, "out", h))
+        at = views.buffer_info()[0]
         C.normpre_attn_forward(self.plan, t, at, at + 24, at + 48, at + 72, self._lse(lse, t),
-                               _current_stream(self.device.index) if stream is None else stream.cuda_stream)
+                               _current_stream(index) if stream is None else stream.cuda_stream)
         return out, lse
 
     def backward(self, q, k, v, out, lse, dout, dq=None, dk=None, dv=None, stream=None):
         """(dq, dk, dv) for the forward pass that gave ``out`` and ``lse``."""
-        t, h, hk = q.shape[0], self.n_heads, self.n_kv_heads
-        check = self._check
-        args = (*check(q, "q", t, h), *check(k, "k", t, hk), *check(v, "v", t, hk), *check(out, "out", t, h),
-                *check(dout, "dout", t, h))
+        t, h, hk, d, index = q.shape[0], self.n_heads, self.n_kv_heads, self.head_dim, self.device.index
+        views = _views(self.dtype, d, index, t, (q, "q", h), (k, "k", hk), (v, "v", hk), (out, "out", h), (dout, "dout", h))
         _used_on(stream, q, k, v, out, lse, dout, dq, dk, dv)
         if dq is None:
-            dq = self._new(t, h, stream)
+            dq = _empty((t, h, d), self.dtype, self.device, stream)
         if dk is None:
-            dk = self._new(t, hk, stream)
+            dk = _empty((t, hk, d), self.dtype, self.device, stream)
         if dv is None:
-            dv = self._new(t, hk, stream)
-        heads = (ctypes.c_int64 * 24)(*args, *check(dq, "dq", t, h), *check(dk, "dk", t, hk), *check(dv, "dv", t, hk))
-        at = ctypes.addressof(heads)
+            dv = _empty((t, hk, d), self.dtype, self.device, stream)
+        views += _views(self.dtype, d, index, t, (dq, "dq", h), (dk, "dk", hk), (dv, "dv", hk))
+        at = views.buffer_info()[0]
         C.normpre_attn_backward(self.plan, t, at, at + 24, at + 48, at + 72, self._lse(lse, t), at + 96, at + 120,
-                                at + 144, at + 168,
-                                _current_stream(self.device.index) if stream is None else stream.cuda_stream)
+                                at + 144, at + 168, _current_stream(index) if stream is None else stream.cuda_stream)
         return dq, dk, dv
 
     def __call__(self, q, k, v) -> torch.Tensor:
@@ -264,23 +266,6 @@ class QKNormRotary:
         self.plan = C.normpre_qkrot_init(cfg, frequencies)
         self._bytes = C.normpre_qkrot_bytes(self.plan)
 
-    def _views(self, index: int, tokens: int, *views) -> array:
-        """Pointers and strides of (tensor, name, heads) after checking them."""
-        dtype, d = self.dtype, self.head_dim
-        out = array("q")
-        for x, name, heads in views:
-            if x.get_device() != index or index < 0:
-                raise ValueError("%s must be on %s" % (name, "a CUDA device" if index < 0 else "cuda:%d" % index))
-            if x.dtype is not dtype:
-                raise TypeError("%s must be %s" % (name, dtype))
-            if x.shape != (tokens, heads, d):
-                raise ValueError("%s must be [%d, %d, %d] (got %s)" % (name, tokens, heads, d, tuple(x.shape)))
-            st, sh, sd = x.stride()
-            if sd != 1 and tokens:
-                raise ValueError("%s: the last dimension must be contiguous" % name)
-            out.extend((x.data_ptr(), st, sh))
-        return out
-
     def _rest(self, positions, q_weight, k_weight, tokens, index):
         """Positions' pointer and bytes, weights' pointers and dtype code."""
         at, size = 0, 8
@@ -310,14 +295,14 @@ class QKNormRotary:
                 used: Optional[int] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """The normed and rotated (q, k).  An output may be its input itself."""
         t, h, hk, index = q.shape[0], self.n_heads, self.n_kv_heads, q.get_device()
-        views = self._views(index, t, (q, "q", h), (k, "k", hk))
+        views = _views(self.dtype, self.head_dim, index, t, (q, "q", h), (k, "k", hk))
         rest = self._rest(positions, q_weight, k_weight, t, index)
         _used_on(stream, q, k, positions, q_weight, k_weight, q_out, k_out)
         if q_out is None:
             q_out = _empty((t, h, self.head_dim), self.dtype, q.device, stream)
         if k_out is None:
             k_out = _empty((t, hk, self.head_dim), self.dtype, q.device, stream)
-        views += self._views(index, t, (q_out, "q_out", h), (k_out, "k_out", hk))
+        views += _views(self.dtype, self.head_dim, index, t, (q_out, "q_out", h), (k_out, "k_out", hk))
         at = views.buffer_info()[0]
         _on_index(index, C.normpre_qkrot_forward, self.plan, t, t if used is None else used, at, at + 24, *rest, at + 48,
                   at + 72, stream=stream)
@@ -329,7 +314,7 @@ class QKNormRotary:
         results.  A weight that is None has no gradient (None); with ``weights``
         False neither has."""
         t, h, hk, index = q.shape[0], self.n_heads, self.n_kv_heads, q.get_device()
-        views = self._views(index, t, (q, "q", h), (k, "k", hk), (dq_out, "dq_out", h), (dk_out, "dk_out", hk))
+        views = _views(self.dtype, self.head_dim, index, t, (q, "q", h), (k, "k", hk), (dq_out, "dq_out", h), (dk_out, "dk_out", hk))
         rest = self._rest(positions, q_weight, k_weight, t, index)
         _used_on(stream, q, k, positions, dq_out, dk_out, q_weight, k_weight, dq, dk)
         device = q.device
@@ -337,7 +322,7 @@ class QKNormRotary:
             dq = _empty((t, h, self.head_dim), self.dtype, device, stream)
         if dk is None:
             dk = _empty((t, hk, self.head_dim), self.dtype, device, stream)
-        views += self._views(index, t, (dq, "dq", h), (dk, "dk", hk))
+        views += _views(self.dtype, self.head_dim, index, t, (dq, "dq", h), (dk, "dk", hk))
         dqw = dkw = None
         to_q = to_k = work = 0
         if weights and (q_weight is not None or k_weight is not None):
