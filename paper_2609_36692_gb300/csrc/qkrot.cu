@@ -276,12 +276,7 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
   }
   __syncthreads();
   auto weights = [&](int e) { return reinterpret_cast<const uint64_t*>(sw)[4 * u + e]; };
-  uint64_t wt[4], dw[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    wt[e] = BWD ? weights(e) : 0;
-    dw[e] = 0;
-  }
+  uint64_t dw[4] = {0, 0, 0, 0};
 
   // the unit on its way: its place, values and position
   const bool want_x = !BWD || g.norm;
@@ -440,6 +435,12 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
     } else {
       float sum[2 * H], r[H], m[H];
       bool fits = true;
+      // the weights are fetched each time: held, they take registers that the next
+      // unit's values need
+      uint64_t wt[4];
+      const uint32_t wa = tc::su32(sw + 8 * u);
+      asm volatile("ld.shared.v2.b64 {%0, %1}, [%4];\n\tld.shared.v2.b64 {%2, %3}, [%4 + 16];"
+                   : "=l"(wt[0]), "=l"(wt[1]), "=l"(wt[2]), "=l"(wt[3]) : "r"(wa));
       auto slope = [&](int i) {                 // <u, x>
         uint64_t v[4];
 #pragma unroll
