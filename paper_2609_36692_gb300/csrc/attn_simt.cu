@@ -25,7 +25,8 @@
 // where the longest CTAs pass ten tiles of 8200 FMA cycles each, two CTAs an SM.
 // 8 x 1024 tokens: 0.39 ms (33 TFLOP/s) and 1.27 ms (25).  With a window of 100 and
 // 3 sinks the three sequences take 0.088 ms backward: 64 x 64 tiles of which 45 % is
-// visible, 576 CTAs of three or four tiles in two rounds.
+// visible, 600 CTAs of two to four tiles in two rounds.  Sinks take a fourth of a
+// tile's products where 16 keys or fewer are visible (forward, 2000 tokens 63 -> 55 us).
 #include <type_traits>
 
 #include "attn.h"
@@ -42,6 +43,10 @@ constexpr int kPs = kB + 4;         // row stride of a score tile
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <int DP> __host__ __device__ constexpr int ld() { return DP + 4; }
+
+// Groups of 16 keys of a tile: four, or one where no more than 16 are visible, as
+// sinks.
+template <int N> using Groups = std::integral_constant<int, N>;
 
 // 64 rows from `row0` of a head into shared memory; rows at or past `rows` and
 // columns at or past `dim` are zero.
@@ -85,8 +90,8 @@ __device__ __forceinline__ void load_tiles(float* dst0, const AttnTensor& t0, fl
   y.put(dst1);
 }
 
-// s[r][c] = <A row ty + 16 r, B row tx + 16 c>
-template <int DP>
+// s[r][c] = <A row ty + 16 r, B row tx + 16 c>, of the first 16 NC rows of B
+template <int DP, int NC = 4>
 __device__ __forceinline__ void scores(const float* A, const float* B, int ty, int tx, float (&s)[4][4]) {
 #pragma unroll
   for (int r = 0; r < 4; ++r)
@@ -94,16 +99,16 @@ __device__ __forceinline__ void scores(const float* A, const float* B, int ty, i
     for (int c = 0; c < 4; ++c) s[r][c] = 0.f;
 #pragma unroll 4
   for (int d = 0; d < DP; d += 4) {
-    float4 a[4], b[4];
+    float4 a[4], b[NC];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       a[i] = *reinterpret_cast<const float4*>(A + (ty + 16 * i) * ld<DP>() + d);
-      b[i] = *reinterpret_cast<const float4*>(B + (tx + 16 * i) * ld<DP>() + d);
+      if (i < NC) b[i] = *reinterpret_cast<const float4*>(B + (tx + 16 * i) * ld<DP>() + d);
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < NC; ++c) {
         s[r][c] = fmaf(a[r].x, b[c].x, s[r][c]);
         s[r][c] = fmaf(a[r].y, b[c].y, s[r][c]);
         s[r][c] = fmaf(a[r].z, b[c].z, s[r][c]);
@@ -112,11 +117,11 @@ __device__ __forceinline__ void scores(const float* A, const float* B, int ty, i
   }
 }
 
-// acc[r] (row ty + 16 r, columns 4 tx + 64 k ..) += sum_j P[ty + 16 r][j] V[j][...]
-template <int DP>
+// acc[r] (row ty + 16 r, columns 4 tx + 64 k ..) += sum_j P[ty + 16 r][j] V[j][...], j < 16 NC
+template <int DP, int NC = 4>
 __device__ __forceinline__ void accumulate(const float* P, const float* V, int ty, int tx, float4 (&acc)[4][DP / 64]) {
 #pragma unroll 2
-  for (int j = 0; j < kB; j += 4) {
+  for (int j = 0; j < 16 * NC; j += 4) {
     float4 p[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r] = *reinterpret_cast<const float4*>(P + (ty + 16 * r) * kPs + j);
@@ -222,13 +227,15 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
     for (int k = 0; k < DP / 64; ++k) acc[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   const int diag = w.first / kB, lo = max(0, w.first - a.window + 1) / kB, sink = min(lo, (a.sinks + kB - 1) / kB);
-  for (int jb = diag; jb >= 0; jb = jb > lo || jb <= sink ? jb - 1 : sink - 1) {
-    const int krows = min(kB, w.len - jb * kB);
+  // keys of a tile, NC groups of 16
+  auto tile = [&](int jb, auto groups) {
+    constexpr int NC = decltype(groups)::value;
+    const int krows = min(16 * NC, w.len - jb * kB);
     __syncthreads();
     load_tile<T, DP>(KV, a.k, w.seq + jb * kB, krows, kvh, a.dim);
     __syncthreads();
     float s[4][4];
-    scores<DP>(Q, KV, ty, tx, s);
+    scores<DP, NC>(Q, KV, ty, tx, s);
     const int up = kB * (diag - jb);
     auto hidden = [&](int r, int c) {
       const int far = up + ty + 16 * r - tx - 16 * c;        // rows between the two
@@ -238,7 +245,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
     for (int r = 0; r < 4; ++r) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < NC; ++c) {
         s[r][c] = hidden(r, c) ? -INFINITY : s[r][c] * a.scale;
         mx = fmaxf(mx, s[r][c]);
       }
@@ -248,7 +255,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
       const float keep = exp2f((m[r] - mx) * kLog2e);
       float sum = 0.f;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < NC; ++c) {
         const float p = hidden(r, c) ? 0.f : exp2f((s[r][c] - mx) * kLog2e);
         P[(ty + 16 * r) * kPs + tx + 16 * c] = p;
         sum += p;
@@ -265,7 +272,11 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
     __syncthreads();
     load_tile<T, DP>(KV, a.v, w.seq + jb * kB, krows, kvh, a.dim);
     __syncthreads();
-    accumulate<DP>(P, KV, ty, tx, acc);
+    accumulate<DP, NC>(P, KV, ty, tx, acc);
+  };
+  for (int jb = diag; jb >= 0; jb = jb > lo || jb <= sink ? jb - 1 : sink - 1) {
+    if (jb < sink && a.sinks - jb * kB <= 16) tile(jb, Groups<1>());
+    else tile(jb, Groups<4>());
   }
   float inv[4];
 #pragma unroll
@@ -279,19 +290,19 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
 // P and dS of query rows i0 .. and key rows j0 .. of a sequence, from tiles in
 // shared memory; zero where i < j or past the sequence's end.  s holds
 // ds / c on return, p the probabilities.
-template <int DP>
+template <int DP, int NC = 4>
 __device__ __forceinline__ void grad_scores(const AttnArgs& a, const float* Q, const float* K, const float* dO,
                                             const float* V, const float* lse, const float* delta, int i0, int j0,
                                             int len, int ty, int tx, float (&p)[4][4], float (&s)[4][4]) {
   float t[4][4];
-  scores<DP>(Q, K, ty, tx, t);
-  scores<DP>(dO, V, ty, tx, s);
+  scores<DP, NC>(Q, K, ty, tx, t);
+  scores<DP, NC>(dO, V, ty, tx, s);
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int i = i0 + ty + 16 * r;
     const float ls = lse[ty + 16 * r], de = delta[ty + 16 * r];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < NC; ++c) {
       const int j = j0 + tx + 16 * c;
       const bool seen = i < len && j <= i && (i - j < a.window || j < a.sinks);
       p[r][c] = seen ? exp2f(fmaf(t[r][c], a.scale, -ls) * kLog2e) : 0.f;
@@ -403,19 +414,24 @@ __device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, i
 #pragma unroll
     for (int k = 0; k < DP / 64; ++k) dq[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
   const int lo = max(0, w.first - a.window + 1) / kB * kB, sink = min(lo, (a.sinks + kB - 1) / kB * kB);
-  for (int j0 = sink ? 0 : lo; j0 <= w.first; j0 = j0 + kB == sink ? lo : j0 + kB) {
-    const int krows = min(kB, w.len - j0);
+  auto tile = [&](int j0, auto groups) {
+    constexpr int NC = decltype(groups)::value;
+    const int krows = min(16 * NC, w.len - j0);
     __syncthreads();
     load_tiles<T, DP>(K, a.k, V, a.v, w.seq + j0, krows, kvh, a.dim);
     __syncthreads();
     float p[4][4], s[4][4];
-    grad_scores<DP>(a, Q, K, dO, V, lse, delta, w.first, j0, w.len, ty, tx, p, s);
+    grad_scores<DP, NC>(a, Q, K, dO, V, lse, delta, w.first, j0, w.len, ty, tx, p, s);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) S[(ty + 16 * r) * kPs + tx + 16 * c] = s[r][c];
+      for (int c = 0; c < NC; ++c) S[(ty + 16 * r) * kPs + tx + 16 * c] = s[r][c];
     __syncthreads();
-    accumulate<DP>(S, K, ty, tx, dq);
+    accumulate<DP, NC>(S, K, ty, tx, dq);
+  };
+  for (int j0 = sink ? 0 : lo; j0 <= w.first; j0 = j0 + kB == sink ? lo : j0 + kB) {
+    if (j0 < sink && a.sinks - j0 <= 16) tile(j0, Groups<1>());
+    else tile(j0, Groups<4>());
   }
   const float c[4] = {a.scale, a.scale, a.scale, a.scale};
   store_tile<T, DP>(a.dq, row0, rows, head, a.dim, ty, tx, dq, c);
@@ -502,7 +518,7 @@ static __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant_
   const int head = blockIdx.y, row = 16 * (blockIdx.x & 7) + threadIdx.x / 16, c = 8 * (threadIdx.x & 15);
   const AttnBlock b = a.by_split[blockIdx.x >> 3];
   int n = 0;
-  if (block_fits(b, a.total) && 128 * b.blk + 128 <= b.len)
+  if (block_fits(b, a.total) && 128 * b.blk + 128 <= b.len && a.chunk > 0)
     n = key_parts(last_query(b.blk, b.len, a.window, a.sinks) - b.blk + 1, a.chunk);
   if (n < 2 || b.part < 0 || n > a.slots - b.part) {
     if (threadIdx.x == 0) raise_host_flag(a.flags, kFlagLists);
