@@ -15,8 +15,8 @@
 // 42 us and 66 (45 and 69 with the launch, 4.4 TB/s).  More warps have fewer
 // registers: with four CTAs an SM instead of three, or heads one by one, 51 to 70.
 //
-// A lane holds four pairs of a row (8 values), (bf16: of two heads at once): with them
-// the pairs' cos and sin, which it forms once per token and uses for all of its
+// A lane holds four pairs of a row (8 values), in bf16 of two heads at once, and with
+// them the pairs' cos and sin, which it forms once per token and uses for all of its
 // heads; 1 to 32 lanes share a row, and all sums of a unit travel through the
 // lanes together.  Half-split pairs (i, i + R/2) are two runs of up to
 // four values, read V at a time (V: the largest of 4, 2, 1 that divides R/2, so
@@ -211,6 +211,14 @@ __device__ __forceinline__ float dot(const uint64_t (&x)[4], const uint64_t (&y)
   tc::unpack2(sum, lo, hi);
   return lo + hi;
 }
+// The same of x with itself, scaled first.
+__device__ __forceinline__ float squares(const uint64_t (&x)[4], float f) {
+  uint64_t v[4];
+  const uint64_t f2 = tc::pack2(f, f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = tc::mul2(x[e], f2);
+  return dot(v, v);
+}
 __device__ __forceinline__ void scale(uint64_t (&x)[4], float f) {
   const uint64_t f2 = tc::pack2(f, f);
 #pragma unroll
@@ -402,39 +410,47 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
         }
       }
     } else if constexpr (!BWD) {
-      float sum[H], r[H], mine = 0.f;
-      bool fits = true;
-#pragma unroll
-      for (int i = 0; i < H; ++i) sum[i] = dot(x[i], x[i]);
+      // 1 / root mean square of the rows; `down`: by how much they are scaled for it
+      float sum[H], down[H], r[H];
       const bool split = H == 2 && g.lanes > 1;
-      if (split) {
-        mine = split_sum(sum[0], sum[H - 1], g.lanes, upper);
-        fits = mine < kLargeSum;
-      } else {
-        row_sums(sum, g.lanes);
+      auto roots = [&](bool scaled) {
 #pragma unroll
-        for (int i = 0; i < H; ++i) fits = fits && sum[i] < kLargeSum;
-      }
-      if (__any_sync(0xffffffffu, !fits)) {
-        if (split) row_sums(sum, g.lanes);
+        for (int i = 0; i < H; ++i) sum[i] = scaled ? squares(x[i], down[i]) : dot(x[i], x[i]);
+        if (split) {
+          if constexpr (H == 2) {
+            const float mine = split_sum(sum[0], sum[1], g.lanes, upper), d = upper ? down[1] : down[0];
+            join_halves(inverse_root(mine, g, g.eps * d * d), g.lanes, upper, r);
+            return mine < kLargeSum;
+          }
+        }
+        row_sums(sum, g.lanes);
+        bool fits = true;
 #pragma unroll
         for (int i = 0; i < H; ++i) {
-          const float down = sum[i] < kLargeSum ? 1.f : kDown;
-          scale(x[i], down);
-          float again[1] = {dot(x[i], x[i])};
-          row_sums(again, g.lanes);
-          r[i] = inverse_root(again[0], g, g.eps * down * down);
+          r[i] = inverse_root(sum[i], g, g.eps * down[i] * down[i]);
+          fits = fits && sum[i] < kLargeSum;
         }
-      } else if (split) {
-        if constexpr (H == 2) join_halves(inverse_root(mine, g, g.eps), g.lanes, upper, r);
-      } else {
+        return fits;
+      };
 #pragma unroll
-        for (int i = 0; i < H; ++i) r[i] = inverse_root(sum[i], g, g.eps);
+      for (int i = 0; i < H; ++i) down[i] = 1.f;
+      if (__any_sync(0xffffffffu, !roots(false))) {
+        // once more, the large rows scaled (small values of theirs only after their
+        // root has raised them); the others come out as they were
+        if (split) row_sums(sum, g.lanes);
+#pragma unroll
+        for (int i = 0; i < H; ++i) down[i] = sum[i] < 0.5f * kLargeSum ? 1.f : kDown;
+        roots(true);
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          scale(x[i], r[i]);
+          r[i] = down[i];
+        }
       }
 #pragma unroll
       for (int i = 0; i < H; ++i) {
-        turn(x[i]);
         scale(x[i], r[i]);
+        turn(x[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[i][e] = x[i][e];
       }
@@ -463,18 +479,20 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
 #pragma unroll
       for (int i = 0; i < H; ++i) fits = fits && sum[i] < kLargeSum && fabsf(sum[H + i]) < INFINITY;
       if (__any_sync(0xffffffffu, !fits)) {
-        // <u, x> may be out of range with x: from xh instead
+        // <u, x> may be out of range with x: from xh instead; rows that are in range
+        // come out as they would have
 #pragma unroll
         for (int i = 0; i < H; ++i) {
           const float down = sum[i] < kLargeSum ? 1.f : kDown;
-          scale(x[i], down);
-          float again[1] = {dot(x[i], x[i])};
+          const bool in = sum[i] < kLargeSum && fabsf(sum[H + i]) < INFINITY;
+          float again[1] = {squares(x[i], down)};
           row_sums(again, g.lanes);
           r[i] = inverse_root(again[0], g, g.eps * down * down);
           scale(x[i], r[i]);
+          scale(x[i], down);
           again[0] = slope(i);
           row_sums(again, g.lanes);
-          m[i] = again[0] * g.inv_dim;
+          m[i] = in ? sum[H + i] * g.inv_dim * r[i] : again[0] * g.inv_dim;
           r[i] *= down;
         }
       } else {

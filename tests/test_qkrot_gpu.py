@@ -198,11 +198,31 @@ def test_rows_of_any_size(size, dtype):
     within(dqw, ref[4], ref[5], 60)
 
 
-@pytest.mark.parametrize("bad", [math.nan, math.inf])
-def test_what_is_not_finite_stays_in_its_row(bad):
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_small_values_beside_large_ones(dtype):
+    """A row of values from 1e-20 to 1e25: each to its own size."""
     import torch
-    s = make(4, 40, 4, 2, 64, "bf16")
-    plan = plan_for(4, 2, 64, "bf16", 32, False)
+    s = make(13, 33, 4, 2, 128, dtype)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    size = 10.0 ** (-20 + 45 * torch.rand(33, 4, 1, 128, generator=g, device="cuda"))
+    size = torch.cat([size, size], 2).reshape(33, 4, 256)[..., ::2]
+    s["q"].copy_((s["q"].float() * size).to(s["q"].dtype))
+    plan = plan_for(4, 2, 128, dtype, 64, True)
+    q, _ = plan.forward(s["q"], s["k"], s["positions"], s["qw"], s["kw"])
+    dq, _, dqw, _ = plan.backward(s["q"], s["k"], s["positions"], s["dq"], s["dk"], s["qw"], s["kw"])
+    ref = reference(s["q"], s["qw"], s["positions"], s["dq"], 64, True)
+    within(q, ref[0], ref[1], 21)
+    within(dq, ref[2], ref[3], 75)
+    within(dqw, ref[4], ref[5], 60)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, 1e30])
+def test_what_is_not_finite_stays_in_its_row(bad, dtype):
+    """Nothing of a row, large ones included, changes a bit of the others."""
+    import torch
+    s = make(4, 40, 4, 2, 64, dtype)
+    plan = plan_for(4, 2, 64, dtype, 32, False)
     args = s["positions"], s["qw"], s["kw"]
     q, k = plan.forward(s["q"], s["k"], *args)
     dq, dk = plan.backward(s["q"], s["k"], s["positions"], s["dq"], s["dk"], s["qw"], s["kw"])[:2]
@@ -212,10 +232,10 @@ def test_what_is_not_finite_stays_in_its_row(bad):
     rest[17, 2] = False
     got = plan.forward(q2, s["k"], *args)
     assert torch.equal(got[0][rest], q[rest]) and torch.equal(got[1], k)
-    assert bool(torch.isnan(got[0][17, 2, 5]))
+    assert bool(torch.isnan(got[0][17, 2, 5])) or bad == 1e30
     got = plan.backward(q2, s["k"], s["positions"], s["dq"], s["dk"], s["qw"], s["kw"])
     assert torch.equal(got[0][rest], dq[rest]) and torch.equal(got[1], dk)
-    assert bool(torch.isnan(got[2][5]))
+    assert bool(torch.isnan(got[2][5])) or bad == 1e30
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
