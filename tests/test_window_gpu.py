@@ -104,7 +104,8 @@ def test_long(window, sinks, dtype):
     """Many more blocks than the window has, so that the sinks' gradients come
     from parts of the queries; the same bits again."""
     import torch
-    for layout, lengths in (((2, 1, 64), [5000, 37]), ((1, 1, 128), [4100]), ((4, 2, 24), [2000, 1999, 1100])):
+    for layout, lengths in (((2, 1, 64), [5000, 37]), ((1, 1, 128), [4100]), ((4, 2, 24), [2000, 1999, 1100]),
+                            ((8, 1, 128), [2600, 300])):
         plan, (q, k, v, do), (out, lse, *grads) = check(layout, lengths, window, sinks, dtype)
         for a, b in zip(plan.backward(q, k, v, out, lse, do), grads):
             assert torch.equal(a, b)
@@ -226,11 +227,12 @@ def test_sharp_scores(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_layouts_streams_and_capture(dtype):
+@pytest.mark.parametrize("lengths, window", [([650, 33, 200], 150), ([3000, 33], 60)], ids=str)   # the latter's sinks in parts
+def test_layouts_streams_and_capture(lengths, window, dtype):
     import torch
-    h, hk, d, lengths = 4, 2, 64, [650, 33, 200]
-    q, k, v, do = make(10, 890, h, hk, d, dtype)
-    plan = plan_for(h, hk, d, 890, lengths, dtype, window=150, sinks=4)
+    h, hk, d, n = 4, 2, 64, sum(lengths) + 7
+    q, k, v, do = make(10, n, h, hk, d, dtype)
+    plan = plan_for(h, hk, d, n, lengths, dtype, window=window, sinks=4)
     c = [x.contiguous() for x in (q, k, v, do)]
     out, lse = plan.forward(*c[:3])
     want = (out, lse, *plan.backward(*c[:3], out, lse, c[3]))
@@ -252,7 +254,7 @@ def test_layouts_streams_and_capture(dtype):
     for outs in got:
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
     # other lengths, and these again: nothing of the others is left
-    for other in ([890], [10] * 3, []):
+    for other in ([n], [10] * len(lengths), []):
         plan.set_lengths(other)
         calls(c)
         plan.set_lengths(lengths)
