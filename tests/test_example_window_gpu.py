@@ -82,3 +82,44 @@ def test_one_step_against_plain_torch(window, sinks):
     assert abs(float(clip_grad_norm_(model.parameters(), 0.5 * norm)) - norm) < 1e-5 * norm
     for name, p in model.named_parameters():
         assert float((p.grad - 0.5 * got[name]).abs().max()) <= 1e-5 * float(got[name].abs().max())
+
+
+def test_together_in_a_graph():
+    """Norms with rotation, windowed attention, their gradients and clipping in one
+    captured step: the bits of the calls one by one, replay after replay."""
+    import torch
+    from paper_2609_36692_gb300 import layers, optim
+    torch.manual_seed(0)
+    t, h, hk, d = 300, 4, 2, 64
+    x = torch.randn(t, h + 2 * hk, d, device="cuda").bfloat16().requires_grad_()
+    qw, kw = (torch.ones(d, device="cuda", requires_grad=True) for _ in range(2))
+    places, dout = torch.arange(t, device="cuda"), torch.randn(t, h, d, device="cuda").bfloat16()
+    rotary = layers.QKNormRotary(h, hk, d)
+    attention = layers.PackedAttention(h, hk, d, t, 4, window=40, sinks=3)
+    attention.set_lengths([200, 90])
+
+    def step():
+        q, k = rotary(x[:, :h], x[:, h:h + hk], places, qw, kw, used=290)
+        out = attention(q, k, x[:, h + hk:])
+        grads = torch.autograd.grad(out, (x, qw, kw), dout)
+        clipped = [torch.empty_like(g) for g in grads]
+        norm = optim.clip_grads(grads, 1.0, out=clipped)
+        return [out.detach(), norm, *clipped]
+    want = step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(2):
+        for y in got:
+            y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert attention.status() == 0
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
