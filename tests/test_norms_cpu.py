@@ -130,6 +130,28 @@ int main() {
           for (int i = b; i < n; ++i)
             if (meets(i, b, 1 << 20, w, s)) last = i;
           bad += last_query(b, len, w, s) != last;
+          // the parts of its queries follow one another, from its own block to the last
+          AttnBlock e = {0, len, b, 0};
+          const KeyPart whole = key_part(e, w, s, 3, 0);
+          bad += whole.slot != -1 || !whole.fits || whole.first != b || whole.end != last + 1;
+          for (int chunk : {1, 2, 3, 8}) {
+            const int parts = key_parts(last - b + 1, chunk);
+            for (int i = 0, at = b; i < parts; ++i) {
+              e.part = i << 12 | (i + 6);
+              const KeyPart k = key_part(e, w, s, chunk, 100);
+              bad += !k.fits || k.slot != i + 5 || k.first != at || k.end <= k.first || k.end - k.first > chunk;
+              at = k.end;
+              bad += i + 1 == parts && at != last + 1;
+            }
+            e.part = parts << 12 | 1;                       // what is not of the call is known as such
+            bad += key_part(e, w, s, chunk, 100).fits;
+            e.part = 0 << 12 | 101;
+            bad += key_part(e, w, s, chunk, 100).fits;
+          }
+          e.part = 1;
+          bad += key_part(e, w, s, 0, 100).fits;
+          e.part = -1;
+          bad += key_part(e, w, s, 2, 100).fits;
         }
   std::printf("%d\n", bad);
 }
