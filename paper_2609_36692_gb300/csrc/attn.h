@@ -122,10 +122,11 @@ struct AttnArgs {
 inline bool attn_pair_heads(int group) { return group % 2 == 0; }
 
 // Kinds of tensor-core kernels: no window; one; one whose narrow sink block (see
-// KeySpan::narrow) has a path of its own.  That path pays where it is a good part
-// of the walk, and its code costs 4 % everywhere (forward, one H of 128 or 64: window
-// 256 with 4 sinks 39.6 -> 38.7 and 62.7 -> 58.6 us, window 1024 54.0 -> 55.0 and 88.9 ->
-// 90.1), so that only short windows take it.
+// KeySpan::narrow) has a path of its own.  That path pays where it is a good part of
+// the walk, and its code costs up to 4 % everywhere, so that only short windows take
+// it.  Forward, without and with it: window 256, 4 sinks 39.6 and 38.7 us (8192 tokens
+// in seven sequences, 16 / 8 heads of 128), 62.7 and 58.6 (8 x 2432, 12 heads of 64);
+// window 1024 54.0 and 55.0, 88.9 and 90.1.
 enum WindowKind { kWhole = 0, kWindow = 1, kWindowNarrow = 2 };
 inline int window_kind(const AttnArgs& a) {
   if (a.window >= kNoWindow) return kWhole;
