@@ -610,8 +610,10 @@ int normpre_qkrot_forward(const normpre_qkrot* p, int64_t tokens, int64_t used, 
  * dq_out, dk_out: gradients of the forward call's results; dq, dk: of its
  * inputs (either may be the former itself).  dq_weight, dk_weight: head_dim
  * values of weight_dtype each, or null where no gradient is wanted (a null
- * weight has none); then no workspace is needed.  The sums run in a fixed
- * order: the same inputs give the same bits.
+ * weight has none); then no workspace is needed.  A weight's gradient is off by
+ * the rounding of its terms and of sums of at most 16 rows in fp32, however many
+ * rows there are; the sums run in a fixed order: the same inputs give the same
+ * bits.
  */
 int normpre_qkrot_backward(const normpre_qkrot* p, int64_t tokens, int64_t used, const normpre_heads* q,
                            const normpre_heads* k, const void* positions, int position_bytes, const void* q_weight,

@@ -12,7 +12,7 @@
 // What bounds it: HBM would (16384 tokens of 16 / 8 heads of 128 in bf16: 30 us
 // forward, 45 backward at 6.75 TB/s), but a unit of work, four rows, takes 250 and
 // 400 instructions, of which the scheduler's 4 to 6 warps issue one in two cycles:
-// 42 us and 66 (45 and 69 with the launch, 4.4 TB/s).  More warps have fewer
+// 42 us and 66 (45 and 70 with the launch, 4.3 TB/s).  More warps have fewer
 // registers: with four CTAs an SM instead of three, or heads one by one, 51 to 70.
 //
 // A lane holds four pairs of a row (8 values), in bf16 of two heads at once, and with
@@ -51,10 +51,33 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 
+// A sum hi + lo of two fp32 numbers: the exact difference that an addition to hi
+// rounds off goes to lo (the two-sum of Knuth and Moller), so that it carries about
+// 46 bits.  16384 tokens, 16 / 8 heads of 128 in bf16 take 70.5 us backward (69 with
+// one fp32 number), 333 tokens of 32 / 32 heads of 64 12.3 us; with fp64 sums from
+// the threads on they took 74.6 and 18.5.
+struct Two {
+  float hi, lo;
+  __device__ __forceinline__ void add(float v) {
+    const float s = hi + v, b = s - hi;
+    lo += (hi - (s - b)) + (v - b);
+    hi = s;
+  }
+  __device__ __forceinline__ void add(const Two& v) {
+    add(v.hi);
+    lo += v.lo;
+  }
+  // what an infinite sum rounds off is NaN
+  __device__ __forceinline__ float value() const { return fabsf(hi) < INFINITY ? hi + lo : hi; }
+};
+__device__ __forceinline__ Two shuffled(const Two& v, int o) {
+  return Two{__shfl_xor_sync(0xffffffffu, v.hi, o), __shfl_xor_sync(0xffffffffu, v.lo, o)};
+}
+
 struct RotArgs {
   HeadsView x[2], dz[2], out[2];   // queries, keys: inputs, gradients of the results, results
   const void* w[2];                // weights, null: ones
-  float* part;                     // backward: weight gradients by CTA, [ctas][d]
+  Two* part;                       // backward: weight gradients by CTA, [ctas][d]
   const void* pos;
   int pos64, w_bf16;
   int64_t tokens, used;
@@ -228,7 +251,7 @@ __device__ __forceinline__ void scale(uint64_t (&x)[4], float f) {
 // The sums of two heads over the lanes of a row (two or more): the row's upper
 // half of lanes ends with the second head's, the lower half with the first's, in
 // one shuffle a step instead of two.  (Forward only: backward, where two sums travel,
-// it gained nothing, 69.4 us against 68.6.)
+// it gained nothing, 69.4 us against 68.6 with the sums of then.)
 __device__ __forceinline__ float split_sum(float first, float second, int lanes, bool upper) {
   float mine = (upper ? second : first) + __shfl_xor_sync(0xffffffffu, upper ? first : second, lanes >> 1);
 #pragma unroll
@@ -260,12 +283,56 @@ template <typename T, bool BWD> constexpr int per_sm() { return BWD ? 2 : 3; }
 // Heads of a unit: fp32 has no registers for two on their way.
 template <typename T> constexpr int kUnitHeads = sizeof(T) == 2 ? 2 : 1;
 
+// Backward: a thread's sums over rows of its 8 weight gradients.  Eight units at a
+// time are summed in fp32 registers; all beyond, of threads, warps and CTAs too, as
+// Two.  So a sum is off by what 16 rows' additions and the terms round, however many
+// tokens there are.
+struct alignas(16) Sums {
+  float4 hi[2][kThreads], lo[2][kThreads];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) hi[i][threadIdx.x] = lo[i][threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  // pairs of values; they start again from zero
+  __device__ __forceinline__ void take(uint64_t (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 h = hi[i][threadIdx.x], l = lo[i][threadIdx.x];
+      Two t[4] = {{h.x, l.x}, {h.y, l.y}, {h.z, l.z}, {h.w, l.w}};
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        float a, b;
+        tc::unpack2(v[2 * i + e / 2], a, b);
+        t[e].add(a);
+        t[e + 1].add(b);
+        v[2 * i + e / 2] = 0;
+      }
+      hi[i][threadIdx.x] = make_float4(t[0].hi, t[1].hi, t[2].hi, t[3].hi);
+      lo[i][threadIdx.x] = make_float4(t[0].lo, t[1].lo, t[2].lo, t[3].lo);
+    }
+  }
+  __device__ __forceinline__ Two get(int e) const {
+    return Two{reinterpret_cast<const float*>(&hi[e >> 2][threadIdx.x])[e & 3],
+               reinterpret_cast<const float*>(&lo[e >> 2][threadIdx.x])[e & 3]};
+  }
+};
+constexpr int kSumUnits = 8;   // a power of two
+
+template <bool BWD> struct alignas(16) Shared {
+  float w[8 * 32];   // the weights by lane
+};
+template <> struct alignas(16) Shared<true> {
+  float w[8 * 32];
+  Sums sums;
+  Two by_warp[kWarps][8 * 32];
+};
+
 // Each warp walks its share of the (token group, heads) units: 32 / lanes tokens
 // at once.  The next unit is on its way while one is worked on.  BWD:
 // gradients.  side: 0 queries, 1 keys, known to the compiler so that what the
 // launch's arguments hold for it needs no registers.
 template <typename T, int V, bool INTER, bool BWD, int side>
-__device__ __forceinline__ void walk(const RotArgs& g) {
+__device__ __forceinline__ void walk(const RotArgs& g, Shared<BWD>& sh) {
   constexpr int H = kUnitHeads<T>;
   using tc::fma2;
   using tc::mul2;
@@ -283,7 +350,7 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (4 * u + e < g.half && (INTER || u < g.rot_units)) turned |= 1u << e;
-  __shared__ __align__(16) float sw[8 * 32];   // the weights by lane
+  float* const sw = sh.w;
   if (threadIdx.x < 8 * g.lanes) {
     const int at = place<INTER>(unit_of<INTER>(g, threadIdx.x >> 3), threadIdx.x & 7);
     sw[threadIdx.x] = at < 0 ? 0.f : weight(g, side, at);
@@ -291,6 +358,9 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
   __syncthreads();
   auto weights = [&](int e) { return reinterpret_cast<const uint64_t*>(sw)[4 * u + e]; };
   uint64_t dw[4] = {0, 0, 0, 0};
+  if constexpr (BWD) {
+    if (g.part) sh.sums.clear();
+  }
 
   // the unit on its way: its place, values and position
   const bool want_x = !BWD || g.norm;
@@ -525,27 +595,25 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
       for (int i = 0; i < H; ++i)
         if (i == 0 || i < here) Raw<T, V>::template store<INTER>(to + i * g.out[side].hs, t, y[i]);
     }
+    if constexpr (BWD) {
+      if (g.part && left % kSumUnits == 0) sh.sums.take(dw);
+    }
   }
   if constexpr (BWD) {
     // the CTA's weight gradients: over the rows of a warp, then over the warps
     if (!g.part) return;
-    __shared__ float sm[kWarps][8 * 32];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float v[2];
-      tc::unpack2(dw[e], v[0], v[1]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        for (int o = g.lanes; o < 32; o <<= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        if (sub == 0) sm[warp][8 * u + 2 * e + i] = v[i];
-      }
+    for (int e = 0; e < 8; ++e) {
+      Two v = sh.sums.get(e);
+      for (int o = g.lanes; o < 32; o <<= 1) v.add(shuffled(v, o));
+      if (sub == 0) sh.by_warp[warp][8 * u + e] = v;
     }
     __syncthreads();
     if (threadIdx.x < 8 * g.lanes) {
       const int to = place<INTER>(unit_of<INTER>(g, threadIdx.x >> 3), threadIdx.x & 7);
-      float sum = 0.f;
+      Two sum = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < kWarps; ++i) sum += sm[i][threadIdx.x];
+      for (int i = 0; i < kWarps; ++i) sum.add(sh.by_warp[i][threadIdx.x]);
       if (to >= 0) g.part[static_cast<int64_t>(blockIdx.x) * g.dim + to] = sum;
     }
   }
@@ -553,27 +621,30 @@ __device__ __forceinline__ void walk(const RotArgs& g) {
 
 template <typename T, int V, bool INTER, bool BWD>
 __global__ void __launch_bounds__(kThreads, per_sm<T, BWD>()) k_qkrot(const __grid_constant__ RotArgs g) {
-  if (blockIdx.x < g.ctas) walk<T, V, INTER, BWD, 0>(g);
-  else walk<T, V, INTER, BWD, 1>(g);
+  __shared__ Shared<BWD> sh;
+  if (blockIdx.x < g.ctas) walk<T, V, INTER, BWD, 0>(g, sh);
+  else walk<T, V, INTER, BWD, 1>(g, sh);
 }
 
 // Sums the CTAs' weight gradients in a fixed order: 32 columns of one weight.
-__global__ void __launch_bounds__(1024) k_qkrot_fold(const float* part, int q_ctas, int ctas, int dim, void* dqw, void* dkw,
+__global__ void __launch_bounds__(1024) k_qkrot_fold(const Two* part, int q_ctas, int ctas, int dim, void* dqw, void* dkw,
                                                      int w_bf16) {
-  __shared__ float sm[32][33];
+  __shared__ Two sm[32][33];
   const int side = blockIdx.y, col = 32 * blockIdx.x + threadIdx.x;
   const int first = side ? q_ctas : 0, last = side ? ctas : q_ctas;
-  float sum = 0.f;
+  Two sum = {0.f, 0.f};
   if (col < dim)
-    for (int i = first + threadIdx.y; i < last; i += 32) sum += part[static_cast<int64_t>(i) * dim + col];
+    for (int i = first + threadIdx.y; i < last; i += 32) sum.add(part[static_cast<int64_t>(i) * dim + col]);
   sm[threadIdx.y][threadIdx.x] = sum;
   __syncthreads();
-  sum = warp_sum(sm[threadIdx.x][threadIdx.y]);
+  sum = sm[threadIdx.x][threadIdx.y];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum.add(shuffled(sum, o));
   void* out = side ? dkw : dqw;
   const int to = 32 * blockIdx.x + threadIdx.y;
   if (threadIdx.x == 0 && to < dim && out) {
-    if (w_bf16) static_cast<bf16*>(out)[to] = from_f32<bf16>(sum);
-    else static_cast<float*>(out)[to] = sum;
+    if (w_bf16) static_cast<bf16*>(out)[to] = from_f32<bf16>(sum.value());
+    else static_cast<float*>(out)[to] = sum.value();
   }
 }
 
@@ -692,7 +763,7 @@ int normpre_qkrot_init(const normpre_qkrot_config* cfg, const double* frequencie
 
 int normpre_qkrot_bytes(const normpre_qkrot* p, int64_t* bytes) {
   if (!p || !bytes) return fail(NORMPRE_ERR_ARG, "null argument");
-  *bytes = static_cast<int64_t>(kMaxCtas) * p->cfg.head_dim * static_cast<int64_t>(sizeof(float));
+  *bytes = static_cast<int64_t>(kMaxCtas) * p->cfg.head_dim * static_cast<int64_t>(sizeof(Two));
   return NORMPRE_OK;
 }
 
@@ -741,13 +812,13 @@ int normpre_qkrot_backward(const normpre_qkrot* p, int64_t tokens, int64_t used,
         (rc = take_heads(dq, tokens, c.n_heads, c.head_dim, c.dtype, "dq", true, &g.out[0])) ||
         (rc = take_heads(dk, tokens, c.n_kv_heads, c.head_dim, c.dtype, "dk", true, &g.out[1])))
       return rc;
-    g.part = weights ? static_cast<float*>(workspace) : nullptr;
+    g.part = weights ? static_cast<Two*>(workspace) : nullptr;
     ctas = c.dtype == NORMPRE_BF16 ? launch<bf16, true>(&g, width(p->half), c.interleaved, s)
                                    : launch<float, true>(&g, width(p->half), c.interleaved, s);
   }
   if (weights)
     k_qkrot_fold<<<dim3(static_cast<unsigned>(cdiv(c.head_dim, 32)), 2), dim3(32, 32), 0, s>>>(
-        static_cast<const float*>(workspace), g.ctas, static_cast<int>(ctas), c.head_dim, dq_weight, dk_weight,
+        static_cast<const Two*>(workspace), g.ctas, static_cast<int>(ctas), c.head_dim, dq_weight, dk_weight,
         weight_dtype == NORMPRE_BF16);
   return done(cudaGetLastError(), "query and key norms, backward");
 }
