@@ -631,7 +631,8 @@ void normpre_qkrot_free(normpre_qkrot* p);
  * (normpre_dtype), aligned to its elements, at most 2^40 values in all; arrays of pointers, sizes and dtypes are host memory
  * and are read before the call returns.  fp32 products; sums of squares in fp32
  * over 64 bytes of values (fp64 where they would leave its range), fp64 beyond,
- * in a fixed order: the same inputs give the same bits.
+ * in a fixed order: the same inputs give the same bits; norm and c are their 64-bit
+ * values rounded once.
  *   norm       device, one fp32 value, written.  A gradient that holds a NaN
  *              gives NaN, one that holds an infinity infinity.
  *   workspace  device, 16-byte aligned, normpre_grad_bytes(n) bytes, whose

@@ -195,10 +195,26 @@ __device__ __forceinline__ double fold(const double* part, int parts, double* re
   return block_sum(sum, red);
 }
 
-// The root of a sum in fp32: where its range allows, of the sum rounded to fp32,
-// off by 1.5 units of 2^-24 (the fp64 root takes a microsecond).
-__device__ __forceinline__ float root(double sum) {
-  return sum > 0x1p-120 && sum < 0x1p120 ? sqrtf(static_cast<float>(sum)) : static_cast<float>(sqrt(sum));
+// The root of a sum in fp64.  Where fp32's range allows, its fp32 root f and one
+// step of Heron's method, f + (sum - f^2) / (2 f), whose last quotient needs fp32
+// only: off by 2^-46 (the fp64 root takes a microsecond).
+__device__ __forceinline__ double root(double sum) {
+  if (!(sum > 0x1p-120 && sum < 0x1p120)) return sqrt(sum);
+  const float f = sqrtf(static_cast<float>(sum));
+  const double n = f;
+  return fma(fma(-n, n, sum), static_cast<double>(0.5f / f), n);
+}
+
+// min(1, limit / (n + eps)), rounded once: the fp32 quotient q and one step of its
+// refinement, q + (limit - q to) / to, where fp32's range allows.  A norm that is
+// NaN gives NaN; all zeros are left as they are.
+__device__ __forceinline__ float clip_factor(double n, float max_norm, float eps) {
+  const double to = n + static_cast<double>(eps), limit = max_norm;
+  if (to <= limit) return 1.f;
+  if (!(to > 0x1p-60 && to < 0x1p60 && limit > 0x1p-60)) return static_cast<float>(limit / to);
+  const float f = static_cast<float>(to), inv = 1.f / f;
+  const double q = max_norm * inv;
+  return static_cast<float>(fma(fma(-q, to, limit), static_cast<double>(inv), q));
 }
 
 template <typename T, typename U>
@@ -215,16 +231,9 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_grad_scale(const __grid_co
   __shared__ float factor;
   const double sum = fold(part, parts, red);
   if (threadIdx.x == 0) {
-    float n = root(sum);
-    // all zeros are left as they are; a norm that is NaN gives NaN
-    if (n > 0x1p-60f && n < 0x1p100f) {
-      const float to = n + eps;
-      factor = to <= max_norm ? 1.f : max_norm / to;
-    } else {
-      const double to = sqrt(sum) + static_cast<double>(eps);
-      factor = to <= static_cast<double>(max_norm) ? 1.f : static_cast<float>(static_cast<double>(max_norm) / to);
-    }
-    if (norm && blockIdx.x == 0) *norm = n;
+    const double n = root(sum);
+    factor = clip_factor(n, max_norm, eps);
+    if (norm && blockIdx.x == 0) *norm = static_cast<float>(n);
   }
   __syncthreads();
   const float f = factor;
@@ -249,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) k_grad_scale(const __grid_co
 __global__ void __launch_bounds__(kThreads) k_grad_norm(const double* part, int parts, float* norm) {
   __shared__ double red[kThreads / 32];
   const double sum = fold(part, parts, red);
-  if (threadIdx.x == 0) *norm = root(sum);
+  if (threadIdx.x == 0) *norm = static_cast<float>(root(sum));
 }
 
 int fail(int code, const std::string& msg) {
