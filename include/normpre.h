@@ -375,6 +375,8 @@ int normpre_normalize_cols_noalloc(int64_t rows, int64_t cols, float mu, const v
  * another sequence holds never reaches a sequence.  Within a sequence a
  * non-finite value of token j reaches, besides the rows i >= j that see it,
  * the rows of j's aligned block of 128 rows (0 * NaN in the tile products).
+ * BF16: values v up to 2^120 over the number of keys that a row sees; beyond, o
+ * may overflow.
  */
 typedef struct normpre_attn normpre_attn;
 

@@ -26,10 +26,11 @@
 // and V tiles pass through one ring that a TMA warp fills.
 //
 // The running maximum is only raised when it would grow by more than 2^8 (with a
-// window 2^24; O and l then are rescaled by the softmax warps themselves): P stays
-// below that relative to the row's maximum, which bf16 and the fp32 sums hold as
-// precisely (and values of V below 2^90 without overflow), and the rescale, which
-// has to wait for P V, is rare.
+// window 2^24; O and l then are rescaled by the softmax warps themselves), so that
+// the rescale, which has to wait for P V, is rare.  P stays below 2^8 (with a window
+// it is formed 2^16 times smaller), which bf16 and the fp32 sums hold as precisely;
+// O does not overflow where V stays below 2^120 over the number of visible keys, and
+// a probability below 2^-110 of the row's largest may vanish.
 //
 // S - m' is formed before the scale: near the maximum it is exact however large
 // the scores, while c S - c m' would carry the rounding of c m' (0.002 in the
@@ -60,8 +61,9 @@ constexpr int kThreads = 384;   // softmax 2 x 4 warps, TMA, MMA of tile 0, sequ
 // log2 of the growth that raises the maximum.  With a window an item has few
 // blocks, and the diagonal one shows its upper rows few keys, so that a larger
 // maximum in the next is common where scores are sharp: at a standard deviation of
-// 3 raising cost a fourth of the time at 2^8.
-constexpr float kGrow = 8.f, kGrowWindow = 24.f;
+// 3 raising cost a fourth of the time at 2^8.  There P, l and O are 2^kLift times
+// smaller, so that they stay below what kGrow allows.
+constexpr float kGrow = 8.f, kGrowWindow = 24.f, kLift = kGrowWindow - kGrow;
 
 template <int DP> struct Fwd {
   static constexpr int kChunks = DP / 64;
@@ -413,7 +415,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float lo, hi;
-            tc::unpack2(tc::mul2(tc::add2(tc::pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), m2), c2), lo, hi);
+            const uint64_t d2 = tc::add2(tc::pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), m2);
+            tc::unpack2(WIN ? tc::fma2(d2, c2, tc::pack2(-kLift, -kLift)) : tc::mul2(d2, c2), lo, hi);
             lo = tc::exp2_fast(lo);
             hi = tc::exp2_fast(hi);
             sum[i & 1] = tc::add2(sum[i & 1], tc::pack2(lo, hi));
@@ -532,7 +535,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       if (lane == 0) tc::mbar_arrive(&b->o_empty[s][acc]);
       if (kAcc == 2) acc ^= 1;
       if (row < rows)
-        f.a.lse[static_cast<int64_t>(head) * f.a.tokens + at + row] = fmaf(m, f.a.scale, log2f(l) * 0.6931471805599453f);
+        f.a.lse[static_cast<int64_t>(head) * f.a.tokens + at + row] =
+            fmaf(m, f.a.scale, log2f(WIN ? l * exp2f(kLift) : l) * 0.6931471805599453f);
     }
   }
   if (!ok && lane == 0) {
