@@ -197,7 +197,10 @@ __device__ __forceinline__ bool rows_of(const AttnArgs& a, const AttnBlock* list
   return w.seq < a.tokens;
 }
 
-template <typename T, int DP>
+// WIN: the rows have a window.  The kernels without one are kernels of their own:
+// its tests in every pair of rows and its second kind of tile cost them 3 to 11 %
+// forward, 1 to 3 % backward.
+template <typename T, int DP, bool WIN>
 __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ AttnArgs a) {
   extern __shared__ float sm[];
   float* Q = sm;
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
 #pragma unroll
     for (int k = 0; k < DP / 64; ++k) acc[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  const int diag = w.first / kB, lo = max(0, w.first - a.window + 1) / kB, sink = min(lo, (a.sinks + kB - 1) / kB);
+  const int diag = w.first / kB;
   // keys of a tile, NC groups of 16
   auto tile = [&](int jb, auto groups) {
     constexpr int NC = decltype(groups)::value;
@@ -238,6 +241,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
     scores<DP, NC>(Q, KV, ty, tx, s);
     const int up = kB * (diag - jb);
     auto hidden = [&](int r, int c) {
+      if constexpr (!WIN) return jb == diag && tx + 16 * c > ty + 16 * r;
       const int far = up + ty + 16 * r - tx - 16 * c;        // rows between the two
       return far < 0 || (far >= a.window && kB * jb + tx + 16 * c >= a.sinks);
     };
@@ -274,9 +278,14 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
     __syncthreads();
     accumulate<DP, NC>(P, KV, ty, tx, acc);
   };
-  for (int jb = diag; jb >= 0; jb = jb > lo || jb <= sink ? jb - 1 : sink - 1) {
-    if (jb < sink && a.sinks - jb * kB <= 16) tile(jb, Groups<1>());
-    else tile(jb, Groups<4>());
+  if constexpr (WIN) {
+    const int lo = max(0, w.first - a.window + 1) / kB, sink = min(lo, (a.sinks + kB - 1) / kB);
+    for (int jb = diag; jb >= 0; jb = jb > lo || jb <= sink ? jb - 1 : sink - 1) {
+      if (jb < sink && a.sinks - jb * kB <= 16) tile(jb, Groups<1>());
+      else tile(jb, Groups<4>());
+    }
+  } else {
+    for (int jb = diag; jb >= 0; --jb) tile(jb, Groups<4>());
   }
   float inv[4];
 #pragma unroll
@@ -290,7 +299,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_fwd(const __grid_constant__ A
 // P and dS of query rows i0 .. and key rows j0 .. of a sequence, from tiles in
 // shared memory; zero where i < j or past the sequence's end.  s holds
 // ds / c on return, p the probabilities.
-template <int DP, int NC = 4>
+template <int DP, bool WIN, int NC = 4>
 __device__ __forceinline__ void grad_scores(const AttnArgs& a, const float* Q, const float* K, const float* dO,
                                             const float* V, const float* lse, const float* delta, int i0, int j0,
                                             int len, int ty, int tx, float (&p)[4][4], float (&s)[4][4]) {
@@ -304,9 +313,9 @@ __device__ __forceinline__ void grad_scores(const AttnArgs& a, const float* Q, c
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int j = j0 + tx + 16 * c;
-      const bool seen = i < len && j <= i && (i - j < a.window || j < a.sinks);
+      const bool seen = i < len && j <= i && (!WIN || i - j < a.window || j < a.sinks);
       p[r][c] = seen ? exp2f(fmaf(t[r][c], a.scale, -ls) * kLog2e) : 0.f;
-      s[r][c] = seen && !sees_itself(a.window, a.sinks) ? p[r][c] * (s[r][c] - de) : 0.f;
+      s[r][c] = seen && !(WIN && sees_itself(a.window, a.sinks)) ? p[r][c] * (s[r][c] - de) : 0.f;
     }
   }
 }
@@ -321,7 +330,7 @@ __device__ __forceinline__ void load_stats(const AttnArgs& a, float* lse, float*
   }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool WIN>
 __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int kvh, float* sm, float* lse, float* delta) {
   float* K = sm;
   float* V = K + kB * ld<DP>();
@@ -338,7 +347,8 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
     zero_rows<T>(a.dv, row0, rows, kvh, a.dim);
     return;
   }
-  const KeyPart part = key_part(w.block, a.window, a.sinks, a.chunk, a.slots);
+  KeyPart part = {0, 0, -1, w.block.part == 0};
+  if constexpr (WIN) part = key_part(w.block, a.window, a.sinks, a.chunk, a.slots);
   if (!part.fits) {
     if (threadIdx.x == 0) raise_host_flag(a.flags, kFlagLists);
     return;
@@ -351,9 +361,13 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int k = 0; k < DP / 64; ++k) dk[r][k] = dv[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  // rows past the last one that sees any of these keys
-  const int last = w.first < a.sinks ? w.len : min(w.len, w.first + kB - 1 + a.window);
-  const int begin = max(w.first, 128 * part.first), end = min(last, 128 * part.end);
+  int begin = w.first, end = w.len;
+  if constexpr (WIN) {
+    // to the last row that sees any of these keys
+    if (w.first >= a.sinks) end = min(end, w.first + kB - 1 + a.window);
+    begin = max(begin, 128 * part.first);
+    end = min(end, 128 * part.end);
+  }
   for (int g = 0; g < a.group; ++g) {
     const int head = kvh * a.group + g;
     for (int i0 = begin; i0 < end; i0 += kB) {
@@ -363,7 +377,7 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
       load_stats(a, lse, delta, head, w.seq + i0, qrows);
       __syncthreads();
       float p[4][4], s[4][4];
-      grad_scores<DP>(a, Q, K, dO, V, lse, delta, i0, w.first, w.len, ty, tx, p, s);
+      grad_scores<DP, WIN>(a, Q, K, dO, V, lse, delta, i0, w.first, w.len, ty, tx, p, s);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -377,7 +391,7 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
     }
   }
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, c[4] = {a.scale, a.scale, a.scale, a.scale};
-  if (part.slot >= 0) {
+  if (WIN && part.slot >= 0) {
     // 128 rows of the slot, these the first or second 64
     float* p = a.partial + ((static_cast<int64_t>(part.slot) * a.kv_heads + kvh) * 2 * 128 + (w.first & 127)) * a.dim;
     const AttnTensor pk = {p, a.dim, 0}, pv = {p + 128 * a.dim, a.dim, 0};
@@ -389,7 +403,7 @@ __device__ __forceinline__ void owned_keys(const AttnArgs& a, int64_t item, int 
   store_tile<T, DP>(a.dv, row0, rows, kvh, a.dim, ty, tx, dv, one);
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool WIN>
 __device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, int head, float* sm, float* lse, float* delta) {
   float* Q = sm;
   float* dO = Q + kB * ld<DP>();
@@ -413,7 +427,6 @@ __device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, i
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int k = 0; k < DP / 64; ++k) dq[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int lo = max(0, w.first - a.window + 1) / kB * kB, sink = min(lo, (a.sinks + kB - 1) / kB * kB);
   auto tile = [&](int j0, auto groups) {
     constexpr int NC = decltype(groups)::value;
     const int krows = min(16 * NC, w.len - j0);
@@ -421,7 +434,7 @@ __device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, i
     load_tiles<T, DP>(K, a.k, V, a.v, w.seq + j0, krows, kvh, a.dim);
     __syncthreads();
     float p[4][4], s[4][4];
-    grad_scores<DP, NC>(a, Q, K, dO, V, lse, delta, w.first, j0, w.len, ty, tx, p, s);
+    grad_scores<DP, WIN, NC>(a, Q, K, dO, V, lse, delta, w.first, j0, w.len, ty, tx, p, s);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -429,9 +442,14 @@ __device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, i
     __syncthreads();
     accumulate<DP, NC>(S, K, ty, tx, dq);
   };
-  for (int j0 = sink ? 0 : lo; j0 <= w.first; j0 = j0 + kB == sink ? lo : j0 + kB) {
-    if (j0 < sink && a.sinks - j0 <= 16) tile(j0, Groups<1>());
-    else tile(j0, Groups<4>());
+  if constexpr (WIN) {
+    const int lo = max(0, w.first - a.window + 1) / kB * kB, sink = min(lo, (a.sinks + kB - 1) / kB * kB);
+    for (int j0 = sink ? 0 : lo; j0 <= w.first; j0 = j0 + kB == sink ? lo : j0 + kB) {
+      if (j0 < sink && a.sinks - j0 <= 16) tile(j0, Groups<1>());
+      else tile(j0, Groups<4>());
+    }
+  } else {
+    for (int j0 = 0; j0 <= w.first; j0 += kB) tile(j0, Groups<4>());
   }
   const float c[4] = {a.scale, a.scale, a.scale, a.scale};
   store_tile<T, DP>(a.dq, row0, rows, head, a.dim, ty, tx, dq, c);
@@ -440,14 +458,14 @@ __device__ __forceinline__ void owned_queries(const AttnArgs& a, int64_t item, i
 // Both kinds of work in one launch, side by side for each 64 rows, so that the
 // SMs that run out of the one take the other.  At head dimensions up to 64 two
 // CTAs share an SM.
-template <typename T, int DP>
+template <typename T, int DP, bool WIN>
 __global__ void __launch_bounds__(kThreads, DP == 64 ? 2 : 1) k_attn_bwd(const __grid_constant__ AttnArgs a) {
   extern __shared__ float sm[];
   __shared__ float lse[kB], delta[kB];
   const int all = a.kv_heads + a.heads, which = static_cast<int>(blockIdx.x % all);
   const int64_t item = blockIdx.x / all;
-  if (which < a.kv_heads) owned_keys<T, DP>(a, item, which, sm, lse, delta);
-  else owned_queries<T, DP>(a, item, which - a.kv_heads, sm, lse, delta);
+  if (which < a.kv_heads) owned_keys<T, DP, WIN>(a, item, which, sm, lse, delta);
+  else owned_queries<T, DP, WIN>(a, item, which - a.kv_heads, sm, lse, delta);
 }
 
 // LANES (8 or 16) lanes per row and head, 8 columns each; EACH rows and heads a
@@ -500,15 +518,22 @@ template <int DP> constexpr size_t bwd_smem() { return sizeof(float) * (4 * kB *
 
 }  // namespace
 
+template <int DP, bool WIN>
+static cudaError_t forward(const AttnArgs& a, cudaStream_t s) {
+  return run<k_attn_fwd<float, DP, WIN>>(a, a.heads, fwd_smem<DP>(), s);
+}
 cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t s) {
-  return a.dim <= 64 ? run<k_attn_fwd<float, 64>>(a, a.heads, fwd_smem<64>(), s)
-                     : run<k_attn_fwd<float, 128>>(a, a.heads, fwd_smem<128>(), s);
+  if (window_kind(a) == kWhole) return a.dim <= 64 ? forward<64, false>(a, s) : forward<128, false>(a, s);
+  return a.dim <= 64 ? forward<64, true>(a, s) : forward<128, true>(a, s);
 }
 
+template <int DP, bool WIN>
+static cudaError_t backward(const AttnArgs& a, cudaStream_t s) {
+  return run<k_attn_bwd<float, DP, WIN>>(a, a.kv_heads + a.heads, bwd_smem<DP>(), s);
+}
 cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t s) {
-  const int each = a.kv_heads + a.heads;
-  return a.dim <= 64 ? run<k_attn_bwd<float, 64>>(a, each, bwd_smem<64>(), s)
-                     : run<k_attn_bwd<float, 128>>(a, each, bwd_smem<128>(), s);
+  if (window_kind(a) == kWhole) return a.dim <= 64 ? backward<64, false>(a, s) : backward<128, false>(a, s);
+  return a.dim <= 64 ? backward<64, true>(a, s) : backward<128, true>(a, s);
 }
 
 // One CTA for 16 rows of dk or dv of a split key block and head: 16 lanes a row,
