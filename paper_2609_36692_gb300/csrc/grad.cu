@@ -75,10 +75,12 @@ template <typename T> struct Piece {
     else return i & 1 ? bf16hi(w[i >> 1]) : bf16lo(w[i >> 1]);
   }
   // elements i .. of the tensor's n, i a multiple of 16 bytes' worth before its
-  // first one or behind it: zeros outside
-  __device__ __forceinline__ void load(const T* p, int64_t i, int64_t n) {
+  // first one or behind it: zeros outside.  ONLY_READ: the launch writes nothing of
+  // the memory, which the read-only path asks for; clipping in place does.
+  template <bool ONLY_READ> __device__ __forceinline__ void load(const T* p, int64_t i, int64_t n) {
+    auto get = [](const auto* at) { return ONLY_READ ? __ldg(at) : *at; };
     if (i >= 0 && i + kN <= n) {
-      const uint4 q = __ldg(reinterpret_cast<const uint4*>(p + i));
+      const uint4 q = get(reinterpret_cast<const uint4*>(p + i));
       w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
     } else {
 #pragma unroll
@@ -86,8 +88,8 @@ template <typename T> struct Piece {
 #pragma unroll
       for (int e = 0; e < kN; ++e)
         if (i + e >= 0 && i + e < n) {
-          if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(__ldg(p + i + e));
-          else w[e >> 1] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const unsigned short*>(p) + i + e)) << (16 * (e & 1));
+          if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(get(p + i + e));
+          else w[e >> 1] |= static_cast<uint32_t>(get(reinterpret_cast<const unsigned short*>(p) + i + e)) << (16 * (e & 1));
         }
     }
   }
@@ -127,9 +129,9 @@ template <typename T> struct Share {
     return (static_cast<int64_t>(chunk - e.first) * (kChunkBytes / 16) + i * kThreads + static_cast<int>(threadIdx.x)) *
                Piece<T>::kN - lead;
   }
-  __device__ __forceinline__ void load(const Entry& e, uint32_t chunk) {
+  template <bool ONLY_READ> __device__ __forceinline__ void load(const Entry& e, uint32_t chunk) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[i].load(static_cast<const T*>(e.in), index(e, chunk, i), e.size);
+    for (int i = 0; i < 4; ++i) q[i].template load<ONLY_READ>(static_cast<const T*>(e.in), index(e, chunk, i), e.size);
   }
   __device__ __forceinline__ double squares() const {
     float p[4];
@@ -167,7 +169,7 @@ template <typename T> struct Share {
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const Entry& e, uint32_t chunk) {
   Share<T> x;
-  x.load(e, chunk);
+  x.template load<true>(e, chunk);
   return x.squares();
 }
 
@@ -220,7 +222,7 @@ __device__ __forceinline__ float clip_factor(double n, float max_norm, float eps
 template <typename T, typename U>
 __device__ __forceinline__ void scale_chunk(const Entry& e, uint32_t chunk, float c) {
   Share<T> x;
-  x.load(e, chunk);
+  x.template load<false>(e, chunk);
   x.template store<U>(e, chunk, c);
 }
 

@@ -34,3 +34,25 @@ def test_norm_and_factor_are_rounded_once(shift):
         c = min(1.0, limit / (n + eps))
         assert abs(float(out[0][0]) / unit - c) <= half_ulp(c) * (1 + 2.0 ** -20), (i, limit, eps)
         assert float(optim.grad_norm([g])) == norm
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_in_place_each_value_once(dtype):
+    """Slices of one buffer side by side, which share lines of memory with their
+    neighbours in other CTAs: each value is halved once, whoever is first."""
+    import torch
+    from paper_2609_36692_gb300 import optim
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    sizes = [1 + (i * 7919) % 9001 for i in range(400)]
+    buf = torch.ones(sum(sizes) + 2, dtype=t, device="cuda")
+    grads = list(buf[1:-1].split(sizes))
+    n = math.sqrt(sum(sizes))
+    for i in range(10):
+        # the norm is n 2^-i, the limit half of it, both rounded once; the factor is within 2^-22 of a half
+        c = float(torch.tensor(0.5 * n * 2.0 ** -i, dtype=torch.float32)) / (n * 2.0 ** -i)
+        before = buf.clone()
+        optim.clip_grads(grads, c * n * 2.0 ** -i, eps=0.0)
+        want = before[1:-1].float() * torch.tensor(c, dtype=torch.float32, device="cuda")
+        assert bool((buf[1:-1].float() - want).abs().max() <= 2.0 ** -22 * want.max() + (2.0 ** -8 * want.max() if dtype == "bf16" else 0))
+        assert float(buf[0]) == 1.0 == float(buf[-1])
+        buf[1:-1] = 2.0 ** -(i + 1)
