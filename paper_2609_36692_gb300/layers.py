@@ -60,6 +60,12 @@ def _used_on(stream, *tensors) -> None:
                 t.record_stream(stream)
 
 
+def _overwrites(*tensors) -> None:
+    """Tells autograd that a call writes these tensors of the caller's: a backward
+    pass that needs what they held raises, as behind torch's own in-place calls."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _empty(shape, dtype, device: torch.device, stream) -> torch.Tensor:
     """An output that work on `stream` (None: the current one) writes.  It comes
     from that stream's own pool: memory of the current stream's may still be
@@ -149,6 +155,8 @@ class PackedAttention:
         t, h, hk, d, index = q.shape[0], self.n_heads, self.n_kv_heads, self.head_dim, self.device.index
         views = _views(self.dtype, d, index, t, (q, "q", h), (k, "k", hk), (v, "v", hk))
         _used_on(stream, q, k, v, out, lse)
+        if out is not None or lse is not None:
+            _overwrites(out, lse)
         if out is None:
             out = _empty((t, h, d), self.dtype, self.device, stream)
         if lse is None:
@@ -164,6 +172,8 @@ class PackedAttention:
         t, h, hk, d, index = q.shape[0], self.n_heads, self.n_kv_heads, self.head_dim, self.device.index
         views = _views(self.dtype, d, index, t, (q, "q", h), (k, "k", hk), (v, "v", hk), (out, "out", h), (dout, "dout", h))
         _used_on(stream, q, k, v, out, lse, dout, dq, dk, dv)
+        if dq is not None or dk is not None or dv is not None:
+            _overwrites(dq, dk, dv)
         if dq is None:
             dq = _empty((t, h, d), self.dtype, self.device, stream)
         if dk is None:
@@ -298,6 +308,8 @@ class QKNormRotary:
         views = _views(self.dtype, self.head_dim, index, t, (q, "q", h), (k, "k", hk))
         rest = self._rest(positions, q_weight, k_weight, t, index)
         _used_on(stream, q, k, positions, q_weight, k_weight, q_out, k_out)
+        if q_out is not None or k_out is not None:
+            _overwrites(q_out, k_out)
         if q_out is None:
             q_out = _empty((t, h, self.head_dim), self.dtype, q.device, stream)
         if k_out is None:
@@ -317,6 +329,8 @@ class QKNormRotary:
         views = _views(self.dtype, self.head_dim, index, t, (q, "q", h), (k, "k", hk), (dq_out, "dq_out", h), (dk_out, "dk_out", hk))
         rest = self._rest(positions, q_weight, k_weight, t, index)
         _used_on(stream, q, k, positions, dq_out, dk_out, q_weight, k_weight, dq, dk)
+        if dq is not None or dk is not None:
+            _overwrites(dq, dk)
         device = q.device
         if dq is None:
             dq = _empty((t, h, self.head_dim), self.dtype, device, stream)
@@ -404,6 +418,8 @@ class Checkpoint:
             out = torch.empty((self.tokens, self.features), dtype=dtype or self.dtype, device=self.device)
         elif dtype is not None and out.dtype != dtype:
             raise TypeError("out must be %s" % dtype)
+        else:
+            _overwrites(out)
         ld = _matrix(out, "out", (self.tokens, self.features), self.device)
         _on(self.device, C.normpre_ckpt_restore, self.tokens, self.features, self.codes_ptr, self.steps_ptr,
             out.data_ptr(), _dtype_code(out), ld)
@@ -453,6 +469,8 @@ def ckpt_wgrad(dy: torch.Tensor, ck: Checkpoint, dtype: Optional[torch.dtype] = 
         out = torch.empty(shape, dtype=dtype or dy.dtype, device=ck.device)
     elif dtype is not None and out.dtype != dtype:
         raise TypeError("out must be %s" % dtype)
+    else:
+        _overwrites(out)
     out_ld = _matrix(out, "out", shape, ck.device)
     _on(ck.device, C.normpre_ckpt_wgrad, ck.tokens, shape[0], shape[1], dy.data_ptr(), _dtype_code(dy), ld,
         ck.codes_ptr, ck.steps_ptr, out.data_ptr(), _dtype_code(out), out_ld, accumulate)

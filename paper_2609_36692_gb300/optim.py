@@ -285,6 +285,8 @@ def clip_grads(grads, max_norm: float, eps: float = 1e-6, out=None):
                 raise ValueError("out %d must have its gradient's shape" % i)
             if not (plain and plain_out) and not (o.is_contiguous() and g.is_contiguous()) and o.stride() != g.stride():
                 raise ValueError("out %d must have its gradient's strides" % i)
+    # autograd: a backward pass that needs what they held raises, as behind torch's own in-place calls
+    torch.autograd.graph.increment_version(grads if out is None else out)
     return _grad_call(grads[0].device, C.normpre_grad_clip, *lists, to[0], to[1], float(max_norm), float(eps))
 
 
