@@ -563,8 +563,8 @@ int normpre_ckpt_sync_status(void* stream);
  *   dx = r (u - xh mean(u xh)),  dw = sum of g xh over tokens and heads
  * One weight of head_dim values serves all query heads, one all key heads; a
  * null weight is one of ones.  fp32 arithmetic (rows whose squares leave its
- * range are scaled first), results rounded once; angles are exact to 2^-53 of a
- * turn per position, whatever the position.
+ * range are scaled first), results rounded once.  p f_i is off by at most 2^-64 of a
+ * turn for each position p, whatever f_i, and its cos and sin by 4 units of 2^-24.
  * Rows from `used` on (padding) are written as zeros and add nothing to the
  * weights' gradients, whatever they hold.  A row that is not finite reaches its
  * own results and the weights' gradients.

@@ -23,8 +23,9 @@
 // that no access leaves its alignment); interleaved pairs two runs of four.
 //
 // Angles: a position is a whole number p, and a frequency is kept as a 64-bit
-// fraction F of a turn.  p F mod 2^64 is the angle's fraction of a turn, exact
-// for every p, however far: no table, no rounding that grows with p.
+// fraction F of a turn, the nearest one.  p F mod 2^64 is the product's fraction of a
+// turn without a rounding, and there is no table; what grows with p is F's own
+// rounding alone, at most 2^-65 of a turn for each position.
 #include <algorithm>
 #include <cmath>
 #include <memory>
@@ -725,6 +726,17 @@ int base(const normpre_qkrot* p, int64_t tokens, int64_t used, const normpre_hea
   return NORMPRE_OK;
 }
 
+// A frequency in radians as a fraction of a turn, in units of 2^-64: |f| / (2 pi) in
+// two parts, high + low, with 1 / (2 pi) in two parts as well (106 bits), so that the
+// whole turns of a large frequency cost nothing.
+uint64_t turns_of(double f) {
+  constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;   // 1 / (2 pi)
+  const double a = std::fabs(f), high = a * kHigh, low = std::fma(a, kHigh, -high) + a * kLow;
+  const double part = std::ldexp(high - std::floor(high), 64), whole = std::floor(part);   // exact
+  const uint64_t t = static_cast<uint64_t>(whole) + static_cast<uint64_t>(std::llround(part - whole + std::ldexp(low, 64)));
+  return f < 0 ? 0 - t : t;
+}
+
 // The most values that one access may take: of a run that starts at a multiple of half.
 int width(int half) { return half % 4 == 0 ? 4 : half % 2 == 0 ? 2 : 1; }
 
@@ -753,9 +765,7 @@ int normpre_qkrot_init(const normpre_qkrot_config* cfg, const double* frequencie
   p->half = cfg->rotary_dim / 2;
   for (int i = 0; i < p->half; ++i) {
     if (!(std::fabs(frequencies[i]) <= 1e6)) return fail(NORMPRE_ERR_ARG, "a frequency must be finite and at most 1e6 in absolute value");
-    double t = frequencies[i] * 0.15915494309189533577;   // 1 / (2 pi)
-    t -= std::floor(t);
-    p->turns[i] = t >= 1.0 ? 0 : static_cast<uint64_t>(std::ldexp(t, 64));
+    p->turns[i] = turns_of(frequencies[i]);
   }
   *out = p.release();
   return NORMPRE_OK;
