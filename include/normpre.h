@@ -393,7 +393,8 @@ typedef struct normpre_attn_config {
   float scale;         /* c, finite and > 0; 0 selects 1 / sqrt(head_dim) */
   int test_stall;      /* tests only, 0 otherwise.  1: one CTA of the BF16 forward pass issues no copies, so
                           that its bounded waits give up after about two seconds (TIMEOUT; the context stays
-                          usable) */
+                          usable).  2: one CTA of the BF16 backward pass's walk of dK and dV issues the copies
+                          of its first keys and values, but none of queries, with the same result */
 } normpre_attn_config;
 
 /* One [tokens][heads][head_dim] tensor on the device; the last dimension is

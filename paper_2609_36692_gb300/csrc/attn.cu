@@ -332,7 +332,7 @@ int normpre_attn_init_window(const normpre_attn_config* cfg, int64_t window, int
     return fail(NORMPRE_ERR_SHAPE, "max_tokens must be in [1, 2^24] and max_seqs in [1, 65536]");
   if (!std::isfinite(cfg->scale) || cfg->scale < 0.f) return fail(NORMPRE_ERR_ARG, "scale must be finite and >= 0");
   if (window < 0 || sinks < 0) return fail(NORMPRE_ERR_ARG, "window and sinks must be >= 0");
-  if (cfg->test_stall != 0 && cfg->test_stall != 1) return fail(NORMPRE_ERR_ARG, "test_stall must be 0 or 1");
+  if (cfg->test_stall < 0 || cfg->test_stall > 2) return fail(NORMPRE_ERR_ARG, "test_stall must be 0, 1 or 2");
   try {
     std::unique_ptr<normpre_attn, Release> a(new normpre_attn());
     a->cfg = *cfg;

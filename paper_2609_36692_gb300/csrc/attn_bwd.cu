@@ -351,6 +351,7 @@ __device__ __forceinline__ bool walk_dkdv(const BwdArgs& f, uint8_t* smem, uint3
       for (int64_t r = 0; w.ok && get(r, it); ++r, set.next()) {
         const int64_t row = it.start + static_cast<int64_t>(kTile) * it.blk;
         if (!w.load_own(own, kTileBytes, set.i, set.parity, &f.k, &f.v, row, it.head, kChunks)) break;
+        if (a.test_stall == 2 && blockIdx.x == 0) break;          // no queries: the others' waits run out
         for (int g = 0; g < a.group && w.ok; ++g)
           for (int i = it.first; i < it.end && w.ok; ++i) {
             const int64_t qrow = it.start + static_cast<int64_t>(kTile) * i;

@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_fwd_tc(const __grid_consta
       if (tc::elect_one()) {
         int slot = 0;
         uint32_t phase = 0, q_phase[2] = {0, 0};
-        const bool stall = f.a.test_stall && blockIdx.x == 0;   // nothing is loaded: the others' waits run out
+        const bool stall = f.a.test_stall == 1 && blockIdx.x == 0;   // nothing is loaded: the others' waits run out
         auto load = [&](const CUtensorMap* map, int64_t row, int head, bool tail) {
           ok = ok && tc::mbar_wait(&b->empty[slot], phase ^ 1u, &b->abort);
           if (!ok) return;
