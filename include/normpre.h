@@ -422,9 +422,13 @@ int normpre_attn_init(const normpre_attn_config* cfg, normpre_attn** out);
  * counted from the sequence's first).  window = 0: all rows up to i, as
  * normpre_attn_init; sinks then change nothing.  All other calls are the same.
  * The work grows with window + sinks instead of the sequence's length; with sinks
- * the plan's workspace has up to 64 MiB more.  A
- * non-finite value of token j reaches, besides the rows that see it, the rows of
- * every aligned block of 128 rows that has a row which sees one of j's block.
+ * the plan's workspace has up to 64 MiB more.
+ * What is not finite spreads by aligned blocks of 128 rows (0 * NaN in the tile
+ * products); a block of rows meets a block of keys if one of its rows sees one of
+ * those keys.  A key or value reaches o and dq of the rows of every block that meets
+ * its own.  q, do, o or lse of a row reach its own o and dq, and dk and dv of every
+ * key of the blocks that its block meets, seen by the row or not: with sinks, those
+ * of the first block, however far it is.
  * Errors: as normpre_attn_init; ARG for a negative window or sinks.
  */
 int normpre_attn_init_window(const normpre_attn_config* cfg, int64_t window, int64_t sinks, normpre_attn** out);
