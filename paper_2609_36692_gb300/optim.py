@@ -8,6 +8,7 @@ gradients before the step.
 """
 from __future__ import annotations
 
+import math
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -266,7 +267,8 @@ def clip_grads(grads, max_norm: float, eps: float = 1e-6, out=None):
     (``grad_norm``) before that.  In place, or into the tensors of ``out`` (their
     dtypes may differ: gradients summed in fp32, clipped ones in bf16 for the
     step).  In place nothing is written where the norm is below the limit.  A
-    tensor may be listed once only."""
+    tensor may be listed once only; all are fp32 or bf16, without gaps in their
+    memory, and on one device.  max_norm and eps must be finite and >= 0."""
     import torch
     grads = list(grads)
     if not grads:
@@ -293,11 +295,13 @@ def clip_grads(grads, max_norm: float, eps: float = 1e-6, out=None):
 def clip_grad_norm_(parameters, max_norm: float, eps: float = 1e-6):
     """Clips the gradients of parameters (or one) in place by their global norm,
     and returns it: ``clip_grads`` of their ``.grad``, between the backward pass
-    and the optimizers' steps."""
+    and the optimizers' steps.  max_norm infinite: the norm alone.  The gradients
+    must be on one device."""
     import torch
     if isinstance(parameters, torch.Tensor):
         parameters = [parameters]
-    return clip_grads([p.grad for p in parameters if p.grad is not None], max_norm, eps)
+    grads = [p.grad for p in parameters if p.grad is not None]
+    return grad_norm(grads) if max_norm == math.inf else clip_grads(grads, max_norm, eps)
 
 
 def newton_schulz(X, **config):

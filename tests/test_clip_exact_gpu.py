@@ -56,3 +56,20 @@ def test_in_place_each_value_once(dtype):
         assert bool((buf[1:-1].float() - want).abs().max() <= 2.0 ** -22 * want.max() + (2.0 ** -8 * want.max() if dtype == "bf16" else 0))
         assert float(buf[0]) == 1.0 == float(buf[-1])
         buf[1:-1] = 2.0 ** -(i + 1)
+
+
+def test_an_infinite_limit_asks_for_the_norm_alone():
+    import torch
+    from paper_2609_36692_gb300 import optim
+    p = [torch.nn.Parameter(torch.ones(n, device="cuda")) for n in (9, 16, 5)]
+    assert float(optim.clip_grad_norm_(p, math.inf)) == 0.0
+    p[0].grad, p[1].grad = (torch.full_like(x, y) for x, y in zip(p, (1.0, 2.5)))
+    p[0].grad[3] = 0.0
+    keep = [x.grad.clone() for x in p[:2]]
+    for limit in (math.inf, torch.tensor(math.inf)):
+        assert float(optim.clip_grad_norm_(p, limit)) == float(torch.tensor(math.sqrt(108.0), dtype=torch.float32))
+        assert all(torch.equal(x.grad, k) for x, k in zip(p, keep))
+    assert float(optim.clip_grad_norm_(p[0], math.inf)) == float(torch.tensor(math.sqrt(8.0), dtype=torch.float32))
+    for bad in (-math.inf, math.nan):
+        with pytest.raises(RuntimeError):
+            optim.clip_grad_norm_(p, bad)
