@@ -96,6 +96,16 @@ def _views(dtype: torch.dtype, dim: int, index: int, tokens: int, *views) -> arr
     return out
 
 
+def _remade(cls, made: dict, closed: bool, lengths: tuple = ()):
+    """A copy of a plan: another one of the library's, made from the same arguments."""
+    plan = cls(**made)
+    if lengths:
+        plan.set_lengths(lengths)
+    if closed:
+        plan.close()
+    return plan
+
+
 # ---------------------------------------------------------------------------
 # packed causal attention
 # ---------------------------------------------------------------------------
@@ -116,7 +126,8 @@ class PackedAttention:
     rows up to itself.
 
     A plan has one workspace for its backward passes: they run one after the
-    other, in whatever streams and graphs they are.
+    other, in whatever streams and graphs they are.  A copy (``copy``, ``pickle``)
+    is a plan of its own, with the same lengths.
 
     With `stream`, a call's work runs there instead of on the current stream;
     the caller orders it after what wrote its inputs and lengths, and before
@@ -132,9 +143,14 @@ class PackedAttention:
         if code is None:
             raise TypeError("unsupported dtype %s (float32 or bfloat16)" % dtype)
         self.plan, self.lengths = None, ()
+        self._made = dict(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, max_tokens=max_tokens, max_seqs=max_seqs,
+                          dtype=dtype, scale=scale, device=self.device, window=window, sinks=sinks)
         cfg = C.normpre_attn_config(n_heads, n_kv_heads, head_dim, max_seqs, max_tokens, code, scale)
         with torch.cuda.device(self.device):
             self.plan = C.normpre_attn_init_window(cfg, window, sinks)
+
+    def __reduce__(self):
+        return _remade, (type(self), self._made, not self.plan, self.lengths)
 
     def set_lengths(self, lengths: Sequence[int], stream=None) -> None:
         lengths = tuple(int(n) for n in lengths)
@@ -275,6 +291,11 @@ class QKNormRotary:
         cfg = C.normpre_qkrot_config(n_heads, n_kv_heads, head_dim, self.rotary_dim, int(interleaved), int(norm), code, eps)
         self.plan = C.normpre_qkrot_init(cfg, frequencies)
         self._bytes = C.normpre_qkrot_bytes(self.plan)
+        self._made = dict(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, rotary_dim=self.rotary_dim,
+                          interleaved=interleaved, eps=eps, norm=norm, dtype=dtype, frequencies=list(frequencies))
+
+    def __reduce__(self):
+        return _remade, (type(self), self._made, not self.plan)
 
     def _rest(self, positions, q_weight, k_weight, tokens, index):
         """Positions' pointer and bytes, weights' pointers and dtype code."""
@@ -403,6 +424,9 @@ class Checkpoint:
         self.tokens, self.features, self.dtype, self.device = tokens, features, dtype, device
         self.codes_ptr = self.data.data_ptr()
         self.steps_ptr = self.codes_ptr + codes
+
+    def __reduce__(self):
+        return Checkpoint, (self.tokens, self.features, self.dtype, self.device, self.data)
 
     @property
     def codes(self) -> torch.Tensor:
