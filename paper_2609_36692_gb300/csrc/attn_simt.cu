@@ -24,7 +24,7 @@
 // sequences, 12 heads of 64: forward 0.062 ms (14 TFLOP/s), backward 0.127 ms (16),
 // where the longest CTAs pass ten tiles of 8200 FMA cycles each, two CTAs an SM.
 // 8 x 1024 tokens: 0.39 ms (33 TFLOP/s) and 1.27 ms (25).  With a window of 100 and
-// 3 sinks the three sequences take 0.088 ms backward: 64 x 64 tiles of which 45 % is
+// 3 sinks the three sequences take 0.088 to 0.094 ms backward: 64 x 64 tiles of which 45 % is
 // visible, 600 CTAs of two to four tiles in two rounds.  Sinks take a fourth of a
 // tile's products where 16 keys or fewer are visible (forward, 2000 tokens 63 -> 55 us).
 #include <type_traits>
